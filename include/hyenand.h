@@ -265,6 +265,80 @@ int hyenand_synth_device_status(void);
 
 
 /*
+ * Gated linear recurrence, the other causal mixer of a sequence layer (1-D): the gates of the long convolution around a state
+ * with a decay per token instead of a fixed kernel.  For every batch entry and channel
+ *
+ *     s_t = a_t s_{t-1} + k_t v_t,    y_t = q_t s_t,    t = 0 .. L-1,
+ *     a_t = g_t (HYENAND_DECAY_VALUE)  |  exp(g_t) (HYENAND_DECAY_LOG)  |  1 / (1 + exp(-g_t)) (HYENAND_DECAY_SIGMOID)
+ *
+ * q, k, v, g, y: [B][C][L] of one dtype, DEVICE pointers, 16-byte aligned.  s0: the state before the row, [B][C] fp32, or NULL
+ * (zero).  lengths: [B] int32 on the device, or NULL: entry b holds lengths[b] positions (values outside 0 .. L count as the
+ * nearer of the two); the positions behind are not looked at, y is zero there and the state passes through.  s_end: the state
+ * behind the row, [B][C] fp32, or NULL; it may be the buffer s0.  marks: NULL, or B C hyenand_recurrence_marks(L) floats that the
+ * backward pass of the same inputs needs.
+ * Decays are meant to be at most 1 in size (g <= 0 for LOG); larger ones are taken, but products of many of them are formed, which
+ * can overflow where the state itself does not.  A state is fp32 and every value of y is rounded once, at its store.  A NaN or an
+ * infinity spreads to the later positions of its row.  Results do not depend on timing.
+ * Limits: L <= 2^30, B C <= 2^28.  No call allocates, synchronises or keeps anything; errors and stream as hyenand_forward_ex.
+ */
+enum { HYENAND_DECAY_VALUE = 0, HYENAND_DECAY_LOG = 1, HYENAND_DECAY_SIGMOID = 2 };
+long long hyenand_recurrence_marks(int L);        /* floats per row of marks; 0 for an L out of range */
+int hyenand_recurrence_forward(int B, int C, int L, int decay, int dtype, const void *q, const void *k, const void *v,
+                               const void *g, const float *s0, const int *lengths, void *y, float *s_end, float *marks,
+                               void *cuda_stream);
+/* The gradient, from marks of a forward call on the same q, k, v, g, s0 and lengths; with lam_t = q_t dy_t + a_{t+1} lam_{t+1}
+ * (at the last position ds_end in place of the second term):
+ *     dq = dy s,   dk = lam v,   dv = lam k,   dg_t = lam_t s_{t-1} da_t/dg_t,   ds0 = a_0 lam_0.
+ * dy: [B][C][L]; ds_end: [B][C] fp32 or NULL (zero).  dq, dk, dv, dg: [B][C][L], zero behind an entry's length; ds0: [B][C] fp32
+ * or NULL; it may be the buffer ds_end.  Each is rounded once, at its store. */
+int hyenand_recurrence_backward(int B, int C, int L, int decay, int dtype, const void *q, const void *k, const void *v,
+                                const void *g, const int *lengths, const float *marks, const void *dy, const float *ds_end,
+                                void *dq, void *dk, void *dv, void *dg, float *ds0, void *cuda_stream);
+/* One token, for generation: q, k, v, g, y are [B][C]; new_state (fp32 [B][C]) may be the buffer `state`.  active: [B] int32 on the
+ * device or NULL; an entry whose value is below 1 keeps its state and gets y = 0. */
+int hyenand_recurrence_step(int B, int C, int decay, int dtype, const void *q, const void *k, const void *v, const void *g,
+                            const float *state, const int *active, void *y, float *new_state, void *cuda_stream);
+
+/*
+ * What stands between two mixers of a residual stream x: the first one's output m normalised, gated, dropped out, scaled and
+ * added, the sum normalised for the next.  Per token (one of T grid positions of one batch entry), means over its C channels:
+ *
+ *     w = act(z) m / sqrt(mean(m^2) + eps) g_post      act: HYENAND_GATE_SIGMOID, HYENAND_GATE_SILU (z sigmoid(z)), or none
+ *     r = x + scale D w                                D: dropout factors, as hyenand_dropout over [B][C][T]
+ *     n = r / sqrt(mean(r^2) + eps) g_pre
+ *
+ * x, m, z, r, n: [B][C][T] of one dtype, DEVICE pointers, 16-byte aligned; z is NULL exactly where gate is HYENAND_GATE_NONE.
+ * g_post, scale, g_pre: C fp32 weights on the device; NULL leaves out the first norm, the scale, or n with its norm.  p = 0: no
+ * dropout, rng may be NULL.  stats: NULL, or 2 B T floats that the backward pass needs.  All arithmetic is fp32; n is formed
+ * before r is rounded.  eps > 0.  Errors and stream as hyenand_forward_ex; no call allocates, synchronises or keeps anything.
+ */
+enum { HYENAND_GATE_NONE = 0, HYENAND_GATE_SIGMOID = 1, HYENAND_GATE_SILU = 2 };
+int hyenand_block_forward(int B, int C, int T, int dtype, const void *x, const void *m, const void *z, const float *g_post,
+                          const float *scale, const float *g_pre, float eps, int gate, float p, const long long *rng, int site,
+                          void *r, void *n, float *stats, void *cuda_stream);
+/* The gradient: dr and dn (either may be NULL: zero; dn is given only with g_pre) in, dx, dm, dz ([B][C][T]) and the sums over all
+ * tokens dg_post, dscale, dg_pre (C fp32 each, or NULL) out.  The forward's inputs are read again, stats are the forward's (needed
+ * where a norm is).  workspace: hyenand_block_workspace_bytes() bytes on the device, whose contents mean nothing before and
+ * after; calls that may overlap need one each.  The sums are formed in an order that does not depend on timing. */
+int hyenand_block_backward(int B, int C, int T, int dtype, const void *x, const void *m, const void *z, const float *g_post,
+                           const float *scale, const float *g_pre, float eps, int gate, float p, const long long *rng, int site,
+                           const float *stats, const void *dr, const void *dn, void *dx, void *dm, void *dz, float *dg_post,
+                           float *dscale, float *dg_pre, void *workspace, void *cuda_stream);
+long long hyenand_block_workspace_bytes(int B, int C, int T, int dtype);
+
+/*
+ * Dropout whose mask is a function of counters and stored nowhere: y_i = x_i / (1 - p') or 0, for n elements; the backward pass is
+ * the same call on dy.  y may be the buffer x.  rng: two 64-bit words on the device, read when the kernel runs (so that a captured
+ * graph draws anew once they change): the seed, and a step, of which the low 32 bits count.  site tells apart the dropouts of one
+ * step.  The bits are Philox4x32-10 (Salmon, Moraes, Dror, Shaw, SC 2011) with key (seed low, seed high) and counter
+ * (i/8 low, i/8 high, step, site): element i takes 16 of the 128 bits, the low half of word 0 where i mod 8 is 0, its high half
+ * where it is 1, the low half of word 1 where it is 2, and so on.  It is dropped (zero, whatever it was) where they are below
+ * thr = min(65535, floor(65536 p + 1/2)); p' = thr / 65536.  0 <= p < 1.
+ */
+int hyenand_dropout(long long n, int dtype, const void *x, float p, const long long *rng, int site, void *y, void *cuda_stream);
+
+
+/*
  * Forward pass that allocates nothing (no counterpart in the paper: an integration aid).
  *
  * For callers that cannot allocate device memory when they need the operator -- host code running

@@ -25,8 +25,9 @@ DEBUG_FLAGS = ["-lineinfo", "--compress-mode=size", "-DHYENAND_DEBUG"]
 # --use_fast_math: approximate division and exponentials, subnormals flushed.  The transforms themselves use neither (their
 # twiddles come from tables computed in double on the host).  What does are the gates and norms of Eq. 2 (mixer.cu, and
 # mix_sigmoid inside fused2d.cu and slice_mix*.cu), at fp32 errors of a few 1e-7; 1 / (1 + exp(x)) is 0 above x = 87.3, where
-# it is below 2^-126.  Kernel synthesis, whose sines reach 30 radians and more, is compiled without it.
-PRECISE = {"synth.cu"}
+# it is below 2^-126.  Kernel synthesis, whose sines reach 30 radians and more, and the linear recurrence, whose decays are multiplied
+# up over thousands of positions, are compiled without it.
+PRECISE = {"synth.cu", "recurrence.cu"}
 
 
 def _sources():

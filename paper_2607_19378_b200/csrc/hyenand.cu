@@ -10,6 +10,7 @@
 
 #include "../../include/hyenand.h"
 #include "common.cuh"
+#include "entry.cuh"
 #include "ct1d.cuh"
 #include "planes.cuh"
 #include "core_tma.cuh"
@@ -26,7 +27,8 @@ using namespace hn;
 static thread_local char g_err[512] = "";
 static thread_local int g_code = 0;
 
-static int fail(int code, const char *fmt, ...)
+namespace hn {
+int fail(int code, const char *fmt, ...)
 {
     va_list ap;
     va_start(ap, fmt);
@@ -35,32 +37,8 @@ static int fail(int code, const char *fmt, ...)
     g_code = code;
     return code;
 }
-
-// Checked build: the address ranges a call may touch (the caller's tensors, the device allocations of the objects
-// involved), handed to every translation unit before the call's kernels are enqueued.
-struct DbgScope {
-#ifdef HYENAND_DEBUG
-    DbgRanges r;
-    DbgScope() { r.n = 0; }
-    void add(const void *ptr, size_t bytes)
-    {
-        if (ptr && bytes && r.n < kDbgRanges) { r.lo[r.n] = (unsigned long long)ptr; r.hi[r.n] = r.lo[r.n] + bytes; ++r.n; }
-    }
-    void add(const GuardedAllocs &g)
-    {
-        for (int i = 0; i < g.n; ++i) add(g.recs[i].base + kGuardBytes, g.recs[i].bytes);
-    }
-    void commit()
-    {
-        cudaDeviceSynchronize();               // kernels of earlier calls still compare against the previous list
-        dbg_set_ranges(r);
-    }
-#else
-    void add(const void *, size_t) {}
-    void add(const GuardedAllocs &) {}
-    void commit() {}
-#endif
-};
+void clear_error() { g_err[0] = 0; }
+}  // namespace hn
 
 extern "C" int hyenand_debug_build(void)
 {
@@ -199,7 +177,6 @@ static int len3_id(int need)
     return 0;
 }
 
-static size_t elsize(int dtype) { return dtype == HYENAND_F32 ? 4 : 2; }
 
 static int dev_alloc(hyenand_plan *p, void **ptr, size_t bytes, bool in_call = false)
 {

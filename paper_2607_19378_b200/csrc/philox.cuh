@@ -1,0 +1,57 @@
+// Philox4x32-10, the counter-based generator of Salmon, Moraes, Dror and Shaw, "Parallel random numbers: as easy as 1, 2, 3"
+// (SC 2011), as the dropout kernels use it (internal).  Ten rounds of two 32 x 32 -> 64 bit products on a counter of four words,
+// the two key words moved on by constants; every bit of the four output words is a random bit of (counter, key).
+#pragma once
+#include "common.cuh"
+
+namespace hn {
+
+struct DropArgs {
+    const long long *rng;     // device: [0] seed (the key), [1] step (counter word 2, its low 32 bits); nullptr: nothing is dropped
+    unsigned site;            // counter word 3: which dropout of a step
+    unsigned threshold;       // an element is dropped where its 16 bits are below
+    float scale;              // 65536 / (65536 - threshold): the kept elements
+};
+
+// false: p is not a probability below 1 (dropout.cu)
+bool drop_args(float p, const long long *rng, int site, DropArgs *d);
+
+// The factors of the eight elements [8 octet, 8 octet + 8) of a tensor, 16 bits each: low half of word 0, high half of word 0, ...
+struct DropKey {
+    unsigned k0, k1, step, site, threshold;
+    DropKey() = default;
+    __device__ __forceinline__ explicit DropKey(const DropArgs &d) : site(d.site), threshold(d.threshold)
+    {
+        HN_G(d.rng, 16);
+        const long long seed = __ldg(d.rng);
+        k0 = (unsigned)seed; k1 = (unsigned)((unsigned long long)seed >> 32);
+        step = (unsigned)__ldg(d.rng + 1);
+    }
+    __device__ __forceinline__ uint4 words(long long octet) const
+    {
+        unsigned c0 = (unsigned)octet, c1 = (unsigned)((unsigned long long)octet >> 32), c2 = step, c3 = site, a = k0, b = k1;
+#pragma unroll
+        for (int r = 0; r < 10; ++r) {
+            const unsigned long long p0 = (unsigned long long)c0 * 0xD2511F53u, p1 = (unsigned long long)c2 * 0xCD9E8D57u;
+            c0 = (unsigned)(p1 >> 32) ^ c1 ^ a; c1 = (unsigned)p1;
+            c2 = (unsigned)(p0 >> 32) ^ c3 ^ b; c3 = (unsigned)p0;
+            a += 0x9E3779B9u; b += 0xBB67AE85u;
+        }
+        return make_uint4(c0, c1, c2, c3);
+    }
+    // bit e set: element e of the octet stays
+    __device__ __forceinline__ unsigned keep(long long octet) const
+    {
+        const uint4 w = words(octet);
+        const unsigned v[4] = {w.x, w.y, w.z, w.w};
+        unsigned m = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if ((v[j] & 0xffffu) >= threshold) m |= 1u << (2 * j);
+            if ((v[j] >> 16) >= threshold) m |= 2u << (2 * j);
+        }
+        return m;
+    }
+};
+
+}  // namespace hn

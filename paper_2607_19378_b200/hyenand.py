@@ -7,8 +7,10 @@ library has not been built, loading raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import functools
+import math
 import os
 
 import torch
@@ -22,6 +24,12 @@ HYENAND_BF16 = 1
 HYENAND_MODE_LINEAR = 0
 HYENAND_MODE_CAUSAL = 1
 HYENAND_MODE_CIRCULAR = 2
+HYENAND_DECAY_VALUE = 0
+HYENAND_DECAY_LOG = 1
+HYENAND_DECAY_SIGMOID = 2
+HYENAND_GATE_NONE = 0
+HYENAND_GATE_SIGMOID = 1
+HYENAND_GATE_SILU = 2
 HYENAND_OK = 0
 HYENAND_ERR_INVALID_ARG = 1
 HYENAND_ERR_UNSUPPORTED = 2
@@ -99,6 +107,17 @@ def lib() -> ctypes.CDLL:
         L.hyenand_backward_destroy.restype = None
         L.hyenand_backward_destroy.argtypes = [vp]
         L.hyenand_synthesize_kernel.argtypes = [ctypes.c_int, ip] + [ctypes.c_int] * 5 + [vp] * 10 + [ctypes.c_int, vp, vp]
+        ci, cf = ctypes.c_int, ctypes.c_float
+        L.hyenand_recurrence_marks.restype = ll
+        L.hyenand_recurrence_marks.argtypes = [ci]
+        L.hyenand_recurrence_forward.argtypes = [ci] * 5 + [vp] * 10
+        L.hyenand_recurrence_backward.argtypes = [ci] * 5 + [vp] * 14
+        L.hyenand_recurrence_step.argtypes = [ci] * 4 + [vp] * 9
+        L.hyenand_block_workspace_bytes.restype = ll
+        L.hyenand_block_workspace_bytes.argtypes = [ci] * 4
+        L.hyenand_block_forward.argtypes = [ci] * 4 + [vp] * 6 + [cf, ci, cf, vp, ci] + [vp] * 4
+        L.hyenand_block_backward.argtypes = [ci] * 4 + [vp] * 6 + [cf, ci, cf, vp, ci] + [vp] * 11
+        L.hyenand_dropout.argtypes = [ll, ci, vp, cf, vp, ci, vp, vp]
         L.hyenand_plan_set_timing.argtypes = [vp, ctypes.c_int]
         L.hyenand_plan_kernel_time.argtypes = [vp, ctypes.c_int, dpp, dpp]
         _lib = L
@@ -335,6 +354,52 @@ def hyenand_backward_destroy(grad: int) -> None:
     lib().hyenand_backward_destroy(grad)
 
 
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def hyenand_recurrence_marks(L: int) -> int:
+    return int(lib().hyenand_recurrence_marks(int(L)))
+
+
+def hyenand_recurrence_forward(B: int, C: int, L: int, decay: int, dtype: int, q, k, v, g, s0, lengths, y, s_end, marks, stream=None) -> None:
+    _check(lib().hyenand_recurrence_forward(B, C, L, decay, dtype, q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), _ptr(s0),
+                                            _ptr(lengths), y.data_ptr(), _ptr(s_end), _ptr(marks), _stream_ptr(stream)))
+
+
+def hyenand_recurrence_backward(B: int, C: int, L: int, decay: int, dtype: int, q, k, v, g, lengths, marks, dy, ds_end, dq, dk, dv, dg, ds0,
+                                stream=None) -> None:
+    _check(lib().hyenand_recurrence_backward(B, C, L, decay, dtype, q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), _ptr(lengths),
+                                             marks.data_ptr(), dy.data_ptr(), _ptr(ds_end), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
+                                             dg.data_ptr(), _ptr(ds0), _stream_ptr(stream)))
+
+
+def hyenand_recurrence_step(B: int, C: int, decay: int, dtype: int, q, k, v, g, state, active, y, new_state, stream=None) -> None:
+    _check(lib().hyenand_recurrence_step(B, C, decay, dtype, q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), state.data_ptr(),
+                                         _ptr(active), y.data_ptr(), new_state.data_ptr(), _stream_ptr(stream)))
+
+
+def hyenand_block_workspace_bytes(B: int, C: int, T: int, dtype: int) -> int:
+    return int(lib().hyenand_block_workspace_bytes(B, C, T, dtype))
+
+
+def hyenand_block_forward(B: int, C: int, T: int, dtype: int, x, m, z, g_post, scale, g_pre, eps: float, gate: int, p: float, rng, site: int,
+                          r, n, stats, stream=None) -> None:
+    _check(lib().hyenand_block_forward(B, C, T, dtype, x.data_ptr(), m.data_ptr(), _ptr(z), _ptr(g_post), _ptr(scale), _ptr(g_pre), eps, gate,
+                                       p, _ptr(rng), site, r.data_ptr(), _ptr(n), _ptr(stats), _stream_ptr(stream)))
+
+
+def hyenand_block_backward(B: int, C: int, T: int, dtype: int, x, m, z, g_post, scale, g_pre, eps: float, gate: int, p: float, rng, site: int,
+                           stats, dr, dn, dx, dm, dz, dg_post, dscale, dg_pre, workspace, stream=None) -> None:
+    _check(lib().hyenand_block_backward(B, C, T, dtype, x.data_ptr(), m.data_ptr(), _ptr(z), _ptr(g_post), _ptr(scale), _ptr(g_pre), eps, gate,
+                                        p, _ptr(rng), site, _ptr(stats), _ptr(dr), _ptr(dn), dx.data_ptr(), dm.data_ptr(), _ptr(dz),
+                                        _ptr(dg_post), _ptr(dscale), _ptr(dg_pre), workspace.data_ptr(), _stream_ptr(stream)))
+
+
+def hyenand_dropout(n: int, dtype: int, x, p: float, rng, site: int, y, stream=None) -> None:
+    _check(lib().hyenand_dropout(n, dtype, x.data_ptr(), p, rng.data_ptr(), site, y.data_ptr(), _stream_ptr(stream)))
+
+
 def _check_tensors(tensors, dtype, what):
     for t in tensors:
         if not (t.is_cuda and t.is_contiguous() and t.dtype == dtype):
@@ -462,3 +527,134 @@ class Plan:
             self.close()
         except Exception:
             pass
+
+
+def _expect(device, shape, dtype, **tensors):
+    """Dense tensors of one shape and type on the current device; None passes."""
+    for name, t in tensors.items():
+        if t is not None and not (t.dtype == dtype and t.shape == shape and t.is_cuda and t.get_device() == device and t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on CUDA device {device} (the current one)")
+
+
+def _pool(stream):
+    """Outputs and workspaces belong to the stream that the kernels run on, as the allocator sees it."""
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream)))
+
+
+class Recurrence:
+    """The gated linear recurrence s_t = a_t s_{t-1} + k_t v_t, y_t = q_t s_t on [B, C, L], with a_t = g_t ("value"), exp(g_t)
+    ("log") or sigmoid(g_t) ("sigmoid").  Holds the shape only: every call stands for itself, on any stream."""
+
+    def __init__(self, L: int, B: int, C: int, decay: str = "log", dtype=torch.float32):
+        self.L, self.B, self.C, self.decay, self.dtype = int(L), int(B), int(C), decay, dtype
+        self._code = {"value": HYENAND_DECAY_VALUE, "log": HYENAND_DECAY_LOG, "sigmoid": HYENAND_DECAY_SIGMOID}[decay]
+        self._shape, self._states, self._marks = (self.B, self.C, self.L), (self.B, self.C), (self.B, self.C, hyenand_recurrence_marks(self.L))
+        if min(self.B, self.C, self._marks[2]) < 1:
+            raise ValueError("B and C must be >= 1, L between 1 and 2^30")
+        self._head = (self.B, self.C, self.L, self._code, _DTYPES[dtype])
+
+    def forward(self, q, k, v, g, s0=None, lengths=None, marks: bool = False, y=None, stream=None):
+        """(y, state behind the row), and with marks=True what `backward` needs of this call as a third."""
+        dev = torch.cuda.current_device()
+        _expect(dev, self._shape, self.dtype, q=q, k=k, v=v, g=g, y=y)
+        _expect(dev, self._states, torch.float32, s0=s0)
+        _expect(dev, (self.B,), torch.int32, lengths=lengths)
+        with _pool(stream):
+            if y is None:
+                y = torch.empty_like(q)
+            s_end = torch.empty(self._states, device=q.device)
+            m = torch.empty(self._marks, device=q.device) if marks else None
+        hyenand_recurrence_forward(*self._head, q, k, v, g, s0, lengths, y, s_end, m, stream)
+        return (y, s_end, m) if marks else (y, s_end)
+
+    def backward(self, q, k, v, g, marks, dy, ds_end=None, lengths=None, stream=None):
+        """dq, dk, dv, dg and ds0, from the marks of a forward call on the same q, k, v, g, s0 and lengths."""
+        dev = torch.cuda.current_device()
+        _expect(dev, self._shape, self.dtype, q=q, k=k, v=v, g=g, dy=dy)
+        _expect(dev, self._states, torch.float32, ds_end=ds_end)
+        _expect(dev, self._marks, torch.float32, marks=marks)
+        _expect(dev, (self.B,), torch.int32, lengths=lengths)
+        with _pool(stream):
+            dq, dk, dv, dg = torch.empty_like(q), torch.empty_like(q), torch.empty_like(q), torch.empty_like(q)
+            ds0 = torch.empty(self._states, device=q.device)
+        hyenand_recurrence_backward(*self._head, q, k, v, g, lengths, marks, dy, ds_end, dq, dk, dv, dg, ds0, stream)
+        return dq, dk, dv, dg, ds0
+
+    def step(self, q, k, v, g, state, new_state=None, active=None, y=None, stream=None):
+        """One token: q, k, v, g [B, C] -> y [B, C]; the state is replaced, or left and the new one written to new_state."""
+        dev = torch.cuda.current_device()
+        _expect(dev, self._states, self.dtype, q=q, k=k, v=v, g=g, y=y)
+        _expect(dev, self._states, torch.float32, state=state, new_state=new_state)
+        _expect(dev, (self.B,), torch.int32, active=active)
+        if y is None:
+            with _pool(stream):
+                y = torch.empty_like(q)
+        hyenand_recurrence_step(self.B, self.C, self._code, _DTYPES[self.dtype], q, k, v, g, state, active, y,
+                                state if new_state is None else new_state, stream)
+        return y
+
+
+class Block:
+    """Between two mixers of a residual stream: r = x + scale * dropout(act(z) * RMSNorm(m, g_post)), n = RMSNorm(r, g_pre), the norms
+    over the channels of each token of [B, C, L_1..L_N].  Weights that are not given leave their part out.  Holds the shape only."""
+
+    def __init__(self, dims, B: int, C: int, dtype=torch.float32, gate: str = "none", eps: float = 1e-6, p: float = 0.0, site: int = 0):
+        self.dims = tuple(int(d) for d in dims)
+        self.B, self.C, self.dtype, self.gate, self.eps, self.p, self.site = int(B), int(C), dtype, gate, float(eps), float(p), int(site)
+        self._gate = {"none": HYENAND_GATE_NONE, "sigmoid": HYENAND_GATE_SIGMOID, "silu": HYENAND_GATE_SILU}[gate]
+        self._shape, T = (self.B, self.C) + self.dims, math.prod(self.dims)
+        if min(self._shape) < 1:
+            raise ValueError("B, C and every extent must be >= 1")
+        self._head, self._stats = (self.B, self.C, T, _DTYPES[dtype]), (2, self.B, T)
+        self._workspace = hyenand_block_workspace_bytes(*self._head)
+
+    def _check(self, x, m, z, g_post, scale, g_pre, rng, **more):
+        dev = torch.cuda.current_device()
+        _expect(dev, self._shape, self.dtype, x=x, m=m, z=z, **more)
+        _expect(dev, (self.C,), torch.float32, g_post=g_post, scale=scale, g_pre=g_pre)
+        _expect(dev, (2,), torch.int64, rng=rng)
+        return dev
+
+    def forward(self, x, m, z=None, g_post=None, scale=None, g_pre=None, rng=None, stats: bool = False, stream=None):
+        """(r, n), n None without g_pre; with stats=True what `backward` needs of this call as a third."""
+        self._check(x, m, z, g_post, scale, g_pre, rng)
+        with _pool(stream):
+            r, n = torch.empty_like(x), torch.empty_like(x) if g_pre is not None else None
+            st = torch.empty(self._stats, device=x.device) if stats else None
+        hyenand_block_forward(*self._head, x, m, z, g_post, scale, g_pre, self.eps, self._gate, self.p, rng, self.site, r, n, st, stream)
+        return (r, n, st) if stats else (r, n)
+
+    def backward(self, x, m, stats, z=None, g_post=None, scale=None, g_pre=None, rng=None, dr=None, dn=None, stream=None):
+        """dx, dm, dz, dg_post, dscale, dg_pre (None for what was not given), from the stats of a forward call on the same inputs."""
+        dev = self._check(x, m, z, g_post, scale, g_pre, rng, dr=dr, dn=dn)
+        _expect(dev, self._stats, torch.float32, stats=stats)
+        with _pool(stream):
+            dx, dm, dz = torch.empty_like(x), torch.empty_like(x), torch.empty_like(x) if z is not None else None
+            weights = [None if t is None else torch.empty_like(t) for t in (g_post, scale, g_pre)]
+            work = torch.empty(self._workspace, dtype=torch.uint8, device=x.device)
+        hyenand_block_backward(*self._head, x, m, z, g_post, scale, g_pre, self.eps, self._gate, self.p, rng, self.site, stats, dr, dn,
+                               dx, dm, dz, *weights, work, stream)
+        return (dx, dm, dz, *weights)
+
+
+class Dropout:
+    """y = x / (1 - p) or 0, the mask drawn from rng (int64 [2] on the device: seed, step) and site; the backward pass is the same
+    call on dy."""
+
+    def __init__(self, p: float, site: int = 0):
+        self.p, self.site = float(p), int(site)
+
+    def __call__(self, x, rng, y=None, stream=None):
+        if x.dtype not in _DTYPES:
+            raise ValueError("x must be a float32 or bfloat16 tensor")
+        dev = torch.cuda.current_device()
+        _expect(dev, x.shape, x.dtype, x=x, y=y)
+        _expect(dev, (2,), torch.int64, rng=rng)
+        if y is None:
+            with _pool(stream):
+                y = torch.empty_like(x)
+        if x.numel():
+            hyenand_dropout(x.numel(), _DTYPES[x.dtype], x, self.p, rng, self.site, y, stream)
+        return y
