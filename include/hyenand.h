@@ -325,6 +325,10 @@ int hyenand_block_backward(int B, int C, int T, int dtype, const void *x, const 
                            const float *stats, const void *dr, const void *dn, void *dx, void *dm, void *dz, float *dg_post,
                            float *dscale, float *dg_pre, void *workspace, void *cuda_stream);
 long long hyenand_block_workspace_bytes(int B, int C, int T, int dtype);
+/* Channels that one CTA does not hold are shared by a cluster of them, which wait for one another's sums; every such wait is bounded.
+ * Returns 0, or 1 once one has given up since the library was loaded (the call that met it left its results incomplete), -1 if the
+ * word cannot be read.  Synchronises the device. */
+int hyenand_block_device_status(void);
 
 /*
  * Dropout whose mask is a function of counters and stored nowhere: y_i = x_i / (1 - p') or 0, for n elements; the backward pass is

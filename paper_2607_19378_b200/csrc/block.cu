@@ -15,35 +15,10 @@
 //
 // Any number of channels: a CTA takes a tile of neighbouring tokens, its warps share the channels, and what a second walk needs is
 // read again (from the caches).
+#include "block.cuh"
 #include "entry.cuh"
-#include "octet.cuh"
-#include "philox.cuh"
 
 namespace hn {
-
-enum { GATE_NONE = 0, GATE_SIGMOID = 1, GATE_SILU = 2 };
-
-struct BlockArgs {
-    const void *x, *m, *z, *dr, *dn;
-    const float *g_post, *scale, *g_pre;      // [C] or nullptr
-    float eps;
-    int gate;
-    DropArgs drop;
-    void *r, *n, *dx, *dm, *dz;
-    float *stats;                             // [2][B][T]: rho_m, rho_r
-    float *partial;                           // [slots][3][C]: dg_post, dscale, dg_pre
-    int B, C, T;
-    long long tiles;                          // of all batch entries
-    int tiles_b;                              // of one
-};
-
-// act(z) and act'(z); 1 - sigmoid is formed without cancellation
-__device__ __forceinline__ void gate_of(int kind, float z, float &a, float &da)
-{
-    const float e = __expf(-fabsf(z)), r = 1.f / (1.f + e), s = z >= 0.f ? r : e * r, t = z >= 0.f ? e * r : r;
-    if (kind == GATE_SILU) { a = z * s; da = s * fmaf(z, t, 1.f); }
-    else { a = s; da = s * t; }
-}
 
 // V neighbouring tokens of one channel (V = 4 only where 4 divides T)
 template <typename T, int V> __device__ __forceinline__ void ld_tokens(const void *p, long long i, float (&f)[V])
@@ -293,18 +268,39 @@ __global__ void __launch_bounds__(256) block_sum_kernel(const float *partial, in
     if (out) { HN_G(out + i % C, 4); out[i % C] = s; }
 }
 
-constexpr int kBlockSlots = 4 * kSms;
+// How the tile kernels take a shape: few channels in one CTA with wide tiles of tokens, more in a cluster.  false: more channels than
+// a cluster holds.
+static bool tile_shape(const BlockArgs &a, int dtype, bool backward, TileShape *s)
+{
+    int most = (backward ? kBackwardBytes : kForwardBytes) / (int)elsize(dtype);       // channels of a thread
+    if (!backward && a.T * elsize(dtype) % 16 && a.C <= kTileCtas * 16 * most) most /= 2;     // (rows with a piece more: two CTAs an SM all the same)
+    s->lt = a.C <= 8 * (most < 4 ? most : 4) ? 32 : 8;
+    const int rows = kTileThreads / s->lt;
+    s->ctas = (a.C + rows * most - 1) / (rows * most);
+    if (s->ctas > kTileCtas) return false;
+    const int each = ((a.C + s->ctas - 1) / s->ctas + rows - 1) / rows;
+    s->n = each <= 2 ? each : each <= 4 ? 4 : 8;
+    return true;
+}
 
+// workspace slots written, or -1
 static int block_launch(BlockArgs &a, int dtype, bool backward, cudaStream_t st)
 {
-    const int V = a.T % 4 == 0 ? 4 : 1;
-    a.tiles_b = (a.T + 32 * V - 1) / (32 * V);
+    TileShape s{};
+    if (tile_shape(a, dtype, backward, &s)) {
+        const int tokens = s.lt * V;
+        a.tiles_b = (a.T + tokens - 1) / tokens;
+        a.tiles = (long long)a.B * a.tiles_b;
+        return (backward ? launch_block_tile_backward : launch_block_tile_forward)(a, dtype, s, st);
+    }
+    const int tokens = a.T % 4 == 0 ? 4 : 1;
+    a.tiles_b = (a.T + 32 * tokens - 1) / (32 * tokens);
     a.tiles = (long long)a.B * a.tiles_b;
     const long long blocks = backward && a.tiles > kBlockSlots ? kBlockSlots : a.tiles;
     if (blocks > 0x7fffffffll) return -1;
 #define HN_BLK(T, V) launch_pdl(backward ? block_backward_kernel<T, V> : block_forward_kernel<T, V>, dim3((unsigned)blocks), kBlockWarps * 32, 0, st, a)
-    if (dtype == HYENAND_F32) { if (V == 4) HN_BLK(float, 4); else HN_BLK(float, 1); }
-    else { if (V == 4) HN_BLK(bf16, 4); else HN_BLK(bf16, 1); }
+    if (dtype == HYENAND_F32) { if (tokens == 4) HN_BLK(float, 4); else HN_BLK(float, 1); }
+    else { if (tokens == 4) HN_BLK(bf16, 4); else HN_BLK(bf16, 1); }
 #undef HN_BLK
     return (int)blocks;
 }
@@ -366,6 +362,13 @@ extern "C" long long hyenand_block_workspace_bytes(int B, int C, int T, int dtyp
 {
     (void)B; (void)T; (void)dtype;
     return C < 1 ? 0 : (long long)kBlockSlots * 3 * C * (long long)sizeof(float);
+}
+
+extern "C" int hyenand_block_device_status(void)
+{
+    if (cudaDeviceSynchronize() != cudaSuccess) return -1;
+    const int f = block_forward_status(), b = block_backward_status();
+    return f < 0 || b < 0 ? -1 : f | b;
 }
 
 extern "C" int hyenand_block_backward(int B, int C, int T, int dtype, const void *x, const void *m, const void *z, const float *g_post,

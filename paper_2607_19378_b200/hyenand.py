@@ -383,6 +383,10 @@ def hyenand_block_workspace_bytes(B: int, C: int, T: int, dtype: int) -> int:
     return int(lib().hyenand_block_workspace_bytes(B, C, T, dtype))
 
 
+def hyenand_block_device_status() -> int:
+    return int(lib().hyenand_block_device_status())
+
+
 def hyenand_block_forward(B: int, C: int, T: int, dtype: int, x, m, z, g_post, scale, g_pre, eps: float, gate: int, p: float, rng, site: int,
                           r, n, stats, stream=None) -> None:
     _check(lib().hyenand_block_forward(B, C, T, dtype, x.data_ptr(), m.data_ptr(), _ptr(z), _ptr(g_post), _ptr(scale), _ptr(g_pre), eps, gate,
