@@ -298,6 +298,10 @@ int hyenand_recurrence_backward(int B, int C, int L, int decay, int dtype, const
  * device or NULL; an entry whose value is below 1 keeps its state and gets y = 0. */
 int hyenand_recurrence_step(int B, int C, int decay, int dtype, const void *q, const void *k, const void *v, const void *g,
                             const float *state, const int *active, void *y, float *new_state, void *cuda_stream);
+/* Rows too few to fill the GPU are shared by clusters of CTAs, which wait for one another's states; every such wait is bounded.
+ * Returns 0, or 1 once one has given up since the library was loaded (the call that met it left its results incomplete), -1 if the
+ * word cannot be read.  Synchronises the device. */
+int hyenand_recurrence_device_status(void);
 
 /*
  * What stands between two mixers of a residual stream x: the first one's output m normalised, gated, dropped out, scaled and

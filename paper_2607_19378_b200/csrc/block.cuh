@@ -45,15 +45,14 @@ constexpr int kTileCtas = 8;                                 // of a cluster at 
 // N at most, times the element's bytes: two stages of a tile for two CTAs in an SM's shared memory
 constexpr int kForwardBytes = 16, kBackwardBytes = 8;
 
-// Two fp32 values in one instruction each.  They live in one 64-bit register pair from load to store: as struct members they would be
-// moved in front of every instruction.
-typedef unsigned long long f2;
-__device__ __forceinline__ f2 make2(float x, float y) { f2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y)); return r; }
-__device__ __forceinline__ void split2(f2 a, float &x, float &y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(a)); }
-__device__ __forceinline__ f2 pair(float x) { return make2(x, x); }
-__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) { f2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
-__device__ __forceinline__ f2 mul2(f2 a, f2 b) { f2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
-__device__ __forceinline__ f2 add2(f2 a, f2 b) { f2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+// two fp32 values in one instruction each
+typedef float2 f2;
+__device__ __forceinline__ f2 make2(float x, float y) { return make_float2(x, y); }
+__device__ __forceinline__ void split2(f2 a, float &x, float &y) { x = a.x; y = a.y; }
+__device__ __forceinline__ f2 pair(float x) { return make_float2(x, x); }
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) { return __ffma2_rn(a, b, c); }
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) { return __fmul2_rn(a, b); }
+__device__ __forceinline__ f2 add2(f2 a, f2 b) { return __fadd2_rn(a, b); }
 __device__ __forceinline__ float sum2(f2 a) { float x, y; split2(a, x, y); return x + y; }
 __device__ __forceinline__ f2 widen2(unsigned w) { return make2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
 __device__ __forceinline__ unsigned narrow2(f2 a) { float x, y; split2(a, x, y); return pack2(x, y); }
@@ -136,8 +135,8 @@ template <typename T, int LT, int N, int TENSORS, bool ALIGNED> struct Stage {
                 const uint2 w = reinterpret_cast<const uint2 *>(row)[tl];
                 f[0] = widen2(w.x); f[1] = widen2(w.y);
             } else {
-                const ulonglong2 w = reinterpret_cast<const ulonglong2 *>(row)[tl];
-                f[0] = w.x; f[1] = w.y;
+                const float4 w = reinterpret_cast<const float4 *>(row)[tl];
+                f[0] = make2(w.x, w.y); f[1] = make2(w.z, w.w);
             }
         } else {
             const int at = tl * V + ((int)start & (PER - 1));
@@ -167,7 +166,7 @@ template <typename T, bool ALIGNED> __device__ __forceinline__ void st_vector(vo
     if constexpr (ALIGNED) {                                 // (called with whole vectors only)
         HN_G(p, V * sizeof(T));
         if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2 *>(p) = make_uint2(narrow2(f[0]), narrow2(f[1]));
-        else *reinterpret_cast<ulonglong2 *>(p) = make_ulonglong2(f[0], f[1]);
+        else *reinterpret_cast<float4 *>(p) = make_float4(f[0].x, f[0].y, f[1].x, f[1].y);
     } else {
         float v[V];
         split2(f[0], v[0], v[1]); split2(f[1], v[2], v[3]);

@@ -75,7 +75,13 @@ template <typename T, int LT, int N, bool ALIGNED> __global__ void __launch_boun
         fetch(stages + (turn ^ 1) * St::BYTES, rho[turn ^ 1], ahead);
         const int t0 = here.r * TT, t = t0 + tl * V, count = p.T - t;
         const long long row0 = here.b * entry + first + t0;
-        auto token = [&](const float *v, int e) { return *reinterpret_cast<const f2 *>(v + tl * V + 2 * e); };
+        auto tokens = [&](const float *v, f2 (&f)[P]) {
+            const float4 w = *reinterpret_cast<const float4 *>(v + tl * V);
+            f[0] = make2(w.x, w.y); f[1] = make2(w.z, w.w);
+        };
+        f2 rm[P], rr[P], c1[P], c2[P];
+        tokens(rho[turn][0], rm);
+        tokens(rho[turn][1], rr);
         unsigned keep[N];
         if (drop) keep_bits<N>(key, p.T % 8 == 0, row0 + tl * V, hop, keep);
         // rho is kept out of the sums over channels: with k = scale D g_post act m,  x + rho_m k is r,  and with n' = rho_r dn,
@@ -106,8 +112,8 @@ template <typename T, int LT, int N, bool ALIGNED> __global__ void __launch_boun
                 St::get(stage, X, j, start, count, r);
 #pragma unroll
                 for (int e = 0; e < P; ++e) {
-                    r[e] = fma2(token(rho[turn][0], e), k[e], r[e]);
-                    n[e] = mul2(n[e], token(rho[turn][1], e));
+                    r[e] = fma2(rm[e], k[e], r[e]);
+                    n[e] = mul2(n[e], rr[e]);
                     local = fma2(n[e], r[e], local);
                     n[e] = mul2(n[e], pair(gn[j]));
                     s[0][e] = fma2(n[e], r[e], s[0][e]);
@@ -121,12 +127,14 @@ template <typename T, int LT, int N, bool ALIGNED> __global__ void __launch_boun
         }
         const float inv = 1.f / (float)p.C;
         sums.sum(s, ctas, rank, meeting & 1, meeting >> 1 & 1, [&](int k, const float (&a)[3]) {
-            const float rm = rho[turn][0][k], rr = rho[turn][1][k], c1 = a[0] * inv;
-            sums.total[0][k] = -rr * rr * c1;                                    // d = dr + g_pre n' - rho_r^2 c1 r
-            sums.total[1][k] = -rm * rm * (rm * (a[1] - rr * rr * c1 * a[2]) * inv);     // dm = rho_m (f - m^ c2)
+            const float om = rho[turn][0][k], on = rho[turn][1][k], mean = a[0] * inv;
+            sums.total[0][k] = -on * on * mean;                                    // d = dr + g_pre n' - rho_r^2 c1 r
+            sums.total[1][k] = -om * om * (om * (a[1] - on * on * mean * a[2]) * inv);     // dm = rho_m (f - m^ c2)
         });
         __syncthreads();
         if (sums.failed) break;
+        tokens(sums.total[0], c1);
+        tokens(sums.total[1], c2);
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             if (j * ROWS + row >= mine || count <= 0) continue;
@@ -154,23 +162,23 @@ template <typename T, int LT, int N, bool ALIGNED> __global__ void __launch_boun
                 if (drop) drop_pairs(keep[j], k);
 #pragma unroll
                 for (int e = 0; e < P; ++e) {
-                    r[e] = fma2(token(rho[turn][0], e), k[e], r[e]);
-                    d[e] = fma2(mul2(n[e], token(rho[turn][1], e)), pair(gn[j]), d[e]);
-                    d[e] = fma2(r[e], token(sums.total[0], e), d[e]);
+                    r[e] = fma2(rm[e], k[e], r[e]);
+                    d[e] = fma2(mul2(n[e], rr[e]), pair(gn[j]), d[e]);
+                    d[e] = fma2(r[e], c1[e], d[e]);
                 }
             }
             st_vector<T, ALIGNED>(p.dx, i, count, d);
             if (drop) drop_pairs(keep[j], d);
 #pragma unroll
             for (int e = 0; e < P; ++e) {
-                f2 q = mul2(d[e], token(rho[turn][0], e));
+                f2 q = mul2(d[e], rm[e]);
                 local = fma2(q, am[e], local);               // sum of keep d act m^: dg_post and dscale but for their constants
                 q = mul2(q, pair(w[j]));
                 if (p.z) {
                     da[e] = mul2(mul2(q, m[e]), da[e]);
                     q = mul2(q, a[e]);
                 }
-                d[e] = p.g_post ? fma2(m[e], token(sums.total[1], e), q) : q;
+                d[e] = p.g_post ? fma2(m[e], c2[e], q) : q;
             }
             acc[j][0] += sum2(local);
             st_vector<T, ALIGNED>(p.dm, i, count, d);

@@ -14,6 +14,7 @@
 
 #include "entry.cuh"
 #include "octet.cuh"
+#include "tma_util.cuh"
 
 namespace cg = cooperative_groups;
 
@@ -33,6 +34,8 @@ struct RecArgs {
     long long rows, n;                    // n = rows * L
     int C, L, marks_row;
 };
+
+static __device__ int hn_rec_status;                         // 1: a bounded wait gave up
 
 struct Map { float A, P, S; };            // s -> (1 + P) s + S, A = 1 + P
 __device__ __forceinline__ float apply(const Map &m, float s)
@@ -55,22 +58,35 @@ template <int DECAY, bool FAST> __device__ __forceinline__ void decay(float g, f
     }
 }
 
-// A row's live octet, positions [t0, t0 + 8): a, 1 - a, u for its live elements [lo, hi), the identity elsewhere; and A, P of the whole.
-template <int DECAY, bool FAST>
-__device__ __forceinline__ void decays(const float (&g)[8], int lo, int hi, float (&a)[8], float (&na)[8], float &A, float &P)
+// exp(x) - 1 for x <= 0, given exp(x): the series where they are close to 0 and 1 (its first term left out is below 2^-24 of it)
+__device__ __forceinline__ float expm1_of(float x, float ex)
+{
+    float p = 1.f / 40320.f;
+    p = fmaf(p, x, 1.f / 5040.f); p = fmaf(p, x, 1.f / 720.f); p = fmaf(p, x, 1.f / 120.f); p = fmaf(p, x, 1.f / 24.f);
+    p = fmaf(p, x, 1.f / 6.f); p = fmaf(p, x, 0.5f); p = fmaf(p, x, 1.f);
+    return x > -0.5f ? p * x : ex - 1.f;
+}
+
+// a and 1 - a of an octet's positions, and A, P of the whole.  Positions outside [lo, hi) are the identity: their gate is made one
+// that decays nothing before anything is computed (whatever was in them).
+template <int DECAY, bool FAST> __device__ __forceinline__ void decays(float (&g)[8], float (&a)[8], float (&na)[8], float &A, float &P)
 {
     A = 1.f; P = 0.f;
     float sum = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const bool in = e >= lo && e < hi;
         decay<DECAY, FAST>(g[e], a[e], na[e]);
-        if (!in) { a[e] = 1.f; na[e] = 0.f; }
         A *= a[e];
-        if constexpr (DECAY == DECAY_LOG) sum += in ? g[e] : 0.f;
+        if constexpr (DECAY == DECAY_LOG) sum += g[e];
         else P = fmaf(P, a[e], -na[e]);
     }
-    if constexpr (DECAY == DECAY_LOG) P = expm1f(sum);
+    if constexpr (DECAY == DECAY_LOG) P = expm1_of(sum, A);
+}
+template <int DECAY> __device__ __forceinline__ float no_decay() { return DECAY == DECAY_VALUE ? 1.f : DECAY == DECAY_LOG ? 0.f : __int_as_float(0x7f800000); }
+__device__ __forceinline__ void mask(float (&f)[8], int lo, int hi, float with)
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = e >= lo && e < hi ? f[e] : with;
 }
 
 // inclusive scan over the LANES lanes of a row towards higher (UP) or lower lanes
@@ -105,211 +121,343 @@ template <int LANES, int CL> struct RowLane {
     static constexpr int kSpan = LANES * CL;                         // octets of a tile
 };
 
-// From the maps of this thread's octets and the state that enters the tile: the state that enters the thread's octet, and `carry`
-// moved on to the one that leaves the tile.  Warps meet in slots[parity], which the caller alternates.
-template <int LANES, int CL, bool UP>
-__device__ __forceinline__ float enter(const Map &own, float &carry, Map (*slots)[RowLane<LANES, CL>::kWarps * CL])
-{
+// How the threads of a row learn the state that enters their octets.  The warps of a CTA leave their maps in shared memory; CTAs of a
+// cluster send each other theirs as asynchronous stores, counted by a barrier in the receiver's memory (a barrier of the whole
+// cluster would wait for the results of the last tile to reach memory too).  A slot is written again two tiles later: by then its
+// readers have left the barrier, or sent the map of the tile, between.
+template <int LANES, int CL> struct alignas(16) Meeting {
     using R = RowLane<LANES, CL>;
-    const int lane = threadIdx.x % R::kWarpLanes, warp = threadIdx.x / 32;
-    const Map inc = scan_lanes<R::kWarpLanes, UP>(own, lane);
-    const Map before = neighbour<R::kWarpLanes, UP>(inc, lane);
-    constexpr int last = UP ? R::kWarpLanes - 1 : 0;
-    if constexpr (LANES <= 32) {
-        const Map all = {__shfl_sync(~0u, inc.A, last, LANES), __shfl_sync(~0u, inc.P, last, LANES), __shfl_sync(~0u, inc.S, last, LANES)};
-        const float s = apply(before, carry);
-        carry = apply(all, carry);
-        return s;
-    } else {
-        constexpr int N = R::kWarps * CL;
-        int me = warp;
-        if constexpr (CL == 1) {
-            if (lane == last) slots[0][warp] = inc;
-            __syncthreads();
-        } else {
-            auto cluster = cg::this_cluster();
-            me += cluster.block_rank() * R::kWarps;
-            const Map all = {__shfl_sync(~0u, inc.A, last), __shfl_sync(~0u, inc.P, last), __shfl_sync(~0u, inc.S, last)};
-            if (lane < CL) cluster.map_shared_rank(&slots[0][0], lane)[me] = all;
-            cluster.sync();
-        }
-        float in = 0.f;
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int j = UP ? i : N - 1 - i;
-            if (j == me) in = carry;
-            carry = apply(slots[0][j], carry);
-        }
-        return apply(before, in);
+    float4 warp[2][R::kWarps];
+    float4 peers[2][CL];
+    uint64_t arrived[2];
+
+    __device__ __forceinline__ void init()
+    {
+        if (CL > 1 && threadIdx.x == 0) { mbar_init(&arrived[0], 1); mbar_init(&arrived[1], 1); fence_mbar_init(); }
     }
-}
+};
+template <int LANES, bool UP> struct Step {                   // one thread's part of a tile
+    static constexpr int W = LANES < 32 ? LANES : 32;
+    Map before;                                              // the octets of the warp in front of this thread's
+    Map all;                                                 // those of the whole warp (LANES <= 32: of the row)
+    __device__ __forceinline__ explicit Step(const Map &own)
+    {
+        const int lane = threadIdx.x % W;
+        constexpr int last = UP ? W - 1 : 0;
+        const Map inc = scan_lanes<W, UP>(own, lane);
+        before = neighbour<W, UP>(inc, lane);
+        if constexpr (LANES <= 32) all = {__shfl_sync(~0u, inc.A, last, W), __shfl_sync(~0u, inc.P, last, W), __shfl_sync(~0u, inc.S, last, W)};
+        else all = inc;                                      // (the last lane's)
+    }
+    // before the CTA's barrier
+    template <int CL> __device__ __forceinline__ void leave(Meeting<LANES, CL> &m, int count) const
+    {
+        if (LANES > 32 && threadIdx.x % 32 == (UP ? 31 : 0)) m.warp[count & 1][threadIdx.x / 32] = make_float4(all.A, all.P, all.S, 0.f);
+    }
+    // after it: the state in front of this thread's octet; carry moves on to the one behind the tile.  ok: no wait has given up yet
+    template <int CL> __device__ __forceinline__ float enter(Meeting<LANES, CL> &m, int count, int rank, float &carry, bool &ok) const
+    {
+        constexpr int NW = RowLane<LANES, CL>::kWarps;
+        if constexpr (LANES <= 32) {
+            const float s = apply(before, carry);
+            carry = apply(all, carry);
+            return s;
+        } else if constexpr (CL == 1) {
+            float in = 0.f;
+#pragma unroll
+            for (int i = 0; i < NW; ++i) {
+                const int j = UP ? i : NW - 1 - i;
+                if (j == (int)(threadIdx.x / 32)) in = carry;
+                const float4 w = m.warp[count & 1][j];
+                carry = apply({w.x, w.y, w.z}, carry);
+            }
+            return apply(before, in);
+        } else {
+            Map pre = {1.f, 0.f, 0.f}, tot = {1.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < NW; ++i) {
+                const int j = UP ? i : NW - 1 - i;
+                if (j == (int)(threadIdx.x / 32)) pre = tot;
+                const float4 w = m.warp[count & 1][j];
+                tot = compose(tot, {w.x, w.y, w.z});
+            }
+            if (threadIdx.x < 32) {
+                if (threadIdx.x == 0) mbar_expect_tx(&m.arrived[count & 1], CL * 16);
+                __syncwarp();
+                if (threadIdx.x < CL) {
+                    unsigned to, bar;
+                    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(smem_u32(&m.peers[count & 1][rank])), "r"((int)threadIdx.x));
+                    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(bar) : "r"(smem_u32(&m.arrived[count & 1])), "r"((int)threadIdx.x));
+                    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];\n"
+                                 ::"r"(to), "f"(tot.A), "f"(tot.P), "f"(tot.S), "f"(0.f), "r"(bar) : "memory");
+                }
+            }
+            if (ok) ok = mbar_wait(&m.arrived[count & 1], count >> 1 & 1);
+            float in = 0.f;
+#pragma unroll
+            for (int i = 0; i < CL; ++i) {
+                const int r = UP ? i : CL - 1 - i;
+                if (r == rank) in = carry;
+                const float4 w = m.peers[count & 1][r];
+                carry = apply({w.x, w.y, w.z}, carry);
+            }
+            return apply(before, apply(pre, in));
+        }
+    }
+};
+
+// A row as its threads see it.
+template <int LANES, int CL> struct Row {
+    using R = RowLane<LANES, CL>;
+    long long row, start;                                    // start: its first element
+    int l, lead, len, tiles, live;                           // this thread's octet of a tile; elements of the first octet in front of it
+    bool real;
+    __device__ __forceinline__ Row(const RecArgs &p, int rank)
+    {
+        row = (long long)(blockIdx.x / CL) * R::kRows + threadIdx.x / LANES;
+        real = row < p.rows;
+        l = threadIdx.x % LANES + rank * LANES;
+        len = real ? p.L : 0;
+        if (real && p.lengths) {
+            const int b = (int)(row / p.C);
+            HN_G(p.lengths + b, 4);
+            len = max(0, min(p.L, __ldg(p.lengths + b)));
+        }
+        start = real ? row * p.L : 0;
+        lead = (int)(start & 7);
+        tiles = (lead + p.L + 8 * R::kSpan - 1) / (8 * R::kSpan);
+        live = len ? (lead + len + 8 * R::kSpan - 1) / (8 * R::kSpan) : 0;
+    }
+};
+
+// A thread's octets.  Rows of several tiles (AHEAD): the next tile's travel into shared memory, each thread's into its own place, while
+// this one is worked on.
+template <typename T, int TENSORS, int THREADS, bool AHEAD> struct Octets {
+    static constexpr int HALVES = (int)sizeof(T) / 2, STAGE = AHEAD ? TENSORS * HALVES * THREADS * 16 : 0;
+    static __device__ __forceinline__ char *slot(char *stages, int turn, int tensor, int half) { return stages + turn * STAGE + ((tensor * HALVES + half) * THREADS + threadIdx.x) * 16; }
+    static __device__ __forceinline__ void fetch(char *stages, int turn, int tensor, const T *p, long long i, long long n)
+    {
+        const long long left = n - i;
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h) {
+            constexpr int E = 16 / (int)sizeof(T);
+            const long long have = left - h * E;
+            const int bytes = have >= E ? 16 : have > 0 ? (int)have * (int)sizeof(T) : 0;
+            const T *src = p + i + h * E;
+            if (bytes) HN_G(src, bytes);
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(smem_u32(slot(stages, turn, tensor, h))), "l"(bytes ? src : p), "r"(bytes) : "memory");
+        }
+    }
+    static __device__ __forceinline__ void get(char *stages, int turn, int tensor, const T *p, long long i, long long n, float (&f)[8])
+    {
+        Octet<T> o;
+        if constexpr (AHEAD) {
+            if constexpr (sizeof(T) == 2) o.w = *reinterpret_cast<const uint4 *>(slot(stages, turn, tensor, 0));
+            else { o.a = *reinterpret_cast<const float4 *>(slot(stages, turn, tensor, 0)); o.b = *reinterpret_cast<const float4 *>(slot(stages, turn, tensor, 1)); }
+        } else o.ld(p, i, n);
+        o.get(f);
+    }
+};
 
 template <typename T, int DECAY, int LANES, int CL>
-__global__ void __launch_bounds__(RowLane<LANES, CL>::kThreads) recurrence_forward_kernel(RecArgs p)
+__global__ void __launch_bounds__(RowLane<LANES, CL>::kThreads, LANES >= 128 ? 1024 / LANES : 8) recurrence_forward_kernel(RecArgs p)
 {
     using R = RowLane<LANES, CL>;
-    constexpr bool FAST = sizeof(T) == 2;
-    __shared__ Map slots[2][R::kWarps * CL];
+    constexpr bool FAST = sizeof(T) == 2, AHEAD = LANES >= 128;          // (shorter rows are one tile)
+    __shared__ Meeting<LANES, CL> meeting;
     const T *q = (const T *)p.q, *k = (const T *)p.k, *v = (const T *)p.v, *g = (const T *)p.g;
     T *y = (T *)p.y;
     pdl_join();
     int rank = 0;
     if constexpr (CL > 1) {
         rank = cg::this_cluster().block_rank();
-        cg::this_cluster().sync();                           // every CTA's slots exist before one is written
+        meeting.init();
+        cg::this_cluster().sync();                           // every CTA's barriers exist before something is sent to one
     }
-    const long long row = (long long)(blockIdx.x / CL) * R::kRows + threadIdx.x / LANES;
-    const bool real = row < p.rows;
-    const int l = threadIdx.x % LANES + rank * LANES;
-    int len = real ? p.L : 0;
-    if (real && p.lengths) {
-        const int b = (int)(row / p.C);
-        HN_G(p.lengths + b, 4);
-        len = max(0, min(p.L, __ldg(p.lengths + b)));
-    }
-    const long long start = real ? row * p.L : 0;
-    const int lead = (int)(start & 7);
+    const Row<LANES, CL> r(p, rank);
     float state = 0.f;
-    if (real && p.s0) { HN_G(p.s0 + row, 4); state = p.s0[row]; }
-    const int tiles = (lead + p.L + 8 * R::kSpan - 1) / (8 * R::kSpan);
-    const int live = len ? (lead + len + 8 * R::kSpan - 1) / (8 * R::kSpan) : 0;
-    for (int j = 0; j < tiles; ++j) {
-        const int oct = j * R::kSpan + l, t0 = oct * 8 - lead;
-        const long long i = start + t0;
-        const int lo = max(0, -t0), hi = min(8, len - t0), end = min(8, p.L - t0);
+    if (r.real && p.s0) { HN_G(p.s0 + r.row, 4); state = p.s0[r.row]; }
+    bool ok = true;                                          // no wait has given up
+    using Oct = Octets<T, 4, R::kThreads, AHEAD>;
+    extern __shared__ __align__(16) char stages[];
+    auto fetch = [&](int j, int turn) {
+        const int t0 = (j * R::kSpan + r.l) * 8 - r.lead;
+        if (t0 < r.len && t0 > -8) {
+            const long long i = r.start + t0;
+            Oct::fetch(stages, turn, 0, k, i, p.n); Oct::fetch(stages, turn, 1, v, i, p.n); Oct::fetch(stages, turn, 2, g, i, p.n); Oct::fetch(stages, turn, 3, q, i, p.n);
+        }
+        asm volatile("cp.async.commit_group;\n" ::: "memory");
+    };
+    if (AHEAD) fetch(0, 0);
+    for (int j = 0; j < r.tiles; ++j) {
+        const int oct = j * R::kSpan + r.l, t0 = oct * 8 - r.lead;
+        const long long i = r.start + t0;
+        const int lo = max(0, -t0), hi = min(8, r.len - t0), end = min(8, p.L - t0);
+        if (AHEAD) {
+            fetch(j + 1, (j + 1) & 1);
+            asm volatile("cp.async.wait_group 1;\n" ::: "memory");
+        }
         float out[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) out[e] = 0.f;
-        if (LANES <= 32 || j < live) {
-            Octet<T> rq, rk, rv, rg;
-            float a[8], na[8], u[8];
+        if (LANES <= 32 || j < r.live) {
+            float a[8], na[8], u[8], x[8];
             Map own = {1.f, 0.f, 0.f};
-            const bool some = lo < hi;
+            const bool some = lo < hi, whole = lo == 0 && hi == 8;
             if (some) {
-                rk.ld(k, i, p.n); rv.ld(v, i, p.n); rg.ld(g, i, p.n); rq.ld(q, i, p.n);
-                float x[8];
-                rk.get(u); rv.get(x);
+                Oct::get(stages, j & 1, 0, k, i, p.n, u); Oct::get(stages, j & 1, 1, v, i, p.n, x); Oct::get(stages, j & 1, 2, g, i, p.n, a);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) u[e] = e >= lo && e < hi ? u[e] * x[e] : 0.f;
-                rg.get(x);
-                decays<DECAY, FAST>(x, lo, hi, a, na, own.A, own.P);
+                for (int e = 0; e < 8; ++e) u[e] *= x[e];
+                if (!whole) { mask(u, lo, hi, 0.f); mask(a, lo, hi, no_decay<DECAY>()); }
+                float gate[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) gate[e] = a[e];
+                decays<DECAY, FAST>(gate, a, na, own.A, own.P);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) own.S = fmaf(a[e], own.S, u[e]);
             }
-            float s = enter<LANES, CL, true>(own, state, slots + (j & 1));
-            if (p.marks && real && oct % kMarkOctets == 0 && oct / kMarkOctets < p.marks_row) {
-                float *m = p.marks + row * p.marks_row + oct / kMarkOctets;
+            const Step<LANES, true> step(own);
+            if constexpr (LANES > 32) { step.leave(meeting, j); __syncthreads(); }
+            float s = step.enter(meeting, j, rank, state, ok);
+            if (p.marks && r.real && oct % kMarkOctets == 0 && oct / kMarkOctets < p.marks_row) {
+                float *m = p.marks + r.row * p.marks_row + oct / kMarkOctets;
                 HN_G(m, 4);
                 *m = s;
             }
             if (some) {
-                float x[8];
-                rq.get(x);
+                Oct::get(stages, j & 1, 3, q, i, p.n, x);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    s = fmaf(a[e], s, u[e]);
-                    out[e] = e >= lo && e < hi ? x[e] * s : 0.f;
-                }
+                for (int e = 0; e < 8; ++e) { s = fmaf(a[e], s, u[e]); out[e] = x[e] * s; }
+                if (!whole) mask(out, lo, hi, 0.f);
             }
+            if (r.real && lo < end) {
+                if (!some)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) out[e] = 0.f;
+                st_octet(y, i, lo, end, out);
+            }
+        } else if (r.real && lo < end) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) out[e] = 0.f;
+            st_octet(y, i, lo, end, out);
         }
-        if (real && lo < end) st_octet(y, i, lo, end, out);
     }
-    if (real && p.s_end && l == 0) { HN_G(p.s_end + row, 4); p.s_end[row] = state; }
+    if (r.real && p.s_end && r.l == 0) { HN_G(p.s_end + r.row, 4); p.s_end[r.row] = state; }
+    if constexpr (CL > 1) {
+        if (!ok) atomicExch(&hn_rec_status, 1);
+        cg::this_cluster().sync();                           // no CTA leaves while another may still send to it
+    }
 }
 
 template <typename T, int DECAY, int LANES, int CL>
-__global__ void __launch_bounds__(RowLane<LANES, CL>::kThreads) recurrence_backward_kernel(RecArgs p)
+__global__ void __launch_bounds__(RowLane<LANES, CL>::kThreads, LANES >= 128 ? 512 / LANES : 4) recurrence_backward_kernel(RecArgs p)
 {
     using R = RowLane<LANES, CL>;
-    constexpr bool FAST = sizeof(T) == 2;
-    __shared__ Map up[2][R::kWarps * CL], down[2][R::kWarps * CL];
+    constexpr bool FAST = sizeof(T) == 2, AHEAD = LANES >= 128;
+    __shared__ Meeting<LANES, 1> along;                      // the states, from each CTA's mark
+    __shared__ Meeting<LANES, CL> back;                      // the gradients of the states, from the row's end
     const T *q = (const T *)p.q, *k = (const T *)p.k, *v = (const T *)p.v, *g = (const T *)p.g, *dy = (const T *)p.dy;
     pdl_join();
     int rank = 0;
     if constexpr (CL > 1) {
         rank = cg::this_cluster().block_rank();
+        back.init();
         cg::this_cluster().sync();
     }
-    const long long row = (long long)(blockIdx.x / CL) * R::kRows + threadIdx.x / LANES;
-    const bool real = row < p.rows;
-    const int l = threadIdx.x % LANES + rank * LANES;
-    int len = real ? p.L : 0;
-    if (real && p.lengths) {
-        const int b = (int)(row / p.C);
-        HN_G(p.lengths + b, 4);
-        len = max(0, min(p.L, __ldg(p.lengths + b)));
-    }
-    const long long start = real ? row * p.L : 0;
-    const int lead = (int)(start & 7);
+    const Row<LANES, CL> r(p, rank);
     float mu = 0.f;                                          // a_{t+1} lam_{t+1} of the position behind the tile
-    if (real && p.ds_end) { HN_G(p.ds_end + row, 4); mu = __ldg(p.ds_end + row); }
-    const int tiles = (lead + p.L + 8 * R::kSpan - 1) / (8 * R::kSpan);
-    const int live = len ? (lead + len + 8 * R::kSpan - 1) / (8 * R::kSpan) : 0;
-    for (int j = tiles - 1; j >= 0; --j) {
-        const int oct = j * R::kSpan + l, t0 = oct * 8 - lead;
-        const long long i = start + t0;
-        const int lo = max(0, -t0), hi = min(8, len - t0), end = min(8, p.L - t0);
-        float oq[8], ok[8], ov[8], og[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) oq[e] = ok[e] = ov[e] = og[e] = 0.f;
-        if (LANES <= 32 || j < live) {
-            float a[8], na[8], w[8], xk[8], xv[8], xd[8];
-            Map own = {1.f, 0.f, 0.f}, back = {1.f, 0.f, 0.f};
-            const bool some = lo < hi;
-            float s = 0.f;
-            if (real && p.marks && oct / kMarkOctets < p.marks_row) {           // (every thread of a CTA reads its tile's mark)
-                const float *m = p.marks + row * p.marks_row + oct / kMarkOctets;
-                HN_G(m, 4);
-                s = __ldg(m);
-            }
+    if (r.real && p.ds_end) { HN_G(p.ds_end + r.row, 4); mu = __ldg(p.ds_end + r.row); }
+    bool ok = true;                                          // no wait has given up
+    using Oct = Octets<T, 5, R::kThreads, AHEAD>;
+    extern __shared__ __align__(16) char stages[];
+    auto mark_of = [&](int j) {                              // in front of this CTA's part of a tile, or of the row
+        const int mark = (j * R::kSpan + r.l - (LANES > kMarkOctets ? (int)threadIdx.x : 0)) / kMarkOctets;
+        if (j < 0 || !r.real || mark >= p.marks_row) return 0.f;
+        const float *m = p.marks + r.row * p.marks_row + mark;
+        HN_G(m, 4);
+        return __ldg(m);
+    };
+    auto fetch = [&](int j, int turn) {
+        const int t0 = (j * R::kSpan + r.l) * 8 - r.lead;
+        if (j >= 0 && t0 < r.len && t0 > -8) {
+            const long long i = r.start + t0;
+            Oct::fetch(stages, turn, 0, k, i, p.n); Oct::fetch(stages, turn, 1, v, i, p.n); Oct::fetch(stages, turn, 2, g, i, p.n); Oct::fetch(stages, turn, 3, q, i, p.n);
+            Oct::fetch(stages, turn, 4, dy, i, p.n);
+        }
+        asm volatile("cp.async.commit_group;\n" ::: "memory");
+    };
+    float mark = mark_of(r.tiles - 1);
+    if (AHEAD) fetch(r.tiles - 1, (r.tiles - 1) & 1);
+    for (int j = r.tiles - 1; j >= 0; --j) {
+        const int oct = j * R::kSpan + r.l, t0 = oct * 8 - r.lead, count = r.tiles - 1 - j;
+        const long long i = r.start + t0;
+        const int lo = max(0, -t0), hi = min(8, r.len - t0), end = min(8, p.L - t0);
+        const float from = mark;
+        if (AHEAD) {
+            fetch(j - 1, (j - 1) & 1);
+            mark = mark_of(j - 1);
+            asm volatile("cp.async.wait_group 1;\n" ::: "memory");
+        }
+        const bool some = lo < hi, whole = lo == 0 && hi == 8;
+        if (LANES <= 32 || j < r.live) {
+            const int met = LANES <= 32 ? count : r.live - 1 - j;
+            float a[8], na[8], w[8], xk[8], xv[8], xd[8], u[8];
+            Map own = {1.f, 0.f, 0.f}, rev = {1.f, 0.f, 0.f};
             if (some) {
-                Octet<T> rq, rk, rv, rg, rd;
-                rk.ld(k, i, p.n); rv.ld(v, i, p.n); rg.ld(g, i, p.n); rq.ld(q, i, p.n); rd.ld(dy, i, p.n);
-                float x[8];
-                rg.get(x);
-                decays<DECAY, FAST>(x, lo, hi, a, na, own.A, own.P);
-                back.A = own.A; back.P = own.P;
-                rk.get(xk); rv.get(xv); rq.get(w); rd.get(xd);
+                float gate[8];
+                Oct::get(stages, j & 1, 0, k, i, p.n, xk); Oct::get(stages, j & 1, 1, v, i, p.n, xv); Oct::get(stages, j & 1, 2, g, i, p.n, gate);
+                Oct::get(stages, j & 1, 3, q, i, p.n, w); Oct::get(stages, j & 1, 4, dy, i, p.n, xd);
+                if (!whole) { mask(gate, lo, hi, no_decay<DECAY>()); mask(xk, lo, hi, 0.f); mask(xv, lo, hi, 0.f); mask(w, lo, hi, 0.f); mask(xd, lo, hi, 0.f); }
+                decays<DECAY, FAST>(gate, a, na, own.A, own.P);
+                rev.A = own.A; rev.P = own.P;
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (e < lo || e >= hi) xk[e] = xv[e] = w[e] = xd[e] = 0.f;
+                for (int e = 0; e < 8; ++e) { u[e] = xk[e] * xv[e]; own.S = fmaf(a[e], own.S, u[e]); }
 #pragma unroll
-                for (int e = 0; e < 8; ++e) own.S = fmaf(a[e], own.S, xk[e] * xv[e]);
-#pragma unroll
-                for (int e = 7; e >= 0; --e) { w[e] *= xd[e]; back.S = a[e] * (w[e] + back.S); }
+                for (int e = 7; e >= 0; --e) { w[e] *= xd[e]; rev.S = a[e] * (w[e] + rev.S); }
             }
-            // the states from this CTA's mark, the gradients from the tile behind
-            float in = s;
-            s = enter<LANES, 1, true>(own, in, (Map(*)[RowLane<LANES, 1>::kWarps]) up[j & 1]);
-            float m = enter<LANES, CL, false>(back, mu, down + (j & 1));
+            const Step<LANES, true> ahead(own);
+            const Step<LANES, false> behind(rev);
+            if constexpr (LANES > 32) { ahead.leave(along, met); behind.leave(back, met); __syncthreads(); }
+            float in = from;
+            bool fine = true;
+            float s = ahead.enter(along, met, 0, in, fine);
+            float m = behind.enter(back, met, rank, mu, ok);
             if (some) {
-                float before[8];
+                float before[8], out[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     before[e] = s;
-                    s = fmaf(a[e], s, xk[e] * xv[e]);
-                    oq[e] = xd[e] * s;
+                    s = fmaf(a[e], s, u[e]);
+                    out[e] = xd[e] * s;
                 }
+                st_octet((T *)p.dq, i, lo, end, out);
 #pragma unroll
                 for (int e = 7; e >= 0; --e) {
                     const float lam = w[e] + m;
                     m = a[e] * lam;
-                    ok[e] = lam * xv[e];
-                    ov[e] = lam * xk[e];
-                    const float da = lam * before[e];
-                    og[e] = DECAY == DECAY_VALUE ? da : DECAY == DECAY_LOG ? da * a[e] : da * (a[e] * na[e]);
-                    if (e < lo || e >= hi) og[e] = 0.f;
+                    before[e] *= lam;
+                    if (DECAY == DECAY_LOG) before[e] *= a[e];
+                    if (DECAY == DECAY_SIGMOID) before[e] *= a[e] * na[e];
+                    out[e] = lam * xk[e];
+                    xv[e] *= lam;
                 }
+                if (!whole) mask(before, lo, hi, 0.f);
+                st_octet((T *)p.dk, i, lo, end, xv);
+                st_octet((T *)p.dv, i, lo, end, out);
+                st_octet((T *)p.dg, i, lo, end, before);
             }
         }
-        if (real && lo < end) {
-            st_octet((T *)p.dq, i, lo, end, oq);
-            st_octet((T *)p.dk, i, lo, end, ok);
-            st_octet((T *)p.dv, i, lo, end, ov);
-            st_octet((T *)p.dg, i, lo, end, og);
+        if (r.real && lo < end && !some) {
+            const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            st_octet((T *)p.dq, i, lo, end, zero);
+            st_octet((T *)p.dk, i, lo, end, zero);
+            st_octet((T *)p.dv, i, lo, end, zero);
+            st_octet((T *)p.dg, i, lo, end, zero);
         }
     }
-    if (real && p.ds0 && l == 0) { HN_G(p.ds0 + row, 4); p.ds0[row] = mu; }
+    if (r.real && p.ds0 && r.l == 0) { HN_G(p.ds0 + r.row, 4); p.ds0[r.row] = mu; }
+    if constexpr (CL > 1) {
+        if (!ok) atomicExch(&hn_rec_status, 1);
+        cg::this_cluster().sync();
+    }
 }
 
 // One token: a thread per channel.
@@ -336,38 +484,47 @@ template <typename T, int DECAY> __global__ void __launch_bounds__(256) recurren
     if (p.s_end) { HN_G(p.s_end + i, 4); p.s_end[i] = s; }
 }
 
-template <int LANES, int CL> static int launch_rows(void (*fn)(RecArgs), const RecArgs &a, cudaStream_t st)
+template <auto FN, int LANES, int CL, int BYTES> static int launch_rows(const RecArgs &a, cudaStream_t st)
 {
     using R = RowLane<LANES, CL>;
     const long long blocks = (a.rows + R::kRows - 1) / R::kRows * CL;
     if (blocks > 0x7fffffffll) return -1;
+    static DevOnce attr;
+    if (BYTES > 32 * 1024 && attr.first() && cudaFuncSetAttribute(FN, cudaFuncAttributeMaxDynamicSharedMemorySize, BYTES) != cudaSuccess) return -1;
     if constexpr (CL == 1) {
-        launch_pdl(fn, dim3((unsigned)blocks), R::kThreads, 0, st, a);
+        launch_pdl(FN, dim3((unsigned)blocks), R::kThreads, BYTES, st, a);
     } else {
         cudaLaunchConfig_t c{};
-        c.gridDim = dim3((unsigned)blocks); c.blockDim = dim3(R::kThreads); c.stream = st;
+        c.gridDim = dim3((unsigned)blocks); c.blockDim = dim3(R::kThreads); c.stream = st; c.dynamicSmemBytes = BYTES;
         cudaLaunchAttribute at;
         at.id = cudaLaunchAttributeClusterDimension;
         at.val.clusterDim.x = CL; at.val.clusterDim.y = 1; at.val.clusterDim.z = 1;
         c.attrs = &at; c.numAttrs = 1;
-        cudaLaunchKernelEx(&c, fn, a);
+        cudaLaunchKernelEx(&c, FN, a);
     }
     return 0;
 }
+template <typename T, int DECAY, bool BWD, int LANES, int CL> static int launch_lanes(const RecArgs &a, cudaStream_t st)
+{
+    constexpr int THREADS = RowLane<LANES, CL>::kThreads;
+    if constexpr (BWD) return launch_rows<recurrence_backward_kernel<T, DECAY, LANES, CL>, LANES, CL, 2 * Octets<T, 5, THREADS, (LANES >= 128)>::STAGE>(a, st);
+    else return launch_rows<recurrence_forward_kernel<T, DECAY, LANES, CL>, LANES, CL, 2 * Octets<T, 4, THREADS, (LANES >= 128)>::STAGE>(a, st);
+}
 
-// Lanes of a row: as few as hold it in one tile, a CTA that walks it where it is longer.  Rows fewer than four CTAs an SM are shared
+// Lanes of a row: as few as hold it in one tile, a CTA that walks it where it is longer.  Rows fewer than two CTAs an SM are shared
 // by a cluster.
 template <typename T, int DECAY, bool BWD> static int launch_recurrence_td(const RecArgs &a, cudaStream_t st)
 {
     const int octets = (a.L + (a.L % 8 ? 7 : 0) + 7) / 8;
-#define HN_REC(LANES, CL) return launch_rows<LANES, CL>(BWD ? recurrence_backward_kernel<T, DECAY, LANES, CL> : recurrence_forward_kernel<T, DECAY, LANES, CL>, a, st)
+#define HN_REC(LANES, CL) return launch_lanes<T, DECAY, BWD, LANES, CL>(a, st)
     if (octets <= 4) HN_REC(4, 1);
     if (octets <= 8) HN_REC(8, 1);
     if (octets <= 32) HN_REC(32, 1);
-    if (octets <= 128 || a.rows >= 4 * kSms) HN_REC(128, 1);
-    if (octets <= 256 || a.rows * 2 >= 4 * kSms) HN_REC(128, 2);
-    if (octets <= 512 || a.rows * 4 >= 4 * kSms) HN_REC(128, 4);
-    HN_REC(128, 8);
+    if (octets <= 128 || a.rows >= 8 * kSms) HN_REC(128, 1);
+    if (octets <= 256 || a.rows >= 2 * kSms) HN_REC(256, 1);
+    if (octets <= 512 || a.rows >= kSms) HN_REC(256, 2);
+    if (octets <= 1024 || a.rows * 2 >= kSms) HN_REC(256, 4);
+    HN_REC(256, 8);
 #undef HN_REC
 }
 
@@ -416,6 +573,13 @@ static int marks_of(int L) { return (int)(((long long)L + 7 + 8 * kMarkOctets - 
 using namespace hn;
 
 extern "C" long long hyenand_recurrence_marks(int L) { return L < 1 || L > (1 << 30) ? 0 : marks_of(L); }
+
+extern "C" int hyenand_recurrence_device_status(void)
+{
+    int v = 0;
+    if (cudaDeviceSynchronize() != cudaSuccess || cudaMemcpyFromSymbol(&v, hn_rec_status, sizeof(int)) != cudaSuccess) return -1;
+    return v;
+}
 
 extern "C" int hyenand_recurrence_forward(int B, int C, int L, int decay, int dtype, const void *q, const void *k, const void *v,
                                           const void *g, const float *s0, const int *lengths, void *y, float *s_end, float *marks,

@@ -362,6 +362,10 @@ def hyenand_recurrence_marks(L: int) -> int:
     return int(lib().hyenand_recurrence_marks(int(L)))
 
 
+def hyenand_recurrence_device_status() -> int:
+    return int(lib().hyenand_recurrence_device_status())
+
+
 def hyenand_recurrence_forward(B: int, C: int, L: int, decay: int, dtype: int, q, k, v, g, s0, lengths, y, s_end, marks, stream=None) -> None:
     _check(lib().hyenand_recurrence_forward(B, C, L, decay, dtype, q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), _ptr(s0),
                                             _ptr(lengths), y.data_ptr(), _ptr(s_end), _ptr(marks), _stream_ptr(stream)))
