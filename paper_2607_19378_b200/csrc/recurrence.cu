@@ -67,26 +67,25 @@ __device__ __forceinline__ float expm1_of(float x, float ex)
     return x > -0.5f ? p * x : ex - 1.f;
 }
 
-// a and 1 - a of an octet's positions, and A, P of the whole.  Positions outside [lo, hi) are the identity: their gate is made one
+// a and 1 - a of a thread's positions, and A, P of the whole.  Positions outside [lo, hi) are the identity: their gate is made one
 // that decays nothing before anything is computed (whatever was in them).
-template <int DECAY, bool FAST> __device__ __forceinline__ void decays(float (&g)[8], float (&a)[8], float (&na)[8], float &A, float &P)
+template <int DECAY, bool FAST, int E> __device__ __forceinline__ void decays(const float (&g)[E], float (&a)[E], float (&na)[E], float &A, float &P)
 {
     A = 1.f; P = 0.f;
     float sum = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
+    for (int e = 0; e < E; ++e) {
         decay<DECAY, FAST>(g[e], a[e], na[e]);
-        A *= a[e];
         if constexpr (DECAY == DECAY_LOG) sum += g[e];
-        else P = fmaf(P, a[e], -na[e]);
+        else { A *= a[e]; P = fmaf(P, a[e], -na[e]); }
     }
-    if constexpr (DECAY == DECAY_LOG) P = expm1_of(sum, A);
+    if constexpr (DECAY == DECAY_LOG) { A = FAST ? __expf(sum) : expf(sum); P = expm1_of(sum, A); }
 }
 template <int DECAY> __device__ __forceinline__ float no_decay() { return DECAY == DECAY_VALUE ? 1.f : DECAY == DECAY_LOG ? 0.f : __int_as_float(0x7f800000); }
-__device__ __forceinline__ void mask(float (&f)[8], int lo, int hi, float with)
+template <int E> __device__ __forceinline__ void mask(float (&f)[E], int lo, int hi, float with)
 {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = e >= lo && e < hi ? f[e] : with;
+    for (int e = 0; e < E; ++e) f[e] = e >= lo && e < hi ? f[e] : with;
 }
 
 // inclusive scan over the LANES lanes of a row towards higher (UP) or lower lanes
@@ -112,13 +111,14 @@ template <int LANES, bool UP> __device__ __forceinline__ Map neighbour(const Map
     return o;
 }
 
-// Where a thread stands: LANES lanes share a row (a part of a warp, or a CTA of LANES threads), CL CTAs in a row of tiles.
+// Where a thread stands: LANES lanes share a row (a part of a warp, or a CTA of LANES threads), CL CTAs in a row of tiles.  A thread
+// takes one octet, or in longer rows of bf16 two (OCT): what a tile costs besides its elements (the scans, half of all instructions
+// with one octet) is then a smaller part of what the memory allows.
 template <int LANES, int CL> struct RowLane {
     static constexpr int kThreads = LANES <= 32 ? 128 : LANES;
     static constexpr int kRows = LANES <= 32 ? kThreads / LANES : 1;
-    static constexpr int kWarpLanes = LANES < 32 ? LANES : 32;
     static constexpr int kWarps = LANES <= 32 ? 1 : LANES / 32;      // of one CTA, that share a row
-    static constexpr int kSpan = LANES * CL;                         // octets of a tile
+    static constexpr int kSpan = LANES * CL;                         // threads of a tile
 };
 
 // How the threads of a row learn the state that enters their octets.  The warps of a CTA leave their maps in shared memory; CTAs of a
@@ -130,6 +130,7 @@ template <int LANES, int CL> struct alignas(16) Meeting {
     float4 warp[2][R::kWarps];
     float4 peers[2][CL];
     uint64_t arrived[2];
+    float carry[2];                                          // CL == 1: the state behind a tile, left by the thread that forms it
 
     __device__ __forceinline__ void init()
     {
@@ -154,7 +155,8 @@ template <int LANES, bool UP> struct Step {                   // one thread's pa
     {
         if (LANES > 32 && threadIdx.x % 32 == (UP ? 31 : 0)) m.warp[count & 1][threadIdx.x / 32] = make_float4(all.A, all.P, all.S, 0.f);
     }
-    // after it: the state in front of this thread's octet; carry moves on to the one behind the tile.  ok: no wait has given up yet
+    // after it: the state in front of this thread's positions.  LANES <= 32 and CL > 1: carry moves on to the one behind the tile; else
+    // the thread that forms it stores it (Meeting::carry).  ok: no wait has given up yet
     template <int CL> __device__ __forceinline__ float enter(Meeting<LANES, CL> &m, int count, int rank, float &carry, bool &ok) const
     {
         constexpr int NW = RowLane<LANES, CL>::kWarps;
@@ -163,13 +165,13 @@ template <int LANES, bool UP> struct Step {                   // one thread's pa
             carry = apply(all, carry);
             return s;
         } else if constexpr (CL == 1) {
-            float in = 0.f;
+            float in = carry;
+            const int w = threadIdx.x / 32;
 #pragma unroll
-            for (int i = 0; i < NW; ++i) {
-                const int j = UP ? i : NW - 1 - i;
-                if (j == (int)(threadIdx.x / 32)) in = carry;
-                const float4 w = m.warp[count & 1][j];
-                carry = apply({w.x, w.y, w.z}, carry);
+            for (int i = 0; i < NW - 1; ++i) {
+                if (i >= (UP ? w : NW - 1 - w)) break;
+                const float4 f = m.warp[count & 1][UP ? i : NW - 1 - i];
+                in = apply({f.x, f.y, f.z}, in);
             }
             return apply(before, in);
         } else {
@@ -207,10 +209,11 @@ template <int LANES, bool UP> struct Step {                   // one thread's pa
 };
 
 // A row as its threads see it.
-template <int LANES, int CL> struct Row {
+template <int LANES, int CL, int E> struct Row {
     using R = RowLane<LANES, CL>;
+    static constexpr int kTile = E * R::kSpan;
     long long row, start;                                    // start: its first element
-    int l, lead, len, tiles, live;                           // this thread's octet of a tile; elements of the first octet in front of it
+    int l, lead, len, tiles, live;                           // this thread of a tile; elements of the row's first octet in front of it
     bool real;
     __device__ __forceinline__ Row(const RecArgs &p, int rank)
     {
@@ -225,46 +228,123 @@ template <int LANES, int CL> struct Row {
         }
         start = real ? row * p.L : 0;
         lead = (int)(start & 7);
-        tiles = (lead + p.L + 8 * R::kSpan - 1) / (8 * R::kSpan);
-        live = len ? (lead + len + 8 * R::kSpan - 1) / (8 * R::kSpan) : 0;
+        tiles = (lead + p.L + kTile - 1) / kTile;
+        live = len ? (lead + len + kTile - 1) / kTile : 0;
     }
 };
 
-// A thread's octets.  Rows of several tiles (AHEAD): the next tile's travel into shared memory, each thread's into its own place, while
-// this one is worked on.
-template <typename T, int TENSORS, int THREADS, bool AHEAD> struct Octets {
-    static constexpr int HALVES = (int)sizeof(T) / 2, STAGE = AHEAD ? TENSORS * HALVES * THREADS * 16 : 0;
-    static __device__ __forceinline__ char *slot(char *stages, int turn, int tensor, int half) { return stages + turn * STAGE + ((tensor * HALVES + half) * THREADS + threadIdx.x) * 16; }
-    static __device__ __forceinline__ void fetch(char *stages, int turn, int tensor, const T *p, long long i, long long n)
+// A thread's positions.  Rows of several tiles and of two octets a thread (STAGED) pass through shared memory, 32 bytes a thread and
+// tensor: a warp's 1024 of the next tile travel in as one bulk copy a tensor while this tile is worked on, results go out the same way.
+// (As 16-byte copies, each lane its own two: 404 and 697 us for 512 rows of 262144, bf16; neighbouring lanes neighbouring pieces:
+// 514 and 657, the addresses and conditions of sixteen copies being most of the instructions.)  Every warp has its own barriers.
+template <typename T, int OCT, int TENSORS, int THREADS, bool STAGED> struct Places {
+    static constexpr int E = 8 * OCT, STAGE = STAGED ? TENSORS * THREADS * 32 : 0;
+    static_assert(!STAGED || E * sizeof(T) == 32, "32 bytes a thread");
+    const T *in[TENSORS];
+    char *mine;                                              // this thread's place of tensor 0 in stage 0
+    uint64_t *bars;                                          // this warp's two
+    long long n;
+    int len, lane;
+    bool ok;                                                 // no wait has given up
+
+    __device__ __forceinline__ char *place(int turn, int tensor) const { return mine + turn * STAGE + tensor * THREADS * 32; }
+    __device__ __forceinline__ void init(char *stages, uint64_t *barriers, int row_len, long long elements)
     {
-        const long long left = n - i;
+        mine = stages + threadIdx.x * 32; bars = barriers + 2 * (threadIdx.x / 32); lane = threadIdx.x & 31;
+        len = row_len; n = elements; ok = true;
+        if (STAGED && lane == 0) { mbar_init(bars, 1); mbar_init(bars + 1, 1); fence_mbar_init(); }
+        __syncwarp();
+    }
+    // the positions of this warp, whose first is t of its row and element i of the tensor; by all its lanes.  Nothing is in the way: the
+    // lanes have read what was in this stage, and results that left from it have been read by their copies
+    __device__ __forceinline__ void fetch(int turn, long long i, int t) const
+    {
+        if (t >= len) return;
+        const long long last = i + min(32 * E, (len - t + 7) & ~7), end = last <= n ? last : n & ~7ll;        // whole octets of the tensor
+        if (lane == 0) {
+            const unsigned bytes = (unsigned)(end - i) * (unsigned)sizeof(T);
+            mbar_expect_tx(bars + turn, TENSORS * bytes);
+            if (bytes)
 #pragma unroll
-        for (int h = 0; h < HALVES; ++h) {
-            constexpr int E = 16 / (int)sizeof(T);
-            const long long have = left - h * E;
-            const int bytes = have >= E ? 16 : have > 0 ? (int)have * (int)sizeof(T) : 0;
-            const T *src = p + i + h * E;
-            if (bytes) HN_G(src, bytes);
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(smem_u32(slot(stages, turn, tensor, h))), "l"(bytes ? src : p), "r"(bytes) : "memory");
+                for (int k = 0; k < TENSORS; ++k) { HN_G(in[k] + i, bytes); bulk_load(place(turn, k), in[k] + i, bytes, bars + turn); }
+        }
+        if (last > n && end + lane < n)                      // (the octet that the tensor ends in)
+#pragma unroll
+            for (int k = 0; k < TENSORS; ++k) {
+                HN_G(in[k] + end + lane, sizeof(T));
+                reinterpret_cast<T *>(place(turn, k) - lane * 32)[end - i + lane] = in[k][end + lane];
+            }
+    }
+    __device__ __forceinline__ void wait(int turn, int phase, int t)
+    {
+        if (t < len && ok) ok = mbar_wait(bars + turn, phase);
+        __syncwarp();
+    }
+    // this thread's positions, the first at element i
+    __device__ __forceinline__ void get(int turn, int tensor, long long i, float (&f)[E]) const
+    {
+        Octet<T> w[OCT];
+        if constexpr (!STAGED) w[0].ld(in[tensor], i, n);
+        else if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int o = 0; o < OCT; ++o) w[o].w = reinterpret_cast<const uint4 *>(place(turn, tensor))[o];
+        } else {
+            w[0].a = reinterpret_cast<const float4 *>(place(turn, tensor))[0];
+            w[0].b = reinterpret_cast<const float4 *>(place(turn, tensor))[1];
+        }
+#pragma unroll
+        for (int o = 0; o < OCT; ++o) {
+            float x[8];
+            w[o].get(x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[8 * o + e] = x[e];
         }
     }
-    static __device__ __forceinline__ void get(char *stages, int turn, int tensor, const T *p, long long i, long long n, float (&f)[8])
+    // Results of the row's L positions; by all lanes of a warp at once, through the place of a tensor that nobody reads any more.
+    // t, i: as in fetch; t0, i0: this thread's first
+    __device__ __forceinline__ void put(int turn, int tensor, T *p, long long i, int t, long long i0, int t0, int L, const float (&f)[E]) const
     {
-        Octet<T> o;
-        if constexpr (AHEAD) {
-            if constexpr (sizeof(T) == 2) o.w = *reinterpret_cast<const uint4 *>(slot(stages, turn, tensor, 0));
-            else { o.a = *reinterpret_cast<const float4 *>(slot(stages, turn, tensor, 0)); o.b = *reinterpret_cast<const float4 *>(slot(stages, turn, tensor, 1)); }
-        } else o.ld(p, i, n);
-        o.get(f);
+        if constexpr (!STAGED) {
+            if (t0 < L && t0 > -8) st_octet(p, i0, max(0, -t0), min(8, L - t0), f);
+        } else {
+            uint4 *to = reinterpret_cast<uint4 *>(place(turn, tensor));
+#pragma unroll
+            for (int o = 0; o < 2; ++o) {
+                if constexpr (sizeof(T) == 2) to[o] = make_uint4(pack2(f[8 * o], f[8 * o + 1]), pack2(f[8 * o + 2], f[8 * o + 3]), pack2(f[8 * o + 4], f[8 * o + 5]), pack2(f[8 * o + 6], f[8 * o + 7]));
+                else to[o] = make_uint4(__float_as_uint(f[4 * o]), __float_as_uint(f[4 * o + 1]), __float_as_uint(f[4 * o + 2]), __float_as_uint(f[4 * o + 3]));
+            }
+            fence_async_smem();
+            __syncwarp();
+            const int from = t < 0 ? 8 : 0, whole = min(32 * E, (L - t) & ~7);         // octets that are the row's alone
+            if (lane == 0 && whole > from) {
+                HN_G(p + i + from, (whole - from) * sizeof(T));
+                bulk_store(p + i + from, place(turn, tensor) + from * sizeof(T), (whole - from) * sizeof(T));
+            }
+            // the octets that it shares with its neighbours
+            const T *base = reinterpret_cast<const T *>(place(turn, tensor) - lane * 32);
+            if (t < 0 && lane < 8 && t + lane >= 0 && t + lane < L) { HN_G(p + i + lane, sizeof(T)); p[i + lane] = base[lane]; }
+            const int rest = max(whole, from);
+            if (rest < 32 * E && t + rest + lane < L && lane < 8) { HN_G(p + i + rest + lane, sizeof(T)); p[i + rest + lane] = base[rest + lane]; }
+        }
+    }
+    __device__ __forceinline__ void put_done() const { if (STAGED && lane == 0) tma_commit(); }           // behind a tile's results
+    __device__ __forceinline__ void stage_free() const                                              // the last tile's results have left
+    {
+        if (STAGED && lane == 0) tma_wait_read0();
+        __syncwarp();
     }
 };
 
-template <typename T, int DECAY, int LANES, int CL>
-__global__ void __launch_bounds__(RowLane<LANES, CL>::kThreads, LANES >= 128 ? 1024 / LANES : 8) recurrence_forward_kernel(RecArgs p)
+template <typename T, int DECAY, int OCT, int LANES, int CL>
+__global__ void __launch_bounds__(RowLane<LANES, CL>::kThreads, LANES >= 128 ? 768 / LANES : LANES == 64 ? 12 : 6) recurrence_forward_kernel(RecArgs p)
 {
     using R = RowLane<LANES, CL>;
-    constexpr bool FAST = sizeof(T) == 2, AHEAD = LANES >= 128;          // (shorter rows are one tile)
+    constexpr int E = 8 * OCT;
+    constexpr bool FAST = sizeof(T) == 2, STAGED = LANES >= 128 || OCT == 2;         // (shorter rows are one tile)
+    using Pl = Places<T, OCT, 4, R::kThreads, STAGED>;
+    extern __shared__ __align__(16) char stages[];
     __shared__ Meeting<LANES, CL> meeting;
+    __shared__ uint64_t barriers[STAGED ? R::kThreads / 16 : 1];
     const T *q = (const T *)p.q, *k = (const T *)p.k, *v = (const T *)p.v, *g = (const T *)p.g;
     T *y = (T *)p.y;
     pdl_join();
@@ -274,85 +354,79 @@ __global__ void __launch_bounds__(RowLane<LANES, CL>::kThreads, LANES >= 128 ? 1
         meeting.init();
         cg::this_cluster().sync();                           // every CTA's barriers exist before something is sent to one
     }
-    const Row<LANES, CL> r(p, rank);
+    const Row<LANES, CL, E> r(p, rank);
     float state = 0.f;
     if (r.real && p.s0) { HN_G(p.s0 + r.row, 4); state = p.s0[r.row]; }
-    bool ok = true;                                          // no wait has given up
-    using Oct = Octets<T, 4, R::kThreads, AHEAD>;
-    extern __shared__ __align__(16) char stages[];
-    auto fetch = [&](int j, int turn) {
-        const int t0 = (j * R::kSpan + r.l) * 8 - r.lead;
-        if (t0 < r.len && t0 > -8) {
-            const long long i = r.start + t0;
-            Oct::fetch(stages, turn, 0, k, i, p.n); Oct::fetch(stages, turn, 1, v, i, p.n); Oct::fetch(stages, turn, 2, g, i, p.n); Oct::fetch(stages, turn, 3, q, i, p.n);
-        }
-        asm volatile("cp.async.commit_group;\n" ::: "memory");
-    };
-    if (AHEAD) fetch(0, 0);
+    Pl pl;
+    pl.in[0] = k; pl.in[1] = v; pl.in[2] = g; pl.in[3] = q;
+    pl.init(stages, barriers, r.len, p.n);
+    auto first = [&](int j) { return (j * R::kSpan + r.l - ((int)threadIdx.x & 31)) * E - r.lead; };       // position of this warp's first lane
+    if (STAGED) pl.fetch(0, r.start + first(0), first(0));
     for (int j = 0; j < r.tiles; ++j) {
-        const int oct = j * R::kSpan + r.l, t0 = oct * 8 - r.lead;
+        const int th = j * R::kSpan + r.l, t0 = th * E - r.lead;
         const long long i = r.start + t0;
-        const int lo = max(0, -t0), hi = min(8, r.len - t0), end = min(8, p.L - t0);
-        if (AHEAD) {
-            fetch(j + 1, (j + 1) & 1);
-            asm volatile("cp.async.wait_group 1;\n" ::: "memory");
+        const int lo = max(0, -t0), hi = min(E, r.len - t0);
+        if (STAGED) {
+            pl.stage_free();
+            if (j + 1 < r.tiles) pl.fetch((j + 1) & 1, r.start + first(j + 1), first(j + 1));
+            pl.wait(j & 1, j >> 1 & 1, first(j));
         }
-        float out[8];
+        const bool some = lo < hi, whole = lo == 0 && hi == E;
+        float out[E];
         if (LANES <= 32 || j < r.live) {
-            float a[8], na[8], u[8], x[8];
+            float a[E], u[E];
             Map own = {1.f, 0.f, 0.f};
-            const bool some = lo < hi, whole = lo == 0 && hi == 8;
             if (some) {
-                Oct::get(stages, j & 1, 0, k, i, p.n, u); Oct::get(stages, j & 1, 1, v, i, p.n, x); Oct::get(stages, j & 1, 2, g, i, p.n, a);
+                float x[E], na[E];
+                pl.get(j & 1, 0, i, u); pl.get(j & 1, 1, i, x);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) u[e] *= x[e];
-                if (!whole) { mask(u, lo, hi, 0.f); mask(a, lo, hi, no_decay<DECAY>()); }
-                float gate[8];
+                for (int e = 0; e < E; ++e) u[e] *= x[e];
+                pl.get(j & 1, 2, i, x);
+                if (!whole) { mask(u, lo, hi, 0.f); mask(x, lo, hi, no_decay<DECAY>()); }
+                decays<DECAY, FAST>(x, a, na, own.A, own.P);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) gate[e] = a[e];
-                decays<DECAY, FAST>(gate, a, na, own.A, own.P);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) own.S = fmaf(a[e], own.S, u[e]);
+                for (int e = 0; e < E; ++e) own.S = fmaf(a[e], own.S, u[e]);
             }
             const Step<LANES, true> step(own);
-            if constexpr (LANES > 32) { step.leave(meeting, j); __syncthreads(); }
-            float s = step.enter(meeting, j, rank, state, ok);
-            if (p.marks && r.real && oct % kMarkOctets == 0 && oct / kMarkOctets < p.marks_row) {
-                float *m = p.marks + r.row * p.marks_row + oct / kMarkOctets;
+            if constexpr (LANES > 32) {
+                step.leave(meeting, j);
+                __syncthreads();
+                if (CL == 1 && j) state = meeting.carry[(j - 1) & 1];
+            }
+            float s = step.enter(meeting, j, rank, state, pl.ok);
+            if (p.marks && r.real && th * OCT % kMarkOctets == 0 && th * OCT / kMarkOctets < p.marks_row) {
+                float *m = p.marks + r.row * p.marks_row + th * OCT / kMarkOctets;
                 HN_G(m, 4);
                 *m = s;
             }
             if (some) {
-                Oct::get(stages, j & 1, 3, q, i, p.n, x);
+                pl.get(j & 1, 3, i, out);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) { s = fmaf(a[e], s, u[e]); out[e] = x[e] * s; }
+                for (int e = 0; e < E; ++e) { s = fmaf(a[e], s, u[e]); out[e] *= s; }
                 if (!whole) mask(out, lo, hi, 0.f);
             }
-            if (r.real && lo < end) {
-                if (!some)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) out[e] = 0.f;
-                st_octet(y, i, lo, end, out);
-            }
-        } else if (r.real && lo < end) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) out[e] = 0.f;
-            st_octet(y, i, lo, end, out);
+            if (LANES > 32 && CL == 1 && threadIdx.x == LANES - 1) meeting.carry[j & 1] = state = s;
         }
+        if (!some) mask(out, 0, 0, 0.f);
+        if (r.real) pl.put(j & 1, 0, y, r.start + first(j), first(j), i, t0, p.L, out);
+        pl.put_done();
     }
-    if (r.real && p.s_end && r.l == 0) { HN_G(p.s_end + r.row, 4); p.s_end[r.row] = state; }
-    if constexpr (CL > 1) {
-        if (!ok) atomicExch(&hn_rec_status, 1);
-        cg::this_cluster().sync();                           // no CTA leaves while another may still send to it
-    }
+    if (r.real && p.s_end && r.l == (LANES > 32 && CL == 1 ? LANES - 1 : 0)) { HN_G(p.s_end + r.row, 4); p.s_end[r.row] = state; }
+    if (STAGED && pl.lane == 0) tma_wait_all0();
+    if (!pl.ok) atomicExch(&hn_rec_status, 1);
+    if constexpr (CL > 1) cg::this_cluster().sync();         // no CTA leaves while another may still send to it
 }
 
-template <typename T, int DECAY, int LANES, int CL>
-__global__ void __launch_bounds__(RowLane<LANES, CL>::kThreads, LANES >= 128 ? 512 / LANES : 4) recurrence_backward_kernel(RecArgs p)
+template <typename T, int DECAY, int OCT, int LANES, int CL>
+__global__ void __launch_bounds__(RowLane<LANES, CL>::kThreads, LANES >= 128 ? 512 / LANES : LANES == 64 ? 8 : 4) recurrence_backward_kernel(RecArgs p)
 {
     using R = RowLane<LANES, CL>;
-    constexpr bool FAST = sizeof(T) == 2, AHEAD = LANES >= 128;
+    constexpr int E = 8 * OCT;
+    constexpr bool FAST = sizeof(T) == 2, STAGED = LANES >= 128 || OCT == 2;
+    using Pl = Places<T, OCT, 5, R::kThreads, STAGED>;
+    extern __shared__ __align__(16) char stages[];
     __shared__ Meeting<LANES, 1> along;                      // the states, from each CTA's mark
+    __shared__ uint64_t barriers[STAGED ? R::kThreads / 16 : 1];
     __shared__ Meeting<LANES, CL> back;                      // the gradients of the states, from the row's end
     const T *q = (const T *)p.q, *k = (const T *)p.k, *v = (const T *)p.v, *g = (const T *)p.g, *dy = (const T *)p.dy;
     pdl_join();
@@ -362,102 +436,124 @@ __global__ void __launch_bounds__(RowLane<LANES, CL>::kThreads, LANES >= 128 ? 5
         back.init();
         cg::this_cluster().sync();
     }
-    const Row<LANES, CL> r(p, rank);
+    const Row<LANES, CL, E> r(p, rank);
     float mu = 0.f;                                          // a_{t+1} lam_{t+1} of the position behind the tile
     if (r.real && p.ds_end) { HN_G(p.ds_end + r.row, 4); mu = __ldg(p.ds_end + r.row); }
-    bool ok = true;                                          // no wait has given up
-    using Oct = Octets<T, 5, R::kThreads, AHEAD>;
-    extern __shared__ __align__(16) char stages[];
     auto mark_of = [&](int j) {                              // in front of this CTA's part of a tile, or of the row
-        const int mark = (j * R::kSpan + r.l - (LANES > kMarkOctets ? (int)threadIdx.x : 0)) / kMarkOctets;
+        const int mark = STAGED ? (j * R::kSpan + rank * LANES) * OCT / kMarkOctets : 0;
         if (j < 0 || !r.real || mark >= p.marks_row) return 0.f;
         const float *m = p.marks + r.row * p.marks_row + mark;
         HN_G(m, 4);
         return __ldg(m);
     };
-    auto fetch = [&](int j, int turn) {
-        const int t0 = (j * R::kSpan + r.l) * 8 - r.lead;
-        if (j >= 0 && t0 < r.len && t0 > -8) {
-            const long long i = r.start + t0;
-            Oct::fetch(stages, turn, 0, k, i, p.n); Oct::fetch(stages, turn, 1, v, i, p.n); Oct::fetch(stages, turn, 2, g, i, p.n); Oct::fetch(stages, turn, 3, q, i, p.n);
-            Oct::fetch(stages, turn, 4, dy, i, p.n);
-        }
-        asm volatile("cp.async.commit_group;\n" ::: "memory");
-    };
+    Pl pl;
+    pl.in[0] = k; pl.in[1] = v; pl.in[2] = g; pl.in[3] = q; pl.in[4] = dy;
+    pl.init(stages, barriers, r.len, p.n);
+    auto first = [&](int j) { return (j * R::kSpan + r.l - ((int)threadIdx.x & 31)) * E - r.lead; };       // position of this warp's first lane
     float mark = mark_of(r.tiles - 1);
-    if (AHEAD) fetch(r.tiles - 1, (r.tiles - 1) & 1);
+    int used[2] = {0, 0};                                    // copies waited for, of each stage
+    if (STAGED) pl.fetch((r.tiles - 1) & 1, r.start + first(r.tiles - 1), first(r.tiles - 1));
     for (int j = r.tiles - 1; j >= 0; --j) {
-        const int oct = j * R::kSpan + r.l, t0 = oct * 8 - r.lead, count = r.tiles - 1 - j;
+        const int t0 = (j * R::kSpan + r.l) * E - r.lead;
         const long long i = r.start + t0;
-        const int lo = max(0, -t0), hi = min(8, r.len - t0), end = min(8, p.L - t0);
-        const float from = mark;
-        if (AHEAD) {
-            fetch(j - 1, (j - 1) & 1);
+        const int lo = max(0, -t0), hi = min(E, r.len - t0);
+        float from = mark;
+        if (STAGED) {
+            pl.stage_free();
+            if (j) pl.fetch((j - 1) & 1, r.start + first(j - 1), first(j - 1));
             mark = mark_of(j - 1);
-            asm volatile("cp.async.wait_group 1;\n" ::: "memory");
+            pl.wait(j & 1, (j & 1 ? used[1] : used[0]) & 1, first(j));
+            if (first(j) < r.len) { if (j & 1) ++used[1]; else ++used[0]; }
         }
-        const bool some = lo < hi, whole = lo == 0 && hi == 8;
+        const bool some = lo < hi, whole = lo == 0 && hi == E;
         if (LANES <= 32 || j < r.live) {
-            const int met = LANES <= 32 ? count : r.live - 1 - j;
-            float a[8], na[8], w[8], xk[8], xv[8], xd[8], u[8];
+            const int met = LANES <= 32 ? 0 : r.live - 1 - j;
+            float a[E], na[E], w[E], u[E];
             Map own = {1.f, 0.f, 0.f}, rev = {1.f, 0.f, 0.f};
             if (some) {
-                float gate[8];
-                Oct::get(stages, j & 1, 0, k, i, p.n, xk); Oct::get(stages, j & 1, 1, v, i, p.n, xv); Oct::get(stages, j & 1, 2, g, i, p.n, gate);
-                Oct::get(stages, j & 1, 3, q, i, p.n, w); Oct::get(stages, j & 1, 4, dy, i, p.n, xd);
-                if (!whole) { mask(gate, lo, hi, no_decay<DECAY>()); mask(xk, lo, hi, 0.f); mask(xv, lo, hi, 0.f); mask(w, lo, hi, 0.f); mask(xd, lo, hi, 0.f); }
-                decays<DECAY, FAST>(gate, a, na, own.A, own.P);
+                float x[E];
+                pl.get(j & 1, 0, i, u); pl.get(j & 1, 1, i, x);
+#pragma unroll
+                for (int e = 0; e < E; ++e) u[e] *= x[e];
+                pl.get(j & 1, 3, i, w); pl.get(j & 1, 4, i, x);
+#pragma unroll
+                for (int e = 0; e < E; ++e) w[e] *= x[e];
+                pl.get(j & 1, 2, i, x);
+                if (!whole) { mask(u, lo, hi, 0.f); mask(w, lo, hi, 0.f); mask(x, lo, hi, no_decay<DECAY>()); }
+                decays<DECAY, FAST>(x, a, na, own.A, own.P);
                 rev.A = own.A; rev.P = own.P;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) { u[e] = xk[e] * xv[e]; own.S = fmaf(a[e], own.S, u[e]); }
+                for (int e = 0; e < E; ++e) own.S = fmaf(a[e], own.S, u[e]);
 #pragma unroll
-                for (int e = 7; e >= 0; --e) { w[e] *= xd[e]; rev.S = a[e] * (w[e] + rev.S); }
+                for (int e = E - 1; e >= 0; --e) rev.S = a[e] * (w[e] + rev.S);
             }
             const Step<LANES, true> ahead(own);
             const Step<LANES, false> behind(rev);
-            if constexpr (LANES > 32) { ahead.leave(along, met); behind.leave(back, met); __syncthreads(); }
-            float in = from;
-            bool fine = true;
-            float s = ahead.enter(along, met, 0, in, fine);
-            float m = behind.enter(back, met, rank, mu, ok);
-            if (some) {
-                float before[8], out[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    before[e] = s;
-                    s = fmaf(a[e], s, u[e]);
-                    out[e] = xd[e] * s;
-                }
-                st_octet((T *)p.dq, i, lo, end, out);
-#pragma unroll
-                for (int e = 7; e >= 0; --e) {
-                    const float lam = w[e] + m;
-                    m = a[e] * lam;
-                    before[e] *= lam;
-                    if (DECAY == DECAY_LOG) before[e] *= a[e];
-                    if (DECAY == DECAY_SIGMOID) before[e] *= a[e] * na[e];
-                    out[e] = lam * xk[e];
-                    xv[e] *= lam;
-                }
-                if (!whole) mask(before, lo, hi, 0.f);
-                st_octet((T *)p.dk, i, lo, end, xv);
-                st_octet((T *)p.dv, i, lo, end, out);
-                st_octet((T *)p.dg, i, lo, end, before);
+            if constexpr (LANES > 32) {
+                ahead.leave(along, met);
+                behind.leave(back, met);
+                __syncthreads();
+                if (CL == 1 && met) mu = back.carry[(met - 1) & 1];
             }
+            bool fine = true;
+            float s = ahead.enter(along, met, 0, from, fine);
+            float m = behind.enter(back, met, rank, mu, pl.ok);
+            auto put = [&](T *to, int place, float (&f)[E]) {
+                if (!whole) mask(f, lo, hi, 0.f);
+                if (r.real) pl.put(j & 1, place, to, r.start + first(j), first(j), i, t0, p.L, f);
+            };
+            // (lanes without a position take part in the stores and write zeros)
+            float x[E];
+            if (some) {
+                pl.get(j & 1, 4, i, x);
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const float now = fmaf(a[e], s, u[e]);
+                    u[e] = s;                                // from here the state in front of each position
+                    s = now;
+                    x[e] *= s;
+                }
+            }
+            put((T *)p.dq, 4, x);
+            if (some) {
+#pragma unroll
+                for (int e = E - 1; e >= 0; --e) {           // w: from here lam
+                    w[e] += m;
+                    m = a[e] * w[e];
+                    u[e] *= w[e];
+                    if (DECAY == DECAY_LOG) u[e] *= a[e];
+                    if (DECAY == DECAY_SIGMOID) u[e] *= a[e] * na[e];
+                }
+            }
+            put((T *)p.dg, 2, u);
+            if (some) {
+                pl.get(j & 1, 1, i, x);
+#pragma unroll
+                for (int e = 0; e < E; ++e) x[e] *= w[e];
+            }
+            put((T *)p.dk, 1, x);
+            if (some) {
+                pl.get(j & 1, 0, i, x);
+#pragma unroll
+                for (int e = 0; e < E; ++e) x[e] *= w[e];
+            }
+            put((T *)p.dv, 0, x);
+            if (LANES > 32 && CL == 1 && threadIdx.x == 0) back.carry[met & 1] = mu = m;
+        } else if (r.real) {
+            float zero[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) zero[e] = 0.f;
+            pl.put(j & 1, 4, (T *)p.dq, r.start + first(j), first(j), i, t0, p.L, zero);
+            pl.put(j & 1, 1, (T *)p.dk, r.start + first(j), first(j), i, t0, p.L, zero);
+            pl.put(j & 1, 0, (T *)p.dv, r.start + first(j), first(j), i, t0, p.L, zero);
+            pl.put(j & 1, 2, (T *)p.dg, r.start + first(j), first(j), i, t0, p.L, zero);
         }
-        if (r.real && lo < end && !some) {
-            const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            st_octet((T *)p.dq, i, lo, end, zero);
-            st_octet((T *)p.dk, i, lo, end, zero);
-            st_octet((T *)p.dv, i, lo, end, zero);
-            st_octet((T *)p.dg, i, lo, end, zero);
-        }
+        pl.put_done();
     }
     if (r.real && p.ds0 && r.l == 0) { HN_G(p.ds0 + r.row, 4); p.ds0[r.row] = mu; }
-    if constexpr (CL > 1) {
-        if (!ok) atomicExch(&hn_rec_status, 1);
-        cg::this_cluster().sync();
-    }
+    if (STAGED && pl.lane == 0) tma_wait_all0();
+    if (!pl.ok) atomicExch(&hn_rec_status, 1);
+    if constexpr (CL > 1) cg::this_cluster().sync();
 }
 
 // One token: a thread per channel.
@@ -504,27 +600,33 @@ template <auto FN, int LANES, int CL, int BYTES> static int launch_rows(const Re
     }
     return 0;
 }
-template <typename T, int DECAY, bool BWD, int LANES, int CL> static int launch_lanes(const RecArgs &a, cudaStream_t st)
+template <typename T, int DECAY, bool BWD, int OCT, int LANES, int CL> static int launch_lanes(const RecArgs &a, cudaStream_t st)
 {
     constexpr int THREADS = RowLane<LANES, CL>::kThreads;
-    if constexpr (BWD) return launch_rows<recurrence_backward_kernel<T, DECAY, LANES, CL>, LANES, CL, 2 * Octets<T, 5, THREADS, (LANES >= 128)>::STAGE>(a, st);
-    else return launch_rows<recurrence_forward_kernel<T, DECAY, LANES, CL>, LANES, CL, 2 * Octets<T, 4, THREADS, (LANES >= 128)>::STAGE>(a, st);
+    constexpr bool STAGED = LANES >= 128 || OCT == 2;
+    if constexpr (BWD) return launch_rows<recurrence_backward_kernel<T, DECAY, OCT, LANES, CL>, LANES, CL, 2 * Places<T, OCT, 5, THREADS, STAGED>::STAGE>(a, st);
+    else return launch_rows<recurrence_forward_kernel<T, DECAY, OCT, LANES, CL>, LANES, CL, 2 * Places<T, OCT, 4, THREADS, STAGED>::STAGE>(a, st);
 }
 
 // Lanes of a row: as few as hold it in one tile, a CTA that walks it where it is longer.  Rows fewer than two CTAs an SM are shared
 // by a cluster.
 template <typename T, int DECAY, bool BWD> static int launch_recurrence_td(const RecArgs &a, cudaStream_t st)
 {
-    const int octets = (a.L + (a.L % 8 ? 7 : 0) + 7) / 8;
-#define HN_REC(LANES, CL) return launch_lanes<T, DECAY, BWD, LANES, CL>(a, st)
-    if (octets <= 4) HN_REC(4, 1);
-    if (octets <= 8) HN_REC(8, 1);
-    if (octets <= 32) HN_REC(32, 1);
-    if (octets <= 128 || a.rows >= 8 * kSms) HN_REC(128, 1);
-    if (octets <= 256 || a.rows >= 2 * kSms) HN_REC(256, 1);
-    if (octets <= 512 || a.rows >= kSms) HN_REC(256, 2);
-    if (octets <= 1024 || a.rows * 2 >= kSms) HN_REC(256, 4);
-    HN_REC(256, 8);
+    constexpr int LONG = sizeof(T) == 2 ? 2 : 1;             // octets of a thread where a row is long
+    const int octets = (a.L + (a.L % 8 ? 7 : 0) + 7) / 8;    // that a row touches, wherever in one it starts
+#define HN_REC(OCT, LANES, CL) return launch_lanes<T, DECAY, BWD, OCT, LANES, CL>(a, st)
+    if (octets <= 4) HN_REC(1, 4, 1);
+    if (octets <= 8) HN_REC(1, 8, 1);
+    if (octets <= 16) HN_REC(1, 16, 1);
+    if (octets <= 32) HN_REC(1, 32, 1);
+    if (octets <= 64) HN_REC(1, 64, 1);
+    if constexpr (LONG == 2) if (octets <= 128) HN_REC(2, 64, 1);
+    const int threads = (octets + LONG - 1) / LONG;
+    if (threads <= 128 || a.rows >= 6 * kSms) HN_REC(LONG, 128, 1);
+    if (threads <= 256 || a.rows >= 2 * kSms) HN_REC(LONG, 256, 1);
+    if (threads <= 512 || a.rows >= kSms) HN_REC(LONG, 256, 2);
+    if (threads <= 1024 || a.rows * 2 >= kSms) HN_REC(LONG, 256, 4);
+    HN_REC(LONG, 256, 8);
 #undef HN_REC
 }
 

@@ -75,7 +75,7 @@ def check(B, C, L, dtype, decay, seed, ragged=False):
 # one position to several tiles; octets that rows share, tiles that end inside one, every number of lanes and of CTAs a row
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("decay", ["value", "log", "sigmoid"])
-@pytest.mark.parametrize("L", [1, 2, 7, 8, 25, 26, 57, 64, 65, 249, 256, 257, 1000, 1018, 1024, 1025, 3001])
+@pytest.mark.parametrize("L", [1, 2, 7, 8, 25, 26, 57, 58, 64, 65, 121, 122, 249, 256, 257, 505, 506, 1000, 1018, 1024, 1025, 2041, 2042, 2048, 3001, 4096, 4105])
 def test_lengths(L, decay, dtype):
     check(2, 5, L, dtype, decay, seed=L, ragged=False)
 
