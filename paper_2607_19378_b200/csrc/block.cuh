@@ -4,6 +4,7 @@
 
 #include "common.cuh"
 #include "octet.cuh"
+#include "pair.cuh"
 #include "philox.cuh"
 #include "tma_util.cuh"
 
@@ -45,19 +46,6 @@ constexpr int kTileCtas = 8;                                 // of a cluster at 
 // N at most, times the element's bytes: two stages of a tile for two CTAs in an SM's shared memory
 constexpr int kForwardBytes = 16, kBackwardBytes = 8;
 
-// two fp32 values in one instruction each
-typedef float2 f2;
-__device__ __forceinline__ f2 make2(float x, float y) { return make_float2(x, y); }
-__device__ __forceinline__ void split2(f2 a, float &x, float &y) { x = a.x; y = a.y; }
-__device__ __forceinline__ f2 pair(float x) { return make_float2(x, x); }
-__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) { return __ffma2_rn(a, b, c); }
-__device__ __forceinline__ f2 mul2(f2 a, f2 b) { return __fmul2_rn(a, b); }
-__device__ __forceinline__ f2 add2(f2 a, f2 b) { return __fadd2_rn(a, b); }
-__device__ __forceinline__ float sum2(f2 a) { float x, y; split2(a, x, y); return x + y; }
-__device__ __forceinline__ f2 widen2(unsigned w) { return make2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
-__device__ __forceinline__ unsigned narrow2(f2 a) { float x, y; split2(a, x, y); return pack2(x, y); }
-__device__ __forceinline__ float ex2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
-__device__ __forceinline__ float rcp(float x) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 
 constexpr int V = 4, P = V / 2;                              // tokens of a thread, and pairs of them
 

@@ -5,27 +5,40 @@
 // ten rounds for eight elements (16 random bits each).
 #include "entry.cuh"
 #include "octet.cuh"
+#include "pair.cuh"
 #include "philox.cuh"
 
 namespace hn {
 
-constexpr int kDropThreads = 256;
+constexpr int kDropThreads = 256, kDropCtas = 4;             // an SM holds
 
-template <typename T> __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const T *x, T *y, long long n, DropArgs d)
+template <typename T> __global__ void __launch_bounds__(kDropThreads, kDropCtas) dropout_kernel(const T *x, T *y, long long n, DropArgs d)
 {
+    constexpr int U = 8 / (int)sizeof(T);                    // octets of a thread on their way at once
     pdl_join();
     const DropKey key(d);
-    const long long octets = (n + 7) >> 3;
-    for (long long o = (long long)blockIdx.x * kDropThreads + threadIdx.x; o < octets; o += (long long)gridDim.x * kDropThreads) {
-        const long long i = o << 3;
-        Octet<T> raw;
-        raw.ld(x, i, n);
-        const unsigned keep = key.keep(o);
-        float f[8];
-        raw.get(f);
+    const long long octets = (n + 7) >> 3, stride = (long long)gridDim.x * kDropThreads;
+    for (long long o = (long long)blockIdx.x * kDropThreads + threadIdx.x; o < octets; o += U * stride) {
+        Octet<T> raw[U];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = keep >> e & 1 ? f[e] * d.scale : 0.f;       // (dropped: zero, whatever was there)
-        st_octet(y, i, 0, n - i < 8 ? (int)(n - i) : 8, f);
+        for (int u = 0; u < U; ++u)
+            if (o + u * stride < octets) raw[u].ld(x, (o + u * stride) << 3, n);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const long long at = o + u * stride, i = at << 3;
+            if (at >= octets) break;
+            const uint4 w = key.words(at);
+            float f[8];
+            raw[u].get(f);
+            const unsigned v[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {                    // (dropped: zero, whatever was there)
+                const f2 k = mul2(make2(f[2 * j], f[2 * j + 1]), pair(d.scale));
+                f[2 * j] = key.low(v[j]) ? k.x : 0.f;
+                f[2 * j + 1] = key.high(v[j]) ? k.y : 0.f;
+            }
+            st_octet(y, i, 0, n - i < 8 ? (int)(n - i) : 8, f);
+        }
     }
 }
 
@@ -58,7 +71,7 @@ extern "C" int hyenand_dropout(long long n, int dtype, const void *x, float p, c
     if (int e = c.check()) return e;
     c.register_ranges();
     const long long octets = (n + 7) / 8, blocks = (octets + kDropThreads - 1) / kDropThreads;
-    const dim3 grid((unsigned)(blocks < kSms * 8 ? blocks : kSms * 8));
+    const dim3 grid((unsigned)(blocks < kSms * kDropCtas ? blocks : kSms * kDropCtas));
     const cudaStream_t st = (cudaStream_t)cuda_stream;
     if (dtype == HYENAND_F32) launch_pdl(dropout_kernel<float>, grid, kDropThreads, 0, st, (const float *)x, (float *)y, n, d);
     else launch_pdl(dropout_kernel<bf16>, grid, kDropThreads, 0, st, (const bf16 *)x, (bf16 *)y, n, d);

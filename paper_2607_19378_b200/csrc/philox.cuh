@@ -18,9 +18,9 @@ bool drop_args(float p, const long long *rng, int site, DropArgs *d);
 
 // The factors of the eight elements [8 octet, 8 octet + 8) of a tensor, 16 bits each: low half of word 0, high half of word 0, ...
 struct DropKey {
-    unsigned k0, k1, step, site, threshold;
+    unsigned k0, k1, step, site, threshold;                  // threshold: in the upper half of the word
     DropKey() = default;
-    __device__ __forceinline__ explicit DropKey(const DropArgs &d) : site(d.site), threshold(d.threshold)
+    __device__ __forceinline__ explicit DropKey(const DropArgs &d) : site(d.site), threshold(d.threshold << 16)
     {
         HN_G(d.rng, 16);
         const long long seed = __ldg(d.rng);
@@ -29,16 +29,18 @@ struct DropKey {
     }
     __device__ __forceinline__ uint4 words(long long octet) const
     {
-        unsigned c0 = (unsigned)octet, c1 = (unsigned)((unsigned long long)octet >> 32), c2 = step, c3 = site, a = k0, b = k1;
+        unsigned c0 = (unsigned)octet, c1 = (unsigned)((unsigned long long)octet >> 32), c2 = step, c3 = site;
 #pragma unroll
-        for (int r = 0; r < 10; ++r) {
+        for (unsigned r = 0; r < 10; ++r) {                  // (where a thread works out many octets, the twenty key words stay in registers)
             const unsigned long long p0 = (unsigned long long)c0 * 0xD2511F53u, p1 = (unsigned long long)c2 * 0xCD9E8D57u;
-            c0 = (unsigned)(p1 >> 32) ^ c1 ^ a; c1 = (unsigned)p1;
-            c2 = (unsigned)(p0 >> 32) ^ c3 ^ b; c3 = (unsigned)p0;
-            a += 0x9E3779B9u; b += 0xBB67AE85u;
+            c0 = (unsigned)(p1 >> 32) ^ c1 ^ (k0 + r * 0x9E3779B9u); c1 = (unsigned)p1;
+            c2 = (unsigned)(p0 >> 32) ^ c3 ^ (k1 + r * 0xBB67AE85u); c3 = (unsigned)p0;
         }
         return make_uint4(c0, c1, c2, c3);
     }
+    // whether the element of a word's lower and of its upper half stays (an upper half is compared together with the lower: it decides)
+    __device__ __forceinline__ bool low(unsigned w) const { return w << 16 >= threshold; }
+    __device__ __forceinline__ bool high(unsigned w) const { return w >= threshold; }
     // bit e set: element e of the octet stays
     __device__ __forceinline__ unsigned keep(long long octet) const
     {
@@ -47,8 +49,8 @@ struct DropKey {
         unsigned m = 0;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            if ((v[j] & 0xffffu) >= threshold) m |= 1u << (2 * j);
-            if ((v[j] >> 16) >= threshold) m |= 2u << (2 * j);
+            if (low(v[j])) m |= 1u << (2 * j);
+            if (high(v[j])) m |= 2u << (2 * j);
         }
         return m;
     }

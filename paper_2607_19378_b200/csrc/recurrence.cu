@@ -14,6 +14,7 @@
 
 #include "entry.cuh"
 #include "octet.cuh"
+#include "pair.cuh"
 #include "tma_util.cuh"
 
 namespace cg = cooperative_groups;
@@ -69,23 +70,40 @@ __device__ __forceinline__ float expm1_of(float x, float ex)
 
 // a and 1 - a of a thread's positions, and A, P of the whole.  Positions outside [lo, hi) are the identity: their gate is made one
 // that decays nothing before anything is computed (whatever was in them).
-template <int DECAY, bool FAST, int E> __device__ __forceinline__ void decays(const float (&g)[E], float (&a)[E], float (&na)[E], float &A, float &P)
+template <int DECAY, bool FAST, int N> __device__ __forceinline__ void decays(const f2 (&g)[N], f2 (&a)[N], f2 (&na)[N], float &A, float &P)
 {
     A = 1.f; P = 0.f;
-    float sum = 0.f;
+    if constexpr (DECAY == DECAY_LOG) {
+        f2 sum = pair(0.f);
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-        decay<DECAY, FAST>(g[e], a[e], na[e]);
-        if constexpr (DECAY == DECAY_LOG) sum += g[e];
-        else { A *= a[e]; P = fmaf(P, a[e], -na[e]); }
+        for (int e = 0; e < N; ++e) {
+            if constexpr (FAST) {
+                const f2 y = mul2(g[e], pair(1.4426950408889634f));
+                a[e] = make2(ex2(y.x), ex2(y.y));
+            } else a[e] = make2(expf(g[e].x), expf(g[e].y));
+            sum = add2(sum, g[e]);
+        }
+        const float x = sum2(sum);
+        A = FAST ? __expf(x) : expf(x);
+        P = expm1_of(x, A);
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            decay<DECAY, FAST>(g[e].x, a[e].x, na[e].x);
+            decay<DECAY, FAST>(g[e].y, a[e].y, na[e].y);
+            A *= a[e].x * a[e].y;
+            P = fmaf(fmaf(P, a[e].x, -na[e].x), a[e].y, -na[e].y);
+        }
     }
-    if constexpr (DECAY == DECAY_LOG) { A = FAST ? __expf(sum) : expf(sum); P = expm1_of(sum, A); }
 }
 template <int DECAY> __device__ __forceinline__ float no_decay() { return DECAY == DECAY_VALUE ? 1.f : DECAY == DECAY_LOG ? 0.f : __int_as_float(0x7f800000); }
-template <int E> __device__ __forceinline__ void mask(float (&f)[E], int lo, int hi, float with)
+template <int N> __device__ __forceinline__ void mask(f2 (&f)[N], int lo, int hi, float with)
 {
 #pragma unroll
-    for (int e = 0; e < E; ++e) f[e] = e >= lo && e < hi ? f[e] : with;
+    for (int e = 0; e < N; ++e) {
+        if (2 * e < lo || 2 * e >= hi) f[e].x = with;
+        if (2 * e + 1 < lo || 2 * e + 1 >= hi) f[e].y = with;
+    }
 }
 
 // inclusive scan over the LANES lanes of a row towards higher (UP) or lower lanes
@@ -239,6 +257,7 @@ template <int LANES, int CL, int E> struct Row {
 // 514 and 657, the addresses and conditions of sixteen copies being most of the instructions.)  Every warp has its own barriers.
 template <typename T, int OCT, int TENSORS, int THREADS, bool STAGED> struct Places {
     static constexpr int E = 8 * OCT, STAGE = STAGED ? TENSORS * THREADS * 32 : 0;
+    static constexpr unsigned WARP_BYTES = 1024;
     static_assert(!STAGED || E * sizeof(T) == 32, "32 bytes a thread");
     const T *in[TENSORS];
     char *mine;                                              // this thread's place of tensor 0 in stage 0
@@ -259,17 +278,23 @@ template <typename T, int OCT, int TENSORS, int THREADS, bool STAGED> struct Pla
     // lanes have read what was in this stage, and results that left from it have been read by their copies
     __device__ __forceinline__ void fetch(int turn, long long i, int t) const
     {
+        if (t + 32 * E <= len) {                             // (what one lane does counts as much as what 32 do: few instructions here)
+            if (lane == 0) {
+                mbar_expect_tx(bars + turn, TENSORS * WARP_BYTES);
+#pragma unroll
+                for (int k = 0; k < TENSORS; ++k) { HN_G(in[k] + i, WARP_BYTES); bulk_load(place(turn, k), in[k] + i, WARP_BYTES, bars + turn); }
+            }
+            return;
+        }
         if (t >= len) return;
         const long long last = i + min(32 * E, (len - t + 7) & ~7), end = last <= n ? last : n & ~7ll;        // whole octets of the tensor
         if (lane == 0) {
             const unsigned bytes = (unsigned)(end - i) * (unsigned)sizeof(T);
             mbar_expect_tx(bars + turn, TENSORS * bytes);
             if (bytes)
-#pragma unroll
                 for (int k = 0; k < TENSORS; ++k) { HN_G(in[k] + i, bytes); bulk_load(place(turn, k), in[k] + i, bytes, bars + turn); }
         }
         if (last > n && end + lane < n)                      // (the octet that the tensor ends in)
-#pragma unroll
             for (int k = 0; k < TENSORS; ++k) {
                 HN_G(in[k] + end + lane, sizeof(T));
                 reinterpret_cast<T *>(place(turn, k) - lane * 32)[end - i + lane] = in[k][end + lane];
@@ -281,40 +306,45 @@ template <typename T, int OCT, int TENSORS, int THREADS, bool STAGED> struct Pla
         __syncwarp();
     }
     // this thread's positions, the first at element i
-    __device__ __forceinline__ void get(int turn, int tensor, long long i, float (&f)[E]) const
+    __device__ __forceinline__ void get(int turn, int tensor, long long i, f2 (&f)[E / 2]) const
     {
-        Octet<T> w[OCT];
-        if constexpr (!STAGED) w[0].ld(in[tensor], i, n);
-        else if constexpr (sizeof(T) == 2) {
+        if constexpr (sizeof(T) == 2) {
 #pragma unroll
-            for (int o = 0; o < OCT; ++o) w[o].w = reinterpret_cast<const uint4 *>(place(turn, tensor))[o];
+            for (int o = 0; o < OCT; ++o) {
+                uint4 w;
+                if constexpr (STAGED) w = reinterpret_cast<const uint4 *>(place(turn, tensor))[o];
+                else { Octet<T> x; x.ld(in[tensor], i, n); w = x.w; }
+                f[4 * o] = widen2(w.x); f[4 * o + 1] = widen2(w.y); f[4 * o + 2] = widen2(w.z); f[4 * o + 3] = widen2(w.w);
+            }
         } else {
-            w[0].a = reinterpret_cast<const float4 *>(place(turn, tensor))[0];
-            w[0].b = reinterpret_cast<const float4 *>(place(turn, tensor))[1];
-        }
-#pragma unroll
-        for (int o = 0; o < OCT; ++o) {
-            float x[8];
-            w[o].get(x);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) f[8 * o + e] = x[e];
+            float4 a, b;
+            if constexpr (STAGED) { a = reinterpret_cast<const float4 *>(place(turn, tensor))[0]; b = reinterpret_cast<const float4 *>(place(turn, tensor))[1]; }
+            else { Octet<T> x; x.ld(in[tensor], i, n); a = x.a; b = x.b; }
+            f[0] = make2(a.x, a.y); f[1] = make2(a.z, a.w); f[2] = make2(b.x, b.y); f[3] = make2(b.z, b.w);
         }
     }
     // Results of the row's L positions; by all lanes of a warp at once, through the place of a tensor that nobody reads any more.
     // t, i: as in fetch; t0, i0: this thread's first
-    __device__ __forceinline__ void put(int turn, int tensor, T *p, long long i, int t, long long i0, int t0, int L, const float (&f)[E]) const
+    __device__ __forceinline__ void put(int turn, int tensor, T *p, long long i, int t, long long i0, int t0, int L, const f2 (&f)[E / 2]) const
     {
         if constexpr (!STAGED) {
-            if (t0 < L && t0 > -8) st_octet(p, i0, max(0, -t0), min(8, L - t0), f);
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) split2(f[e], x[2 * e], x[2 * e + 1]);
+            if (t0 < L && t0 > -8) st_octet(p, i0, max(0, -t0), min(8, L - t0), x);
         } else {
             uint4 *to = reinterpret_cast<uint4 *>(place(turn, tensor));
 #pragma unroll
             for (int o = 0; o < 2; ++o) {
-                if constexpr (sizeof(T) == 2) to[o] = make_uint4(pack2(f[8 * o], f[8 * o + 1]), pack2(f[8 * o + 2], f[8 * o + 3]), pack2(f[8 * o + 4], f[8 * o + 5]), pack2(f[8 * o + 6], f[8 * o + 7]));
-                else to[o] = make_uint4(__float_as_uint(f[4 * o]), __float_as_uint(f[4 * o + 1]), __float_as_uint(f[4 * o + 2]), __float_as_uint(f[4 * o + 3]));
+                if constexpr (sizeof(T) == 2) to[o] = make_uint4(narrow2(f[4 * o]), narrow2(f[4 * o + 1]), narrow2(f[4 * o + 2]), narrow2(f[4 * o + 3]));
+                else reinterpret_cast<float4 *>(to)[o] = make_float4(f[2 * o].x, f[2 * o].y, f[2 * o + 1].x, f[2 * o + 1].y);
             }
             fence_async_smem();
             __syncwarp();
+            if (t >= 0 && t + 32 * E <= L) {
+                if (lane == 0) { HN_G(p + i, WARP_BYTES); bulk_store(p + i, place(turn, tensor), WARP_BYTES); }
+                return;
+            }
             const int from = t < 0 ? 8 : 0, whole = min(32 * E, (L - t) & ~7);         // octets that are the row's alone
             if (lane == 0 && whole > from) {
                 HN_G(p + i + from, (whole - from) * sizeof(T));
@@ -336,10 +366,10 @@ template <typename T, int OCT, int TENSORS, int THREADS, bool STAGED> struct Pla
 };
 
 template <typename T, int DECAY, int OCT, int LANES, int CL>
-__global__ void __launch_bounds__(RowLane<LANES, CL>::kThreads, LANES >= 128 ? 768 / LANES : LANES == 64 ? 12 : 6) recurrence_forward_kernel(RecArgs p)
+__global__ void __launch_bounds__(RowLane<LANES, CL>::kThreads, LANES > 32 ? 768 / LANES : 6) recurrence_forward_kernel(RecArgs p)
 {
     using R = RowLane<LANES, CL>;
-    constexpr int E = 8 * OCT;
+    constexpr int E = 8 * OCT, N = E / 2;
     constexpr bool FAST = sizeof(T) == 2, STAGED = LANES >= 128 || OCT == 2;         // (shorter rows are one tile)
     using Pl = Places<T, OCT, 4, R::kThreads, STAGED>;
     extern __shared__ __align__(16) char stages[];
@@ -372,20 +402,20 @@ __global__ void __launch_bounds__(RowLane<LANES, CL>::kThreads, LANES >= 128 ? 7
             pl.wait(j & 1, j >> 1 & 1, first(j));
         }
         const bool some = lo < hi, whole = lo == 0 && hi == E;
-        float out[E];
+        f2 out[N];
         if (LANES <= 32 || j < r.live) {
-            float a[E], u[E];
+            f2 a[N], u[N];
             Map own = {1.f, 0.f, 0.f};
             if (some) {
-                float x[E], na[E];
+                f2 x[N], na[N];
                 pl.get(j & 1, 0, i, u); pl.get(j & 1, 1, i, x);
 #pragma unroll
-                for (int e = 0; e < E; ++e) u[e] *= x[e];
+                for (int e = 0; e < N; ++e) u[e] = mul2(u[e], x[e]);
                 pl.get(j & 1, 2, i, x);
                 if (!whole) { mask(u, lo, hi, 0.f); mask(x, lo, hi, no_decay<DECAY>()); }
                 decays<DECAY, FAST>(x, a, na, own.A, own.P);
 #pragma unroll
-                for (int e = 0; e < E; ++e) own.S = fmaf(a[e], own.S, u[e]);
+                for (int e = 0; e < N; ++e) own.S = fmaf(a[e].y, fmaf(a[e].x, own.S, u[e].x), u[e].y);
             }
             const Step<LANES, true> step(own);
             if constexpr (LANES > 32) {
@@ -402,7 +432,11 @@ __global__ void __launch_bounds__(RowLane<LANES, CL>::kThreads, LANES >= 128 ? 7
             if (some) {
                 pl.get(j & 1, 3, i, out);
 #pragma unroll
-                for (int e = 0; e < E; ++e) { s = fmaf(a[e], s, u[e]); out[e] *= s; }
+                for (int e = 0; e < N; ++e) {
+                    const float first = fmaf(a[e].x, s, u[e].x);
+                    s = fmaf(a[e].y, first, u[e].y);
+                    out[e] = mul2(out[e], make2(first, s));
+                }
                 if (!whole) mask(out, lo, hi, 0.f);
             }
             if (LANES > 32 && CL == 1 && threadIdx.x == LANES - 1) meeting.carry[j & 1] = state = s;
@@ -418,10 +452,10 @@ __global__ void __launch_bounds__(RowLane<LANES, CL>::kThreads, LANES >= 128 ? 7
 }
 
 template <typename T, int DECAY, int OCT, int LANES, int CL>
-__global__ void __launch_bounds__(RowLane<LANES, CL>::kThreads, LANES >= 128 ? 512 / LANES : LANES == 64 ? 8 : 4) recurrence_backward_kernel(RecArgs p)
+__global__ void __launch_bounds__(RowLane<LANES, CL>::kThreads, LANES > 32 ? 512 / LANES : 4) recurrence_backward_kernel(RecArgs p)
 {
     using R = RowLane<LANES, CL>;
-    constexpr int E = 8 * OCT;
+    constexpr int E = 8 * OCT, N = E / 2;
     constexpr bool FAST = sizeof(T) == 2, STAGED = LANES >= 128 || OCT == 2;
     using Pl = Places<T, OCT, 5, R::kThreads, STAGED>;
     extern __shared__ __align__(16) char stages[];
@@ -468,24 +502,24 @@ __global__ void __launch_bounds__(RowLane<LANES, CL>::kThreads, LANES >= 128 ? 5
         const bool some = lo < hi, whole = lo == 0 && hi == E;
         if (LANES <= 32 || j < r.live) {
             const int met = LANES <= 32 ? 0 : r.live - 1 - j;
-            float a[E], na[E], w[E], u[E];
+            f2 a[N], na[N], w[N], u[N];
             Map own = {1.f, 0.f, 0.f}, rev = {1.f, 0.f, 0.f};
             if (some) {
-                float x[E];
+                f2 x[N];
                 pl.get(j & 1, 0, i, u); pl.get(j & 1, 1, i, x);
 #pragma unroll
-                for (int e = 0; e < E; ++e) u[e] *= x[e];
+                for (int e = 0; e < N; ++e) u[e] = mul2(u[e], x[e]);
                 pl.get(j & 1, 3, i, w); pl.get(j & 1, 4, i, x);
 #pragma unroll
-                for (int e = 0; e < E; ++e) w[e] *= x[e];
+                for (int e = 0; e < N; ++e) w[e] = mul2(w[e], x[e]);
                 pl.get(j & 1, 2, i, x);
                 if (!whole) { mask(u, lo, hi, 0.f); mask(w, lo, hi, 0.f); mask(x, lo, hi, no_decay<DECAY>()); }
                 decays<DECAY, FAST>(x, a, na, own.A, own.P);
                 rev.A = own.A; rev.P = own.P;
 #pragma unroll
-                for (int e = 0; e < E; ++e) own.S = fmaf(a[e], own.S, u[e]);
+                for (int e = 0; e < N; ++e) own.S = fmaf(a[e].y, fmaf(a[e].x, own.S, u[e].x), u[e].y);
 #pragma unroll
-                for (int e = E - 1; e >= 0; --e) rev.S = a[e] * (w[e] + rev.S);
+                for (int e = N - 1; e >= 0; --e) rev.S = a[e].x * (w[e].x + a[e].y * (w[e].y + rev.S));
             }
             const Step<LANES, true> ahead(own);
             const Step<LANES, false> behind(rev);
@@ -498,51 +532,52 @@ __global__ void __launch_bounds__(RowLane<LANES, CL>::kThreads, LANES >= 128 ? 5
             bool fine = true;
             float s = ahead.enter(along, met, 0, from, fine);
             float m = behind.enter(back, met, rank, mu, pl.ok);
-            auto put = [&](T *to, int place, float (&f)[E]) {
+            auto put = [&](T *to, int place, f2 (&f)[N]) {
                 if (!whole) mask(f, lo, hi, 0.f);
                 if (r.real) pl.put(j & 1, place, to, r.start + first(j), first(j), i, t0, p.L, f);
             };
             // (lanes without a position take part in the stores and write zeros)
-            float x[E];
+            f2 x[N];
             if (some) {
                 pl.get(j & 1, 4, i, x);
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const float now = fmaf(a[e], s, u[e]);
-                    u[e] = s;                                // from here the state in front of each position
-                    s = now;
-                    x[e] *= s;
+                for (int e = 0; e < N; ++e) {
+                    const float mid = fmaf(a[e].x, s, u[e].x), end = fmaf(a[e].y, mid, u[e].y);
+                    u[e] = make2(s, mid);                    // from here the state in front of each position
+                    x[e] = mul2(x[e], make2(mid, end));
+                    s = end;
                 }
             }
             put((T *)p.dq, 4, x);
             if (some) {
 #pragma unroll
-                for (int e = E - 1; e >= 0; --e) {           // w: from here lam
-                    w[e] += m;
-                    m = a[e] * w[e];
-                    u[e] *= w[e];
-                    if (DECAY == DECAY_LOG) u[e] *= a[e];
-                    if (DECAY == DECAY_SIGMOID) u[e] *= a[e] * na[e];
+                for (int e = N - 1; e >= 0; --e) {           // w: from here lam
+                    w[e].y += m;
+                    w[e].x = fmaf(a[e].y, w[e].y, w[e].x);
+                    m = a[e].x * w[e].x;
+                    u[e] = mul2(u[e], w[e]);
+                    if (DECAY == DECAY_LOG) u[e] = mul2(u[e], a[e]);
+                    if (DECAY == DECAY_SIGMOID) u[e] = mul2(u[e], mul2(a[e], na[e]));
                 }
             }
             put((T *)p.dg, 2, u);
             if (some) {
                 pl.get(j & 1, 1, i, x);
 #pragma unroll
-                for (int e = 0; e < E; ++e) x[e] *= w[e];
+                for (int e = 0; e < N; ++e) x[e] = mul2(x[e], w[e]);
             }
             put((T *)p.dk, 1, x);
             if (some) {
                 pl.get(j & 1, 0, i, x);
 #pragma unroll
-                for (int e = 0; e < E; ++e) x[e] *= w[e];
+                for (int e = 0; e < N; ++e) x[e] = mul2(x[e], w[e]);
             }
             put((T *)p.dv, 0, x);
             if (LANES > 32 && CL == 1 && threadIdx.x == 0) back.carry[met & 1] = mu = m;
         } else if (r.real) {
-            float zero[E];
+            f2 zero[N];
 #pragma unroll
-            for (int e = 0; e < E; ++e) zero[e] = 0.f;
+            for (int e = 0; e < N; ++e) zero[e] = pair(0.f);
             pl.put(j & 1, 4, (T *)p.dq, r.start + first(j), first(j), i, t0, p.L, zero);
             pl.put(j & 1, 1, (T *)p.dk, r.start + first(j), first(j), i, t0, p.L, zero);
             pl.put(j & 1, 0, (T *)p.dv, r.start + first(j), first(j), i, t0, p.L, zero);
@@ -608,8 +643,7 @@ template <typename T, int DECAY, bool BWD, int OCT, int LANES, int CL> static in
     else return launch_rows<recurrence_forward_kernel<T, DECAY, OCT, LANES, CL>, LANES, CL, 2 * Places<T, OCT, 4, THREADS, STAGED>::STAGE>(a, st);
 }
 
-// Lanes of a row: as few as hold it in one tile, a CTA that walks it where it is longer.  Rows fewer than two CTAs an SM are shared
-// by a cluster.
+// Lanes of a row: as few as hold it in one tile, a CTA that walks it where it is longer.
 template <typename T, int DECAY, bool BWD> static int launch_recurrence_td(const RecArgs &a, cudaStream_t st)
 {
     constexpr int LONG = sizeof(T) == 2 ? 2 : 1;             // octets of a thread where a row is long
@@ -622,10 +656,21 @@ template <typename T, int DECAY, bool BWD> static int launch_recurrence_td(const
     if (octets <= 64) HN_REC(1, 64, 1);
     if constexpr (LONG == 2) if (octets <= 128) HN_REC(2, 64, 1);
     const int threads = (octets + LONG - 1) / LONG;
-    if (threads <= 128 || a.rows >= 6 * kSms) HN_REC(LONG, 128, 1);
-    if (threads <= 256 || a.rows >= 2 * kSms) HN_REC(LONG, 256, 1);
-    if (threads <= 512 || a.rows >= kSms) HN_REC(LONG, 256, 2);
-    if (threads <= 1024 || a.rows * 2 >= kSms) HN_REC(LONG, 256, 4);
+    // Rows that fill the GPU: one CTA each, of as many lanes as still lets all of them run at once (768 threads an SM forward, 512
+    // backward), and small CTAs where they come in several waves anyhow.  512 rows of 65536, bf16, forward: 128 lanes 73 us, 192 70,
+    // 256 (a second wave of 68) 86; backward 119, 145, 129.  12288 rows of 2000: 64 lanes 54 and 107 us, 128 (one tile, nothing travels
+    // ahead) 62 and 118.
+    if constexpr (LONG == 2) {
+        if (threads <= 128 && a.rows >= 12 * kSms) HN_REC(LONG, 64, 1);
+        if constexpr (!BWD) if (threads > 128 && a.rows > 3 * kSms && a.rows <= 4 * kSms) HN_REC(LONG, 192, 1);
+    }
+    if (threads <= 128) HN_REC(LONG, 128, 1);
+    const bool two = BWD ? a.rows > 4 * kSms && a.rows <= 8 * kSms : a.rows >= 2 * kSms && a.rows <= 3 * kSms;
+    if (!two && a.rows >= 2 * kSms) HN_REC(LONG, 128, 1);
+    if (threads <= 256 || two) HN_REC(LONG, 256, 1);
+    // fewer: clusters of as many CTAs as bring one to every SM (128 rows of 65536, bf16: two 31 and 41 us, four 35 and 47)
+    if (threads <= 512 || a.rows * 2 >= kSms) HN_REC(LONG, 256, 2);
+    if (threads <= 1024 || a.rows * 4 >= kSms) HN_REC(LONG, 256, 4);
     HN_REC(LONG, 256, 8);
 #undef HN_REC
 }

@@ -96,7 +96,7 @@ def test_sizes(hn):
 
 def test_classes_refuse_tensors(hn, monkeypatch):
     """Shapes, types, layouts and devices that are not the handle's: ValueError before the library is called."""
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(hn, "_current_device", lambda: 0)
     rec = hn.Recurrence(8, 2, 3)
     t = torch.zeros(2, 3, 8)
     with pytest.raises(ValueError, match="q must be"):
