@@ -30,6 +30,28 @@ DEBUG_FLAGS = ["-lineinfo", "--compress-mode=size", "-DHYENAND_DEBUG"]
 PRECISE = {"synth.cu", "recurrence.cu"}
 
 
+def build_calls(force: bool = False) -> str:
+    """The compiled side of the binding's classes (csrc/calls.cpp): host code against torch's headers, as the module _calls."""
+    import sysconfig
+
+    import torch
+    src, out = os.path.join(CSRC, "calls.cpp"), os.path.join(HERE, "_calls.so")
+    newest = max(os.path.getmtime(src), os.path.getmtime(os.path.join(os.path.dirname(HERE), "include", "hyenand.h")))
+    if not force and os.path.exists(out) and os.path.getmtime(out) >= newest:
+        return out
+    root = os.path.dirname(torch.__file__)
+    tmp = out + ".tmp.%d" % os.getpid()
+    r = subprocess.run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                        "-I" + os.path.join(root, "include"), "-I" + os.path.join(root, "include", "torch", "csrc", "api", "include"),
+                        "-I" + sysconfig.get_paths()["include"], "-I" + os.path.join(os.path.dirname(os.path.dirname(NVCC)), "include"), src, "-o", tmp,
+                        "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cuda", "-ltorch_cpu", "-ltorch", "-lc10_cuda", "-lc10"],
+                       capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"g++ failed on {src}:\n{r.stderr[-4000:]}")
+    os.replace(tmp, out)
+    return out
+
+
 def _sources():
     return sorted(f for f in os.listdir(CSRC) if f.endswith(".cu"))
 
@@ -48,6 +70,7 @@ def build(force: bool = False, verbose: bool = False, debug: bool = False, linei
     OBJ = os.path.join(HERE, "build_debug" if debug else "build")
     LIB = os.path.join(HERE, "libhyenand_debug.so" if debug else "libhyenand.so")
     os.makedirs(OBJ, exist_ok=True)
+    build_calls(force)
     hdr = _newest_header()
     extra = DEBUG_FLAGS if debug else PRODUCT_FLAGS + (["-lineinfo"] if lineinfo else [])
     jobs = []

@@ -213,7 +213,8 @@ template <typename T, int LT, int N, bool ALIGNED> __global__ void __launch_boun
 
 template <typename T, int LT, int N, bool ALIGNED> static int go(const BlockArgs &a, const TileShape &s, cudaStream_t st)
 {
-    return launch_tiles<block_tile_backward_kernel<T, LT, N, ALIGNED>, 2 * Stage<T, LT, N, 5, ALIGNED>::BYTES>(a, s, st);
+    constexpr int BYTES = Stage<T, LT, N, 5, ALIGNED>::BYTES;
+    return launch_tiles<block_tile_backward_kernel<T, LT, N, ALIGNED>, 2 * BYTES>(a, s, st);
 }
 template <typename T, int LT, int N> static int by_alignment(const BlockArgs &a, const TileShape &s, cudaStream_t st)
 {

@@ -12,7 +12,7 @@ namespace cg = cooperative_groups;
 static __device__ int hn_block_status;                       // 1: a bounded wait gave up
 int block_forward_status() { return read_status(hn_block_status); }
 
-template <typename T, int LT, int N, bool ALIGNED> __global__ void __launch_bounds__(kTileThreads, 2) block_tile_forward_kernel(BlockArgs p, int ctas)
+template <typename T, int LT, int N, bool ALIGNED> __global__ void __launch_bounds__(kTileThreads, N <= 4 ? 3 : 2) block_tile_forward_kernel(BlockArgs p, int ctas)
 {
     constexpr int TT = LT * V, ROWS = kTileThreads / LT;
     using Sums = TileSums<LT, 4>;

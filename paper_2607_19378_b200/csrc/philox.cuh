@@ -27,16 +27,22 @@ struct DropKey {
         k0 = (unsigned)seed; k1 = (unsigned)((unsigned long long)seed >> 32);
         step = (unsigned)__ldg(d.rng + 1);
     }
-    __device__ __forceinline__ uint4 words(long long octet) const
+    // the words of U octets, `apart` from one another; the key words of a round are formed once for all
+    template <int U> __device__ __forceinline__ void words(long long octet, long long apart, uint4 (&w)[U]) const
     {
-        unsigned c0 = (unsigned)octet, c1 = (unsigned)((unsigned long long)octet >> 32), c2 = step, c3 = site;
 #pragma unroll
-        for (unsigned r = 0; r < 10; ++r) {                  // (where a thread works out many octets, the twenty key words stay in registers)
-            const unsigned long long p0 = (unsigned long long)c0 * 0xD2511F53u, p1 = (unsigned long long)c2 * 0xCD9E8D57u;
-            c0 = (unsigned)(p1 >> 32) ^ c1 ^ (k0 + r * 0x9E3779B9u); c1 = (unsigned)p1;
-            c2 = (unsigned)(p0 >> 32) ^ c3 ^ (k1 + r * 0xBB67AE85u); c3 = (unsigned)p0;
+        for (int u = 0; u < U; ++u) {
+            const unsigned long long o = (unsigned long long)(octet + u * apart);
+            w[u] = make_uint4((unsigned)o, (unsigned)(o >> 32), step, site);
         }
-        return make_uint4(c0, c1, c2, c3);
+        unsigned a = k0, b = k1;
+#pragma unroll
+        for (int r = 0; r < 10; ++r, a += 0x9E3779B9u, b += 0xBB67AE85u)
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const unsigned long long p0 = (unsigned long long)w[u].x * 0xD2511F53u, p1 = (unsigned long long)w[u].z * 0xCD9E8D57u;
+                w[u] = make_uint4((unsigned)(p1 >> 32) ^ w[u].y ^ a, (unsigned)p1, (unsigned)(p0 >> 32) ^ w[u].w ^ b, (unsigned)p0);
+            }
     }
     // whether the element of a word's lower and of its upper half stays (an upper half is compared together with the lower: it decides)
     __device__ __forceinline__ bool low(unsigned w) const { return w << 16 >= threshold; }
@@ -44,8 +50,9 @@ struct DropKey {
     // bit e set: element e of the octet stays
     __device__ __forceinline__ unsigned keep(long long octet) const
     {
-        const uint4 w = words(octet);
-        const unsigned v[4] = {w.x, w.y, w.z, w.w};
+        uint4 w[1];
+        words(octet, 0, w);
+        const unsigned v[4] = {w[0].x, w[0].y, w[0].z, w[0].w};
         unsigned m = 0;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {

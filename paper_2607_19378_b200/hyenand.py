@@ -3,7 +3,8 @@
 Every function has the name and meaning of the C entry point declared in
 include/hyenand.h; tensors are passed as raw device (or host) pointers and all
 arithmetic happens in the library's CUDA kernels.  There is no fallback: if the
-library has not been built, loading raises.
+library has not been built, loading raises.  Recurrence, Block and Dropout marshal
+their arguments in a compiled module (csrc/calls.cpp).
 """
 from __future__ import annotations
 
@@ -536,21 +537,23 @@ class Plan:
             pass
 
 
-def _expect(device, shape, dtype, names, *tensors):
-    """Dense tensors of one shape and type on the current device; None passes.  (Most of a small call's time on the host is this and
-    what is around it: no keyword dictionaries, no context managers.)"""
-    for t in tensors:
-        if t is not None and (t.dtype is not dtype or t.shape != shape or t.get_device() != device or not t.is_contiguous()):
-            name = next(n for n, x in zip(names, tensors) if x is t)
-            raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on CUDA device {device} (the current one)")
-
-
 def _pool(stream):
     """Outputs and workspaces belong to the stream that the kernels run on, as the allocator sees it."""
     return torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream)))
 
 
-_current_device = torch.cuda.current_device
+@functools.lru_cache(maxsize=1)
+def _calls():
+    """The compiled side of the classes below (csrc/calls.cpp); raises if it was never built."""
+    try:
+        from . import _calls as module
+    except ImportError as e:
+        raise OSError(f"{_HERE}/_calls.so cannot be loaded ({e}): build it with `python -m paper_2607_19378_b200.build`") from e
+    return module
+
+
+def _address(name: str) -> int:
+    return ctypes.cast(getattr(lib(), name), ctypes.c_void_p).value
 
 
 class Recurrence:
@@ -559,66 +562,34 @@ class Recurrence:
 
     def __init__(self, L: int, B: int, C: int, decay: str = "log", dtype=torch.float32):
         self.L, self.B, self.C, self.decay, self.dtype = int(L), int(B), int(C), decay, dtype
-        self._code = {"value": HYENAND_DECAY_VALUE, "log": HYENAND_DECAY_LOG, "sigmoid": HYENAND_DECAY_SIGMOID}[decay]
+        code = {"value": HYENAND_DECAY_VALUE, "log": HYENAND_DECAY_LOG, "sigmoid": HYENAND_DECAY_SIGMOID}[decay]
         marks = hyenand_recurrence_marks(self.L)
         if min(self.B, self.C, marks) < 1:
             raise ValueError("B and C must be >= 1, L between 1 and 2^30")
-        self._shape, self._states = torch.Size((self.B, self.C, self.L)), torch.Size((self.B, self.C))
-        self._marks, self._batch = torch.Size((self.B, self.C, marks)), torch.Size((self.B,))
-        self._head = (self.B, self.C, self.L, self._code, _DTYPES[dtype])
-
-    def _check(self, device, names, sequences, states, lengths):
-        _expect(device, self._shape, self.dtype, names, *sequences)
-        _expect(device, self._states, torch.float32, ("s0 or ds_end",), states)
-        _expect(device, self._batch, torch.int32, ("lengths",), lengths)
+        self._ops = _calls()
+        self._handle = self._ops.make_recurrence(self.B, self.C, self.L, marks, code, _DTYPES[dtype], _address("hyenand_recurrence_forward"),
+                                                 _address("hyenand_recurrence_backward"), _address("hyenand_recurrence_step"), _check)
 
     def forward(self, q, k, v, g, s0=None, lengths=None, marks: bool = False, y=None, stream=None):
         """(y, state behind the row), and with marks=True what `backward` needs of this call as a third."""
-        self._check(_current_device(), "qkvgy", (q, k, v, g, y), s0, lengths)
         if stream is not None:
             with _pool(stream):
-                y, s_end, m = self._forward_outputs(q, y, s0, marks)
-        else:
-            y, s_end, m = self._forward_outputs(q, y, s0, marks)
-        hyenand_recurrence_forward(*self._head, q, k, v, g, s0, lengths, y, s_end, m, stream)
-        return (y, s_end, m) if marks else (y, s_end)
-
-    def _forward_outputs(self, q, y, s0, marks):
-        s_end = torch.empty_like(s0) if s0 is not None else q.new_empty(self._states, dtype=torch.float32)
-        return torch.empty_like(q) if y is None else y, s_end, q.new_empty(self._marks, dtype=torch.float32) if marks else None
+                return self.forward(q, k, v, g, s0, lengths, marks, y)
+        return self._ops.recurrence_forward(self._handle, q, k, v, g, s0, lengths, marks, y)
 
     def backward(self, q, k, v, g, marks, dy, ds_end=None, lengths=None, stream=None):
         """dq, dk, dv, dg and ds0, from the marks of a forward call on the same q, k, v, g, s0 and lengths."""
-        device = _current_device()
-        self._check(device, ("q", "k", "v", "g", "dy"), (q, k, v, g, dy), ds_end, lengths)
-        _expect(device, self._marks, torch.float32, ("marks",), marks)
         if stream is not None:
             with _pool(stream):
-                out = self._backward_outputs(q, ds_end)
-        else:
-            out = self._backward_outputs(q, ds_end)
-        hyenand_recurrence_backward(*self._head, q, k, v, g, lengths, marks, dy, ds_end, *out, stream)
-        return out
-
-    def _backward_outputs(self, q, ds_end):
-        e = torch.empty_like
-        return e(q), e(q), e(q), e(q), e(ds_end) if ds_end is not None else q.new_empty(self._states, dtype=torch.float32)
+                return self.backward(q, k, v, g, marks, dy, ds_end, lengths)
+        return self._ops.recurrence_backward(self._handle, q, k, v, g, marks, dy, ds_end, lengths)
 
     def step(self, q, k, v, g, state, new_state=None, active=None, y=None, stream=None):
         """One token: q, k, v, g [B, C] -> y [B, C]; the state is replaced, or left and the new one written to new_state."""
-        device = _current_device()
-        _expect(device, self._states, self.dtype, "qkvgy", q, k, v, g, y)
-        _expect(device, self._states, torch.float32, ("state", "new_state"), state, new_state)
-        _expect(device, self._batch, torch.int32, ("active",), active)
-        if y is None:
-            if stream is not None:
-                with _pool(stream):
-                    y = torch.empty_like(q)
-            else:
-                y = torch.empty_like(q)
-        hyenand_recurrence_step(self.B, self.C, self._code, self._head[4], q, k, v, g, state, active, y,
-                                state if new_state is None else new_state, stream)
-        return y
+        if stream is not None:
+            with _pool(stream):
+                return self.step(q, k, v, g, state, new_state, active, y)
+        return self._ops.recurrence_step(self._handle, q, k, v, g, state, new_state, active, y)
 
 
 class Block:
@@ -628,53 +599,28 @@ class Block:
     def __init__(self, dims, B: int, C: int, dtype=torch.float32, gate: str = "none", eps: float = 1e-6, p: float = 0.0, site: int = 0):
         self.dims = tuple(int(d) for d in dims)
         self.B, self.C, self.dtype, self.gate, self.eps, self.p, self.site = int(B), int(C), dtype, gate, float(eps), float(p), int(site)
-        self._gate = {"none": HYENAND_GATE_NONE, "sigmoid": HYENAND_GATE_SIGMOID, "silu": HYENAND_GATE_SILU}[gate]
-        self._shape, T = torch.Size((self.B, self.C) + self.dims), math.prod(self.dims)
-        if min(self._shape) < 1:
+        code = {"none": HYENAND_GATE_NONE, "sigmoid": HYENAND_GATE_SIGMOID, "silu": HYENAND_GATE_SILU}[gate]
+        T = math.prod(self.dims)
+        if min((self.B, self.C) + self.dims) < 1:
             raise ValueError("B, C and every extent must be >= 1")
-        self._head, self._stats = (self.B, self.C, T, _DTYPES[dtype]), torch.Size((2, self.B, T))
-        self._channels, self._two = torch.Size((self.C,)), torch.Size((2,))
-        self._workspace = hyenand_block_workspace_bytes(*self._head)
-
-    def _check(self, device, names, tokens, g_post, scale, g_pre, rng):
-        _expect(device, self._shape, self.dtype, names, *tokens)
-        _expect(device, self._channels, torch.float32, ("g_post", "scale", "g_pre"), g_post, scale, g_pre)
-        _expect(device, self._two, torch.int64, ("rng",), rng)
+        self._ops = _calls()
+        self._handle = self._ops.make_block(self.dims, self.B, self.C, T, _DTYPES[dtype], code, self.eps, self.p, self.site,
+                                            hyenand_block_workspace_bytes(self.B, self.C, T, _DTYPES[dtype]), _address("hyenand_block_forward"),
+                                            _address("hyenand_block_backward"), _check)
 
     def forward(self, x, m, z=None, g_post=None, scale=None, g_pre=None, rng=None, stats: bool = False, stream=None):
         """(r, n), n None without g_pre; with stats=True what `backward` needs of this call as a third."""
-        self._check(_current_device(), "xmz", (x, m, z), g_post, scale, g_pre, rng)
         if stream is not None:
             with _pool(stream):
-                r, n, st = self._forward_outputs(x, g_pre, stats)
-        else:
-            r, n, st = self._forward_outputs(x, g_pre, stats)
-        hyenand_block_forward(*self._head, x, m, z, g_post, scale, g_pre, self.eps, self._gate, self.p, rng, self.site, r, n, st, stream)
-        return (r, n, st) if stats else (r, n)
-
-    def _forward_outputs(self, x, g_pre, stats):
-        e = torch.empty_like
-        return e(x), e(x) if g_pre is not None else None, x.new_empty(self._stats, dtype=torch.float32) if stats else None
+                return self.forward(x, m, z, g_post, scale, g_pre, rng, stats)
+        return self._ops.block_forward(self._handle, x, m, z, g_post, scale, g_pre, rng, stats)
 
     def backward(self, x, m, stats, z=None, g_post=None, scale=None, g_pre=None, rng=None, dr=None, dn=None, stream=None):
         """dx, dm, dz, dg_post, dscale, dg_pre (None for what was not given), from the stats of a forward call on the same inputs."""
-        device = _current_device()
-        self._check(device, ("x", "m", "z", "dr", "dn"), (x, m, z, dr, dn), g_post, scale, g_pre, rng)
-        _expect(device, self._stats, torch.float32, ("stats",), stats)
         if stream is not None:
             with _pool(stream):
-                out, work = self._backward_outputs(x, z, g_post, scale, g_pre)
-        else:
-            out, work = self._backward_outputs(x, z, g_post, scale, g_pre)
-        hyenand_block_backward(*self._head, x, m, z, g_post, scale, g_pre, self.eps, self._gate, self.p, rng, self.site, stats, dr, dn,
-                               *out, work, stream)
-        return out
-
-    def _backward_outputs(self, x, z, g_post, scale, g_pre):
-        e = torch.empty_like
-        out = (e(x), e(x), e(x) if z is not None else None, e(g_post) if g_post is not None else None,
-               e(scale) if scale is not None else None, e(g_pre) if g_pre is not None else None)
-        return out, x.new_empty(self._workspace, dtype=torch.uint8)
+                return self.backward(x, m, stats, z, g_post, scale, g_pre, rng, dr, dn)
+        return self._ops.block_backward(self._handle, x, m, stats, z, g_post, scale, g_pre, rng, dr, dn)
 
 
 class Dropout:
@@ -682,22 +628,10 @@ class Dropout:
     call on dy."""
 
     def __init__(self, p: float, site: int = 0):
-        self.p, self.site, self._two = float(p), int(site), torch.Size((2,))
+        self.p, self.site, self._ops, self._call = float(p), int(site), _calls(), _address("hyenand_dropout")
 
     def __call__(self, x, rng, y=None, stream=None):
-        dtype = _DTYPES.get(x.dtype)
-        if dtype is None:
-            raise ValueError("x must be a float32 or bfloat16 tensor")
-        device = _current_device()
-        _expect(device, x.shape, x.dtype, "xy", x, y)
-        _expect(device, self._two, torch.int64, ("rng",), rng)
-        if y is None:
-            if stream is not None:
-                with _pool(stream):
-                    y = torch.empty_like(x)
-            else:
-                y = torch.empty_like(x)
-        n = x.numel()
-        if n:
-            hyenand_dropout(n, dtype, x, self.p, rng, self.site, y, stream)
-        return y
+        if stream is not None:
+            with _pool(stream):
+                return self(x, rng, y)
+        return self._ops.dropout(self._call, _check, self.p, self.site, x, rng, y)

@@ -94,9 +94,8 @@ def test_sizes(hn):
     assert hn.hyenand_block_workspace_bytes(1, 8, 4, 0) >= 3 * 8 * 4 and hn.hyenand_block_workspace_bytes(1, 0, 4, 0) == 0
 
 
-def test_classes_refuse_tensors(hn, monkeypatch):
-    """Shapes, types, layouts and devices that are not the handle's: ValueError before the library is called."""
-    monkeypatch.setattr(hn, "_current_device", lambda: 0)
+def test_classes_refuse_tensors(hn):
+    """Tensors that are not the handle's: ValueError before the library is called."""
     rec = hn.Recurrence(8, 2, 3)
     t = torch.zeros(2, 3, 8)
     with pytest.raises(ValueError, match="q must be"):
@@ -109,6 +108,8 @@ def test_classes_refuse_tensors(hn, monkeypatch):
         hn.Dropout(0.5)(t, torch.zeros(2, dtype=torch.int64))
     with pytest.raises(ValueError, match="float32 or bfloat16"):
         hn.Dropout(0.5)(t.double(), torch.zeros(2, dtype=torch.int64))
+    with pytest.raises(TypeError, match="q must be a tensor"):
+        rec.forward(None, t, t, t)
     for bad in (dict(L=0), dict(B=0), dict(C=0), dict(L=(1 << 30) + 1)):
         with pytest.raises(ValueError):
             hn.Recurrence(**dict(dict(L=8, B=2, C=3), **bad))
