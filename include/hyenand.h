@@ -279,13 +279,17 @@ int hyenand_synth_device_status(void);
  * Decays are meant to be at most 1 in size (g <= 0 for LOG); larger ones are taken, but products of many of them are formed, which
  * can overflow where the state itself does not.  A state is fp32 and every value of y is rounded once, at its store.  A NaN or an
  * infinity spreads to the later positions of its row.  Results do not depend on timing.
+ * workspace: hyenand_recurrence_workspace_bytes() bytes on the device, 16-byte aligned, whose contents mean nothing before and after
+ * (NULL where that is 0); calls that may overlap need one each.
  * Limits: L <= 2^30, B C <= 2^28.  No call allocates, synchronises or keeps anything; errors and stream as hyenand_forward_ex.
  */
 enum { HYENAND_DECAY_VALUE = 0, HYENAND_DECAY_LOG = 1, HYENAND_DECAY_SIGMOID = 2 };
 long long hyenand_recurrence_marks(int L);        /* floats per row of marks; 0 for an L out of range */
+long long hyenand_recurrence_workspace_bytes(int B, int C, int L, int dtype);      /* of a forward or backward call (some 30 KB at most: rows
+                                                                                    * too few to fill the GPU are cut into segments) */
 int hyenand_recurrence_forward(int B, int C, int L, int decay, int dtype, const void *q, const void *k, const void *v,
                                const void *g, const float *s0, const int *lengths, void *y, float *s_end, float *marks,
-                               void *cuda_stream);
+                               void *workspace, void *cuda_stream);
 /* The gradient, from marks of a forward call on the same q, k, v, g, s0 and lengths; with lam_t = q_t dy_t + a_{t+1} lam_{t+1}
  * (at the last position ds_end in place of the second term):
  *     dq = dy s,   dk = lam v,   dv = lam k,   dg_t = lam_t s_{t-1} da_t/dg_t,   ds0 = a_0 lam_0.
@@ -293,13 +297,12 @@ int hyenand_recurrence_forward(int B, int C, int L, int decay, int dtype, const 
  * or NULL; it may be the buffer ds_end.  Each is rounded once, at its store. */
 int hyenand_recurrence_backward(int B, int C, int L, int decay, int dtype, const void *q, const void *k, const void *v,
                                 const void *g, const int *lengths, const float *marks, const void *dy, const float *ds_end,
-                                void *dq, void *dk, void *dv, void *dg, float *ds0, void *cuda_stream);
+                                void *dq, void *dk, void *dv, void *dg, float *ds0, void *workspace, void *cuda_stream);
 /* One token, for generation: q, k, v, g, y are [B][C]; new_state (fp32 [B][C]) may be the buffer `state`.  active: [B] int32 on the
  * device or NULL; an entry whose value is below 1 keeps its state and gets y = 0. */
 int hyenand_recurrence_step(int B, int C, int decay, int dtype, const void *q, const void *k, const void *v, const void *g,
                             const float *state, const int *active, void *y, float *new_state, void *cuda_stream);
-/* Rows too few to fill the GPU are shared by clusters of CTAs, which wait for one another's states; every such wait is bounded.
- * Returns 0, or 1 once one has given up since the library was loaded (the call that met it left its results incomplete), -1 if the
+/* Long rows travel through shared memory as bulk copies, and every wait for one is bounded.  Returns 0, or 1 once one has given up since the library was loaded (the call that met it left its results incomplete), -1 if the
  * word cannot be read.  Synchronises the device. */
 int hyenand_recurrence_device_status(void);
 

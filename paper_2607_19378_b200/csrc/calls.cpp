@@ -101,6 +101,7 @@ ScalarType type_of(int dtype) { return dtype == HYENAND_F32 ? at::kFloat : at::k
 
 struct Recurrence {
     int B, C, L, decay, dtype;
+    int64_t workspace;
     ScalarType type;
     Shape shape, states, marks, batch;
     decltype(&hyenand_recurrence_forward) forward;
@@ -123,10 +124,11 @@ template <typename S> void release(PyObject *o)
 PyObject *make_recurrence(PyObject *, PyObject *args)
 {
     int B, C, L, marks, decay, dtype;
+    long long workspace;
     unsigned long long f, b, st;
     PyObject *raise_error;
-    if (!PyArg_ParseTuple(args, "iiiiiiKKKO", &B, &C, &L, &marks, &decay, &dtype, &f, &b, &st, &raise_error)) return nullptr;
-    auto *r = new Recurrence{B, C, L, decay, dtype, type_of(dtype), {B, C, L}, {B, C}, {B, C, marks}, {B}, (decltype(&hyenand_recurrence_forward))f,
+    if (!PyArg_ParseTuple(args, "iiiiiiLKKKO", &B, &C, &L, &marks, &decay, &dtype, &workspace, &f, &b, &st, &raise_error)) return nullptr;
+    auto *r = new Recurrence{B, C, L, decay, dtype, workspace, type_of(dtype), {B, C, L}, {B, C}, {B, C, marks}, {B}, (decltype(&hyenand_recurrence_forward))f,
                              (decltype(&hyenand_recurrence_backward))b, (decltype(&hyenand_recurrence_step))st, Py_NewRef(raise_error)};
     return PyCapsule_New(r, nullptr, release<Recurrence>);
 }
@@ -143,9 +145,9 @@ PyObject *recurrence_forward(PyObject *, PyObject *const *a, Py_ssize_t n)
                      *len = want(a[6], "lengths", at::kInt, r->batch, true), *given = want(a[8], "y", r->type, r->shape, true);
         const Tensor y = given ? *given : want.empty(r->shape, r->type), end = want.empty(r->states, at::kFloat);
         const bool keep = PyObject_IsTrue(a[7]) == 1;
-        const Tensor marks = keep ? want.empty(r->marks, at::kFloat) : Tensor();
+        const Tensor marks = keep ? want.empty(r->marks, at::kFloat) : Tensor(), work = r->workspace ? want.empty({r->workspace}, at::kByte) : Tensor();
         check(r->forward(r->B, r->C, r->L, r->decay, r->dtype, data(q), data(k), data(v), data(g), (const float *)data(s0), (const int *)data(len),
-                         y.data_ptr(), (float *)end.data_ptr(), keep ? (float *)marks.data_ptr() : nullptr, want.stream()), r->raise_error);
+                         y.data_ptr(), (float *)end.data_ptr(), keep ? (float *)marks.data_ptr() : nullptr, r->workspace ? work.data_ptr() : nullptr, want.stream()), r->raise_error);
         return keep ? tuple({y, end, marks}) : tuple({y, end});
     });
 }
@@ -162,10 +164,10 @@ PyObject *recurrence_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
                      *ds = want(a[7], "ds_end", at::kFloat, r->states, true), *len = want(a[8], "lengths", at::kInt, r->batch, true);
         Tensor o[4];
         for (Tensor &t : o) t = want.empty(r->shape, r->type);
-        const Tensor ds0 = want.empty(r->states, at::kFloat);
+        const Tensor ds0 = want.empty(r->states, at::kFloat), work = r->workspace ? want.empty({r->workspace}, at::kByte) : Tensor();
         check(r->backward(r->B, r->C, r->L, r->decay, r->dtype, data(q), data(k), data(v), data(g), (const int *)data(len), (const float *)data(marks),
                           data(dy), (const float *)data(ds), o[0].data_ptr(), o[1].data_ptr(), o[2].data_ptr(), o[3].data_ptr(),
-                          (float *)ds0.data_ptr(), want.stream()), r->raise_error);
+                          (float *)ds0.data_ptr(), r->workspace ? work.data_ptr() : nullptr, want.stream()), r->raise_error);
         return tuple({o[0], o[1], o[2], o[3], ds0});
     });
 }

@@ -2,26 +2,22 @@
 //
 //     s_t = a_t s_{t-1} + k_t v_t,      y_t = q_t s_t,      a_t = g_t | exp(g_t) | sigmoid(g_t)
 //
-// One pass over the data.  Maps s -> A s + S of neighbouring positions compose to (A1 A2, S2 + A2 S1); a thread composes the eight of
-// its octet, the lanes of a row scan those by shuffles, the warps of a row meet in shared memory, and then every thread runs its
-// eight steps from the state that enters them.  Long rows are walked tile by tile, the state carried in a register.  Where there are
-// fewer rows than the SMs can hold, a cluster of CTAs shares a row's tiles and the maps travel through distributed shared memory.
+// One pass over the data.  Maps s -> A s + S of neighbouring positions compose to (A1 A2, S2 + A2 S1); a thread composes those of its
+// positions, the lanes of a row scan the threads' by shuffles, the warps of a row meet in shared memory, and then every thread runs
+// its steps from the state that enters them.  Long rows are walked tile by tile, the state carried on.  Rows too few to fill the GPU
+// are cut into segments: a first kernel leaves every segment's map in the workspace, the second composes those in front of its own.
 //
 // All states and maps are fp32.  A product of thousands of decays close to 1 would collect the rounding of each of them, always to
 // the same side where the decay is constant; the maps therefore carry P = A - 1 beside A (P1 P2 + P1 + P2), built from 1 - a_t
 // (sigmoid), from the sum of the g_t (exp), and use whichever of the two is the precise one.
-#include <cooperative_groups.h>
-
 #include "entry.cuh"
 #include "octet.cuh"
 #include "pair.cuh"
 #include "tma_util.cuh"
 
-namespace cg = cooperative_groups;
-
 namespace hn {
 
-constexpr int kMarkOctets = 128;          // the state is marked in front of every 1024 positions of a row (octets of the flat tensor)
+constexpr int kMarkOctets = 32;           // the state is marked in front of every 256 positions of a row (octets of the flat tensor)
 
 enum { DECAY_VALUE = 0, DECAY_LOG = 1, DECAY_SIGMOID = 2 };
 
@@ -32,6 +28,8 @@ struct RecArgs {
     void *y, *dq, *dk, *dv, *dg;
     float *s_end, *ds0;                   // [rows] or nullptr
     float *marks;                         // [rows][marks_row] or nullptr (forward); read by the backward
+    float4 *maps;                         // [rows][segments], where there are several
+    int segments;                         // of a row
     long long rows, n;                    // n = rows * L
     int C, L, marks_row;
 };
@@ -47,13 +45,15 @@ __device__ __forceinline__ float apply(const Map &m, float s)
 // a first, then b
 __device__ __forceinline__ Map compose(const Map &a, const Map &b) { return {a.A * b.A, fmaf(a.P, b.P, a.P + b.P), apply(b, a.S)}; }
 
-// a_t and 1 - a_t (LOG: not needed, 0)
-template <int DECAY, bool FAST> __device__ __forceinline__ void decay(float g, float &a, float &na)
+// a_t and 1 - a_t (LOG: not needed, 0).  The approximate exponential and reciprocal are off by a few roundings, which a thread's steps
+// can multiply up sixteen-fold at most: what goes on from thread to thread is built from 1 - a_t and the sum of the g_t.
+constexpr float kLog2e = 1.4426950408889634f;
+template <int DECAY> __device__ __forceinline__ void decay(float g, float &a, float &na)
 {
     if constexpr (DECAY == DECAY_VALUE) { a = g; na = 1.f - g; }
-    else if constexpr (DECAY == DECAY_LOG) { a = FAST ? __expf(g) : expf(g); na = 0.f; }
+    else if constexpr (DECAY == DECAY_LOG) { a = ex2(g * kLog2e); na = 0.f; }
     else {
-        const float e = FAST ? __expf(-fabsf(g)) : expf(-fabsf(g)), r = FAST ? __fdividef(1.f, 1.f + e) : __frcp_rn(1.f + e), x = e * r;
+        const float e = ex2(-kLog2e * fabsf(g)), r = rcp(1.f + e), x = e * r;
         a = g >= 0.f ? r : x;
         na = g >= 0.f ? x : r;
     }
@@ -70,27 +70,25 @@ __device__ __forceinline__ float expm1_of(float x, float ex)
 
 // a and 1 - a of a thread's positions, and A, P of the whole.  Positions outside [lo, hi) are the identity: their gate is made one
 // that decays nothing before anything is computed (whatever was in them).
-template <int DECAY, bool FAST, int N> __device__ __forceinline__ void decays(const f2 (&g)[N], f2 (&a)[N], f2 (&na)[N], float &A, float &P)
+template <int DECAY, int N> __device__ __forceinline__ void decays(const f2 (&g)[N], f2 (&a)[N], f2 (&na)[N], float &A, float &P)
 {
     A = 1.f; P = 0.f;
     if constexpr (DECAY == DECAY_LOG) {
         f2 sum = pair(0.f);
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            if constexpr (FAST) {
-                const f2 y = mul2(g[e], pair(1.4426950408889634f));
-                a[e] = make2(ex2(y.x), ex2(y.y));
-            } else a[e] = make2(expf(g[e].x), expf(g[e].y));
+            const f2 y = mul2(g[e], pair(kLog2e));
+            a[e] = make2(ex2(y.x), ex2(y.y));
             sum = add2(sum, g[e]);
         }
         const float x = sum2(sum);
-        A = FAST ? __expf(x) : expf(x);
+        A = ex2(x * kLog2e);
         P = expm1_of(x, A);
     } else {
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            decay<DECAY, FAST>(g[e].x, a[e].x, na[e].x);
-            decay<DECAY, FAST>(g[e].y, a[e].y, na[e].y);
+            decay<DECAY>(g[e].x, a[e].x, na[e].x);
+            decay<DECAY>(g[e].y, a[e].y, na[e].y);
             A *= a[e].x * a[e].y;
             P = fmaf(fmaf(P, a[e].x, -na[e].x), a[e].y, -na[e].y);
         }
@@ -129,35 +127,24 @@ template <int LANES, bool UP> __device__ __forceinline__ Map neighbour(const Map
     return o;
 }
 
-// Where a thread stands: LANES lanes share a row (a part of a warp, or a CTA of LANES threads), CL CTAs in a row of tiles.  A thread
-// takes one octet, or in longer rows of bf16 two (OCT): what a tile costs besides its elements (the scans, half of all instructions
-// with one octet) is then a smaller part of what the memory allows.
-template <int LANES, int CL> struct RowLane {
+// Where a thread stands: LANES lanes share a row (a part of a warp, or a CTA of LANES threads).  A thread takes one octet, or in longer
+// rows of bf16 two (OCT): what a tile costs besides its elements (the scans, half of all instructions with one octet) is then a
+// smaller part of what the memory allows.
+template <int LANES> struct RowLane {
     static constexpr int kThreads = LANES <= 32 ? 128 : LANES;
     static constexpr int kRows = LANES <= 32 ? kThreads / LANES : 1;
     static constexpr int kWarps = LANES <= 32 ? 1 : LANES / 32;      // of one CTA, that share a row
-    static constexpr int kSpan = LANES * CL;                         // threads of a tile
 };
 
-// How the threads of a row learn the state that enters their octets.  The warps of a CTA leave their maps in shared memory; CTAs of a
-// cluster send each other theirs as asynchronous stores, counted by a barrier in the receiver's memory (a barrier of the whole
-// cluster would wait for the results of the last tile to reach memory too).  A slot is written again two tiles later: by then its
-// readers have left the barrier, or sent the map of the tile, between.
-template <int LANES, int CL> struct alignas(16) Meeting {
-    using R = RowLane<LANES, CL>;
-    float4 warp[2][R::kWarps];
-    float4 peers[2][CL];
-    uint64_t arrived[2];
-    float carry[2];                                          // CL == 1: the state behind a tile, left by the thread that forms it
-
-    __device__ __forceinline__ void init()
-    {
-        if (CL > 1 && threadIdx.x == 0) { mbar_init(&arrived[0], 1); mbar_init(&arrived[1], 1); fence_mbar_init(); }
-    }
+// How the warps of a row learn the state that enters them: each leaves its map, the thread that forms the state behind a tile leaves
+// that.  A slot is written again two tiles later, when all have passed the barrier of the tile between.
+template <int LANES> struct alignas(16) Meeting {
+    float4 warp[2][RowLane<LANES>::kWarps];
+    float carry[2];
 };
 template <int LANES, bool UP> struct Step {                   // one thread's part of a tile
-    static constexpr int W = LANES < 32 ? LANES : 32;
-    Map before;                                              // the octets of the warp in front of this thread's
+    static constexpr int W = LANES < 32 ? LANES : 32, NW = RowLane<LANES>::kWarps;
+    Map before;                                              // the positions of the warp in front of this thread's
     Map all;                                                 // those of the whole warp (LANES <= 32: of the row)
     __device__ __forceinline__ explicit Step(const Map &own)
     {
@@ -169,20 +156,19 @@ template <int LANES, bool UP> struct Step {                   // one thread's pa
         else all = inc;                                      // (the last lane's)
     }
     // before the CTA's barrier
-    template <int CL> __device__ __forceinline__ void leave(Meeting<LANES, CL> &m, int count) const
+    __device__ __forceinline__ void leave(Meeting<LANES> &m, int count) const
     {
         if (LANES > 32 && threadIdx.x % 32 == (UP ? 31 : 0)) m.warp[count & 1][threadIdx.x / 32] = make_float4(all.A, all.P, all.S, 0.f);
     }
-    // after it: the state in front of this thread's positions.  LANES <= 32 and CL > 1: carry moves on to the one behind the tile; else
-    // the thread that forms it stores it (Meeting::carry).  ok: no wait has given up yet
-    template <int CL> __device__ __forceinline__ float enter(Meeting<LANES, CL> &m, int count, int rank, float &carry, bool &ok) const
+    // After it: the state in front of this thread's positions, from the one in front of the tile.  LANES <= 32: carry moves on to the
+    // one behind it; else the thread that forms that one stores it (Meeting::carry).
+    __device__ __forceinline__ float enter(const Meeting<LANES> &m, int count, float &carry) const
     {
-        constexpr int NW = RowLane<LANES, CL>::kWarps;
         if constexpr (LANES <= 32) {
             const float s = apply(before, carry);
             carry = apply(all, carry);
             return s;
-        } else if constexpr (CL == 1) {
+        } else {
             float in = carry;
             const int w = threadIdx.x / 32;
 #pragma unroll
@@ -192,52 +178,24 @@ template <int LANES, bool UP> struct Step {                   // one thread's pa
                 in = apply({f.x, f.y, f.z}, in);
             }
             return apply(before, in);
-        } else {
-            Map pre = {1.f, 0.f, 0.f}, tot = {1.f, 0.f, 0.f};
-#pragma unroll
-            for (int i = 0; i < NW; ++i) {
-                const int j = UP ? i : NW - 1 - i;
-                if (j == (int)(threadIdx.x / 32)) pre = tot;
-                const float4 w = m.warp[count & 1][j];
-                tot = compose(tot, {w.x, w.y, w.z});
-            }
-            if (threadIdx.x < 32) {
-                if (threadIdx.x == 0) mbar_expect_tx(&m.arrived[count & 1], CL * 16);
-                __syncwarp();
-                if (threadIdx.x < CL) {
-                    unsigned to, bar;
-                    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(smem_u32(&m.peers[count & 1][rank])), "r"((int)threadIdx.x));
-                    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(bar) : "r"(smem_u32(&m.arrived[count & 1])), "r"((int)threadIdx.x));
-                    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];\n"
-                                 ::"r"(to), "f"(tot.A), "f"(tot.P), "f"(tot.S), "f"(0.f), "r"(bar) : "memory");
-                }
-            }
-            if (ok) ok = mbar_wait(&m.arrived[count & 1], count >> 1 & 1);
-            float in = 0.f;
-#pragma unroll
-            for (int i = 0; i < CL; ++i) {
-                const int r = UP ? i : CL - 1 - i;
-                if (r == rank) in = carry;
-                const float4 w = m.peers[count & 1][r];
-                carry = apply({w.x, w.y, w.z}, carry);
-            }
-            return apply(before, apply(pre, in));
         }
     }
 };
 
-// A row as its threads see it.
-template <int LANES, int CL, int E> struct Row {
-    using R = RowLane<LANES, CL>;
-    static constexpr int kTile = E * R::kSpan;
+// A row, or a segment of one, as its threads see it.
+template <int LANES, int E> struct Row {
+    using R = RowLane<LANES>;
+    static constexpr int kTile = E * LANES;
     long long row, start;                                    // start: its first element
-    int l, lead, len, tiles, live;                           // this thread of a tile; elements of the row's first octet in front of it
+    int l, lead, len;                                        // this thread of a tile; elements of the row's first octet in front of it
+    int segment, first, last, live;                          // tiles [first, last) of the row; those below `live` have a position
     bool real;
-    __device__ __forceinline__ Row(const RecArgs &p, int rank)
+    __device__ __forceinline__ explicit Row(const RecArgs &p)
     {
-        row = (long long)(blockIdx.x / CL) * R::kRows + threadIdx.x / LANES;
+        row = (long long)(blockIdx.x / p.segments) * R::kRows + threadIdx.x / LANES;
+        segment = (int)(blockIdx.x % p.segments);
         real = row < p.rows;
-        l = threadIdx.x % LANES + rank * LANES;
+        l = threadIdx.x % LANES;
         len = real ? p.L : 0;
         if (real && p.lengths) {
             const int b = (int)(row / p.C);
@@ -246,8 +204,38 @@ template <int LANES, int CL, int E> struct Row {
         }
         start = real ? row * p.L : 0;
         lead = (int)(start & 7);
-        tiles = (lead + p.L + kTile - 1) / kTile;
+        const int tiles = (lead + p.L + kTile - 1) / kTile, each = (tiles + p.segments - 1) / p.segments;
+        first = min(tiles, segment * each);
+        last = min(tiles, first + each);
         live = len ? (lead + len + kTile - 1) / kTile : 0;
+    }
+    __device__ __forceinline__ int position(int tile) const { return (tile * LANES + l) * E - lead; }           // this thread's first
+    __device__ __forceinline__ int warp_position(int tile) const { return (tile * LANES + l - ((int)threadIdx.x & 31)) * E - lead; }
+    // by the lanes of one warp: from the state at the row's end that the maps come from, through the segments on the way to this one
+    template <bool UP> __device__ __forceinline__ float entering(const RecArgs &p, float state) const
+    {
+        const int lane = threadIdx.x & 31, each = ((UP ? segment : p.segments - 1 - segment) + 31) / 32;
+        int n = UP ? segment : p.segments - 1 - segment;
+        if (!real) n = 0;
+        Map m = {1.f, 0.f, 0.f};
+        const int end = min(n, (lane + 1) * each);
+        for (int i = lane * each; i < end; i += 8) {
+            float4 w[8];                                     // (on their way together)
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                w[u] = make_float4(1.f, 0.f, 0.f, 0.f);
+                if (i + u < end) {
+                    const float4 *f = p.maps + row * p.segments + (UP ? i + u : p.segments - 1 - i - u);
+                    HN_G(f, 16);
+                    w[u] = *f;
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                if (i + u < end) m = compose(m, {w[u].x, w[u].y, w[u].z});
+        }
+        m = scan_lanes<32, true>(m, lane);
+        return __shfl_sync(~0u, apply(m, state), 31);
     }
 };
 
@@ -365,41 +353,88 @@ template <typename T, int OCT, int TENSORS, int THREADS, bool STAGED> struct Pla
     }
 };
 
-template <typename T, int DECAY, int OCT, int LANES, int CL>
-__global__ void __launch_bounds__(RowLane<LANES, CL>::kThreads, LANES > 32 ? 768 / LANES : 6) recurrence_forward_kernel(RecArgs p)
+// The map of every segment: of the states (UP, from k, v, g) or of their gradients (from q, dy, g, from the end).
+template <typename T, int DECAY, int OCT, bool UP>
+__global__ void __launch_bounds__(128, 8) recurrence_maps_kernel(RecArgs p)
 {
-    using R = RowLane<LANES, CL>;
+    constexpr int LANES = 32;
     constexpr int E = 8 * OCT, N = E / 2;
-    constexpr bool FAST = sizeof(T) == 2, STAGED = LANES >= 128 || OCT == 2;         // (shorter rows are one tile)
-    using Pl = Places<T, OCT, 4, R::kThreads, STAGED>;
+    using Pl = Places<T, OCT, 3, 128, true>;
     extern __shared__ __align__(16) char stages[];
-    __shared__ Meeting<LANES, CL> meeting;
+    __shared__ uint64_t barriers[128 / 16];
+    pdl_join();
+    const Row<LANES, E> r(p);
+    Pl pl;
+    pl.in[0] = (const T *)(UP ? p.k : p.q); pl.in[1] = (const T *)(UP ? p.v : p.dy); pl.in[2] = (const T *)p.g;
+    pl.init(stages, barriers, r.len, p.n);
+    const int tiles = max(0, min(r.last, r.live) - r.first);
+    auto tile_of = [&](int c) { return UP ? r.first + c : r.first + tiles - 1 - c; };
+    auto fetch = [&](int c) { pl.fetch(c & 1, r.start + r.warp_position(tile_of(c)), r.warp_position(tile_of(c))); };
+    Map total = {1.f, 0.f, 0.f};
+    int waited[2] = {0, 0};
+    if (tiles) fetch(0);
+    for (int c = 0; c < tiles; ++c) {
+        const int j = tile_of(c), t0 = r.position(j), turn = c & 1, lo = max(0, -t0), hi = min(E, r.len - t0);
+        const long long i = r.start + t0;
+        __syncwarp();                                        // (the other stage has been read)
+        if (c + 1 < tiles) fetch(c + 1);
+        pl.wait(turn, (turn ? waited[1] : waited[0]) & 1, r.warp_position(j));
+        if (r.warp_position(j) < r.len) { if (turn) ++waited[1]; else ++waited[0]; }
+        Map own = {1.f, 0.f, 0.f};
+        if (lo < hi) {
+            f2 a[N], na[N], u[N], x[N];
+            pl.get(turn, 0, i, u); pl.get(turn, 1, i, x);
+#pragma unroll
+            for (int e = 0; e < N; ++e) u[e] = mul2(u[e], x[e]);
+            pl.get(turn, 2, i, x);
+            if (lo > 0 || hi < E) { mask(u, lo, hi, 0.f); mask(x, lo, hi, no_decay<DECAY>()); }
+            decays<DECAY>(x, a, na, own.A, own.P);
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                if (UP) own.S = fmaf(a[e].y, fmaf(a[e].x, own.S, u[e].x), u[e].y);
+                else own.S = a[N - 1 - e].x * (u[N - 1 - e].x + a[N - 1 - e].y * (u[N - 1 - e].y + own.S));
+        }
+        const Map inc = scan_lanes<32, UP>(own, pl.lane);
+        total = compose(total, inc);                         // (of use in the last lane on the way)
+    }
+    if (r.real && pl.lane == (UP ? 31 : 0)) {
+        float4 *f = p.maps + r.row * p.segments + r.segment;
+        HN_G(f, 16);
+        *f = make_float4(total.A, total.P, total.S, 0.f);
+    }
+    if (!pl.ok) atomicExch(&hn_rec_status, 1);
+}
+
+template <typename T, int DECAY, int OCT, int LANES, bool STAGED>
+__global__ void __launch_bounds__(RowLane<LANES>::kThreads, LANES > 32 ? 768 / LANES : 6) recurrence_forward_kernel(RecArgs p)
+{
+    using R = RowLane<LANES>;
+    constexpr int E = 8 * OCT, N = E / 2;
+        using Pl = Places<T, OCT, 4, R::kThreads, STAGED>;
+    extern __shared__ __align__(16) char stages[];
+    __shared__ Meeting<LANES> meeting;
     __shared__ uint64_t barriers[STAGED ? R::kThreads / 16 : 1];
     const T *q = (const T *)p.q, *k = (const T *)p.k, *v = (const T *)p.v, *g = (const T *)p.g;
     T *y = (T *)p.y;
     pdl_join();
-    int rank = 0;
-    if constexpr (CL > 1) {
-        rank = cg::this_cluster().block_rank();
-        meeting.init();
-        cg::this_cluster().sync();                           // every CTA's barriers exist before something is sent to one
-    }
-    const Row<LANES, CL, E> r(p, rank);
+    const Row<LANES, E> r(p);
     float state = 0.f;
     if (r.real && p.s0) { HN_G(p.s0 + r.row, 4); state = p.s0[r.row]; }
+    if (STAGED && LANES > 32 && threadIdx.x == 0) meeting.carry[1] = state;      // (read behind the first tile's barrier)
     Pl pl;
     pl.in[0] = k; pl.in[1] = v; pl.in[2] = g; pl.in[3] = q;
     pl.init(stages, barriers, r.len, p.n);
-    auto first = [&](int j) { return (j * R::kSpan + r.l - ((int)threadIdx.x & 31)) * E - r.lead; };       // position of this warp's first lane
-    if (STAGED) pl.fetch(0, r.start + first(0), first(0));
-    for (int j = 0; j < r.tiles; ++j) {
-        const int th = j * R::kSpan + r.l, t0 = th * E - r.lead;
+    auto first = [&](int j) { return r.warp_position(j); };
+    if (STAGED && r.first < r.last) pl.fetch(0, r.start + first(r.first), first(r.first));
+    if (LANES == 32 && r.segment) state = r.template entering<true>(p, state);
+    for (int j = r.first; j < r.last; ++j) {
+        const int th = j * LANES + r.l, t0 = th * E - r.lead, met = j - r.first, turn = met & 1;
         const long long i = r.start + t0;
         const int lo = max(0, -t0), hi = min(E, r.len - t0);
         if (STAGED) {
             pl.stage_free();
-            if (j + 1 < r.tiles) pl.fetch((j + 1) & 1, r.start + first(j + 1), first(j + 1));
-            pl.wait(j & 1, j >> 1 & 1, first(j));
+            if (j + 1 < r.last) pl.fetch(turn ^ 1, r.start + first(j + 1), first(j + 1));
+            pl.wait(turn, met >> 1 & 1, first(j));
         }
         const bool some = lo < hi, whole = lo == 0 && hi == E;
         f2 out[N];
@@ -408,29 +443,29 @@ __global__ void __launch_bounds__(RowLane<LANES, CL>::kThreads, LANES > 32 ? 768
             Map own = {1.f, 0.f, 0.f};
             if (some) {
                 f2 x[N], na[N];
-                pl.get(j & 1, 0, i, u); pl.get(j & 1, 1, i, x);
+                pl.get(turn, 0, i, u); pl.get(turn, 1, i, x);
 #pragma unroll
                 for (int e = 0; e < N; ++e) u[e] = mul2(u[e], x[e]);
-                pl.get(j & 1, 2, i, x);
+                pl.get(turn, 2, i, x);
                 if (!whole) { mask(u, lo, hi, 0.f); mask(x, lo, hi, no_decay<DECAY>()); }
-                decays<DECAY, FAST>(x, a, na, own.A, own.P);
+                decays<DECAY>(x, a, na, own.A, own.P);
 #pragma unroll
                 for (int e = 0; e < N; ++e) own.S = fmaf(a[e].y, fmaf(a[e].x, own.S, u[e].x), u[e].y);
             }
             const Step<LANES, true> step(own);
             if constexpr (LANES > 32) {
-                step.leave(meeting, j);
+                step.leave(meeting, met);
                 __syncthreads();
-                if (CL == 1 && j) state = meeting.carry[(j - 1) & 1];
+                if (STAGED || met) state = meeting.carry[(met - 1) & 1];
             }
-            float s = step.enter(meeting, j, rank, state, pl.ok);
+            float s = step.enter(meeting, met, state);
             if (p.marks && r.real && th * OCT % kMarkOctets == 0 && th * OCT / kMarkOctets < p.marks_row) {
                 float *m = p.marks + r.row * p.marks_row + th * OCT / kMarkOctets;
                 HN_G(m, 4);
                 *m = s;
             }
             if (some) {
-                pl.get(j & 1, 3, i, out);
+                pl.get(turn, 3, i, out);
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
                     const float first = fmaf(a[e].x, s, u[e].x);
@@ -439,42 +474,36 @@ __global__ void __launch_bounds__(RowLane<LANES, CL>::kThreads, LANES > 32 ? 768
                 }
                 if (!whole) mask(out, lo, hi, 0.f);
             }
-            if (LANES > 32 && CL == 1 && threadIdx.x == LANES - 1) meeting.carry[j & 1] = state = s;
+            if (LANES > 32 && threadIdx.x == LANES - 1) meeting.carry[turn] = state = s;
         }
         if (!some) mask(out, 0, 0, 0.f);
-        if (r.real) pl.put(j & 1, 0, y, r.start + first(j), first(j), i, t0, p.L, out);
+        if (r.real) pl.put(turn, 0, y, r.start + first(j), first(j), i, t0, p.L, out);
         pl.put_done();
     }
-    if (r.real && p.s_end && r.l == (LANES > 32 && CL == 1 ? LANES - 1 : 0)) { HN_G(p.s_end + r.row, 4); p.s_end[r.row] = state; }
+    if (STAGED && LANES > 32 && r.first >= r.live) { __syncthreads(); state = meeting.carry[1]; }       // (no tile has a position)
+    if (r.real && p.s_end && r.segment == p.segments - 1 && r.l == (LANES > 32 ? LANES - 1 : 0)) { HN_G(p.s_end + r.row, 4); p.s_end[r.row] = state; }
     if (STAGED && pl.lane == 0) tma_wait_all0();
     if (!pl.ok) atomicExch(&hn_rec_status, 1);
-    if constexpr (CL > 1) cg::this_cluster().sync();         // no CTA leaves while another may still send to it
 }
 
-template <typename T, int DECAY, int OCT, int LANES, int CL>
-__global__ void __launch_bounds__(RowLane<LANES, CL>::kThreads, LANES > 32 ? 512 / LANES : 4) recurrence_backward_kernel(RecArgs p)
+template <typename T, int DECAY, int OCT, int LANES, bool STAGED>
+__global__ void __launch_bounds__(RowLane<LANES>::kThreads, LANES > 32 ? 512 / LANES : 4) recurrence_backward_kernel(RecArgs p)
 {
-    using R = RowLane<LANES, CL>;
+    using R = RowLane<LANES>;
     constexpr int E = 8 * OCT, N = E / 2;
-    constexpr bool FAST = sizeof(T) == 2, STAGED = LANES >= 128 || OCT == 2;
     using Pl = Places<T, OCT, 5, R::kThreads, STAGED>;
     extern __shared__ __align__(16) char stages[];
-    __shared__ Meeting<LANES, 1> along;                      // the states, from each CTA's mark
+    __shared__ Meeting<LANES> along;                         // the states, from each tile's mark
     __shared__ uint64_t barriers[STAGED ? R::kThreads / 16 : 1];
-    __shared__ Meeting<LANES, CL> back;                      // the gradients of the states, from the row's end
+    __shared__ Meeting<LANES> back;                          // the gradients of the states, from the row's end
     const T *q = (const T *)p.q, *k = (const T *)p.k, *v = (const T *)p.v, *g = (const T *)p.g, *dy = (const T *)p.dy;
     pdl_join();
-    int rank = 0;
-    if constexpr (CL > 1) {
-        rank = cg::this_cluster().block_rank();
-        back.init();
-        cg::this_cluster().sync();
-    }
-    const Row<LANES, CL, E> r(p, rank);
+    const Row<LANES, E> r(p);
     float mu = 0.f;                                          // a_{t+1} lam_{t+1} of the position behind the tile
-    if (r.real && p.ds_end) { HN_G(p.ds_end + r.row, 4); mu = __ldg(p.ds_end + r.row); }
-    auto mark_of = [&](int j) {                              // in front of this CTA's part of a tile, or of the row
-        const int mark = STAGED ? (j * R::kSpan + rank * LANES) * OCT / kMarkOctets : 0;
+    if (r.real && p.ds_end) { HN_G(p.ds_end + r.row, 4); mu = p.ds_end[r.row]; }
+    if (STAGED && LANES > 32 && threadIdx.x == 0) back.carry[1] = mu;
+    auto mark_of = [&](int j) {                              // in front of a tile
+        const int mark = STAGED ? j * LANES * OCT / kMarkOctets : 0;
         if (j < 0 || !r.real || mark >= p.marks_row) return 0.f;
         const float *m = p.marks + r.row * p.marks_row + mark;
         HN_G(m, 4);
@@ -483,25 +512,26 @@ __global__ void __launch_bounds__(RowLane<LANES, CL>::kThreads, LANES > 32 ? 512
     Pl pl;
     pl.in[0] = k; pl.in[1] = v; pl.in[2] = g; pl.in[3] = q; pl.in[4] = dy;
     pl.init(stages, barriers, r.len, p.n);
-    auto first = [&](int j) { return (j * R::kSpan + r.l - ((int)threadIdx.x & 31)) * E - r.lead; };       // position of this warp's first lane
-    float mark = mark_of(r.tiles - 1);
+    auto first = [&](int j) { return r.warp_position(j); };
+    float mark = mark_of(r.last - 1);
     int used[2] = {0, 0};                                    // copies waited for, of each stage
-    if (STAGED) pl.fetch((r.tiles - 1) & 1, r.start + first(r.tiles - 1), first(r.tiles - 1));
-    for (int j = r.tiles - 1; j >= 0; --j) {
-        const int t0 = (j * R::kSpan + r.l) * E - r.lead;
+    if (STAGED && r.first < r.last) pl.fetch((r.last - 1) & 1, r.start + first(r.last - 1), first(r.last - 1));
+    if (LANES == 32 && r.segment < p.segments - 1) mu = r.template entering<false>(p, mu);
+    for (int j = r.last - 1; j >= r.first; --j) {
+        const int t0 = r.position(j);
         const long long i = r.start + t0;
         const int lo = max(0, -t0), hi = min(E, r.len - t0);
         float from = mark;
         if (STAGED) {
             pl.stage_free();
-            if (j) pl.fetch((j - 1) & 1, r.start + first(j - 1), first(j - 1));
+            if (j > r.first) pl.fetch((j - 1) & 1, r.start + first(j - 1), first(j - 1));
             mark = mark_of(j - 1);
             pl.wait(j & 1, (j & 1 ? used[1] : used[0]) & 1, first(j));
             if (first(j) < r.len) { if (j & 1) ++used[1]; else ++used[0]; }
         }
         const bool some = lo < hi, whole = lo == 0 && hi == E;
         if (LANES <= 32 || j < r.live) {
-            const int met = LANES <= 32 ? 0 : r.live - 1 - j;
+            const int met = min(r.live, r.last) - 1 - j;
             f2 a[N], na[N], w[N], u[N];
             Map own = {1.f, 0.f, 0.f}, rev = {1.f, 0.f, 0.f};
             if (some) {
@@ -514,7 +544,7 @@ __global__ void __launch_bounds__(RowLane<LANES, CL>::kThreads, LANES > 32 ? 512
                 for (int e = 0; e < N; ++e) w[e] = mul2(w[e], x[e]);
                 pl.get(j & 1, 2, i, x);
                 if (!whole) { mask(u, lo, hi, 0.f); mask(w, lo, hi, 0.f); mask(x, lo, hi, no_decay<DECAY>()); }
-                decays<DECAY, FAST>(x, a, na, own.A, own.P);
+                decays<DECAY>(x, a, na, own.A, own.P);
                 rev.A = own.A; rev.P = own.P;
 #pragma unroll
                 for (int e = 0; e < N; ++e) own.S = fmaf(a[e].y, fmaf(a[e].x, own.S, u[e].x), u[e].y);
@@ -527,11 +557,10 @@ __global__ void __launch_bounds__(RowLane<LANES, CL>::kThreads, LANES > 32 ? 512
                 ahead.leave(along, met);
                 behind.leave(back, met);
                 __syncthreads();
-                if (CL == 1 && met) mu = back.carry[(met - 1) & 1];
+                if (STAGED || met) mu = back.carry[(met - 1) & 1];
             }
-            bool fine = true;
-            float s = ahead.enter(along, met, 0, from, fine);
-            float m = behind.enter(back, met, rank, mu, pl.ok);
+            float s = ahead.enter(along, met, from);
+            float m = behind.enter(back, met, mu);
             auto put = [&](T *to, int place, f2 (&f)[N]) {
                 if (!whole) mask(f, lo, hi, 0.f);
                 if (r.real) pl.put(j & 1, place, to, r.start + first(j), first(j), i, t0, p.L, f);
@@ -573,7 +602,7 @@ __global__ void __launch_bounds__(RowLane<LANES, CL>::kThreads, LANES > 32 ? 512
                 for (int e = 0; e < N; ++e) x[e] = mul2(x[e], w[e]);
             }
             put((T *)p.dv, 0, x);
-            if (LANES > 32 && CL == 1 && threadIdx.x == 0) back.carry[met & 1] = mu = m;
+            if (LANES > 32 && threadIdx.x == 0) back.carry[met & 1] = mu = m;
         } else if (r.real) {
             f2 zero[N];
 #pragma unroll
@@ -585,10 +614,10 @@ __global__ void __launch_bounds__(RowLane<LANES, CL>::kThreads, LANES > 32 ? 512
         }
         pl.put_done();
     }
-    if (r.real && p.ds0 && r.l == 0) { HN_G(p.ds0 + r.row, 4); p.ds0[r.row] = mu; }
+    if (STAGED && LANES > 32 && r.first >= r.live) { __syncthreads(); mu = back.carry[1]; }
+    if (r.real && p.ds0 && r.segment == 0 && r.l == 0) { HN_G(p.ds0 + r.row, 4); p.ds0[r.row] = mu; }
     if (STAGED && pl.lane == 0) tma_wait_all0();
     if (!pl.ok) atomicExch(&hn_rec_status, 1);
-    if constexpr (CL > 1) cg::this_cluster().sync();
 }
 
 // One token: a thread per channel.
@@ -607,7 +636,7 @@ template <typename T, int DECAY> __global__ void __launch_bounds__(256) recurren
     }
     if (in) {
         float a, na;
-        decay<DECAY, false>(IO<T>::ld((const T *)p.g, i), a, na);
+        decay<DECAY>(IO<T>::ld((const T *)p.g, i), a, na);
         s = fmaf(a, s, IO<T>::ld((const T *)p.k, i) * IO<T>::ld((const T *)p.v, i));
         out = IO<T>::ld((const T *)p.q, i) * s;
     }
@@ -615,32 +644,36 @@ template <typename T, int DECAY> __global__ void __launch_bounds__(256) recurren
     if (p.s_end) { HN_G(p.s_end + i, 4); p.s_end[i] = s; }
 }
 
-template <auto FN, int LANES, int CL, int BYTES> static int launch_rows(const RecArgs &a, cudaStream_t st)
+template <auto FN, int LANES, int BYTES> static int launch_rows(const RecArgs &a, cudaStream_t st)
 {
-    using R = RowLane<LANES, CL>;
-    const long long blocks = (a.rows + R::kRows - 1) / R::kRows * CL;
+    using R = RowLane<LANES>;
+    const long long blocks = (a.rows + R::kRows - 1) / R::kRows * a.segments;
     if (blocks > 0x7fffffffll) return -1;
     static DevOnce attr;
     if (BYTES > 32 * 1024 && attr.first() && cudaFuncSetAttribute(FN, cudaFuncAttributeMaxDynamicSharedMemorySize, BYTES) != cudaSuccess) return -1;
-    if constexpr (CL == 1) {
-        launch_pdl(FN, dim3((unsigned)blocks), R::kThreads, BYTES, st, a);
-    } else {
-        cudaLaunchConfig_t c{};
-        c.gridDim = dim3((unsigned)blocks); c.blockDim = dim3(R::kThreads); c.stream = st; c.dynamicSmemBytes = BYTES;
-        cudaLaunchAttribute at;
-        at.id = cudaLaunchAttributeClusterDimension;
-        at.val.clusterDim.x = CL; at.val.clusterDim.y = 1; at.val.clusterDim.z = 1;
-        c.attrs = &at; c.numAttrs = 1;
-        cudaLaunchKernelEx(&c, FN, a);
-    }
+    launch_pdl(FN, dim3((unsigned)blocks), R::kThreads, BYTES, st, a);
     return 0;
 }
-template <typename T, int DECAY, bool BWD, int OCT, int LANES, int CL> static int launch_lanes(const RecArgs &a, cudaStream_t st)
+template <typename T, int DECAY, bool BWD, int OCT, int LANES, bool STAGED> static int launch_lanes(const RecArgs &a, cudaStream_t st)
 {
-    constexpr int THREADS = RowLane<LANES, CL>::kThreads;
-    constexpr bool STAGED = LANES >= 128 || OCT == 2;
-    if constexpr (BWD) return launch_rows<recurrence_backward_kernel<T, DECAY, OCT, LANES, CL>, LANES, CL, 2 * Places<T, OCT, 5, THREADS, STAGED>::STAGE>(a, st);
-    else return launch_rows<recurrence_forward_kernel<T, DECAY, OCT, LANES, CL>, LANES, CL, 2 * Places<T, OCT, 4, THREADS, STAGED>::STAGE>(a, st);
+    constexpr int THREADS = RowLane<LANES>::kThreads;
+    if constexpr (STAGED && LANES == 32)
+        if (a.segments > 1 && launch_rows<recurrence_maps_kernel<T, DECAY, OCT, !BWD>, LANES, 2 * Places<T, OCT, 3, THREADS, true>::STAGE>(a, st)) return -1;
+    if constexpr (BWD) return launch_rows<recurrence_backward_kernel<T, DECAY, OCT, LANES, STAGED>, LANES, 2 * Places<T, OCT, 5, THREADS, STAGED>::STAGE>(a, st);
+    else return launch_rows<recurrence_forward_kernel<T, DECAY, OCT, LANES, STAGED>, LANES, 2 * Places<T, OCT, 4, THREADS, STAGED>::STAGE>(a, st);
+}
+
+// Rows that leave places free are cut into segments, one warp each, as many as run at once: the second reading of two (backward: three)
+// tensors costs less than the idle places, forward below 128 rows, backward below two an SM.  64 rows of 65536, bf16: 22 and 28 us,
+// whole rows 34 and 82; 180 rows of 262144: 148 and 202, whole 139 and 348; 256 rows of 65536, fp32: 105 and 142, whole 68 and 166.  A row of
+// fewer than 32 tiles of a warp is walked as fast by one CTA (20 rows of 5000, bf16: 8 and 12 us, in segments 13 and 15).
+static int segments_of(long long rows, int L, int dtype, bool backward)
+{
+    const int tile = 32 * (dtype == HYENAND_F32 ? 8 : 16);
+    const long long tiles = ((long long)L + (L % 8 ? 7 : 0) + tile - 1) / tile, places = (backward ? 512 : 768) / 32 * kSms;
+    if (rows >= (backward ? 2 * kSms : 128) || tiles < 32) return 1;
+    const long long n = places / rows, most = tiles / 2;
+    return (int)(n < most ? n : most);
 }
 
 // Lanes of a row: as few as hold it in one tile, a CTA that walks it where it is longer.
@@ -648,30 +681,29 @@ template <typename T, int DECAY, bool BWD> static int launch_recurrence_td(const
 {
     constexpr int LONG = sizeof(T) == 2 ? 2 : 1;             // octets of a thread where a row is long
     const int octets = (a.L + (a.L % 8 ? 7 : 0) + 7) / 8;    // that a row touches, wherever in one it starts
-#define HN_REC(OCT, LANES, CL) return launch_lanes<T, DECAY, BWD, OCT, LANES, CL>(a, st)
-    if (octets <= 4) HN_REC(1, 4, 1);
-    if (octets <= 8) HN_REC(1, 8, 1);
-    if (octets <= 16) HN_REC(1, 16, 1);
-    if (octets <= 32) HN_REC(1, 32, 1);
-    if (octets <= 64) HN_REC(1, 64, 1);
-    if constexpr (LONG == 2) if (octets <= 128) HN_REC(2, 64, 1);
+#define HN_REC(OCT, LANES, STAGED) return launch_lanes<T, DECAY, BWD, OCT, LANES, STAGED>(a, st)
+    if (octets <= 4) HN_REC(1, 4, false);
+    if (octets <= 8) HN_REC(1, 8, false);
+    if (octets <= 16) HN_REC(1, 16, false);
+    if (octets <= 32) HN_REC(1, 32, false);
+    if (octets <= 64) HN_REC(1, 64, false);
+    if (a.segments > 1) HN_REC(LONG, 32, true);
+    if constexpr (LONG == 2) if (octets <= 128) HN_REC(2, 64, true);
     const int threads = (octets + LONG - 1) / LONG;
     // Rows that fill the GPU: one CTA each, of as many lanes as still lets all of them run at once (768 threads an SM forward, 512
-    // backward), and small CTAs where they come in several waves anyhow.  512 rows of 65536, bf16, forward: 128 lanes 73 us, 192 70,
-    // 256 (a second wave of 68) 86; backward 119, 145, 129.  12288 rows of 2000: 64 lanes 54 and 107 us, 128 (one tile, nothing travels
-    // ahead) 62 and 118.
+    // backward), and small ones where they come in several waves anyhow.  512 rows of 65536, bf16, forward: 128 lanes 73 us, 192 70,
+    // 256 (a second wave of 68) 86; backward 119, 145, 129.  12288 rows of 2000, bf16: 32 lanes 53 and 94 us, 64 55 and 107, 128 (one
+    // tile, nothing travels ahead) 62 and 118; of 1531, fp32: 32 lanes 72 and 126, 128 76 and 144.  8192 rows of 8192, bf16: 32 lanes
+    // 123 and 211, 64 117 and 197, 128 115 and 211.
+    constexpr int PLACES = BWD ? 512 : 768;
+    if (threads <= 128 && a.rows >= PLACES / 64 * kSms) HN_REC(LONG, 32, true);
     if constexpr (LONG == 2) {
-        if (threads <= 128 && a.rows >= 12 * kSms) HN_REC(LONG, 64, 1);
-        if constexpr (!BWD) if (threads > 128 && a.rows > 3 * kSms && a.rows <= 4 * kSms) HN_REC(LONG, 192, 1);
+        if (a.rows >= PLACES / 64 * kSms) HN_REC(LONG, 64, true);
+        if constexpr (!BWD) if (threads > 128 && a.rows > 3 * kSms && a.rows <= 4 * kSms) HN_REC(LONG, 192, true);
     }
-    if (threads <= 128) HN_REC(LONG, 128, 1);
-    const bool two = BWD ? a.rows > 4 * kSms && a.rows <= 8 * kSms : a.rows >= 2 * kSms && a.rows <= 3 * kSms;
-    if (!two && a.rows >= 2 * kSms) HN_REC(LONG, 128, 1);
-    if (threads <= 256 || two) HN_REC(LONG, 256, 1);
-    // fewer: clusters of as many CTAs as bring one to every SM (128 rows of 65536, bf16: two 31 and 41 us, four 35 and 47)
-    if (threads <= 512 || a.rows * 2 >= kSms) HN_REC(LONG, 256, 2);
-    if (threads <= 1024 || a.rows * 4 >= kSms) HN_REC(LONG, 256, 4);
-    HN_REC(LONG, 256, 8);
+    const bool two = BWD ? a.rows > 4 * kSms && a.rows <= 8 * kSms : a.rows <= 3 * kSms;
+    if (threads <= 128 || !two) HN_REC(LONG, 128, true);
+    HN_REC(LONG, 256, true);
 #undef HN_REC
 }
 
@@ -721,6 +753,13 @@ using namespace hn;
 
 extern "C" long long hyenand_recurrence_marks(int L) { return L < 1 || L > (1 << 30) ? 0 : marks_of(L); }
 
+extern "C" long long hyenand_recurrence_workspace_bytes(int B, int C, int L, int dtype)
+{
+    if (B < 1 || C < 1 || L < 1 || L > (1 << 30)) return 0;
+    const long long rows = (long long)B * C, f = segments_of(rows, L, dtype, false), b = segments_of(rows, L, dtype, true), most = f > b ? f : b;
+    return most > 1 ? rows * most * (long long)sizeof(float4) : 0;
+}
+
 extern "C" int hyenand_recurrence_device_status(void)
 {
     int v = 0;
@@ -730,7 +769,7 @@ extern "C" int hyenand_recurrence_device_status(void)
 
 extern "C" int hyenand_recurrence_forward(int B, int C, int L, int decay, int dtype, const void *q, const void *k, const void *v,
                                           const void *g, const float *s0, const int *lengths, void *y, float *s_end, float *marks,
-                                          void *cuda_stream)
+                                          void *workspace, void *cuda_stream)
 {
     clear_error();
     if (int e = check_shape(B, C, L, decay, dtype)) return e;
@@ -738,11 +777,14 @@ extern "C" int hyenand_recurrence_forward(int B, int C, int L, int decay, int dt
     RecArgs a{};
     a.q = q; a.k = k; a.v = v; a.g = g; a.s0 = s0; a.lengths = lengths; a.y = y; a.s_end = s_end; a.marks = marks;
     a.rows = (long long)B * C; a.n = a.rows * L; a.C = C; a.L = L; a.marks_row = marks_of(L);
+    a.segments = segments_of(a.rows, L, dtype, false); a.maps = (float4 *)workspace;
+    if (a.segments > 1 && !workspace) return fail(HYENAND_ERR_INVALID_ARG, "workspace must be non-NULL for this shape");
     CallTensors c;
     const size_t nb = (size_t)a.n * elsize(dtype), rb = (size_t)a.rows * sizeof(float);
     c.in("q", q, nb); c.in("k", k, nb); c.in("v", v, nb); c.in("g", g, nb);
     c.in("s0", s0, rb, 4); c.in("lengths", lengths, (size_t)B * sizeof(int), 4);
     c.out("y", y, nb); c.out("s_end", s_end, rb, 4, s0); c.out("marks", marks, rb * a.marks_row, 4);
+    if (a.segments > 1) c.out("workspace", workspace, (size_t)a.rows * a.segments * sizeof(float4));
     if (int e = c.check()) return e;
     c.register_ranges();
     return finish(launch_recurrence<false>(a, decay, dtype, (cudaStream_t)cuda_stream));
@@ -750,7 +792,7 @@ extern "C" int hyenand_recurrence_forward(int B, int C, int L, int decay, int dt
 
 extern "C" int hyenand_recurrence_backward(int B, int C, int L, int decay, int dtype, const void *q, const void *k, const void *v,
                                            const void *g, const int *lengths, const float *marks, const void *dy, const float *ds_end,
-                                           void *dq, void *dk, void *dv, void *dg, float *ds0, void *cuda_stream)
+                                           void *dq, void *dk, void *dv, void *dg, float *ds0, void *workspace, void *cuda_stream)
 {
     clear_error();
     if (int e = check_shape(B, C, L, decay, dtype)) return e;
@@ -760,11 +802,14 @@ extern "C" int hyenand_recurrence_backward(int B, int C, int L, int decay, int d
     a.q = q; a.k = k; a.v = v; a.g = g; a.lengths = lengths; a.marks = (float *)marks; a.dy = dy; a.ds_end = ds_end;
     a.dq = dq; a.dk = dk; a.dv = dv; a.dg = dg; a.ds0 = ds0;
     a.rows = (long long)B * C; a.n = a.rows * L; a.C = C; a.L = L; a.marks_row = marks_of(L);
+    a.segments = segments_of(a.rows, L, dtype, true); a.maps = (float4 *)workspace;
+    if (a.segments > 1 && !workspace) return fail(HYENAND_ERR_INVALID_ARG, "workspace must be non-NULL for this shape");
     CallTensors c;
     const size_t nb = (size_t)a.n * elsize(dtype), rb = (size_t)a.rows * sizeof(float);
     c.in("q", q, nb); c.in("k", k, nb); c.in("v", v, nb); c.in("g", g, nb); c.in("dy", dy, nb);
     c.in("lengths", lengths, (size_t)B * sizeof(int), 4); c.in("marks", marks, rb * a.marks_row, 4); c.in("ds_end", ds_end, rb, 4);
     c.out("dq", dq, nb); c.out("dk", dk, nb); c.out("dv", dv, nb); c.out("dg", dg, nb); c.out("ds0", ds0, rb, 4, ds_end);
+    if (a.segments > 1) c.out("workspace", workspace, (size_t)a.rows * a.segments * sizeof(float4));
     if (int e = c.check()) return e;
     c.register_ranges();
     return finish(launch_recurrence<true>(a, decay, dtype, (cudaStream_t)cuda_stream));
@@ -779,7 +824,7 @@ extern "C" int hyenand_recurrence_step(int B, int C, int decay, int dtype, const
         return fail(HYENAND_ERR_INVALID_ARG, "q, k, v, g, state, y, new_state must be non-NULL");
     RecArgs a{};
     a.q = q; a.k = k; a.v = v; a.g = g; a.s0 = state; a.lengths = active; a.y = y; a.s_end = new_state;
-    a.rows = a.n = (long long)B * C; a.C = C; a.L = 1;
+    a.rows = a.n = (long long)B * C; a.C = C; a.L = 1; a.segments = 1;
     CallTensors c;
     const size_t nb = (size_t)a.n * elsize(dtype), rb = (size_t)a.rows * sizeof(float);
     c.in("q", q, nb); c.in("k", k, nb); c.in("v", v, nb); c.in("g", g, nb);

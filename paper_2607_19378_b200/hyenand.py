@@ -110,8 +110,10 @@ def lib() -> ctypes.CDLL:
         ci, cf = ctypes.c_int, ctypes.c_float
         L.hyenand_recurrence_marks.restype = ll
         L.hyenand_recurrence_marks.argtypes = [ci]
-        L.hyenand_recurrence_forward.argtypes = [ci] * 5 + [vp] * 10
-        L.hyenand_recurrence_backward.argtypes = [ci] * 5 + [vp] * 14
+        L.hyenand_recurrence_forward.argtypes = [ci] * 5 + [vp] * 11
+        L.hyenand_recurrence_backward.argtypes = [ci] * 5 + [vp] * 15
+        L.hyenand_recurrence_workspace_bytes.restype = ll
+        L.hyenand_recurrence_workspace_bytes.argtypes = [ci] * 4
         L.hyenand_recurrence_step.argtypes = [ci] * 4 + [vp] * 9
         L.hyenand_block_workspace_bytes.restype = ll
         L.hyenand_block_workspace_bytes.argtypes = [ci] * 4
@@ -362,20 +364,25 @@ def hyenand_recurrence_marks(L: int) -> int:
     return int(lib().hyenand_recurrence_marks(int(L)))
 
 
+def hyenand_recurrence_workspace_bytes(B: int, C: int, L: int, dtype: int) -> int:
+    return int(lib().hyenand_recurrence_workspace_bytes(B, C, L, dtype))
+
+
 def hyenand_recurrence_device_status() -> int:
     return int(lib().hyenand_recurrence_device_status())
 
 
-def hyenand_recurrence_forward(B: int, C: int, L: int, decay: int, dtype: int, q, k, v, g, s0, lengths, y, s_end, marks, stream=None) -> None:
+def hyenand_recurrence_forward(B: int, C: int, L: int, decay: int, dtype: int, q, k, v, g, s0, lengths, y, s_end, marks, workspace=None,
+                               stream=None) -> None:
     _check(lib().hyenand_recurrence_forward(B, C, L, decay, dtype, q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), _ptr(s0),
-                                            _ptr(lengths), y.data_ptr(), _ptr(s_end), _ptr(marks), _stream_ptr(stream)))
+                                            _ptr(lengths), y.data_ptr(), _ptr(s_end), _ptr(marks), _ptr(workspace), _stream_ptr(stream)))
 
 
 def hyenand_recurrence_backward(B: int, C: int, L: int, decay: int, dtype: int, q, k, v, g, lengths, marks, dy, ds_end, dq, dk, dv, dg, ds0,
-                                stream=None) -> None:
+                                workspace=None, stream=None) -> None:
     _check(lib().hyenand_recurrence_backward(B, C, L, decay, dtype, q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), _ptr(lengths),
                                              marks.data_ptr(), dy.data_ptr(), _ptr(ds_end), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
-                                             dg.data_ptr(), _ptr(ds0), _stream_ptr(stream)))
+                                             dg.data_ptr(), _ptr(ds0), _ptr(workspace), _stream_ptr(stream)))
 
 
 def hyenand_recurrence_step(B: int, C: int, decay: int, dtype: int, q, k, v, g, state, active, y, new_state, stream=None) -> None:
@@ -567,8 +574,9 @@ class Recurrence:
         if min(self.B, self.C, marks) < 1:
             raise ValueError("B and C must be >= 1, L between 1 and 2^30")
         self._ops = _calls()
-        self._handle = self._ops.make_recurrence(self.B, self.C, self.L, marks, code, _DTYPES[dtype], _address("hyenand_recurrence_forward"),
-                                                 _address("hyenand_recurrence_backward"), _address("hyenand_recurrence_step"), _check)
+        self._handle = self._ops.make_recurrence(self.B, self.C, self.L, marks, code, _DTYPES[dtype],
+                                                 hyenand_recurrence_workspace_bytes(self.B, self.C, self.L, _DTYPES[dtype]),
+                                                 _address("hyenand_recurrence_forward"), _address("hyenand_recurrence_backward"), _address("hyenand_recurrence_step"), _check)
 
     def forward(self, q, k, v, g, s0=None, lengths=None, marks: bool = False, y=None, stream=None):
         """(y, state behind the row), and with marks=True what `backward` needs of this call as a third."""

@@ -45,10 +45,11 @@ def run(t, L, B, C, dtype, decay):
     bands = {n: guarded(d["q"]) for n in ("y", "dq", "dk", "dv", "dg")}
     bands.update({n: guarded(t["ds"]) for n in ("s_end", "ds0")})
     bands["marks"] = guarded(torch.empty(B, C, hn.hyenand_recurrence_marks(L)))
+    bands["work"] = guarded(torch.empty(hn.hyenand_recurrence_workspace_bytes(B, C, L, head[4]) // 4))
     o = {n: b[1] for n, b in bands.items()}
-    hn.hyenand_recurrence_forward(*head, d["q"], d["k"], d["v"], d["g"], d["s0"], d["lengths"], o["y"], o["s_end"], o["marks"])
+    hn.hyenand_recurrence_forward(*head, d["q"], d["k"], d["v"], d["g"], d["s0"], d["lengths"], o["y"], o["s_end"], o["marks"], o["work"])
     hn.hyenand_recurrence_backward(*head, d["q"], d["k"], d["v"], d["g"], d["lengths"], o["marks"], d["dy"], d["ds"], o["dq"], o["dk"], o["dv"],
-                                   o["dg"], o["ds0"])
+                                   o["dg"], o["ds0"], o["work"])
     assert hn.hyenand_recurrence_device_status() == 0, "a kernel gave up a bounded wait"
     for n, (big, x) in bands.items():
         assert bool((big[:256] == 7.0).all()) and bool((big[256 + x.numel():] == 7.0).all()), f"a kernel wrote outside {n}"
@@ -81,7 +82,8 @@ def test_lengths(L, decay, dtype):
 
 
 @pytest.mark.parametrize("dtype,decay", [("f32", "log"), ("bf16", "sigmoid"), ("f32", "value")])
-@pytest.mark.parametrize("B,C,L", [(7, 3, 13), (5, 4, 100), (6, 3, 700), (4, 3, 5003), (3, 200, 2050), (2, 300, 1029), (1, 160, 2500)], ids=str)
+@pytest.mark.parametrize("B,C,L", [(7, 3, 13), (5, 4, 100), (6, 3, 700), (4, 3, 5003), (3, 200, 2050), (2, 300, 1029), (1, 160, 2500), (7, 2, 20011), (1, 199, 9000),
+                                   (1, 205, 9001), (3, 150, 6000), (4, 160, 8200)], ids=str)
 def test_padded_batches(B, C, L, dtype, decay):
     check(B, C, L, dtype, decay, seed=B * L, ragged=True)
 
@@ -104,7 +106,7 @@ def test_values_behind_an_entry_are_not_looked_at():
             t[n][b, :, m:] = bad
     got = run(t, L, B, C, torch.float32, "log")
     for n in clean:
-        if n != "marks":
+        if n not in ("marks", "work"):
             assert torch.equal(clean[n], got[n]), n
     assert float(got["y"][0].abs().max()) == 0 and torch.equal(got["s_end"][0], t["s0"][0]) and torch.equal(got["ds0"][4], t["ds"][4])
     assert float(got["dg"][1, :, 1:].abs().max()) == 0
@@ -179,9 +181,10 @@ def test_state_in_place_and_results_repeat():
         y, end, marks = op.forward(t["q"], t["k"], t["v"], t["g"], s0=t["s0"], marks=True)
         grads = op.backward(t["q"], t["k"], t["v"], t["g"], marks, t["dy"], ds_end=t["ds"])
         buf, y2 = t["s0"].clone(), torch.empty_like(y)
-        hn.hyenand_recurrence_forward(B, C, L, 1, 1, t["q"], t["k"], t["v"], t["g"], buf, None, y2, buf, None)
+        work = torch.empty(hn.hyenand_recurrence_workspace_bytes(B, C, L, 1), dtype=torch.uint8, device="cuda")
+        hn.hyenand_recurrence_forward(B, C, L, 1, 1, t["q"], t["k"], t["v"], t["g"], buf, None, y2, buf, None, work)
         dbuf, outs = t["ds"].clone(), [torch.empty_like(y) for _ in range(4)]
-        hn.hyenand_recurrence_backward(B, C, L, 1, 1, t["q"], t["k"], t["v"], t["g"], None, marks, t["dy"], dbuf, *outs, dbuf)
+        hn.hyenand_recurrence_backward(B, C, L, 1, 1, t["q"], t["k"], t["v"], t["g"], None, marks, t["dy"], dbuf, *outs, dbuf, work)
         torch.cuda.synchronize()
         assert torch.equal(y, y2) and torch.equal(end, buf) and all(torch.equal(a, b) for a, b in zip(grads, outs + [dbuf]))
         zero, full = torch.zeros_like(t["s0"]), torch.full((B,), L, dtype=torch.int32, device="cuda")

@@ -21,7 +21,7 @@ def refused(hn, code, word):
 
 
 def forward_args(**kw):
-    a = dict(B=2, C=3, L=40, decay=1, dtype=0, q=A[0], k=A[1], v=A[2], g=A[3], s0=None, lengths=None, y=A[4], s_end=None, marks=None, stream=None)
+    a = dict(B=2, C=3, L=40, decay=1, dtype=0, q=A[0], k=A[1], v=A[2], g=A[3], s0=None, lengths=None, y=A[4], s_end=None, marks=None, workspace=None, stream=None)
     a.update(kw)
     return list(a.values())
 
@@ -31,7 +31,8 @@ def forward_args(**kw):
     (dict(B=1 << 15, C=(1 << 13) + 1, L=1), "2^28"), (dict(decay=3), "decay"), (dict(decay=-1), "decay"), (dict(dtype=2), "dtype"),
     (dict(q=None), "non-NULL"), (dict(g=None), "non-NULL"), (dict(y=None), "non-NULL"), (dict(v=A[2] + 8), "aligned"), (dict(s0=A[5] + 2), "aligned"),
     (dict(y=A[0]), "overlaps"), (dict(y=A[3] + 944), "overlaps"), (dict(s_end=A[4] + 16), "overlaps"), (dict(s0=A[5], s_end=A[5] + 4), "overlaps"),
-    (dict(marks=A[2] - 16), "overlaps"), (dict(lengths=A[6], s_end=A[6]), "overlaps")], ids=str)
+    (dict(marks=A[2] - 16), "overlaps"), (dict(lengths=A[6], s_end=A[6]), "overlaps"),
+    (dict(L=100000), "workspace"), (dict(L=100000, workspace=A[7] + 8), "aligned"), (dict(L=100000, workspace=A[3]), "overlaps")], ids=str)
 def test_recurrence_forward_refuses(hn, change, word):
     refused(hn, hn.lib().hyenand_recurrence_forward(*forward_args(**change)), word)
 
@@ -41,7 +42,7 @@ def test_recurrence_forward_refuses(hn, change, word):
     (dict(ds0=A[5]), "overlaps"), (dict(dy=A[6] + 4), "aligned"), (dict(L=0), "B, C and L")], ids=str)
 def test_recurrence_backward_refuses(hn, change, word):
     a = dict(B=2, C=3, L=40, decay=2, dtype=1, q=A[0], k=A[1], v=A[2], g=A[3], lengths=None, marks=A[5], dy=A[6], ds_end=None, dq=A[7], dk=A[8],
-             dv=A[9], dg=A[10], ds0=None, stream=None)
+             dv=A[9], dg=A[10], ds0=None, workspace=None, stream=None)
     a.update(change)
     refused(hn, hn.lib().hyenand_recurrence_backward(*a.values()), word)
 
@@ -90,7 +91,9 @@ def test_dropout_refuses(hn, change, word):
 
 
 def test_sizes(hn):
-    assert [hn.hyenand_recurrence_marks(L) for L in (0, 1, 1017, 1018, 2041, 2042, 1 << 30, (1 << 30) + 1)] == [0, 1, 1, 2, 2, 3, (1 << 20) + 1, 0]
+    assert [hn.hyenand_recurrence_marks(L) for L in (0, 1, 249, 250, 505, 506, 1 << 30, (1 << 30) + 1)] == [0, 1, 1, 2, 2, 3, (1 << 22) + 1, 0]
+    assert [hn.hyenand_recurrence_workspace_bytes(*a) for a in ((1, 24, 0, 0), (1, 0, 9, 0), (1, 24, 1000, 0), (64, 64, 1 << 20, 1))] == [0] * 4
+    assert 16 * 24 * 2 <= hn.hyenand_recurrence_workspace_bytes(1, 24, 100003, 0) <= 1 << 16
     assert hn.hyenand_block_workspace_bytes(1, 8, 4, 0) >= 3 * 8 * 4 and hn.hyenand_block_workspace_bytes(1, 0, 4, 0) == 0
 
 
