@@ -317,7 +317,8 @@ int hyenand_recurrence_device_status(void);
  * x, m, z, r, n: [B][C][T] of one dtype, DEVICE pointers, 16-byte aligned; z is NULL exactly where gate is HYENAND_GATE_NONE.
  * g_post, scale, g_pre: C fp32 weights on the device; NULL leaves out the first norm, the scale, or n with its norm.  p = 0: no
  * dropout, rng may be NULL.  stats: NULL, or 2 B T floats that the backward pass needs.  All arithmetic is fp32; n is formed
- * before r is rounded.  eps > 0.  Errors and stream as hyenand_forward_ex; no call allocates, synchronises or keeps anything.
+ * before r is rounded.  eps > 0.  Limits: T <= 2^30, C <= 2^20, B C T <= 2^40.  Errors and stream as hyenand_forward_ex; no call
+ * allocates, synchronises or keeps anything.
  */
 enum { HYENAND_GATE_NONE = 0, HYENAND_GATE_SIGMOID = 1, HYENAND_GATE_SILU = 2 };
 int hyenand_block_forward(int B, int C, int T, int dtype, const void *x, const void *m, const void *z, const float *g_post,

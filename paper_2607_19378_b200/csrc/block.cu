@@ -16,7 +16,6 @@
 // Any number of channels: a CTA takes a tile of neighbouring tokens, its warps share the channels, and what a second walk needs is
 // read again (from the caches).
 #include "block.cuh"
-#include "entry.cuh"
 
 namespace hn {
 
@@ -309,6 +308,8 @@ static int check_block(int B, int C, int T, int dtype, const void *x, const void
                        const long long *rng, int site, BlockArgs *a)
 {
     if (B < 1 || C < 1 || T < 1) return fail(HYENAND_ERR_INVALID_ARG, "B, C and T must be >= 1");
+    if (T > (1 << 30) || C > (1 << 20) || (long long)B * T > (1ll << 40) / C)
+        return fail(HYENAND_ERR_UNSUPPORTED, "T is above 2^30, C above 2^20 or B C T above 2^40");
     if (dtype != HYENAND_F32 && dtype != HYENAND_BF16) return fail(HYENAND_ERR_INVALID_ARG, "unknown dtype %d", dtype);
     if (gate < GATE_NONE || gate > GATE_SILU) return fail(HYENAND_ERR_INVALID_ARG, "unknown gate %d", gate);
     if (!x || !m) return fail(HYENAND_ERR_INVALID_ARG, "x and m must be non-NULL");
@@ -360,8 +361,10 @@ extern "C" int hyenand_block_forward(int B, int C, int T, int dtype, const void 
 
 extern "C" long long hyenand_block_workspace_bytes(int B, int C, int T, int dtype)
 {
-    (void)B; (void)T; (void)dtype;
-    return C < 1 ? 0 : (long long)kBlockSlots * 3 * C * (long long)sizeof(float);
+    (void)dtype;
+    if (B < 1 || C < 1 || T < 1) return 0;
+    const long long tiles = (long long)B * (((long long)T + 31) / 32);       // (no kernel's are smaller)
+    return (tiles < kBlockSlots ? tiles : kBlockSlots) * 3 * C * (long long)sizeof(float);
 }
 
 extern "C" int hyenand_block_device_status(void)

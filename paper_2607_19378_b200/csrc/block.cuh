@@ -3,6 +3,7 @@
 #include <cooperative_groups.h>
 
 #include "common.cuh"
+#include "entry.cuh"
 #include "octet.cuh"
 #include "pair.cuh"
 #include "philox.cuh"
@@ -181,16 +182,19 @@ template <typename T, bool ALIGNED> __device__ __forceinline__ void st_vector(vo
 // out every other channel's and they exchange them.
 template <int N> __device__ __forceinline__ void keep_bits(const DropKey &key, bool paired, long long start, long long hop, unsigned (&keep)[N])
 {
-    if (N % 2 == 0 && paired) {
-        const int odd = threadIdx.x & 1;
+    if constexpr (N % 2 == 0)
+        if (paired) {
+            const int odd = threadIdx.x & 1;
+            uint4 w[N / 2];
+            key.words((start + odd * hop) >> 3, hop >> 2, w);
 #pragma unroll
-        for (int j = 0; j < N; j += 2) {
-            const unsigned own = key.keep((start + (j + odd) * hop) >> 3), other = __shfl_xor_sync(~0u, own, 1);
-            keep[j] = (odd ? other : own) >> (4 * odd);
-            keep[j + (N > 1)] = (odd ? own : other) >> (4 * odd);
+            for (int j = 0; j < N; j += 2) {
+                const unsigned own = key.bits(w[j / 2]), other = __shfl_xor_sync(~0u, own, 1);
+                keep[j] = (odd ? other : own) >> (4 * odd);
+                keep[j + 1] = (odd ? own : other) >> (4 * odd);
+            }
+            return;
         }
-        return;
-    }
 #pragma unroll
     for (int j = 0; j < N; ++j) {
         const long long i = start + j * hop;
@@ -332,9 +336,7 @@ int launch_block_tile_backward(const BlockArgs &a, int dtype, const TileShape &s
 // where 90 fit: twice the time).
 template <auto FN, int BYTES> static int launch_tiles(const BlockArgs &a, const TileShape &s, cudaStream_t st)
 {
-    static DevOnce attr;
-    static int fit[64][kTileCtas + 1];                       // clusters that run at once, per device; 0: not asked yet
-    if (attr.first() && cudaFuncSetAttribute(FN, cudaFuncAttributeMaxDynamicSharedMemorySize, BYTES) != cudaSuccess) return -1;
+    static PerDevice fit[kTileCtas + 1];                     // clusters of so many CTAs that run at once
     cudaLaunchConfig_t c{};
     c.gridDim = dim3((unsigned)s.ctas); c.blockDim = dim3(kTileThreads); c.stream = st; c.dynamicSmemBytes = BYTES;
     cudaLaunchAttribute at[1];
@@ -346,22 +348,20 @@ template <auto FN, int BYTES> static int launch_tiles(const BlockArgs &a, const 
         at[0].val.programmaticStreamSerializationAllowed = 1;
     }
     c.attrs = at; c.numAttrs = 1;
-    int dev = 0;
-    cudaGetDevice(&dev);
-    int &most = fit[dev & 63][s.ctas];
-    if (!most) {
-        int n = 0;
+    const int most = fit[s.ctas].get([&] {
+        int n = 0, dev = 0, sms = kSms;
+        if (cudaFuncSetAttribute(FN, cudaFuncAttributeMaxDynamicSharedMemorySize, BYTES) != cudaSuccess) return -1;
         if (s.ctas > 1) {
             if (cudaOccupancyMaxActiveClusters(&n, FN, &c) != cudaSuccess) return -1;
         } else {
-            int sms = kSms;
+            cudaGetDevice(&dev);
             cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
             if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, FN, kTileThreads, BYTES) != cudaSuccess) return -1;
             n *= sms;
         }
-        if (n < 1) return -1;
-        most = n < kBlockSlots ? n : kBlockSlots;
-    }
+        return n < 1 ? -1 : n < kBlockSlots ? n : kBlockSlots;
+    });
+    if (most < 1) return -1;
     const long long clusters = a.tiles < most ? a.tiles : most;
     c.gridDim = dim3((unsigned)(clusters * s.ctas));
     return cudaLaunchKernelEx(&c, FN, a, s.ctas) == cudaSuccess ? (int)clusters : -1;

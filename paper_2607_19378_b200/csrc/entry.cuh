@@ -3,6 +3,8 @@
 #pragma once
 #include <stdint.h>
 
+#include <mutex>
+
 #include "../../include/hyenand.h"
 #include "common.cuh"
 
@@ -12,6 +14,22 @@ int fail(int code, const char *fmt, ...);            // records the message for 
 void clear_error();                                  // at the head of every entry point
 
 static inline size_t elsize(int dtype) { return dtype == HYENAND_F32 ? 4 : 2; }
+
+// What a launch works out once per device (a kernel's limits, how many of its CTAs run at once), whichever thread comes first.
+struct PerDevice {
+    std::mutex lock;
+    int value[64] = {0};                             // 0: not worked out yet
+    template <typename F> int get(F f)               // f() > 0, or -1: it failed, and is tried again at the next call
+    {
+        int dev = 0;
+        cudaGetDevice(&dev);
+        std::lock_guard<std::mutex> hold(lock);
+        int &v = value[dev & 63];
+        if (v <= 0) v = f();
+        return v;
+    }
+    template <typename F> bool once(F f) { return get(f) > 0; }
+};
 
 // Checked build: the address ranges a call may touch (the caller's tensors, the device allocations of the objects
 // involved), handed to every translation unit before the call's kernels are enqueued.

@@ -48,11 +48,9 @@ struct DropKey {
     __device__ __forceinline__ bool low(unsigned w) const { return w << 16 >= threshold; }
     __device__ __forceinline__ bool high(unsigned w) const { return w >= threshold; }
     // bit e set: element e of the octet stays
-    __device__ __forceinline__ unsigned keep(long long octet) const
+    __device__ __forceinline__ unsigned bits(const uint4 &w) const
     {
-        uint4 w[1];
-        words(octet, 0, w);
-        const unsigned v[4] = {w[0].x, w[0].y, w[0].z, w[0].w};
+        const unsigned v[4] = {w.x, w.y, w.z, w.w};
         unsigned m = 0;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -60,6 +58,12 @@ struct DropKey {
             if (high(v[j])) m |= 2u << (2 * j);
         }
         return m;
+    }
+    __device__ __forceinline__ unsigned keep(long long octet) const
+    {
+        uint4 w[1];
+        words(octet, 0, w);
+        return bits(w[0]);
     }
 };
 

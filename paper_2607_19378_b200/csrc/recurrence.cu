@@ -59,13 +59,13 @@ template <int DECAY> __device__ __forceinline__ void decay(float g, float &a, fl
     }
 }
 
-// exp(x) - 1 for x <= 0, given exp(x): the series where they are close to 0 and 1 (its first term left out is below 2^-24 of it)
+// exp(x) - 1, given exp(x): the series where they are close to 0 and 1 (its first term left out is below 2^-24 of it)
 __device__ __forceinline__ float expm1_of(float x, float ex)
 {
     float p = 1.f / 40320.f;
     p = fmaf(p, x, 1.f / 5040.f); p = fmaf(p, x, 1.f / 720.f); p = fmaf(p, x, 1.f / 120.f); p = fmaf(p, x, 1.f / 24.f);
     p = fmaf(p, x, 1.f / 6.f); p = fmaf(p, x, 0.5f); p = fmaf(p, x, 1.f);
-    return x > -0.5f ? p * x : ex - 1.f;
+    return fabsf(x) < 0.5f ? p * x : ex - 1.f;
 }
 
 // a and 1 - a of a thread's positions, and A, P of the whole.  Positions outside [lo, hi) are the identity: their gate is made one
@@ -649,8 +649,8 @@ template <auto FN, int LANES, int BYTES> static int launch_rows(const RecArgs &a
     using R = RowLane<LANES>;
     const long long blocks = (a.rows + R::kRows - 1) / R::kRows * a.segments;
     if (blocks > 0x7fffffffll) return -1;
-    static DevOnce attr;
-    if (BYTES > 32 * 1024 && attr.first() && cudaFuncSetAttribute(FN, cudaFuncAttributeMaxDynamicSharedMemorySize, BYTES) != cudaSuccess) return -1;
+    static PerDevice ready;
+    if (BYTES > 32 * 1024 && !ready.once([] { return cudaFuncSetAttribute(FN, cudaFuncAttributeMaxDynamicSharedMemorySize, BYTES) == cudaSuccess ? 1 : -1; })) return -1;
     launch_pdl(FN, dim3((unsigned)blocks), R::kThreads, BYTES, st, a);
     return 0;
 }

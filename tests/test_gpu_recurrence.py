@@ -130,6 +130,19 @@ def test_resets_and_extreme_gates(decay):
     compare(got, ref, L)
 
 
+def test_negative_and_growing_decays():
+    """Decays in [-1, 1], and above 1 over rows where nothing overflows (a product of 1.3 over 60 positions is 7e6; their roundings add
+    up as those of any product, 60 more of 2^-24)."""
+    for dtype in (torch.float32, torch.bfloat16):
+        t = inputs(2, 3, 700, dtype, "value", 14)
+        t["g"] = (2.0 * torch.rand(2, 3, 700, generator=torch.Generator().manual_seed(15)) - 1.0).to(dtype)
+        compare(run(t, 700, 2, 3, dtype, "value"), orec.recurrence(t["q"], t["k"], t["v"], t["g"], "value", t["s0"], None, t["dy"], t["ds"]), 700)
+        for decay, g in (("value", 1.3), ("log", 0.25)):
+            t = inputs(2, 3, 60, dtype, decay, 16)
+            t["g"].fill_(g)
+            compare(run(t, 60, 2, 3, dtype, decay), orec.recurrence(t["q"], t["k"], t["v"], t["g"], decay, t["s0"], None, t["dy"], t["ds"]), 60 + 64 * 60)
+
+
 @pytest.mark.parametrize("decay,g", [("log", -1e-6), ("log", -3e-5), ("sigmoid", 12.0), ("value", 1.0)])
 def test_long_memories(decay, g):
     """A constant decay next to 1 over a long row: the rounding of each a_t, always to one side, must not add up."""

@@ -59,7 +59,8 @@ BLOCK = dict(B=2, C=3, T=40, dtype=0, x=A[0], m=A[1], z=A[2], g_post=A[3], scale
 
 
 @pytest.mark.parametrize("change,word", [
-    (dict(B=0), "B, C and T"), (dict(T=0), "B, C and T"), (dict(dtype=5), "dtype"), (dict(gate=3), "gate"), (dict(gate=0), "z is given"), (dict(z=None), "z is given"),
+    (dict(B=0), "B, C and T"), (dict(T=0), "B, C and T"), (dict(T=(1 << 30) + 1), "2^30"), (dict(C=(1 << 20) + 1), "2^20"),
+    (dict(B=1 << 12, C=1 << 10, T=(1 << 18) + 1), "2^40"), (dict(dtype=5), "dtype"), (dict(gate=3), "gate"), (dict(gate=0), "z is given"), (dict(z=None), "z is given"),
     (dict(x=None), "x and m"), (dict(eps=0.0), "eps"), (dict(eps=-1.0), "eps"), (dict(eps=float("nan")), "eps"), (dict(eps=float("inf")), "eps"),
     (dict(p=1.0), "p must"), (dict(p=-0.1), "p must"), (dict(p=float("nan")), "p must"), (dict(rng=None), "rng"), (dict(r=None), "r must"),
     (dict(n=None), "n is given"), (dict(g_pre=None), "n is given"), (dict(r=A[0]), "overlaps"), (dict(n=A[7]), "overlaps"), (dict(stats=A[2]), "overlaps"),
