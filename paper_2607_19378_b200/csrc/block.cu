@@ -67,7 +67,8 @@ __device__ __forceinline__ void branch_of(const BlockArgs &p, const DropKey *key
     }
 }
 
-constexpr int kBlockWarps = 8;
+// warps of a CTA: many where a lane has one token, so that few tokens of many channels keep the GPU busy
+template <int V> constexpr int kBlockWarps = V == 1 ? 32 : 16;
 
 // sums[k][e] over the CTA's warps, for this lane's tokens
 template <int K, int V> __device__ __forceinline__ void sum_warps(float (&s)[K][V], float (*red)[K * 32 * V])
@@ -85,14 +86,14 @@ template <int K, int V> __device__ __forceinline__ void sum_warps(float (&s)[K][
         for (int e = 0; e < V; ++e) {
             float a = 0.f;
 #pragma unroll
-            for (int j = 0; j < kBlockWarps; ++j) a += red[j][(k * V + e) * 32 + lane];
+            for (int j = 0; j < kBlockWarps<V>; ++j) a += red[j][(k * V + e) * 32 + lane];
             s[k][e] = a;
         }
 }
 
-template <typename T, int V> __global__ void __launch_bounds__(kBlockWarps * 32) block_forward_kernel(BlockArgs p)
+template <typename T, int V> __global__ void __launch_bounds__(kBlockWarps<V> * 32) block_forward_kernel(BlockArgs p)
 {
-    __shared__ float red[kBlockWarps][32 * V];
+    __shared__ float red[kBlockWarps<V>][32 * V];
     pdl_join();
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     const bool drop = p.drop.rng && p.drop.threshold;
@@ -105,7 +106,8 @@ template <typename T, int V> __global__ void __launch_bounds__(kBlockWarps * 32)
     for (int e = 0; e < V; ++e) { rho[e] = 1.f; s[0][e] = 0.f; }
     if (p.g_post) {
         if (live)
-            for (int c = w; c < p.C; c += kBlockWarps) {
+#pragma unroll 4
+            for (int c = w; c < p.C; c += kBlockWarps<V>) {
                 float m[V];
                 ld_tokens<T, V>(p.m, base + (long long)c * p.T, m);
 #pragma unroll
@@ -126,7 +128,8 @@ template <typename T, int V> __global__ void __launch_bounds__(kBlockWarps * 32)
         for (int e = 0; e < V; ++e) r[e] += o.D[e] != 0.f ? o.sc * (o.D[e] * (o.act[e] * (o.mh[e] * o.gp))) : 0.f;
     };
     if (live)
-        for (int c = w; c < p.C; c += kBlockWarps) {
+#pragma unroll 4
+        for (int c = w; c < p.C; c += kBlockWarps<V>) {
             float r[V];
             value(c, r);
             st_tokens<T, V>(p.r, base + (long long)c * p.T, r);
@@ -139,7 +142,8 @@ template <typename T, int V> __global__ void __launch_bounds__(kBlockWarps * 32)
 #pragma unroll
         for (int e = 0; e < V; ++e) rho_r[e] = rsqrtf(s[0][e] / (float)p.C + p.eps);
         if (live)
-            for (int c = w; c < p.C; c += kBlockWarps) {
+#pragma unroll 4
+            for (int c = w; c < p.C; c += kBlockWarps<V>) {
                 float r[V];
                 value(c, r);
                 HN_G(p.g_pre + c, 4);
@@ -155,9 +159,9 @@ template <typename T, int V> __global__ void __launch_bounds__(kBlockWarps * 32)
     }
 }
 
-template <typename T, int V> __global__ void __launch_bounds__(kBlockWarps * 32) block_backward_kernel(BlockArgs p)
+template <typename T, int V> __global__ void __launch_bounds__(kBlockWarps<V> * 32) block_backward_kernel(BlockArgs p)
 {
-    __shared__ float red[kBlockWarps][3 * 32 * V];
+    __shared__ float red[kBlockWarps<V>][3 * 32 * V];
     pdl_join();
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     const bool drop = p.drop.rng && p.drop.threshold;
@@ -193,7 +197,8 @@ template <typename T, int V> __global__ void __launch_bounds__(kBlockWarps * 32)
             }
         };
         if (live && (p.g_pre || p.g_post))
-            for (int c = w; c < p.C; c += kBlockWarps) {
+#pragma unroll 4
+            for (int c = w; c < p.C; c += kBlockWarps<V>) {
                 Branch<V> o;
                 float en[V], rh[V], dr[V], g;
                 values(c, o, en, rh, dr, g);
@@ -212,7 +217,8 @@ template <typename T, int V> __global__ void __launch_bounds__(kBlockWarps * 32)
             c1[e] = s[0][e] / (float)p.C;
             c2[e] = p.g_post ? (s[1][e] - rho_r[e] * c1[e] * s[2][e]) / (float)p.C : 0.f;
         }
-        for (int c = w; c < p.C; c += kBlockWarps) {
+#pragma unroll 2
+        for (int c = w; c < p.C; c += kBlockWarps<V>) {
             float sum[3] = {0.f, 0.f, 0.f};
             if (live) {
                 Branch<V> o;
@@ -267,16 +273,22 @@ __global__ void __launch_bounds__(256) block_sum_kernel(const float *partial, in
     if (out) { HN_G(out + i % C, 4); out[i % C] = s; }
 }
 
-// How the tile kernels take a shape: few channels in one CTA with wide tiles of tokens, more in a cluster.  false: more channels than
-// a cluster holds.
+// How the tile kernels take a shape: few channels in one CTA with wide tiles of tokens, more in a cluster, at two CTAs an SM; twice as
+// many channels at one CTA an SM (backward, 4 x 64 x 64 tokens of 768 channels, fp32: 103 us, the general kernels 347).  false: more
+// channels than a cluster holds.
 static bool tile_shape(const BlockArgs &a, int dtype, bool backward, TileShape *s)
 {
+    const bool ragged = a.T * elsize(dtype) % 16 != 0;
     int most = (backward ? kBackwardBytes : kForwardBytes) / (int)elsize(dtype);       // channels of a thread
-    if (!backward && a.T * elsize(dtype) % 16 && a.C <= kTileCtas * 16 * most) most /= 2;     // (rows with a piece more: two CTAs an SM all the same)
+    if (!backward && ragged && a.C <= kTileCtas * 16 * most) most /= 2;                // (rows with a piece more: two CTAs an SM all the same)
     s->lt = a.C <= 8 * (most < 4 ? most : 4) ? 32 : 8;
     const int rows = kTileThreads / s->lt;
+    if (a.C > kTileCtas * rows * most) {
+        if (!backward && ragged && dtype == HYENAND_F32) return false;                 // (would not fit in an SM's shared memory)
+        most *= 2;
+    }
     s->ctas = (a.C + rows * most - 1) / (rows * most);
-    if (s->ctas > kTileCtas) return false;
+    if (s->ctas > kTileCtas || most > 8) return false;
     const int each = ((a.C + s->ctas - 1) / s->ctas + rows - 1) / rows;
     s->n = each <= 2 ? each : each <= 4 ? 4 : 8;
     return true;
@@ -292,12 +304,12 @@ static int block_launch(BlockArgs &a, int dtype, bool backward, cudaStream_t st)
         a.tiles = (long long)a.B * a.tiles_b;
         return (backward ? launch_block_tile_backward : launch_block_tile_forward)(a, dtype, s, st);
     }
-    const int tokens = a.T % 4 == 0 ? 4 : 1;
+    const int tokens = a.T % 4 == 0 && (long long)a.B * ((a.T + 127) / 128) >= kSms ? 4 : 1;
     a.tiles_b = (a.T + 32 * tokens - 1) / (32 * tokens);
     a.tiles = (long long)a.B * a.tiles_b;
     const long long blocks = backward && a.tiles > kBlockSlots ? kBlockSlots : a.tiles;
     if (blocks > 0x7fffffffll) return -1;
-#define HN_BLK(T, V) launch_pdl(backward ? block_backward_kernel<T, V> : block_forward_kernel<T, V>, dim3((unsigned)blocks), kBlockWarps * 32, 0, st, a)
+#define HN_BLK(T, V) launch_pdl(backward ? block_backward_kernel<T, V> : block_forward_kernel<T, V>, dim3((unsigned)blocks), kBlockWarps<V> * 32, 0, st, a)
     if (dtype == HYENAND_F32) { if (tokens == 4) HN_BLK(float, 4); else HN_BLK(float, 1); }
     else { if (tokens == 4) HN_BLK(bf16, 4); else HN_BLK(bf16, 1); }
 #undef HN_BLK

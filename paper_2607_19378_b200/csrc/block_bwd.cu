@@ -11,7 +11,7 @@ namespace cg = cooperative_groups;
 static __device__ int hn_block_status;                       // 1: a bounded wait gave up
 int block_backward_status() { return read_status(hn_block_status); }
 
-template <typename T, int LT, int N, bool ALIGNED> __global__ void __launch_bounds__(kTileThreads, 2) block_tile_backward_kernel(BlockArgs p, int ctas)
+template <typename T, int LT, int N, bool ALIGNED> __global__ void __launch_bounds__(kTileThreads, N * (int)sizeof(T) > kBackwardBytes ? 1 : 2) block_tile_backward_kernel(BlockArgs p, int ctas)
 {
     constexpr int TT = LT * V, ROWS = kTileThreads / LT;
     using Sums = TileSums<LT, 3>;
@@ -225,7 +225,9 @@ template <typename T> static int by_shape(const BlockArgs &a, const TileShape &s
     constexpr int MOST = kBackwardBytes / (int)sizeof(T);
     if (s.n == 1) return s.lt == 32 ? by_alignment<T, 32, 1>(a, s, st) : by_alignment<T, 8, 1>(a, s, st);
     if (s.n == 2) return s.lt == 32 ? by_alignment<T, 32, 2>(a, s, st) : by_alignment<T, 8, 2>(a, s, st);
-    if constexpr (MOST >= 4) return s.lt == 32 ? by_alignment<T, 32, 4>(a, s, st) : by_alignment<T, 8, 4>(a, s, st);
+    if constexpr (MOST >= 4) if (s.lt == 32) return by_alignment<T, 32, 4>(a, s, st);
+    if (s.n == 4) return by_alignment<T, 8, 4>(a, s, st);
+    if constexpr (MOST >= 4) if (s.n == 8) return by_alignment<T, 8, 8>(a, s, st);
     return -1;
 }
 

@@ -12,7 +12,7 @@ namespace cg = cooperative_groups;
 static __device__ int hn_block_status;                       // 1: a bounded wait gave up
 int block_forward_status() { return read_status(hn_block_status); }
 
-template <typename T, int LT, int N, bool ALIGNED> __global__ void __launch_bounds__(kTileThreads, N <= 4 ? 3 : 2) block_tile_forward_kernel(BlockArgs p, int ctas)
+template <typename T, int LT, int N, bool ALIGNED> __global__ void __launch_bounds__(kTileThreads, N <= 4 ? 3 : N * (int)sizeof(T) > kForwardBytes ? 1 : 2) block_tile_forward_kernel(BlockArgs p, int ctas)
 {
     constexpr int TT = LT * V, ROWS = kTileThreads / LT;
     using Sums = TileSums<LT, 4>;
@@ -170,13 +170,11 @@ template <typename T, int LT, int N> static int by_alignment(const BlockArgs &a,
 }
 template <typename T> static int by_shape(const BlockArgs &a, const TileShape &s, cudaStream_t st)
 {
-    constexpr int MOST = kForwardBytes / (int)sizeof(T);
     if (s.lt == 32) return s.n == 1 ? by_alignment<T, 32, 1>(a, s, st) : s.n == 2 ? by_alignment<T, 32, 2>(a, s, st) : by_alignment<T, 32, 4>(a, s, st);
     if (s.n == 1) return by_alignment<T, 8, 1>(a, s, st);
     if (s.n == 2) return by_alignment<T, 8, 2>(a, s, st);
     if (s.n == 4) return by_alignment<T, 8, 4>(a, s, st);
-    if constexpr (MOST >= 8) return by_alignment<T, 8, 8>(a, s, st);
-    return -1;
+    return by_alignment<T, 8, 8>(a, s, st);
 }
 
 int launch_block_tile_forward(const BlockArgs &a, int dtype, const TileShape &s, cudaStream_t st)
