@@ -28,7 +28,7 @@ struct RecArgs {
     void *y, *dq, *dk, *dv, *dg;
     float *s_end, *ds0;                   // [rows] or nullptr
     float *marks;                         // [rows][marks_row] or nullptr (forward); read by the backward
-    float4 *maps;                         // [rows][segments], where there are several
+    float4 *maps;                         // [rows][segments], where there are several (Row::way_end)
     int segments;                         // of a row
     long long rows, n;                    // n = rows * L
     int C, L, marks_row;
@@ -211,9 +211,18 @@ template <int LANES, int E> struct Row {
     }
     __device__ __forceinline__ int position(int tile) const { return (tile * LANES + l) * E - lead; }           // this thread's first
     __device__ __forceinline__ int warp_position(int tile) const { return (tile * LANES + l - ((int)threadIdx.x & 31)) * E - lead; }
-    // by the lanes of one warp: from the state at the row's end that the maps come from, through the segments on the way to this one
-    template <bool UP> __device__ __forceinline__ float entering(const RecArgs &p, float state) const
+    // Where the way through the segments ends; nothing needs that one's map, its place holds the state that the way begins with
+    // (s0 and s_end may be one tensor, and the segments of a row run in any order).
+    template <bool UP> __device__ __forceinline__ int way_end(const RecArgs &p) const { return UP ? p.segments - 1 : 0; }
+    // by the lanes of one warp: from that state through the segments on the way to this one
+    template <bool UP> __device__ __forceinline__ float entering(const RecArgs &p) const
     {
+        float state = 0.f;
+        if (real) {
+            const float4 *f = p.maps + row * p.segments + way_end<UP>(p);
+            HN_G(f, 16);
+            state = f->z;
+        }
         const int lane = threadIdx.x & 31, each = ((UP ? segment : p.segments - 1 - segment) + 31) / 32;
         int n = UP ? segment : p.segments - 1 - segment;
         if (!real) n = 0;
@@ -367,10 +376,13 @@ __global__ void __launch_bounds__(128, 8) recurrence_maps_kernel(RecArgs p)
     Pl pl;
     pl.in[0] = (const T *)(UP ? p.k : p.q); pl.in[1] = (const T *)(UP ? p.v : p.dy); pl.in[2] = (const T *)p.g;
     pl.init(stages, barriers, r.len, p.n);
-    const int tiles = max(0, min(r.last, r.live) - r.first);
+    const bool end = r.segment == r.template way_end<UP>(p);
+    const int tiles = end ? 0 : max(0, min(r.last, r.live) - r.first);
     auto tile_of = [&](int c) { return UP ? r.first + c : r.first + tiles - 1 - c; };
     auto fetch = [&](int c) { pl.fetch(c & 1, r.start + r.warp_position(tile_of(c)), r.warp_position(tile_of(c))); };
     Map total = {1.f, 0.f, 0.f};
+    const float *from = UP ? p.s0 : p.ds_end;
+    if (end && r.real && from) { HN_G(from + r.row, 4); total.S = from[r.row]; }
     int waited[2] = {0, 0};
     if (tiles) fetch(0);
     for (int c = 0; c < tiles; ++c) {
@@ -410,7 +422,7 @@ __global__ void __launch_bounds__(RowLane<LANES>::kThreads, LANES > 32 ? 768 / L
 {
     using R = RowLane<LANES>;
     constexpr int E = 8 * OCT, N = E / 2;
-        using Pl = Places<T, OCT, 4, R::kThreads, STAGED>;
+    using Pl = Places<T, OCT, 4, R::kThreads, STAGED>;
     extern __shared__ __align__(16) char stages[];
     __shared__ Meeting<LANES> meeting;
     __shared__ uint64_t barriers[STAGED ? R::kThreads / 16 : 1];
@@ -419,14 +431,14 @@ __global__ void __launch_bounds__(RowLane<LANES>::kThreads, LANES > 32 ? 768 / L
     pdl_join();
     const Row<LANES, E> r(p);
     float state = 0.f;
-    if (r.real && p.s0) { HN_G(p.s0 + r.row, 4); state = p.s0[r.row]; }
+    if (r.real && p.s0 && p.segments == 1) { HN_G(p.s0 + r.row, 4); state = p.s0[r.row]; }
     if (STAGED && LANES > 32 && threadIdx.x == 0) meeting.carry[1] = state;      // (read behind the first tile's barrier)
     Pl pl;
     pl.in[0] = k; pl.in[1] = v; pl.in[2] = g; pl.in[3] = q;
     pl.init(stages, barriers, r.len, p.n);
     auto first = [&](int j) { return r.warp_position(j); };
     if (STAGED && r.first < r.last) pl.fetch(0, r.start + first(r.first), first(r.first));
-    if (LANES == 32 && r.segment) state = r.template entering<true>(p, state);
+    if (LANES == 32 && p.segments > 1) state = r.template entering<true>(p);
     for (int j = r.first; j < r.last; ++j) {
         const int th = j * LANES + r.l, t0 = th * E - r.lead, met = j - r.first, turn = met & 1;
         const long long i = r.start + t0;
@@ -500,7 +512,7 @@ __global__ void __launch_bounds__(RowLane<LANES>::kThreads, LANES > 32 ? 512 / L
     pdl_join();
     const Row<LANES, E> r(p);
     float mu = 0.f;                                          // a_{t+1} lam_{t+1} of the position behind the tile
-    if (r.real && p.ds_end) { HN_G(p.ds_end + r.row, 4); mu = p.ds_end[r.row]; }
+    if (r.real && p.ds_end && p.segments == 1) { HN_G(p.ds_end + r.row, 4); mu = p.ds_end[r.row]; }
     if (STAGED && LANES > 32 && threadIdx.x == 0) back.carry[1] = mu;
     auto mark_of = [&](int j) {                              // in front of a tile
         const int mark = STAGED ? j * LANES * OCT / kMarkOctets : 0;
@@ -516,7 +528,7 @@ __global__ void __launch_bounds__(RowLane<LANES>::kThreads, LANES > 32 ? 512 / L
     float mark = mark_of(r.last - 1);
     int used[2] = {0, 0};                                    // copies waited for, of each stage
     if (STAGED && r.first < r.last) pl.fetch((r.last - 1) & 1, r.start + first(r.last - 1), first(r.last - 1));
-    if (LANES == 32 && r.segment < p.segments - 1) mu = r.template entering<false>(p, mu);
+    if (LANES == 32 && p.segments > 1) mu = r.template entering<false>(p);
     for (int j = r.last - 1; j >= r.first; --j) {
         const int t0 = r.position(j);
         const long long i = r.start + t0;

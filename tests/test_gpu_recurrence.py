@@ -1,10 +1,11 @@
 """The gated linear recurrence on the GPU against oracle/recurrence.py.
 
 Bound of an element.  A rounding to the output type is at most eps(type) / 2 of the value.  Everything before it is fp32, and every
-term of a sum passes through a number of fp32 operations on its way to an element, each off by at most 2^-24 (a decay from exp or
-sigmoid by 4 of them): at most 8 steps with their decays inside an octet (50), 5 compositions between lanes (25), one map a 256
-positions (3 each) and the last 8 steps (40), the products at the end (4).  So |error| <= eps / 2 |ref| + K 2^-24 abs, K = 160 +
-L / 64, with abs the same sum over absolute values; a product of two such sums (dg) takes 2 K.
+term of a sum passes through a number of fp32 operations on its way to an element, counted in units of 2^-24: a decay from the
+approximate exponential (4) and reciprocal (2) with the sum and product around them is off by at most 8, a step adds one more, so the
+8 steps of a thread that a term starts in and the 8 of the one it ends in are 144 (16 of bf16 each: 288); 5 compositions between lanes
+(5 each), one map a 256 positions or fewer (3 each), the products at the end (4).  So |error| <= eps / 2 |ref| + K 2^-24 abs, K = 176 +
+L / 64 (bf16: 320 + L / 64), with abs the same sum over absolute values; a product of two such sums (dg) takes 2 K.
 """
 import numpy as np
 import pytest
@@ -57,7 +58,7 @@ def run(t, L, B, C, dtype, decay):
 
 
 def compare(got, ref, L, names=("y", "s_end", "dq", "dk", "dv", "dg", "ds0")):
-    K = 160 + L / 64
+    K = (320 if got[names[0]].dtype == torch.bfloat16 else 176) + L / 64
     for n in names:
         half = HALF[got[n].dtype]
         bound = half * np.abs(ref[n]) + (2 * K if n == "dg" else K) * 2.0 ** -24 * ref[n + "_abs"] * (1 + half) + 1e-37
@@ -188,7 +189,7 @@ def test_steps_follow_a_sequence(decay, dtype):
 def test_state_in_place_and_results_repeat():
     """s_end may be s0's buffer, ds0 ds_end's; two calls give the same bits; without s0, lengths and marks the same as with zeros."""
     from paper_2607_19378_b200 import hyenand as hn
-    for B, C, L in ((2, 3, 50), (1, 4, 9000), (2, 300, 2100)):
+    for B, C, L in ((2, 3, 50), (1, 4, 9000), (2, 300, 2100), (1, 3, 40001), (4, 29, 20000)):
         t = {k: v.cuda() for k, v in inputs(B, C, L, torch.bfloat16, "log", 10).items() if v is not None}
         op = hn.Recurrence(L, B, C, "log", torch.bfloat16)
         y, end, marks = op.forward(t["q"], t["k"], t["v"], t["g"], s0=t["s0"], marks=True)
