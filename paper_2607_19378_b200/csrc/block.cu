@@ -254,23 +254,34 @@ template <typename T, int V> __global__ void __launch_bounds__(kBlockWarps<V> * 
     }
 }
 
-// out[k][c] = sum of the slots, a fixed order whatever the timing: 8 chains a channel, then those
-__global__ void __launch_bounds__(256) block_sum_kernel(const float *partial, int slots, int C, float *dg_post, float *dscale, float *dg_pre)
+// out[k][c] = sum of the slots, a fixed order whatever the timing: 32 chains a channel, four loads of each on their way, then those
+constexpr int kSumWarps = 32;
+__global__ void __launch_bounds__(kSumWarps * 32) block_sum_kernel(const float *partial, int slots, int C, float *dg_post, float *dscale, float *dg_pre)
 {
-    __shared__ float red[8][33];
+    __shared__ float red[kSumWarps][33];
     pdl_join();
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, i = blockIdx.x * 32 + lane;
     float s = 0.f;
     if (i < 3 * C)
-        for (int j = w; j < slots; j += 8) { HN_G(partial + (long long)j * 3 * C + i, 4); s += partial[(long long)j * 3 * C + i]; }
+        for (int j = w; j < slots; j += 4 * kSumWarps) {
+            float v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const float *q = partial + (long long)(j + u * kSumWarps) * 3 * C + i;
+                v[u] = 0.f;
+                if (j + u * kSumWarps < slots) { HN_G(q, 4); v[u] = *q; }
+            }
+            s += (v[0] + v[1]) + (v[2] + v[3]);
+        }
     red[w][lane] = s;
     __syncthreads();
-    if (w || i >= 3 * C) return;
-    s = 0.f;
+    s = red[lane][w];                                        // warp w: the block's channel w
 #pragma unroll
-    for (int j = 0; j < 8; ++j) s += red[j][lane];
-    float *out = i < C ? dg_post : i < 2 * C ? dscale : dg_pre;
-    if (out) { HN_G(out + i % C, 4); out[i % C] = s; }
+    for (int o = 16; o; o /= 2) s += __shfl_xor_sync(~0u, s, o);
+    const int c = blockIdx.x * 32 + w;
+    if (lane || c >= 3 * C) return;
+    float *out = c < C ? dg_post : c < 2 * C ? dscale : dg_pre;
+    if (out) { HN_G(out + c % C, 4); out[c % C] = s; }
 }
 
 // How the tile kernels take a shape: few channels in one CTA with wide tiles of tokens, more in a cluster, at two CTAs an SM; twice as
@@ -414,6 +425,6 @@ extern "C" int hyenand_block_backward(int B, int C, int T, int dtype, const void
     c.register_ranges();
     const int slots = block_launch(a, dtype, true, (cudaStream_t)cuda_stream);
     if (slots > 0 && (dg_post || dscale || dg_pre))
-        launch_pdl(block_sum_kernel, dim3((unsigned)((3ll * C + 31) / 32)), 256, 0, (cudaStream_t)cuda_stream, (const float *)a.partial, slots, C, dg_post, dscale, dg_pre);
+        launch_pdl(block_sum_kernel, dim3((unsigned)((3ll * C + 31) / 32)), kSumWarps * 32, 0, (cudaStream_t)cuda_stream, (const float *)a.partial, slots, C, dg_post, dscale, dg_pre);
     return finish(slots);
 }
