@@ -285,7 +285,7 @@ int hyenand_synth_device_status(void);
  */
 enum { HYENAND_DECAY_VALUE = 0, HYENAND_DECAY_LOG = 1, HYENAND_DECAY_SIGMOID = 2 };
 long long hyenand_recurrence_marks(int L);        /* floats per row of marks; 0 for an L out of range */
-long long hyenand_recurrence_workspace_bytes(int B, int C, int L, int dtype);      /* of a forward or backward call (some 30 KB at most: rows
+long long hyenand_recurrence_workspace_bytes(int B, int C, int L, int dtype);      /* of a forward or backward call (57 KB at most: rows
                                                                                     * too few to fill the GPU are cut into segments) */
 int hyenand_recurrence_forward(int B, int C, int L, int decay, int dtype, const void *q, const void *k, const void *v,
                                const void *g, const float *s0, const int *lengths, void *y, float *s_end, float *marks,

@@ -25,7 +25,7 @@ using Shape = std::vector<int64_t>;
 
 struct PythonError : std::exception {};                      // the interpreter's error is set
 
-struct Checker {
+struct Arguments {
     int device = -1;
     // None: a null pointer where that is allowed
     const Tensor *operator()(PyObject *o, const char *name, ScalarType type, c10::IntArrayRef shape, bool optional = false)
@@ -139,7 +139,7 @@ PyObject *recurrence_forward(PyObject *, PyObject *const *a, Py_ssize_t n)
     if (!count(n, 9)) return nullptr;
     return guarded([&] {
         const Recurrence *r = handle<Recurrence>(a[0]);
-        Checker want;
+        Arguments want;
         const Tensor *q = want(a[1], "q", r->type, r->shape), *k = want(a[2], "k", r->type, r->shape), *v = want(a[3], "v", r->type, r->shape),
                      *g = want(a[4], "g", r->type, r->shape), *s0 = want(a[5], "s0", at::kFloat, r->states, true),
                      *len = want(a[6], "lengths", at::kInt, r->batch, true), *given = want(a[8], "y", r->type, r->shape, true);
@@ -158,7 +158,7 @@ PyObject *recurrence_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
     if (!count(n, 9)) return nullptr;
     return guarded([&] {
         const Recurrence *r = handle<Recurrence>(a[0]);
-        Checker want;
+        Arguments want;
         const Tensor *q = want(a[1], "q", r->type, r->shape), *k = want(a[2], "k", r->type, r->shape), *v = want(a[3], "v", r->type, r->shape),
                      *g = want(a[4], "g", r->type, r->shape), *marks = want(a[5], "marks", at::kFloat, r->marks), *dy = want(a[6], "dy", r->type, r->shape),
                      *ds = want(a[7], "ds_end", at::kFloat, r->states, true), *len = want(a[8], "lengths", at::kInt, r->batch, true);
@@ -178,7 +178,7 @@ PyObject *recurrence_step(PyObject *, PyObject *const *a, Py_ssize_t n)
     if (!count(n, 9)) return nullptr;
     return guarded([&] {
         const Recurrence *r = handle<Recurrence>(a[0]);
-        Checker want;
+        Arguments want;
         const Tensor *q = want(a[1], "q", r->type, r->states), *k = want(a[2], "k", r->type, r->states), *v = want(a[3], "v", r->type, r->states),
                      *g = want(a[4], "g", r->type, r->states), *state = want(a[5], "state", at::kFloat, r->states),
                      *next = want(a[6], "new_state", at::kFloat, r->states, true), *active = want(a[7], "active", at::kInt, r->batch, true),
@@ -226,7 +226,7 @@ PyObject *block_forward(PyObject *, PyObject *const *a, Py_ssize_t n)
     if (!count(n, 9)) return nullptr;
     return guarded([&] {
         const Block *b = handle<Block>(a[0]);
-        Checker want;
+        Arguments want;
         const Tensor *x = want(a[1], "x", b->type, b->shape), *m = want(a[2], "m", b->type, b->shape), *z = want(a[3], "z", b->type, b->shape, true),
                      *gp = want(a[4], "g_post", at::kFloat, b->channels, true), *sc = want(a[5], "scale", at::kFloat, b->channels, true),
                      *gn = want(a[6], "g_pre", at::kFloat, b->channels, true), *rng = want(a[7], "rng", at::kLong, kTwo, true);
@@ -246,7 +246,7 @@ PyObject *block_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
     if (!count(n, 11)) return nullptr;
     return guarded([&] {
         const Block *b = handle<Block>(a[0]);
-        Checker want;
+        Arguments want;
         const Tensor *x = want(a[1], "x", b->type, b->shape), *m = want(a[2], "m", b->type, b->shape), *st = want(a[3], "stats", at::kFloat, b->stats, true),
                      *z = want(a[4], "z", b->type, b->shape, true), *gp = want(a[5], "g_post", at::kFloat, b->channels, true),
                      *sc = want(a[6], "scale", at::kFloat, b->channels, true), *gn = want(a[7], "g_pre", at::kFloat, b->channels, true),
@@ -273,7 +273,7 @@ PyObject *dropout(PyObject *, PyObject *const *a, Py_ssize_t n)
         if (!THPVariable_Check(a[4])) { PyErr_SetString(PyExc_TypeError, "x must be a tensor"); throw PythonError(); }
         const ScalarType type = THPVariable_Unpack(a[4]).scalar_type();
         if (type != at::kFloat && type != at::kBFloat16) { PyErr_SetString(PyExc_ValueError, "x must be a float32 or bfloat16 tensor"); throw PythonError(); }
-        Checker want;
+        Arguments want;
         const c10::IntArrayRef shape = THPVariable_Unpack(a[4]).sizes();
         const Tensor *x = want(a[4], "x", type, shape), *rng = want(a[5], "rng", at::kLong, kTwo), *given = want(a[6], "y", type, shape, true);
         const auto f = (decltype(&hyenand_dropout))PyLong_AsUnsignedLongLong(a[0]);

@@ -684,8 +684,8 @@ static int segments_of(long long rows, int L, int dtype, bool backward)
     const int tile = 32 * (dtype == HYENAND_F32 ? 8 : 16);
     const long long tiles = ((long long)L + (L % 8 ? 7 : 0) + tile - 1) / tile, places = (backward ? 512 : 768) / 32 * kSms;
     if (rows >= (backward ? 2 * kSms : 128) || tiles < 32) return 1;
-    const long long n = places / rows, most = tiles / 2;
-    return (int)(n < most ? n : most);
+    const long long n = places / rows, each = (tiles + n - 1) / n;
+    return (int)((tiles + (each > 2 ? each : 2) - 1) / (each > 2 ? each : 2));       // (none of them empty)
 }
 
 // Lanes of a row: as few as hold it in one tile, a CTA that walks it where it is longer.
