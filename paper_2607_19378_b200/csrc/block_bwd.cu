@@ -228,9 +228,11 @@ template <typename T, int LT, int N> static int by_alignment(const BlockArgs &a,
 template <typename T> static int by_shape(const BlockArgs &a, const TileShape &s, cudaStream_t st)
 {
     constexpr int MOST = kBackwardBytes / (int)sizeof(T);
-    if (s.n == 1) return s.lt == 32 ? by_alignment<T, 32, 1>(a, s, st) : by_alignment<T, 8, 1>(a, s, st);
+    if (s.n == 1 && s.lt == 32) return by_alignment<T, 32, 1>(a, s, st);
+    if constexpr (sizeof(T) == 4) if (s.n == 1) return by_alignment<T, 8, 1>(a, s, st);
     if (s.n == 2) return s.lt == 32 ? by_alignment<T, 32, 2>(a, s, st) : by_alignment<T, 8, 2>(a, s, st);
     if constexpr (MOST >= 4) if (s.lt == 32) return by_alignment<T, 32, 4>(a, s, st);
+    if constexpr (MOST >= 4) if (s.n == 3) return by_alignment<T, 8, 3>(a, s, st);
     if (s.n == 4) return by_alignment<T, 8, 4>(a, s, st);
     if constexpr (MOST >= 4) if (s.n == 8) return by_alignment<T, 8, 8>(a, s, st);
     return -1;

@@ -177,9 +177,11 @@ template <typename T, int LT, int N> static int by_alignment(const BlockArgs &a,
 template <typename T> static int by_shape(const BlockArgs &a, const TileShape &s, cudaStream_t st)
 {
     if (s.lt == 32) return s.n == 1 ? by_alignment<T, 32, 1>(a, s, st) : s.n == 2 ? by_alignment<T, 32, 2>(a, s, st) : by_alignment<T, 32, 4>(a, s, st);
-    if (s.n == 1) return by_alignment<T, 8, 1>(a, s, st);
+    if constexpr (sizeof(T) == 4) if (s.n == 1) return by_alignment<T, 8, 1>(a, s, st);
     if (s.n == 2) return by_alignment<T, 8, 2>(a, s, st);
+    if (s.n == 3) return by_alignment<T, 8, 3>(a, s, st);
     if (s.n == 4) return by_alignment<T, 8, 4>(a, s, st);
+    if constexpr (sizeof(T) == 2) if (s.n == 6) return go<T, 8, 6, true>(a, s, st);      // (fp32 and ragged rows come with at least seven)
     return by_alignment<T, 8, 8>(a, s, st);
 }
 

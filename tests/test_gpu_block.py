@@ -87,7 +87,7 @@ def test_parts(gate, post, scaled, pre, dtype):
 # tokens: one, odd, even, multiples of four and of eight, tiles that end inside; channels from one to thousands
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("B,C,T", [(1, 1, 1), (2, 3, 2), (3, 5, 4), (1, 7, 8), (2, 64, 210), (1, 33, 1023), (4, 100, 36), (2, 300, 31), (1, 768, 72), (2, 200, 1024),
-                                   (1, 1000, 17), (1, 600, 35), (2, 700, 24), (1, 1030, 21), (1, 1500, 33), (1, 2048, 40), (1, 2100, 33), (1, 5000, 12), (70, 40, 9), (300, 17, 40), (2, 129, 66)], ids=str)
+                                   (1, 1000, 17), (1, 600, 35), (2, 700, 24), (1, 1030, 21), (1, 1500, 33), (1, 2048, 40), (1, 2100, 33), (1, 5000, 12), (70, 40, 9), (300, 17, 40), (2, 129, 66), (2, 90, 72), (1, 170, 80), (2, 380, 48), (1, 185, 45)], ids=str)
 def test_sizes(B, C, T, dtype):
     check(B, C, T, dtype, p=0.2 if T % 3 else 0.0, seed=B + C + T, site=3)
 
