@@ -53,7 +53,9 @@ template <int DECAY> __device__ __forceinline__ void decay(float g, float &a, fl
     if constexpr (DECAY == DECAY_VALUE) { a = g; na = 1.f - g; }
     else if constexpr (DECAY == DECAY_LOG) { a = ex2(g * kLog2e); na = 0.f; }
     else {
-        const float e = ex2(-kLog2e * fabsf(g)), r = rcp(1.f + e), x = e * r;
+        // the larger one as 1 - the smaller: half a unit off, to no side, where the reciprocal's 1 / (1 + e) drifted by 5e-7 of a state over a
+        // thread's steps
+        const float e = ex2(-kLog2e * fabsf(g)), x = e * rcp(1.f + e), r = 1.f - x;
         a = g >= 0.f ? r : x;
         na = g >= 0.f ? x : r;
     }

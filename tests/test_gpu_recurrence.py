@@ -113,6 +113,21 @@ def test_values_behind_an_entry_are_not_looked_at():
     assert float(got["dg"][1, :, 1:].abs().max()) == 0
 
 
+@pytest.mark.parametrize("dtype,L", [("f32", 20011), ("bf16", 40000)])
+def test_entries_that_end_in_a_segment(dtype, L):
+    """Few long rows, cut into segments: entries of no position, of one, of a part of the first segment, of all; NaN behind them."""
+    lengths = [0, 1, 511, 512, 513, L - 1, L]
+    t = inputs(len(lengths), 2, L, DTYPES[dtype], "sigmoid", 17)
+    t["lengths"] = torch.tensor(lengths, dtype=torch.int32)
+    ref = orec.recurrence(t["q"], t["k"], t["v"], t["g"], "sigmoid", t["s0"], t["lengths"], t["dy"], t["ds"])
+    for n in ("q", "k", "v", "g", "dy"):
+        for b, m in enumerate(lengths):
+            t[n][b, :, m:] = float("nan")
+    got = run(t, L, len(lengths), 2, DTYPES[dtype], "sigmoid")
+    compare(got, ref, L)
+    assert torch.equal(got["s_end"][0], t["s0"][0]) and torch.equal(got["ds0"][0], t["ds"][0])
+
+
 @pytest.mark.parametrize("decay", ["value", "log", "sigmoid"])
 def test_resets_and_extreme_gates(decay):
     """A decay of exactly zero cuts a row; gates of the type's lowest and highest values stay finite."""
