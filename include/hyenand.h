@@ -302,9 +302,13 @@ int hyenand_recurrence_backward(int B, int C, int L, int decay, int dtype, const
  * device or NULL; an entry whose value is below 1 keeps its state and gets y = 0. */
 int hyenand_recurrence_step(int B, int C, int decay, int dtype, const void *q, const void *k, const void *v, const void *g,
                             const float *state, const int *active, void *y, float *new_state, void *cuda_stream);
-/* Long rows travel through shared memory as bulk copies, and every wait for one is bounded.  Returns 0, or 1 once one has given up since the library was loaded (the call that met it left its results incomplete), -1 if the
- * word cannot be read.  Synchronises the device. */
+/* Long rows travel through shared memory as bulk copies, and every wait for one is bounded.  Returns 0, or 1 once one has given up
+ * since the library was loaded: the call that met it left the results of those positions unwritten, and what follows from them is
+ * unwritten or NaN; -1 if the word cannot be read.  Synchronises the device. */
 int hyenand_recurrence_device_status(void);
+/* Checked build: from now on the recurrence takes the copies of one tile of every row to have come too late, those of one warp of a CTA
+ * or of all (warp < 0), as a test of what it does then; tile < 0: none again.  Returns 0, -1 in the product library. */
+int hyenand_debug_recurrence_late(int tile, int warp);
 
 /*
  * What stands between two mixers of a residual stream x: the first one's output m normalised, gated, dropped out, scaled and

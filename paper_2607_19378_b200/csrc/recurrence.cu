@@ -10,6 +10,8 @@
 // All states and maps are fp32.  A product of thousands of decays close to 1 would collect the rounding of each of them, always to
 // the same side where the decay is constant; the maps therefore carry P = A - 1 beside A (P1 P2 + P1 + P2), built from 1 - a_t
 // (sigmoid), from the sum of the g_t (exp), and use whichever of the two is the precise one.
+#include <atomic>
+
 #include "entry.cuh"
 #include "octet.cuh"
 #include "pair.cuh"
@@ -32,7 +34,15 @@ struct RecArgs {
     int segments;                         // of a row
     long long rows, n;                    // n = rows * L
     int C, L, marks_row;
+#ifdef HYENAND_DEBUG
+    int late_tile, late_warp;             // whose copies are taken to come too late: of every row (-1: none), of a CTA (-1: all)
+#endif
 };
+#ifdef HYENAND_DEBUG
+static __device__ __forceinline__ bool is_late(const RecArgs &p, int tile) { return p.late_tile == tile && (p.late_warp < 0 || p.late_warp == (int)threadIdx.x / 32); }
+#else
+static __device__ __forceinline__ bool is_late(const RecArgs &, int) { return false; }
+#endif
 
 static __device__ int hn_rec_status;                         // 1: a bounded wait gave up
 
@@ -47,6 +57,7 @@ __device__ __forceinline__ Map compose(const Map &a, const Map &b) { return {a.A
 
 // a_t and 1 - a_t (LOG: not needed, 0).  The approximate exponential and reciprocal are off by a few roundings, which a thread's steps
 // can multiply up sixteen-fold at most: what goes on from thread to thread is built from 1 - a_t and the sum of the g_t.
+__device__ __forceinline__ float not_known() { return __int_as_float(0x7fffffff); }      // NaN
 constexpr float kLog2e = 1.4426950408889634f;
 template <int DECAY> __device__ __forceinline__ void decay(float g, float &a, float &na)
 {
@@ -254,6 +265,9 @@ template <int LANES, int E> struct Row {
 // tensor: a warp's 1024 of the next tile travel in as one bulk copy a tensor while this tile is worked on, results go out the same way.
 // (As 16-byte copies, each lane its own two: 404 and 697 us for 512 rows of 262144, bf16; neighbouring lanes neighbouring pieces:
 // 514 and 657, the addresses and conditions of sixteen copies being most of the instructions.)  Every warp has its own barriers.
+// A wait for copies is bounded.  A warp whose wait gives up fetches and stores nothing more, and its map is NaN for those who go on
+// from there; when the row is done, what was still on its way gets the same time once more to land, so that nothing reaches
+// shared memory that is another CTA's by then.
 template <typename T, int OCT, int TENSORS, int THREADS, bool STAGED> struct Places {
     static constexpr int E = 8 * OCT, STAGE = STAGED ? TENSORS * THREADS * 32 : 0;
     static constexpr unsigned WARP_BYTES = 1024;
@@ -263,13 +277,13 @@ template <typename T, int OCT, int TENSORS, int THREADS, bool STAGED> struct Pla
     uint64_t *bars;                                          // this warp's two
     long long n;
     int len, lane;
-    bool ok;                                                 // no wait has given up
+    int late;                                                // the tile at which a wait gave up (the same in all lanes), or -1
 
     __device__ __forceinline__ char *place(int turn, int tensor) const { return mine + turn * STAGE + tensor * THREADS * 32; }
     __device__ __forceinline__ void init(char *stages, uint64_t *barriers, int row_len, long long elements)
     {
         mine = stages + threadIdx.x * 32; bars = barriers + 2 * (threadIdx.x / 32); lane = threadIdx.x & 31;
-        len = row_len; n = elements; ok = true;
+        len = row_len; n = elements; late = -1;
         if (STAGED && lane == 0) { mbar_init(bars, 1); mbar_init(bars + 1, 1); fence_mbar_init(); }
         __syncwarp();
     }
@@ -299,11 +313,14 @@ template <typename T, int OCT, int TENSORS, int THREADS, bool STAGED> struct Pla
                 reinterpret_cast<T *>(place(turn, k) - lane * 32)[end - i + lane] = in[k][end + lane];
             }
     }
-    __device__ __forceinline__ void wait(int turn, int phase, int t)
+    __device__ __forceinline__ bool good() const { return !STAGED || late < 0; }
+    __device__ __forceinline__ void wait(int turn, int phase, int t, int tile, bool hold)
     {
-        if (t < len && ok) ok = mbar_wait(bars + turn, phase);
-        __syncwarp();
+        bool here = true;
+        if (t < len && late < 0) here = !hold && mbar_wait(bars + turn, phase);
+        if (__any_sync(~0u, !here)) late = tile;
     }
+    __device__ __forceinline__ void drain(int turn, int phase, int t) const { if (t < len) mbar_wait(bars + turn, phase); }
     // this thread's positions, the first at element i
     __device__ __forceinline__ void get(int turn, int tensor, long long i, f2 (&f)[E / 2]) const
     {
@@ -385,14 +402,15 @@ __global__ void __launch_bounds__(128, 8) recurrence_maps_kernel(RecArgs p)
     Map total = {1.f, 0.f, 0.f};
     const float *from = UP ? p.s0 : p.ds_end;
     if (end && r.real && from) { HN_G(from + r.row, 4); total.S = from[r.row]; }
-    int waited[2] = {0, 0};
+    int waited[2] = {0, 0};                                  // copies waited for, of each stage
     if (tiles) fetch(0);
     for (int c = 0; c < tiles; ++c) {
         const int j = tile_of(c), t0 = r.position(j), turn = c & 1, lo = max(0, -t0), hi = min(E, r.len - t0);
         const long long i = r.start + t0;
         __syncwarp();                                        // (the other stage has been read)
         if (c + 1 < tiles) fetch(c + 1);
-        pl.wait(turn, (turn ? waited[1] : waited[0]) & 1, r.warp_position(j));
+        pl.wait(turn, (turn ? waited[1] : waited[0]) & 1, r.warp_position(j), c, is_late(p, j));
+        if (!pl.good()) break;
         if (r.warp_position(j) < r.len) { if (turn) ++waited[1]; else ++waited[0]; }
         Map own = {1.f, 0.f, 0.f};
         if (lo < hi) {
@@ -411,12 +429,18 @@ __global__ void __launch_bounds__(128, 8) recurrence_maps_kernel(RecArgs p)
         const Map inc = scan_lanes<32, UP>(own, pl.lane);
         total = compose(total, inc);                         // (of use in the last lane on the way)
     }
+    if (!pl.good()) {
+        const int c = pl.late, turn = c & 1;
+        total.S = not_known();
+        pl.drain(turn, (turn ? waited[1] : waited[0]) & 1, r.warp_position(tile_of(c)));
+        if (c + 1 < tiles) pl.drain(turn ^ 1, (turn ? waited[0] : waited[1]) & 1, r.warp_position(tile_of(c + 1)));
+    }
     if (r.real && pl.lane == (UP ? 31 : 0)) {
         float4 *f = p.maps + r.row * p.segments + r.segment;
         HN_G(f, 16);
         *f = make_float4(total.A, total.P, total.S, 0.f);
     }
-    if (!pl.ok) atomicExch(&hn_rec_status, 1);
+    if (!pl.good()) atomicExch(&hn_rec_status, 1);
 }
 
 template <typename T, int DECAY, int OCT, int LANES, bool STAGED>
@@ -447,8 +471,8 @@ __global__ void __launch_bounds__(RowLane<LANES>::kThreads, LANES > 32 ? 768 / L
         const int lo = max(0, -t0), hi = min(E, r.len - t0);
         if (STAGED) {
             pl.stage_free();
-            if (j + 1 < r.last) pl.fetch(turn ^ 1, r.start + first(j + 1), first(j + 1));
-            pl.wait(turn, met >> 1 & 1, first(j));
+            if (j + 1 < r.last && pl.good()) pl.fetch(turn ^ 1, r.start + first(j + 1), first(j + 1));
+            pl.wait(turn, met >> 1 & 1, first(j), j, is_late(p, j));
         }
         const bool some = lo < hi, whole = lo == 0 && hi == E;
         f2 out[N];
@@ -466,6 +490,7 @@ __global__ void __launch_bounds__(RowLane<LANES>::kThreads, LANES > 32 ? 768 / L
 #pragma unroll
                 for (int e = 0; e < N; ++e) own.S = fmaf(a[e].y, fmaf(a[e].x, own.S, u[e].x), u[e].y);
             }
+            if (!pl.good()) own.S = not_known();
             const Step<LANES, true> step(own);
             if constexpr (LANES > 32) {
                 step.leave(meeting, met);
@@ -491,13 +516,18 @@ __global__ void __launch_bounds__(RowLane<LANES>::kThreads, LANES > 32 ? 768 / L
             if (LANES > 32 && threadIdx.x == LANES - 1) meeting.carry[turn] = state = s;
         }
         if (!some) mask(out, 0, 0, 0.f);
-        if (r.real) pl.put(turn, 0, y, r.start + first(j), first(j), i, t0, p.L, out);
+        if (r.real && pl.good()) pl.put(turn, 0, y, r.start + first(j), first(j), i, t0, p.L, out);
         pl.put_done();
     }
     if (STAGED && LANES > 32 && r.first >= r.live) { __syncthreads(); state = meeting.carry[1]; }       // (no tile has a position)
     if (r.real && p.s_end && r.segment == p.segments - 1 && r.l == (LANES > 32 ? LANES - 1 : 0)) { HN_G(p.s_end + r.row, 4); p.s_end[r.row] = state; }
     if (STAGED && pl.lane == 0) tma_wait_all0();
-    if (!pl.ok) atomicExch(&hn_rec_status, 1);
+    if (!pl.good()) {
+        const int j = pl.late, met = j - r.first;
+        pl.drain(met & 1, met >> 1 & 1, first(j));
+        if (j + 1 < r.last) pl.drain((met + 1) & 1, (met + 1) >> 1 & 1, first(j + 1));
+        atomicExch(&hn_rec_status, 1);
+    }
 }
 
 template <typename T, int DECAY, int OCT, int LANES, bool STAGED>
@@ -538,10 +568,10 @@ __global__ void __launch_bounds__(RowLane<LANES>::kThreads, LANES > 32 ? 512 / L
         float from = mark;
         if (STAGED) {
             pl.stage_free();
-            if (j > r.first) pl.fetch((j - 1) & 1, r.start + first(j - 1), first(j - 1));
+            if (j > r.first && pl.good()) pl.fetch((j - 1) & 1, r.start + first(j - 1), first(j - 1));
             mark = mark_of(j - 1);
-            pl.wait(j & 1, (j & 1 ? used[1] : used[0]) & 1, first(j));
-            if (first(j) < r.len) { if (j & 1) ++used[1]; else ++used[0]; }
+            pl.wait(j & 1, (j & 1 ? used[1] : used[0]) & 1, first(j), j, is_late(p, j));
+            if (first(j) < r.len && pl.good()) { if (j & 1) ++used[1]; else ++used[0]; }
         }
         const bool some = lo < hi, whole = lo == 0 && hi == E;
         if (LANES <= 32 || j < r.live) {
@@ -565,6 +595,7 @@ __global__ void __launch_bounds__(RowLane<LANES>::kThreads, LANES > 32 ? 512 / L
 #pragma unroll
                 for (int e = N - 1; e >= 0; --e) rev.S = a[e].x * (w[e].x + a[e].y * (w[e].y + rev.S));
             }
+            if (!pl.good()) own.S = rev.S = not_known();
             const Step<LANES, true> ahead(own);
             const Step<LANES, false> behind(rev);
             if constexpr (LANES > 32) {
@@ -577,7 +608,7 @@ __global__ void __launch_bounds__(RowLane<LANES>::kThreads, LANES > 32 ? 512 / L
             float m = behind.enter(back, met, mu);
             auto put = [&](T *to, int place, f2 (&f)[N]) {
                 if (!whole) mask(f, lo, hi, 0.f);
-                if (r.real) pl.put(j & 1, place, to, r.start + first(j), first(j), i, t0, p.L, f);
+                if (r.real && pl.good()) pl.put(j & 1, place, to, r.start + first(j), first(j), i, t0, p.L, f);
             };
             // (lanes without a position take part in the stores and write zeros)
             f2 x[N];
@@ -617,7 +648,7 @@ __global__ void __launch_bounds__(RowLane<LANES>::kThreads, LANES > 32 ? 512 / L
             }
             put((T *)p.dv, 0, x);
             if (LANES > 32 && threadIdx.x == 0) back.carry[met & 1] = mu = m;
-        } else if (r.real) {
+        } else if (r.real && pl.good()) {
             f2 zero[N];
 #pragma unroll
             for (int e = 0; e < N; ++e) zero[e] = pair(0.f);
@@ -631,7 +662,12 @@ __global__ void __launch_bounds__(RowLane<LANES>::kThreads, LANES > 32 ? 512 / L
     if (STAGED && LANES > 32 && r.first >= r.live) { __syncthreads(); mu = back.carry[1]; }
     if (r.real && p.ds0 && r.segment == 0 && r.l == 0) { HN_G(p.ds0 + r.row, 4); p.ds0[r.row] = mu; }
     if (STAGED && pl.lane == 0) tma_wait_all0();
-    if (!pl.ok) atomicExch(&hn_rec_status, 1);
+    if (!pl.good()) {
+        const int j = pl.late;
+        pl.drain(j & 1, (j & 1 ? used[1] : used[0]) & 1, first(j));
+        if (j > r.first) pl.drain((j - 1) & 1, (j & 1 ? used[0] : used[1]) & 1, first(j - 1));
+        atomicExch(&hn_rec_status, 1);
+    }
 }
 
 // One token: a thread per channel.
@@ -751,6 +787,18 @@ static int check_shape(int B, int C, int L, int decay, int dtype)
     return HYENAND_OK;
 }
 
+#ifdef HYENAND_DEBUG
+static std::atomic<int> late_tile{-1}, late_warp{-1};
+#endif
+static RecArgs rec_args()
+{
+    RecArgs a{};
+#ifdef HYENAND_DEBUG
+    a.late_tile = late_tile; a.late_warp = late_warp;
+#endif
+    return a;
+}
+
 static int finish(int launched)
 {
     if (launched < 0) return fail(HYENAND_ERR_UNSUPPORTED, "kernel grid too large for one launch");
@@ -774,6 +822,17 @@ extern "C" long long hyenand_recurrence_workspace_bytes(int B, int C, int L, int
     return most > 1 ? rows * most * (long long)sizeof(float4) : 0;
 }
 
+extern "C" int hyenand_debug_recurrence_late(int tile, int warp)
+{
+#ifdef HYENAND_DEBUG
+    late_tile = tile; late_warp = warp;
+    return 0;
+#else
+    (void)tile; (void)warp;
+    return -1;
+#endif
+}
+
 extern "C" int hyenand_recurrence_device_status(void)
 {
     int v = 0;
@@ -788,7 +847,7 @@ extern "C" int hyenand_recurrence_forward(int B, int C, int L, int decay, int dt
     clear_error();
     if (int e = check_shape(B, C, L, decay, dtype)) return e;
     if (!q || !k || !v || !g || !y) return fail(HYENAND_ERR_INVALID_ARG, "q, k, v, g, y must be non-NULL");
-    RecArgs a{};
+    RecArgs a = rec_args();
     a.q = q; a.k = k; a.v = v; a.g = g; a.s0 = s0; a.lengths = lengths; a.y = y; a.s_end = s_end; a.marks = marks;
     a.rows = (long long)B * C; a.n = a.rows * L; a.C = C; a.L = L; a.marks_row = marks_of(L);
     a.segments = segments_of(a.rows, L, dtype, false); a.maps = (float4 *)workspace;
@@ -812,7 +871,7 @@ extern "C" int hyenand_recurrence_backward(int B, int C, int L, int decay, int d
     if (int e = check_shape(B, C, L, decay, dtype)) return e;
     if (!q || !k || !v || !g || !marks || !dy || !dq || !dk || !dv || !dg)
         return fail(HYENAND_ERR_INVALID_ARG, "q, k, v, g, marks, dy, dq, dk, dv, dg must be non-NULL");
-    RecArgs a{};
+    RecArgs a = rec_args();
     a.q = q; a.k = k; a.v = v; a.g = g; a.lengths = lengths; a.marks = (float *)marks; a.dy = dy; a.ds_end = ds_end;
     a.dq = dq; a.dk = dk; a.dv = dv; a.dg = dg; a.ds0 = ds0;
     a.rows = (long long)B * C; a.n = a.rows * L; a.C = C; a.L = L; a.marks_row = marks_of(L);
@@ -836,7 +895,7 @@ extern "C" int hyenand_recurrence_step(int B, int C, int decay, int dtype, const
     if (int e = check_shape(B, C, 1, decay, dtype)) return e;
     if (!q || !k || !v || !g || !state || !y || !new_state)
         return fail(HYENAND_ERR_INVALID_ARG, "q, k, v, g, state, y, new_state must be non-NULL");
-    RecArgs a{};
+    RecArgs a = rec_args();
     a.q = q; a.k = k; a.v = v; a.g = g; a.s0 = state; a.lengths = active; a.y = y; a.s_end = new_state;
     a.rows = a.n = (long long)B * C; a.C = C; a.L = 1; a.segments = 1;
     CallTensors c;

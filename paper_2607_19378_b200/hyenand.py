@@ -372,6 +372,10 @@ def hyenand_recurrence_device_status() -> int:
     return int(lib().hyenand_recurrence_device_status())
 
 
+def hyenand_debug_recurrence_late(tile: int, warp: int = -1) -> int:
+    return int(lib().hyenand_debug_recurrence_late(int(tile), int(warp)))
+
+
 def hyenand_recurrence_forward(B: int, C: int, L: int, decay: int, dtype: int, q, k, v, g, s0, lengths, y, s_end, marks, workspace=None,
                                stream=None) -> None:
     _check(lib().hyenand_recurrence_forward(B, C, L, decay, dtype, q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), _ptr(s0),
