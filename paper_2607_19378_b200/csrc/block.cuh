@@ -7,6 +7,7 @@
 #include "octet.cuh"
 #include "pair.cuh"
 #include "philox.cuh"
+#include "tile_walk.cuh"
 #include "tma_util.cuh"
 
 namespace hn {
@@ -212,18 +213,6 @@ __device__ __forceinline__ void drop_pairs(unsigned keep, f2 (&f)[P])
         f[e] = make2(keep >> (2 * e) & 1 ? x : 0.f, keep >> (2 * e + 1) & 1 ? y : 0.f);
     }
 }
-
-// A cluster's tiles: every `step`-th, as batch entry and first token, without a division per tile.
-struct TileWalk {
-    int b, r, step_b, step_r, per;                           // r: tile of the entry
-    __device__ __forceinline__ TileWalk(long long first, long long step, int tiles_b) : b((int)(first / tiles_b)), r((int)(first % tiles_b)),
-        step_b((int)(step / tiles_b)), step_r((int)(step % tiles_b)), per(tiles_b) {}
-    __device__ __forceinline__ void next()
-    {
-        b += step_b; r += step_r;
-        if (r >= per) { r -= per; ++b; }
-    }
-};
 
 // Sums over the channels of a tile's tokens: K sums of V tokens a thread -> K x TT totals of the cluster.
 template <int LT, int K> struct alignas(16) TileSums {

@@ -50,7 +50,7 @@ template <typename T, int LT, int N, bool ALIGNED> __global__ void __launch_boun
     }
     const long long entry = (long long)p.C * p.T, first = (long long)c0 * p.T, hop = (long long)ROWS * p.T;
     auto fetch = [&](char *stage, float (*to)[TT], const TileWalk &at) {
-        if (at.b < p.B) {
+        if (at.inside(p.B)) {
             const int t0 = at.r * TT;
             St::fetch(stage, at.b * entry + (long long)rank * share * p.T + t0, p.T, mine, p.T - t0, elements, [&](auto piece) {
                 piece(M, p.m);
@@ -72,7 +72,7 @@ template <typename T, int LT, int N, bool ALIGNED> __global__ void __launch_boun
     TileWalk here(blockIdx.x / ctas, gridDim.x / ctas, p.tiles_b), ahead = here;
     fetch(stages, rho[0], ahead);
     int meeting = 0;
-    for (int turn = 0; here.b < p.B; here.next(), turn ^= 1, ++meeting) {
+    for (int turn = 0; here.inside(p.B); here.next(), turn ^= 1, ++meeting) {
         char *stage = stages + turn * St::BYTES;
         stage_wait<0>();
         __syncthreads();                                     // this tile and its rho are here, and the other stage has been read

@@ -50,7 +50,7 @@ template <typename T, int LT, int N, bool ALIGNED> __global__ void __launch_boun
     }
     const long long entry = (long long)p.C * p.T, first = (long long)c0 * p.T, hop = (long long)ROWS * p.T;
     auto fetch = [&](char *stage, const TileWalk &w) {
-        if (w.b < p.B) {
+        if (w.inside(p.B)) {
             const int t0 = w.r * TT;
             St::fetch(stage, w.b * entry + (long long)rank * share * p.T + t0, p.T, mine, p.T - t0, elements, [&](auto piece) {
                 piece(M, p.m);
@@ -63,13 +63,14 @@ template <typename T, int LT, int N, bool ALIGNED> __global__ void __launch_boun
     TileWalk here(blockIdx.x / ctas, gridDim.x / ctas, p.tiles_b), ahead = here;
     fetch(stages, ahead);
     int meeting = 0;                                         // counted: parity of its slots, phase of its barrier
-    for (int turn = 0; here.b < p.B; here.next(), turn ^= 1, ++meeting) {
+    for (int turn = 0; here.inside(p.B); here.next(), turn ^= 1, ++meeting) {
         char *stage = stages + turn * St::BYTES;
         stage_wait<0>();
         __syncthreads();                                     // this tile is here, and the other stage has been read
         ahead.next();
         fetch(stages + (turn ^ 1) * St::BYTES, ahead);
-        const int b = here.b, t0 = here.r * TT, t = t0 + tl * V, count = p.T - t;
+        const unsigned b = here.b;
+        const int t0 = here.r * TT, t = t0 + tl * V, count = p.T - t;
         const long long row0 = b * entry + first + t0;       // element where the row of this thread's first channel starts
         f2 br[N][P], s[4][P];
         unsigned keep[N];
