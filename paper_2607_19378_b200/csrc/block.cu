@@ -307,7 +307,7 @@ static bool tile_shape(const BlockArgs &a, int dtype, bool backward, TileShape *
     return true;
 }
 
-// workspace slots written, or -1
+// workspace slots written, or below 0 (finish)
 static int block_launch(BlockArgs &a, int dtype, bool backward, cudaStream_t st)
 {
     TileShape s{};
@@ -321,7 +321,7 @@ static int block_launch(BlockArgs &a, int dtype, bool backward, cudaStream_t st)
     a.tiles_b = (a.T + 32 * tokens - 1) / (32 * tokens);
     a.tiles = (long long)a.B * a.tiles_b;
     const long long blocks = backward && a.tiles > kBlockSlots ? kBlockSlots : a.tiles;
-    if (blocks > 0x7fffffffll) return -1;
+    if (blocks > 0x7fffffffll) return kTooLarge;
 #define HN_BLK(T, V) launch_pdl(backward ? block_backward_kernel<T, V> : block_forward_kernel<T, V>, dim3((unsigned)blocks), kBlockWarps<V> * 32, 0, st, a)
     if (dtype == HYENAND_F32) { if (tokens == 4) HN_BLK(float, 4); else HN_BLK(float, 1); }
     else { if (tokens == 4) HN_BLK(bf16, 4); else HN_BLK(bf16, 1); }
@@ -352,13 +352,6 @@ static void block_inputs(CallTensors &c, const BlockArgs &a, size_t nb)
     c.in("x", a.x, nb); c.in("m", a.m, nb); c.in("z", a.z, nb);
     c.in("g_post", a.g_post, wb, 4); c.in("scale", a.scale, wb, 4); c.in("g_pre", a.g_pre, wb, 4);
     if (a.drop.threshold) c.in("rng", a.drop.rng, 2 * sizeof(long long));
-}
-
-static int finish(int launched)
-{
-    if (launched < 0) return fail(HYENAND_ERR_UNSUPPORTED, "kernel grid too large for one launch");
-    const cudaError_t e = cudaGetLastError();
-    return e == cudaSuccess ? HYENAND_OK : fail(HYENAND_ERR_CUDA, "kernel launch failed: %s", cudaGetErrorString(e));
 }
 
 }  // namespace hn

@@ -317,7 +317,7 @@ int block_backward_status();
 
 // How the tile kernels take a shape (block.cu): lanes along the tokens, channels of a thread, CTAs of a cluster.
 struct TileShape { int lt, n, ctas; };
-// clusters launched (slots of the workspace that a backward has written), or -1
+// clusters launched (slots of the workspace that a backward has written), or below 0 (finish)
 int launch_block_tile_forward(const BlockArgs &a, int dtype, const TileShape &s, cudaStream_t st);
 int launch_block_tile_backward(const BlockArgs &a, int dtype, const TileShape &s, cudaStream_t st);
 
@@ -350,10 +350,10 @@ template <auto FN, int BYTES> static int launch_tiles(const BlockArgs &a, const 
         }
         return n < 1 ? -1 : n < kBlockSlots ? n : kBlockSlots;
     });
-    if (most < 1) return -1;
+    if (most < 1) return kNoLaunch;
     const long long clusters = a.tiles < most ? a.tiles : most;
     c.gridDim = dim3((unsigned)(clusters * s.ctas));
-    return cudaLaunchKernelEx(&c, FN, a, s.ctas) == cudaSuccess ? (int)clusters : -1;
+    return cudaLaunchKernelEx(&c, FN, a, s.ctas) == cudaSuccess ? (int)clusters : kNoLaunch;
 }
 
 }  // namespace hn

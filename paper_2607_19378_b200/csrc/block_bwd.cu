@@ -235,7 +235,7 @@ template <typename T> static int by_shape(const BlockArgs &a, const TileShape &s
     if constexpr (MOST >= 4) if (s.n == 3) return by_alignment<T, 8, 3>(a, s, st);
     if (s.n == 4) return by_alignment<T, 8, 4>(a, s, st);
     if constexpr (MOST >= 4) if (s.n == 8) return by_alignment<T, 8, 8>(a, s, st);
-    return -1;
+    return kNoLaunch;
 }
 
 int launch_block_tile_backward(const BlockArgs &a, int dtype, const TileShape &s, cudaStream_t st)

@@ -79,6 +79,5 @@ extern "C" int hyenand_dropout(long long n, int dtype, const void *x, float p, c
     const cudaStream_t st = (cudaStream_t)cuda_stream;
     if (dtype == HYENAND_F32) launch_pdl(dropout_kernel<float>, grid, kDropThreads, 0, st, (const float *)x, (float *)y, n, d);
     else launch_pdl(dropout_kernel<bf16>, grid, kDropThreads, 0, st, (const bf16 *)x, (bf16 *)y, n, d);
-    const cudaError_t e = cudaGetLastError();
-    return e == cudaSuccess ? HYENAND_OK : fail(HYENAND_ERR_CUDA, "kernel launch failed: %s", cudaGetErrorString(e));
+    return finish(0);
 }

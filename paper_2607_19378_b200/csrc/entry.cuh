@@ -15,6 +15,17 @@ void clear_error();                                  // at the head of every ent
 
 static inline size_t elsize(int dtype) { return dtype == HYENAND_F32 ? 4 : 2; }
 
+// What became of a call's launches; `launched` below 0: one was not made (kTooLarge, or the runtime's error says why).  The error is
+// taken with it: left behind, it would be the next call's, whose kernel is on its way.
+constexpr int kNoLaunch = -1, kTooLarge = -2;
+static inline int finish(int launched)
+{
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return fail(HYENAND_ERR_CUDA, "kernel launch failed: %s", cudaGetErrorString(e));
+    if (launched == kTooLarge) return fail(HYENAND_ERR_UNSUPPORTED, "kernel grid too large for one launch");
+    return launched < 0 ? fail(HYENAND_ERR_CUDA, "kernel launch failed: the device holds no such CTA or cluster") : HYENAND_OK;
+}
+
 // What a launch works out once per device (a kernel's limits, how many of its CTAs run at once), whichever thread comes first.
 struct PerDevice {
     std::mutex lock;

@@ -698,9 +698,9 @@ template <auto FN, int LANES, int BYTES> static int launch_rows(const RecArgs &a
 {
     using R = RowLane<LANES>;
     const long long blocks = (a.rows + R::kRows - 1) / R::kRows * a.segments;
-    if (blocks > 0x7fffffffll) return -1;
+    if (blocks > 0x7fffffffll) return kTooLarge;
     static PerDevice ready;
-    if (BYTES > 32 * 1024 && !ready.once([] { return cudaFuncSetAttribute(FN, cudaFuncAttributeMaxDynamicSharedMemorySize, BYTES) == cudaSuccess ? 1 : -1; })) return -1;
+    if (BYTES > 32 * 1024 && !ready.once([] { return cudaFuncSetAttribute(FN, cudaFuncAttributeMaxDynamicSharedMemorySize, BYTES) == cudaSuccess ? 1 : -1; })) return kNoLaunch;
     launch_pdl(FN, dim3((unsigned)blocks), R::kThreads, BYTES, st, a);
     return 0;
 }
@@ -708,7 +708,8 @@ template <typename T, int DECAY, bool BWD, int OCT, int LANES, bool STAGED> stat
 {
     constexpr int THREADS = RowLane<LANES>::kThreads;
     if constexpr (STAGED && LANES == 32)
-        if (a.segments > 1 && launch_rows<recurrence_maps_kernel<T, DECAY, OCT, !BWD>, LANES, 2 * Places<T, OCT, 3, THREADS, true>::STAGE>(a, st)) return -1;
+        if (a.segments > 1)
+            if (const int e = launch_rows<recurrence_maps_kernel<T, DECAY, OCT, !BWD>, LANES, 2 * Places<T, OCT, 3, THREADS, true>::STAGE>(a, st)) return e;
     if constexpr (BWD) return launch_rows<recurrence_backward_kernel<T, DECAY, OCT, LANES, STAGED>, LANES, 2 * Places<T, OCT, 5, THREADS, STAGED>::STAGE>(a, st);
     else return launch_rows<recurrence_forward_kernel<T, DECAY, OCT, LANES, STAGED>, LANES, 2 * Places<T, OCT, 4, THREADS, STAGED>::STAGE>(a, st);
 }
@@ -769,7 +770,7 @@ template <bool BWD> static int launch_recurrence(const RecArgs &a, int decay, in
 static int launch_step(const RecArgs &a, int decay, int dtype, cudaStream_t st)
 {
     const long long blocks = (a.rows + 255) / 256;
-    if (blocks > 0x7fffffffll) return -1;
+    if (blocks > 0x7fffffffll) return kTooLarge;
     void (*fn)(RecArgs) = dtype == HYENAND_F32
         ? (decay == DECAY_VALUE ? recurrence_step_kernel<float, DECAY_VALUE> : decay == DECAY_LOG ? recurrence_step_kernel<float, DECAY_LOG> : recurrence_step_kernel<float, DECAY_SIGMOID>)
         : (decay == DECAY_VALUE ? recurrence_step_kernel<bf16, DECAY_VALUE> : decay == DECAY_LOG ? recurrence_step_kernel<bf16, DECAY_LOG> : recurrence_step_kernel<bf16, DECAY_SIGMOID>);
@@ -797,13 +798,6 @@ static RecArgs rec_args()
     a.late_tile = late_tile; a.late_warp = late_warp;
 #endif
     return a;
-}
-
-static int finish(int launched)
-{
-    if (launched < 0) return fail(HYENAND_ERR_UNSUPPORTED, "kernel grid too large for one launch");
-    const cudaError_t e = cudaGetLastError();
-    return e == cudaSuccess ? HYENAND_OK : fail(HYENAND_ERR_CUDA, "kernel launch failed: %s", cudaGetErrorString(e));
 }
 
 // marks of a row: one in front of every tile of kMarkOctets octets a row of L positions can touch
