@@ -2,7 +2,8 @@
 //
 // One meeting of the cluster a tile: beside sum m^2 it gathers sum x^2, sum x b and sum b^2 with b = scale D act(z) g_post m, and since
 // r = x + rho_m b,   sum r^2 = sum x^2 + 2 rho_m sum x b + rho_m^2 sum b^2.   Where the branch cancels most of x that difference
-// loses what matters (below a quarter of the squares it comes from); such a tile meets once more and adds up r^2 itself.
+// loses what matters (below a quarter of the squares it comes from), and where m is above 1e17 or so the squares of b, which rho_m has
+// not brought down yet, are infinite; such a tile meets once more and adds up r^2 itself.
 //
 // 44 instructions an element with gate and dropout, and 16 warps an SM (registers; two stages of three tensors in shared memory) keep the
 // issue slots 44 % busy: the CTA's three barriers a tile and the meeting take the rest.  16 x 4096 tokens of 768 channels, bf16: 144 us
@@ -103,8 +104,8 @@ template <typename T, int LT, int N, bool ALIGNED> __global__ void __launch_boun
         bool cancelled = false;
         const float inv = 1.f / (float)p.C;
         sums.sum(s, ctas, rank, meeting & 1, meeting >> 1 & 1, [&](int k, const float (&a)[4]) {
-            const float rm = p.g_post ? rsqrtf(a[0] * inv + p.eps) : 1.f, bb = rm * rm * a[3], rr = fmaf(2.f * rm, a[2], a[1]) + bb;
-            cancelled = p.g_pre && rr < 0.25f * (a[1] + bb);
+            const float rm = p.g_post ? rsqrtf(a[0] * inv + p.eps) : 1.f, bb = rm * (rm * a[3]), rr = fmaf(2.f * rm, a[2], a[1]) + bb;
+            cancelled = p.g_pre && !(rr >= 0.25f * (a[1] + bb) && rr <= 3.402823466e38f);
             const float rn = rsqrtf(fmaxf(rr, 0.f) * inv + p.eps);
             sums.total[0][k] = rm;
             sums.total[1][k] = rn;
