@@ -229,9 +229,9 @@ template <typename T, int V> __global__ void __launch_bounds__(kBlockWarps<V> * 
                 for (int e = 0; e < V; ++e) {
                     d[e] = dr[e] + rho_r[e] * (en[e] * g - rh[e] * c1[e]);
                     const bool kept = o.D[e] != 0.f;
-                    const float mn = o.mh[e] * o.gp, dD = kept ? d[e] * o.D[e] : 0.f, dw = o.sc * dD, df = dw * o.act[e];
-                    dz[e] = dw * mn * o.slope[e];
-                    sum[0] += df * o.mh[e];
+                    const float mn = o.mh[e] * o.gp, dD = kept ? d[e] * o.D[e] : 0.f, dw = o.sc * dD, df = kept ? dw * o.act[e] : 0.f;
+                    dz[e] = kept ? dw * mn * o.slope[e] : 0.f;
+                    sum[0] += kept ? df * o.mh[e] : 0.f;
                     sum[1] += kept ? dD * (o.act[e] * mn) : 0.f;
                     sum[2] = fmaf(en[e], rh[e], sum[2]);
                     dm[e] = p.g_post ? rho_m[e] * (df * o.gp - o.mh[e] * c2[e]) : df;

@@ -155,7 +155,7 @@ template <typename T, int LT, int N, bool ALIGNED> __global__ void __launch_boun
 #pragma unroll
                 for (int e = 0; e < P; ++e) am[e] = m[e];
             }
-            if (drop && !p.g_post) { drop_pairs(keep[j], m); drop_pairs(keep[j], am); }      // (nothing may come of what was dropped, not even 0 times infinity)
+            if (drop) drop_pairs(keep[j], am);               // (nothing may come of what was dropped, not even 0 times infinity)
             if (p.dr) St::get(stage, DR, j, start, count, d);
             else d[0] = d[1] = pair(0.f);
             if (p.dn) {
@@ -163,27 +163,31 @@ template <typename T, int LT, int N, bool ALIGNED> __global__ void __launch_boun
                 St::get(stage, DN, j, start, count, n);
                 St::get(stage, X, j, start, count, r);
 #pragma unroll
-                for (int e = 0; e < P; ++e) k[e] = mul2(am[e], pair(w[j]));
-                if (drop) drop_pairs(keep[j], k);
-#pragma unroll
                 for (int e = 0; e < P; ++e) {
+                    k[e] = mul2(am[e], pair(w[j]));
                     r[e] = fma2(rm[e], k[e], r[e]);
                     d[e] = fma2(mul2(n[e], rr[e]), pair(gn[j]), d[e]);
                     d[e] = fma2(r[e], c1[e], d[e]);
                 }
             }
             st_vector<T, ALIGNED>(p.dx, i, count, d);
-            if (drop) drop_pairs(keep[j], d);
 #pragma unroll
             for (int e = 0; e < P; ++e) {
-                f2 q = mul2(d[e], rm[e]);
-                local = fma2(q, am[e], local);               // sum of keep d act m^: dg_post and dscale but for their constants
-                q = mul2(q, pair(w[j]));
+                d[e] = mul2(d[e], rm[e]);
+                local = fma2(d[e], am[e], local);            // sum of keep d act m^: dg_post and dscale but for their constants
+                d[e] = mul2(d[e], pair(w[j]));
                 if (p.z) {
-                    da[e] = mul2(mul2(q, m[e]), da[e]);
-                    q = mul2(q, a[e]);
+                    da[e] = mul2(mul2(d[e], m[e]), da[e]);
+                    d[e] = mul2(d[e], a[e]);
                 }
-                d[e] = p.g_post ? fma2(m[e], c2[e], q) : q;
+            }
+            if (drop) {
+                drop_pairs(keep[j], d);
+                if (p.z) drop_pairs(keep[j], da);
+            }
+            if (p.g_post) {
+#pragma unroll
+                for (int e = 0; e < P; ++e) d[e] = fma2(m[e], c2[e], d[e]);
             }
             acc[j][0] += sum2(local);
             st_vector<T, ALIGNED>(p.dm, i, count, d);
