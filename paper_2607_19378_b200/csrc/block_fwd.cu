@@ -136,6 +136,7 @@ template <typename T, int LT, int N, bool ALIGNED> __global__ void __launch_boun
                 for (int j = 0; j < N; ++j) s[0][e] = fma2(br[j][e], br[j][e], s[0][e]);
             }
             sums.sum(s, ctas, rank, meeting & 1, meeting >> 1 & 1, [&](int k, const float (&a)[4]) {
+                if (!cancelled) return;                      // (a token's result is its own: its neighbours in the tile do not change it)
                 const float rn = rsqrtf(a[0] * inv + p.eps);
                 sums.total[1][k] = rn;
                 if (p.stats && rank == 0 && t0 + k < p.T) {

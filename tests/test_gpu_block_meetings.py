@@ -52,3 +52,17 @@ def test_squares_beyond_fp32(B, C, T, dtype):
     t["m"], t["z"] = (t["m"].float() * 1e17 / 3).to(DTYPES[dtype]), torch.full_like(t["z"], 100.0)
     t["m"][:, :, 1::5] *= 1e-17
     check(t, B, C, T, dtype, "silu")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,C,T", SHAPES, ids=str)
+def test_tokens_do_not_change_their_neighbours(B, C, T, dtype):
+    """A token that cancels, or holds a NaN, sends its tile into the second meeting: the others keep their bits."""
+    t = inputs(B, C, T, DTYPES[dtype], "silu", True, True, True, 7 + C + T)
+    want = run(t, B, C, T, DTYPES[dtype], "silu", 0.0)
+    branch = torch.from_numpy(ob.block(torch.zeros_like(t["x"]), t["m"], t["z"], t["g_post"], t["scale"], None, EPS, "silu")["r"])
+    other = torch.arange(T) % 3 == 1
+    for change in ((-(1 - 2.0 ** -12) * branch).to(DTYPES[dtype]), torch.full_like(t["x"], float("nan")), torch.full_like(t["x"], 3e19)):
+        got = run(dict(t, x=torch.where(other, change, t["x"])), B, C, T, DTYPES[dtype], "silu", 0.0)
+        for name in ("r", "n", "dx", "dm", "dz"):
+            assert torch.equal(got[name][:, :, ~other], want[name][:, :, ~other]), name
