@@ -51,13 +51,16 @@ constexpr int kForwardBytes = 16, kBackwardBytes = 8;
 
 constexpr int V = 4, P = V / 2;                              // tokens of a thread, and pairs of them
 
+// the smaller of two, NaN where either is (fminf takes the other)
+__device__ __forceinline__ float min_or_nan(float x, float y) { float r; asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y)); return r; }
+
 // act(z), and with SLOPE act'(z).  exp(-z) is held below the largest float: where it would be infinite, sigmoid(z) is 0 and
 // 1 - sigmoid(z) = exp(-z) sigmoid(z) must not be infinity times 0.
 template <bool SILU, bool SLOPE> __device__ __forceinline__ void gate_pair(f2 z, f2 &a, f2 &da)
 {
     float x, y;
     split2(mul2(z, pair(-1.4426950408889634f)), x, y);
-    const f2 e = SLOPE ? make2(fminf(ex2(x), 3e38f), fminf(ex2(y), 3e38f)) : make2(ex2(x), ex2(y));
+    const f2 e = SLOPE ? make2(min_or_nan(ex2(x), 3e38f), min_or_nan(ex2(y), 3e38f)) : make2(ex2(x), ex2(y));
     split2(add2(e, pair(1.f)), x, y);
     const f2 s = make2(rcp(x), rcp(y));
     a = SILU ? mul2(z, s) : s;
