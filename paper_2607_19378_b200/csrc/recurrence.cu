@@ -55,15 +55,15 @@ __device__ __forceinline__ float apply(const Map &m, float s)
 // a first, then b
 __device__ __forceinline__ Map compose(const Map &a, const Map &b) { return {a.A * b.A, fmaf(a.P, b.P, a.P + b.P), apply(b, a.S)}; }
 
-// a_t and 1 - a_t (LOG: not needed, 0).  The approximate exponential and reciprocal are off by a few roundings, which a thread's steps
+// a_t and 1 - a_t (LOG: see decays).  The approximate exponential and reciprocal are off by a few roundings, which a thread's steps
 // can multiply up sixteen-fold at most: what goes on from thread to thread is built from 1 - a_t and the sum of the g_t.
 __device__ __forceinline__ float not_known() { return __int_as_float(0x7fffffff); }      // NaN
 constexpr float kLog2e = 1.4426950408889634f;
 template <int DECAY> __device__ __forceinline__ void decay(float g, float &a, float &na)
 {
     if constexpr (DECAY == DECAY_VALUE) { a = g; na = 1.f - g; }
-    else if constexpr (DECAY == DECAY_LOG) { a = ex2(g * kLog2e); na = 0.f; }
     else {
+        static_assert(DECAY == DECAY_SIGMOID, "");
         // the larger one as 1 - the smaller: half a unit off, to no side, where the reciprocal's 1 / (1 + e) drifted by 5e-7 of a state over a
         // thread's steps
         const float e = ex2(-kLog2e * fabsf(g)), x = e * rcp(1.f + e), r = 1.f - x;
@@ -670,6 +670,27 @@ __global__ void __launch_bounds__(RowLane<LANES>::kThreads, LANES > 32 ? 512 / L
     }
 }
 
+// a s + u for one token.  A decay next to 1 loses what it is in its own rounding (exp(-1e-6) is off by 2 % of its distance from 1, and
+// 40000 tokens one by one by 5e-4 of the state): there it is s + (a - 1) s + u with a - 1 as precise as a number of its own, and the
+// sum's is the one rounding of the state's size.  An infinite state stays one.  The call is a launch whatever it computes.
+template <int DECAY> __device__ __forceinline__ float step_state(float g, float s, float u)
+{
+    if constexpr (DECAY == DECAY_VALUE) return fmaf(g, s, u);
+    float a, less;                                           // a, and a - 1 where a is above a half
+    bool close;
+    if constexpr (DECAY == DECAY_LOG) {
+        close = g > -0.6931472f;
+        a = expf(g);
+        less = expm1f(g);
+    } else {
+        const float e = expf(-fabsf(g)), x = e / (1.f + e);
+        close = g >= 0.f;
+        a = close ? 1.f - x : x;
+        less = -x;
+    }
+    return close && fabsf(s) <= 3.402823466e38f ? s + fmaf(less, s, u) : fmaf(a, s, u);
+}
+
 // One token: a thread per channel.
 template <typename T, int DECAY> __global__ void __launch_bounds__(256) recurrence_step_kernel(RecArgs p)
 {
@@ -685,9 +706,7 @@ template <typename T, int DECAY> __global__ void __launch_bounds__(256) recurren
         in = __ldg(p.lengths + b) > 0;
     }
     if (in) {
-        float a, na;
-        decay<DECAY>(IO<T>::ld((const T *)p.g, i), a, na);
-        s = fmaf(a, s, IO<T>::ld((const T *)p.k, i) * IO<T>::ld((const T *)p.v, i));
+        s = step_state<DECAY>(IO<T>::ld((const T *)p.g, i), s, IO<T>::ld((const T *)p.k, i) * IO<T>::ld((const T *)p.v, i));
         out = IO<T>::ld((const T *)p.q, i) * s;
     }
     IO<T>::st((T *)p.y, i, out);
