@@ -82,8 +82,8 @@ template <typename F> PyObject *guarded(F f)
         return f();
     } catch (const PythonError &) {
         return nullptr;
-    } catch (const std::exception &e) {
-        PyErr_SetString(PyExc_RuntimeError, e.what());
+    } catch (...) {                                          // (as torch's own calls raise it: an allocation that fails is OutOfMemoryError)
+        torch::translate_exception_to_python(std::current_exception());
         return nullptr;
     }
 }
