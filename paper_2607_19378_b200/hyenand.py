@@ -641,6 +641,8 @@ class Dropout:
 
     def __init__(self, p: float, site: int = 0):
         self.p, self.site, self._ops, self._call = float(p), int(site), _calls(), _address("hyenand_dropout")
+        if not -1 << 31 <= self.site < 1 << 31:
+            raise OverflowError("site must fit in 32 bits")     # (cut off, it would be another dropout's)
 
     def __call__(self, x, rng, y=None, stream=None):
         if stream is not None:
