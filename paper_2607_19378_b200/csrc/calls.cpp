@@ -57,6 +57,12 @@ struct Arguments {
     void *stream() const { return (void *)c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream(); }
 };
 
+bool truth(PyObject *o)
+{
+    const int t = PyObject_IsTrue(o);
+    if (t < 0) throw PythonError();
+    return t == 1;
+}
 void *data(const Tensor *t) { return t ? t->data_ptr() : nullptr; }
 PyObject *wrap(const Tensor &t) { return t.defined() ? THPVariable_Wrap(t) : Py_NewRef(Py_None); }
 PyObject *tuple(std::initializer_list<Tensor> ts)
@@ -144,7 +150,7 @@ PyObject *recurrence_forward(PyObject *, PyObject *const *a, Py_ssize_t n)
                      *g = want(a[4], "g", r->type, r->shape), *s0 = want(a[5], "s0", at::kFloat, r->states, true),
                      *len = want(a[6], "lengths", at::kInt, r->batch, true), *given = want(a[8], "y", r->type, r->shape, true);
         const Tensor y = given ? *given : want.empty(r->shape, r->type), end = want.empty(r->states, at::kFloat);
-        const bool keep = PyObject_IsTrue(a[7]) == 1;
+        const bool keep = truth(a[7]);
         const Tensor marks = keep ? want.empty(r->marks, at::kFloat) : Tensor(), work = r->workspace ? want.empty({r->workspace}, at::kByte) : Tensor();
         check(r->forward(r->B, r->C, r->L, r->decay, r->dtype, data(q), data(k), data(v), data(g), (const float *)data(s0), (const int *)data(len),
                          y.data_ptr(), (float *)end.data_ptr(), keep ? (float *)marks.data_ptr() : nullptr, r->workspace ? work.data_ptr() : nullptr, want.stream()), r->raise_error);
@@ -230,7 +236,7 @@ PyObject *block_forward(PyObject *, PyObject *const *a, Py_ssize_t n)
         const Tensor *x = want(a[1], "x", b->type, b->shape), *m = want(a[2], "m", b->type, b->shape), *z = want(a[3], "z", b->type, b->shape, true),
                      *gp = want(a[4], "g_post", at::kFloat, b->channels, true), *sc = want(a[5], "scale", at::kFloat, b->channels, true),
                      *gn = want(a[6], "g_pre", at::kFloat, b->channels, true), *rng = want(a[7], "rng", at::kLong, kTwo, true);
-        const bool keep = PyObject_IsTrue(a[8]) == 1;
+        const bool keep = truth(a[8]);
         const Tensor r = want.empty(b->shape, b->type), nn = gn ? want.empty(b->shape, b->type) : Tensor(),
                      st = keep ? want.empty(b->stats, at::kFloat) : Tensor();
         check(b->forward(b->B, b->C, b->T, b->dtype, data(x), data(m), data(z), (const float *)data(gp), (const float *)data(sc), (const float *)data(gn),
