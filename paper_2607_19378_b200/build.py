@@ -30,12 +30,21 @@ DEBUG_FLAGS = ["-lineinfo", "--compress-mode=size", "-DHYENAND_DEBUG"]
 PRECISE = {"synth.cu", "recurrence.cu"}
 
 
+def calls_path() -> str:
+    """Where the module _calls lies for this interpreter and this torch: it is compiled against the headers of both, and another's would
+    fail as it is loaded, or later."""
+    import sysconfig
+
+    import torch
+    return os.path.join(HERE, f"_calls.{sysconfig.get_config_var('SOABI')}.torch-{torch.__version__}.so")
+
+
 def build_calls(force: bool = False) -> str:
     """The compiled side of the binding's classes (csrc/calls.cpp): host code against torch's headers, as the module _calls."""
     import sysconfig
 
     import torch
-    src, out = os.path.join(CSRC, "calls.cpp"), os.path.join(HERE, "_calls.so")
+    src, out = os.path.join(CSRC, "calls.cpp"), calls_path()
     newest = max(os.path.getmtime(src), os.path.getmtime(os.path.join(os.path.dirname(HERE), "include", "hyenand.h")))
     if not force and os.path.exists(out) and os.path.getmtime(out) >= newest:
         return out

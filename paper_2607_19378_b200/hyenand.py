@@ -10,10 +10,14 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import importlib.machinery
+import importlib.util
 import math
 import os
 
 import torch
+
+from .build import calls_path
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 # HYENAND_LIB=debug selects the checked build (libhyenand_debug.so, see hyenand_debug_build in the header)
@@ -556,10 +560,13 @@ def _pool(stream):
 @functools.lru_cache(maxsize=1)
 def _calls():
     """The compiled side of the classes below (csrc/calls.cpp); raises if it was never built."""
+    path, name = calls_path(), __package__ + "._calls"
     try:
-        from . import _calls as module
+        spec = importlib.util.spec_from_file_location(name, path, loader=importlib.machinery.ExtensionFileLoader(name, path))
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
     except ImportError as e:
-        raise OSError(f"{_HERE}/_calls.so cannot be loaded ({e}): build it with `python -m paper_2607_19378_b200.build`") from e
+        raise OSError(f"{path} cannot be loaded ({e}): build it with `python -m paper_2607_19378_b200.build`") from e
     return module
 
 
