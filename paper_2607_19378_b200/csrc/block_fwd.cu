@@ -177,15 +177,26 @@ template <typename T, int LT, int N> static int by_alignment(const BlockArgs &a,
 {
     return a.T % (16 / sizeof(T)) == 0 ? go<T, LT, N, true>(a, s, st) : go<T, LT, N, false>(a, s, st);
 }
+// for shapes that come with rows on 16-byte boundaries only
+template <typename T, int LT, int N> static int aligned_only(const BlockArgs &a, const TileShape &s, cudaStream_t st)
+{
+    return a.T % (16 / sizeof(T)) == 0 ? go<T, LT, N, true>(a, s, st) : kNoLaunch;
+}
+// What tile_shape (block.cu) can ask for.  Ragged rows have half the channels a thread: of fp32 they come with 1, 2 or 4 (1 with them
+// alone), of bf16 never with 6; fp32 never with 6 either (from 1025 channels on it is at least seven).
 template <typename T> static int by_shape(const BlockArgs &a, const TileShape &s, cudaStream_t st)
 {
-    if (s.lt == 32) return s.n == 1 ? by_alignment<T, 32, 1>(a, s, st) : s.n == 2 ? by_alignment<T, 32, 2>(a, s, st) : by_alignment<T, 32, 4>(a, s, st);
-    if constexpr (sizeof(T) == 4) if (s.n == 1) return by_alignment<T, 8, 1>(a, s, st);
-    if (s.n == 2) return by_alignment<T, 8, 2>(a, s, st);
-    if (s.n == 3) return by_alignment<T, 8, 3>(a, s, st);
-    if (s.n == 4) return by_alignment<T, 8, 4>(a, s, st);
-    if constexpr (sizeof(T) == 2) if (s.n == 6) return go<T, 8, 6, true>(a, s, st);      // (fp32 and ragged rows come with at least seven)
-    return by_alignment<T, 8, 8>(a, s, st);
+    constexpr bool F32 = sizeof(T) == 4;
+    if (s.n == 2) return s.lt == 32 ? by_alignment<T, 32, 2>(a, s, st) : by_alignment<T, 8, 2>(a, s, st);
+    if constexpr (F32) {
+        if (s.n == 1) return s.lt == 32 ? by_alignment<T, 32, 1>(a, s, st) : go<T, 8, 1, false>(a, s, st);
+        if (s.n == 4) return s.lt == 32 ? aligned_only<T, 32, 4>(a, s, st) : by_alignment<T, 8, 4>(a, s, st);
+        return s.n == 3 ? aligned_only<T, 8, 3>(a, s, st) : aligned_only<T, 8, 8>(a, s, st);
+    } else {
+        if (s.n == 1) return by_alignment<T, 32, 1>(a, s, st);
+        if (s.n == 4) return s.lt == 32 ? by_alignment<T, 32, 4>(a, s, st) : by_alignment<T, 8, 4>(a, s, st);
+        return s.n == 3 ? by_alignment<T, 8, 3>(a, s, st) : s.n == 6 ? aligned_only<T, 8, 6>(a, s, st) : by_alignment<T, 8, 8>(a, s, st);
+    }
 }
 
 int launch_block_tile_forward(const BlockArgs &a, int dtype, const TileShape &s, cudaStream_t st)
