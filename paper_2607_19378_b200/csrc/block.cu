@@ -59,10 +59,16 @@ __device__ __forceinline__ void branch_of(const BlockArgs &p, const DropKey *key
     if (p.scale) { HN_G(p.scale + c, 4); o.sc = __ldg(p.scale + c); }
     unsigned keep = ~0u;
     if (key) keep = key->keep(i >> 3) >> (i & 7);
+    const bool silu = p.gate == GATE_SILU;
 #pragma unroll
     for (int e = 0; e < V; ++e) {
         o.act[e] = 1.f; o.slope[e] = 0.f;
-        if (p.z) gate_of(p.gate, z[e], o.act[e], o.slope[e]);
+        if (p.z) {
+            f2 s, st;                                        // sigmoid and its slope; z s and s + z s' without a branch between the loads
+            gate_pair<false, true>(pair(z[e]), s, st);
+            o.act[e] = silu ? z[e] * s.x : s.x;
+            o.slope[e] = silu ? fmaf(z[e], st.x, s.x) : st.x;
+        }
         o.D[e] = key ? (keep >> e & 1 ? p.drop.scale : 0.f) : 1.f;
         o.mh[e] = m[e] * rho[e];
     }

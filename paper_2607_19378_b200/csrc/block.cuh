@@ -28,14 +28,6 @@ struct BlockArgs {
     int tiles_b;                              // of one
 };
 
-// act(z) and act'(z); 1 - sigmoid is formed without cancellation
-__device__ __forceinline__ void gate_of(int kind, float z, float &a, float &da)
-{
-    const float e = __expf(-fabsf(z)), r = 1.f / (1.f + e), s = z >= 0.f ? r : e * r, t = z >= 0.f ? e * r : r;
-    if (kind == GATE_SILU) { a = z * s; da = s * fmaf(z, t, 1.f); }
-    else { a = s; da = s * t; }
-}
-
 // ---- tile kernels ---------------------------------------------------------------------------------------------------
 //
 // A thread works on four neighbouring tokens of N channels; LT lanes side by side make a tile of tokens, the other lanes and the warps
