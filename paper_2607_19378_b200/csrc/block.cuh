@@ -199,14 +199,14 @@ template <int N> __device__ __forceinline__ void keep_bits(const DropKey &key, b
         if (shift + V > 8) keep[j] |= key.keep((i >> 3) + 1) << (8 - shift);
     }
 }
+__device__ __forceinline__ void drop_pair(unsigned keep, int e, f2 &f)
+{
+    f = make2(keep >> (2 * e) & 1 ? f.x : 0.f, keep >> (2 * e + 1) & 1 ? f.y : 0.f);
+}
 __device__ __forceinline__ void drop_pairs(unsigned keep, f2 (&f)[P])
 {
 #pragma unroll
-    for (int e = 0; e < P; ++e) {
-        float x, y;
-        split2(f[e], x, y);
-        f[e] = make2(keep >> (2 * e) & 1 ? x : 0.f, keep >> (2 * e + 1) & 1 ? y : 0.f);
-    }
+    for (int e = 0; e < P; ++e) drop_pair(keep, e, f[e]);
 }
 
 // Sums over the channels of a tile's tokens: K sums of V tokens a thread -> K x TT totals of the cluster.

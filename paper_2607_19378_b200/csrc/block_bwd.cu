@@ -173,21 +173,16 @@ template <typename T, int LT, int N, bool ALIGNED> __global__ void __launch_boun
             st_vector<T, ALIGNED>(p.dx, i, count, d);
 #pragma unroll
             for (int e = 0; e < P; ++e) {
-                d[e] = mul2(d[e], rm[e]);
-                local = fma2(d[e], am[e], local);            // sum of keep d act m^: dg_post and dscale but for their constants
-                d[e] = mul2(d[e], pair(w[j]));
+                f2 q = mul2(d[e], rm[e]);
+                local = fma2(q, am[e], local);               // sum of keep d act m^: dg_post and dscale but for their constants
+                q = mul2(q, pair(w[j]));
                 if (p.z) {
-                    da[e] = mul2(mul2(d[e], m[e]), da[e]);
-                    d[e] = mul2(d[e], a[e]);
+                    da[e] = mul2(mul2(q, m[e]), da[e]);
+                    q = mul2(q, a[e]);
+                    if (drop) drop_pair(keep[j], e, da[e]);
                 }
-            }
-            if (drop) {
-                drop_pairs(keep[j], d);
-                if (p.z) drop_pairs(keep[j], da);
-            }
-            if (p.g_post) {
-#pragma unroll
-                for (int e = 0; e < P; ++e) d[e] = fma2(m[e], c2[e], d[e]);
+                if (drop) drop_pair(keep[j], e, q);
+                d[e] = p.g_post ? fma2(m[e], c2[e], q) : q;
             }
             acc[j][0] += sum2(local);
             st_vector<T, ALIGNED>(p.dm, i, count, d);
