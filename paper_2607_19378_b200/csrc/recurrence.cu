@@ -307,11 +307,13 @@ template <typename T, int OCT, int TENSORS, int THREADS, bool STAGED> struct Pla
             if (bytes)
                 for (int k = 0; k < TENSORS; ++k) { HN_G(in[k] + i, bytes); bulk_load(place(turn, k), in[k] + i, bytes, bars + turn); }
         }
-        if (last > n && end + lane < n)                      // (the octet that the tensor ends in)
+        if (last > n && end + lane < n) {                    // (the octet that the tensor ends in)
             for (int k = 0; k < TENSORS; ++k) {
                 HN_G(in[k] + end + lane, sizeof(T));
                 reinterpret_cast<T *>(place(turn, k) - lane * 32)[end - i + lane] = in[k][end + lane];
             }
+            fence_async_smem();                              // (rows walked from the end have copies land in this stage later)
+        }
     }
     __device__ __forceinline__ bool good() const { return !STAGED || late < 0; }
     __device__ __forceinline__ void wait(int turn, int phase, int t, int tile, bool hold)
@@ -765,6 +767,10 @@ template <typename T, int DECAY, bool BWD> static int launch_recurrence_td(const
     // 256 (a second wave of 68) 86; backward 119, 145, 129.  12288 rows of 2000, bf16: 32 lanes 53 and 94 us, 64 55 and 107, 128 (one
     // tile, nothing travels ahead) 62 and 118; of 1531, fp32: 32 lanes 72 and 126, 128 76 and 144.  8192 rows of 8192, bf16: 32 lanes
     // 123 and 211, 64 117 and 197, 128 115 and 211.
+    // At the borders, rows of 65536, bf16 (in brackets what the rule does not take): forward 444 rows by 256 lanes 60 us (128: 66), 450 by
+    // 192 69 (128: 72, 256: 77), 592 by 192 78 (128: 74), 600 by 128 83 (256: 86), 1000 by 128 155 (256: 127), 1800 by 64 262 (256: 201, 32:
+    // 211): long rows of more than some 800 leave time there.  Backward 592 by 128 122 (256: 131), 600 by 256 171 (128: 188), 888 by 256 192
+    // (128: 212), 1184 by 64 252 (128: 240).  fp32, rows of 32768, backward: 600 by 256 170 (128: 131), 888 by 256 181 (128: 248).
     constexpr int PLACES = BWD ? 512 : 768;
     if (threads <= 128 && a.rows >= PLACES / 64 * kSms) HN_REC(LONG, 32, true);
     if constexpr (LONG == 2) {
