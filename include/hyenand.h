@@ -277,8 +277,8 @@ int hyenand_synth_device_status(void);
  * behind the row, [B][C] fp32, or NULL; it may be the buffer s0.  marks: NULL, or B C hyenand_recurrence_marks(L) floats that the
  * backward pass of the same inputs needs.
  * Decays are meant to be at most 1 in size (g <= 0 for LOG); larger ones are taken, but products of many of them are formed, which
- * can overflow where the state itself does not.  A state is fp32 and every value of y is rounded once, at its store.  A NaN or an
- * infinity spreads to the later positions of its row.  Results do not depend on timing.
+ * can overflow where the state itself does not.  A state is fp32 and every value of y is rounded once, at its store.  A NaN spreads to
+ * the later positions of its row, an infinity does as one or as NaN.  Results do not depend on timing.
  * workspace: hyenand_recurrence_workspace_bytes() bytes on the device, 16-byte aligned, whose contents mean nothing before and after
  * (NULL where that is 0); calls that may overlap need one each.
  * Limits: L <= 2^30, B C <= 2^28.  No call allocates, synchronises or keeps anything; errors and stream as hyenand_forward_ex.
@@ -298,8 +298,9 @@ int hyenand_recurrence_forward(int B, int C, int L, int decay, int dtype, const 
 int hyenand_recurrence_backward(int B, int C, int L, int decay, int dtype, const void *q, const void *k, const void *v,
                                 const void *g, const int *lengths, const float *marks, const void *dy, const float *ds_end,
                                 void *dq, void *dk, void *dv, void *dg, float *ds0, void *workspace, void *cuda_stream);
-/* One token, for generation: q, k, v, g, y are [B][C]; new_state (fp32 [B][C]) may be the buffer `state`.  active: [B] int32 on the
- * device or NULL; an entry whose value is below 1 keeps its state and gets y = 0. */
+/* One token, for generation: q, k, v, g, y are [B][C] (16-byte aligned as above); new_state (fp32 [B][C]) may be the buffer `state`.
+ * active: [B] int32 on the device or NULL; an entry whose value is below 1 keeps its state and gets y = 0.  The new state is rounded
+ * once: a decay next to 1 is applied as a - 1. */
 int hyenand_recurrence_step(int B, int C, int decay, int dtype, const void *q, const void *k, const void *v, const void *g,
                             const float *state, const int *active, void *y, float *new_state, void *cuda_stream);
 /* Long rows travel through shared memory as bulk copies, and every wait for one is bounded.  Returns 0, or 1 once one has given up
@@ -315,23 +316,28 @@ int hyenand_debug_recurrence_late(int tile, int warp);
  * added, the sum normalised for the next.  Per token (one of T grid positions of one batch entry), means over its C channels:
  *
  *     w = act(z) m / sqrt(mean(m^2) + eps) g_post      act: HYENAND_GATE_SIGMOID, HYENAND_GATE_SILU (z sigmoid(z)), or none
- *     r = x + scale D w                                D: dropout factors, as hyenand_dropout over [B][C][T]
+ *     r = x + scale D w                                D: dropout factors, as hyenand_dropout over [B][C][T]: what is dropped
+ *                                                         is zero, whatever m and z were there, and so is all that its gradient gives
  *     n = r / sqrt(mean(r^2) + eps) g_pre
  *
- * x, m, z, r, n: [B][C][T] of one dtype, DEVICE pointers, 16-byte aligned; z is NULL exactly where gate is HYENAND_GATE_NONE.
+ * x, m, z, r, n: [B][C][T] of one dtype, DEVICE pointers, 16-byte aligned (rng and stats too); z is NULL exactly where gate is
+ * HYENAND_GATE_NONE.
  * g_post, scale, g_pre: C fp32 weights on the device; NULL leaves out the first norm, the scale, or n with its norm.  p = 0: no
  * dropout, rng may be NULL.  stats: NULL, or 2 B T floats that the backward pass needs.  All arithmetic is fp32; n is formed
  * before r is rounded.  eps > 0.  Limits: T <= 2^30, C <= 2^20, B C T <= 2^40.  Errors and stream as hyenand_forward_ex; no call
  * allocates, synchronises or keeps anything.
+ * Up to 2048 channels (fp32 forward where 4 does not divide T, and fp32 gradients: 1024) a tile of tokens stays on the chip and each
+ * tensor is read once; beyond, kernels that read everything twice take over, at three to five times the time an element.
  */
 enum { HYENAND_GATE_NONE = 0, HYENAND_GATE_SIGMOID = 1, HYENAND_GATE_SILU = 2 };
 int hyenand_block_forward(int B, int C, int T, int dtype, const void *x, const void *m, const void *z, const float *g_post,
                           const float *scale, const float *g_pre, float eps, int gate, float p, const long long *rng, int site,
                           void *r, void *n, float *stats, void *cuda_stream);
-/* The gradient: dr and dn (either may be NULL: zero; dn is given only with g_pre) in, dx, dm, dz ([B][C][T]) and the sums over all
- * tokens dg_post, dscale, dg_pre (C fp32 each, or NULL) out.  The forward's inputs are read again, stats are the forward's (needed
- * where a norm is).  workspace: hyenand_block_workspace_bytes() bytes on the device, whose contents mean nothing before and
- * after; calls that may overlap need one each.  The sums are formed in an order that does not depend on timing. */
+/* The gradient: dr and dn in (dr may be NULL: zero; dn is given exactly where g_pre is; one of them is), dx, dm, dz ([B][C][T]) and
+ * the sums over all tokens dg_post, dscale, dg_pre (C fp32 each, or NULL) out.  The forward's inputs are read again, stats are the
+ * forward's (needed where a norm is).  workspace: hyenand_block_workspace_bytes() bytes on the device, 16-byte aligned, whose contents
+ * mean nothing before and after; calls that may overlap need one each.  The sums are fp32 throughout, formed in an order that does not
+ * depend on timing. */
 int hyenand_block_backward(int B, int C, int T, int dtype, const void *x, const void *m, const void *z, const float *g_post,
                            const float *scale, const float *g_pre, float eps, int gate, float p, const long long *rng, int site,
                            const float *stats, const void *dr, const void *dn, void *dx, void *dm, void *dz, float *dg_post,
@@ -344,8 +350,8 @@ int hyenand_block_device_status(void);
 
 /*
  * Dropout whose mask is a function of counters and stored nowhere: y_i = x_i / (1 - p') or 0, for n elements; the backward pass is
- * the same call on dy.  y may be the buffer x.  rng: two 64-bit words on the device, read when the kernel runs (so that a captured
- * graph draws anew once they change): the seed, and a step, of which the low 32 bits count.  site tells apart the dropouts of one
+ * the same call on dy.  y may be the buffer x.  rng: two 64-bit words on the device, 16-byte aligned (as x and y), read when the kernel
+ * runs (so that a captured graph draws anew once they change): the seed, and a step, of which the low 32 bits count.  site tells apart the dropouts of one
  * step.  The bits are Philox4x32-10 (Salmon, Moraes, Dror, Shaw, SC 2011) with key (seed low, seed high) and counter
  * (i/8 low, i/8 high, step, site): element i takes 16 of the 128 bits, the low half of word 0 where i mod 8 is 0, its high half
  * where it is 1, the low half of word 1 where it is 2, and so on.  It is dropped (zero, whatever it was) where they are below

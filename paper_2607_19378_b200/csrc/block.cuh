@@ -317,7 +317,8 @@ int launch_block_tile_forward(const BlockArgs &a, int dtype, const TileShape &s,
 int launch_block_tile_backward(const BlockArgs &a, int dtype, const TileShape &s, cudaStream_t st);
 
 // As many clusters as run at once, each walking its share of the tiles: one more would run after all the others (98 clusters of three
-// where 90 fit: twice the time).
+// where 90 fit: twice the time).  Single CTAs are launched with the programmatic start; clusters plainly (the early start was not tried
+// with them).
 template <auto FN, int BYTES> static int launch_tiles(const BlockArgs &a, const TileShape &s, cudaStream_t st)
 {
     static PerDevice fit[kTileCtas + 1];                     // clusters of so many CTAs that run at once

@@ -635,7 +635,8 @@ class Block:
         return self._ops.block_forward(self._handle, x, m, z, g_post, scale, g_pre, rng, stats)
 
     def backward(self, x, m, stats, z=None, g_post=None, scale=None, g_pre=None, rng=None, dr=None, dn=None, stream=None):
-        """dx, dm, dz, dg_post, dscale, dg_pre (None for what was not given), from the stats of a forward call on the same inputs."""
+        """dx, dm, dz, dg_post, dscale, dg_pre (None for what was not given), from the stats of a forward call on the same inputs; dn is
+        given exactly with g_pre, dr may be None (zero) beside it."""
         if stream is not None:
             with _pool(stream):
                 return self.backward(x, m, stats, z, g_post, scale, g_pre, rng, dr, dn)
@@ -643,8 +644,8 @@ class Block:
 
 
 class Dropout:
-    """y = x / (1 - p) or 0, the mask drawn from rng (int64 [2] on the device: seed, step) and site; the backward pass is the same
-    call on dy."""
+    """y = x / (1 - p) or 0, the mask drawn from rng (int64 [2] on the device, 16-byte aligned: seed, step) and site; the backward pass
+    is the same call on dy."""
 
     def __init__(self, p: float, site: int = 0):
         self.p, self.site, self._ops, self._call = float(p), int(site), _calls(), _address("hyenand_dropout")
