@@ -57,7 +57,6 @@ __device__ __forceinline__ Map compose(const Map &a, const Map &b) { return {a.A
 
 // a_t and 1 - a_t (LOG: see decays).  The approximate exponential and reciprocal are off by a few roundings, which a thread's steps
 // can multiply up sixteen-fold at most: what goes on from thread to thread is built from 1 - a_t and the sum of the g_t.
-__device__ __forceinline__ float not_known() { return __int_as_float(0x7fffffff); }      // NaN
 constexpr float kLog2e = 1.4426950408889634f;
 template <int DECAY> __device__ __forceinline__ void decay(float g, float &a, float &na)
 {
@@ -266,24 +265,25 @@ template <int LANES, int E> struct Row {
 // (As 16-byte copies, each lane its own two: 404 and 697 us for 512 rows of 262144, bf16; neighbouring lanes neighbouring pieces:
 // 514 and 657, the addresses and conditions of sixteen copies being most of the instructions.)  Every warp has its own barriers.
 // A wait for copies is bounded.  A warp whose wait gives up fetches and stores nothing more, and its map is NaN for those who go on
-// from there; when the row is done, what was still on its way gets the same time once more to land, so that nothing reaches
-// shared memory that is another CTA's by then.
+// from there; what was still on its way gets the same time once more to land before the warp leaves, so that nothing reaches shared
+// memory that is another CTA's by then.  (Where that second wait stands is the faster of two ways: behind the row forward, 512 rows of
+// 262144 242 us and 244 at once; at once backward, 250 rows of 262144 269 and 279 behind the row.)
 template <typename T, int OCT, int TENSORS, int THREADS, bool STAGED> struct Places {
     static constexpr int E = 8 * OCT, STAGE = STAGED ? TENSORS * THREADS * 32 : 0;
     static constexpr unsigned WARP_BYTES = 1024;
     static_assert(!STAGED || E * sizeof(T) == 32, "32 bytes a thread");
     const T *in[TENSORS];
     char *mine;                                              // this thread's place of tensor 0 in stage 0
-    uint64_t *bars;                                          // this warp's two
+    uint64_t *bars;                                          // this warp's two, and behind them the tile at which a wait gave up
     long long n;
     int len, lane;
-    int late;                                                // the tile at which a wait gave up (the same in all lanes), or -1
+    float none;                                              // 0; NaN once a wait has given up (the same in all lanes)
 
     __device__ __forceinline__ char *place(int turn, int tensor) const { return mine + turn * STAGE + tensor * THREADS * 32; }
     __device__ __forceinline__ void init(char *stages, uint64_t *barriers, int row_len, long long elements)
     {
-        mine = stages + threadIdx.x * 32; bars = barriers + 2 * (threadIdx.x / 32); lane = threadIdx.x & 31;
-        len = row_len; n = elements; late = -1;
+        mine = stages + threadIdx.x * 32; bars = barriers + 3 * (threadIdx.x / 32); lane = threadIdx.x & 31;
+        len = row_len; n = elements; none = 0.f;
         if (STAGED && lane == 0) { mbar_init(bars, 1); mbar_init(bars + 1, 1); fence_mbar_init(); }
         __syncwarp();
     }
@@ -315,14 +315,19 @@ template <typename T, int OCT, int TENSORS, int THREADS, bool STAGED> struct Pla
             fence_async_smem();                              // (rows walked from the end have copies land in this stage later)
         }
     }
-    __device__ __forceinline__ bool good() const { return !STAGED || late < 0; }
-    __device__ __forceinline__ void wait(int turn, int phase, int t, int tile, bool hold)
+    __device__ __forceinline__ bool good() const { return !STAGED || none == 0.f; }
+    __device__ __forceinline__ void drain(int turn, int phase, int t) const { if (t < len) mbar_wait(bars + turn, phase); }
+    // All lanes alike; whether the copies of this tile (positions from t on) are here.  Where it first says no, the caller drains.
+    __device__ __forceinline__ bool wait(int turn, int phase, int t, bool hold)
     {
         bool here = true;
-        if (t < len && late < 0) here = !hold && mbar_wait(bars + turn, phase);
-        if (__any_sync(~0u, !here)) late = tile;
+        if (t < len && good()) here = !hold && mbar_wait(bars + turn, phase);
+        if (!__any_sync(~0u, !here)) return true;
+        none = __int_as_float(0x7fffffff);
+        return false;
     }
-    __device__ __forceinline__ void drain(int turn, int phase, int t) const { if (t < len) mbar_wait(bars + turn, phase); }
+    __device__ __forceinline__ void keep_late(int tile) const { if (lane == 0) bars[2] = (uint64_t)tile; }
+    __device__ __forceinline__ int late() const { __syncwarp(); return (int)bars[2]; }
     // this thread's positions, the first at element i
     __device__ __forceinline__ void get(int turn, int tensor, long long i, f2 (&f)[E / 2]) const
     {
@@ -391,7 +396,7 @@ __global__ void __launch_bounds__(128, 8) recurrence_maps_kernel(RecArgs p)
     constexpr int E = 8 * OCT, N = E / 2;
     using Pl = Places<T, OCT, 3, 128, true>;
     extern __shared__ __align__(16) char stages[];
-    __shared__ uint64_t barriers[128 / 16];
+    __shared__ uint64_t barriers[3 * 128 / 32];
     pdl_join();
     const Row<LANES, E> r(p);
     Pl pl;
@@ -404,16 +409,17 @@ __global__ void __launch_bounds__(128, 8) recurrence_maps_kernel(RecArgs p)
     Map total = {1.f, 0.f, 0.f};
     const float *from = UP ? p.s0 : p.ds_end;
     if (end && r.real && from) { HN_G(from + r.row, 4); total.S = from[r.row]; }
-    int waited[2] = {0, 0};                                  // copies waited for, of each stage
-    if (tiles) fetch(0);
+    if (tiles) fetch(0);                                     // (every one of them has copies: the c-th is its stage's c/2-th)
     for (int c = 0; c < tiles; ++c) {
         const int j = tile_of(c), t0 = r.position(j), turn = c & 1, lo = max(0, -t0), hi = min(E, r.len - t0);
         const long long i = r.start + t0;
         __syncwarp();                                        // (the other stage has been read)
         if (c + 1 < tiles) fetch(c + 1);
-        pl.wait(turn, (turn ? waited[1] : waited[0]) & 1, r.warp_position(j), c, is_late(p, j));
-        if (!pl.good()) break;
-        if (r.warp_position(j) < r.len) { if (turn) ++waited[1]; else ++waited[0]; }
+        if (!pl.wait(turn, c >> 1 & 1, r.warp_position(j), is_late(p, j))) {
+            pl.drain(turn, c >> 1 & 1, r.warp_position(j));
+            if (c + 1 < tiles) pl.drain(turn ^ 1, (c + 1) >> 1 & 1, r.warp_position(tile_of(c + 1)));
+            break;
+        }
         Map own = {1.f, 0.f, 0.f};
         if (lo < hi) {
             f2 a[N], na[N], u[N], x[N];
@@ -431,12 +437,7 @@ __global__ void __launch_bounds__(128, 8) recurrence_maps_kernel(RecArgs p)
         const Map inc = scan_lanes<32, UP>(own, pl.lane);
         total = compose(total, inc);                         // (of use in the last lane on the way)
     }
-    if (!pl.good()) {
-        const int c = pl.late, turn = c & 1;
-        total.S = not_known();
-        pl.drain(turn, (turn ? waited[1] : waited[0]) & 1, r.warp_position(tile_of(c)));
-        if (c + 1 < tiles) pl.drain(turn ^ 1, (turn ? waited[0] : waited[1]) & 1, r.warp_position(tile_of(c + 1)));
-    }
+    total.S += pl.none;
     if (r.real && pl.lane == (UP ? 31 : 0)) {
         float4 *f = p.maps + r.row * p.segments + r.segment;
         HN_G(f, 16);
@@ -453,7 +454,7 @@ __global__ void __launch_bounds__(RowLane<LANES>::kThreads, LANES > 32 ? 768 / L
     using Pl = Places<T, OCT, 4, R::kThreads, STAGED>;
     extern __shared__ __align__(16) char stages[];
     __shared__ Meeting<LANES> meeting;
-    __shared__ uint64_t barriers[STAGED ? R::kThreads / 16 : 1];
+    __shared__ uint64_t barriers[STAGED ? 3 * R::kThreads / 32 : 1];
     const T *q = (const T *)p.q, *k = (const T *)p.k, *v = (const T *)p.v, *g = (const T *)p.g;
     T *y = (T *)p.y;
     pdl_join();
@@ -474,13 +475,13 @@ __global__ void __launch_bounds__(RowLane<LANES>::kThreads, LANES > 32 ? 768 / L
         if (STAGED) {
             pl.stage_free();
             if (j + 1 < r.last && pl.good()) pl.fetch(turn ^ 1, r.start + first(j + 1), first(j + 1));
-            pl.wait(turn, met >> 1 & 1, first(j), j, is_late(p, j));
+            if (!pl.wait(turn, met >> 1 & 1, first(j), is_late(p, j))) pl.keep_late(j);
         }
         const bool some = lo < hi, whole = lo == 0 && hi == E;
         f2 out[N];
         if (LANES <= 32 || j < r.live) {
             f2 a[N], u[N];
-            Map own = {1.f, 0.f, 0.f};
+            Map own = {1.f, 0.f, pl.none};
             if (some) {
                 f2 x[N], na[N];
                 pl.get(turn, 0, i, u); pl.get(turn, 1, i, x);
@@ -492,7 +493,6 @@ __global__ void __launch_bounds__(RowLane<LANES>::kThreads, LANES > 32 ? 768 / L
 #pragma unroll
                 for (int e = 0; e < N; ++e) own.S = fmaf(a[e].y, fmaf(a[e].x, own.S, u[e].x), u[e].y);
             }
-            if (!pl.good()) own.S = not_known();
             const Step<LANES, true> step(own);
             if constexpr (LANES > 32) {
                 step.leave(meeting, met);
@@ -525,7 +525,7 @@ __global__ void __launch_bounds__(RowLane<LANES>::kThreads, LANES > 32 ? 768 / L
     if (r.real && p.s_end && r.segment == p.segments - 1 && r.l == (LANES > 32 ? LANES - 1 : 0)) { HN_G(p.s_end + r.row, 4); p.s_end[r.row] = state; }
     if (STAGED && pl.lane == 0) tma_wait_all0();
     if (!pl.good()) {
-        const int j = pl.late, met = j - r.first;
+        const int j = pl.late(), met = j - r.first;
         pl.drain(met & 1, met >> 1 & 1, first(j));
         if (j + 1 < r.last) pl.drain((met + 1) & 1, (met + 1) >> 1 & 1, first(j + 1));
         atomicExch(&hn_rec_status, 1);
@@ -540,7 +540,7 @@ __global__ void __launch_bounds__(RowLane<LANES>::kThreads, LANES > 32 ? 512 / L
     using Pl = Places<T, OCT, 5, R::kThreads, STAGED>;
     extern __shared__ __align__(16) char stages[];
     __shared__ Meeting<LANES> along;                         // the states, from each tile's mark
-    __shared__ uint64_t barriers[STAGED ? R::kThreads / 16 : 1];
+    __shared__ uint64_t barriers[STAGED ? 3 * R::kThreads / 32 : 1];
     __shared__ Meeting<LANES> back;                          // the gradients of the states, from the row's end
     const T *q = (const T *)p.q, *k = (const T *)p.k, *v = (const T *)p.v, *g = (const T *)p.g, *dy = (const T *)p.dy;
     pdl_join();
@@ -560,7 +560,8 @@ __global__ void __launch_bounds__(RowLane<LANES>::kThreads, LANES > 32 ? 512 / L
     pl.init(stages, barriers, r.len, p.n);
     auto first = [&](int j) { return r.warp_position(j); };
     float mark = mark_of(r.last - 1);
-    int used[2] = {0, 0};                                    // copies waited for, of each stage
+    // the last tile that this warp has copies of: the phases of the stages count from there
+    const int top = min(r.last, (r.len + r.lead - (r.l - pl.lane) * E + Row<LANES, E>::kTile - 1) / Row<LANES, E>::kTile) - 1;
     if (STAGED && r.first < r.last) pl.fetch((r.last - 1) & 1, r.start + first(r.last - 1), first(r.last - 1));
     if (LANES == 32 && p.segments > 1) mu = r.template entering<false>(p);
     for (int j = r.last - 1; j >= r.first; --j) {
@@ -572,14 +573,16 @@ __global__ void __launch_bounds__(RowLane<LANES>::kThreads, LANES > 32 ? 512 / L
             pl.stage_free();
             if (j > r.first && pl.good()) pl.fetch((j - 1) & 1, r.start + first(j - 1), first(j - 1));
             mark = mark_of(j - 1);
-            pl.wait(j & 1, (j & 1 ? used[1] : used[0]) & 1, first(j), j, is_late(p, j));
-            if (first(j) < r.len && pl.good()) { if (j & 1) ++used[1]; else ++used[0]; }
+            if (!pl.wait(j & 1, (top - j) >> 1 & 1, first(j), is_late(p, j))) {
+                pl.drain(j & 1, (top - j) >> 1 & 1, first(j));
+                if (j > r.first) pl.drain((j - 1) & 1, (top - j + 1) >> 1 & 1, first(j - 1));
+            }
         }
         const bool some = lo < hi, whole = lo == 0 && hi == E;
         if (LANES <= 32 || j < r.live) {
             const int met = min(r.live, r.last) - 1 - j;
             f2 a[N], na[N], w[N], u[N];
-            Map own = {1.f, 0.f, 0.f}, rev = {1.f, 0.f, 0.f};
+            Map own = {1.f, 0.f, pl.none}, rev = {1.f, 0.f, pl.none};
             if (some) {
                 f2 x[N];
                 pl.get(j & 1, 0, i, u); pl.get(j & 1, 1, i, x);
@@ -597,7 +600,6 @@ __global__ void __launch_bounds__(RowLane<LANES>::kThreads, LANES > 32 ? 512 / L
 #pragma unroll
                 for (int e = N - 1; e >= 0; --e) rev.S = a[e].x * (w[e].x + a[e].y * (w[e].y + rev.S));
             }
-            if (!pl.good()) own.S = rev.S = not_known();
             const Step<LANES, true> ahead(own);
             const Step<LANES, false> behind(rev);
             if constexpr (LANES > 32) {
@@ -664,12 +666,7 @@ __global__ void __launch_bounds__(RowLane<LANES>::kThreads, LANES > 32 ? 512 / L
     if (STAGED && LANES > 32 && r.first >= r.live) { __syncthreads(); mu = back.carry[1]; }
     if (r.real && p.ds0 && r.segment == 0 && r.l == 0) { HN_G(p.ds0 + r.row, 4); p.ds0[r.row] = mu; }
     if (STAGED && pl.lane == 0) tma_wait_all0();
-    if (!pl.good()) {
-        const int j = pl.late;
-        pl.drain(j & 1, (j & 1 ? used[1] : used[0]) & 1, first(j));
-        if (j > r.first) pl.drain((j - 1) & 1, (j & 1 ? used[0] : used[1]) & 1, first(j - 1));
-        atomicExch(&hn_rec_status, 1);
-    }
+    if (!pl.good()) atomicExch(&hn_rec_status, 1);
 }
 
 // a s + u for one token.  A decay next to 1 loses what it is in its own rounding (exp(-1e-6) is off by 2 % of its distance from 1, and
