@@ -327,7 +327,7 @@ int hyenand_debug_recurrence_late(int tile, int warp);
  * before r is rounded.  eps > 0.  Limits: T <= 2^30, C <= 2^20, B C T <= 2^40.  Errors and stream as hyenand_forward_ex; no call
  * allocates, synchronises or keeps anything.
  * Up to 2048 channels (fp32 forward where 4 does not divide T, and fp32 gradients: 1024) a tile of tokens stays on the chip and each
- * tensor is read once; beyond, kernels that read everything twice take over, at three to five times the time an element.
+ * tensor is read once; beyond, kernels that read everything twice take over, at two to three times the time an element.
  */
 enum { HYENAND_GATE_NONE = 0, HYENAND_GATE_SIGMOID = 1, HYENAND_GATE_SILU = 2 };
 int hyenand_block_forward(int B, int C, int T, int dtype, const void *x, const void *m, const void *z, const float *g_post,

@@ -14,8 +14,9 @@
 // channels.  The backward reads what the forward read and recomputes the rest; only the two rho of a token are kept.
 //
 // The kernels here take any number of channels: a CTA takes a tile of neighbouring tokens, its warps share the channels, and what a second
-// walk needs is read again (from the caches, where it still is): 4096 tokens of 5000 channels, bf16, 243 and 495 us, 0.13 and 0.10 of the
-// measured copy rate, latency of dependent loads.  Up to 2048 channels (fewer in fp32) tiles stay in shared memory (block_fwd.cu, block_bwd.cu).
+// walk needs is read again (from the caches, where it still is): 4096 tokens of 5000 channels, bf16, 234 and 470 us, 0.13 and 0.11 of the
+// measured copy rate, latency of dependent loads.  Up to 2048 channels (1024 of fp32 forward where rows are no multiple of 16 bytes, and
+// backward) tiles stay in shared memory (block_fwd.cu, block_bwd.cu): 2048 channels 35 and 77 us, 2100 here 90 and 212.
 #include "block.cuh"
 
 namespace hn {
@@ -308,7 +309,7 @@ static bool tile_shape(const BlockArgs &a, int dtype, bool backward, TileShape *
     s->ctas = (a.C + rows * most - 1) / (rows * most);
     if (s->ctas > kTileCtas || most > 8) return false;
     const int each = ((a.C + s->ctas - 1) / s->ctas + rows - 1) / rows;
-    // (widths of 96, 192, 384: 16 x 4096 tokens of 192 channels, bf16, forward with six 37 us, with eight 45; backward with three 79, with four 83)
+    // (widths of 96, 192, 384: 16 x 4096 tokens of 192 channels, bf16, dropout: forward with six 37 us, with eight 45; backward with three 79, with four 83)
     s->n = each <= 2 ? each : each == 3 && s->lt == 8 ? 3 : each <= 4 ? 4 : each <= 6 && !backward ? 6 : 8;
     return true;
 }

@@ -4,9 +4,9 @@
 // registers over all tiles of a cluster; a slot of the workspace takes them at the end.
 //
 // 90 instructions an element with gate and dropout (values read again from shared memory and the gate worked out again behind the meeting,
-// as registers for 16 warps an SM do not hold them) at 47 % of the issue slots; the barriers and the meeting take the rest.  16 x 4096 tokens
-// of 768 channels, bf16: 277 us (0.44 of the measured copy rate), without dropout 249 (0.49); 884736 tokens of 64, fp32, no gate: 269
-// (0.77).  The same overlap of tiles as in the forward: 296 us.
+// as registers for 16 warps an SM do not hold them) at 46 % of the issue slots; the barriers and the meeting take the rest.  16 x 4096 tokens
+// of 768 channels, bf16: 274 us (0.45 of the measured copy rate), without dropout 241 (0.51); 884736 tokens of 64, fp32, no gate: 265
+// (0.78).  The same overlap of tiles as in the forward: 296 us.
 #include "block.cuh"
 
 namespace hn {

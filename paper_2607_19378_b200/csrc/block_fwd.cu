@@ -6,8 +6,8 @@
 // not brought down yet, are infinite; such a tile meets once more and adds up r^2 itself.
 //
 // 44 instructions an element with gate and dropout, and 16 warps an SM (registers; two stages of three tensors in shared memory) keep the
-// issue slots 44 % busy: the CTA's three barriers a tile and the meeting take the rest.  16 x 4096 tokens of 768 channels, bf16: 144 us
-// (0.53 of the measured copy rate), without dropout 120 (0.64); 884736 tokens of 64, fp32, no gate: 178 (0.78).  Four lanes along the
+// issue slots 45 % busy: the CTA's three barriers a tile and the meeting take the rest.  16 x 4096 tokens of 768 channels, bf16: 143 us
+// (0.54 of the measured copy rate), without dropout 119 (0.65); 884736 tokens of 64, fp32, no gate: 178 (0.78).  Four lanes along the
 // tokens, or half the channels a thread, and the sums of a tile worked on before the results of the one before it (24 warps an SM): 195 us
 // at the least; tiles of half the tokens are rows of 32 bytes, and clusters of twice the CTAs are slower to meet.
 #include "block.cuh"

@@ -2,8 +2,9 @@
 // worked out wherever it is needed and stored nowhere; the backward pass is the same call on dy.
 //
 // One pass over the data.  A thread takes four octets of bf16 or two of fp32, one Philox call of ten rounds for eight elements (16
-// random bits each): 15 instructions an element, of which bf16 needs as many as the memory allows.  50 M elements: fp32 66 us (0.93 of
-// the measured bandwidth), bf16 47 us (0.65; the two instruction pipes of the generator's products and of its logic bound it).
+// random bits each): 15 instructions an element.  50 M elements behind a cold L2: fp32 64 us (0.96 of the measured bandwidth), bf16 46 us
+// (0.66), in calls that follow each other 40 (0.75): the generator's integer instructions take the ALU to 55 %, and the warps wait for
+// their loads and for that pipe in turn.
 // Threads that walk over several such pieces: 84 and 48 us.
 #include "entry.cuh"
 #include "octet.cuh"

@@ -761,9 +761,9 @@ template <typename T, int DECAY, bool BWD> static int launch_recurrence_td(const
     const int threads = (octets + LONG - 1) / LONG;
     // Rows that fill the GPU: one CTA each, of as many lanes as still lets all of them run at once (768 threads an SM forward, 512
     // backward), and small ones where they come in several waves anyhow.  512 rows of 65536, bf16, forward: 128 lanes 73 us, 192 70,
-    // 256 (a second wave of 68) 86; backward 119, 145, 129.  12288 rows of 2000, bf16: 32 lanes 53 and 94 us, 64 55 and 107, 128 (one
-    // tile, nothing travels ahead) 62 and 118; of 1531, fp32: 32 lanes 72 and 126, 128 76 and 144.  8192 rows of 8192, bf16: 32 lanes
-    // 123 and 211, 64 117 and 197, 128 115 and 211.
+    // 256 (a second wave of 68) 86; backward 119, 145, 129.  12288 rows of 2000, bf16: 32 lanes 49 and 88 us, 64 52 and 100, 128 (one
+    // tile, nothing travels ahead) 62 and 117; of 1531, fp32, 128 lanes 76 and 148 (32, which fp32 rows above 1024 do not take, 72 and
+    // 127).  8192 rows of 8192, bf16: 32 lanes 121 and 213, 64 117 and 201, 128 117 and 215.
     // At the borders, rows of 65536, bf16 (in brackets what the rule does not take): forward 444 rows by 256 lanes 60 us (128: 66), 450 by
     // 192 69 (128: 72, 256: 77), 592 by 192 78 (128: 74), 600 by 128 83 (256: 86), 1000 by 128 155 (256: 127), 1800 by 64 262 (256: 201, 32:
     // 211): long rows of more than some 800 leave time there.  Backward 592 by 128 122 (256: 131), 600 by 256 171 (128: 188), 888 by 256 192
