@@ -317,7 +317,8 @@ int hyenand_debug_recurrence_late(int tile, int warp);
  *
  *     w = act(z) m / sqrt(mean(m^2) + eps) g_post      act: HYENAND_GATE_SIGMOID, HYENAND_GATE_SILU (z sigmoid(z)), or none
  *     r = x + scale D w                                D: dropout factors, as hyenand_dropout over [B][C][T]: what is dropped
- *                                                         is zero, whatever m and z were there, and so is all that its gradient gives
+ *                                                         is zero whatever z was there, and so is what its gradient gives (m counts
+ *                                                         in its norm all the same; without g_post the same holds for m)
  *     n = r / sqrt(mean(r^2) + eps) g_pre
  *
  * x, m, z, r, n: [B][C][T] of one dtype, DEVICE pointers, 16-byte aligned (rng and stats too); z is NULL exactly where gate is

@@ -312,7 +312,8 @@ template <typename T, int OCT, int TENSORS, int THREADS, bool STAGED> struct Pla
                 HN_G(in[k] + end + lane, sizeof(T));
                 reinterpret_cast<T *>(place(turn, k) - lane * 32)[end - i + lane] = in[k][end + lane];
             }
-            fence_async_smem();                              // (rows walked from the end have copies land in this stage later)
+            fence_async_smem();                              // (rows walked from the end have copies land in this stage later; the warp meets
+                                                             // once more before it reads the octet)
         }
     }
     __device__ __forceinline__ bool good() const { return !STAGED || none == 0.f; }
