@@ -312,6 +312,78 @@ int hyenand_recurrence_device_status(void);
 int hyenand_debug_recurrence_late(int tile, int warp);
 
 /*
+ * Gated delta rule, a causal mixer whose state is a matrix per head (1-D; a grid is read in the order of its tokens): what a token
+ * writes under its key replaces what the state held there.  For every batch entry and value head, S in R^{Dv x Dk},
+ *
+ *     u_t = beta_t (v_t - a_t S_{t-1} k_t),    S_t = a_t S_{t-1} + u_t k_t^T,    y_t = S_t q_t,    t = 0 .. L-1,
+ *     a_t = exp(g_t) (HYENAND_DECAY_LOG)  |  1 / (1 + exp(-g_t)) (HYENAND_DECAY_SIGMOID)  |  1 (HYENAND_DECAY_NONE, g is NULL)
+ *
+ * q, k: [B][Hk Dk][L], v, y: [B][H Dv][L] of one dtype, DEVICE pointers, 16-byte aligned; H is a multiple of Hk, and value head h goes with
+ * head h / (H / Hk) of queries and keys.  g, beta: [B][H][L] fp32.  s0: the states before the rows, [B][H][Dv][Dk] fp32, 16-byte aligned,
+ * or NULL (zero).  lengths: [B] int32 on the device, or NULL: entry b holds lengths[b] tokens (values outside 0 .. L count as the
+ * nearer of the two); what lies behind them does not count, y is zero there and the state passes through.  s_end: the states behind
+ * the rows or NULL; it may be the buffer s0.  marks: NULL, or hyenand_delta_marks(L) states per head (fp32, 16-byte aligned) that the
+ * backward pass of the same inputs needs.
+ * Keys are meant to have a norm of about 1 at most and beta to lie in 0 .. 2 (else the rule itself grows without bound), decays to be at
+ * most 1; a decay below exp(-110) is taken as exp(-110), which fp32 cannot hold.  Tokens are taken 64 at a time on the tensor cores;
+ * states, sums and decays are fp32, and what enters a product is a sum of bf16 values: exact to 2^-17 for bf16 tensors, to
+ * 2^-24 for fp32 ones.  y is rounded once, at its store.  A NaN spreads to its chunk of 64 tokens and everything behind it, an infinity
+ * does as NaN.  Results do not depend on timing.
+ * workspace: hyenand_delta_workspace_bytes() bytes on the device, 16-byte aligned, whose contents mean nothing before and after; calls
+ * that may overlap need one each.
+ * Limits: Dk, Dv <= 128 (a wider value head is several heads that share queries and keys), L <= 2^30, B H <= 2^24, B H L <= 2^36.  No
+ * call allocates, synchronises or keeps anything; errors and stream as hyenand_forward_ex.
+ */
+enum { HYENAND_DECAY_NONE = 3 };
+int hyenand_delta_marks(int L);                   /* states per head in marks; 0 for an L out of range */
+long long hyenand_delta_workspace_bytes(int B, int H, int Hk, int L, int Dk, int Dv, int dtype, int backward);      /* 0 for a shape out of range */
+int hyenand_delta_forward(int B, int H, int Hk, int L, int Dk, int Dv, int decay, int dtype, const void *q, const void *k, const void *v,
+                          const float *g, const float *beta, const float *s0, const int *lengths, void *y, float *s_end, float *marks,
+                          void *workspace, void *cuda_stream);
+/* The gradient, from marks of a forward call on the same q, k, v, g, beta, s0 and lengths.  dy: [B][H Dv][L]; ds_end:
+ * [B][H][Dv][Dk] fp32 or NULL (zero).  dq, dk ([B][Hk Dk][L], summed over the value heads that share them), dv, dg, dbeta as their
+ * inputs, zero behind an entry's length; dg may be NULL, and is with HYENAND_DECAY_NONE; ds0 or NULL; it may be the buffer ds_end.  Each is
+ * rounded once, at its store.  The workspace is the larger one (backward != 0). */
+int hyenand_delta_backward(int B, int H, int Hk, int L, int Dk, int Dv, int decay, int dtype, const void *q, const void *k, const void *v,
+                           const float *g, const float *beta, const int *lengths, const float *marks, const void *dy, const float *ds_end,
+                           void *dq, void *dk, void *dv, float *dg, float *dbeta, float *ds0, void *workspace, void *cuda_stream);
+/* One token, for generation: q, k [B][Hk Dk], v, y [B][H Dv], g, beta [B][H]; new_state may be the buffer `state`.  active: [B] int32 on
+ * the device or NULL; an entry whose value is below 1 keeps its states and gets y = 0.  All arithmetic is fp32; the new state is
+ * rounded once: a decay next to 1 is applied as a - 1. */
+int hyenand_delta_step(int B, int H, int Hk, int Dk, int Dv, int decay, int dtype, const void *q, const void *k, const void *v, const float *g,
+                       const float *beta, const float *state, const int *active, void *y, float *new_state, void *cuda_stream);
+/* Every wait of the kernels (for copies, for the tensor cores) is bounded.  Returns 0, or 1 once one has given up since the library
+ * was loaded (the call that met it left its results incomplete), -1 if the word cannot be read.  Synchronises the device. */
+int hyenand_delta_device_status(void);
+
+/*
+ * Queries and keys as heads: the norm of each head and the rotation by its token's position on the native grid, in one pass, as a mixer
+ * with queries and keys (hyenand_delta_*) takes them.  q: [B][Hq D][T], k: [B][Hk D][T], T = dims[0] .. dims[ndim-1], of one dtype,
+ * DEVICE pointers, 16-byte aligned.  Per token and head, over its D channels,
+ *
+ *     n = x g / sqrt(mean(x^2) + eps) (HYENAND_NORM_RMS)  |  x g / sqrt(sum(x^2) + eps) (HYENAND_NORM_L2)  |  x g (HYENAND_NORM_NONE)
+ *     y_i = n_i cos t - n_{i+D/2} sin t,   y_{i+D/2} = n_i sin t + n_{i+D/2} cos t,      t = p base^(-j / axes[a])
+ *
+ * The first axes[0] pairs i turn with the position p on axis 0, the next axes[1] with that on axis 1, and so on; j counts the pairs of an
+ * axis, and pairs behind them all stay as they are (axes may be NULL: no rotation).  Positions are the token's place on the grid, or
+ * positions, int32 [B][ndim][T] on the device.  g_q, g_k: D fp32 weights or NULL (1).  Sums are fp32, angles 64 bits wide; every result
+ * is rounded once.  q_out may be the buffer q, k_out the buffer k.
+ * Limits: ndim <= 3, D even and <= 256, T <= 2^30, B (Hq + Hk) <= 2^28, 2^40 elements; eps > 0.  Errors and stream as
+ * hyenand_forward_ex; no call allocates, synchronises or keeps anything.
+ */
+enum { HYENAND_NORM_NONE = 0, HYENAND_NORM_RMS = 1, HYENAND_NORM_L2 = 2 };
+int hyenand_heads_forward(int ndim, const int *dims, int B, int Hq, int Hk, int D, int dtype, int norm, const int *axes, double base, float eps,
+                          const void *q, const void *k, const float *g_q, const float *g_k, const int *positions, void *q_out, void *k_out,
+                          void *cuda_stream);
+/* The gradient: dq_out, dk_out in, dq, dk (dq may be the buffer dq_out, dk the buffer dk_out) and the sums over all tokens dg_q, dg_k (D fp32
+ * each, or NULL) out; the forward's inputs are read again.  workspace: hyenand_heads_workspace_bytes() bytes on the device, 16-byte
+ * aligned, where dg_q or dg_k is given; calls that may overlap need one each.  The order of the sums does not depend on timing. */
+int hyenand_heads_backward(int ndim, const int *dims, int B, int Hq, int Hk, int D, int dtype, int norm, const int *axes, double base, float eps,
+                           const void *q, const void *k, const float *g_q, const float *g_k, const int *positions, const void *dq_out,
+                           const void *dk_out, void *dq, void *dk, float *dg_q, float *dg_k, void *workspace, void *cuda_stream);
+long long hyenand_heads_workspace_bytes(int ndim, const int *dims, int B, int Hq, int Hk, int D, int dtype);
+
+/*
  * What stands between two mixers of a residual stream x: the first one's output m normalised, gated, dropped out, scaled and
  * added, the sum normalised for the next.  Per token (one of T grid positions of one batch entry), means over its C channels:
  *

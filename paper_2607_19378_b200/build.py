@@ -27,7 +27,7 @@ DEBUG_FLAGS = ["-lineinfo", "--compress-mode=size", "-DHYENAND_DEBUG"]
 # mix_sigmoid inside fused2d.cu and slice_mix*.cu), at fp32 errors of a few 1e-7; 1 / (1 + exp(x)) is 0 above x = 87.3, where
 # it is below 2^-126.  Kernel synthesis, whose sines reach 30 radians and more, and the linear recurrence, whose decays are multiplied
 # up over thousands of positions, are compiled without it.
-PRECISE = {"synth.cu", "recurrence.cu"}
+PRECISE = {"synth.cu", "recurrence.cu", "heads.cu", "delta.cu", "delta_backward.cu"}
 
 
 def calls_path() -> str:

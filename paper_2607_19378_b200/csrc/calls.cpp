@@ -1,4 +1,4 @@
-// The classes Recurrence, Block and Dropout from Python to the C ABI: checks of the tensors, outputs from the caching allocator, the
+// The classes Recurrence, DeltaRule, Heads, Block and Dropout from Python to the C ABI: checks of the tensors, outputs from the caching allocator, the
 // current stream, one call of the library.  As Python this takes longer than the kernels of small calls (a token for 32 sequences of
 // 768 channels 11.4 us a call, the kernel 3; here 5.3); nothing is computed here.  The library's functions come as addresses, so that
 // one module serves the product library and the checked build.
@@ -269,6 +269,173 @@ PyObject *block_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// ---- delta rule -----------------------------------------------------------------------------------------------------
+
+struct Delta {
+    int B, H, Hk, L, Dk, Dv, decay, dtype;
+    int64_t work_forward, work_backward;
+    ScalarType type;
+    Shape keys, values, gates, states, marks, key, value, gate, batch;      // (of a sequence, of a token)
+    decltype(&hyenand_delta_forward) forward;
+    decltype(&hyenand_delta_backward) backward;
+    decltype(&hyenand_delta_step) step;
+    PyObject *raise_error;
+};
+
+PyObject *make_delta(PyObject *, PyObject *args)
+{
+    int B, H, Hk, L, Dk, Dv, marks, decay, dtype;
+    long long wf, wb;
+    unsigned long long f, b, st;
+    PyObject *raise_error;
+    if (!PyArg_ParseTuple(args, "iiiiiiiiiLLKKKO", &B, &H, &Hk, &L, &Dk, &Dv, &marks, &decay, &dtype, &wf, &wb, &f, &b, &st, &raise_error)) return nullptr;
+    const int64_t kc = (int64_t)Hk * Dk, vc = (int64_t)H * Dv;
+    auto *d = new Delta{B, H, Hk, L, Dk, Dv, decay, dtype, wf, wb, type_of(dtype), {B, kc, L}, {B, vc, L}, {B, H, L}, {B, H, Dv, Dk}, {B, H, marks, Dv, Dk},
+                        {B, kc}, {B, vc}, {B, H}, {B}, (decltype(&hyenand_delta_forward))f, (decltype(&hyenand_delta_backward))b,
+                        (decltype(&hyenand_delta_step))st, Py_NewRef(raise_error)};
+    return PyCapsule_New(d, nullptr, release<Delta>);
+}
+// g: a tensor where there is a decay, None where there is none
+const Tensor *gate_of(Arguments &want, PyObject *o, const Delta *d, const Shape &shape)
+{
+    if (d->decay != HYENAND_DECAY_NONE) return want(o, "g", at::kFloat, shape);
+    if (o != Py_None) { PyErr_SetString(PyExc_ValueError, "g must be None where there is no decay"); throw PythonError(); }
+    return nullptr;
+}
+
+// handle, q, k, v, g, beta, s0, lengths, marks, y
+PyObject *delta_forward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (!count(n, 10)) return nullptr;
+    return guarded([&] {
+        const Delta *d = handle<Delta>(a[0]);
+        Arguments want;
+        const Tensor *q = want(a[1], "q", d->type, d->keys), *k = want(a[2], "k", d->type, d->keys), *v = want(a[3], "v", d->type, d->values),
+                     *g = gate_of(want, a[4], d, d->gates), *beta = want(a[5], "beta", at::kFloat, d->gates), *s0 = want(a[6], "s0", at::kFloat, d->states, true),
+                     *len = want(a[7], "lengths", at::kInt, d->batch, true), *given = want(a[9], "y", d->type, d->values, true);
+        const bool keep = truth(a[8]);
+        const Tensor y = given ? *given : want.empty(d->values, d->type), end = want.empty(d->states, at::kFloat),
+                     marks = keep ? want.empty(d->marks, at::kFloat) : Tensor(), work = want.empty({d->work_forward}, at::kByte);
+        check(d->forward(d->B, d->H, d->Hk, d->L, d->Dk, d->Dv, d->decay, d->dtype, data(q), data(k), data(v), (const float *)data(g), (const float *)data(beta),
+                         (const float *)data(s0), (const int *)data(len), y.data_ptr(), (float *)end.data_ptr(), keep ? (float *)marks.data_ptr() : nullptr,
+                         work.data_ptr(), want.stream()), d->raise_error);
+        return keep ? tuple({y, end, marks}) : tuple({y, end});
+    });
+}
+
+// handle, q, k, v, g, beta, marks, dy, ds_end, lengths
+PyObject *delta_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (!count(n, 10)) return nullptr;
+    return guarded([&] {
+        const Delta *d = handle<Delta>(a[0]);
+        Arguments want;
+        const Tensor *q = want(a[1], "q", d->type, d->keys), *k = want(a[2], "k", d->type, d->keys), *v = want(a[3], "v", d->type, d->values),
+                     *g = gate_of(want, a[4], d, d->gates), *beta = want(a[5], "beta", at::kFloat, d->gates), *marks = want(a[6], "marks", at::kFloat, d->marks),
+                     *dy = want(a[7], "dy", d->type, d->values), *ds = want(a[8], "ds_end", at::kFloat, d->states, true),
+                     *len = want(a[9], "lengths", at::kInt, d->batch, true);
+        const Tensor dq = want.empty(d->keys, d->type), dk = want.empty(d->keys, d->type), dv = want.empty(d->values, d->type),
+                     dg = g ? want.empty(d->gates, at::kFloat) : Tensor(), dbeta = want.empty(d->gates, at::kFloat), ds0 = want.empty(d->states, at::kFloat),
+                     work = want.empty({d->work_backward}, at::kByte);
+        check(d->backward(d->B, d->H, d->Hk, d->L, d->Dk, d->Dv, d->decay, d->dtype, data(q), data(k), data(v), (const float *)data(g), (const float *)data(beta),
+                          (const int *)data(len), (const float *)data(marks), data(dy), (const float *)data(ds), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
+                          g ? (float *)dg.data_ptr() : nullptr, (float *)dbeta.data_ptr(), (float *)ds0.data_ptr(), work.data_ptr(), want.stream()), d->raise_error);
+        return tuple({dq, dk, dv, dg, dbeta, ds0});
+    });
+}
+
+// handle, q, k, v, g, beta, state, new_state, active, y
+PyObject *delta_step(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (!count(n, 10)) return nullptr;
+    return guarded([&] {
+        const Delta *d = handle<Delta>(a[0]);
+        Arguments want;
+        const Tensor *q = want(a[1], "q", d->type, d->key), *k = want(a[2], "k", d->type, d->key), *v = want(a[3], "v", d->type, d->value),
+                     *g = gate_of(want, a[4], d, d->gate), *beta = want(a[5], "beta", at::kFloat, d->gate), *state = want(a[6], "state", at::kFloat, d->states),
+                     *next = want(a[7], "new_state", at::kFloat, d->states, true), *active = want(a[8], "active", at::kInt, d->batch, true),
+                     *given = want(a[9], "y", d->type, d->value, true);
+        const Tensor y = given ? *given : want.empty(d->value, d->type);
+        check(d->step(d->B, d->H, d->Hk, d->Dk, d->Dv, d->decay, d->dtype, data(q), data(k), data(v), (const float *)data(g), (const float *)data(beta),
+                      (const float *)data(state), (const int *)data(active), y.data_ptr(), (float *)data(next ? next : state), want.stream()), d->raise_error);
+        return wrap(y);
+    });
+}
+
+// ---- heads ----------------------------------------------------------------------------------------------------------
+
+struct Heads {
+    int ndim, dims[3], axes[3], B, Hq, Hk, D, dtype, norm;
+    double base;
+    float eps;
+    int64_t workspace;
+    ScalarType type;
+    Shape queries, keys, weights, places;
+    decltype(&hyenand_heads_forward) forward;
+    decltype(&hyenand_heads_backward) backward;
+    PyObject *raise_error;
+};
+
+PyObject *make_heads(PyObject *, PyObject *args)
+{
+    PyObject *dims, *axes, *raise_error;
+    int B, Hq, Hk, D, dtype, norm;
+    double base;
+    float eps;
+    long long workspace;
+    unsigned long long f, b;
+    if (!PyArg_ParseTuple(args, "O!O!iiiiiidfLKKO", &PyTuple_Type, &dims, &PyTuple_Type, &axes, &B, &Hq, &Hk, &D, &dtype, &norm, &base, &eps, &workspace, &f, &b, &raise_error))
+        return nullptr;
+    auto *h = new Heads{(int)PyTuple_GET_SIZE(dims), {0}, {0}, B, Hq, Hk, D, dtype, norm, base, eps, workspace, type_of(dtype), {B, (int64_t)Hq * D}, {B, (int64_t)Hk * D}, {D},
+                        {B, (int64_t)PyTuple_GET_SIZE(dims)}, (decltype(&hyenand_heads_forward))f, (decltype(&hyenand_heads_backward))b, Py_NewRef(raise_error)};
+    for (int i = 0; i < h->ndim && i < 3; ++i) {
+        h->dims[i] = (int)PyLong_AsLong(PyTuple_GET_ITEM(dims, i));
+        h->axes[i] = (int)PyLong_AsLong(PyTuple_GET_ITEM(axes, i));
+        h->queries.push_back(h->dims[i]);
+        h->keys.push_back(h->dims[i]);
+        h->places.push_back(h->dims[i]);
+    }
+    PyObject *c = PyCapsule_New(h, nullptr, release<Heads>);
+    if (PyErr_Occurred()) { Py_XDECREF(c); return nullptr; }
+    return c;
+}
+
+// handle, q, k, g_q, g_k, positions, q_out, k_out
+PyObject *heads_forward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (!count(n, 8)) return nullptr;
+    return guarded([&] {
+        const Heads *h = handle<Heads>(a[0]);
+        Arguments want;
+        const Tensor *q = want(a[1], "q", h->type, h->queries), *k = want(a[2], "k", h->type, h->keys), *gq = want(a[3], "g_q", at::kFloat, h->weights, true),
+                     *gk = want(a[4], "g_k", at::kFloat, h->weights, true), *pos = want(a[5], "positions", at::kInt, h->places, true),
+                     *oq = want(a[6], "q_out", h->type, h->queries, true), *ok = want(a[7], "k_out", h->type, h->keys, true);
+        const Tensor yq = oq ? *oq : want.empty(h->queries, h->type), yk = ok ? *ok : want.empty(h->keys, h->type);
+        check(h->forward(h->ndim, h->dims, h->B, h->Hq, h->Hk, h->D, h->dtype, h->norm, h->axes, h->base, h->eps, data(q), data(k), (const float *)data(gq),
+                         (const float *)data(gk), (const int *)data(pos), yq.data_ptr(), yk.data_ptr(), want.stream()), h->raise_error);
+        return tuple({yq, yk});
+    });
+}
+
+// handle, q, k, dq_out, dk_out, g_q, g_k, positions
+PyObject *heads_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (!count(n, 8)) return nullptr;
+    return guarded([&] {
+        const Heads *h = handle<Heads>(a[0]);
+        Arguments want;
+        const Tensor *q = want(a[1], "q", h->type, h->queries), *k = want(a[2], "k", h->type, h->keys), *yq = want(a[3], "dq_out", h->type, h->queries),
+                     *yk = want(a[4], "dk_out", h->type, h->keys), *gq = want(a[5], "g_q", at::kFloat, h->weights, true),
+                     *gk = want(a[6], "g_k", at::kFloat, h->weights, true), *pos = want(a[7], "positions", at::kInt, h->places, true);
+        const Tensor dq = want.empty(h->queries, h->type), dk = want.empty(h->keys, h->type), dgq = gq ? want.empty(h->weights, at::kFloat) : Tensor(),
+                     dgk = gk ? want.empty(h->weights, at::kFloat) : Tensor(), work = gq || gk ? want.empty({h->workspace}, at::kByte) : Tensor();
+        check(h->backward(h->ndim, h->dims, h->B, h->Hq, h->Hk, h->D, h->dtype, h->norm, h->axes, h->base, h->eps, data(q), data(k), (const float *)data(gq),
+                          (const float *)data(gk), (const int *)data(pos), data(yq), data(yk), dq.data_ptr(), dk.data_ptr(), gq ? (float *)dgq.data_ptr() : nullptr,
+                          gk ? (float *)dgk.data_ptr() : nullptr, gq || gk ? work.data_ptr() : nullptr, want.stream()), h->raise_error);
+        return tuple({dq, dk, dgq, dgk});
+    });
+}
+
 // ---- dropout --------------------------------------------------------------------------------------------------------
 
 // address of hyenand_dropout, function that raises, p, site, x, rng, y
@@ -302,9 +469,16 @@ PyMethodDef methods[] = {
     {"make_block", make_block, METH_VARARGS, nullptr},
     {"block_forward", (PyCFunction)(void (*)(void))block_forward, METH_FASTCALL, nullptr},
     {"block_backward", (PyCFunction)(void (*)(void))block_backward, METH_FASTCALL, nullptr},
+    {"make_delta", make_delta, METH_VARARGS, nullptr},
+    {"delta_forward", (PyCFunction)(void (*)(void))delta_forward, METH_FASTCALL, nullptr},
+    {"delta_backward", (PyCFunction)(void (*)(void))delta_backward, METH_FASTCALL, nullptr},
+    {"delta_step", (PyCFunction)(void (*)(void))delta_step, METH_FASTCALL, nullptr},
+    {"make_heads", make_heads, METH_VARARGS, nullptr},
+    {"heads_forward", (PyCFunction)(void (*)(void))heads_forward, METH_FASTCALL, nullptr},
+    {"heads_backward", (PyCFunction)(void (*)(void))heads_backward, METH_FASTCALL, nullptr},
     {"dropout", (PyCFunction)(void (*)(void))dropout, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
-PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", "Recurrence, Block and Dropout: from tensors to the C ABI", -1, methods, nullptr, nullptr, nullptr, nullptr};
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", "Recurrence, DeltaRule, Heads, Block and Dropout: from tensors to the C ABI", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 

@@ -1,0 +1,681 @@
+// The gated delta rule: forward pass, in chunks (formulas and number formats in delta.cuh).
+//
+// prepare: a CTA per chunk and head, all at once: k k^T and q k^T as one product of 128 rows, decays, A by forward substitution
+//     (a thread per column; fp32), A and P as planes into the workspace.
+// walk: a CTA per head walks its chunks.  The state's rows are the lanes of tensor memory (Dv of 128), so that S^T products chain without a
+//     transposition: S k, then A Z, then the new state each take the result of the one before as their A operand in tensor memory, through
+//     registers (256 threads: a lane's columns in two halves).  The fp32 state stays in registers.  Four warps fetch the next chunks.
+// Few heads and many chunks: the walk is serial, so a head is cut into segments.  Where a segment starts from nothing it gives N, where it
+//     starts from the identity without values it gives Phi, and from any state S it ends at S Phi + N: both walks run for all
+//     segments at once, a small kernel joins them, and the walk proper starts every segment at once.
+#include "delta.cuh"
+
+namespace hn {
+
+static __device__ int hn_delta_status;
+
+// ---- prepare --------------------------------------------------------------------------------------------------------
+
+template <typename T, int KD> struct Prep {
+    static constexpr int PI = Planes<T>::IN, PM = Planes<T>::MID, TILE = KD * 128, PITCH = 2 * TILE, TROW = 68;
+    static constexpr int IMAGES = PI * PITCH > 2 * PM * kMatrix ? PI * PITCH : 2 * PM * kMatrix;          // (the results take the tiles' place)
+    static constexpr int BYTES = 1024 + IMAGES + kTok * TROW * 4;
+};
+
+template <typename T, int KD> __global__ void __launch_bounds__(128) delta_prepare_kernel(DeltaArgs a)
+{
+    using C = Prep<T, KD>;
+    extern __shared__ __align__(1024) unsigned char raw[];
+    __shared__ double G[kTok];
+    __shared__ float beta[kTok];
+    __shared__ uint64_t bar;
+    __shared__ unsigned slot;
+    unsigned char *sm = align_images(raw);
+    float *Ts = (float *)(sm + C::IMAGES);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const long long at = blockIdx.x, bh = at / a.chunks;
+    const int chunk = (int)(at % a.chunks), b = (int)(bh / a.H), h = (int)(bh % a.H), t0 = chunk * kTok;
+    pdl_wait();
+    const int n = live_tokens(a, b), nv = n - t0 < kTok ? n - t0 : kTok;
+    if (nv <= 0) return;
+    if (warp == 0) tmem_alloc(smem_u32(&slot), 64);
+    if (tid == 0) { mbar_init(&bar, 1); fence_mbar_init(); }
+    const long long qk = ((long long)b * a.Hk + h / (a.H / a.Hk)) * a.Dk * a.L + t0, all = (long long)a.B * a.Hk * a.Dk * a.L;
+    load_tile<T>(sm, C::PITCH, (const T *)a.k, qk, all, a.L, a.Dk, nv, tid, 128);
+    load_tile<T>(sm + C::TILE, C::PITCH, (const T *)a.q, qk, all, a.L, a.Dk, nv, tid, 128);
+    const int steps = (a.Dk + 15) / 16;
+    clear_rows(sm, C::PITCH, C::PI, a.Dk, steps * 16, tid, 128);
+    clear_rows(sm + C::TILE, C::PITCH, C::PI, a.Dk, steps * 16, tid, 128);
+    const long long row = bh * a.L + t0;
+    if (warp == 1) chunk_sums(G, a.g + row, a.decay, nv, lane);
+    if (warp >= 2) {
+        const int t = tid - 64;
+        beta[t] = 0.f;
+        if (t < nv) { HN_G(a.beta + row + t, 4); beta[t] = __ldg(a.beta + row + t); }
+    }
+    fence_async_smem();
+    tmem_fence_before_sync();
+    __syncthreads();
+    tmem_fence_after_sync();
+    const unsigned tb = slot, images = smem_u32(sm);
+    if (tid == 0) {
+        issue_ss<C::PI, C::PI, C::PI, true, true>(tb, images, C::PITCH, C::TILE, images, C::PITCH, steps, kTok, false);
+        umma_commit(&bar);
+    }
+    __syncwarp();
+    if (tid < kTok) {                                        // (the decays meanwhile)
+        float *gates = a.gates + at * (4 * kTok);
+        HN_G(gates + tid, 4); HN_G(gates + 2 * kTok + tid, 4);
+        gates[tid] = expf((float)G[tid]);
+        gates[kTok + tid] = expf((float)(G[kTok - 1] - G[tid]));
+        gates[2 * kTok + tid] = beta[tid];
+    }
+    const bool ok = mbar_wait(&bar, 0);
+    if (!ok) atomicExch(&hn_delta_status, 1);
+    tmem_fence_after_sync();
+    // lanes 0 .. 63: rows of k k^T, lanes 64 .. 127: rows of q k^T
+    const int i = tid & 63;
+    const double Gi = G[i];
+    const float bi = beta[i];
+    __syncthreads();                                          // (every thread has waited: the tiles' place is free)
+    unsigned char *imageA = sm, *imageP = sm + C::PM * kMatrix;
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+        float x[32];
+        TmemIO<32>::ld(x, tmem_addr(tb, warp, 32 * hf));
+        tmem_wait_ld();
+#pragma unroll
+        for (int c = 0; c < 32; ++c) {
+            const int j = 32 * hf + c;
+            const float r = expf((float)(Gi - G[j]));
+            x[c] = tid < kTok ? (j < i ? bi * r * x[c] : 0.f) : (j <= i ? r * x[c] : 0.f);
+        }
+        if (tid < kTok) {
+#pragma unroll
+            for (int c = 0; c < 32; c += 4) *(float4 *)(Ts + i * C::TROW + 32 * hf + c) = make_float4(x[c], x[c + 1], x[c + 2], x[c + 3]);
+        } else planes_to_image<C::PM>(imageP, kMatrix, i, hf, x);
+    }
+    tmem_fence_before_sync();
+    __syncthreads();
+    if (warp == 0) tmem_dealloc(tb, 64);
+    if (tid < kTok) {                                         // column tid of A: (I + T) A = I from the top
+        float c[kTok];
+#pragma unroll
+        for (int r = 0; r < kTok; ++r) {
+            float s[4] = {r == tid ? 1.f : 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int m = 0; m < r; m += 4) {
+                const float4 w = *(const float4 *)(Ts + r * C::TROW + m);
+                s[0] = fmaf(-w.x, c[m], s[0]);
+                if (m + 1 < r) s[1] = fmaf(-w.y, c[m + 1], s[1]);
+                if (m + 2 < r) s[2] = fmaf(-w.z, c[m + 2], s[2]);
+                if (m + 3 < r) s[3] = fmaf(-w.w, c[m + 3], s[3]);
+            }
+            c[r] = (s[0] + s[1]) + (s[2] + s[3]);
+        }
+#pragma unroll
+        for (int r = 0; r < kTok; r += 2) {
+            unsigned w[C::PM];
+            split_pair<C::PM>(c[r], c[r + 1], w);
+#pragma unroll
+            for (int p = 0; p < C::PM; ++p) {
+                *(unsigned short *)(imageA + p * kMatrix + image_at(r, tid >> 3) + (tid & 7) * 2) = (unsigned short)(w[p] & 0xffffu);
+                *(unsigned short *)(imageA + p * kMatrix + image_at(r + 1, tid >> 3) + (tid & 7) * 2) = (unsigned short)(w[p] >> 16);
+            }
+        }
+    }
+    __syncthreads();
+    uint4 *to = (uint4 *)(a.images + at * (2 * C::PM * kMatrix));
+    for (int e = tid; e < 2 * C::PM * kMatrix / 16; e += 128) { HN_G(to + e, 16); to[e] = ((const uint4 *)sm)[e]; }
+}
+
+#define WAIT(bar, parity) walk_wait(&ws, bar, parity, &hn_delta_status)
+// ---- walk -----------------------------------------------------------------------------------------------------------
+
+template <typename T, int KD> struct Walk {
+    static constexpr int PI = Planes<T>::IN, PM = Planes<T>::MID, TILE = KD * 128, TENSOR = PI * TILE;
+    static constexpr int IMAGES = 2 * PM * kMatrix;
+    static constexpr int STAGE = 2 * TENSOR + IMAGES + 1024;                  // K, Q, A, P, gates
+    static constexpr int STAGES = 3 * STAGE <= 220 * 1024 ? 3 : 2 * STAGE <= 220 * 1024 ? 2 : 1;
+    static constexpr int BYTES = 1024 + STAGES * STAGE;
+    // tensor memory: S (later delta U) as an operand | Z, later U, as an operand | sums | Y
+    static constexpr int SCOLS = PM * KD / 2, ZCOLS = PM * kTok / 2, S0 = 0, Z0 = SCOLS, X0 = Z0 + ZCOLS, Y0 = X0 + (KD > kTok ? KD : kTok);
+    static_assert(Y0 + kTok <= 512, "tensor memory");
+};
+
+template <typename T, int KD, int MODE> __global__ void __launch_bounds__(384, 1) delta_walk_kernel(DeltaArgs a)
+{
+    using C = Walk<T, KD>;
+    constexpr int PI = C::PI, PM = C::PM, HC = KD / 2;
+    extern __shared__ __align__(1024) unsigned char raw[];
+    __shared__ WalkShared ws;
+    unsigned char *sm = align_images(raw);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    long long id = blockIdx.x;
+    const bool phi = MODE == WALK_MAPS && (id & 1);          // from the identity, without values
+    if (MODE == WALK_MAPS) id >>= 1;
+    const long long bh = id / a.segments;
+    const int segment = (int)(id % a.segments), b = (int)(bh / a.H), h = (int)(bh % a.H);
+    pdl_wait();
+    const int n = live_tokens(a, b), first = segment * a.per_segment, end = first + a.per_segment < a.chunks ? first + a.per_segment : a.chunks;
+    int last = (n + kTok - 1) / kTok;                        // chunks first .. last - 1 hold tokens
+    last = last < end ? last : end;
+    if (warp == 0) tmem_alloc(smem_u32(&ws.slot), 512);
+    if (tid == 0) {
+        for (int s = 0; s < C::STAGES; ++s) { mbar_init(&ws.full[s], 129); mbar_init(&ws.empty[s], 1); }
+        mbar_init(&ws.bar_a, 1); mbar_init(&ws.bar_b, 1); mbar_init(&ws.bar_c, 1); mbar_init(&ws.bar_q, 1); mbar_init(&ws.bar_y, 1);
+        ws.gave_up = 0;
+        fence_mbar_init();
+    }
+    for (int s = 0; s < C::STAGES; ++s) clear_rows(sm + s * C::STAGE, C::TILE, 2 * PI, a.Dk, KD, tid, 384);
+    fence_async_smem();
+    tmem_fence_before_sync();
+    __syncthreads();
+    tmem_fence_after_sync();
+    const unsigned tb = ws.slot;
+    const int steps = (a.Dk + 15) / 16;
+    if (warp >= 8) {
+        // ---- the four warps that fetch
+        const int ft = tid - 256;
+        const long long qk = ((long long)b * a.Hk + h / (a.H / a.Hk)) * a.Dk * a.L, all = (long long)a.B * a.Hk * a.Dk * a.L;
+        for (int c = first, i = 0; c < last; ++c, ++i) {
+            const int s = i % C::STAGES, t0 = c * kTok, nv = n - t0 < kTok ? n - t0 : kTok;
+            if (i >= C::STAGES) WAIT(&ws.empty[s], (i / C::STAGES - 1) & 1);
+            unsigned char *st = sm + s * C::STAGE;
+            if (ft == 0) {
+                const long long at = bh * a.chunks + c;
+                const unsigned bytes = MODE == WALK_MAPS ? PM * kMatrix : 2 * PM * kMatrix;
+                mbar_expect_tx(&ws.full[s], bytes + 3 * kTok * 4);
+                bulk_load(st + 2 * C::TENSOR, a.images + at * C::IMAGES, bytes, &ws.full[s]);
+                bulk_load(st + 2 * C::TENSOR + C::IMAGES, a.gates + at * (4 * kTok), 3 * kTok * 4, &ws.full[s]);
+            }
+            load_tile<T>(st, C::TILE, (const T *)a.k, qk + t0, all, a.L, a.Dk, nv, ft, 128);
+            if (MODE != WALK_MAPS) load_tile<T>(st + C::TENSOR, C::TILE, (const T *)a.q, qk + t0, all, a.L, a.Dk, nv, ft, 128);
+            fence_async_smem();
+            mbar_arrive(&ws.full[s]);
+        }
+    } else {
+        // ---- the eight that compute: lane of tensor memory = row of the state, `half` = which half of the columns
+        const int row = 32 * (warp & 3) + lane, half = warp >> 2, rows = phi ? a.Dk : a.Dv;
+        const unsigned lane_s = tmem_addr(tb, warp, C::S0 + half * (HC / 2)), lane_z = tmem_addr(tb, warp, C::Z0 + half * 16),
+                       lane_x = tmem_addr(tb, warp, C::X0), lane_y = tmem_addr(tb, warp, C::Y0 + half * 32);
+        const long long vrow = (bh * a.Dv + row) * a.L, vall = (long long)a.B * a.H * a.Dv * a.L, states = (long long)a.Dv * a.Dk;
+        const bool real = row < a.Dv;
+        float S[HC];
+#pragma unroll
+        for (int i = 0; i < HC; ++i) S[i] = 0.f;
+        if (MODE == WALK_MAPS) {
+            if (phi) {
+#pragma unroll
+                for (int i = 0; i < HC; ++i) S[i] = row == half * HC + i && row < a.Dk ? 1.f : 0.f;
+            }
+        } else {
+            const float *from = a.segments > 1 ? a.starts + (bh * a.segments + segment) * states : a.s0 ? a.s0 + bh * states : nullptr;
+            if (from) load_state<HC>(S, from, row, a.Dv, half * HC, a.Dk);
+        }
+        RowPart<T> v;
+        auto fetch_v = [&](int c) {
+            const int t = c * kTok + 32 * half;
+            v.load((const T *)a.v, vrow + t, vall, a.L, real && !phi ? n - t : 0);
+        };
+        auto put_y = [&](int c) {
+            float y[32];
+            TmemIO<32>::ld(y, lane_y);
+            tmem_wait_ld();
+            const int t = c * kTok + 32 * half;
+            if (real && t < a.L) store_row<T>((T *)a.y, vrow + t, a.L, a.L - t, n - t, y);
+        };
+        if (first < last) fetch_v(first);
+        for (int c = first, i = 0; c < last; ++c, ++i) {
+            const int s = i % C::STAGES;
+            const unsigned par = i & 1;
+            unsigned char *st = sm + s * C::STAGE;
+            const unsigned k = smem_u32(st), q = k + C::TENSOR, A = q + C::TENSOR, P = A + PM * kMatrix;
+            const float *gates = (const float *)(st + 2 * C::TENSOR + C::IMAGES);
+            if (MODE != WALK_MAPS && a.marks) store_state<HC>(a.marks + (bh * a.chunks + c) * states, S, row, a.Dv, half * HC, a.Dk);
+            planes_to_tmem<PM, HC / 2>(lane_s, KD / 2, S);
+            tmem_wait_st();
+            tmem_fence_before_sync();
+            WAIT(&ws.full[s], (i / C::STAGES) & 1);
+            walkers_sync();
+            if (tid == 0) {
+                tmem_fence_after_sync();
+                issue_ts<PM, PI, PM, true>(tb + C::X0, tb + C::S0, KD / 2, k, C::TILE, steps, kTok, false);
+                umma_commit(&ws.bar_a);
+            }
+            __syncwarp();
+            if (MODE != WALK_MAPS) {
+                if (i) {
+                    WAIT(&ws.bar_y, par ^ 1);
+                    tmem_fence_after_sync();
+                    put_y(c - 1);
+                    tmem_fence_before_sync();
+                }
+                walkers_sync();
+                if (tid == 0) {
+                    tmem_fence_after_sync();
+                    issue_ts<PM, PI, PM, true>(tb + C::Y0, tb + C::S0, KD / 2, q, C::TILE, steps, kTok, false);
+                    umma_commit(&ws.bar_q);
+                }
+                __syncwarp();
+            }
+            float x[32];
+            WAIT(&ws.bar_a, par);
+            tmem_fence_after_sync();
+            TmemIO<32>::ld(x, lane_x + 32 * half);
+            tmem_wait_ld();
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) {
+                const float4 ga = *(const float4 *)(gates + 32 * half + e), be = *(const float4 *)(gates + 2 * kTok + 32 * half + e);
+                x[e] = be.x * fmaf(-ga.x, x[e], v.get(e));
+                x[e + 1] = be.y * fmaf(-ga.y, x[e + 1], v.get(e + 1));
+                x[e + 2] = be.z * fmaf(-ga.z, x[e + 2], v.get(e + 2));
+                x[e + 3] = be.w * fmaf(-ga.w, x[e + 3], v.get(e + 3));
+            }
+            planes_to_tmem<PM, 16>(lane_z, kTok / 2, x);
+            tmem_wait_st();
+            tmem_fence_before_sync();
+            walkers_sync();
+            if (tid == 0) {
+                tmem_fence_after_sync();
+                issue_ts<PM, PM, PM, false>(tb + C::X0, tb + C::Z0, kTok / 2, A, kMatrix, kTok / 16, kTok, false);
+                umma_commit(&ws.bar_b);
+            }
+            __syncwarp();
+            if (c + 1 < last) fetch_v(c + 1);
+            if (MODE != WALK_MAPS) {                         // y's first sum by gamma, while A Z is formed
+                WAIT(&ws.bar_q, par);
+                tmem_fence_after_sync();
+                TmemIO<32>::ld(x, lane_y);
+                tmem_wait_ld();
+#pragma unroll
+                for (int e = 0; e < 32; e += 4) {
+                    const float4 ga = *(const float4 *)(gates + 32 * half + e);
+                    x[e] *= ga.x; x[e + 1] *= ga.y; x[e + 2] *= ga.z; x[e + 3] *= ga.w;
+                }
+                TmemIO<32>::st(lane_y, x);
+            }
+            WAIT(&ws.bar_b, par);
+            tmem_fence_after_sync();
+            TmemIO<32>::ld(x, lane_x + 32 * half);
+            tmem_wait_ld();
+            if (MODE != WALK_MAPS) planes_to_tmem<PM, 16>(lane_z, kTok / 2, x);
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) {
+                const float4 de = *(const float4 *)(gates + kTok + 32 * half + e);
+                x[e] *= de.x; x[e + 1] *= de.y; x[e + 2] *= de.z; x[e + 3] *= de.w;
+            }
+            planes_to_tmem<PM, 16>(tmem_addr(tb, warp, C::S0 + half * 16), kTok / 2, x);
+            const float fade = gates[kTok - 1];
+            tmem_wait_st();
+            tmem_fence_before_sync();
+            walkers_sync();
+            if (tid == 0) {
+                tmem_fence_after_sync();
+                issue_ts<PM, PI, PM, false>(tb + C::X0, tb + C::S0, kTok / 2, k, C::TILE, kTok / 16, KD, false);
+                umma_commit(&ws.bar_c);
+                if (MODE != WALK_MAPS) {
+                    issue_ts<PM, PM, PM, false>(tb + C::Y0, tb + C::Z0, kTok / 2, P, kMatrix, kTok / 16, kTok, true);
+                    umma_commit(&ws.bar_y);
+                }
+                umma_commit(&ws.empty[s]);
+            }
+            __syncwarp();
+            WAIT(&ws.bar_c, par);
+            tmem_fence_after_sync();
+#pragma unroll
+            for (int e = 0; e < HC; e += 32) {
+                TmemIO<32>::ld(x, lane_x + half * HC + e);
+                tmem_wait_ld();
+#pragma unroll
+                for (int j = 0; j < 32; ++j) S[e + j] = fmaf(fade, S[e + j], x[j]);
+            }
+        }
+        if (MODE == WALK_MAPS) {
+            float *to = a.maps + (bh * a.segments + segment) * (long long)(a.Dv + a.Dk) * a.Dk + (phi ? states : 0);
+            store_state<HC>(to, S, row, rows, half * HC, a.Dk);
+        } else {
+            if (first < last) {
+                WAIT(&ws.bar_y, (last - first - 1) & 1);
+                tmem_fence_after_sync();
+                put_y(last - 1);
+            }
+            float none[32];
+#pragma unroll
+            for (int e = 0; e < 32; ++e) none[e] = 0.f;
+            for (int c = first > last ? first : last; c < end; ++c) {
+                const int t = c * kTok + 32 * half;
+                if (real && t < a.L) store_row<T>((T *)a.y, vrow + t, a.L, a.L - t, 0, none);
+            }
+            if (a.s_end && segment == a.segments - 1) store_state<HC>(a.s_end + bh * states, S, row, a.Dv, half * HC, a.Dk);
+        }
+        tmem_fence_before_sync();
+    }
+    __syncthreads();
+    if (ws.gave_up && tid == 0)                              // copies on their way end before the memory they go to is another CTA's
+        for (int s = 0; s < C::STAGES; ++s) mbar_wait(&ws.full[s], 0);
+    if (warp == 0) tmem_dealloc(tb, 512);
+}
+
+// ---- segments -------------------------------------------------------------------------------------------------------
+
+// States at the segments' starts from the maps S -> S Phi + N: eight rows to a CTA, four quarters of the sum over Phi's rows; the next
+// segment's Phi is on its way meanwhile.  `reverse`: from the last segment to the first (the gradient's states).
+__global__ void __launch_bounds__(512) delta_join_kernel(DeltaArgs a, const float *from, int reverse)
+{
+    constexpr int R = 8;
+    __shared__ float S[R][128], part[4][R][128];
+    const int j = threadIdx.x & 127, quarter = threadIdx.x >> 7, tiles = (a.Dv + R - 1) / R;
+    const long long bh = blockIdx.x / tiles, states = (long long)a.Dv * a.Dk, map = states + (long long)a.Dk * a.Dk;
+    const int r0 = (int)(blockIdx.x % tiles) * R;
+    pdl_join();
+    for (int e = threadIdx.x; e < R * 128; e += 512) {
+        const int r = e >> 7, c = e & 127;
+        float v = 0.f;
+        if (from && r0 + r < a.Dv && c < a.Dk) { const float *p = from + bh * states + (long long)(r0 + r) * a.Dk + c; HN_G(p, 4); v = *p; }
+        S[r][c] = v;
+    }
+    float phi[32];
+    auto fetch = [&](int s) {
+        const float *p = a.maps + (bh * a.segments + s) * map + states;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            const int k = quarter * 32 + i;
+            phi[i] = 0.f;
+            if (k < a.Dk && j < a.Dk) { HN_G(p + (long long)k * a.Dk + j, 4); phi[i] = p[(long long)k * a.Dk + j]; }
+        }
+    };
+    const int n = a.segments, step = reverse ? -1 : 1;
+    int s = reverse ? n - 1 : 0;
+    fetch(s);
+    __syncthreads();
+    for (int i = 0; i < n; ++i, s += step) {
+        for (int r = quarter; r < R; r += 4)
+            if (r0 + r < a.Dv && j < a.Dk) {
+                float *p = a.starts + (bh * n + s) * states + (long long)(r0 + r) * a.Dk + j;
+                HN_G(p, 4);
+                *p = S[r][j];
+            }
+        if (i == n - 1) break;
+        float acc[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            acc[r] = 0.f;
+#pragma unroll
+            for (int k = 0; k < 32; k += 4) {
+                const float4 w = *(const float4 *)&S[r][quarter * 32 + k];
+                acc[r] = fmaf(w.x, phi[k], fmaf(w.y, phi[k + 1], fmaf(w.z, phi[k + 2], fmaf(w.w, phi[k + 3], acc[r]))));
+            }
+        }
+        float add[2] = {0.f, 0.f};
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int r = quarter + 4 * e;
+            if (r0 + r < a.Dv && j < a.Dk) { const float *p = a.maps + (bh * n + s) * map + (long long)(r0 + r) * a.Dk + j; HN_G(p, 4); add[e] = *p; }
+        }
+        fetch(s + step);
+#pragma unroll
+        for (int r = 0; r < R; ++r) part[quarter][r][j] = acc[r];
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int r = quarter + 4 * e;
+            S[r][j] = ((part[0][r][j] + part[1][r][j]) + (part[2][r][j] + part[3][r][j])) + add[e];
+        }
+        __syncthreads();
+    }
+}
+
+// ---- one token ------------------------------------------------------------------------------------------------------
+
+// W lanes to a row of the state, four columns each; the products with k and q are formed in one reading, the new state is written in
+// the same: bandwidth is the bound.  A decay next to 1 is applied as a - 1, so that thousands of tokens one by one cost a rounding each.
+template <typename T, int W> __global__ void __launch_bounds__(256) delta_step_kernel(DeltaArgs a)
+{
+    constexpr int ROWS = 256 / W, EACH = 4;                  // rows at a time, and times
+    const int lane = threadIdx.x % W, c0 = 4 * lane, tiles = (a.Dv + ROWS * EACH - 1) / (ROWS * EACH);
+    const long long bh = blockIdx.x / tiles;
+    const int b = (int)(bh / a.H), h = (int)(bh % a.H), r0 = (int)(blockIdx.x % tiles) * ROWS * EACH + threadIdx.x / W;
+    pdl_join();
+    const float *from = a.s0 + bh * a.Dv * a.Dk;
+    float *to = a.s_end + bh * a.Dv * a.Dk;
+    float S[EACH][4], k[4], q[4];
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) load_state<4>(S[e], from, r0 + e * ROWS, a.Dv, c0, a.Dk);
+    bool in = true;
+    if (a.lengths) { HN_G(a.lengths + b, 4); in = __ldg(a.lengths + b) > 0; }
+    const long long qk = ((long long)b * a.Hk + h / (a.H / a.Hk)) * a.Dk, vr = bh * a.Dv;
+    float kq = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        k[i] = in && c0 + i < a.Dk ? IO<T>::ld((const T *)a.k, qk + c0 + i) : 0.f;
+        q[i] = in && c0 + i < a.Dk ? IO<T>::ld((const T *)a.q, qk + c0 + i) : 0.f;
+        kq = fmaf(k[i], q[i], kq);
+    }
+    float fade = 1.f, less = 0.f, beta = 0.f;
+    if (in) {
+        HN_G(a.beta + bh, 4);
+        beta = __ldg(a.beta + bh);
+        if (a.decay != DELTA_NONE) {
+            HN_G(a.g + bh, 4);
+            const float g = __ldg(a.g + bh);
+            if (a.decay == DELTA_LOG) { fade = expf(g); less = expm1f(g); }
+            else { const float e = expf(-fabsf(g)), x = e / (1.f + e); fade = g >= 0.f ? 1.f - x : x; less = g >= 0.f ? -x : x - 1.f; }
+        }
+    }
+#pragma unroll
+    for (int m = 1; m < W; m <<= 1) kq += __shfl_xor_sync(~0u, kq, m);
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+        const int r = r0 + e * ROWS;
+        float sk = 0.f, sq = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { sk = fmaf(S[e][i], k[i], sk); sq = fmaf(S[e][i], q[i], sq); }
+#pragma unroll
+        for (int m = 1; m < W; m <<= 1) { sk += __shfl_xor_sync(~0u, sk, m); sq += __shfl_xor_sync(~0u, sq, m); }
+        float v = 0.f;
+        if (in && r < a.Dv) v = IO<T>::ld((const T *)a.v, vr + r);
+        const float u = beta * fmaf(-fade, sk, v);
+        if (in) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) S[e][i] = fade > 0.5f ? S[e][i] + fmaf(less, S[e][i], u * k[i]) : fmaf(fade, S[e][i], u * k[i]);
+        }
+        if (r < a.Dv && lane == 0) IO<T>::st((T *)a.y, vr + r, in ? fmaf(fade, sq, u * kq) : 0.f);
+        store_state<4>(to, S[e], r, a.Dv, c0, a.Dk);
+    }
+}
+
+// ---- host -----------------------------------------------------------------------------------------------------------
+
+static size_t up(size_t n) { return (n + 255) / 256 * 256; }
+DeltaSizes delta_sizes(const DeltaArgs &a, int dtype, bool backward)
+{
+    const size_t bh = (size_t)a.B * a.H, chunks = bh * a.chunks, planes = dtype == HYENAND_F32 ? Planes<float>::MID : Planes<bf16>::MID;
+    DeltaSizes s{};
+    s.images = chunks * 2 * planes * kMatrix;
+    s.gates = chunks * kGates;
+    if (a.segments > 1) {
+        s.maps = up(bh * a.segments * ((size_t)a.Dv + a.Dk) * a.Dk * 4);
+        s.starts = up(bh * a.segments * (size_t)a.Dv * a.Dk * 4);
+    }
+    if (backward) {
+        s.dstates = up(chunks * a.Dv * a.Dk * 4);
+        s.dz = chunks * a.Dv * kTok * 4;
+    }
+    s.all = s.images + s.gates + s.maps + s.starts + s.dstates + s.dz;
+    return s;
+}
+static void place_workspace(DeltaArgs &a, const DeltaSizes &s, void *workspace)
+{
+    unsigned char *p = (unsigned char *)workspace;
+    a.images = p; p += s.images;
+    a.gates = (float *)p; p += s.gates;
+    a.maps = (float *)p; p += s.maps;
+    a.starts = (float *)p; p += s.starts;
+    a.dstates = (float *)p; p += s.dstates;
+    a.dz = (float *)p;
+}
+
+template <typename T> static int launch_prepare(const DeltaArgs &a, cudaStream_t st)
+{
+    const long long blocks = (long long)a.B * a.H * a.chunks;
+    return a.Dk <= 64 ? launch_delta<delta_prepare_kernel<T, 64>>(a, blocks, 128, Prep<T, 64>::BYTES, st)
+                      : launch_delta<delta_prepare_kernel<T, 128>>(a, blocks, 128, Prep<T, 128>::BYTES, st);
+}
+int launch_delta_prepare(const DeltaArgs &a, int dtype, cudaStream_t st) { return dtype == HYENAND_F32 ? launch_prepare<float>(a, st) : launch_prepare<bf16>(a, st); }
+
+int launch_delta_join(const DeltaArgs &a, const float *from, bool backward, cudaStream_t st)
+{
+    const long long blocks = (long long)a.B * a.H * ((a.Dv + 7) / 8);
+    if (blocks > 0x7fffffffll) return kTooLarge;
+    launch_pdl(delta_join_kernel, dim3((unsigned)blocks), 512, 0, st, a, from, (int)backward);
+    return 0;
+}
+
+template <typename T, int KD> static int launch_walk(const DeltaArgs &a, cudaStream_t st)
+{
+    const long long blocks = (long long)a.B * a.H * a.segments;
+    if (a.segments > 1) {
+        if (const int e = launch_delta<delta_walk_kernel<T, KD, WALK_MAPS>>(a, 2 * blocks, 384, Walk<T, KD>::BYTES, st)) return e;
+        if (const int e = launch_delta_join(a, a.s0, false, st)) return e;
+    }
+    return launch_delta<delta_walk_kernel<T, KD, WALK_RUN>>(a, blocks, 384, Walk<T, KD>::BYTES, st);
+}
+template <typename T> static int launch_forward(const DeltaArgs &a, cudaStream_t st)
+{
+    if (const int e = launch_prepare<T>(a, st)) return e;
+    return a.Dk <= 64 ? launch_walk<T, 64>(a, st) : launch_walk<T, 128>(a, st);
+}
+template <typename T> static int launch_step(const DeltaArgs &a, cudaStream_t st)
+{
+    const int W = a.Dk <= 32 ? 8 : a.Dk <= 64 ? 16 : 32, per = 256 / W * 4;
+    const long long blocks = (long long)a.B * a.H * ((a.Dv + per - 1) / per);
+    return W == 8 ? launch_delta<delta_step_kernel<T, 8>>(a, blocks, 256, 0, st)
+           : W == 16 ? launch_delta<delta_step_kernel<T, 16>>(a, blocks, 256, 0, st) : launch_delta<delta_step_kernel<T, 32>>(a, blocks, 256, 0, st);
+}
+
+// Segments of a head.  They cost three walks in place of one (two CTAs for the maps), so they pay where each SM would otherwise have a
+// quarter of a head or less.
+static int segments_of(long long heads, int chunks)
+{
+    const long long n = kSms / heads;
+    if (n < 4 || chunks < 16) return 1;
+    const long long each = (chunks + n - 1) / n, most = each > 4 ? each : 4;
+    return (int)((chunks + most - 1) / most);
+}
+
+static int fill(DeltaArgs &a, int B, int H, int Hk, int L, int Dk, int Dv, int decay, int dtype)
+{
+    if (B < 1 || H < 1 || Hk < 1 || L < 1 || Dk < 1 || Dv < 1) return fail(HYENAND_ERR_INVALID_ARG, "B, H, Hk, L, Dk and Dv must be >= 1");
+    if (decay != DELTA_LOG && decay != DELTA_SIGMOID && decay != DELTA_NONE) return fail(HYENAND_ERR_INVALID_ARG, "unknown decay %d", decay);
+    if (dtype != HYENAND_F32 && dtype != HYENAND_BF16) return fail(HYENAND_ERR_INVALID_ARG, "unknown dtype %d", dtype);
+    if (H % Hk) return fail(HYENAND_ERR_INVALID_ARG, "H = %d is no multiple of Hk = %d", H, Hk);
+    if (Dk > 128 || Dv > 128) return fail(HYENAND_ERR_UNSUPPORTED, "heads of up to 128 channels (Dk = %d, Dv = %d)", Dk, Dv);
+    if (L > (1 << 30)) return fail(HYENAND_ERR_UNSUPPORTED, "L = %d is above 2^30", L);
+    if ((long long)B * H > (1 << 24)) return fail(HYENAND_ERR_UNSUPPORTED, "B * H is above 2^24");
+    a.B = B; a.H = H; a.Hk = Hk; a.L = L; a.Dk = Dk; a.Dv = Dv; a.decay = decay;
+    a.chunks = (L + kTok - 1) / kTok;
+    if ((long long)B * H * a.chunks > 0x3fffffffll) return fail(HYENAND_ERR_UNSUPPORTED, "B * H * L is above 2^36");
+    a.segments = segments_of((long long)B * H, a.chunks);
+    a.per_segment = (a.chunks + a.segments - 1) / a.segments;
+    return HYENAND_OK;
+}
+static size_t state_bytes(const DeltaArgs &a) { return (size_t)a.B * a.H * a.Dv * a.Dk * sizeof(float); }
+// what every call takes: q, k, v, g, beta (of T tokens)
+static int inputs(CallTensors &c, const DeltaArgs &a, size_t T, int dtype)
+{
+    if (!a.q || !a.k || !a.v || !a.beta) return fail(HYENAND_ERR_INVALID_ARG, "q, k, v, beta must be non-NULL");
+    if ((a.g != nullptr) != (a.decay != DELTA_NONE)) return fail(HYENAND_ERR_INVALID_ARG, "g is given exactly where there is a decay");
+    const size_t es = elsize(dtype) * T * a.B, gb = (size_t)a.B * a.H * T * sizeof(float);
+    c.in("q", a.q, es * a.Hk * a.Dk); c.in("k", a.k, es * a.Hk * a.Dk); c.in("v", a.v, es * a.H * a.Dv);
+    c.in("g", a.g, gb, 4); c.in("beta", a.beta, gb, 4);
+    c.in("lengths", a.lengths, (size_t)a.B * sizeof(int), 4);
+    return HYENAND_OK;
+}
+
+}  // namespace hn
+
+using namespace hn;
+
+extern "C" int hyenand_delta_marks(int L) { return L < 1 || L > (1 << 30) ? 0 : (L + kTok - 1) / kTok; }
+
+extern "C" long long hyenand_delta_workspace_bytes(int B, int H, int Hk, int L, int Dk, int Dv, int dtype, int backward)
+{
+    clear_error();
+    DeltaArgs a{};
+    if (fill(a, B, H, Hk, L, Dk, Dv, DELTA_NONE, dtype)) return 0;
+    return (long long)delta_sizes(a, dtype, backward != 0).all;
+}
+
+extern "C" int hyenand_delta_device_status(void)
+{
+    int v = 0;
+    if (cudaDeviceSynchronize() != cudaSuccess || cudaMemcpyFromSymbol(&v, hn_delta_status, sizeof(int)) != cudaSuccess) return -1;
+    const int w = delta_backward_status();
+    return w < 0 ? w : v | w;
+}
+
+extern "C" int hyenand_delta_forward(int B, int H, int Hk, int L, int Dk, int Dv, int decay, int dtype, const void *q, const void *k, const void *v,
+                                     const float *g, const float *beta, const float *s0, const int *lengths, void *y, float *s_end, float *marks,
+                                     void *workspace, void *cuda_stream)
+{
+    clear_error();
+    DeltaArgs a{};
+    if (int e = fill(a, B, H, Hk, L, Dk, Dv, decay, dtype)) return e;
+    if (!y || !workspace) return fail(HYENAND_ERR_INVALID_ARG, "y and workspace must be non-NULL");
+    a.q = q; a.k = k; a.v = v; a.g = g; a.beta = beta; a.s0 = s0; a.lengths = lengths; a.y = y; a.s_end = s_end; a.marks = marks;
+    CallTensors c;
+    if (int e = inputs(c, a, L, dtype)) return e;
+    const DeltaSizes s = delta_sizes(a, dtype, false);
+    place_workspace(a, s, workspace);
+    c.in("s0", s0, state_bytes(a));
+    c.out("y", y, (size_t)B * H * Dv * L * elsize(dtype)); c.out("s_end", s_end, state_bytes(a), 16, s0);
+    c.out("marks", marks, state_bytes(a) * a.chunks); c.out("workspace", workspace, s.all);
+    if (int e = c.check()) return e;
+    c.register_ranges();
+    const cudaStream_t st = (cudaStream_t)cuda_stream;
+    return finish(dtype == HYENAND_F32 ? launch_forward<float>(a, st) : launch_forward<bf16>(a, st));
+}
+
+extern "C" int hyenand_delta_backward(int B, int H, int Hk, int L, int Dk, int Dv, int decay, int dtype, const void *q, const void *k, const void *v,
+                                      const float *g, const float *beta, const int *lengths, const float *marks, const void *dy, const float *ds_end,
+                                      void *dq, void *dk, void *dv, float *dg, float *dbeta, float *ds0, void *workspace, void *cuda_stream)
+{
+    clear_error();
+    DeltaArgs a{};
+    if (int e = fill(a, B, H, Hk, L, Dk, Dv, decay, dtype)) return e;
+    if (!marks || !dy || !dq || !dk || !dv || !dbeta || !workspace)
+        return fail(HYENAND_ERR_INVALID_ARG, "marks, dy, dq, dk, dv, dbeta, workspace must be non-NULL");
+    if (decay == DELTA_NONE && dg) return fail(HYENAND_ERR_INVALID_ARG, "dg of a rule without a decay");
+    a.q = q; a.k = k; a.v = v; a.g = g; a.beta = beta; a.lengths = lengths; a.marks = (float *)marks; a.dy = dy; a.ds_end = ds_end;
+    a.dq = dq; a.dk = dk; a.dv = dv; a.dg = dg; a.dbeta = dbeta; a.ds0 = ds0;
+    CallTensors c;
+    if (int e = inputs(c, a, L, dtype)) return e;
+    const DeltaSizes s = delta_sizes(a, dtype, true);
+    place_workspace(a, s, workspace);
+    const size_t es = elsize(dtype) * (size_t)L * B, gb = (size_t)B * H * L * sizeof(float);
+    c.in("marks", marks, state_bytes(a) * a.chunks); c.in("dy", dy, es * H * Dv); c.in("ds_end", ds_end, state_bytes(a));
+    c.out("dq", dq, es * Hk * Dk); c.out("dk", dk, es * Hk * Dk); c.out("dv", dv, es * H * Dv); c.out("dg", dg, gb, 4); c.out("dbeta", dbeta, gb, 4);
+    c.out("ds0", ds0, state_bytes(a), 16, ds_end); c.out("workspace", workspace, s.all);
+    if (int e = c.check()) return e;
+    c.register_ranges();
+    return finish(launch_delta_backward(a, dtype, (cudaStream_t)cuda_stream));
+}
+
+extern "C" int hyenand_delta_step(int B, int H, int Hk, int Dk, int Dv, int decay, int dtype, const void *q, const void *k, const void *v, const float *g,
+                                  const float *beta, const float *state, const int *active, void *y, float *new_state, void *cuda_stream)
+{
+    clear_error();
+    DeltaArgs a{};
+    if (int e = fill(a, B, H, Hk, 1, Dk, Dv, decay, dtype)) return e;
+    if (!state || !y || !new_state) return fail(HYENAND_ERR_INVALID_ARG, "state, y, new_state must be non-NULL");
+    a.q = q; a.k = k; a.v = v; a.g = g; a.beta = beta; a.s0 = state; a.lengths = active; a.y = y; a.s_end = new_state;
+    CallTensors c;
+    if (int e = inputs(c, a, 1, dtype)) return e;
+    c.in("state", state, state_bytes(a));
+    c.out("y", y, (size_t)B * H * Dv * elsize(dtype)); c.out("new_state", new_state, state_bytes(a), 16, state);
+    if (int e = c.check()) return e;
+    c.register_ranges();
+    const cudaStream_t st = (cudaStream_t)cuda_stream;
+    return finish(dtype == HYENAND_F32 ? launch_step<float>(a, st) : launch_step<bf16>(a, st));
+}

@@ -1,0 +1,415 @@
+// The gated delta rule in chunks of 64 tokens: what its kernels share (internal).
+//
+// For one value head, S in R^{Dv x Dk}:   u_t = beta_t (v_t - a_t S_{t-1} k_t),   S_t = a_t S_{t-1} + u_t k_t^T,   y_t = S_t q_t.
+// Over a chunk that starts from S0, with G_i = log a_1 + .. + log a_i, gamma_i = exp(G_i), delta_i = exp(G_64 - G_i), r_ij = exp(G_i - G_j):
+//     T_ij = beta_i r_ij (k_i . k_j)  (j < i),   A = (I + T)^{-1},   P_ij = r_ij (q_i . k_j)  (j <= i),
+//     R_i = v_i - gamma_i S0 k_i,   U = A (beta R),   Y_i = gamma_i S0 q_i + sum_j P_ij u_j,   S1 = gamma_64 S0 + sum_j delta_j u_j k_j^T.
+// Gradient, from dY and dS1:
+//     dU_j = sum_i P_ij dY_i + delta_j dS1 k_j,   dZ = A^T dU,   dV = beta dZ,
+//     dS0 = gamma_64 dS1 + sum_i gamma_i (dY_i q_i^T - beta_i dZ_i k_i^T),
+//     F_ij = r_ij (dY_i . u_j)  (j <= i),   E_ij = - beta_i r_ij (dZ_i . u_j)  (j < i),
+//     dQ_i = gamma_i S0^T dY_i + sum_j F_ij k_j,
+//     dK_i = [sum_j E_ij k_j - gamma_i beta_i S0^T dZ_i]  +  [sum_j (F_ji q_j + E_ji k_j) + delta_i dS1^T u_i]      (erased, written),
+//     dbeta_i = dZ_i . R_i - sum_{j<i} (dZ_i . u_j) r_ij (k_i . k_j),
+//     dG_i = q_i . dQ_i + k_i . dK_i^erased - k_i . dK_i^written,   dG_64 += <S1, dS1>,   d log a_t = sum_{i >= t} dG_i.
+// (A token's decay scales its query and what it erases, and divides what it writes: hence dG.)
+//
+// The products run on the tensor cores in bf16 with fp32 sums.  A number that is no bf16 value goes in as a sum of bf16 values ("planes"):
+// two for bf16 tensors (16 bits, errors of 2^-17: states and sums are fp32 and a result is rounded once, so these errors stay far
+// below a bf16 result's own), three for fp32 tensors (24 bits).  Tensors of bf16 are one plane as they are.  A product of planes
+// p and q is formed where p + q is below the number of planes.
+#pragma once
+#include "entry.cuh"
+#include "umma.cuh"
+
+namespace hn {
+
+constexpr int kTok = 64;                                  // tokens of a chunk
+enum { DELTA_LOG = HYENAND_DECAY_LOG, DELTA_SIGMOID = HYENAND_DECAY_SIGMOID, DELTA_NONE = HYENAND_DECAY_NONE };
+
+template <typename T> struct Planes { static constexpr int IN = 1, MID = 2; };
+template <> struct Planes<float> { static constexpr int IN = 3, MID = 3; };
+constexpr int kMatrix = kTok * 128;                       // bytes of one plane of a 64 x 64 matrix
+constexpr int kGates = 4 * kTok * 4;                      // gamma, delta, beta of a chunk, and room
+
+struct DeltaArgs {
+    const void *q, *k, *v;
+    const float *g, *beta, *s0;
+    const int *lengths;
+    void *y;
+    float *s_end, *marks;
+    // gradient
+    const void *dy;
+    const float *ds_end;
+    void *dq, *dk, *dv;
+    float *dg, *dbeta, *ds0;
+    // workspace
+    unsigned char *images;                                // [B H][chunks]: planes of A, planes of P
+    float *gates;                                         // [B H][chunks][4][64]
+    float *maps, *starts;                                 // [B H][segments][Dv + Dk][Dk], [B H][segments][Dv][Dk]
+    float *dstates, *dz;                                  // [B H][chunks][Dv][Dk], [B H][chunks][Dv][64]
+    int B, H, Hk, L, Dk, Dv, decay, chunks, segments, per_segment;
+};
+
+__device__ __forceinline__ int live_tokens(const DeltaArgs &a, int b)
+{
+    if (!a.lengths) return a.L;
+    HN_G(a.lengths + b, 4);
+    const int n = __ldg(a.lengths + b);
+    return n < 0 ? 0 : n < a.L ? n : a.L;
+}
+
+// a pair of numbers as PM planes of bf16 pairs, each the rest of the ones before, rounded to nearest (so that a rest has either sign
+// and what is left out of a product, rest times rest, averages out: cut off instead, states were off by 7e-6, now by 2e-6)
+template <int PM> __device__ __forceinline__ void split_pair(float x, float y, unsigned (&w)[PM])
+{
+#pragma unroll
+    for (int p = 0; p < PM; ++p) {
+        const __nv_bfloat162 r = __floats2bfloat162_rn(x, y);
+        w[p] = *(const unsigned *)&r;
+        x -= __uint_as_float(w[p] << 16);
+        y -= __uint_as_float(w[p] & 0xffff0000u);
+    }
+}
+
+// 2 C numbers of this thread's row as the A operand in tensor memory: C columns per plane, planes `pitch` columns apart
+template <int PM, int C> __device__ __forceinline__ void planes_to_tmem(unsigned at, int pitch, const float (&x)[2 * C])
+{
+    float w[PM][C];
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+        unsigned u[PM];
+        split_pair<PM>(x[2 * i], x[2 * i + 1], u);
+#pragma unroll
+        for (int p = 0; p < PM; ++p) w[p][i] = __uint_as_float(u[p]);
+    }
+#pragma unroll
+    for (int p = 0; p < PM; ++p) TmemIO<C>::st(at + p * pitch, w[p]);
+}
+// 32 numbers, tokens 32 half .. of row `row` of an image
+template <int PM> __device__ __forceinline__ void planes_to_image(unsigned char *image, int pitch, int row, int half, const float (&x)[32])
+{
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        unsigned u[4][PM];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) split_pair<PM>(x[8 * c + 2 * i], x[8 * c + 2 * i + 1], u[i]);
+#pragma unroll
+        for (int p = 0; p < PM; ++p) *(uint4 *)(image + p * pitch + image_at(row, half * 4 + c)) = make_uint4(u[0][p], u[1][p], u[2][p], u[3][p]);
+    }
+}
+// the numbers of a row of an image of a tensor: its planes' sum
+template <int PI> __device__ __forceinline__ void image_row(float (&x)[32], const unsigned char *image, int pitch, int row, int half)
+{
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+#pragma unroll
+        for (int p = PI - 1; p >= 0; --p) {
+            const uint4 w = *(const uint4 *)(image + p * pitch + image_at(row, half * 4 + c));
+            const unsigned u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float lo = __uint_as_float(u[i] << 16), hi = __uint_as_float(u[i] & 0xffff0000u);
+                if (p == PI - 1) { x[8 * c + 2 * i] = lo; x[8 * c + 2 * i + 1] = hi; }
+                else { x[8 * c + 2 * i] += lo; x[8 * c + 2 * i + 1] += hi; }
+            }
+        }
+    }
+}
+
+// ---- tensors in device memory ---------------------------------------------------------------------------------------
+
+// 16 bytes from element `at` of a tensor of n elements whose rows do not start on 16 bytes: cut out of two words
+__device__ __forceinline__ uint4 load_unaligned(const bf16 *p, long long at, long long n)
+{
+    const int s = (int)(at & 7);
+    const bf16 *base = p + (at - s);
+    if (at - s + (s ? 16 : 8) > n) {                      // (the tensor's last words: element by element)
+        unsigned u[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (at + i < n) { HN_G(p + at + i, 2); u[i >> 1] |= (unsigned)__ldg((const unsigned short *)p + at + i) << (16 * (i & 1)); }
+        return make_uint4(u[0], u[1], u[2], u[3]);
+    }
+    HN_G(base, 16);
+    const uint4 a = __ldg((const uint4 *)base);
+    if (!s) return a;
+    HN_G(base + 8, 16);
+    const uint4 b = __ldg((const uint4 *)base + 1);
+    unsigned w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}, o[5];
+    const int ws = s >> 1;
+#pragma unroll
+    for (int i = 0; i < 5; ++i) o[i] = ws == 0 ? w[i] : ws == 1 ? w[i + 1] : ws == 2 ? w[i + 2] : w[i + 3];
+    const int sh = (s & 1) * 16;
+    return make_uint4(__funnelshift_r(o[0], o[1], sh), __funnelshift_r(o[1], o[2], sh), __funnelshift_r(o[2], o[3], sh), __funnelshift_r(o[3], o[4], sh));
+}
+// all but the first n (0 .. 8) of eight bf16 values replaced by zero
+__device__ __forceinline__ uint4 keep_first(uint4 w, int n)
+{
+    const unsigned half = (n & 1) ? 0xffffu : 0u;
+    const int full = n >> 1;
+    w.x = full > 0 ? w.x : full == 0 ? w.x & half : 0u;
+    w.y = full > 1 ? w.y : full == 1 ? w.y & half : 0u;
+    w.z = full > 2 ? w.z : full == 2 ? w.z & half : 0u;
+    w.w = full > 3 ? w.w : full == 3 ? w.w & half : 0u;
+    return w;
+}
+
+// A chunk's tile of a tensor as images: `rows` rows of [.][L] from element `at` (row 0, the chunk's first token), the first nv of 64
+// tokens of each, zero behind them; `threads` threads together.  Rows behind `rows` are the caller's.
+template <typename T> __device__ __forceinline__ void load_tile(unsigned char *image, int pitch, const T *p, long long at, long long n, int L, int rows, int nv, int tid, int threads)
+{
+    constexpr int V = sizeof(T) == 2 ? 4 : 2;             // vectors of eight tokens in flight
+    const bool aligned = sizeof(T) == 2 ? L % 8 == 0 : L % 4 == 0;
+    for (int i0 = tid; i0 < rows * 8; i0 += threads * V) {
+        if constexpr (sizeof(T) == 2) {
+            uint4 w[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const int i = i0 + j * threads, row = i >> 3, c = i & 7, left = nv - c * 8;
+                w[j] = make_uint4(0, 0, 0, 0);
+                if (i >= rows * 8 || left <= 0) continue;
+                const long long e = at + (long long)row * L + c * 8;
+                if (aligned) { HN_G((const bf16 *)p + e, 16); w[j] = __ldg((const uint4 *)((const bf16 *)p + e)); }
+                else w[j] = load_unaligned((const bf16 *)p, e, n);
+                if (left < 8) w[j] = keep_first(w[j], left);
+            }
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const int i = i0 + j * threads;
+                if (i < rows * 8) *(uint4 *)(image + image_at(i >> 3, i & 7)) = w[j];
+            }
+        } else {
+            float x[V][8];
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const int i = i0 + j * threads, row = i >> 3, c = i & 7, left = nv - c * 8;
+#pragma unroll
+                for (int t = 0; t < 8; ++t) x[j][t] = 0.f;
+                if (i >= rows * 8 || left <= 0) continue;
+                const long long e = at + (long long)row * L + c * 8;
+                if (aligned && left >= 8) {
+                    HN_G((const float *)p + e, 32);
+                    const float4 lo = __ldg((const float4 *)((const float *)p + e)), hi = __ldg((const float4 *)((const float *)p + e) + 1);
+                    x[j][0] = lo.x; x[j][1] = lo.y; x[j][2] = lo.z; x[j][3] = lo.w; x[j][4] = hi.x; x[j][5] = hi.y; x[j][6] = hi.z; x[j][7] = hi.w;
+                } else {
+#pragma unroll
+                    for (int t = 0; t < 8; ++t)
+                        if (t < left) x[j][t] = IO<float>::ld((const float *)p, e + t);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const int i = i0 + j * threads;
+                if (i >= rows * 8) continue;
+                unsigned u[4][3];
+#pragma unroll
+                for (int t = 0; t < 4; ++t) split_pair<3>(x[j][2 * t], x[j][2 * t + 1], u[t]);
+#pragma unroll
+                for (int q = 0; q < 3; ++q) *(uint4 *)(image + q * pitch + image_at(i >> 3, i & 7)) = make_uint4(u[0][q], u[1][q], u[2][q], u[3][q]);
+            }
+        }
+    }
+}
+// rows `from` .. `to` of an image's planes: zero
+__device__ __forceinline__ void clear_rows(unsigned char *image, int pitch, int planes, int from, int to, int tid, int threads)
+{
+    for (int p = 0; p < planes; ++p)
+        for (int i = from * 8 + tid; i < to * 8; i += threads) *(uint4 *)(image + p * pitch + i * 16) = make_uint4(0, 0, 0, 0);
+}
+
+// 32 tokens of one row in registers, as they lie; zero behind the first nv
+template <typename T> struct RowPart;
+template <> struct RowPart<bf16> {
+    uint4 w[4];
+    __device__ __forceinline__ void load(const bf16 *p, long long at, long long n, int L, int nv)
+    {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            w[c] = make_uint4(0, 0, 0, 0);
+            const int left = nv - 8 * c;
+            if (left <= 0) continue;
+            if (L % 8 == 0) { HN_G(p + at + 8 * c, 16); w[c] = __ldg((const uint4 *)(p + at + 8 * c)); }
+            else w[c] = load_unaligned(p, at + 8 * c, n);
+            if (left < 8) w[c] = keep_first(w[c], left);
+        }
+    }
+    __device__ __forceinline__ float get(int i) const
+    {
+        const unsigned u = (i >> 1 & 3) == 0 ? w[i >> 3].x : (i >> 1 & 3) == 1 ? w[i >> 3].y : (i >> 1 & 3) == 2 ? w[i >> 3].z : w[i >> 3].w;
+        return __uint_as_float(i & 1 ? u & 0xffff0000u : u << 16);
+    }
+};
+template <> struct RowPart<float> {
+    float x[32];
+    __device__ __forceinline__ void load(const float *p, long long at, long long, int L, int nv)
+    {
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+            if (L % 4 == 0 && nv >= 4 * c + 4) {
+                HN_G(p + at + 4 * c, 16);
+                const float4 w = __ldg((const float4 *)(p + at) + c);
+                x[4 * c] = w.x; x[4 * c + 1] = w.y; x[4 * c + 2] = w.z; x[4 * c + 3] = w.w;
+            } else {
+#pragma unroll
+                for (int i = 4 * c; i < 4 * c + 4; ++i) x[i] = i < nv ? IO<float>::ld(p, at + i) : 0.f;
+            }
+        }
+    }
+    __device__ __forceinline__ float get(int i) const { return x[i]; }
+};
+// the first `room` of 32 tokens of one row; from token nv on they are zero
+template <typename T> __device__ __forceinline__ void store_row(T *p, long long at, int L, int room, int nv, const float (&x)[32])
+{
+    constexpr int V = 16 / sizeof(T);
+    if (L % V == 0) {
+#pragma unroll
+        for (int c = 0; c < 32 / V; ++c) {
+            if (c * V >= room) break;
+            uint4 w;
+            T *e = (T *)&w;
+#pragma unroll
+            for (int i = 0; i < V; ++i) e[i] = (T)(c * V + i < nv ? x[c * V + i] : 0.f);
+            HN_G(p + at + c * V, 16);
+            *(uint4 *)(p + at + c * V) = w;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+            if (i < room) IO<T>::st(p, at + i, i < nv ? x[i] : 0.f);
+    }
+}
+// this thread's C columns from `col` of row `row` of a state [rows][D], zero outside it
+template <int C> __device__ __forceinline__ void load_state(float (&s)[C], const float *p, int row, int rows, int col, int D)
+{
+    if (row < rows && D % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < C; i += 4) {
+            float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (col + i < D) { HN_G(p + (long long)row * D + col + i, 16); w = *(const float4 *)(p + (long long)row * D + col + i); }
+            s[i] = w.x; s[i + 1] = w.y; s[i + 2] = w.z; s[i + 3] = w.w;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            s[i] = 0.f;
+            if (row < rows && col + i < D) { HN_G(p + (long long)row * D + col + i, 4); s[i] = p[(long long)row * D + col + i]; }
+        }
+    }
+}
+template <int C> __device__ __forceinline__ void store_state(float *p, const float (&s)[C], int row, int rows, int col, int D)
+{
+    if (row >= rows) return;
+    if (D % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < C; i += 4)
+            if (col + i < D) { HN_G(p + (long long)row * D + col + i, 16); *(float4 *)(p + (long long)row * D + col + i) = make_float4(s[i], s[i + 1], s[i + 2], s[i + 3]); }
+    } else {
+#pragma unroll
+        for (int i = 0; i < C; ++i)
+            if (col + i < D) { HN_G(p + (long long)row * D + col + i, 4); p[(long long)row * D + col + i] = s[i]; }
+    }
+}
+
+// ---- a chunk's decays ---------------------------------------------------------------------------------------------------
+
+// log a.  Below -110 the factor is zero in fp32: the sum of a chunk stays small enough for differences.  A NaN stays one.
+__device__ __forceinline__ float log_decay(float g, int decay)
+{
+    if (decay == DELTA_NONE) return 0.f;
+    float x = g;
+    if (decay == DELTA_SIGMOID) x = g >= 0.f ? -log1pf(expf(-g)) : g - log1pf(expf(g));
+    return x < -110.f ? -110.f : x;
+}
+// G of a chunk's 64 tokens, by one warp, in 64 bits (differences of neighbours beside a sum of many); tokens from nv on decay nothing
+__device__ __forceinline__ void chunk_sums(double *G, const float *g, int decay, int nv, int lane)
+{
+    double x[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int t = 2 * lane + i;
+        x[i] = 0.;
+        if (decay != DELTA_NONE && t < nv) { HN_G(g + t, 4); x[i] = log_decay(__ldg(g + t), decay); }
+    }
+    double s = x[0] + x[1];
+#pragma unroll
+    for (int m = 1; m < 32; m <<= 1) {
+        const double o = __shfl_up_sync(~0u, s, m);
+        if (lane >= m) s += o;
+    }
+    G[2 * lane] = s - x[1];
+    G[2 * lane + 1] = s;
+}
+
+// ---- products ------------------------------------------------------------------------------------------------------------
+
+// d (+)= sum of the products of planes p of A (tensor memory, `pa` columns apart) and q of B (images, `pb` bytes apart), p < NA, q < NB,
+// p + q < MAX, over `steps` 16-steps; the smallest first (the sums are cut off, not rounded, at every instruction)
+template <int NA, int NB, int MAX, bool BCOLS> __device__ __forceinline__ void issue_ts(unsigned d, unsigned a, int pa, unsigned b, int pb, int steps, int n, bool add)
+{
+    const unsigned kind = umma_kind(n, false, BCOLS);
+#pragma unroll
+    for (int sum = MAX - 1; sum >= 0; --sum)
+#pragma unroll
+        for (int p = 0; p <= sum; ++p)
+            if (const int q = sum - p; p < NA && q < NB)
+                for (int k = 0; k < steps; ++k) {
+                    umma_ts(d, a + p * pa + k * 8, BCOLS ? umma_cols(b + q * pb, k) : umma_rows(b + q * pb, k), kind, add);
+                    add = true;
+                }
+}
+// the same with A in images; `next`: see umma_cols
+template <int NA, int NB, int MAX, bool ACOLS, bool BCOLS> __device__ __forceinline__ void issue_ss(unsigned d, unsigned a, int pa, unsigned next, unsigned b, int pb, int steps, int n, bool add)
+{
+    const unsigned kind = umma_kind(n, ACOLS, BCOLS);
+#pragma unroll
+    for (int sum = MAX - 1; sum >= 0; --sum)
+#pragma unroll
+        for (int p = 0; p <= sum; ++p)
+            if (const int q = sum - p; p < NA && q < NB)
+                for (int k = 0; k < steps; ++k) {
+                    umma_ss(d, ACOLS ? umma_cols(a + p * pa, k, next) : umma_rows(a + p * pa, k), BCOLS ? umma_cols(b + q * pb, k) : umma_rows(b + q * pb, k), kind, add);
+                    add = true;
+                }
+}
+
+// ---- walks -----------------------------------------------------------------------------------------------------------
+
+// What the warps of a walk share beside the stages.  A wait that gives up ends all later ones of the CTA.
+struct WalkShared {
+    uint64_t full[4], empty[4], bar_a, bar_b, bar_c, bar_q, bar_y;
+    unsigned slot;
+    int gave_up;
+};
+__device__ __forceinline__ void walk_wait(WalkShared *w, uint64_t *bar, unsigned parity, int *status)
+{
+    volatile int *f = &w->gave_up;
+    if (*f) return;
+    if (!mbar_wait(bar, parity)) { *f = 1; atomicExch(status, 1); }
+}
+__device__ __forceinline__ void mbar_arrive(uint64_t *bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];\n" ::"r"(smem_u32(bar)) : "memory"); }
+__device__ __forceinline__ void walkers_sync() { asm volatile("bar.sync 1, 256;\n" ::: "memory"); }
+
+__device__ __forceinline__ unsigned char *align_images(unsigned char *p) { return p + ((1024u - (smem_u32(p) & 1023u)) & 1023u); }
+
+enum { WALK_RUN = 0, WALK_MAPS = 1 };
+
+// ---- host ------------------------------------------------------------------------------------------------------------
+
+struct DeltaSizes { size_t images, gates, maps, starts, dstates, dz, all; };          // bytes of the parts of a workspace, in this order
+DeltaSizes delta_sizes(const DeltaArgs &a, int dtype, bool backward);
+int launch_delta_prepare(const DeltaArgs &a, int dtype, cudaStream_t st);
+int launch_delta_join(const DeltaArgs &a, const float *from, bool backward, cudaStream_t st);
+int launch_delta_backward(const DeltaArgs &a, int dtype, cudaStream_t st);
+int delta_backward_status();
+
+template <auto FN> static int launch_delta(const DeltaArgs &a, long long blocks, unsigned threads, int bytes, cudaStream_t st)
+{
+    if (blocks > 0x7fffffffll) return kTooLarge;
+    static PerDevice ready;
+    if (bytes > 48 * 1024 - 4096 && !ready.once([&] { return cudaFuncSetAttribute(FN, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess ? 1 : -1; })) return kNoLaunch;
+    launch_pdl(FN, dim3((unsigned)blocks), threads, bytes, st, a);
+    return 0;
+}
+
+}  // namespace hn

@@ -1,0 +1,593 @@
+// The gated delta rule: gradients, in chunks (formulas and number formats in delta.cuh).
+//
+// prepare: as in the forward pass.
+// walk: from the last chunk to the first, a CTA per head: the gradient of the state.  As in the forward walk its rows are the lanes of
+//     tensor memory and every product takes the one before as its operand there: dS k, then A^T dU, then the new dS.  It writes dV, dZ
+//     and the gradient behind every chunk.  Few heads and many chunks go in segments as there (dS0 = dS1 Phi + N).
+// gradients: a CTA per chunk and head of queries and keys, all at once: from the state before the chunk (the forward's mark) and the gradient
+//     behind it, U again, then dQ, dK, and the sums over tokens for beta and the decay.  Value heads that share queries and keys follow
+//     one another in the CTA, so their sum has one order and needs no atomics.
+#include "delta.cuh"
+
+namespace hn {
+
+static __device__ int hn_delta_backward_status;
+#define WAIT(bar, parity) walk_wait(&ws, bar, parity, &hn_delta_backward_status)
+
+// ---- walk -----------------------------------------------------------------------------------------------------------
+
+template <typename T, int KD> struct WalkBack {
+    static constexpr int PI = Planes<T>::IN, PM = Planes<T>::MID, TILE = KD * 128, TENSOR = PI * TILE;
+    static constexpr int IMAGES = 2 * PM * kMatrix;
+    static constexpr int STAGE = 3 * TENSOR + IMAGES + 1024;                  // K, Q, dY, A, P, gates
+    static constexpr int STAGES = 3 * STAGE <= 220 * 1024 ? 3 : 2 * STAGE <= 220 * 1024 ? 2 : 1;
+    // (the product of dY and P takes 128 rows of dY's image: with 64 it reads on into the images that follow, for rows nothing looks at)
+    static constexpr int BYTES = 1024 + STAGES * STAGE;
+    // tensor memory: dS, later gamma dY, as operands | dU, later -gamma beta dZ | sums | P^T dY
+    static constexpr int SCOLS = PM * KD / 2 > PM * kTok / 2 ? PM * KD / 2 : PM * kTok / 2, ZCOLS = PM * kTok / 2, S0 = 0, Z0 = SCOLS, X0 = Z0 + ZCOLS,
+                         Y0 = X0 + (KD > kTok ? KD : kTok);
+    static_assert(Y0 + kTok <= 512 && BYTES <= 227 * 1024, "tensor and shared memory");
+};
+
+template <typename T, int KD, int MODE> __global__ void __launch_bounds__(384, 1) delta_walk_back_kernel(DeltaArgs a)
+{
+    using C = WalkBack<T, KD>;
+    constexpr int PI = C::PI, PM = C::PM, HC = KD / 2;
+    extern __shared__ __align__(1024) unsigned char raw[];
+    __shared__ WalkShared ws;
+    unsigned char *sm = align_images(raw);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    long long id = blockIdx.x;
+    const bool phi = MODE == WALK_MAPS && (id & 1);          // from the identity, without dY
+    if (MODE == WALK_MAPS) id >>= 1;
+    const long long bh = id / a.segments;
+    const int segment = (int)(id % a.segments), b = (int)(bh / a.H), h = (int)(bh % a.H);
+    pdl_wait();
+    const int n = live_tokens(a, b), first = segment * a.per_segment, end = first + a.per_segment < a.chunks ? first + a.per_segment : a.chunks;
+    int last = (n + kTok - 1) / kTok;                        // chunks last - 1 .. first hold tokens
+    last = last < end ? last : end;
+    const int count = last > first ? last - first : 0;
+    if (warp == 0) tmem_alloc(smem_u32(&ws.slot), 512);
+    if (tid == 0) {
+        for (int s = 0; s < C::STAGES; ++s) { mbar_init(&ws.full[s], 129); mbar_init(&ws.empty[s], 1); }
+        mbar_init(&ws.bar_a, 1); mbar_init(&ws.bar_b, 1); mbar_init(&ws.bar_c, 1); mbar_init(&ws.bar_q, 1); mbar_init(&ws.bar_y, 1);
+        ws.gave_up = 0;
+        fence_mbar_init();
+    }
+    for (int s = 0; s < C::STAGES; ++s) {
+        clear_rows(sm + s * C::STAGE, C::TILE, 2 * PI, a.Dk, KD, tid, 384);
+        clear_rows(sm + s * C::STAGE + 2 * C::TENSOR, C::TILE, PI, phi ? 0 : a.Dv, KD, tid, 384);
+    }
+    fence_async_smem();
+    tmem_fence_before_sync();
+    __syncthreads();
+    tmem_fence_after_sync();
+    const unsigned tb = ws.slot;
+    const int steps = (a.Dk + 15) / 16;
+    const long long vhead = bh * a.Dv * a.L, vall = (long long)a.B * a.H * a.Dv * a.L;
+    if (warp >= 8) {
+        const int ft = tid - 256;
+        const long long qk = ((long long)b * a.Hk + h / (a.H / a.Hk)) * a.Dk * a.L, all = (long long)a.B * a.Hk * a.Dk * a.L;
+        for (int i = 0; i < count; ++i) {
+            const int c = last - 1 - i, s = i % C::STAGES, t0 = c * kTok, nv = n - t0 < kTok ? n - t0 : kTok;
+            if (i >= C::STAGES) WAIT(&ws.empty[s], (i / C::STAGES - 1) & 1);
+            unsigned char *st = sm + s * C::STAGE;
+            if (ft == 0) {
+                const long long at = bh * a.chunks + c;
+                mbar_expect_tx(&ws.full[s], C::IMAGES + 3 * kTok * 4);
+                bulk_load(st + 3 * C::TENSOR, a.images + at * C::IMAGES, C::IMAGES, &ws.full[s]);
+                bulk_load(st + 3 * C::TENSOR + C::IMAGES, a.gates + at * (4 * kTok), 3 * kTok * 4, &ws.full[s]);
+            }
+            load_tile<T>(st, C::TILE, (const T *)a.k, qk + t0, all, a.L, a.Dk, nv, ft, 128);
+            load_tile<T>(st + C::TENSOR, C::TILE, (const T *)a.q, qk + t0, all, a.L, a.Dk, nv, ft, 128);
+            if (!phi) load_tile<T>(st + 2 * C::TENSOR, C::TILE, (const T *)a.dy, vhead + t0, vall, a.L, a.Dv, nv, ft, 128);
+            fence_async_smem();
+            mbar_arrive(&ws.full[s]);
+        }
+    } else {
+        const int row = 32 * (warp & 3) + lane, half = warp >> 2, rows = phi ? a.Dk : a.Dv;
+        const unsigned lane_s = tmem_addr(tb, warp, C::S0 + half * (HC / 2)), lane_g = tmem_addr(tb, warp, C::S0 + half * 16),
+                       lane_z = tmem_addr(tb, warp, C::Z0 + half * 16), lane_x = tmem_addr(tb, warp, C::X0), lane_y = tmem_addr(tb, warp, C::Y0 + half * 32);
+        const long long vrow = vhead + (long long)row * a.L, states = (long long)a.Dv * a.Dk;
+        const bool real = row < a.Dv;
+        float S[HC];
+#pragma unroll
+        for (int i = 0; i < HC; ++i) S[i] = 0.f;
+        if (MODE == WALK_MAPS) {
+            if (phi) {
+#pragma unroll
+                for (int i = 0; i < HC; ++i) S[i] = row == half * HC + i && row < a.Dk ? 1.f : 0.f;
+            }
+        } else {
+            const float *from = a.segments > 1 ? a.starts + (bh * a.segments + segment) * states : a.ds_end ? a.ds_end + bh * states : nullptr;
+            if (from) load_state<HC>(S, from, row, a.Dv, half * HC, a.Dk);
+        }
+        for (int i = 0; i < count; ++i) {
+            const int c = last - 1 - i, s = i % C::STAGES, t = c * kTok + 32 * half;
+            const unsigned par = i & 1;
+            unsigned char *st = sm + s * C::STAGE;
+            const unsigned k = smem_u32(st), q = k + C::TENSOR, g = q + C::TENSOR, A = g + C::TENSOR, P = A + PM * kMatrix;
+            const float *gates = (const float *)(st + 3 * C::TENSOR + C::IMAGES);
+            if (MODE != WALK_MAPS) store_state<HC>(a.dstates + (bh * a.chunks + c) * states, S, row, a.Dv, half * HC, a.Dk);
+            planes_to_tmem<PM, HC / 2>(lane_s, KD / 2, S);
+            tmem_wait_st();
+            tmem_fence_before_sync();
+            WAIT(&ws.full[s], (i / C::STAGES) & 1);
+            walkers_sync();
+            if (tid == 0) {
+                tmem_fence_after_sync();
+                issue_ts<PM, PI, PM, true>(tb + C::X0, tb + C::S0, KD / 2, k, C::TILE, steps, kTok, false);
+                issue_ss<PI, PM, PM, false, true>(tb + C::Y0, g, C::TILE, 0, P, kMatrix, kTok / 16, kTok, false);
+                umma_commit(&ws.bar_a);
+            }
+            __syncwarp();
+            float x[32];
+            WAIT(&ws.bar_a, par);
+            tmem_fence_after_sync();
+            {
+                float y[32];
+                TmemIO<32>::ld(x, lane_x + 32 * half);
+                TmemIO<32>::ld(y, lane_y);
+                tmem_wait_ld();
+#pragma unroll
+                for (int e = 0; e < 32; e += 4) {
+                    const float4 de = *(const float4 *)(gates + kTok + 32 * half + e);
+                    const float d[4] = {de.x, de.y, de.z, de.w};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[e + j] = row < rows ? fmaf(d[j], x[e + j], phi ? 0.f : y[e + j]) : 0.f;
+                }
+            }
+            planes_to_tmem<PM, 16>(lane_z, kTok / 2, x);
+            tmem_wait_st();
+            tmem_fence_before_sync();
+            walkers_sync();
+            if (tid == 0) {
+                tmem_fence_after_sync();
+                issue_ts<PM, PM, PM, true>(tb + C::X0, tb + C::Z0, kTok / 2, A, kMatrix, kTok / 16, kTok, false);
+                umma_commit(&ws.bar_b);
+            }
+            __syncwarp();
+            // gamma dY, in the state's place, meanwhile
+            if (row < KD) image_row<PI>(x, st + 2 * C::TENSOR, C::TILE, row, half);
+            else {
+#pragma unroll
+                for (int e = 0; e < 32; ++e) x[e] = 0.f;
+            }
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) {
+                const float4 ga = *(const float4 *)(gates + 32 * half + e);
+                x[e] *= ga.x; x[e + 1] *= ga.y; x[e + 2] *= ga.z; x[e + 3] *= ga.w;
+            }
+            planes_to_tmem<PM, 16>(lane_g, kTok / 2, x);
+            WAIT(&ws.bar_b, par);
+            tmem_fence_after_sync();
+            TmemIO<32>::ld(x, lane_x + 32 * half);
+            tmem_wait_ld();
+            if (MODE != WALK_MAPS && real) {
+                float *to = a.dz + ((bh * a.chunks + c) * a.Dv + row) * kTok + 32 * half;
+#pragma unroll
+                for (int e = 0; e < 32; e += 4) { HN_G(to + e, 16); *(float4 *)(to + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]); }
+            }
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) {
+                const float4 be = *(const float4 *)(gates + 2 * kTok + 32 * half + e);
+                x[e] *= be.x; x[e + 1] *= be.y; x[e + 2] *= be.z; x[e + 3] *= be.w;
+            }
+            if (MODE != WALK_MAPS && real && t < a.L) store_row<T>((T *)a.dv, vrow + t, a.L, a.L - t, n - t, x);
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) {
+                const float4 ga = *(const float4 *)(gates + 32 * half + e);
+                x[e] *= -ga.x; x[e + 1] *= -ga.y; x[e + 2] *= -ga.z; x[e + 3] *= -ga.w;
+            }
+            planes_to_tmem<PM, 16>(lane_z, kTok / 2, x);
+            const float fade = gates[kTok - 1];
+            tmem_wait_st();
+            tmem_fence_before_sync();
+            walkers_sync();
+            if (tid == 0) {
+                tmem_fence_after_sync();
+                issue_ts<PM, PI, PM, false>(tb + C::X0, tb + C::S0, kTok / 2, q, C::TILE, kTok / 16, KD, false);
+                issue_ts<PM, PI, PM, false>(tb + C::X0, tb + C::Z0, kTok / 2, k, C::TILE, kTok / 16, KD, true);
+                umma_commit(&ws.bar_c);
+                umma_commit(&ws.empty[s]);
+            }
+            __syncwarp();
+            WAIT(&ws.bar_c, par);
+            tmem_fence_after_sync();
+#pragma unroll
+            for (int e = 0; e < HC; e += 32) {
+                TmemIO<32>::ld(x, lane_x + half * HC + e);
+                tmem_wait_ld();
+#pragma unroll
+                for (int j = 0; j < 32; ++j) S[e + j] = fmaf(fade, S[e + j], x[j]);
+            }
+        }
+        if (MODE == WALK_MAPS) {
+            float *to = a.maps + (bh * a.segments + segment) * (long long)(a.Dv + a.Dk) * a.Dk + (phi ? states : 0);
+            store_state<HC>(to, S, row, rows, half * HC, a.Dk);
+        } else {
+            float none[32];
+#pragma unroll
+            for (int e = 0; e < 32; ++e) none[e] = 0.f;
+            for (int c = first > last ? first : last; c < end; ++c) {
+                const int t = c * kTok + 32 * half;
+                if (real && t < a.L) store_row<T>((T *)a.dv, vrow + t, a.L, a.L - t, 0, none);
+            }
+            if (a.ds0 && segment == 0) store_state<HC>(a.ds0 + bh * states, S, row, a.Dv, half * HC, a.Dk);
+        }
+        tmem_fence_before_sync();
+    }
+    __syncthreads();
+    if (ws.gave_up && tid == 0)                              // copies on their way end before the memory they go to is another CTA's
+        for (int s = 0; s < C::STAGES; ++s) mbar_wait(&ws.full[s], 0);
+    if (warp == 0) tmem_dealloc(tb, 512);
+}
+
+// ---- gradients ------------------------------------------------------------------------------------------------------
+
+template <typename T, int KD> struct Grads {
+    static constexpr int PI = Planes<T>::IN, PM = Planes<T>::MID, TILE = KD * 128;
+    // images: dY (later Q) | K | U | dZ (later E) | A (later F)
+    static constexpr int DY = 0, K = PI * TILE, U = K + PI * TILE, DZ = U + PM * TILE, A = DZ + PM * TILE, END = A + PM * kMatrix, BYTES = 1024 + END;
+    // tensor memory: a state as an operand | six sums of 64 columns, Z as an operand in the second and third
+    static constexpr int S0 = 0, SCOLS = PM * KD / 2, R0 = SCOLS;
+    static constexpr int SUMS = Planes<T>::IN < Planes<T>::MID ? 6 : 5;
+    static_assert(R0 + SUMS * kTok <= 512 && BYTES + 4096 <= 227 * 1024 && PM * kTok / 2 <= 2 * kTok && PM * TILE >= PM * kMatrix, "tensor and shared memory");
+};
+
+// x[c] summed over the warp's lanes; lane l is left with column l
+__device__ __forceinline__ float column_sum(float (&x)[32], int lane)
+{
+#pragma unroll
+    for (int m = 16; m; m >>= 1) {
+        const bool up = lane & m;
+#pragma unroll
+        for (int c = 0; c < m; ++c) {
+            const float give = up ? x[c] : x[c + m], keep = up ? x[c + m] : x[c];
+            x[c] = keep + __shfl_xor_sync(~0u, give, m);
+        }
+    }
+    return x[0];
+}
+
+template <typename T, int KD> __global__ void __launch_bounds__(256, 1) delta_gradients_kernel(DeltaArgs a)
+{
+    using C = Grads<T, KD>;
+    constexpr int PI = C::PI, PM = C::PM, HC = KD / 2;
+    extern __shared__ __align__(1024) unsigned char raw[];
+    __shared__ WalkShared ws;
+    __shared__ double G[kTok];
+    __shared__ float beta[kTok], sums[3][4][kTok], erased[2][kTok], total[8];
+    unsigned char *sm = align_images(raw);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, row = 32 * (warp & 3) + lane, half = warp >> 2, share = a.H / a.Hk;
+    const long long bk = blockIdx.x / a.chunks;
+    const int chunk = (int)(blockIdx.x % a.chunks), b = (int)(bk / a.Hk), hk = (int)(bk % a.Hk), t0 = chunk * kTok, t = t0 + 32 * half;
+    pdl_wait();
+    const int n = live_tokens(a, b), nv = n - t0 < kTok ? n - t0 : kTok, room = a.L - t0 < kTok ? a.L - t0 : kTok;
+    const long long qrow = (bk * a.Dk + row) * a.L + t, qk = bk * a.Dk * a.L + t0, all = (long long)a.B * a.Hk * a.Dk * a.L, vall = (long long)a.B * a.H * a.Dv * a.L;
+    const long long states = (long long)a.Dv * a.Dk;
+    float dq[32], dk[32];
+#pragma unroll
+    for (int e = 0; e < 32; ++e) dq[e] = dk[e] = 0.f;
+    if (nv <= 0) {                                           // nothing of this chunk counts
+        if (row < a.Dk && t < a.L) {
+            store_row<T>((T *)a.dq, qrow, a.L, a.L - t, 0, dq);
+            store_row<T>((T *)a.dk, qrow, a.L, a.L - t, 0, dk);
+        }
+        for (int i = tid; i < share * room; i += 256) {
+            const long long at = (((long long)b * a.H + hk * share + i / room) * a.L) + t0 + i % room;
+            HN_G(a.dbeta + at, 4);
+            a.dbeta[at] = 0.f;
+            if (a.dg) { HN_G(a.dg + at, 4); a.dg[at] = 0.f; }
+        }
+        return;
+    }
+    if (warp == 0) tmem_alloc(smem_u32(&ws.slot), 512);
+    if (tid == 0) { mbar_init(&ws.bar_a, 1); ws.gave_up = 0; fence_mbar_init(); }
+    const int ksteps = (a.Dk + 15) / 16, vsteps = (a.Dv + 15) / 16;
+    load_tile<T>(sm + C::K, C::TILE, (const T *)a.k, qk, all, a.L, a.Dk, nv, tid, 256);
+    clear_rows(sm + C::K, C::TILE, PI, a.Dk, KD, tid, 256);
+    const unsigned images = smem_u32(sm), IK = images + C::K, IU = images + C::U, IZ = images + C::DZ, IA = images + C::A, IY = images + C::DY;
+    unsigned par = 0, tb = 0;
+    float x[32], y[32], erase[32];
+    auto go = [&] {                                          // what the threads wrote, for the products
+        tmem_wait_st();
+        fence_async_smem();
+        tmem_fence_before_sync();
+        __syncthreads();
+        tmem_fence_after_sync();
+    };
+    auto done = [&] {
+        __syncwarp();
+        WAIT(&ws.bar_a, par);
+        par ^= 1;
+        tmem_fence_after_sync();
+    };
+    for (int j = 0; j < share; ++j) {
+        const long long bh = (long long)b * a.H + hk * share + j, at = bh * a.chunks + chunk, grow = bh * a.L + t0;
+        const float *S = a.marks + at * states, *D = a.dstates + at * states;
+        if (j) __syncthreads();                              // the images and sums of the head before have been read
+        load_tile<T>(sm + C::DY, C::TILE, (const T *)a.dy, bh * a.Dv * a.L + t0, vall, a.L, a.Dv, nv, tid, 256);
+        clear_rows(sm + C::DY, C::TILE, PI, a.Dv, KD, tid, 256);
+        {
+            const uint4 *from = (const uint4 *)(a.images + at * (2 * PM * kMatrix));
+            for (int e = tid; e < PM * kMatrix / 16; e += 256) { HN_G(from + e, 16); ((uint4 *)(sm + C::A))[e] = __ldg(from + e); }
+        }
+        if (warp == 0) chunk_sums(G, a.g + grow, a.decay, nv, lane);
+        if (warp == 1 || warp == 2) {
+            const int i = tid - 32;
+            beta[i] = 0.f;
+            if (i < nv) { HN_G(a.beta + grow + i, 4); beta[i] = __ldg(a.beta + grow + i); }
+        }
+        float dz[32];
+        if (row < a.Dv) {
+            const float *from = a.dz + (at * a.Dv + row) * kTok + 32 * half;
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) {
+                HN_G(from + e, 16);
+                const float4 w = *(const float4 *)(from + e);
+                dz[e] = w.x; dz[e + 1] = w.y; dz[e + 2] = w.z; dz[e + 3] = w.w;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) dz[e] = 0.f;
+        }
+        if (row < KD) planes_to_image<PM>(sm + C::DZ, C::TILE, row, half, dz);
+        tmem_fence_before_sync();
+        __syncthreads();                                     // (tensor memory and its barrier are there)
+        tmem_fence_after_sync();
+        tb = ws.slot;
+        const unsigned lane_s = tmem_addr(tb, warp, C::S0 + half * (HC / 2)), lane_r = tmem_addr(tb, warp, C::R0 + half * 32);
+        const float fade = expf((float)G[kTok - 1]);
+        {   // the state before the chunk, its rows as lanes: S0 k
+            float s[HC];
+            load_state<HC>(s, S, row, a.Dv, half * HC, a.Dk);
+            planes_to_tmem<PM, HC / 2>(lane_s, KD / 2, s);
+        }
+        go();
+        if (tid == 0) {
+            issue_ts<PM, PI, PM, true>(tb + C::R0, tb + C::S0, KD / 2, IK, C::TILE, ksteps, kTok, false);
+            umma_commit(&ws.bar_a);
+        }
+        RowPart<T> v;
+        v.load((const T *)a.v, (bh * a.Dv + row) * a.L + t, vall, a.L, row < a.Dv ? n - t : 0);
+        done();
+        TmemIO<32>::ld(x, lane_r);
+        tmem_wait_ld();
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+            const int i = 32 * half + e;
+            x[e] = fmaf(-expf((float)G[i]), x[e], v.get(e));                // R
+            y[e] = dz[e] * x[e];
+            x[e] *= beta[i];
+        }
+        sums[0][warp & 3][32 * half + lane] = column_sum(y, lane);
+        planes_to_tmem<PM, 16>(tmem_addr(tb, warp, C::R0 + kTok + half * 16), kTok / 2, x);
+        go();
+        if (tid == 0) {
+            issue_ts<PM, PM, PM, false>(tb + C::R0, tb + C::R0 + kTok, kTok / 2, IA, kMatrix, kTok / 16, kTok, false);
+            umma_commit(&ws.bar_a);
+        }
+        // the same state, its columns as lanes
+        auto columns = [&](const float *p) {
+            float s[32];
+#pragma unroll
+            for (int c = 0; c < HC; c += 32) {
+#pragma unroll
+                for (int e = 0; e < 32; ++e) {
+                    const int r = half * HC + c + e;
+                    s[e] = 0.f;
+                    if (r < a.Dv && row < a.Dk) { HN_G(p + (long long)r * a.Dk + row, 4); s[e] = p[(long long)r * a.Dk + row]; }
+                }
+                planes_to_tmem<PM, 16>(lane_s + c / 2, KD / 2, s);
+            }
+        };
+        columns(S);
+        done();
+        TmemIO<32>::ld(x, lane_r);
+        tmem_wait_ld();
+        if (row < KD) planes_to_image<PM>(sm + C::U, C::TILE, row, half, x);
+        go();
+        if (tid == 0) {
+            // rows 0 .. 63: dY U^T, rows 64 ..: dZ U^T; where dY is one plane, dZ's second goes into a sum of its own
+            issue_ss<PI, PM, PM, true, true>(tb + C::R0 + kTok, IY, C::TILE, C::DZ - C::DY, IU, C::TILE, vsteps, kTok, false);
+            if (PI < PM) issue_ss<1, 1, PM, true, true>(tb + C::R0 + 5 * kTok, IY + C::TILE, C::TILE, C::DZ - C::DY, IU, C::TILE, vsteps, kTok, false);
+            // rows 64 ..: K K^T
+            issue_ss<PI, PI, PI, true, true>(tb + C::R0 + 2 * kTok, IY, C::TILE, C::K - C::DY, IK, C::TILE, ksteps, kTok, false);
+            issue_ts<PM, PI, PM, true>(tb + C::R0, tb + C::S0, KD / 2, IY, C::TILE, vsteps, kTok, false);
+            issue_ts<PM, PM, PM, true>(tb + C::R0 + 3 * kTok, tb + C::S0, KD / 2, IZ, C::TILE, vsteps, kTok, false);
+            umma_commit(&ws.bar_a);
+        }
+        done();
+        __syncthreads();                                     // every thread's wait is over: A and dZ may go
+        {
+            const int i = row & 63;
+            const double Gi = G[i];
+            TmemIO<32>::ld(x, lane_r + kTok);
+            TmemIO<32>::ld(y, lane_r + 2 * kTok);
+            tmem_wait_ld();
+            if (PI < PM && row >= kTok) {
+                float z[32];
+                TmemIO<32>::ld(z, lane_r + 5 * kTok);
+                tmem_wait_ld();
+#pragma unroll
+                for (int e = 0; e < 32; ++e) x[e] += z[e];
+            }
+            float own = 0.f;
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+                const int c = 32 * half + e;
+                const float r = expf((float)(Gi - G[c]));
+                if (row < kTok) x[e] = c <= i ? r * x[e] : 0.f;
+                else {
+                    own += c < i ? x[e] * r * y[e] : 0.f;
+                    x[e] = c < i ? -beta[i] * r * x[e] : 0.f;
+                }
+            }
+            if (row < kTok) planes_to_image<PM>(sm + C::A, kMatrix, i, half, x);                // F
+            else {
+                planes_to_image<PM>(sm + C::DZ, kMatrix, i, half, x);                           // E
+                erased[half][i] = own;
+            }
+        }
+        TmemIO<32>::ld(x, lane_r);
+        TmemIO<32>::ld(erase, lane_r + 3 * kTok);
+        tmem_wait_ld();
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+            const float ga = expf((float)G[32 * half + e]);
+            x[e] *= ga;
+            erase[e] *= -ga * beta[32 * half + e];
+        }
+        go();
+        if (tid == 0) {
+            issue_ss<PI, PM, PM, false, false>(tb + C::R0 + kTok, IK, C::TILE, 0, IA, kMatrix, kTok / 16, kTok, false);         // F k
+            issue_ss<PI, PM, PM, false, false>(tb + C::R0 + 2 * kTok, IK, C::TILE, 0, IZ, kMatrix, kTok / 16, kTok, false);     // E k
+            umma_commit(&ws.bar_a);
+        }
+        done();
+        // queries take dY's place, the gradient behind the chunk the state's
+        load_tile<T>(sm + C::DY, C::TILE, (const T *)a.q, qk, all, a.L, a.Dk, nv, tid, 256);
+        clear_rows(sm + C::DY, C::TILE, PI, a.Dk, KD, tid, 256);
+        columns(D);
+        float inner = 0.f;                                   // <S0, dS1>
+        for (long long e = tid; e < states; e += 256) { HN_G(S + e, 4); HN_G(D + e, 4); inner = fmaf(S[e], D[e], inner); }
+#pragma unroll
+        for (int m = 1; m < 32; m <<= 1) inner += __shfl_xor_sync(~0u, inner, m);
+        if (lane == 0) total[warp] = inner;
+        TmemIO<32>::ld(y, lane_r + kTok);
+        tmem_wait_ld();
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+            x[e] += y[e];                                    // dQ of this head
+            dq[e] += x[e];
+        }
+        TmemIO<32>::ld(y, lane_r + 2 * kTok);
+        tmem_wait_ld();
+#pragma unroll
+        for (int e = 0; e < 32; ++e) erase[e] += y[e];
+        go();
+        if (tid == 0) {
+            issue_ts<PM, PM, PM, true>(tb + C::R0, tb + C::S0, KD / 2, IU, C::TILE, vsteps, kTok, false);                       // dS1 u
+            issue_ss<PI, PM, PM, false, true>(tb + C::R0 + kTok, IY, C::TILE, 0, IA, kMatrix, kTok / 16, kTok, false);          // F q
+            issue_ss<PI, PM, PM, false, true>(tb + C::R0 + kTok, IK, C::TILE, 0, IZ, kMatrix, kTok / 16, kTok, true);           // E k, the other way
+            umma_commit(&ws.bar_a);
+        }
+        {   // what queries and the erased part say about the decays, meanwhile
+            float z[32];
+            if (row < KD) image_row<PI>(z, sm + C::DY, C::TILE, row, half);
+            else {
+#pragma unroll
+                for (int e = 0; e < 32; ++e) z[e] = 0.f;
+            }
+#pragma unroll
+            for (int e = 0; e < 32; ++e) x[e] = row < a.Dk ? x[e] * z[e] : 0.f;      // (a lane without a channel holds whatever lay behind an image)
+        }
+        done();
+        {
+            float z[32], w[32];
+            TmemIO<32>::ld(y, lane_r);
+            TmemIO<32>::ld(w, lane_r + kTok);
+            tmem_wait_ld();
+            if (row < KD) image_row<PI>(z, sm + C::K, C::TILE, row, half);
+            else {
+#pragma unroll
+                for (int e = 0; e < 32; ++e) z[e] = 0.f;
+            }
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+                y[e] *= expf((float)(G[kTok - 1] - G[32 * half + e]));
+                w[e] += y[e];
+                dk[e] += erase[e] + w[e];
+                x[e] = row < a.Dk ? fmaf(z[e], erase[e] - w[e], x[e]) : 0.f;
+                y[e] *= z[e];
+            }
+        }
+        sums[1][warp & 3][32 * half + lane] = column_sum(x, lane);
+        sums[2][warp & 3][32 * half + lane] = column_sum(y, lane);
+        __syncthreads();
+        if (warp < 2) {                                      // two tokens a lane of warp 0: sums from the chunk's end; warp 1: beta
+            float s[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int i = 2 * lane + e;
+                float v = 0.f;
+                if (warp == 0) {
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) v += sums[1][w][i];
+                } else {
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) v += sums[0][w][i];
+                    v -= erased[0][i] + erased[1][i];
+                }
+                s[e] = v;
+            }
+            if (warp == 0) {
+                float written = 0.f, in = 0.f;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) written += sums[2][w][2 * lane] + sums[2][w][2 * lane + 1];
+#pragma unroll
+                for (int m = 1; m < 32; m <<= 1) written += __shfl_xor_sync(~0u, written, m);
+#pragma unroll
+                for (int w = 0; w < 8; ++w) in += total[w];
+                double v = (double)s[0] + s[1];
+                double run = v;                              // (sums of many signs: in 64 bits)
+#pragma unroll
+                for (int m = 1; m < 32; m <<= 1) {
+                    const double o = __shfl_down_sync(~0u, run, m);
+                    if (lane + m < 32) run += o;
+                }
+                run += (double)fade * in + written;
+                s[0] = (float)run;
+                s[1] = (float)(run - (v - s[1]));
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int i = 2 * lane + e;
+                if (i >= room) continue;
+                if (warp == 1) { HN_G(a.dbeta + grow + i, 4); a.dbeta[grow + i] = i < nv ? s[e] : 0.f; }
+                else if (a.dg) {
+                    float d = s[e];
+                    if (a.decay == DELTA_SIGMOID && i < nv) { HN_G(a.g + grow + i, 4); d /= 1.f + expf(__ldg(a.g + grow + i)); }
+                    HN_G(a.dg + grow + i, 4);
+                    a.dg[grow + i] = i < nv ? d : 0.f;
+                }
+            }
+        }
+    }
+    if (row < a.Dk && t < a.L) {
+        store_row<T>((T *)a.dq, qrow, a.L, a.L - t, n - t, dq);
+        store_row<T>((T *)a.dk, qrow, a.L, a.L - t, n - t, dk);
+    }
+    tmem_fence_before_sync();
+    __syncthreads();
+    if (warp == 0) tmem_dealloc(tb, 512);
+}
+
+// ---- host -----------------------------------------------------------------------------------------------------------
+
+int delta_backward_status()
+{
+    int v = 0;
+    return cudaMemcpyFromSymbol(&v, hn_delta_backward_status, sizeof(int)) == cudaSuccess ? v : -1;
+}
+
+template <typename T, int KD> static int launch_back(const DeltaArgs &a, cudaStream_t st)
+{
+    const long long blocks = (long long)a.B * a.H * a.segments;
+    if (a.segments > 1) {
+        if (const int e = launch_delta<delta_walk_back_kernel<T, KD, WALK_MAPS>>(a, 2 * blocks, 384, WalkBack<T, KD>::BYTES, st)) return e;
+        if (const int e = launch_delta_join(a, a.ds_end, true, st)) return e;
+    }
+    if (const int e = launch_delta<delta_walk_back_kernel<T, KD, WALK_RUN>>(a, blocks, 384, WalkBack<T, KD>::BYTES, st)) return e;
+    return launch_delta<delta_gradients_kernel<T, KD>>(a, (long long)a.B * a.Hk * a.chunks, 256, Grads<T, KD>::BYTES, st);
+}
+int launch_delta_backward(const DeltaArgs &a, int dtype, cudaStream_t st)
+{
+    if (const int e = launch_delta_prepare(a, dtype, st)) return e;
+    const bool small = a.Dk <= 64 && a.Dv <= 64;
+    if (dtype == HYENAND_F32) return small ? launch_back<float, 64>(a, st) : launch_back<float, 128>(a, st);
+    return small ? launch_back<bf16, 64>(a, st) : launch_back<bf16, 128>(a, st);
+}
+
+}  // namespace hn

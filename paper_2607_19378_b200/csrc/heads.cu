@@ -1,0 +1,487 @@
+// Queries and keys as heads: the norm of each head and the rotation by its token's position on the grid, in one pass, and its gradient.
+//
+// q is [B][Hq D][T], k is [B][Hk D][T], T = L_1 .. L_N.  Per token and head, over its D channels:
+//     x^ = x rho,  rho = 1 / sqrt(mean(x^2) + eps) | 1 / sqrt(sum(x^2) + eps) | 1,      n = x^ g,
+//     y_i = n_i cos(t) - n_{i+D/2} sin(t),  y_{i+D/2} = n_i sin(t) + n_{i+D/2} cos(t)   for the pairs i that have an axis,
+// t = p_a base^(-j / s_a) for the j-th of the s_a pairs of axis a, p_a the token's place on it.  Gradient: dn is dy turned back,
+//     dg = sum dn x^,   dx = rho (e - x^ (e . x^) / D)  (rms; l2: without the division; none: e),   e = dn g.
+//
+// Each tensor is read and written once: bandwidth is the bound.  Tokens are the contiguous axis, so a CTA takes a tile of 128 bytes of
+// tokens and walks the heads and batch entries on it; a head's channels are spread over R groups of eight lanes (a lane holds 16 bytes of
+// tokens of both channels of a pair), its sums go by shuffles and, beyond a warp, through shared memory.  The tile's sines and cosines
+// are formed once for all heads: angles as turns in 64 bits (in 32 a position of 100000 keeps two digits), reduced to half a
+// turn and rounded, so that an error stays below 2e-7 at any position.  A grid of fewer than eight tokens (generation) goes to a warp
+// per token and head.
+#include <math.h>
+
+#include "entry.cuh"
+
+namespace hn {
+
+enum { NORM_NONE = HYENAND_NORM_NONE, NORM_RMS = HYENAND_NORM_RMS, NORM_L2 = HYENAND_NORM_L2 };
+constexpr int kMaxD = 256, kMaxAxes = 3;
+
+struct HeadsArgs {
+    const void *x[2], *dy[2];                // q and k
+    void *out[2];
+    const float *g[2];
+    const int *positions;                    // [B][N][T], or the grid's
+    float *part;                             // [blocks of q, then of k][D]: sums of the weights' gradients
+    float *dg[2];
+    int H[2], splits[2];
+    int B, D, T, ndim, dims[kMaxAxes], axes[kMaxAxes], turned;
+    int tiles, norm;
+    float eps, per_mean;                     // 1/D, or 1: what a sum over channels counts
+    double log2_base;
+};
+
+// cosine and sine of p base^(-j/s)
+__device__ __forceinline__ float2 rotor(int p, double frequency)
+{
+    double turns = (double)p * frequency;
+    turns -= rint(turns);
+    float s, c;
+    sincospif(2.f * (float)turns, &s, &c);
+    return make_float2(c, s);
+}
+// axis and turns per position of a pair
+__device__ __forceinline__ double pair_frequency(const HeadsArgs &a, int i, int *axis)
+{
+    int n = 0;
+    while (i >= a.axes[n]) i -= a.axes[n++];
+    *axis = n;
+    return exp2(-(double)i / a.axes[n] * a.log2_base) * 0.15915494309189533577;
+}
+__device__ __forceinline__ int place(const HeadsArgs &a, int b, int axis, int t)
+{
+    if (a.positions) {
+        const int *p = a.positions + ((long long)b * a.ndim + axis) * a.T + t;
+        HN_G(p, 4);
+        return __ldg(p);
+    }
+    for (int n = a.ndim - 1; n > axis; --n) t /= a.dims[n];
+    return axis ? t % a.dims[axis] : t;
+}
+
+template <typename T> struct Tile {
+    static constexpr int V = 16 / sizeof(T), TOKENS = 8 * V;
+};
+
+// The V tokens of a lane in one row: side by side as one vector, or (rows that do not start on 16 bytes) every eighth token, so that
+// the eight lanes of a row share a sector
+template <typename T, bool VEC> __device__ __forceinline__ void load_tokens(float (&v)[Tile<T>::V], const T *row, int t0, int vc, int T_)
+{
+    constexpr int V = Tile<T>::V;
+    if constexpr (VEC) {
+        uint4 w = make_uint4(0, 0, 0, 0);
+        const int t = t0 + vc * V;
+        if (t < T_) { HN_G(row + t, 16); w = __ldg((const uint4 *)(row + t)); }
+        const T *e = (const T *)&w;
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = (float)e[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = t0 + i * 8 + vc < T_ ? IO<T>::ld(row, t0 + i * 8 + vc) : 0.f;
+    }
+}
+template <typename T, bool VEC> __device__ __forceinline__ void store_tokens(T *row, const float (&v)[Tile<T>::V], int t0, int vc, int T_)
+{
+    constexpr int V = Tile<T>::V;
+    if constexpr (VEC) {
+        const int t = t0 + vc * V;
+        uint4 w;
+        T *e = (T *)&w;
+#pragma unroll
+        for (int i = 0; i < V; ++i) e[i] = (T)v[i];
+        if (t < T_) { HN_G(row + t, 16); *(uint4 *)(row + t) = w; }
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (t0 + i * 8 + vc < T_) IO<T>::st(row, t0 + i * 8 + vc, v[i]);
+    }
+}
+
+// R groups of eight lanes to a head, P pairs of channels to a lane; 32 / R heads at a time
+template <typename T, int R, int P, bool BWD, bool VEC> __global__ void __launch_bounds__(256) heads_kernel(HeadsArgs a)
+{
+    constexpr int V = Tile<T>::V, TOKENS = Tile<T>::TOKENS, HEADS = 32 / R, WARPS = R / 4, SUMS = BWD ? 2 : 1;
+    extern __shared__ __align__(16) float sm[];
+    __shared__ double freq[kMaxD / 2];
+    __shared__ int axis_of[kMaxD / 2];
+    __shared__ float meet[2][SUMS][8][TOKENS];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, vc = lane & 7, group = warp / WARPS, r = (warp % WARPS) * 4 + (lane >> 3);
+    const int half = a.D / 2, kind = (int)blockIdx.y >= a.splits[0] ? 1 : 0, split = (int)blockIdx.y - (kind ? a.splits[0] : 0), H = a.H[kind];
+    float *cs = sm, *sn = sm + (size_t)a.turned * TOKENS;          // [pair][quarter of V][lane][4]: vectors of four without bank conflicts
+    pdl_join();
+    for (int i = tid; i < a.turned; i += 256) freq[i] = pair_frequency(a, i, &axis_of[i]);
+    float w[P][2], acc[P][2];
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const int i = r + R * p;
+            w[p][s] = 1.f;
+            acc[p][s] = 0.f;
+            if (a.g[kind] && i < half) { HN_G(a.g[kind] + i + s * half, 4); w[p][s] = __ldg(a.g[kind] + i + s * half); }
+        }
+    const long long units = (long long)a.B * H, per = (units + a.splits[kind] - 1) / a.splits[kind], first = split * per, last = first + per < units ? first + per : units;
+    int turn = 0;
+    for (int tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
+        const int t0 = tile * TOKENS;
+        for (long long u = first; u < last;) {
+            const long long b0 = u / H, end = a.positions && (b0 + 1) * H < last ? (b0 + 1) * H : last;
+            __syncthreads();                                       // (the table's readers are through, the frequencies are there)
+            for (int i = tid; i < a.turned * TOKENS; i += 256) {
+                const int pr = i / TOKENS, e = i % TOKENS, t = t0 + e;
+                const int ln = VEC ? e / V : e % 8, el = VEC ? e % V : e / 8, at = pr * TOKENS + (el / 4 * 8 + ln) * 4 + el % 4;
+                const float2 c = t < a.T ? rotor(place(a, (int)b0, axis_of[pr], t), freq[pr]) : make_float2(1.f, 0.f);
+                cs[at] = c.x;
+                sn[at] = c.y;
+            }
+            __syncthreads();
+            for (; u < end; u += HEADS) {
+                const long long unit = u + group;
+                const bool on = unit < end;
+                const long long at = on ? unit * a.D * (long long)a.T : 0;       // (unit = b H + h: its channels lie side by side)
+                float x[P][2][V], d[BWD ? P : 1][2][V], s1[V], s2[V];
+#pragma unroll
+                for (int e = 0; e < V; ++e) s1[e] = s2[e] = 0.f;
+#pragma unroll
+                for (int p = 0; p < P; ++p)
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        const int i = r + R * p, c = i + s * half;
+                        const int live = on && i < half ? a.T : 0;
+                        load_tokens<T, VEC>(x[p][s], (const T *)a.x[kind] + at + (long long)c * a.T, t0, vc, live);
+                        if constexpr (BWD) load_tokens<T, VEC>(d[p][s], (const T *)a.dy[kind] + at + (long long)c * a.T, t0, vc, live);
+                    }
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    const int i = r + R * p;
+                    if constexpr (BWD) {
+                        if (i < a.turned) {
+#pragma unroll
+                            for (int e4 = 0; e4 < V; e4 += 4) {
+                                const float4 c4 = *(const float4 *)&cs[i * TOKENS + (e4 / 4 * 8 + vc) * 4], n4 = *(const float4 *)&sn[i * TOKENS + (e4 / 4 * 8 + vc) * 4];
+                                const float cc[4] = {c4.x, c4.y, c4.z, c4.w}, nn[4] = {n4.x, n4.y, n4.z, n4.w};
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    const float lo = d[p][0][e4 + e], hi = d[p][1][e4 + e];
+                                    d[p][0][e4 + e] = lo * cc[e] + hi * nn[e];
+                                    d[p][1][e4 + e] = hi * cc[e] - lo * nn[e];
+                                }
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int s = 0; s < 2; ++s)
+#pragma unroll
+                        for (int e = 0; e < V; ++e) {
+                            s1[e] = fmaf(x[p][s][e], x[p][s][e], s1[e]);
+                            if constexpr (BWD) s2[e] = fmaf(d[p][s][e] * w[p][s], x[p][s][e], s2[e]);
+                        }
+                }
+                float rho[V];
+                if (a.norm == NORM_NONE) {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) { rho[e] = 1.f; s2[e] = 0.f; }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < V; ++e)
+#pragma unroll
+                        for (int m = 8; m < 32; m <<= 1) {
+                            s1[e] += __shfl_xor_sync(~0u, s1[e], m);
+                            if constexpr (BWD) s2[e] += __shfl_xor_sync(~0u, s2[e], m);
+                        }
+                    if constexpr (WARPS > 1) {
+                        if (lane < 8) {
+#pragma unroll
+                            for (int e = 0; e < V; ++e) {
+                                meet[turn][0][warp][e * 8 + vc] = s1[e];
+                                if constexpr (BWD) meet[turn][SUMS - 1][warp][e * 8 + vc] = s2[e];
+                            }
+                        }
+                        __syncthreads();
+#pragma unroll
+                        for (int e = 0; e < V; ++e) {
+                            s1[e] = s2[e] = 0.f;
+#pragma unroll
+                            for (int j = 0; j < WARPS; ++j) {
+                                s1[e] += meet[turn][0][group * WARPS + j][e * 8 + vc];
+                                if constexpr (BWD) s2[e] += meet[turn][SUMS - 1][group * WARPS + j][e * 8 + vc];
+                            }
+                        }
+                        turn ^= 1;
+                    }
+#pragma unroll
+                    for (int e = 0; e < V; ++e) rho[e] = 1.f / sqrtf(fmaf(s1[e], a.per_mean, a.eps));
+                }
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    const int i = r + R * p;
+                    if constexpr (BWD) {
+#pragma unroll
+                        for (int s = 0; s < 2; ++s)
+#pragma unroll
+                            for (int e = 0; e < V; ++e) {
+                                const float hat = x[p][s][e] * rho[e];
+                                acc[p][s] = fmaf(d[p][s][e], hat, acc[p][s]);
+                                const float e0 = d[p][s][e] * w[p][s];
+                                x[p][s][e] = a.norm == NORM_NONE ? e0 : rho[e] * (e0 - hat * (rho[e] * s2[e] * a.per_mean));
+                            }
+                    } else {
+#pragma unroll
+                        for (int s = 0; s < 2; ++s)
+#pragma unroll
+                            for (int e = 0; e < V; ++e) x[p][s][e] *= rho[e] * w[p][s];
+                        if (i < a.turned) {
+#pragma unroll
+                            for (int e4 = 0; e4 < V; e4 += 4) {
+                                const float4 c4 = *(const float4 *)&cs[i * TOKENS + (e4 / 4 * 8 + vc) * 4], n4 = *(const float4 *)&sn[i * TOKENS + (e4 / 4 * 8 + vc) * 4];
+                                const float cc[4] = {c4.x, c4.y, c4.z, c4.w}, nn[4] = {n4.x, n4.y, n4.z, n4.w};
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    const float lo = x[p][0][e4 + e], hi = x[p][1][e4 + e];
+                                    x[p][0][e4 + e] = lo * cc[e] - hi * nn[e];
+                                    x[p][1][e4 + e] = lo * nn[e] + hi * cc[e];
+                                }
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int s = 0; s < 2; ++s)
+                        store_tokens<T, VEC>((T *)a.out[kind] + at + (long long)(i + s * half) * a.T, x[p][s], t0, vc, on && i < half ? a.T : 0);
+                }
+            }
+            u = end;
+        }
+    }
+    if constexpr (BWD) {
+        if (!a.dg[kind]) return;
+        float *sum = &meet[0][0][0][0];                            // [HEADS][D]: at most 512 of its numbers
+        __syncthreads();
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                float v = acc[p][s];
+#pragma unroll
+                for (int m = 1; m < 8; m <<= 1) v += __shfl_xor_sync(~0u, v, m);
+                if (vc == 0 && r + R * p < half) sum[group * a.D + r + R * p + s * half] = v;
+            }
+        __syncthreads();
+        float *to = a.part + ((long long)blockIdx.y * gridDim.x + blockIdx.x) * a.D;
+        for (int c = tid; c < a.D; c += 256) {
+            float v = 0.f;
+            for (int j = 0; j < HEADS; ++j) v += sum[j * a.D + c];
+            HN_G(to + c, 4);
+            to[c] = v;
+        }
+    }
+}
+
+// the blocks' sums of the weights' gradients, always in the same order: 8 channels and 32 spans of blocks to a CTA
+__global__ void __launch_bounds__(256) heads_sum_kernel(HeadsArgs a, int blocks_x)
+{
+    __shared__ double s[32][8];
+    const int kind = blockIdx.y, c = blockIdx.x * 8 + (threadIdx.x & 7), span = threadIdx.x >> 3;
+    pdl_join();
+    if (!a.dg[kind]) return;
+    const float *part = a.part + (kind ? (long long)a.splits[0] * blocks_x * a.D : 0);
+    const int n = a.splits[kind] * blocks_x;
+    double v = 0.;
+    if (c < a.D)
+        for (int i = span; i < n; i += 32) { HN_G(part + (long long)i * a.D + c, 4); v += part[(long long)i * a.D + c]; }
+    s[span][threadIdx.x & 7] = v;
+    __syncthreads();
+    if (span || c >= a.D) return;
+    for (int j = 1; j < 32; ++j) v += s[j][threadIdx.x & 7];
+    HN_G(a.dg[kind] + c, 4);
+    a.dg[kind][c] = (float)v;
+}
+
+// Few tokens: a warp per token and head, a lane per pair
+template <typename T> __global__ void __launch_bounds__(256) heads_token_kernel(HeadsArgs a)
+{
+    const int lane = threadIdx.x & 31, half = a.D / 2, HT = a.H[0] + a.H[1];
+    const long long i = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+    pdl_join();
+    if (i >= (long long)a.B * HT * a.T) return;
+    const int t = (int)(i % a.T), b = (int)(i / a.T / HT), hh = (int)(i / a.T % HT), kind = hh >= a.H[0], h = kind ? hh - a.H[0] : hh;
+    const long long at = ((long long)b * a.H[kind] + h) * a.D * a.T + t;
+    constexpr int P = kMaxD / 64;
+    float x[P][2], sum = 0.f;
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const int c = lane + 32 * p;
+            x[p][s] = c < half ? IO<T>::ld((const T *)a.x[kind], at + (long long)(c + s * half) * a.T) : 0.f;
+            sum = fmaf(x[p][s], x[p][s], sum);
+        }
+#pragma unroll
+    for (int m = 1; m < 32; m <<= 1) sum += __shfl_xor_sync(~0u, sum, m);
+    const float rho = a.norm == NORM_NONE ? 1.f : 1.f / sqrtf(fmaf(sum, a.per_mean, a.eps));
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        const int c = lane + 32 * p;
+        if (c >= half) break;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            float w = 1.f;
+            if (a.g[kind]) { HN_G(a.g[kind] + c + s * half, 4); w = __ldg(a.g[kind] + c + s * half); }
+            x[p][s] *= rho * w;
+        }
+        if (c < a.turned) {
+            int axis;
+            const double f = pair_frequency(a, c, &axis);
+            const float2 z = rotor(place(a, b, axis, t), f);
+            const float lo = x[p][0], hi = x[p][1];
+            x[p][0] = lo * z.x - hi * z.y;
+            x[p][1] = lo * z.y + hi * z.x;
+        }
+#pragma unroll
+        for (int s = 0; s < 2; ++s) IO<T>::st((T *)a.out[kind], at + (long long)(c + s * half) * a.T, x[p][s]);
+    }
+}
+
+// CTAs along the tiles, and splits of the heads of q and of k: four CTAs an SM in all where there is work for them
+static int plan(HeadsArgs &a, int dtype, int heads_at_once)
+{
+    const int tokens = dtype == HYENAND_F32 ? 32 : 64, want = 2 * kSms;
+    a.tiles = (int)(((long long)a.T + tokens - 1) / tokens);
+    for (int n = 0; n < 2; ++n) {
+        const long long most = ((long long)a.B * a.H[n] + heads_at_once - 1) / heads_at_once;
+        const long long s = a.tiles >= want ? 1 : want / a.tiles;
+        a.splits[n] = (int)(s < most ? s : most);
+    }
+    return a.tiles < want ? a.tiles : want;
+}
+static int rows_of(int D) { return D <= 16 ? 4 : D <= 32 ? 8 : D <= 64 ? 16 : 32; }
+
+template <auto FN, typename T> static int launch_tiles(const HeadsArgs &a, int grid_x, cudaStream_t st)
+{
+    const size_t bytes = (size_t)a.turned * Tile<T>::TOKENS * 8;
+    static PerDevice ready;
+    if (bytes > 24 * 1024 && !ready.once([] { return cudaFuncSetAttribute(FN, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxD / 2 * Tile<T>::TOKENS * 8) == cudaSuccess ? 1 : -1; }))
+        return kNoLaunch;
+    launch_pdl(FN, dim3(grid_x, a.splits[0] + a.splits[1]), 256, bytes, st, a);
+    return 0;
+}
+template <typename T, bool BWD> static int launch_heads(HeadsArgs &a, int dtype, cudaStream_t st)
+{
+    if (!BWD && a.T < 8) {
+        const long long blocks = ((long long)a.B * (a.H[0] + a.H[1]) * a.T + 7) / 8;
+        if (blocks > 0x7fffffffll) return kTooLarge;
+        launch_pdl(heads_token_kernel<T>, dim3((unsigned)blocks), 256, 0, st, a);
+        return 0;
+    }
+    const int R = rows_of(a.D), gx = plan(a, dtype, 32 / R);
+    const bool vec = a.T % Tile<T>::V == 0;
+    int e;
+#define HN_HEADS(R_, P_) e = vec ? launch_tiles<heads_kernel<T, R_, P_, BWD, true>, T>(a, gx, st) : launch_tiles<heads_kernel<T, R_, P_, BWD, false>, T>(a, gx, st)
+    if (a.D <= 16) HN_HEADS(4, 2);
+    else if (a.D <= 32) HN_HEADS(8, 2);
+    else if (a.D <= 64) HN_HEADS(16, 2);
+    else if (a.D <= 128) HN_HEADS(32, 2);
+    else HN_HEADS(32, 4);
+#undef HN_HEADS
+    if (e || !BWD || (!a.dg[0] && !a.dg[1])) return e;
+    launch_pdl(heads_sum_kernel, dim3((a.D + 7) / 8, 2), 256, 0, st, a, gx);
+    return 0;
+}
+
+static int fill(HeadsArgs &a, int ndim, const int *dims, int B, int Hq, int Hk, int D, int dtype, int norm, const int *axes, double base, float eps)
+{
+    if (ndim < 1 || ndim > kMaxAxes || !dims) return fail(HYENAND_ERR_INVALID_ARG, "ndim must be 1 to %d, with dims", kMaxAxes);
+    if (B < 1 || Hq < 1 || Hk < 1 || D < 1) return fail(HYENAND_ERR_INVALID_ARG, "B, Hq, Hk and D must be >= 1");
+    if (dtype != HYENAND_F32 && dtype != HYENAND_BF16) return fail(HYENAND_ERR_INVALID_ARG, "unknown dtype %d", dtype);
+    if (norm < NORM_NONE || norm > NORM_L2) return fail(HYENAND_ERR_INVALID_ARG, "unknown norm %d", norm);
+    if (D % 2 || D > kMaxD) return fail(HYENAND_ERR_UNSUPPORTED, "D = %d: heads have an even number of channels up to %d", D, kMaxD);
+    long long T = 1;
+    for (int n = 0; n < ndim; ++n) {
+        if (dims[n] < 1) return fail(HYENAND_ERR_INVALID_ARG, "every extent must be >= 1");
+        T *= dims[n];
+        if (T > (1 << 30)) return fail(HYENAND_ERR_UNSUPPORTED, "a grid of more than 2^30 tokens");
+    }
+    if ((long long)B * ((long long)Hq + Hk) > (1 << 28)) return fail(HYENAND_ERR_UNSUPPORTED, "B * (Hq + Hk) is above 2^28");
+    if ((long long)B * ((long long)Hq + Hk) * D > (1ll << 40) / T) return fail(HYENAND_ERR_UNSUPPORTED, "more than 2^40 elements");
+    long long pairs = 0;
+    for (int n = 0; n < ndim; ++n) {
+        const int s = axes ? axes[n] : 0;
+        if (s < 0) return fail(HYENAND_ERR_INVALID_ARG, "an axis has %d pairs", s);
+        pairs += s;
+        a.dims[n] = dims[n];
+        a.axes[n] = s;
+    }
+    if (pairs > D / 2) return fail(HYENAND_ERR_INVALID_ARG, "the axes have %lld pairs, a head %d", pairs, D / 2);
+    if (pairs && !(base > 0. && base < 1e300)) return fail(HYENAND_ERR_INVALID_ARG, "base must be positive and finite");
+    if (!(eps > 0.f && eps < 3e38f)) return fail(HYENAND_ERR_INVALID_ARG, "eps must be positive and finite");
+    a.H[0] = Hq; a.H[1] = Hk; a.B = B; a.D = D; a.T = (int)T; a.ndim = ndim; a.turned = (int)pairs; a.norm = norm; a.eps = eps;
+    a.per_mean = norm == NORM_RMS ? 1.f / D : 1.f;
+    a.log2_base = pairs ? log2(base) : 0.;
+    return HYENAND_OK;
+}
+static size_t part_bytes(HeadsArgs a, int dtype)
+{
+    const long long gx = plan(a, dtype, 32 / rows_of(a.D));
+    return (size_t)(gx * (a.splits[0] + a.splits[1]) * a.D * (long long)sizeof(float));
+}
+
+}  // namespace hn
+
+using namespace hn;
+
+extern "C" long long hyenand_heads_workspace_bytes(int ndim, const int *dims, int B, int Hq, int Hk, int D, int dtype)
+{
+    HeadsArgs a{};
+    clear_error();
+    if (fill(a, ndim, dims, B, Hq, Hk, D, dtype, NORM_NONE, nullptr, 1., 1.f)) return 0;
+    return (long long)((part_bytes(a, dtype) + 15) / 16 * 16);
+}
+
+extern "C" int hyenand_heads_forward(int ndim, const int *dims, int B, int Hq, int Hk, int D, int dtype, int norm, const int *axes, double base, float eps,
+                                     const void *q, const void *k, const float *g_q, const float *g_k, const int *positions, void *q_out, void *k_out,
+                                     void *cuda_stream)
+{
+    clear_error();
+    HeadsArgs a{};
+    if (int e = fill(a, ndim, dims, B, Hq, Hk, D, dtype, norm, axes, base, eps)) return e;
+    if (!q || !k || !q_out || !k_out) return fail(HYENAND_ERR_INVALID_ARG, "q, k, q_out, k_out must be non-NULL");
+    a.x[0] = q; a.x[1] = k; a.g[0] = g_q; a.g[1] = g_k; a.positions = positions; a.out[0] = q_out; a.out[1] = k_out;
+    CallTensors c;
+    const size_t one = (size_t)B * D * a.T * elsize(dtype);
+    c.in("q", q, one * Hq); c.in("k", k, one * Hk); c.in("g_q", g_q, (size_t)D * 4, 4); c.in("g_k", g_k, (size_t)D * 4, 4);
+    c.in("positions", positions, (size_t)B * ndim * a.T * sizeof(int), 4);
+    c.out("q_out", q_out, one * Hq, 16, q); c.out("k_out", k_out, one * Hk, 16, k);
+    if (int e = c.check()) return e;
+    c.register_ranges();
+    const cudaStream_t st = (cudaStream_t)cuda_stream;
+    return finish(dtype == HYENAND_F32 ? launch_heads<float, false>(a, dtype, st) : launch_heads<bf16, false>(a, dtype, st));
+}
+
+extern "C" int hyenand_heads_backward(int ndim, const int *dims, int B, int Hq, int Hk, int D, int dtype, int norm, const int *axes, double base, float eps,
+                                      const void *q, const void *k, const float *g_q, const float *g_k, const int *positions, const void *dq_out,
+                                      const void *dk_out, void *dq, void *dk, float *dg_q, float *dg_k, void *workspace, void *cuda_stream)
+{
+    clear_error();
+    HeadsArgs a{};
+    if (int e = fill(a, ndim, dims, B, Hq, Hk, D, dtype, norm, axes, base, eps)) return e;
+    if (!q || !k || !dq_out || !dk_out || !dq || !dk) return fail(HYENAND_ERR_INVALID_ARG, "q, k, dq_out, dk_out, dq, dk must be non-NULL");
+    if ((dg_q && !g_q) || (dg_k && !g_k)) return fail(HYENAND_ERR_INVALID_ARG, "a gradient of a weight that is not given");
+    if ((dg_q || dg_k) && !workspace) return fail(HYENAND_ERR_INVALID_ARG, "workspace must be non-NULL for the weights' gradients");
+    a.x[0] = q; a.x[1] = k; a.dy[0] = dq_out; a.dy[1] = dk_out; a.g[0] = g_q; a.g[1] = g_k; a.positions = positions;
+    a.out[0] = dq; a.out[1] = dk; a.dg[0] = dg_q; a.dg[1] = dg_k; a.part = (float *)workspace;
+    CallTensors c;
+    const size_t one = (size_t)B * D * a.T * elsize(dtype);
+    c.in("q", q, one * Hq); c.in("k", k, one * Hk); c.in("g_q", g_q, (size_t)D * 4, 4); c.in("g_k", g_k, (size_t)D * 4, 4);
+    c.in("positions", positions, (size_t)B * ndim * a.T * sizeof(int), 4);
+    c.in("dq_out", dq_out, one * Hq); c.in("dk_out", dk_out, one * Hk);
+    c.out("dq", dq, one * Hq, 16, dq_out); c.out("dk", dk, one * Hk, 16, dk_out);
+    c.out("dg_q", dg_q, (size_t)D * 4, 4); c.out("dg_k", dg_k, (size_t)D * 4, 4);
+    if (dg_q || dg_k) c.out("workspace", workspace, part_bytes(a, dtype));
+    if (int e = c.check()) return e;
+    c.register_ranges();
+    const cudaStream_t st = (cudaStream_t)cuda_stream;
+    return finish(dtype == HYENAND_F32 ? launch_heads<float, true>(a, dtype, st) : launch_heads<bf16, true>(a, dtype, st));
+}

@@ -3,7 +3,7 @@
 Every function has the name and meaning of the C entry point declared in
 include/hyenand.h; tensors are passed as raw device (or host) pointers and all
 arithmetic happens in the library's CUDA kernels.  There is no fallback: if the
-library has not been built, loading raises.  Recurrence, Block and Dropout marshal
+library has not been built, loading raises.  Recurrence, DeltaRule, Heads, Block and Dropout marshal
 their arguments in a compiled module (csrc/calls.cpp).
 """
 from __future__ import annotations
@@ -31,6 +31,10 @@ HYENAND_MODE_CIRCULAR = 2
 HYENAND_DECAY_VALUE = 0
 HYENAND_DECAY_LOG = 1
 HYENAND_DECAY_SIGMOID = 2
+HYENAND_DECAY_NONE = 3
+HYENAND_NORM_NONE = 0
+HYENAND_NORM_RMS = 1
+HYENAND_NORM_L2 = 2
 HYENAND_GATE_NONE = 0
 HYENAND_GATE_SIGMOID = 1
 HYENAND_GATE_SILU = 2
@@ -119,6 +123,16 @@ def lib() -> ctypes.CDLL:
         L.hyenand_recurrence_workspace_bytes.restype = ll
         L.hyenand_recurrence_workspace_bytes.argtypes = [ci] * 4
         L.hyenand_recurrence_step.argtypes = [ci] * 4 + [vp] * 9
+        L.hyenand_delta_marks.argtypes = [ci]
+        L.hyenand_delta_workspace_bytes.restype = ll
+        L.hyenand_delta_workspace_bytes.argtypes = [ci] * 8
+        L.hyenand_delta_forward.argtypes = [ci] * 8 + [vp] * 12
+        L.hyenand_delta_backward.argtypes = [ci] * 8 + [vp] * 17
+        L.hyenand_delta_step.argtypes = [ci] * 7 + [vp] * 10
+        L.hyenand_heads_workspace_bytes.restype = ll
+        L.hyenand_heads_workspace_bytes.argtypes = [ci, ip] + [ci] * 5
+        L.hyenand_heads_forward.argtypes = [ci, ip] + [ci] * 6 + [ip, ctypes.c_double, ctypes.c_float] + [vp] * 8
+        L.hyenand_heads_backward.argtypes = [ci, ip] + [ci] * 6 + [ip, ctypes.c_double, ctypes.c_float] + [vp] * 13
         L.hyenand_block_workspace_bytes.restype = ll
         L.hyenand_block_workspace_bytes.argtypes = [ci] * 4
         L.hyenand_block_forward.argtypes = [ci] * 4 + [vp] * 6 + [cf, ci, cf, vp, ci] + [vp] * 4
@@ -376,6 +390,61 @@ def hyenand_recurrence_device_status() -> int:
     return int(lib().hyenand_recurrence_device_status())
 
 
+def _ints(values):
+    """A C array of int; what does not fit in one is refused, not cut off."""
+    if any(not -(1 << 31) <= int(n) < 1 << 31 for n in values):
+        raise OverflowError("a size must fit in 32 bits")
+    return (ctypes.c_int * len(values))(*(int(n) for n in values))
+
+
+def hyenand_delta_marks(L: int) -> int:
+    return int(lib().hyenand_delta_marks(int(L)))
+
+
+def hyenand_delta_workspace_bytes(B: int, H: int, Hk: int, L: int, Dk: int, Dv: int, dtype: int, backward: int) -> int:
+    return int(lib().hyenand_delta_workspace_bytes(*_ints((B, H, Hk, L, Dk, Dv, dtype, backward))))
+
+
+def hyenand_delta_device_status() -> int:
+    return int(lib().hyenand_delta_device_status())
+
+
+def hyenand_delta_forward(B: int, H: int, Hk: int, L: int, Dk: int, Dv: int, decay: int, dtype: int, q, k, v, g, beta, s0, lengths, y, s_end, marks,
+                          workspace, stream=None) -> None:
+    _check(lib().hyenand_delta_forward(*_ints((B, H, Hk, L, Dk, Dv, decay, dtype)), q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(g), beta.data_ptr(),
+                                       _ptr(s0), _ptr(lengths), y.data_ptr(), _ptr(s_end), _ptr(marks), workspace.data_ptr(), _stream_ptr(stream)))
+
+
+def hyenand_delta_backward(B: int, H: int, Hk: int, L: int, Dk: int, Dv: int, decay: int, dtype: int, q, k, v, g, beta, lengths, marks, dy, ds_end,
+                           dq, dk, dv, dg, dbeta, ds0, workspace, stream=None) -> None:
+    _check(lib().hyenand_delta_backward(*_ints((B, H, Hk, L, Dk, Dv, decay, dtype)), q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(g), beta.data_ptr(),
+                                        _ptr(lengths), marks.data_ptr(), dy.data_ptr(), _ptr(ds_end), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
+                                        _ptr(dg), dbeta.data_ptr(), _ptr(ds0), workspace.data_ptr(), _stream_ptr(stream)))
+
+
+def hyenand_delta_step(B: int, H: int, Hk: int, Dk: int, Dv: int, decay: int, dtype: int, q, k, v, g, beta, state, active, y, new_state, stream=None) -> None:
+    _check(lib().hyenand_delta_step(*_ints((B, H, Hk, Dk, Dv, decay, dtype)), q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(g), beta.data_ptr(),
+                                    state.data_ptr(), _ptr(active), y.data_ptr(), new_state.data_ptr(), _stream_ptr(stream)))
+
+
+def hyenand_heads_workspace_bytes(ndim: int, dims, B: int, Hq: int, Hk: int, D: int, dtype: int) -> int:
+    return int(lib().hyenand_heads_workspace_bytes(int(ndim), _ints(dims), *_ints((B, Hq, Hk, D, dtype))))
+
+
+def hyenand_heads_forward(ndim: int, dims, B: int, Hq: int, Hk: int, D: int, dtype: int, norm: int, axes, base: float, eps: float, q, k, g_q, g_k,
+                          positions, q_out, k_out, stream=None) -> None:
+    _check(lib().hyenand_heads_forward(int(ndim), _ints(dims), *_ints((B, Hq, Hk, D, dtype, norm)), None if axes is None else _ints(axes), float(base),
+                                       float(eps), q.data_ptr(), k.data_ptr(), _ptr(g_q), _ptr(g_k), _ptr(positions), q_out.data_ptr(), k_out.data_ptr(),
+                                       _stream_ptr(stream)))
+
+
+def hyenand_heads_backward(ndim: int, dims, B: int, Hq: int, Hk: int, D: int, dtype: int, norm: int, axes, base: float, eps: float, q, k, g_q, g_k,
+                           positions, dq_out, dk_out, dq, dk, dg_q, dg_k, workspace, stream=None) -> None:
+    _check(lib().hyenand_heads_backward(int(ndim), _ints(dims), *_ints((B, Hq, Hk, D, dtype, norm)), None if axes is None else _ints(axes), float(base),
+                                        float(eps), q.data_ptr(), k.data_ptr(), _ptr(g_q), _ptr(g_k), _ptr(positions), dq_out.data_ptr(), dk_out.data_ptr(),
+                                        dq.data_ptr(), dk.data_ptr(), _ptr(dg_q), _ptr(dg_k), _ptr(workspace), _stream_ptr(stream)))
+
+
 def hyenand_debug_recurrence_late(tile: int, warp: int = -1) -> int:
     return int(lib().hyenand_debug_recurrence_late(int(tile), int(warp)))
 
@@ -609,6 +678,84 @@ class Recurrence:
             with _pool(stream):
                 return self.step(q, k, v, g, state, new_state, active, y)
         return self._ops.recurrence_step(self._handle, q, k, v, g, state, new_state, active, y)
+
+
+class DeltaRule:
+    """The gated delta rule u_t = beta_t (v_t - a_t S_{t-1} k_t), S_t = a_t S_{t-1} + u_t k_t^T, y_t = S_t q_t on q, k [B, Hk * Dk, L] and
+    v [B, H * Dv, L], with a_t = exp(g_t) ("log"), sigmoid(g_t) ("sigmoid") or 1 ("none", g is None); g, beta [B, H, L] fp32, states
+    [B, H, Dv, Dk] fp32.  Value head h goes with head h // (H // Hk) of queries and keys.  Holds the shape only: every call stands
+    for itself, on any stream."""
+
+    def __init__(self, L: int, B: int, H: int, Dk: int, Dv: int = None, Hk: int = None, decay: str = "log", dtype=torch.float32):
+        self.L, self.B, self.H, self.Dk, self.decay, self.dtype = int(L), int(B), int(H), int(Dk), decay, dtype
+        self.Dv, self.Hk = self.Dk if Dv is None else int(Dv), self.H if Hk is None else int(Hk)
+        code = {"log": HYENAND_DECAY_LOG, "sigmoid": HYENAND_DECAY_SIGMOID, "none": HYENAND_DECAY_NONE}[decay]
+        shape = (self.B, self.H, self.Hk, self.L, self.Dk, self.Dv, _DTYPES[dtype])
+        work = [hyenand_delta_workspace_bytes(*shape, backward) for backward in (0, 1)]
+        if min(work) < 1:
+            raise ValueError(hyenand_last_error())
+        self._ops = _calls()
+        self._handle = self._ops.make_delta(self.B, self.H, self.Hk, self.L, self.Dk, self.Dv, hyenand_delta_marks(self.L), code, _DTYPES[dtype], *work,
+                                            _address("hyenand_delta_forward"), _address("hyenand_delta_backward"), _address("hyenand_delta_step"), _check)
+
+    def forward(self, q, k, v, g, beta, s0=None, lengths=None, marks: bool = False, y=None, stream=None):
+        """(y, states behind the rows), and with marks=True what `backward` needs of this call as a third."""
+        if stream is not None:
+            with _pool(stream):
+                return self.forward(q, k, v, g, beta, s0, lengths, marks, y)
+        return self._ops.delta_forward(self._handle, q, k, v, g, beta, s0, lengths, marks, y)
+
+    def backward(self, q, k, v, g, beta, marks, dy, ds_end=None, lengths=None, stream=None):
+        """dq, dk, dv, dg (None without a decay), dbeta and ds0, from the marks of a forward call on the same inputs."""
+        if stream is not None:
+            with _pool(stream):
+                return self.backward(q, k, v, g, beta, marks, dy, ds_end, lengths)
+        return self._ops.delta_backward(self._handle, q, k, v, g, beta, marks, dy, ds_end, lengths)
+
+    def step(self, q, k, v, g, beta, state, new_state=None, active=None, y=None, stream=None):
+        """One token: q, k [B, Hk * Dk], v [B, H * Dv], g, beta [B, H] -> y [B, H * Dv]; the states are replaced, or left and the new ones
+        written to new_state."""
+        if stream is not None:
+            with _pool(stream):
+                return self.step(q, k, v, g, beta, state, new_state, active, y)
+        return self._ops.delta_step(self._handle, q, k, v, g, beta, state, new_state, active, y)
+
+
+class Heads:
+    """Queries [B, Hq * D, L_1..L_N] and keys [B, Hk * D, L_1..L_N] as heads: the norm over each head's channels ("rms", "l2" or "none") with
+    weights g_q, g_k [D], then the pairs (i, i + D/2) turned by their position: the first axes[0] pairs on the first axis of the grid,
+    the next axes[1] on the second and so on, the j-th of an axis at base^(-j / pairs); pairs behind them stay.  Positions are the
+    grid's, or int32 [B, N, L_1..L_N].  Holds the shape only."""
+
+    def __init__(self, dims, B: int, Hq: int, Hk: int, D: int, dtype=torch.float32, norm: str = "rms", axes=None, base: float = 10000.0, eps: float = 1e-6):
+        self.dims = tuple(int(d) for d in dims)
+        self.axes = (0,) * len(self.dims) if axes is None else tuple(int(n) for n in axes)
+        self.B, self.Hq, self.Hk, self.D, self.dtype, self.norm, self.base, self.eps = int(B), int(Hq), int(Hk), int(D), dtype, norm, float(base), float(eps)
+        code = {"none": HYENAND_NORM_NONE, "rms": HYENAND_NORM_RMS, "l2": HYENAND_NORM_L2}[norm]
+        if len(self.axes) != len(self.dims):
+            raise ValueError("axes must name a number of pairs for every axis of the grid")
+        if min(self.axes, default=0) < 0 or 2 * sum(self.axes) > self.D:
+            raise ValueError("the axes have more pairs than a head")
+        work = hyenand_heads_workspace_bytes(len(self.dims), self.dims, self.B, self.Hq, self.Hk, self.D, _DTYPES[dtype])
+        if work < 1:
+            raise ValueError(hyenand_last_error())
+        self._ops = _calls()
+        self._handle = self._ops.make_heads(self.dims, self.axes, self.B, self.Hq, self.Hk, self.D, _DTYPES[dtype], code, self.base, self.eps, work,
+                                            _address("hyenand_heads_forward"), _address("hyenand_heads_backward"), _check)
+
+    def forward(self, q, k, g_q=None, g_k=None, positions=None, q_out=None, k_out=None, stream=None):
+        """(q, k) normalised and turned; q_out may be q, k_out may be k."""
+        if stream is not None:
+            with _pool(stream):
+                return self.forward(q, k, g_q, g_k, positions, q_out, k_out)
+        return self._ops.heads_forward(self._handle, q, k, g_q, g_k, positions, q_out, k_out)
+
+    def backward(self, q, k, dq_out, dk_out, g_q=None, g_k=None, positions=None, stream=None):
+        """dq, dk, dg_q, dg_k (None for a weight that was not given), from the forward's inputs."""
+        if stream is not None:
+            with _pool(stream):
+                return self.backward(q, k, dq_out, dk_out, g_q, g_k, positions)
+        return self._ops.heads_backward(self._handle, q, k, dq_out, dk_out, g_q, g_k, positions)
 
 
 class Block:
