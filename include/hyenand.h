@@ -322,8 +322,8 @@ int hyenand_debug_recurrence_late(int tile, int warp);
  * head h / (H / Hk) of queries and keys.  g, beta: [B][H][L] fp32.  s0: the states before the rows, [B][H][Dv][Dk] fp32, 16-byte aligned,
  * or NULL (zero).  lengths: [B] int32 on the device, or NULL: entry b holds lengths[b] tokens (values outside 0 .. L count as the
  * nearer of the two); what lies behind them does not count, y is zero there and the state passes through.  s_end: the states behind
- * the rows or NULL; it may be the buffer s0.  marks: NULL, or hyenand_delta_marks(L) states per head (fp32, 16-byte aligned) that the
- * backward pass of the same inputs needs.
+ * the rows or NULL; it may be the buffer s0.  marks: NULL, or B H hyenand_delta_marks(L, Dk, Dv) floats, 16-byte
+ * aligned, that the backward pass of the same inputs needs.
  * Keys are meant to have a norm of about 1 at most and beta to lie in 0 .. 2 (else the rule itself grows without bound), decays to be at
  * most 1; a decay below exp(-110) is taken as exp(-110), which fp32 cannot hold.  Tokens are taken 64 at a time on the tensor cores;
  * states, sums and decays are fp32, and what enters a product is a sum of bf16 values: exact to 2^-17 for bf16 tensors, to
@@ -335,7 +335,7 @@ int hyenand_debug_recurrence_late(int tile, int warp);
  * call allocates, synchronises or keeps anything; errors and stream as hyenand_forward_ex.
  */
 enum { HYENAND_DECAY_NONE = 3 };
-int hyenand_delta_marks(int L);                   /* states per head in marks; 0 for an L out of range */
+long long hyenand_delta_marks(int L, int Dk, int Dv);      /* floats per head in marks; 0 for sizes out of range */
 long long hyenand_delta_workspace_bytes(int B, int H, int Hk, int L, int Dk, int Dv, int dtype, int backward);      /* 0 for a shape out of range */
 int hyenand_delta_forward(int B, int H, int Hk, int L, int Dk, int Dv, int decay, int dtype, const void *q, const void *k, const void *v,
                           const float *g, const float *beta, const float *s0, const int *lengths, void *y, float *s_end, float *marks,

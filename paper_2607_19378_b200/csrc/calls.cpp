@@ -284,13 +284,13 @@ struct Delta {
 
 PyObject *make_delta(PyObject *, PyObject *args)
 {
-    int B, H, Hk, L, Dk, Dv, marks, decay, dtype;
-    long long wf, wb;
+    int B, H, Hk, L, Dk, Dv, decay, dtype;
+    long long marks, wf, wb;
     unsigned long long f, b, st;
     PyObject *raise_error;
-    if (!PyArg_ParseTuple(args, "iiiiiiiiiLLKKKO", &B, &H, &Hk, &L, &Dk, &Dv, &marks, &decay, &dtype, &wf, &wb, &f, &b, &st, &raise_error)) return nullptr;
+    if (!PyArg_ParseTuple(args, "iiiiiiLiiLLKKKO", &B, &H, &Hk, &L, &Dk, &Dv, &marks, &decay, &dtype, &wf, &wb, &f, &b, &st, &raise_error)) return nullptr;
     const int64_t kc = (int64_t)Hk * Dk, vc = (int64_t)H * Dv;
-    auto *d = new Delta{B, H, Hk, L, Dk, Dv, decay, dtype, wf, wb, type_of(dtype), {B, kc, L}, {B, vc, L}, {B, H, L}, {B, H, Dv, Dk}, {B, H, marks, Dv, Dk},
+    auto *d = new Delta{B, H, Hk, L, Dk, Dv, decay, dtype, wf, wb, type_of(dtype), {B, kc, L}, {B, vc, L}, {B, H, L}, {B, H, Dv, Dk}, {B, H, marks},
                         {B, kc}, {B, vc}, {B, H}, {B}, (decltype(&hyenand_delta_forward))f, (decltype(&hyenand_delta_backward))b,
                         (decltype(&hyenand_delta_step))st, Py_NewRef(raise_error)};
     return PyCapsule_New(d, nullptr, release<Delta>);

@@ -22,13 +22,12 @@ template <typename T, int KD> struct Prep {
     static constexpr int BYTES = 1024 + IMAGES + kTok * TROW * 4;
 };
 
-template <typename T, int KD> __global__ void __launch_bounds__(128) delta_prepare_kernel(DeltaArgs a)
+template <typename T, int KD> __global__ void __launch_bounds__(128) delta_prepare_kernel(DeltaArgs a, const __grid_constant__ DeltaMaps maps)
 {
     using C = Prep<T, KD>;
     extern __shared__ __align__(1024) unsigned char raw[];
-    __shared__ double G[kTok];
-    __shared__ float beta[kTok];
-    __shared__ uint64_t bar;
+    __shared__ float hi[kTok], lo[kTok], beta[kTok];
+    __shared__ uint64_t bar, there;
     __shared__ unsigned slot;
     unsigned char *sm = align_images(raw);
     float *Ts = (float *)(sm + C::IMAGES);
@@ -38,16 +37,29 @@ template <typename T, int KD> __global__ void __launch_bounds__(128) delta_prepa
     pdl_wait();
     const int n = live_tokens(a, b), nv = n - t0 < kTok ? n - t0 : kTok;
     if (nv <= 0) return;
-    if (warp == 0) tmem_alloc(smem_u32(&slot), 64);
-    if (tid == 0) { mbar_init(&bar, 1); fence_mbar_init(); }
-    const long long qk = ((long long)b * a.Hk + h / (a.H / a.Hk)) * a.Dk * a.L + t0, all = (long long)a.B * a.Hk * a.Dk * a.L;
-    load_tile<T>(sm, C::PITCH, (const T *)a.k, qk, all, a.L, a.Dk, nv, tid, 128);
-    load_tile<T>(sm + C::TILE, C::PITCH, (const T *)a.q, qk, all, a.L, a.Dk, nv, tid, 128);
+    const long long bk = (long long)b * a.Hk + h / (a.H / a.Hk);
     const int steps = (a.Dk + 15) / 16;
-    clear_rows(sm, C::PITCH, C::PI, a.Dk, steps * 16, tid, 128);
-    clear_rows(sm + C::TILE, C::PITCH, C::PI, a.Dk, steps * 16, tid, 128);
+    const bool copied = by_copy(a, nv, t0);
+    if (tid == 0) {
+        mbar_init(&bar, 1); mbar_init(&there, 1);
+        fence_mbar_init();
+        if (copied) {
+            mbar_expect_tx(&there, 2 * C::TILE);
+            tma_load_3d(sm, &maps.k, &there, t0, 0, (int)bk);
+            tma_load_3d(sm + C::TILE, &maps.q, &there, t0, 0, (int)bk);
+        }
+    }
+    __syncwarp();
+    if (warp == 0) tmem_alloc(smem_u32(&slot), 64);
+    if (!copied) {
+        const long long qk = bk * a.Dk * a.L + t0, all = (long long)a.B * a.Hk * a.Dk * a.L;
+        load_tile<T>(sm, C::PITCH, (const T *)a.k, qk, all, a.L, a.Dk, nv, tid, 128);
+        load_tile<T>(sm + C::TILE, C::PITCH, (const T *)a.q, qk, all, a.L, a.Dk, nv, tid, 128);
+        clear_rows(sm, C::PITCH, C::PI, a.Dk, steps * 16, tid, 128);
+        clear_rows(sm + C::TILE, C::PITCH, C::PI, a.Dk, steps * 16, tid, 128);
+    }
     const long long row = bh * a.L + t0;
-    if (warp == 1) chunk_sums(G, a.g + row, a.decay, nv, lane);
+    if (warp == 1) chunk_sums(hi, lo, a.g + row, a.decay, nv, lane);
     if (warp >= 2) {
         const int t = tid - 64;
         beta[t] = 0.f;
@@ -58,25 +70,24 @@ template <typename T, int KD> __global__ void __launch_bounds__(128) delta_prepa
     __syncthreads();
     tmem_fence_after_sync();
     const unsigned tb = slot, images = smem_u32(sm);
+    bool ok = !copied || mbar_wait(&there, 0);
     if (tid == 0) {
         issue_ss<C::PI, C::PI, C::PI, true, true>(tb, images, C::PITCH, C::TILE, images, C::PITCH, steps, kTok, false);
         umma_commit(&bar);
     }
     __syncwarp();
     if (tid < kTok) {                                        // (the decays meanwhile)
-        float *gates = a.gates + at * (4 * kTok);
-        HN_G(gates + tid, 4); HN_G(gates + 2 * kTok + tid, 4);
-        gates[tid] = expf((float)G[tid]);
-        gates[kTok + tid] = expf((float)(G[kTok - 1] - G[tid]));
-        gates[2 * kTok + tid] = beta[tid];
+        float *gates = a.gates + at * kGates;
+        const float x[5] = {ratio(hi[tid], lo[tid], 0.f, 0.f), ratio(hi[kTok - 1], lo[kTok - 1], hi[tid], lo[tid]), beta[tid], hi[tid], lo[tid]};
+#pragma unroll
+        for (int e = 0; e < 5; ++e) { HN_G(gates + e * kTok + tid, 4); gates[e * kTok + tid] = x[e]; }
     }
-    const bool ok = mbar_wait(&bar, 0);
+    ok = mbar_wait(&bar, 0) && ok;
     if (!ok) atomicExch(&hn_delta_status, 1);
     tmem_fence_after_sync();
     // lanes 0 .. 63: rows of k k^T, lanes 64 .. 127: rows of q k^T
     const int i = tid & 63;
-    const double Gi = G[i];
-    const float bi = beta[i];
+    const float Hi = hi[i], Li = lo[i], bi = beta[i];
     __syncthreads();                                          // (every thread has waited: the tiles' place is free)
     unsigned char *imageA = sm, *imageP = sm + C::PM * kMatrix;
 #pragma unroll
@@ -87,7 +98,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(128) delta_prepa
 #pragma unroll
         for (int c = 0; c < 32; ++c) {
             const int j = 32 * hf + c;
-            const float r = expf((float)(Gi - G[j]));
+            const float r = ratio(Hi, Li, hi[j], lo[j]);
             x[c] = tid < kTok ? (j < i ? bi * r * x[c] : 0.f) : (j <= i ? r * x[c] : 0.f);
         }
         if (tid < kTok) {
@@ -143,7 +154,7 @@ template <typename T, int KD> struct Walk {
     static_assert(Y0 + kTok <= 512, "tensor memory");
 };
 
-template <typename T, int KD, int MODE> __global__ void __launch_bounds__(384, 1) delta_walk_kernel(DeltaArgs a)
+template <typename T, int KD, int MODE> __global__ void __launch_bounds__(384, 1) delta_walk_kernel(DeltaArgs a, const __grid_constant__ DeltaMaps maps)
 {
     using C = Walk<T, KD>;
     constexpr int PI = C::PI, PM = C::PM, HC = KD / 2;
@@ -177,20 +188,25 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(384, 1
     if (warp >= 8) {
         // ---- the four warps that fetch
         const int ft = tid - 256;
-        const long long qk = ((long long)b * a.Hk + h / (a.H / a.Hk)) * a.Dk * a.L, all = (long long)a.B * a.Hk * a.Dk * a.L;
+        const long long bk = (long long)b * a.Hk + h / (a.H / a.Hk), qk = bk * a.Dk * a.L, all = (long long)a.B * a.Hk * a.Dk * a.L;
         for (int c = first, i = 0; c < last; ++c, ++i) {
             const int s = i % C::STAGES, t0 = c * kTok, nv = n - t0 < kTok ? n - t0 : kTok;
             if (i >= C::STAGES) WAIT(&ws.empty[s], (i / C::STAGES - 1) & 1);
             unsigned char *st = sm + s * C::STAGE;
+            const bool copied = by_copy(a, nv, t0);
             if (ft == 0) {
                 const long long at = bh * a.chunks + c;
-                const unsigned bytes = MODE == WALK_MAPS ? PM * kMatrix : 2 * PM * kMatrix;
-                mbar_expect_tx(&ws.full[s], bytes + 3 * kTok * 4);
+                const unsigned bytes = MODE == WALK_MAPS ? PM * kMatrix : 2 * PM * kMatrix, tiles = !copied ? 0 : MODE == WALK_MAPS ? C::TENSOR : 2 * C::TENSOR;
+                mbar_expect_tx(&ws.full[s], bytes + kWalkGates + tiles);
+                if (copied) tma_load_3d(st, &maps.k, &ws.full[s], t0, 0, (int)bk);
+                if (copied && MODE != WALK_MAPS) tma_load_3d(st + C::TENSOR, &maps.q, &ws.full[s], t0, 0, (int)bk);
                 bulk_load(st + 2 * C::TENSOR, a.images + at * C::IMAGES, bytes, &ws.full[s]);
-                bulk_load(st + 2 * C::TENSOR + C::IMAGES, a.gates + at * (4 * kTok), 3 * kTok * 4, &ws.full[s]);
+                bulk_load(st + 2 * C::TENSOR + C::IMAGES, a.gates + at * kGates, kWalkGates, &ws.full[s]);
             }
-            load_tile<T>(st, C::TILE, (const T *)a.k, qk + t0, all, a.L, a.Dk, nv, ft, 128);
-            if (MODE != WALK_MAPS) load_tile<T>(st + C::TENSOR, C::TILE, (const T *)a.q, qk + t0, all, a.L, a.Dk, nv, ft, 128);
+            if (!copied) {
+                load_tile<T>(st, C::TILE, (const T *)a.k, qk + t0, all, a.L, a.Dk, nv, ft, 128);
+                if (MODE != WALK_MAPS) load_tile<T>(st + C::TENSOR, C::TILE, (const T *)a.q, qk + t0, all, a.L, a.Dk, nv, ft, 128);
+            }
             fence_async_smem();
             mbar_arrive(&ws.full[s]);
         }
@@ -232,7 +248,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(384, 1
             unsigned char *st = sm + s * C::STAGE;
             const unsigned k = smem_u32(st), q = k + C::TENSOR, A = q + C::TENSOR, P = A + PM * kMatrix;
             const float *gates = (const float *)(st + 2 * C::TENSOR + C::IMAGES);
-            if (MODE != WALK_MAPS && a.marks) store_state<HC>(a.marks + (bh * a.chunks + c) * states, S, row, a.Dv, half * HC, a.Dk);
+            if (MODE != WALK_MAPS && a.marks) keep_state<HC>(a.marks + (bh * a.chunks + c) * kept_floats(a.Dv, a.Dk), S, row, a.Dv, half * HC, a.Dk);
             planes_to_tmem<PM, HC / 2>(lane_s, KD / 2, S);
             tmem_wait_st();
             tmem_fence_before_sync();
@@ -493,14 +509,14 @@ DeltaSizes delta_sizes(const DeltaArgs &a, int dtype, bool backward)
     const size_t bh = (size_t)a.B * a.H, chunks = bh * a.chunks, planes = dtype == HYENAND_F32 ? Planes<float>::MID : Planes<bf16>::MID;
     DeltaSizes s{};
     s.images = chunks * 2 * planes * kMatrix;
-    s.gates = chunks * kGates;
+    s.gates = up(chunks * kGates * 4);
     if (a.segments > 1) {
         s.maps = up(bh * a.segments * ((size_t)a.Dv + a.Dk) * a.Dk * 4);
         s.starts = up(bh * a.segments * (size_t)a.Dv * a.Dk * 4);
     }
     if (backward) {
-        s.dstates = up(chunks * a.Dv * a.Dk * 4);
-        s.dz = chunks * a.Dv * kTok * 4;
+        s.dstates = up(chunks * (size_t)kept_floats(a.Dv, a.Dk) * 4);
+        s.dz = chunks * (size_t)kept_rows(a.Dv) * kTok * 4;
     }
     s.all = s.images + s.gates + s.maps + s.starts + s.dstates + s.dz;
     return s;
@@ -516,13 +532,15 @@ static void place_workspace(DeltaArgs &a, const DeltaSizes &s, void *workspace)
     a.dz = (float *)p;
 }
 
-template <typename T> static int launch_prepare(const DeltaArgs &a, cudaStream_t st)
+template <typename T> static int launch_prepare(DeltaArgs a, cudaStream_t st)
 {
     const long long blocks = (long long)a.B * a.H * a.chunks;
-    return a.Dk <= 64 ? launch_delta<delta_prepare_kernel<T, 64>>(a, blocks, 128, Prep<T, 64>::BYTES, st)
-                      : launch_delta<delta_prepare_kernel<T, 128>>(a, blocks, 128, Prep<T, 128>::BYTES, st);
+    DeltaMaps m{};
+    a.copies = delta_maps<T>(m, a, a.Dk <= 64 ? 64 : 128);
+    return a.Dk <= 64 ? launch_delta<delta_prepare_kernel<T, 64>>(a, blocks, 128, Prep<T, 64>::BYTES, st, m)
+                      : launch_delta<delta_prepare_kernel<T, 128>>(a, blocks, 128, Prep<T, 128>::BYTES, st, m);
 }
-int launch_delta_prepare(const DeltaArgs &a, int dtype, cudaStream_t st) { return dtype == HYENAND_F32 ? launch_prepare<float>(a, st) : launch_prepare<bf16>(a, st); }
+int launch_delta_prepare(DeltaArgs a, int dtype, cudaStream_t st) { return dtype == HYENAND_F32 ? launch_prepare<float>(a, st) : launch_prepare<bf16>(a, st); }
 
 int launch_delta_join(const DeltaArgs &a, const float *from, bool backward, cudaStream_t st)
 {
@@ -532,14 +550,16 @@ int launch_delta_join(const DeltaArgs &a, const float *from, bool backward, cuda
     return 0;
 }
 
-template <typename T, int KD> static int launch_walk(const DeltaArgs &a, cudaStream_t st)
+template <typename T, int KD> static int launch_walk(DeltaArgs a, cudaStream_t st)
 {
+    DeltaMaps m{};
+    a.copies = delta_maps<T>(m, a, KD);
     const long long blocks = (long long)a.B * a.H * a.segments;
     if (a.segments > 1) {
-        if (const int e = launch_delta<delta_walk_kernel<T, KD, WALK_MAPS>>(a, 2 * blocks, 384, Walk<T, KD>::BYTES, st)) return e;
+        if (const int e = launch_delta<delta_walk_kernel<T, KD, WALK_MAPS>>(a, 2 * blocks, 384, Walk<T, KD>::BYTES, st, m)) return e;
         if (const int e = launch_delta_join(a, a.s0, false, st)) return e;
     }
-    return launch_delta<delta_walk_kernel<T, KD, WALK_RUN>>(a, blocks, 384, Walk<T, KD>::BYTES, st);
+    return launch_delta<delta_walk_kernel<T, KD, WALK_RUN>>(a, blocks, 384, Walk<T, KD>::BYTES, st, m);
 }
 template <typename T> static int launch_forward(const DeltaArgs &a, cudaStream_t st)
 {
@@ -581,6 +601,7 @@ static int fill(DeltaArgs &a, int B, int H, int Hk, int L, int Dk, int Dv, int d
     return HYENAND_OK;
 }
 static size_t state_bytes(const DeltaArgs &a) { return (size_t)a.B * a.H * a.Dv * a.Dk * sizeof(float); }
+static size_t mark_bytes(const DeltaArgs &a) { return (size_t)a.B * a.H * a.chunks * kept_floats(a.Dv, a.Dk) * sizeof(float); }
 // what every call takes: q, k, v, g, beta (of T tokens)
 static int inputs(CallTensors &c, const DeltaArgs &a, size_t T, int dtype)
 {
@@ -597,7 +618,10 @@ static int inputs(CallTensors &c, const DeltaArgs &a, size_t T, int dtype)
 
 using namespace hn;
 
-extern "C" int hyenand_delta_marks(int L) { return L < 1 || L > (1 << 30) ? 0 : (L + kTok - 1) / kTok; }
+extern "C" long long hyenand_delta_marks(int L, int Dk, int Dv)
+{
+    return L < 1 || L > (1 << 30) || Dk < 1 || Dv < 1 || Dk > 128 || Dv > 128 ? 0 : (L + kTok - 1) / kTok * kept_floats(Dv, Dk);
+}
 
 extern "C" long long hyenand_delta_workspace_bytes(int B, int H, int Hk, int L, int Dk, int Dv, int dtype, int backward)
 {
@@ -630,7 +654,7 @@ extern "C" int hyenand_delta_forward(int B, int H, int Hk, int L, int Dk, int Dv
     place_workspace(a, s, workspace);
     c.in("s0", s0, state_bytes(a));
     c.out("y", y, (size_t)B * H * Dv * L * elsize(dtype)); c.out("s_end", s_end, state_bytes(a), 16, s0);
-    c.out("marks", marks, state_bytes(a) * a.chunks); c.out("workspace", workspace, s.all);
+    c.out("marks", marks, mark_bytes(a)); c.out("workspace", workspace, s.all);
     if (int e = c.check()) return e;
     c.register_ranges();
     const cudaStream_t st = (cudaStream_t)cuda_stream;
@@ -654,7 +678,7 @@ extern "C" int hyenand_delta_backward(int B, int H, int Hk, int L, int Dk, int D
     const DeltaSizes s = delta_sizes(a, dtype, true);
     place_workspace(a, s, workspace);
     const size_t es = elsize(dtype) * (size_t)L * B, gb = (size_t)B * H * L * sizeof(float);
-    c.in("marks", marks, state_bytes(a) * a.chunks); c.in("dy", dy, es * H * Dv); c.in("ds_end", ds_end, state_bytes(a));
+    c.in("marks", marks, mark_bytes(a)); c.in("dy", dy, es * H * Dv); c.in("ds_end", ds_end, state_bytes(a));
     c.out("dq", dq, es * Hk * Dk); c.out("dk", dk, es * Hk * Dk); c.out("dv", dv, es * H * Dv); c.out("dg", dg, gb, 4); c.out("dbeta", dbeta, gb, 4);
     c.out("ds0", ds0, state_bytes(a), 16, ds_end); c.out("workspace", workspace, s.all);
     if (int e = c.check()) return e;

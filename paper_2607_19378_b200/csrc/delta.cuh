@@ -30,7 +30,8 @@ enum { DELTA_LOG = HYENAND_DECAY_LOG, DELTA_SIGMOID = HYENAND_DECAY_SIGMOID, DEL
 template <typename T> struct Planes { static constexpr int IN = 1, MID = 2; };
 template <> struct Planes<float> { static constexpr int IN = 3, MID = 3; };
 constexpr int kMatrix = kTok * 128;                       // bytes of one plane of a 64 x 64 matrix
-constexpr int kGates = 4 * kTok * 4;                      // gamma, delta, beta of a chunk, and room
+constexpr int kGates = 5 * kTok;                          // floats of a chunk: gamma, delta, beta, and G in two parts (see ratio)
+constexpr int kWalkGates = 3 * kTok * 4;                  // bytes of the first three
 
 struct DeltaArgs {
     const void *q, *k, *v;
@@ -45,10 +46,11 @@ struct DeltaArgs {
     float *dg, *dbeta, *ds0;
     // workspace
     unsigned char *images;                                // [B H][chunks]: planes of A, planes of P
-    float *gates;                                         // [B H][chunks][4][64]
+    float *gates;                                         // [B H][chunks][5][64]
     float *maps, *starts;                                 // [B H][segments][Dv + Dk][Dk], [B H][segments][Dv][Dk]
-    float *dstates, *dz;                                  // [B H][chunks][Dv][Dk], [B H][chunks][Dv][64]
+    float *dstates, *dz;                                  // [B H][chunks] states as kept, [B H][chunks][Dv][64]
     int B, H, Hk, L, Dk, Dv, decay, chunks, segments, per_segment;
+    int copies;                                           // 1: tiles come as tensor copies
 };
 
 __device__ __forceinline__ int live_tokens(const DeltaArgs &a, int b)
@@ -279,6 +281,24 @@ template <typename T> __device__ __forceinline__ void store_row(T *p, long long 
             if (i < room) IO<T>::st(p, at + i, i < nv ? x[i] : 0.f);
     }
 }
+// A state that stays inside the library (marks, the gradient behind a chunk): column quartets [D / 4][rows], the rows of a group of eight
+// exchanged by the quartet.  Threads that hold rows write and read it in whole lines; from shared memory both rows and columns come
+// without bank conflicts.
+__host__ __device__ __forceinline__ int kept_rows(int rows) { return (rows + 7) & ~7; }
+__host__ __device__ __forceinline__ long long kept_floats(int rows, int D) { return (long long)kept_rows(rows) * ((D + 3) & ~3); }
+__device__ __forceinline__ int kept_at(int row, int quartet, int rows8) { return quartet * rows8 + (row ^ (quartet & 7)); }
+template <int C> __device__ __forceinline__ void keep_state(float *p, const float (&s)[C], int row, int rows, int col, int D)
+{
+    const int rows8 = kept_rows(rows);
+    if (row >= rows8) return;
+#pragma unroll
+    for (int i = 0; i < C; i += 4)
+        if (col + i < D) {
+            float4 *to = (float4 *)p + kept_at(row, (col + i) >> 2, rows8);
+            HN_G(to, 16);
+            *to = make_float4(s[i], s[i + 1], s[i + 2], s[i + 3]);
+        }
+}
 // this thread's C columns from `col` of row `row` of a state [rows][D], zero outside it
 template <int C> __device__ __forceinline__ void load_state(float (&s)[C], const float *p, int row, int rows, int col, int D)
 {
@@ -321,8 +341,9 @@ __device__ __forceinline__ float log_decay(float g, int decay)
     if (decay == DELTA_SIGMOID) x = g >= 0.f ? -log1pf(expf(-g)) : g - log1pf(expf(g));
     return x < -110.f ? -110.f : x;
 }
-// G of a chunk's 64 tokens, by one warp, in 64 bits (differences of neighbours beside a sum of many); tokens from nv on decay nothing
-__device__ __forceinline__ void chunk_sums(double *G, const float *g, int decay, int nv, int lane)
+// G of a chunk's 64 tokens, by one warp, summed in 64 bits (differences of neighbours beside a sum of many) and kept in units of log 2 as a
+// float and the rest; tokens from nv on decay nothing
+__device__ __forceinline__ void chunk_sums(float *hi, float *lo, const float *g, int decay, int nv, int lane)
 {
     double x[2];
 #pragma unroll
@@ -337,9 +358,15 @@ __device__ __forceinline__ void chunk_sums(double *G, const float *g, int decay,
         const double o = __shfl_up_sync(~0u, s, m);
         if (lane >= m) s += o;
     }
-    G[2 * lane] = s - x[1];
-    G[2 * lane + 1] = s;
+    const double G[2] = {(s - x[1]) * 1.4426950408889634, s * 1.4426950408889634};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        hi[2 * lane + i] = (float)G[i];
+        lo[2 * lane + i] = (float)(G[i] - (float)G[i]);
+    }
 }
+// exp(G_i - G_j)
+__device__ __forceinline__ float ratio(float hi, float lo, float hj, float lj) { return exp2f((hi - hj) + (lo - lj)); }
 
 // ---- products ------------------------------------------------------------------------------------------------------------
 
@@ -394,21 +421,40 @@ __device__ __forceinline__ unsigned char *align_images(unsigned char *p) { retur
 
 enum { WALK_RUN = 0, WALK_MAPS = 1 };
 
+// ---- tensor copies -----------------------------------------------------------------------------------------------------
+
+// Tiles of bf16 tensors whose rows start on 16 bytes come as tensor copies: rows behind a head's channels and tokens behind L arrive as
+// zeros.  Others, and a chunk that ends before L, are fetched by threads (load_tile).
+struct DeltaMaps { CUtensorMap k, q, dy; };
+__device__ __forceinline__ bool by_copy(const DeltaArgs &a, int nv, int t0) { return a.copies && (nv == kTok || t0 + nv == a.L); }
+
 // ---- host ------------------------------------------------------------------------------------------------------------
+
+template <typename T> static bool delta_maps(DeltaMaps &m, const DeltaArgs &a, int rows)
+{
+    if (sizeof(T) != 2 || a.L % 8 || !tma_available()) return false;
+    auto one = [&](CUtensorMap *map, const void *p, int D, long long heads) {
+        const unsigned long long dims[3] = {(unsigned long long)a.L, (unsigned long long)D, (unsigned long long)heads},
+                                 strides[2] = {2ull * a.L, 2ull * a.L * D};
+        const unsigned box[3] = {(unsigned)kTok, (unsigned)rows, 1};
+        return tma_encode_3d_cached(map, p, true, dims, strides, box, 128);
+    };
+    return one(&m.k, a.k, a.Dk, (long long)a.B * a.Hk) && one(&m.q, a.q, a.Dk, (long long)a.B * a.Hk) && (!a.dy || one(&m.dy, a.dy, a.Dv, (long long)a.B * a.H));
+}
 
 struct DeltaSizes { size_t images, gates, maps, starts, dstates, dz, all; };          // bytes of the parts of a workspace, in this order
 DeltaSizes delta_sizes(const DeltaArgs &a, int dtype, bool backward);
-int launch_delta_prepare(const DeltaArgs &a, int dtype, cudaStream_t st);
+int launch_delta_prepare(DeltaArgs a, int dtype, cudaStream_t st);
 int launch_delta_join(const DeltaArgs &a, const float *from, bool backward, cudaStream_t st);
 int launch_delta_backward(const DeltaArgs &a, int dtype, cudaStream_t st);
 int delta_backward_status();
 
-template <auto FN> static int launch_delta(const DeltaArgs &a, long long blocks, unsigned threads, int bytes, cudaStream_t st)
+template <auto FN, typename... M> static int launch_delta(const DeltaArgs &a, long long blocks, unsigned threads, int bytes, cudaStream_t st, const M &...maps)
 {
     if (blocks > 0x7fffffffll) return kTooLarge;
     static PerDevice ready;
     if (bytes > 48 * 1024 - 4096 && !ready.once([&] { return cudaFuncSetAttribute(FN, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess ? 1 : -1; })) return kNoLaunch;
-    launch_pdl(FN, dim3((unsigned)blocks), threads, bytes, st, a);
+    launch_pdl(FN, dim3((unsigned)blocks), threads, bytes, st, a, maps...);
     return 0;
 }
 

@@ -29,7 +29,7 @@ template <typename T, int KD> struct WalkBack {
     static_assert(Y0 + kTok <= 512 && BYTES <= 227 * 1024, "tensor and shared memory");
 };
 
-template <typename T, int KD, int MODE> __global__ void __launch_bounds__(384, 1) delta_walk_back_kernel(DeltaArgs a)
+template <typename T, int KD, int MODE> __global__ void __launch_bounds__(384, 1) delta_walk_back_kernel(DeltaArgs a, const __grid_constant__ DeltaMaps maps)
 {
     using C = WalkBack<T, KD>;
     constexpr int PI = C::PI, PM = C::PM, HC = KD / 2;
@@ -67,20 +67,28 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(384, 1
     const long long vhead = bh * a.Dv * a.L, vall = (long long)a.B * a.H * a.Dv * a.L;
     if (warp >= 8) {
         const int ft = tid - 256;
-        const long long qk = ((long long)b * a.Hk + h / (a.H / a.Hk)) * a.Dk * a.L, all = (long long)a.B * a.Hk * a.Dk * a.L;
+        const long long bk = (long long)b * a.Hk + h / (a.H / a.Hk), qk = bk * a.Dk * a.L, all = (long long)a.B * a.Hk * a.Dk * a.L;
         for (int i = 0; i < count; ++i) {
             const int c = last - 1 - i, s = i % C::STAGES, t0 = c * kTok, nv = n - t0 < kTok ? n - t0 : kTok;
             if (i >= C::STAGES) WAIT(&ws.empty[s], (i / C::STAGES - 1) & 1);
             unsigned char *st = sm + s * C::STAGE;
+            const bool copied = by_copy(a, nv, t0);
             if (ft == 0) {
                 const long long at = bh * a.chunks + c;
-                mbar_expect_tx(&ws.full[s], C::IMAGES + 3 * kTok * 4);
+                mbar_expect_tx(&ws.full[s], C::IMAGES + kWalkGates + (copied ? (phi ? 2 : 3) * C::TENSOR : 0));
+                if (copied) {
+                    tma_load_3d(st, &maps.k, &ws.full[s], t0, 0, (int)bk);
+                    tma_load_3d(st + C::TENSOR, &maps.q, &ws.full[s], t0, 0, (int)bk);
+                    if (!phi) tma_load_3d(st + 2 * C::TENSOR, &maps.dy, &ws.full[s], t0, 0, (int)bh);
+                }
                 bulk_load(st + 3 * C::TENSOR, a.images + at * C::IMAGES, C::IMAGES, &ws.full[s]);
-                bulk_load(st + 3 * C::TENSOR + C::IMAGES, a.gates + at * (4 * kTok), 3 * kTok * 4, &ws.full[s]);
+                bulk_load(st + 3 * C::TENSOR + C::IMAGES, a.gates + at * kGates, kWalkGates, &ws.full[s]);
             }
-            load_tile<T>(st, C::TILE, (const T *)a.k, qk + t0, all, a.L, a.Dk, nv, ft, 128);
-            load_tile<T>(st + C::TENSOR, C::TILE, (const T *)a.q, qk + t0, all, a.L, a.Dk, nv, ft, 128);
-            if (!phi) load_tile<T>(st + 2 * C::TENSOR, C::TILE, (const T *)a.dy, vhead + t0, vall, a.L, a.Dv, nv, ft, 128);
+            if (!copied) {
+                load_tile<T>(st, C::TILE, (const T *)a.k, qk + t0, all, a.L, a.Dk, nv, ft, 128);
+                load_tile<T>(st + C::TENSOR, C::TILE, (const T *)a.q, qk + t0, all, a.L, a.Dk, nv, ft, 128);
+                if (!phi) load_tile<T>(st + 2 * C::TENSOR, C::TILE, (const T *)a.dy, vhead + t0, vall, a.L, a.Dv, nv, ft, 128);
+            }
             fence_async_smem();
             mbar_arrive(&ws.full[s]);
         }
@@ -108,7 +116,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(384, 1
             unsigned char *st = sm + s * C::STAGE;
             const unsigned k = smem_u32(st), q = k + C::TENSOR, g = q + C::TENSOR, A = g + C::TENSOR, P = A + PM * kMatrix;
             const float *gates = (const float *)(st + 3 * C::TENSOR + C::IMAGES);
-            if (MODE != WALK_MAPS) store_state<HC>(a.dstates + (bh * a.chunks + c) * states, S, row, a.Dv, half * HC, a.Dk);
+            if (MODE != WALK_MAPS) keep_state<HC>(a.dstates + (bh * a.chunks + c) * kept_floats(a.Dv, a.Dk), S, row, a.Dv, half * HC, a.Dk);
             planes_to_tmem<PM, HC / 2>(lane_s, KD / 2, S);
             tmem_wait_st();
             tmem_fence_before_sync();
@@ -163,10 +171,10 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(384, 1
             tmem_fence_after_sync();
             TmemIO<32>::ld(x, lane_x + 32 * half);
             tmem_wait_ld();
-            if (MODE != WALK_MAPS && real) {
-                float *to = a.dz + ((bh * a.chunks + c) * a.Dv + row) * kTok + 32 * half;
+            if (MODE != WALK_MAPS && row < kept_rows(a.Dv)) {                 // [quartet of tokens][row]
+                float4 *to = (float4 *)a.dz + ((bh * a.chunks + c) * 16 + 8 * half) * kept_rows(a.Dv) + row;
 #pragma unroll
-                for (int e = 0; e < 32; e += 4) { HN_G(to + e, 16); *(float4 *)(to + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]); }
+                for (int e = 0; e < 8; ++e) { HN_G(to + e * kept_rows(a.Dv), 16); to[e * kept_rows(a.Dv)] = make_float4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]); }
             }
 #pragma unroll
             for (int e = 0; e < 32; e += 4) {
@@ -227,12 +235,15 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(384, 1
 
 template <typename T, int KD> struct Grads {
     static constexpr int PI = Planes<T>::IN, PM = Planes<T>::MID, TILE = KD * 128;
-    // images: dY (later Q) | K | U | dZ (later E) | A (later F)
-    static constexpr int DY = 0, K = PI * TILE, U = K + PI * TILE, DZ = U + PM * TILE, A = DZ + PM * TILE, END = A + PM * kMatrix, BYTES = 1024 + END;
+    // images: dY | K | Q | U | dZ (later E) | A (later F), and a state as it is kept.  With three planes there is no room for the last, and
+    // Q comes into dY's place once that is through.
+    static constexpr bool ROOM = PI == 1;
+    static constexpr int DY = 0, K = PI * TILE, Q = ROOM ? 2 * PI * TILE : DY, U = (ROOM ? 3 : 2) * PI * TILE, DZ = U + PM * TILE, A = DZ + PM * TILE, STATE = A + PM * kMatrix,
+                         BYTES = 1024 + STATE + (ROOM ? KD * KD * 4 : 0);
     // tensor memory: a state as an operand | six sums of 64 columns, Z as an operand in the second and third
     static constexpr int S0 = 0, SCOLS = PM * KD / 2, R0 = SCOLS;
-    static constexpr int SUMS = Planes<T>::IN < Planes<T>::MID ? 6 : 5;
-    static_assert(R0 + SUMS * kTok <= 512 && BYTES + 4096 <= 227 * 1024 && PM * kTok / 2 <= 2 * kTok && PM * TILE >= PM * kMatrix, "tensor and shared memory");
+    static constexpr int SUMS = PI < PM ? 6 : 5;
+    static_assert(R0 + SUMS * kTok <= 512 && BYTES + 6144 <= 227 * 1024 && PM * kTok / 2 <= 2 * kTok && PM * TILE >= PM * kMatrix, "tensor and shared memory");
 };
 
 // x[c] summed over the warp's lanes; lane l is left with column l
@@ -250,22 +261,23 @@ __device__ __forceinline__ float column_sum(float (&x)[32], int lane)
     return x[0];
 }
 
-template <typename T, int KD> __global__ void __launch_bounds__(256, 1) delta_gradients_kernel(DeltaArgs a)
+template <typename T, int KD> __global__ void __launch_bounds__(256, 1) delta_gradients_kernel(DeltaArgs a, const __grid_constant__ DeltaMaps maps)
 {
     using C = Grads<T, KD>;
     constexpr int PI = C::PI, PM = C::PM, HC = KD / 2;
     extern __shared__ __align__(1024) unsigned char raw[];
-    __shared__ WalkShared ws;
-    __shared__ double G[kTok];
-    __shared__ float beta[kTok], sums[3][4][kTok], erased[2][kTok], total[8];
+    __shared__ WalkShared ws;                                // bar_a: products, full[0]: a head's inputs, full[1]: the gradient behind the chunk
+    __shared__ __align__(16) float gates[kGates];
+    __shared__ float sums[3][4][kTok], erased[2][kTok], total[8];
+    const float *gamma = gates, *delta = gates + kTok, *beta = gates + 2 * kTok, *ghi = gates + 3 * kTok, *glo = gates + 4 * kTok;
     unsigned char *sm = align_images(raw);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, row = 32 * (warp & 3) + lane, half = warp >> 2, share = a.H / a.Hk;
     const long long bk = blockIdx.x / a.chunks;
     const int chunk = (int)(blockIdx.x % a.chunks), b = (int)(bk / a.Hk), hk = (int)(bk % a.Hk), t0 = chunk * kTok, t = t0 + 32 * half;
     pdl_wait();
-    const int n = live_tokens(a, b), nv = n - t0 < kTok ? n - t0 : kTok, room = a.L - t0 < kTok ? a.L - t0 : kTok;
+    const int n = live_tokens(a, b), nv = n - t0 < kTok ? n - t0 : kTok, room = a.L - t0 < kTok ? a.L - t0 : kTok, rows8 = kept_rows(a.Dv);
     const long long qrow = (bk * a.Dk + row) * a.L + t, qk = bk * a.Dk * a.L + t0, all = (long long)a.B * a.Hk * a.Dk * a.L, vall = (long long)a.B * a.H * a.Dv * a.L;
-    const long long states = (long long)a.Dv * a.Dk;
+    const long long kept = kept_floats(a.Dv, a.Dk);
     float dq[32], dk[32];
 #pragma unroll
     for (int e = 0; e < 32; ++e) dq[e] = dk[e] = 0.f;
@@ -282,12 +294,16 @@ template <typename T, int KD> __global__ void __launch_bounds__(256, 1) delta_gr
         }
         return;
     }
+    const bool copied = by_copy(a, nv, t0);
+    if (tid == 0) {
+        mbar_init(&ws.bar_a, 1); mbar_init(&ws.full[0], 1); mbar_init(&ws.full[1], 1);
+        ws.gave_up = 0;
+        fence_mbar_init();
+    }
+    __syncwarp();
     if (warp == 0) tmem_alloc(smem_u32(&ws.slot), 512);
-    if (tid == 0) { mbar_init(&ws.bar_a, 1); ws.gave_up = 0; fence_mbar_init(); }
     const int ksteps = (a.Dk + 15) / 16, vsteps = (a.Dv + 15) / 16;
-    load_tile<T>(sm + C::K, C::TILE, (const T *)a.k, qk, all, a.L, a.Dk, nv, tid, 256);
-    clear_rows(sm + C::K, C::TILE, PI, a.Dk, KD, tid, 256);
-    const unsigned images = smem_u32(sm), IK = images + C::K, IU = images + C::U, IZ = images + C::DZ, IA = images + C::A, IY = images + C::DY;
+    const unsigned images = smem_u32(sm), IK = images + C::K, IU = images + C::U, IZ = images + C::DZ, IA = images + C::A, IY = images + C::DY, IQ = images + C::Q;
     unsigned par = 0, tb = 0;
     float x[32], y[32], erase[32];
     auto go = [&] {                                          // what the threads wrote, for the products
@@ -305,43 +321,68 @@ template <typename T, int KD> __global__ void __launch_bounds__(256, 1) delta_gr
     };
     for (int j = 0; j < share; ++j) {
         const long long bh = (long long)b * a.H + hk * share + j, at = bh * a.chunks + chunk, grow = bh * a.L + t0;
-        const float *S = a.marks + at * states, *D = a.dstates + at * states;
-        if (j) __syncthreads();                              // the images and sums of the head before have been read
-        load_tile<T>(sm + C::DY, C::TILE, (const T *)a.dy, bh * a.Dv * a.L + t0, vall, a.L, a.Dv, nv, tid, 256);
-        clear_rows(sm + C::DY, C::TILE, PI, a.Dv, KD, tid, 256);
-        {
-            const uint4 *from = (const uint4 *)(a.images + at * (2 * PM * kMatrix));
-            for (int e = tid; e < PM * kMatrix / 16; e += 256) { HN_G(from + e, 16); ((uint4 *)(sm + C::A))[e] = __ldg(from + e); }
+        const float *S = a.marks + at * kept, *D = a.dstates + at * kept;
+        if (j) {                                             // the images and sums of the head before have been read
+            fence_async_smem();
+            __syncthreads();
         }
-        if (warp == 0) chunk_sums(G, a.g + grow, a.decay, nv, lane);
-        if (warp == 1 || warp == 2) {
-            const int i = tid - 32;
-            beta[i] = 0.f;
-            if (i < nv) { HN_G(a.beta + grow + i, 4); beta[i] = __ldg(a.beta + grow + i); }
-        }
-        float dz[32];
-        if (row < a.Dv) {
-            const float *from = a.dz + (at * a.Dv + row) * kTok + 32 * half;
-#pragma unroll
-            for (int e = 0; e < 32; e += 4) {
-                HN_G(from + e, 16);
-                const float4 w = *(const float4 *)(from + e);
-                dz[e] = w.x; dz[e + 1] = w.y; dz[e + 2] = w.z; dz[e + 3] = w.w;
+        if (tid == 0) {
+            mbar_expect_tx(&ws.full[0], PM * kMatrix + kGates * 4 + (C::ROOM ? (unsigned)(kept * 4) : 0) + (copied ? (j ? 1 : 3) * C::TILE : 0));
+            if (C::ROOM) bulk_load(sm + C::STATE, S, (unsigned)(kept * 4), &ws.full[0]);
+            if (copied) {
+                if (!j) tma_load_3d(sm + C::K, &maps.k, &ws.full[0], t0, 0, (int)bk);
+                tma_load_3d(sm + C::DY, &maps.dy, &ws.full[0], t0, 0, (int)bh);
+                if (!j) tma_load_3d(sm + C::Q, &maps.q, &ws.full[0], t0, 0, (int)bk);
             }
-        } else {
+            bulk_load(gates, a.gates + at * kGates, kGates * 4, &ws.full[0]);
+            bulk_load(sm + C::A, a.images + at * (2 * PM * kMatrix), PM * kMatrix, &ws.full[0]);
+        }
+        __syncwarp();
+        float dz[32];
+        {
+            const float4 *from = (const float4 *)a.dz + (at * 16 + 8 * half) * rows8 + row;
 #pragma unroll
-            for (int e = 0; e < 32; ++e) dz[e] = 0.f;
+            for (int e = 0; e < 8; ++e) {
+                float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (row < rows8) { HN_G(from + e * rows8, 16); w = from[e * rows8]; }
+                dz[4 * e] = w.x; dz[4 * e + 1] = w.y; dz[4 * e + 2] = w.z; dz[4 * e + 3] = w.w;
+            }
+        }
+        RowPart<T> v;
+        v.load((const T *)a.v, (bh * a.Dv + row) * a.L + t, vall, a.L, row < a.Dv ? n - t : 0);
+        if (!copied) {
+            load_tile<T>(sm + C::DY, C::TILE, (const T *)a.dy, bh * a.Dv * a.L + t0, vall, a.L, a.Dv, nv, tid, 256);
+            clear_rows(sm + C::DY, C::TILE, PI, a.Dv, KD, tid, 256);
+            if (!j) {
+                load_tile<T>(sm + C::K, C::TILE, (const T *)a.k, qk, all, a.L, a.Dk, nv, tid, 256);
+                clear_rows(sm + C::K, C::TILE, PI, a.Dk, KD, tid, 256);
+                if (C::ROOM) {
+                    load_tile<T>(sm + C::Q, C::TILE, (const T *)a.q, qk, all, a.L, a.Dk, nv, tid, 256);
+                    clear_rows(sm + C::Q, C::TILE, PI, a.Dk, KD, tid, 256);
+                }
+            }
         }
         if (row < KD) planes_to_image<PM>(sm + C::DZ, C::TILE, row, half, dz);
         tmem_fence_before_sync();
         __syncthreads();                                     // (tensor memory and its barrier are there)
         tmem_fence_after_sync();
+        WAIT(&ws.full[0], j & 1);
         tb = ws.slot;
         const unsigned lane_s = tmem_addr(tb, warp, C::S0 + half * (HC / 2)), lane_r = tmem_addr(tb, warp, C::R0 + half * 32);
-        const float fade = expf((float)G[kTok - 1]);
+        const float4 *held = C::ROOM ? (const float4 *)(sm + C::STATE) : nullptr;
         {   // the state before the chunk, its rows as lanes: S0 k
             float s[HC];
-            load_state<HC>(s, S, row, a.Dv, half * HC, a.Dk);
+#pragma unroll
+            for (int e = 0; e < HC; e += 4) {
+                const int c = half * HC + e;
+                float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (row < rows8 && c < a.Dk) {
+                    const int i = kept_at(row, c >> 2, rows8);
+                    if (C::ROOM) w = held[i];
+                    else { HN_G((const float4 *)S + i, 16); w = ((const float4 *)S)[i]; }
+                }
+                s[e] = w.x; s[e + 1] = w.y; s[e + 2] = w.z; s[e + 3] = w.w;
+            }
             planes_to_tmem<PM, HC / 2>(lane_s, KD / 2, s);
         }
         go();
@@ -349,46 +390,66 @@ template <typename T, int KD> __global__ void __launch_bounds__(256, 1) delta_gr
             issue_ts<PM, PI, PM, true>(tb + C::R0, tb + C::S0, KD / 2, IK, C::TILE, ksteps, kTok, false);
             umma_commit(&ws.bar_a);
         }
-        RowPart<T> v;
-        v.load((const T *)a.v, (bh * a.Dv + row) * a.L + t, vall, a.L, row < a.Dv ? n - t : 0);
         done();
         TmemIO<32>::ld(x, lane_r);
         tmem_wait_ld();
 #pragma unroll
         for (int e = 0; e < 32; ++e) {
             const int i = 32 * half + e;
-            x[e] = fmaf(-expf((float)G[i]), x[e], v.get(e));                // R
+            x[e] = fmaf(-gamma[i], x[e], v.get(e));                         // R
             y[e] = dz[e] * x[e];
             x[e] *= beta[i];
         }
-        sums[0][warp & 3][32 * half + lane] = column_sum(y, lane);
         planes_to_tmem<PM, 16>(tmem_addr(tb, warp, C::R0 + kTok + half * 16), kTok / 2, x);
         go();
         if (tid == 0) {
             issue_ts<PM, PM, PM, false>(tb + C::R0, tb + C::R0 + kTok, kTok / 2, IA, kMatrix, kTok / 16, kTok, false);
             umma_commit(&ws.bar_a);
         }
-        // the same state, its columns as lanes
-        auto columns = [&](const float *p) {
-            float s[32];
+        sums[0][warp & 3][32 * half + lane] = column_sum(y, lane);
+        // a state with its columns as lanes; `with`: the sum of its products with the one that is there
+        auto columns = [&](const float *p, bool with) {
+            float s[32], inner = 0.f;
 #pragma unroll
             for (int c = 0; c < HC; c += 32) {
 #pragma unroll
                 for (int e = 0; e < 32; ++e) {
                     const int r = half * HC + c + e;
                     s[e] = 0.f;
-                    if (r < a.Dv && row < a.Dk) { HN_G(p + (long long)r * a.Dk + row, 4); s[e] = p[(long long)r * a.Dk + row]; }
+                    if (r < a.Dv && row < a.Dk) {
+                        const int i = kept_at(r, row >> 2, rows8) * 4 + (row & 3);
+                        if (C::ROOM) s[e] = ((const float *)held)[i];
+                        else { HN_G(p + i, 4); s[e] = p[i]; }
+                    }
+                }
+                if (with) {
+                    float o[16];
+#pragma unroll
+                    for (int q = 0; q < PM; ++q) {
+                        TmemIO<16>::ld(o, lane_s + q * (KD / 2) + c / 2);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            inner = fmaf(__uint_as_float(__float_as_uint(o[e]) << 16), s[2 * e], inner);
+                            inner = fmaf(__uint_as_float(__float_as_uint(o[e]) & 0xffff0000u), s[2 * e + 1], inner);
+                        }
+                    }
                 }
                 planes_to_tmem<PM, 16>(lane_s + c / 2, KD / 2, s);
             }
+            return inner;
         };
-        columns(S);
+        columns(S, false);
         done();
         TmemIO<32>::ld(x, lane_r);
         tmem_wait_ld();
         if (row < KD) planes_to_image<PM>(sm + C::U, C::TILE, row, half, x);
         go();
         if (tid == 0) {
+            if (C::ROOM) {                                   // the state has been read: the gradient behind the chunk into its place
+                mbar_expect_tx(&ws.full[1], (unsigned)(kept * 4));
+                bulk_load(sm + C::STATE, D, (unsigned)(kept * 4), &ws.full[1]);
+            }
             // rows 0 .. 63: dY U^T, rows 64 ..: dZ U^T; where dY is one plane, dZ's second goes into a sum of its own
             issue_ss<PI, PM, PM, true, true>(tb + C::R0 + kTok, IY, C::TILE, C::DZ - C::DY, IU, C::TILE, vsteps, kTok, false);
             if (PI < PM) issue_ss<1, 1, PM, true, true>(tb + C::R0 + 5 * kTok, IY + C::TILE, C::TILE, C::DZ - C::DY, IU, C::TILE, vsteps, kTok, false);
@@ -402,7 +463,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(256, 1) delta_gr
         __syncthreads();                                     // every thread's wait is over: A and dZ may go
         {
             const int i = row & 63;
-            const double Gi = G[i];
+            const float Hi = ghi[i], Li = glo[i], bi = beta[i];
             TmemIO<32>::ld(x, lane_r + kTok);
             TmemIO<32>::ld(y, lane_r + 2 * kTok);
             tmem_wait_ld();
@@ -417,11 +478,11 @@ template <typename T, int KD> __global__ void __launch_bounds__(256, 1) delta_gr
 #pragma unroll
             for (int e = 0; e < 32; ++e) {
                 const int c = 32 * half + e;
-                const float r = expf((float)(Gi - G[c]));
+                const float r = ratio(Hi, Li, ghi[c], glo[c]);
                 if (row < kTok) x[e] = c <= i ? r * x[e] : 0.f;
                 else {
                     own += c < i ? x[e] * r * y[e] : 0.f;
-                    x[e] = c < i ? -beta[i] * r * x[e] : 0.f;
+                    x[e] = c < i ? -bi * r * x[e] : 0.f;
                 }
             }
             if (row < kTok) planes_to_image<PM>(sm + C::A, kMatrix, i, half, x);                // F
@@ -435,7 +496,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(256, 1) delta_gr
         tmem_wait_ld();
 #pragma unroll
         for (int e = 0; e < 32; ++e) {
-            const float ga = expf((float)G[32 * half + e]);
+            const float ga = gamma[32 * half + e];
             x[e] *= ga;
             erase[e] *= -ga * beta[32 * half + e];
         }
@@ -445,16 +506,17 @@ template <typename T, int KD> __global__ void __launch_bounds__(256, 1) delta_gr
             issue_ss<PI, PM, PM, false, false>(tb + C::R0 + 2 * kTok, IK, C::TILE, 0, IZ, kMatrix, kTok / 16, kTok, false);     // E k
             umma_commit(&ws.bar_a);
         }
-        done();
-        // queries take dY's place, the gradient behind the chunk the state's
-        load_tile<T>(sm + C::DY, C::TILE, (const T *)a.q, qk, all, a.L, a.Dk, nv, tid, 256);
-        clear_rows(sm + C::DY, C::TILE, PI, a.Dk, KD, tid, 256);
-        columns(D);
-        float inner = 0.f;                                   // <S0, dS1>
-        for (long long e = tid; e < states; e += 256) { HN_G(S + e, 4); HN_G(D + e, 4); inner = fmaf(S[e], D[e], inner); }
+        __syncwarp();
+        if (C::ROOM) WAIT(&ws.full[1], j & 1);
+        float inner = columns(D, true);
 #pragma unroll
         for (int m = 1; m < 32; m <<= 1) inner += __shfl_xor_sync(~0u, inner, m);
         if (lane == 0) total[warp] = inner;
+        if (!C::ROOM) {                                      // queries take dY's place
+            load_tile<T>(sm + C::Q, C::TILE, (const T *)a.q, qk, all, a.L, a.Dk, nv, tid, 256);
+            clear_rows(sm + C::Q, C::TILE, PI, a.Dk, KD, tid, 256);
+        }
+        done();
         TmemIO<32>::ld(y, lane_r + kTok);
         tmem_wait_ld();
 #pragma unroll
@@ -469,38 +531,31 @@ template <typename T, int KD> __global__ void __launch_bounds__(256, 1) delta_gr
         go();
         if (tid == 0) {
             issue_ts<PM, PM, PM, true>(tb + C::R0, tb + C::S0, KD / 2, IU, C::TILE, vsteps, kTok, false);                       // dS1 u
-            issue_ss<PI, PM, PM, false, true>(tb + C::R0 + kTok, IY, C::TILE, 0, IA, kMatrix, kTok / 16, kTok, false);          // F q
+            issue_ss<PI, PM, PM, false, true>(tb + C::R0 + kTok, IQ, C::TILE, 0, IA, kMatrix, kTok / 16, kTok, false);          // F q
             issue_ss<PI, PM, PM, false, true>(tb + C::R0 + kTok, IK, C::TILE, 0, IZ, kMatrix, kTok / 16, kTok, true);           // E k, the other way
             umma_commit(&ws.bar_a);
         }
-        {   // what queries and the erased part say about the decays, meanwhile
-            float z[32];
-            if (row < KD) image_row<PI>(z, sm + C::DY, C::TILE, row, half);
-            else {
-#pragma unroll
-                for (int e = 0; e < 32; ++e) z[e] = 0.f;
-            }
+        __syncwarp();
+        float z[32];
+        {   // what queries say about the decays, meanwhile
+            if (row < KD) image_row<PI>(z, sm + C::Q, C::TILE, row, half);
 #pragma unroll
             for (int e = 0; e < 32; ++e) x[e] = row < a.Dk ? x[e] * z[e] : 0.f;      // (a lane without a channel holds whatever lay behind an image)
+            if (row < KD) image_row<PI>(z, sm + C::K, C::TILE, row, half);
         }
         done();
         {
-            float z[32], w[32];
+            float w[32];
             TmemIO<32>::ld(y, lane_r);
             TmemIO<32>::ld(w, lane_r + kTok);
             tmem_wait_ld();
-            if (row < KD) image_row<PI>(z, sm + C::K, C::TILE, row, half);
-            else {
-#pragma unroll
-                for (int e = 0; e < 32; ++e) z[e] = 0.f;
-            }
 #pragma unroll
             for (int e = 0; e < 32; ++e) {
-                y[e] *= expf((float)(G[kTok - 1] - G[32 * half + e]));
+                y[e] *= delta[32 * half + e];
                 w[e] += y[e];
                 dk[e] += erase[e] + w[e];
                 x[e] = row < a.Dk ? fmaf(z[e], erase[e] - w[e], x[e]) : 0.f;
-                y[e] *= z[e];
+                y[e] = row < a.Dk ? y[e] * z[e] : 0.f;
             }
         }
         sums[1][warp & 3][32 * half + lane] = column_sum(x, lane);
@@ -537,7 +592,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(256, 1) delta_gr
                     const double o = __shfl_down_sync(~0u, run, m);
                     if (lane + m < 32) run += o;
                 }
-                run += (double)fade * in + written;
+                run += (double)gamma[kTok - 1] * in + written;
                 s[0] = (float)run;
                 s[1] = (float)(run - (v - s[1]));
             }
@@ -572,15 +627,17 @@ int delta_backward_status()
     return cudaMemcpyFromSymbol(&v, hn_delta_backward_status, sizeof(int)) == cudaSuccess ? v : -1;
 }
 
-template <typename T, int KD> static int launch_back(const DeltaArgs &a, cudaStream_t st)
+template <typename T, int KD> static int launch_back(DeltaArgs a, cudaStream_t st)
 {
+    DeltaMaps m{};
+    a.copies = delta_maps<T>(m, a, KD);
     const long long blocks = (long long)a.B * a.H * a.segments;
     if (a.segments > 1) {
-        if (const int e = launch_delta<delta_walk_back_kernel<T, KD, WALK_MAPS>>(a, 2 * blocks, 384, WalkBack<T, KD>::BYTES, st)) return e;
+        if (const int e = launch_delta<delta_walk_back_kernel<T, KD, WALK_MAPS>>(a, 2 * blocks, 384, WalkBack<T, KD>::BYTES, st, m)) return e;
         if (const int e = launch_delta_join(a, a.ds_end, true, st)) return e;
     }
-    if (const int e = launch_delta<delta_walk_back_kernel<T, KD, WALK_RUN>>(a, blocks, 384, WalkBack<T, KD>::BYTES, st)) return e;
-    return launch_delta<delta_gradients_kernel<T, KD>>(a, (long long)a.B * a.Hk * a.chunks, 256, Grads<T, KD>::BYTES, st);
+    if (const int e = launch_delta<delta_walk_back_kernel<T, KD, WALK_RUN>>(a, blocks, 384, WalkBack<T, KD>::BYTES, st, m)) return e;
+    return launch_delta<delta_gradients_kernel<T, KD>>(a, (long long)a.B * a.Hk * a.chunks, 256, Grads<T, KD>::BYTES, st, m);
 }
 int launch_delta_backward(const DeltaArgs &a, int dtype, cudaStream_t st)
 {

@@ -123,7 +123,8 @@ def lib() -> ctypes.CDLL:
         L.hyenand_recurrence_workspace_bytes.restype = ll
         L.hyenand_recurrence_workspace_bytes.argtypes = [ci] * 4
         L.hyenand_recurrence_step.argtypes = [ci] * 4 + [vp] * 9
-        L.hyenand_delta_marks.argtypes = [ci]
+        L.hyenand_delta_marks.restype = ll
+        L.hyenand_delta_marks.argtypes = [ci] * 3
         L.hyenand_delta_workspace_bytes.restype = ll
         L.hyenand_delta_workspace_bytes.argtypes = [ci] * 8
         L.hyenand_delta_forward.argtypes = [ci] * 8 + [vp] * 12
@@ -397,8 +398,8 @@ def _ints(values):
     return (ctypes.c_int * len(values))(*(int(n) for n in values))
 
 
-def hyenand_delta_marks(L: int) -> int:
-    return int(lib().hyenand_delta_marks(int(L)))
+def hyenand_delta_marks(L: int, Dk: int, Dv: int) -> int:
+    return int(lib().hyenand_delta_marks(*_ints((L, Dk, Dv))))
 
 
 def hyenand_delta_workspace_bytes(B: int, H: int, Hk: int, L: int, Dk: int, Dv: int, dtype: int, backward: int) -> int:
@@ -695,7 +696,7 @@ class DeltaRule:
         if min(work) < 1:
             raise ValueError(hyenand_last_error())
         self._ops = _calls()
-        self._handle = self._ops.make_delta(self.B, self.H, self.Hk, self.L, self.Dk, self.Dv, hyenand_delta_marks(self.L), code, _DTYPES[dtype], *work,
+        self._handle = self._ops.make_delta(self.B, self.H, self.Hk, self.L, self.Dk, self.Dv, hyenand_delta_marks(self.L, self.Dk, self.Dv), code, _DTYPES[dtype], *work,
                                             _address("hyenand_delta_forward"), _address("hyenand_delta_backward"), _address("hyenand_delta_step"), _check)
 
     def forward(self, q, k, v, g, beta, s0=None, lengths=None, marks: bool = False, y=None, stream=None):
