@@ -71,11 +71,10 @@ template <typename T, int KD> __global__ void __launch_bounds__(128) delta_prepa
     tmem_fence_after_sync();
     const unsigned tb = slot, images = smem_u32(sm);
     bool ok = !copied || mbar_wait(&there, 0);
-    if (tid == 0) {
-        issue_ss<C::PI, C::PI, C::PI, true, true>(tb, images, C::PITCH, C::TILE, images, C::PITCH, steps, kTok, false);
+    if (uniform_warp(warp) == 0) {
+        issue_ss<C::PI, C::PI, C::PI, true, true, KD / 16>(tb, images, C::PITCH, C::TILE, images, C::PITCH, steps, kTok, false);
         umma_commit(&bar);
     }
-    __syncwarp();
     if (tid < kTok) {                                        // (the decays meanwhile)
         float *gates = a.gates + at * kGates;
         const float x[5] = {ratio(hi[tid], lo[tid], 0.f, 0.f), ratio(hi[kTok - 1], lo[kTok - 1], hi[tid], lo[tid]), beta[tid], hi[tid], lo[tid]};
@@ -145,26 +144,31 @@ template <typename T, int KD> __global__ void __launch_bounds__(128) delta_prepa
 
 template <typename T, int KD> struct Walk {
     static constexpr int PI = Planes<T>::IN, PM = Planes<T>::MID, TILE = KD * 128, TENSOR = PI * TILE;
-    static constexpr int IMAGES = 2 * PM * kMatrix;
-    static constexpr int STAGE = 2 * TENSOR + IMAGES + 1024;                  // K, Q, A, P, gates
-    static constexpr int STAGES = 3 * STAGE <= 220 * 1024 ? 3 : 2 * STAGE <= 220 * 1024 ? 2 : 1;
-    static constexpr int BYTES = 1024 + STAGES * STAGE;
-    // tensor memory: S (later delta U) as an operand | Z, later U, as an operand | sums | Y
-    static constexpr int SCOLS = PM * KD / 2, ZCOLS = PM * kTok / 2, S0 = 0, Z0 = SCOLS, X0 = Z0 + ZCOLS, Y0 = X0 + (KD > kTok ? KD : kTok);
-    static_assert(Y0 + kTok <= 512, "tensor memory");
+    static constexpr bool VALUES = PI == 1;                                   // values and results travel as images
+    static constexpr int IMAGES = 2 * PM * kMatrix, K = 0, Q = TENSOR, A = 2 * TENSOR, V = A + IMAGES, GATES = V + (VALUES ? TILE : 0), STAGE = GATES + 1024;
+    static constexpr int OUT = VALUES ? 2 * TILE : 0;                         // two images of results
+    static constexpr int STAGES = 3 * STAGE + OUT <= 220 * 1024 ? 3 : 2 * STAGE + OUT <= 220 * 1024 ? 2 : 1;
+    static constexpr int BYTES = 1024 + STAGES * STAGE + OUT;
+    // tensor memory: S (later delta U) as an operand | Z, later U, as an operand | S k and S q, then U in the first's place | what S gains
+    static constexpr int SCOLS = PM * KD / 2, ZCOLS = PM * kTok / 2, S0 = 0, Z0 = SCOLS, X0 = Z0 + ZCOLS, Y0 = X0 + kTok;
+    // (with three planes of 128 columns its first half goes where U was)
+    static constexpr bool ROOM = Y0 + kTok + KD <= 512;
+    static constexpr int D0 = ROOM ? Y0 + kTok : X0, D1 = ROOM ? D0 + KD / 2 : Y0 + kTok;
+    static_assert(D1 + KD / 2 <= 512 && (ROOM || KD / 2 == kTok), "tensor memory");
 };
 
-template <typename T, int KD, int MODE> __global__ void __launch_bounds__(384, 1) delta_walk_kernel(DeltaArgs a, const __grid_constant__ DeltaMaps maps)
+template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkThreads, 1) delta_walk_kernel(DeltaArgs a, const __grid_constant__ DeltaMaps maps)
 {
     using C = Walk<T, KD>;
     constexpr int PI = C::PI, PM = C::PM, HC = KD / 2;
+    constexpr bool RUN = MODE == WALK_RUN;
     extern __shared__ __align__(1024) unsigned char raw[];
     __shared__ WalkShared ws;
     unsigned char *sm = align_images(raw);
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, lane = tid & 31, warp = uniform_warp(tid >> 5);
     long long id = blockIdx.x;
-    const bool phi = MODE == WALK_MAPS && (id & 1);          // from the identity, without values
-    if (MODE == WALK_MAPS) id >>= 1;
+    const bool phi = !RUN && (id & 1);                       // from the identity, without values
+    if (!RUN) id >>= 1;
     const long long bh = id / a.segments;
     const int segment = (int)(id % a.segments), b = (int)(bh / a.H), h = (int)(bh % a.H);
     pdl_wait();
@@ -173,54 +177,93 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(384, 1
     last = last < end ? last : end;
     if (warp == 0) tmem_alloc(smem_u32(&ws.slot), 512);
     if (tid == 0) {
-        for (int s = 0; s < C::STAGES; ++s) { mbar_init(&ws.full[s], 129); mbar_init(&ws.empty[s], 1); }
-        mbar_init(&ws.bar_a, 1); mbar_init(&ws.bar_b, 1); mbar_init(&ws.bar_c, 1); mbar_init(&ws.bar_q, 1); mbar_init(&ws.bar_y, 1);
+        for (int s = 0; s < C::STAGES; ++s) { mbar_init(&ws.full[s], kFetchers + 1); mbar_init(&ws.empty[s], 1); }
+        mbar_init(&ws.bar_a, 1); mbar_init(&ws.bar_b, 1); mbar_init(&ws.bar_c, 1); mbar_init(&ws.bar_y, 1); mbar_init(&ws.ready, 8);
         ws.gave_up = 0;
         fence_mbar_init();
     }
-    for (int s = 0; s < C::STAGES; ++s) clear_rows(sm + s * C::STAGE, C::TILE, 2 * PI, a.Dk, KD, tid, 384);
+    for (int s = 0; s < C::STAGES; ++s) {
+        clear_rows(sm + s * C::STAGE, C::TILE, 2 * PI, a.Dk, KD, tid, kWalkThreads);
+        if (C::VALUES) clear_rows(sm + s * C::STAGE + C::V, C::TILE, 1, phi ? 0 : a.Dv, KD, tid, kWalkThreads);
+    }
     fence_async_smem();
     tmem_fence_before_sync();
     __syncthreads();
     tmem_fence_after_sync();
     const unsigned tb = ws.slot;
-    const int steps = (a.Dk + 15) / 16;
-    if (warp >= 8) {
-        // ---- the four warps that fetch
-        const int ft = tid - 256;
+    const long long states = (long long)a.Dv * a.Dk, vhead = bh * a.Dv * a.L, vall = (long long)a.B * a.H * a.Dv * a.L;
+    if (warp > 8) {
+        // ---- fetching
+        const int ft = tid - 288;
         const long long bk = (long long)b * a.Hk + h / (a.H / a.Hk), qk = bk * a.Dk * a.L, all = (long long)a.B * a.Hk * a.Dk * a.L;
         for (int c = first, i = 0; c < last; ++c, ++i) {
             const int s = i % C::STAGES, t0 = c * kTok, nv = n - t0 < kTok ? n - t0 : kTok;
             if (i >= C::STAGES) WAIT(&ws.empty[s], (i / C::STAGES - 1) & 1);
             unsigned char *st = sm + s * C::STAGE;
-            const bool copied = by_copy(a, nv, t0);
+            const bool copied = by_copy(a, nv, t0), values = C::VALUES && !phi;
             if (ft == 0) {
                 const long long at = bh * a.chunks + c;
-                const unsigned bytes = MODE == WALK_MAPS ? PM * kMatrix : 2 * PM * kMatrix, tiles = !copied ? 0 : MODE == WALK_MAPS ? C::TENSOR : 2 * C::TENSOR;
+                const unsigned bytes = RUN ? C::IMAGES : C::IMAGES / 2, tiles = copied ? (RUN ? 2 : 1) * C::TENSOR + (values ? C::TILE : 0) : 0;
                 mbar_expect_tx(&ws.full[s], bytes + kWalkGates + tiles);
-                if (copied) tma_load_3d(st, &maps.k, &ws.full[s], t0, 0, (int)bk);
-                if (copied && MODE != WALK_MAPS) tma_load_3d(st + C::TENSOR, &maps.q, &ws.full[s], t0, 0, (int)bk);
-                bulk_load(st + 2 * C::TENSOR, a.images + at * C::IMAGES, bytes, &ws.full[s]);
-                bulk_load(st + 2 * C::TENSOR + C::IMAGES, a.gates + at * kGates, kWalkGates, &ws.full[s]);
+                if (copied) {
+                    tma_load_3d(st, &maps.k, &ws.full[s], t0, 0, (int)bk);
+                    if (RUN) tma_load_3d(st + C::Q, &maps.q, &ws.full[s], t0, 0, (int)bk);
+                    if (values) tma_load_3d(st + C::V, &maps.v, &ws.full[s], t0, 0, (int)bh);
+                }
+                bulk_load(st + C::A, a.images + at * C::IMAGES, bytes, &ws.full[s]);
+                bulk_load(st + C::GATES, a.gates + at * kGates, kWalkGates, &ws.full[s]);
             }
             if (!copied) {
-                load_tile<T>(st, C::TILE, (const T *)a.k, qk + t0, all, a.L, a.Dk, nv, ft, 128);
-                if (MODE != WALK_MAPS) load_tile<T>(st + C::TENSOR, C::TILE, (const T *)a.q, qk + t0, all, a.L, a.Dk, nv, ft, 128);
+                load_tile<T>(st, C::TILE, (const T *)a.k, qk + t0, all, a.L, a.Dk, nv, ft, kFetchers);
+                if (RUN) load_tile<T>(st + C::Q, C::TILE, (const T *)a.q, qk + t0, all, a.L, a.Dk, nv, ft, kFetchers);
+                if constexpr (C::VALUES)
+                    if (values) load_tile<T>(st + C::V, C::TILE, (const T *)a.v, vhead + t0, vall, a.L, a.Dv, nv, ft, kFetchers);
             }
             fence_async_smem();
             mbar_arrive(&ws.full[s]);
         }
+    } else if (warp == 8) {
+        // ---- the products
+        const int steps = (a.Dk + 15) / 16;
+        unsigned par = 0;
+        for (int c = first, i = 0; c < last; ++c, ++i) {
+            const int s = i % C::STAGES;
+            const unsigned k = smem_u32(sm) + s * C::STAGE, A = k + C::A, P = A + PM * kMatrix;
+            WAIT(&ws.full[s], (i / C::STAGES) & 1);
+            WAIT(&ws.ready, par); par ^= 1;                                     // S is there, and the results of the chunk before are taken
+            tmem_fence_after_sync();
+            issue_ts<PM, PI, PM, true, KD / 16>(tb + C::X0, tb + C::S0, KD / 2, k, C::TILE, steps, RUN ? 2 * kTok : kTok, false, C::Q);
+            umma_commit(&ws.bar_a);
+            WAIT(&ws.ready, par); par ^= 1;                                     // Z
+            tmem_fence_after_sync();
+            issue_ts<PM, PM, PM, false, kTok / 16, B_LOWER>(tb + C::X0, tb + C::Z0, kTok / 2, A, kMatrix, kTok / 16, kTok, false);
+            umma_commit(&ws.bar_b);
+            WAIT(&ws.ready, par); par ^= 1;                                     // U, delta U
+            tmem_fence_after_sync();
+            if (C::ROOM) issue_ts<PM, PI, PM, false, kTok / 16>(tb + C::D0, tb + C::S0, kTok / 2, k, C::TILE, kTok / 16, KD, false);
+            else {
+                issue_ts<PM, PI, PM, false, kTok / 16>(tb + C::D0, tb + C::S0, kTok / 2, k, C::TILE, kTok / 16, KD / 2, false);
+                issue_ts<PM, PI, PM, false, kTok / 16>(tb + C::D1, tb + C::S0, kTok / 2, k + KD / 2 * 128, C::TILE, kTok / 16, KD / 2, false);
+            }
+            umma_commit(&ws.bar_c);
+            if (RUN) {
+                issue_ts<PM, PM, PM, false, kTok / 16, B_LOWER>(tb + C::Y0, tb + C::Z0, kTok / 2, P, kMatrix, kTok / 16, kTok, true);
+                umma_commit(&ws.bar_y);
+            }
+            umma_commit(&ws.empty[s]);
+        }
     } else {
-        // ---- the eight that compute: lane of tensor memory = row of the state, `half` = which half of the columns
+        // ---- computing: lane of tensor memory = row of the state, `half` = which half of the columns
         const int row = 32 * (warp & 3) + lane, half = warp >> 2, rows = phi ? a.Dk : a.Dv;
         const unsigned lane_s = tmem_addr(tb, warp, C::S0 + half * (HC / 2)), lane_z = tmem_addr(tb, warp, C::Z0 + half * 16),
-                       lane_x = tmem_addr(tb, warp, C::X0), lane_y = tmem_addr(tb, warp, C::Y0 + half * 32);
-        const long long vrow = (bh * a.Dv + row) * a.L, vall = (long long)a.B * a.H * a.Dv * a.L, states = (long long)a.Dv * a.Dk;
-        const bool real = row < a.Dv;
-        float S[HC];
+                       lane_x = tmem_addr(tb, warp, C::X0 + half * 32), lane_y = tmem_addr(tb, warp, C::Y0 + half * 32), lane_d = tmem_addr(tb, warp, half ? C::D1 : C::D0);
+        const long long vrow = vhead + (long long)row * a.L;
+        const bool real = row < a.Dv, stored = C::VALUES && a.copies;
+        unsigned char *out = sm + C::STAGES * C::STAGE;
+        float S[HC], x[32], y[32];
 #pragma unroll
         for (int i = 0; i < HC; ++i) S[i] = 0.f;
-        if (MODE == WALK_MAPS) {
+        if (!RUN) {
             if (phi) {
 #pragma unroll
                 for (int i = 0; i < HC; ++i) S[i] = row == half * HC + i && row < a.Dk ? 1.f : 0.f;
@@ -229,141 +272,123 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(384, 1
             const float *from = a.segments > 1 ? a.starts + (bh * a.segments + segment) * states : a.s0 ? a.s0 + bh * states : nullptr;
             if (from) load_state<HC>(S, from, row, a.Dv, half * HC, a.Dk);
         }
-        RowPart<T> v;
-        auto fetch_v = [&](int c) {
-            const int t = c * kTok + 32 * half;
-            v.load((const T *)a.v, vrow + t, vall, a.L, real && !phi ? n - t : 0);
-        };
+        // results of chunk c, from y: as an image that a copy takes away, or by their threads
         auto put_y = [&](int c) {
-            float y[32];
-            TmemIO<32>::ld(y, lane_y);
-            tmem_wait_ld();
             const int t = c * kTok + 32 * half;
-            if (real && t < a.L) store_row<T>((T *)a.y, vrow + t, a.L, a.L - t, n - t, y);
-        };
-        if (first < last) fetch_v(first);
-        for (int c = first, i = 0; c < last; ++c, ++i) {
-            const int s = i % C::STAGES;
-            const unsigned par = i & 1;
-            unsigned char *st = sm + s * C::STAGE;
-            const unsigned k = smem_u32(st), q = k + C::TENSOR, A = q + C::TENSOR, P = A + PM * kMatrix;
-            const float *gates = (const float *)(st + 2 * C::TENSOR + C::IMAGES);
-            if (MODE != WALK_MAPS && a.marks) keep_state<HC>(a.marks + (bh * a.chunks + c) * kept_floats(a.Dv, a.Dk), S, row, a.Dv, half * HC, a.Dk);
-            planes_to_tmem<PM, HC / 2>(lane_s, KD / 2, S);
-            tmem_wait_st();
-            tmem_fence_before_sync();
-            WAIT(&ws.full[s], (i / C::STAGES) & 1);
-            walkers_sync();
-            if (tid == 0) {
-                tmem_fence_after_sync();
-                issue_ts<PM, PI, PM, true>(tb + C::X0, tb + C::S0, KD / 2, k, C::TILE, steps, kTok, false);
-                umma_commit(&ws.bar_a);
-            }
-            __syncwarp();
-            if (MODE != WALK_MAPS) {
-                if (i) {
-                    WAIT(&ws.bar_y, par ^ 1);
-                    tmem_fence_after_sync();
-                    put_y(c - 1);
-                    tmem_fence_before_sync();
-                }
+            if (stored) {
+                unsigned char *image = out + (c & 1) * C::TILE;
+                if (row < KD) row_to_image(image, row, half, n - t, y);
+                fence_async_smem();
                 walkers_sync();
                 if (tid == 0) {
-                    tmem_fence_after_sync();
-                    issue_ts<PM, PI, PM, true>(tb + C::Y0, tb + C::S0, KD / 2, q, C::TILE, steps, kTok, false);
-                    umma_commit(&ws.bar_q);
+                    tma_store_3d(&maps.out, image, c * kTok, 0, (int)bh);
+                    tma_commit();
+                    tma_wait_read1();                        // the other image is free again once thread 0 has been here
                 }
                 __syncwarp();
+            } else if (real && t < a.L) store_row<T>((T *)a.y, vrow + t, a.L, a.L - t, n - t, y);
+        };
+        for (int c = first, i = 0; c < last; ++c, ++i) {
+            const int s = i % C::STAGES, t = c * kTok + 32 * half;
+            const unsigned par = i & 1;
+            const unsigned char *st = sm + s * C::STAGE;
+            const float *gates = (const float *)(st + C::GATES) + 32 * half;
+            planes_to_tmem<PM, HC / 2>(lane_s, KD / 2, S);
+            if (RUN && i) {
+                WAIT(&ws.bar_y, par ^ 1);
+                tmem_fence_after_sync();
+                TmemIO<32>::ld(y, lane_y);
+                tmem_wait_ld();
             }
-            float x[32];
+            tmem_wait_st();
+            tmem_fence_before_sync();
+            walk_ready(&ws, lane);
+            RowPart<T> v;
+            if constexpr (!C::VALUES) v.load((const T *)a.v, vrow + t, vall, a.L, real && !phi ? n - t : 0);
+            if (RUN && i) put_y(c - 1);
+            if (RUN && a.marks) keep_state<HC>(a.marks + (bh * a.chunks + c) * kept_floats(a.Dv, a.Dk), S, row, a.Dv, half * HC, a.Dk);
+            WAIT(&ws.full[s], (i / C::STAGES) & 1);
+            float w[32];
+            if constexpr (C::VALUES) {
+                if (row < KD) image_row<1>(w, st + C::V, C::TILE, row, half);
+                else {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) w[e] = 0.f;
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 32; ++e) w[e] = v.get(e);
+            }
             WAIT(&ws.bar_a, par);
             tmem_fence_after_sync();
-            TmemIO<32>::ld(x, lane_x + 32 * half);
+            TmemIO<32>::ld(x, lane_x);
             tmem_wait_ld();
 #pragma unroll
             for (int e = 0; e < 32; e += 4) {
-                const float4 ga = *(const float4 *)(gates + 32 * half + e), be = *(const float4 *)(gates + 2 * kTok + 32 * half + e);
-                x[e] = be.x * fmaf(-ga.x, x[e], v.get(e));
-                x[e + 1] = be.y * fmaf(-ga.y, x[e + 1], v.get(e + 1));
-                x[e + 2] = be.z * fmaf(-ga.z, x[e + 2], v.get(e + 2));
-                x[e + 3] = be.w * fmaf(-ga.w, x[e + 3], v.get(e + 3));
+                const float4 ga = *(const float4 *)(gates + e), be = *(const float4 *)(gates + 2 * kTok + e);
+                x[e] = be.x * fmaf(-ga.x, x[e], w[e]);
+                x[e + 1] = be.y * fmaf(-ga.y, x[e + 1], w[e + 1]);
+                x[e + 2] = be.z * fmaf(-ga.z, x[e + 2], w[e + 2]);
+                x[e + 3] = be.w * fmaf(-ga.w, x[e + 3], w[e + 3]);
             }
             planes_to_tmem<PM, 16>(lane_z, kTok / 2, x);
             tmem_wait_st();
             tmem_fence_before_sync();
-            walkers_sync();
-            if (tid == 0) {
-                tmem_fence_after_sync();
-                issue_ts<PM, PM, PM, false>(tb + C::X0, tb + C::Z0, kTok / 2, A, kMatrix, kTok / 16, kTok, false);
-                umma_commit(&ws.bar_b);
-            }
-            __syncwarp();
-            if (c + 1 < last) fetch_v(c + 1);
-            if (MODE != WALK_MAPS) {                         // y's first sum by gamma, while A Z is formed
-                WAIT(&ws.bar_q, par);
-                tmem_fence_after_sync();
-                TmemIO<32>::ld(x, lane_y);
+            walk_ready(&ws, lane);
+            if (RUN) {                                       // y's first sum by gamma, while A Z is formed
+                TmemIO<32>::ld(y, lane_y);
                 tmem_wait_ld();
 #pragma unroll
                 for (int e = 0; e < 32; e += 4) {
-                    const float4 ga = *(const float4 *)(gates + 32 * half + e);
-                    x[e] *= ga.x; x[e + 1] *= ga.y; x[e + 2] *= ga.z; x[e + 3] *= ga.w;
+                    const float4 ga = *(const float4 *)(gates + e);
+                    y[e] *= ga.x; y[e + 1] *= ga.y; y[e + 2] *= ga.z; y[e + 3] *= ga.w;
                 }
-                TmemIO<32>::st(lane_y, x);
+                TmemIO<32>::st(lane_y, y);
             }
             WAIT(&ws.bar_b, par);
             tmem_fence_after_sync();
-            TmemIO<32>::ld(x, lane_x + 32 * half);
+            TmemIO<32>::ld(x, lane_x);
             tmem_wait_ld();
-            if (MODE != WALK_MAPS) planes_to_tmem<PM, 16>(lane_z, kTok / 2, x);
+            if (RUN) planes_to_tmem<PM, 16>(lane_z, kTok / 2, x);
 #pragma unroll
             for (int e = 0; e < 32; e += 4) {
-                const float4 de = *(const float4 *)(gates + kTok + 32 * half + e);
+                const float4 de = *(const float4 *)(gates + kTok + e);
                 x[e] *= de.x; x[e + 1] *= de.y; x[e + 2] *= de.z; x[e + 3] *= de.w;
             }
             planes_to_tmem<PM, 16>(tmem_addr(tb, warp, C::S0 + half * 16), kTok / 2, x);
-            const float fade = gates[kTok - 1];
+            const float fade = ((const float *)(st + C::GATES))[kTok - 1];
             tmem_wait_st();
             tmem_fence_before_sync();
-            walkers_sync();
-            if (tid == 0) {
-                tmem_fence_after_sync();
-                issue_ts<PM, PI, PM, false>(tb + C::X0, tb + C::S0, kTok / 2, k, C::TILE, kTok / 16, KD, false);
-                umma_commit(&ws.bar_c);
-                if (MODE != WALK_MAPS) {
-                    issue_ts<PM, PM, PM, false>(tb + C::Y0, tb + C::Z0, kTok / 2, P, kMatrix, kTok / 16, kTok, true);
-                    umma_commit(&ws.bar_y);
-                }
-                umma_commit(&ws.empty[s]);
-            }
-            __syncwarp();
+            walk_ready(&ws, lane);
             WAIT(&ws.bar_c, par);
             tmem_fence_after_sync();
 #pragma unroll
             for (int e = 0; e < HC; e += 32) {
-                TmemIO<32>::ld(x, lane_x + half * HC + e);
+                TmemIO<32>::ld(x, lane_d + e);
                 tmem_wait_ld();
 #pragma unroll
                 for (int j = 0; j < 32; ++j) S[e + j] = fmaf(fade, S[e + j], x[j]);
             }
         }
-        if (MODE == WALK_MAPS) {
+        if (!RUN) {
             float *to = a.maps + (bh * a.segments + segment) * (long long)(a.Dv + a.Dk) * a.Dk + (phi ? states : 0);
             store_state<HC>(to, S, row, rows, half * HC, a.Dk);
         } else {
             if (first < last) {
                 WAIT(&ws.bar_y, (last - first - 1) & 1);
                 tmem_fence_after_sync();
+                TmemIO<32>::ld(y, lane_y);
+                tmem_wait_ld();
                 put_y(last - 1);
             }
-            float none[32];
 #pragma unroll
-            for (int e = 0; e < 32; ++e) none[e] = 0.f;
+            for (int e = 0; e < 32; ++e) y[e] = 0.f;
             for (int c = first > last ? first : last; c < end; ++c) {
                 const int t = c * kTok + 32 * half;
-                if (real && t < a.L) store_row<T>((T *)a.y, vrow + t, a.L, a.L - t, 0, none);
+                if (real && t < a.L) store_row<T>((T *)a.y, vrow + t, a.L, a.L - t, 0, y);
             }
             if (a.s_end && segment == a.segments - 1) store_state<HC>(a.s_end + bh * states, S, row, a.Dv, half * HC, a.Dk);
+            if (stored && tid == 0) tma_wait_all0();
         }
         tmem_fence_before_sync();
     }
@@ -536,7 +561,7 @@ template <typename T> static int launch_prepare(DeltaArgs a, cudaStream_t st)
 {
     const long long blocks = (long long)a.B * a.H * a.chunks;
     DeltaMaps m{};
-    a.copies = delta_maps<T>(m, a, a.Dk <= 64 ? 64 : 128);
+    a.copies = delta_maps<T>(m, a, a.Dk <= 64 ? 64 : 128, a.v, nullptr);
     return a.Dk <= 64 ? launch_delta<delta_prepare_kernel<T, 64>>(a, blocks, 128, Prep<T, 64>::BYTES, st, m)
                       : launch_delta<delta_prepare_kernel<T, 128>>(a, blocks, 128, Prep<T, 128>::BYTES, st, m);
 }
@@ -553,18 +578,18 @@ int launch_delta_join(const DeltaArgs &a, const float *from, bool backward, cuda
 template <typename T, int KD> static int launch_walk(DeltaArgs a, cudaStream_t st)
 {
     DeltaMaps m{};
-    a.copies = delta_maps<T>(m, a, KD);
+    a.copies = delta_maps<T>(m, a, KD, a.v, a.y);
     const long long blocks = (long long)a.B * a.H * a.segments;
     if (a.segments > 1) {
-        if (const int e = launch_delta<delta_walk_kernel<T, KD, WALK_MAPS>>(a, 2 * blocks, 384, Walk<T, KD>::BYTES, st, m)) return e;
+        if (const int e = launch_delta<delta_walk_kernel<T, KD, WALK_MAPS>>(a, 2 * blocks, kWalkThreads, Walk<T, KD>::BYTES, st, m)) return e;
         if (const int e = launch_delta_join(a, a.s0, false, st)) return e;
     }
-    return launch_delta<delta_walk_kernel<T, KD, WALK_RUN>>(a, blocks, 384, Walk<T, KD>::BYTES, st, m);
+    return launch_delta<delta_walk_kernel<T, KD, WALK_RUN>>(a, blocks, kWalkThreads, Walk<T, KD>::BYTES, st, m);
 }
 template <typename T> static int launch_forward(const DeltaArgs &a, cudaStream_t st)
 {
     if (const int e = launch_prepare<T>(a, st)) return e;
-    return a.Dk <= 64 ? launch_walk<T, 64>(a, st) : launch_walk<T, 128>(a, st);
+    return a.Dk <= 64 && a.Dv <= 64 ? launch_walk<T, 64>(a, st) : launch_walk<T, 128>(a, st);
 }
 template <typename T> static int launch_step(const DeltaArgs &a, cudaStream_t st)
 {

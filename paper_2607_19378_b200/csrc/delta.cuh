@@ -331,6 +331,22 @@ template <int C> __device__ __forceinline__ void store_state(float *p, const flo
     }
 }
 
+// 32 tokens of a row as an image of a bf16 tensor's tile, zero from token nv on
+__device__ __forceinline__ void row_to_image(unsigned char *image, int row, int half, int nv, const float (&x)[32])
+{
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        unsigned u[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int e = 8 * c + 2 * i;
+            const __nv_bfloat162 r = __floats2bfloat162_rn(e < nv ? x[e] : 0.f, e + 1 < nv ? x[e + 1] : 0.f);
+            u[i] = *(const unsigned *)&r;
+        }
+        *(uint4 *)(image + image_at(row, half * 4 + c)) = make_uint4(u[0], u[1], u[2], u[3]);
+    }
+}
+
 // ---- a chunk's decays ---------------------------------------------------------------------------------------------------
 
 // log a.  Below -110 the factor is zero in fp32: the sum of a chunk stays small enough for differences.  A NaN stays one.
@@ -370,41 +386,55 @@ __device__ __forceinline__ float ratio(float hi, float lo, float hj, float lj) {
 
 // ---- products ------------------------------------------------------------------------------------------------------------
 
+// The rows of B that a product needs at step k of its contraction: all of them; for a lower triangle of 64 x 64 taken by rows (i >= j)
+// those from 16 k on, taken by columns (j <= i) those below 16 (k + 1)
+enum { B_ALL = 0, B_LOWER = 1, B_LOWER_T = 2 };
+
 // d (+)= sum of the products of planes p of A (tensor memory, `pa` columns apart) and q of B (images, `pb` bytes apart), p < NA, q < NB,
-// p + q < MAX, over `steps` 16-steps; the smallest first (the sums are cut off, not rounded, at every instruction)
-template <int NA, int NB, int MAX, bool BCOLS> __device__ __forceinline__ void issue_ts(unsigned d, unsigned a, int pa, unsigned b, int pb, int steps, int n, bool add)
+// p + q < MAX, over the first `steps` of STEPS 16-steps; the smallest first (the sums are cut off, not rounded, at every instruction)
+template <int NA, int NB, int MAX, bool BCOLS, int STEPS, int PART = B_ALL>
+__device__ __forceinline__ void issue_ts(unsigned d, unsigned a, int pa, unsigned b, int pb, int steps, int n, bool add, unsigned next = 1024)
 {
-    const unsigned kind = umma_kind(n, false, BCOLS);
 #pragma unroll
     for (int sum = MAX - 1; sum >= 0; --sum)
 #pragma unroll
         for (int p = 0; p <= sum; ++p)
             if (const int q = sum - p; p < NA && q < NB)
-                for (int k = 0; k < steps; ++k) {
-                    umma_ts(d, a + p * pa + k * 8, BCOLS ? umma_cols(b + q * pb, k) : umma_rows(b + q * pb, k), kind, add);
+#pragma unroll
+                for (int e = 0; e < STEPS; ++e) {
+                    const int k = PART == B_LOWER_T ? STEPS - 1 - e : e, from = PART == B_LOWER ? 16 * k : 0, cols = PART == B_ALL ? n : PART == B_LOWER ? kTok - 16 * k : 16 * (k + 1);
+                    if (k >= steps) continue;
+                    umma_ts(d + from, a + p * pa + k * 8, BCOLS ? umma_cols(b + q * pb, k, next) : umma_rows(b + q * pb, k, from), umma_kind(cols, false, BCOLS), add);
                     add = true;
                 }
 }
 // the same with A in images; `next`: see umma_cols
-template <int NA, int NB, int MAX, bool ACOLS, bool BCOLS> __device__ __forceinline__ void issue_ss(unsigned d, unsigned a, int pa, unsigned next, unsigned b, int pb, int steps, int n, bool add)
+template <int NA, int NB, int MAX, bool ACOLS, bool BCOLS, int STEPS, int PART = B_ALL>
+__device__ __forceinline__ void issue_ss(unsigned d, unsigned a, int pa, unsigned next, unsigned b, int pb, int steps, int n, bool add)
 {
-    const unsigned kind = umma_kind(n, ACOLS, BCOLS);
 #pragma unroll
     for (int sum = MAX - 1; sum >= 0; --sum)
 #pragma unroll
         for (int p = 0; p <= sum; ++p)
             if (const int q = sum - p; p < NA && q < NB)
-                for (int k = 0; k < steps; ++k) {
-                    umma_ss(d, ACOLS ? umma_cols(a + p * pa, k, next) : umma_rows(a + p * pa, k), BCOLS ? umma_cols(b + q * pb, k) : umma_rows(b + q * pb, k), kind, add);
+#pragma unroll
+                for (int e = 0; e < STEPS; ++e) {
+                    const int k = PART == B_LOWER_T ? STEPS - 1 - e : e, from = PART == B_LOWER ? 16 * k : 0, cols = PART == B_ALL ? n : PART == B_LOWER ? kTok - 16 * k : 16 * (k + 1);
+                    if (k >= steps) continue;
+                    umma_ss(d + from, ACOLS ? umma_cols(a + p * pa, k, next) : umma_rows(a + p * pa, k),
+                            BCOLS ? umma_cols(b + q * pb, k) : umma_rows(b + q * pb, k, from), umma_kind(cols, ACOLS, BCOLS), add);
                     add = true;
                 }
 }
+
+// the warp's number, as a value that the compiler knows to be the same in all its lanes (see umma.cuh)
+__device__ __forceinline__ int uniform_warp(int warp) { return __shfl_sync(~0u, warp, 0); }
 
 // ---- walks -----------------------------------------------------------------------------------------------------------
 
 // What the warps of a walk share beside the stages.  A wait that gives up ends all later ones of the CTA.
 struct WalkShared {
-    uint64_t full[4], empty[4], bar_a, bar_b, bar_c, bar_q, bar_y;
+    uint64_t full[4], empty[4], bar_a, bar_b, bar_c, bar_y, ready;
     unsigned slot;
     int gave_up;
 };
@@ -415,7 +445,15 @@ __device__ __forceinline__ void walk_wait(WalkShared *w, uint64_t *bar, unsigned
     if (!mbar_wait(bar, parity)) { *f = 1; atomicExch(status, 1); }
 }
 __device__ __forceinline__ void mbar_arrive(uint64_t *bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];\n" ::"r"(smem_u32(bar)) : "memory"); }
-__device__ __forceinline__ void walkers_sync() { asm volatile("bar.sync 1, 256;\n" ::: "memory"); }
+// Warps 0 .. 7 compute, warp 8 issues the products, the others fetch.  What the eight wrote is handed to warp 8 by `ready`; what it gives
+// back they see by the products' barriers.
+constexpr int kWalkThreads = 384, kFetchers = kWalkThreads - 288;
+__device__ __forceinline__ void walk_ready(WalkShared *w, int lane)
+{
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&w->ready);
+}
+__device__ __forceinline__ void walkers_sync() { asm volatile("bar.sync 2, 256;\n" ::: "memory"); }
 
 __device__ __forceinline__ unsigned char *align_images(unsigned char *p) { return p + ((1024u - (smem_u32(p) & 1023u)) & 1023u); }
 
@@ -425,12 +463,12 @@ enum { WALK_RUN = 0, WALK_MAPS = 1 };
 
 // Tiles of bf16 tensors whose rows start on 16 bytes come as tensor copies: rows behind a head's channels and tokens behind L arrive as
 // zeros.  Others, and a chunk that ends before L, are fetched by threads (load_tile).
-struct DeltaMaps { CUtensorMap k, q, dy; };
+struct DeltaMaps { CUtensorMap k, q, v, out; };            // v: values, or dy; out: y, or dv
 __device__ __forceinline__ bool by_copy(const DeltaArgs &a, int nv, int t0) { return a.copies && (nv == kTok || t0 + nv == a.L); }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
 
-template <typename T> static bool delta_maps(DeltaMaps &m, const DeltaArgs &a, int rows)
+template <typename T> static bool delta_maps(DeltaMaps &m, const DeltaArgs &a, int rows, const void *v, const void *out)
 {
     if (sizeof(T) != 2 || a.L % 8 || !tma_available()) return false;
     auto one = [&](CUtensorMap *map, const void *p, int D, long long heads) {
@@ -439,7 +477,8 @@ template <typename T> static bool delta_maps(DeltaMaps &m, const DeltaArgs &a, i
         const unsigned box[3] = {(unsigned)kTok, (unsigned)rows, 1};
         return tma_encode_3d_cached(map, p, true, dims, strides, box, 128);
     };
-    return one(&m.k, a.k, a.Dk, (long long)a.B * a.Hk) && one(&m.q, a.q, a.Dk, (long long)a.B * a.Hk) && (!a.dy || one(&m.dy, a.dy, a.Dv, (long long)a.B * a.H));
+    const long long keys = (long long)a.B * a.Hk, values = (long long)a.B * a.H;
+    return one(&m.k, a.k, a.Dk, keys) && one(&m.q, a.q, a.Dk, keys) && one(&m.v, v, a.Dv, values) && (!out || one(&m.out, out, a.Dv, values));
 }
 
 struct DeltaSizes { size_t images, gates, maps, starts, dstates, dz, all; };          // bytes of the parts of a workspace, in this order

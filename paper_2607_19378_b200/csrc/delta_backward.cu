@@ -18,28 +18,32 @@ static __device__ int hn_delta_backward_status;
 
 template <typename T, int KD> struct WalkBack {
     static constexpr int PI = Planes<T>::IN, PM = Planes<T>::MID, TILE = KD * 128, TENSOR = PI * TILE;
-    static constexpr int IMAGES = 2 * PM * kMatrix;
-    static constexpr int STAGE = 3 * TENSOR + IMAGES + 1024;                  // K, Q, dY, A, P, gates
-    static constexpr int STAGES = 3 * STAGE <= 220 * 1024 ? 3 : 2 * STAGE <= 220 * 1024 ? 2 : 1;
+    static constexpr bool VALUES = PI == 1;                                   // dV travels as an image
+    static constexpr int IMAGES = 2 * PM * kMatrix, K = 0, Q = TENSOR, DY = 2 * TENSOR, A = 3 * TENSOR, GATES = A + IMAGES, STAGE = GATES + 1024;
+    static constexpr int OUT = VALUES ? 2 * TILE : 0;
     // (the product of dY and P takes 128 rows of dY's image: with 64 it reads on into the images that follow, for rows nothing looks at)
-    static constexpr int BYTES = 1024 + STAGES * STAGE;
-    // tensor memory: dS, later gamma dY, as operands | dU, later -gamma beta dZ | sums | P^T dY
-    static constexpr int SCOLS = PM * KD / 2 > PM * kTok / 2 ? PM * KD / 2 : PM * kTok / 2, ZCOLS = PM * kTok / 2, S0 = 0, Z0 = SCOLS, X0 = Z0 + ZCOLS,
-                         Y0 = X0 + (KD > kTok ? KD : kTok);
-    static_assert(Y0 + kTok <= 512 && BYTES <= 227 * 1024, "tensor and shared memory");
+    static constexpr int STAGES = 3 * STAGE + OUT <= 220 * 1024 ? 3 : 2 * STAGE + OUT <= 220 * 1024 ? 2 : 1;
+    static constexpr int BYTES = 1024 + STAGES * STAGE + OUT;
+    // tensor memory: dS, later gamma dY, as operands | dU, later -gamma beta dZ | dS k, then dZ | P^T dY | what dS gains
+    static constexpr int SCOLS = PM * KD / 2, ZCOLS = PM * kTok / 2, S0 = 0, Z0 = SCOLS, X0 = Z0 + ZCOLS, Y0 = X0 + kTok;
+    // (with three planes of 128 columns its first half goes where dZ was)
+    static constexpr bool ROOM = Y0 + kTok + KD <= 512;
+    static constexpr int D0 = ROOM ? Y0 + kTok : X0, D1 = ROOM ? D0 + KD / 2 : Y0 + kTok;
+    static_assert(D1 + KD / 2 <= 512 && (ROOM || KD / 2 == kTok) && BYTES + 1024 <= 227 * 1024, "tensor and shared memory");
 };
 
-template <typename T, int KD, int MODE> __global__ void __launch_bounds__(384, 1) delta_walk_back_kernel(DeltaArgs a, const __grid_constant__ DeltaMaps maps)
+template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkThreads, 1) delta_walk_back_kernel(DeltaArgs a, const __grid_constant__ DeltaMaps maps)
 {
     using C = WalkBack<T, KD>;
     constexpr int PI = C::PI, PM = C::PM, HC = KD / 2;
+    constexpr bool RUN = MODE == WALK_RUN;
     extern __shared__ __align__(1024) unsigned char raw[];
     __shared__ WalkShared ws;
     unsigned char *sm = align_images(raw);
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, lane = tid & 31, warp = uniform_warp(tid >> 5);
     long long id = blockIdx.x;
-    const bool phi = MODE == WALK_MAPS && (id & 1);          // from the identity, without dY
-    if (MODE == WALK_MAPS) id >>= 1;
+    const bool phi = !RUN && (id & 1);                       // from the identity, without dY
+    if (!RUN) id >>= 1;
     const long long bh = id / a.segments;
     const int segment = (int)(id % a.segments), b = (int)(bh / a.H), h = (int)(bh % a.H);
     pdl_wait();
@@ -49,24 +53,24 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(384, 1
     const int count = last > first ? last - first : 0;
     if (warp == 0) tmem_alloc(smem_u32(&ws.slot), 512);
     if (tid == 0) {
-        for (int s = 0; s < C::STAGES; ++s) { mbar_init(&ws.full[s], 129); mbar_init(&ws.empty[s], 1); }
-        mbar_init(&ws.bar_a, 1); mbar_init(&ws.bar_b, 1); mbar_init(&ws.bar_c, 1); mbar_init(&ws.bar_q, 1); mbar_init(&ws.bar_y, 1);
+        for (int s = 0; s < C::STAGES; ++s) { mbar_init(&ws.full[s], kFetchers + 1); mbar_init(&ws.empty[s], 1); }
+        mbar_init(&ws.bar_a, 1); mbar_init(&ws.bar_b, 1); mbar_init(&ws.bar_c, 1); mbar_init(&ws.ready, 8);
         ws.gave_up = 0;
         fence_mbar_init();
     }
     for (int s = 0; s < C::STAGES; ++s) {
-        clear_rows(sm + s * C::STAGE, C::TILE, 2 * PI, a.Dk, KD, tid, 384);
-        clear_rows(sm + s * C::STAGE + 2 * C::TENSOR, C::TILE, PI, phi ? 0 : a.Dv, KD, tid, 384);
+        clear_rows(sm + s * C::STAGE, C::TILE, 2 * PI, a.Dk, KD, tid, kWalkThreads);
+        clear_rows(sm + s * C::STAGE + C::DY, C::TILE, PI, phi ? 0 : a.Dv, KD, tid, kWalkThreads);
     }
     fence_async_smem();
     tmem_fence_before_sync();
     __syncthreads();
     tmem_fence_after_sync();
     const unsigned tb = ws.slot;
-    const int steps = (a.Dk + 15) / 16;
-    const long long vhead = bh * a.Dv * a.L, vall = (long long)a.B * a.H * a.Dv * a.L;
-    if (warp >= 8) {
-        const int ft = tid - 256;
+    const long long states = (long long)a.Dv * a.Dk, vhead = bh * a.Dv * a.L, vall = (long long)a.B * a.H * a.Dv * a.L;
+    if (warp > 8) {
+        // ---- fetching
+        const int ft = tid - 288;
         const long long bk = (long long)b * a.Hk + h / (a.H / a.Hk), qk = bk * a.Dk * a.L, all = (long long)a.B * a.Hk * a.Dk * a.L;
         for (int i = 0; i < count; ++i) {
             const int c = last - 1 - i, s = i % C::STAGES, t0 = c * kTok, nv = n - t0 < kTok ? n - t0 : kTok;
@@ -78,30 +82,70 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(384, 1
                 mbar_expect_tx(&ws.full[s], C::IMAGES + kWalkGates + (copied ? (phi ? 2 : 3) * C::TENSOR : 0));
                 if (copied) {
                     tma_load_3d(st, &maps.k, &ws.full[s], t0, 0, (int)bk);
-                    tma_load_3d(st + C::TENSOR, &maps.q, &ws.full[s], t0, 0, (int)bk);
-                    if (!phi) tma_load_3d(st + 2 * C::TENSOR, &maps.dy, &ws.full[s], t0, 0, (int)bh);
+                    tma_load_3d(st + C::Q, &maps.q, &ws.full[s], t0, 0, (int)bk);
+                    if (!phi) tma_load_3d(st + C::DY, &maps.v, &ws.full[s], t0, 0, (int)bh);
                 }
-                bulk_load(st + 3 * C::TENSOR, a.images + at * C::IMAGES, C::IMAGES, &ws.full[s]);
-                bulk_load(st + 3 * C::TENSOR + C::IMAGES, a.gates + at * kGates, kWalkGates, &ws.full[s]);
+                bulk_load(st + C::A, a.images + at * C::IMAGES, C::IMAGES, &ws.full[s]);
+                bulk_load(st + C::GATES, a.gates + at * kGates, kWalkGates, &ws.full[s]);
             }
             if (!copied) {
-                load_tile<T>(st, C::TILE, (const T *)a.k, qk + t0, all, a.L, a.Dk, nv, ft, 128);
-                load_tile<T>(st + C::TENSOR, C::TILE, (const T *)a.q, qk + t0, all, a.L, a.Dk, nv, ft, 128);
-                if (!phi) load_tile<T>(st + 2 * C::TENSOR, C::TILE, (const T *)a.dy, vhead + t0, vall, a.L, a.Dv, nv, ft, 128);
+                load_tile<T>(st, C::TILE, (const T *)a.k, qk + t0, all, a.L, a.Dk, nv, ft, kFetchers);
+                load_tile<T>(st + C::Q, C::TILE, (const T *)a.q, qk + t0, all, a.L, a.Dk, nv, ft, kFetchers);
+                if (!phi) load_tile<T>(st + C::DY, C::TILE, (const T *)a.dy, vhead + t0, vall, a.L, a.Dv, nv, ft, kFetchers);
             }
             fence_async_smem();
             mbar_arrive(&ws.full[s]);
         }
+    } else if (warp == 8) {
+        // ---- the products
+        const int steps = (a.Dk + 15) / 16;
+        unsigned par = 0;
+        for (int i = 0; i < count; ++i) {
+            const int s = i % C::STAGES;
+            const unsigned k = smem_u32(sm) + s * C::STAGE, q = k + C::Q, A = k + C::A, P = A + PM * kMatrix;
+            // what dS gains from columns 0 .. of an operand in tensor memory and an image of Dk rows
+            auto gain = [&](unsigned from, unsigned image, bool add) {
+                if (C::ROOM) issue_ts<PM, PI, PM, false, kTok / 16>(tb + C::D0, from, kTok / 2, image, C::TILE, kTok / 16, KD, add);
+                else {
+                    issue_ts<PM, PI, PM, false, kTok / 16>(tb + C::D0, from, kTok / 2, image, C::TILE, kTok / 16, KD / 2, add);
+                    issue_ts<PM, PI, PM, false, kTok / 16>(tb + C::D1, from, kTok / 2, image + KD / 2 * 128, C::TILE, kTok / 16, KD / 2, add);
+                }
+            };
+            WAIT(&ws.full[s], (i / C::STAGES) & 1);
+            WAIT(&ws.ready, par); par ^= 1;                  // dS
+            tmem_fence_after_sync();
+            issue_ts<PM, PI, PM, true, KD / 16>(tb + C::X0, tb + C::S0, KD / 2, k, C::TILE, steps, kTok, false);
+            issue_ss<PI, PM, PM, false, true, kTok / 16, B_LOWER_T>(tb + C::Y0, k + C::DY, C::TILE, 0, P, kMatrix, kTok / 16, kTok, false);
+            umma_commit(&ws.bar_a);
+            WAIT(&ws.ready, par); par ^= 1;                  // dU
+            tmem_fence_after_sync();
+            issue_ts<PM, PM, PM, true, kTok / 16, B_LOWER_T>(tb + C::X0, tb + C::Z0, kTok / 2, A, kMatrix, kTok / 16, kTok, false);
+            umma_commit(&ws.bar_b);
+            if (C::ROOM) {
+                WAIT(&ws.ready, par); par ^= 1;              // gamma dY
+                tmem_fence_after_sync();
+                gain(tb + C::S0, q, false);
+            }
+            WAIT(&ws.ready, par); par ^= 1;                  // -gamma beta dZ
+            tmem_fence_after_sync();
+            if (!C::ROOM) gain(tb + C::S0, q, false);
+            gain(tb + C::Z0, k, true);
+            umma_commit(&ws.bar_c);
+            umma_commit(&ws.empty[s]);
+        }
     } else {
-        const int row = 32 * (warp & 3) + lane, half = warp >> 2, rows = phi ? a.Dk : a.Dv;
+        // ---- computing
+        const int row = 32 * (warp & 3) + lane, half = warp >> 2, rows = phi ? a.Dk : a.Dv, rows8 = kept_rows(a.Dv);
         const unsigned lane_s = tmem_addr(tb, warp, C::S0 + half * (HC / 2)), lane_g = tmem_addr(tb, warp, C::S0 + half * 16),
-                       lane_z = tmem_addr(tb, warp, C::Z0 + half * 16), lane_x = tmem_addr(tb, warp, C::X0), lane_y = tmem_addr(tb, warp, C::Y0 + half * 32);
-        const long long vrow = vhead + (long long)row * a.L, states = (long long)a.Dv * a.Dk;
-        const bool real = row < a.Dv;
-        float S[HC];
+                       lane_z = tmem_addr(tb, warp, C::Z0 + half * 16), lane_x = tmem_addr(tb, warp, C::X0 + half * 32), lane_y = tmem_addr(tb, warp, C::Y0 + half * 32),
+                       lane_d = tmem_addr(tb, warp, half ? C::D1 : C::D0);
+        const long long vrow = vhead + (long long)row * a.L;
+        const bool real = row < a.Dv, stored = C::VALUES && a.copies;
+        unsigned char *out = sm + C::STAGES * C::STAGE;
+        float S[HC], x[32];
 #pragma unroll
         for (int i = 0; i < HC; ++i) S[i] = 0.f;
-        if (MODE == WALK_MAPS) {
+        if (!RUN) {
             if (phi) {
 #pragma unroll
                 for (int i = 0; i < HC; ++i) S[i] = row == half * HC + i && row < a.Dk ? 1.f : 0.f;
@@ -113,33 +157,24 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(384, 1
         for (int i = 0; i < count; ++i) {
             const int c = last - 1 - i, s = i % C::STAGES, t = c * kTok + 32 * half;
             const unsigned par = i & 1;
-            unsigned char *st = sm + s * C::STAGE;
-            const unsigned k = smem_u32(st), q = k + C::TENSOR, g = q + C::TENSOR, A = g + C::TENSOR, P = A + PM * kMatrix;
-            const float *gates = (const float *)(st + 3 * C::TENSOR + C::IMAGES);
-            if (MODE != WALK_MAPS) keep_state<HC>(a.dstates + (bh * a.chunks + c) * kept_floats(a.Dv, a.Dk), S, row, a.Dv, half * HC, a.Dk);
+            const unsigned char *st = sm + s * C::STAGE;
+            const float *gates = (const float *)(st + C::GATES) + 32 * half;
             planes_to_tmem<PM, HC / 2>(lane_s, KD / 2, S);
             tmem_wait_st();
             tmem_fence_before_sync();
+            walk_ready(&ws, lane);
+            if (RUN) keep_state<HC>(a.dstates + (bh * a.chunks + c) * kept_floats(a.Dv, a.Dk), S, row, a.Dv, half * HC, a.Dk);
             WAIT(&ws.full[s], (i / C::STAGES) & 1);
-            walkers_sync();
-            if (tid == 0) {
-                tmem_fence_after_sync();
-                issue_ts<PM, PI, PM, true>(tb + C::X0, tb + C::S0, KD / 2, k, C::TILE, steps, kTok, false);
-                issue_ss<PI, PM, PM, false, true>(tb + C::Y0, g, C::TILE, 0, P, kMatrix, kTok / 16, kTok, false);
-                umma_commit(&ws.bar_a);
-            }
-            __syncwarp();
-            float x[32];
             WAIT(&ws.bar_a, par);
             tmem_fence_after_sync();
             {
                 float y[32];
-                TmemIO<32>::ld(x, lane_x + 32 * half);
+                TmemIO<32>::ld(x, lane_x);
                 TmemIO<32>::ld(y, lane_y);
                 tmem_wait_ld();
 #pragma unroll
                 for (int e = 0; e < 32; e += 4) {
-                    const float4 de = *(const float4 *)(gates + kTok + 32 * half + e);
+                    const float4 de = *(const float4 *)(gates + kTok + e);
                     const float d[4] = {de.x, de.y, de.z, de.w};
 #pragma unroll
                     for (int j = 0; j < 4; ++j) x[e + j] = row < rows ? fmaf(d[j], x[e + j], phi ? 0.f : y[e + j]) : 0.f;
@@ -148,69 +183,76 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(384, 1
             planes_to_tmem<PM, 16>(lane_z, kTok / 2, x);
             tmem_wait_st();
             tmem_fence_before_sync();
-            walkers_sync();
-            if (tid == 0) {
-                tmem_fence_after_sync();
-                issue_ts<PM, PM, PM, true>(tb + C::X0, tb + C::Z0, kTok / 2, A, kMatrix, kTok / 16, kTok, false);
-                umma_commit(&ws.bar_b);
-            }
-            __syncwarp();
-            // gamma dY, in the state's place, meanwhile
-            if (row < KD) image_row<PI>(x, st + 2 * C::TENSOR, C::TILE, row, half);
+            walk_ready(&ws, lane);
+            // gamma dY, in the state's place, while A^T dU is formed
+            if (row < KD) image_row<PI>(x, st + C::DY, C::TILE, row, half);
             else {
 #pragma unroll
                 for (int e = 0; e < 32; ++e) x[e] = 0.f;
             }
 #pragma unroll
             for (int e = 0; e < 32; e += 4) {
-                const float4 ga = *(const float4 *)(gates + 32 * half + e);
+                const float4 ga = *(const float4 *)(gates + e);
                 x[e] *= ga.x; x[e + 1] *= ga.y; x[e + 2] *= ga.z; x[e + 3] *= ga.w;
             }
             planes_to_tmem<PM, 16>(lane_g, kTok / 2, x);
+            if (C::ROOM) {
+                tmem_wait_st();
+                tmem_fence_before_sync();
+                walk_ready(&ws, lane);
+            }
             WAIT(&ws.bar_b, par);
             tmem_fence_after_sync();
-            TmemIO<32>::ld(x, lane_x + 32 * half);
+            float dz[32];
+            TmemIO<32>::ld(dz, lane_x);
             tmem_wait_ld();
-            if (MODE != WALK_MAPS && row < kept_rows(a.Dv)) {                 // [quartet of tokens][row]
-                float4 *to = (float4 *)a.dz + ((bh * a.chunks + c) * 16 + 8 * half) * kept_rows(a.Dv) + row;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) { HN_G(to + e * kept_rows(a.Dv), 16); to[e * kept_rows(a.Dv)] = make_float4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]); }
-            }
 #pragma unroll
             for (int e = 0; e < 32; e += 4) {
-                const float4 be = *(const float4 *)(gates + 2 * kTok + 32 * half + e);
-                x[e] *= be.x; x[e + 1] *= be.y; x[e + 2] *= be.z; x[e + 3] *= be.w;
-            }
-            if (MODE != WALK_MAPS && real && t < a.L) store_row<T>((T *)a.dv, vrow + t, a.L, a.L - t, n - t, x);
-#pragma unroll
-            for (int e = 0; e < 32; e += 4) {
-                const float4 ga = *(const float4 *)(gates + 32 * half + e);
-                x[e] *= -ga.x; x[e + 1] *= -ga.y; x[e + 2] *= -ga.z; x[e + 3] *= -ga.w;
+                const float4 ga = *(const float4 *)(gates + e), be = *(const float4 *)(gates + 2 * kTok + e);
+                x[e] = -ga.x * (dz[e] * be.x); x[e + 1] = -ga.y * (dz[e + 1] * be.y); x[e + 2] = -ga.z * (dz[e + 2] * be.z); x[e + 3] = -ga.w * (dz[e + 3] * be.w);
             }
             planes_to_tmem<PM, 16>(lane_z, kTok / 2, x);
-            const float fade = gates[kTok - 1];
+            const float fade = ((const float *)(st + C::GATES))[kTok - 1];
+            if (RUN) {
+#pragma unroll
+                for (int e = 0; e < 32; e += 4) {
+                    const float4 be = *(const float4 *)(gates + 2 * kTok + e);
+                    x[e] = dz[e] * be.x; x[e + 1] = dz[e + 1] * be.y; x[e + 2] = dz[e + 2] * be.z; x[e + 3] = dz[e + 3] * be.w;
+                }
+            }
             tmem_wait_st();
             tmem_fence_before_sync();
-            walkers_sync();
-            if (tid == 0) {
-                tmem_fence_after_sync();
-                issue_ts<PM, PI, PM, false>(tb + C::X0, tb + C::S0, kTok / 2, q, C::TILE, kTok / 16, KD, false);
-                issue_ts<PM, PI, PM, false>(tb + C::X0, tb + C::Z0, kTok / 2, k, C::TILE, kTok / 16, KD, true);
-                umma_commit(&ws.bar_c);
-                umma_commit(&ws.empty[s]);
+            walk_ready(&ws, lane);
+            if (RUN) {
+                if (row < rows8) {                           // dZ: [quartet of tokens][row]
+                    float4 *to = (float4 *)a.dz + ((bh * a.chunks + c) * 16 + 8 * half) * rows8 + row;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) { HN_G(to + e * rows8, 16); to[e * rows8] = make_float4(dz[4 * e], dz[4 * e + 1], dz[4 * e + 2], dz[4 * e + 3]); }
+                }
+                if (stored) {                                // dV as an image that a copy takes away
+                    unsigned char *image = out + (i & 1) * C::TILE;
+                    if (row < KD) row_to_image(image, row, half, n - t, x);
+                    fence_async_smem();
+                    walkers_sync();
+                    if (tid == 0) {
+                        tma_store_3d(&maps.out, image, c * kTok, 0, (int)bh);
+                        tma_commit();
+                        tma_wait_read1();                    // the other image is free again once thread 0 has been here
+                    }
+                    __syncwarp();
+                } else if (real && t < a.L) store_row<T>((T *)a.dv, vrow + t, a.L, a.L - t, n - t, x);
             }
-            __syncwarp();
             WAIT(&ws.bar_c, par);
             tmem_fence_after_sync();
 #pragma unroll
             for (int e = 0; e < HC; e += 32) {
-                TmemIO<32>::ld(x, lane_x + half * HC + e);
+                TmemIO<32>::ld(x, lane_d + e);
                 tmem_wait_ld();
 #pragma unroll
                 for (int j = 0; j < 32; ++j) S[e + j] = fmaf(fade, S[e + j], x[j]);
             }
         }
-        if (MODE == WALK_MAPS) {
+        if (!RUN) {
             float *to = a.maps + (bh * a.segments + segment) * (long long)(a.Dv + a.Dk) * a.Dk + (phi ? states : 0);
             store_state<HC>(to, S, row, rows, half * HC, a.Dk);
         } else {
@@ -222,6 +264,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(384, 1
                 if (real && t < a.L) store_row<T>((T *)a.dv, vrow + t, a.L, a.L - t, 0, none);
             }
             if (a.ds0 && segment == 0) store_state<HC>(a.ds0 + bh * states, S, row, a.Dv, half * HC, a.Dk);
+            if (stored && tid == 0) tma_wait_all0();
         }
         tmem_fence_before_sync();
     }
@@ -271,7 +314,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(256, 1) delta_gr
     __shared__ float sums[3][4][kTok], erased[2][kTok], total[8];
     const float *gamma = gates, *delta = gates + kTok, *beta = gates + 2 * kTok, *ghi = gates + 3 * kTok, *glo = gates + 4 * kTok;
     unsigned char *sm = align_images(raw);
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, row = 32 * (warp & 3) + lane, half = warp >> 2, share = a.H / a.Hk;
+    const int tid = threadIdx.x, warp = uniform_warp(tid >> 5), lane = tid & 31, row = 32 * (warp & 3) + lane, half = warp >> 2, share = a.H / a.Hk;
     const long long bk = blockIdx.x / a.chunks;
     const int chunk = (int)(blockIdx.x % a.chunks), b = (int)(bk / a.Hk), hk = (int)(bk % a.Hk), t0 = chunk * kTok, t = t0 + 32 * half;
     pdl_wait();
@@ -331,7 +374,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(256, 1) delta_gr
             if (C::ROOM) bulk_load(sm + C::STATE, S, (unsigned)(kept * 4), &ws.full[0]);
             if (copied) {
                 if (!j) tma_load_3d(sm + C::K, &maps.k, &ws.full[0], t0, 0, (int)bk);
-                tma_load_3d(sm + C::DY, &maps.dy, &ws.full[0], t0, 0, (int)bh);
+                tma_load_3d(sm + C::DY, &maps.v, &ws.full[0], t0, 0, (int)bh);
                 if (!j) tma_load_3d(sm + C::Q, &maps.q, &ws.full[0], t0, 0, (int)bk);
             }
             bulk_load(gates, a.gates + at * kGates, kGates * 4, &ws.full[0]);
@@ -386,8 +429,8 @@ template <typename T, int KD> __global__ void __launch_bounds__(256, 1) delta_gr
             planes_to_tmem<PM, HC / 2>(lane_s, KD / 2, s);
         }
         go();
-        if (tid == 0) {
-            issue_ts<PM, PI, PM, true>(tb + C::R0, tb + C::S0, KD / 2, IK, C::TILE, ksteps, kTok, false);
+        if (warp == 0) {
+            issue_ts<PM, PI, PM, true, KD / 16>(tb + C::R0, tb + C::S0, KD / 2, IK, C::TILE, ksteps, kTok, false);
             umma_commit(&ws.bar_a);
         }
         done();
@@ -402,8 +445,8 @@ template <typename T, int KD> __global__ void __launch_bounds__(256, 1) delta_gr
         }
         planes_to_tmem<PM, 16>(tmem_addr(tb, warp, C::R0 + kTok + half * 16), kTok / 2, x);
         go();
-        if (tid == 0) {
-            issue_ts<PM, PM, PM, false>(tb + C::R0, tb + C::R0 + kTok, kTok / 2, IA, kMatrix, kTok / 16, kTok, false);
+        if (warp == 0) {
+            issue_ts<PM, PM, PM, false, kTok / 16, B_LOWER>(tb + C::R0, tb + C::R0 + kTok, kTok / 2, IA, kMatrix, kTok / 16, kTok, false);
             umma_commit(&ws.bar_a);
         }
         sums[0][warp & 3][32 * half + lane] = column_sum(y, lane);
@@ -445,18 +488,19 @@ template <typename T, int KD> __global__ void __launch_bounds__(256, 1) delta_gr
         tmem_wait_ld();
         if (row < KD) planes_to_image<PM>(sm + C::U, C::TILE, row, half, x);
         go();
-        if (tid == 0) {
-            if (C::ROOM) {                                   // the state has been read: the gradient behind the chunk into its place
+        if (warp == 0) {
+            if (C::ROOM && lane == 0) {                      // the state has been read: the gradient behind the chunk into its place
                 mbar_expect_tx(&ws.full[1], (unsigned)(kept * 4));
                 bulk_load(sm + C::STATE, D, (unsigned)(kept * 4), &ws.full[1]);
             }
+            __syncwarp();
             // rows 0 .. 63: dY U^T, rows 64 ..: dZ U^T; where dY is one plane, dZ's second goes into a sum of its own
-            issue_ss<PI, PM, PM, true, true>(tb + C::R0 + kTok, IY, C::TILE, C::DZ - C::DY, IU, C::TILE, vsteps, kTok, false);
-            if (PI < PM) issue_ss<1, 1, PM, true, true>(tb + C::R0 + 5 * kTok, IY + C::TILE, C::TILE, C::DZ - C::DY, IU, C::TILE, vsteps, kTok, false);
+            issue_ss<PI, PM, PM, true, true, KD / 16>(tb + C::R0 + kTok, IY, C::TILE, C::DZ - C::DY, IU, C::TILE, vsteps, kTok, false);
+            if (PI < PM) issue_ss<1, 1, PM, true, true, KD / 16>(tb + C::R0 + 5 * kTok, IY + C::TILE, C::TILE, C::DZ - C::DY, IU, C::TILE, vsteps, kTok, false);
             // rows 64 ..: K K^T
-            issue_ss<PI, PI, PI, true, true>(tb + C::R0 + 2 * kTok, IY, C::TILE, C::K - C::DY, IK, C::TILE, ksteps, kTok, false);
-            issue_ts<PM, PI, PM, true>(tb + C::R0, tb + C::S0, KD / 2, IY, C::TILE, vsteps, kTok, false);
-            issue_ts<PM, PM, PM, true>(tb + C::R0 + 3 * kTok, tb + C::S0, KD / 2, IZ, C::TILE, vsteps, kTok, false);
+            issue_ss<PI, PI, PI, true, true, KD / 16>(tb + C::R0 + 2 * kTok, IY, C::TILE, C::K - C::DY, IK, C::TILE, ksteps, kTok, false);
+            issue_ts<PM, PI, PM, true, KD / 16>(tb + C::R0, tb + C::S0, KD / 2, IY, C::TILE, vsteps, kTok, false);
+            issue_ts<PM, PM, PM, true, KD / 16>(tb + C::R0 + 3 * kTok, tb + C::S0, KD / 2, IZ, C::TILE, vsteps, kTok, false);
             umma_commit(&ws.bar_a);
         }
         done();
@@ -501,9 +545,9 @@ template <typename T, int KD> __global__ void __launch_bounds__(256, 1) delta_gr
             erase[e] *= -ga * beta[32 * half + e];
         }
         go();
-        if (tid == 0) {
-            issue_ss<PI, PM, PM, false, false>(tb + C::R0 + kTok, IK, C::TILE, 0, IA, kMatrix, kTok / 16, kTok, false);         // F k
-            issue_ss<PI, PM, PM, false, false>(tb + C::R0 + 2 * kTok, IK, C::TILE, 0, IZ, kMatrix, kTok / 16, kTok, false);     // E k
+        if (warp == 0) {
+            issue_ss<PI, PM, PM, false, false, kTok / 16, B_LOWER>(tb + C::R0 + kTok, IK, C::TILE, 0, IA, kMatrix, kTok / 16, kTok, false);         // F k
+            issue_ss<PI, PM, PM, false, false, kTok / 16, B_LOWER>(tb + C::R0 + 2 * kTok, IK, C::TILE, 0, IZ, kMatrix, kTok / 16, kTok, false);     // E k
             umma_commit(&ws.bar_a);
         }
         __syncwarp();
@@ -529,10 +573,10 @@ template <typename T, int KD> __global__ void __launch_bounds__(256, 1) delta_gr
 #pragma unroll
         for (int e = 0; e < 32; ++e) erase[e] += y[e];
         go();
-        if (tid == 0) {
-            issue_ts<PM, PM, PM, true>(tb + C::R0, tb + C::S0, KD / 2, IU, C::TILE, vsteps, kTok, false);                       // dS1 u
-            issue_ss<PI, PM, PM, false, true>(tb + C::R0 + kTok, IQ, C::TILE, 0, IA, kMatrix, kTok / 16, kTok, false);          // F q
-            issue_ss<PI, PM, PM, false, true>(tb + C::R0 + kTok, IK, C::TILE, 0, IZ, kMatrix, kTok / 16, kTok, true);           // E k, the other way
+        if (warp == 0) {
+            issue_ts<PM, PM, PM, true, KD / 16>(tb + C::R0, tb + C::S0, KD / 2, IU, C::TILE, vsteps, kTok, false);                                  // dS1 u
+            issue_ss<PI, PM, PM, false, true, kTok / 16, B_LOWER_T>(tb + C::R0 + kTok, IQ, C::TILE, 0, IA, kMatrix, kTok / 16, kTok, false);        // F q
+            issue_ss<PI, PM, PM, false, true, kTok / 16, B_LOWER_T>(tb + C::R0 + kTok, IK, C::TILE, 0, IZ, kMatrix, kTok / 16, kTok, true);         // E k, the other way
             umma_commit(&ws.bar_a);
         }
         __syncwarp();
@@ -630,13 +674,13 @@ int delta_backward_status()
 template <typename T, int KD> static int launch_back(DeltaArgs a, cudaStream_t st)
 {
     DeltaMaps m{};
-    a.copies = delta_maps<T>(m, a, KD);
+    a.copies = delta_maps<T>(m, a, KD, a.dy, a.dv);
     const long long blocks = (long long)a.B * a.H * a.segments;
     if (a.segments > 1) {
-        if (const int e = launch_delta<delta_walk_back_kernel<T, KD, WALK_MAPS>>(a, 2 * blocks, 384, WalkBack<T, KD>::BYTES, st, m)) return e;
+        if (const int e = launch_delta<delta_walk_back_kernel<T, KD, WALK_MAPS>>(a, 2 * blocks, kWalkThreads, WalkBack<T, KD>::BYTES, st, m)) return e;
         if (const int e = launch_delta_join(a, a.ds_end, true, st)) return e;
     }
-    if (const int e = launch_delta<delta_walk_back_kernel<T, KD, WALK_RUN>>(a, blocks, 384, WalkBack<T, KD>::BYTES, st, m)) return e;
+    if (const int e = launch_delta<delta_walk_back_kernel<T, KD, WALK_RUN>>(a, blocks, kWalkThreads, WalkBack<T, KD>::BYTES, st, m)) return e;
     return launch_delta<delta_gradients_kernel<T, KD>>(a, (long long)a.B * a.Hk * a.chunks, 256, Grads<T, KD>::BYTES, st, m);
 }
 int launch_delta_backward(const DeltaArgs &a, int dtype, cudaStream_t st)
