@@ -440,6 +440,8 @@ struct WalkShared {
 };
 __device__ __forceinline__ void walk_wait(WalkShared *w, uint64_t *bar, unsigned parity, int *status)
 {
+    for (int i = 0; i < 64; ++i)                             // (before the clock is read, which takes longer than most waits)
+        if (mbar_try_wait(bar, parity)) return;
     volatile int *f = &w->gave_up;
     if (*f) return;
     if (!mbar_wait(bar, parity)) { *f = 1; atomicExch(status, 1); }

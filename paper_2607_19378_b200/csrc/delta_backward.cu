@@ -453,16 +453,24 @@ template <typename T, int KD> __global__ void __launch_bounds__(256, 1) delta_gr
         // a state with its columns as lanes; `with`: the sum of its products with the one that is there
         auto columns = [&](const float *p, bool with) {
             float s[32], inner = 0.f;
+            const int q7 = (row >> 2) & 7, mine = row < a.Dk ? (row >> 2) * rows8 * 4 + (row & 3) : 0;
 #pragma unroll
             for (int c = 0; c < HC; c += 32) {
 #pragma unroll
-                for (int e = 0; e < 32; ++e) {
-                    const int r = half * HC + c + e;
-                    s[e] = 0.f;
-                    if (r < a.Dv && row < a.Dk) {
-                        const int i = kept_at(r, row >> 2, rows8) * 4 + (row & 3);
-                        if (C::ROOM) s[e] = ((const float *)held)[i];
-                        else { HN_G(p + i, 4); s[e] = p[i]; }
+                for (int g = 0; g < 32; g += 8) {
+                    const int r = half * HC + c + g;         // rows r .. r + 7, all kept or none
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) s[g + e] = 0.f;
+                    if (r >= rows8) continue;
+                    const float *from = (C::ROOM ? (const float *)held : p) + mine + r * 4;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        if (!C::ROOM) HN_G(from + (e ^ q7) * 4, 4);
+                        s[g + e] = from[(e ^ q7) * 4];
+                    }
+                    if (row >= a.Dk) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) s[g + e] = 0.f;
                     }
                 }
                 if (with) {
