@@ -18,20 +18,51 @@ static __device__ int hn_delta_status;
 
 template <typename T, int KD> struct Prep {
     static constexpr int PI = Planes<T>::IN, PM = Planes<T>::MID, TILE = KD * 128, PITCH = 2 * TILE, TROW = 68;
-    static constexpr int IMAGES = PI * PITCH > 2 * PM * kMatrix ? PI * PITCH : 2 * PM * kMatrix;          // (the results take the tiles' place)
-    static constexpr int BYTES = 1024 + IMAGES + kTok * TROW * 4;
+    // the tiles of k and q; T and the planes of P take their place
+    static constexpr int P = kTok * TROW * 4 + 1024 - kTok * TROW * 4 % 1024, AFTER = P + PM * kMatrix, IMAGES = PI * PITCH > AFTER ? PI * PITCH : AFTER, BYTES = 1024 + IMAGES;
 };
+
+// C = -A B for the lower left block of N x N of a pair of blocks, in place: rows r0 + N .., columns r0 ..; A = T's block, B = the upper
+// inverse (first), or A = the lower inverse, B = C (then).  `threads` threads of a pair, each one row and N N / threads columns.
+template <int N, int THREADS, bool FIRST> __device__ __forceinline__ void merge(float *T, int row, int r0, int t)
+{
+    constexpr int EACH = N * N / THREADS;                    // 4 or 8
+    const int r = r0 + N + t / (N / EACH), c = r0 + t % (N / EACH) * EACH;
+    float acc[EACH];
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) acc[e] = 0.f;
+    // first: sum over m of T[r][r0 + m] B[r0 + m][c]; then: of inverse[r][r0 + N + m] C[r0 + N + m][c]
+    const float *left = T + r * row + (FIRST ? r0 : r0 + N), *right = T + (FIRST ? r0 : r0 + N) * row + c;
+#pragma unroll 2
+    for (int m = 0; m < N; m += 4) {
+        const float4 l = *(const float4 *)(left + m);
+        const float lm[4] = {l.x, l.y, l.z, l.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < EACH; e += 4) {
+                const float4 w = *(const float4 *)(right + (m + i) * row + e);
+                acc[e] = fmaf(lm[i], w.x, acc[e]); acc[e + 1] = fmaf(lm[i], w.y, acc[e + 1]);
+                acc[e + 2] = fmaf(lm[i], w.z, acc[e + 2]); acc[e + 3] = fmaf(lm[i], w.w, acc[e + 3]);
+            }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < EACH; e += 4)
+        *(float4 *)(T + r * row + c + e) = FIRST ? make_float4(acc[e], acc[e + 1], acc[e + 2], acc[e + 3]) : make_float4(-acc[e], -acc[e + 1], -acc[e + 2], -acc[e + 3]);
+    __syncthreads();
+}
 
 template <typename T, int KD> __global__ void __launch_bounds__(128) delta_prepare_kernel(DeltaArgs a, const __grid_constant__ DeltaMaps maps)
 {
     using C = Prep<T, KD>;
     extern __shared__ __align__(1024) unsigned char raw[];
-    __shared__ float hi[kTok], lo[kTok], beta[kTok];
+    __shared__ __align__(16) float hi[kTok], lo[kTok], beta[kTok];
     __shared__ uint64_t bar, there;
     __shared__ unsigned slot;
     unsigned char *sm = align_images(raw);
-    float *Ts = (float *)(sm + C::IMAGES);
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    float *Ts = (float *)sm;
+    const int tid = threadIdx.x, warp = uniform_warp(tid >> 5), lane = tid & 31;
     const long long at = blockIdx.x, bh = at / a.chunks;
     const int chunk = (int)(at % a.chunks), b = (int)(bh / a.H), h = (int)(bh % a.H), t0 = chunk * kTok;
     pdl_wait();
@@ -71,7 +102,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(128) delta_prepa
     tmem_fence_after_sync();
     const unsigned tb = slot, images = smem_u32(sm);
     bool ok = !copied || mbar_wait(&there, 0);
-    if (uniform_warp(warp) == 0) {
+    if (warp == 0) {
         issue_ss<C::PI, C::PI, C::PI, true, true, KD / 16>(tb, images, C::PITCH, C::TILE, images, C::PITCH, steps, kTok, false);
         umma_commit(&bar);
     }
@@ -84,63 +115,89 @@ template <typename T, int KD> __global__ void __launch_bounds__(128) delta_prepa
     ok = mbar_wait(&bar, 0) && ok;
     if (!ok) atomicExch(&hn_delta_status, 1);
     tmem_fence_after_sync();
+    __syncthreads();                                          // (every thread has waited: the tiles' place is free)
     // lanes 0 .. 63: rows of k k^T, lanes 64 .. 127: rows of q k^T
     const int i = tid & 63;
-    const float Hi = hi[i], Li = lo[i], bi = beta[i];
-    __syncthreads();                                          // (every thread has waited: the tiles' place is free)
-    unsigned char *imageA = sm, *imageP = sm + C::PM * kMatrix;
+    {
+        const float Hi = hi[i], Li = lo[i], bi = beta[i];
+        const unsigned at_row = tmem_addr(tb, warp, 0);
+#pragma unroll 2
+        for (int g = 0; g < 8; ++g) {
+            float x[8];
+            tmem_ld8(x, at_row + 8 * g);
+            tmem_wait_ld();
+            const float4 h0 = *(const float4 *)(hi + 8 * g), h1 = *(const float4 *)(hi + 8 * g + 4), l0 = *(const float4 *)(lo + 8 * g), l1 = *(const float4 *)(lo + 8 * g + 4);
+            const float hj[8] = {h0.x, h0.y, h0.z, h0.w, h1.x, h1.y, h1.z, h1.w}, lj[8] = {l0.x, l0.y, l0.z, l0.w, l1.x, l1.y, l1.z, l1.w};
+            // (a later token's ratio is of no use and may be no number)
 #pragma unroll
-    for (int hf = 0; hf < 2; ++hf) {
-        float x[32];
-        TmemIO<32>::ld(x, tmem_addr(tb, warp, 32 * hf));
-        tmem_wait_ld();
-#pragma unroll
-        for (int c = 0; c < 32; ++c) {
-            const int j = 32 * hf + c;
-            const float r = ratio(Hi, Li, hi[j], lo[j]);
-            x[c] = tid < kTok ? (j < i ? bi * r * x[c] : 0.f) : (j <= i ? r * x[c] : 0.f);
+            for (int e = 0; e < 8; ++e) {
+                const int j = 8 * g + e;
+                const float r = ratio(Hi, Li, hj[e], lj[e]);
+                x[e] = warp < 2 ? (j < i ? bi * r * x[e] : 0.f) : (j <= i ? r * x[e] : 0.f);
+            }
+            if (warp < 2) {
+                *(float4 *)(Ts + i * C::TROW + 8 * g) = make_float4(x[0], x[1], x[2], x[3]);
+                *(float4 *)(Ts + i * C::TROW + 8 * g + 4) = make_float4(x[4], x[5], x[6], x[7]);
+            } else planes8_to_image<C::PM>(sm + C::P, kMatrix, i, g, x);
         }
-        if (tid < kTok) {
-#pragma unroll
-            for (int c = 0; c < 32; c += 4) *(float4 *)(Ts + i * C::TROW + 32 * hf + c) = make_float4(x[c], x[c + 1], x[c + 2], x[c + 3]);
-        } else planes_to_image<C::PM>(imageP, kMatrix, i, hf, x);
     }
+    fence_async_smem();
     tmem_fence_before_sync();
     __syncthreads();
+    unsigned char *to = a.images + at * (2 * C::PM * kMatrix);
+    if (tid == 96) {
+        bulk_store(to + C::PM * kMatrix, sm + C::P, C::PM * kMatrix);
+        tma_commit();
+    }
     if (warp == 0) tmem_dealloc(tb, 64);
-    if (tid < kTok) {                                         // column tid of A: (I + T) A = I from the top
-        float c[kTok];
+    // A = (I + T)^{-1} in T's place: blocks of 16 by forward substitution, a thread a column; then pairs of blocks,
+    //     (D1 0; T21 D2)^{-1} = (D1^{-1} 0; -D2^{-1} T21 D1^{-1} D2^{-1}), to 32 and to 64
+    if (tid < kTok) {
+        float *D = Ts + (tid & 48) * (C::TROW + 1);
+        const int j = tid & 15;
+        float c[16];
 #pragma unroll
-        for (int r = 0; r < kTok; ++r) {
-            float s[4] = {r == tid ? 1.f : 0.f, 0.f, 0.f, 0.f};
+        for (int r = 0; r < 16; ++r) {
+            float s[2] = {r == j ? 1.f : 0.f, 0.f};
 #pragma unroll
             for (int m = 0; m < r; m += 4) {
-                const float4 w = *(const float4 *)(Ts + r * C::TROW + m);
+                const float4 w = *(const float4 *)(D + r * C::TROW + m);
                 s[0] = fmaf(-w.x, c[m], s[0]);
                 if (m + 1 < r) s[1] = fmaf(-w.y, c[m + 1], s[1]);
-                if (m + 2 < r) s[2] = fmaf(-w.z, c[m + 2], s[2]);
-                if (m + 3 < r) s[3] = fmaf(-w.w, c[m + 3], s[3]);
+                if (m + 2 < r) s[0] = fmaf(-w.z, c[m + 2], s[0]);
+                if (m + 3 < r) s[1] = fmaf(-w.w, c[m + 3], s[1]);
             }
-            c[r] = (s[0] + s[1]) + (s[2] + s[3]);
+            c[r] = s[0] + s[1];
         }
+        __syncwarp();                                         // (the block's columns are in one warp)
 #pragma unroll
-        for (int r = 0; r < kTok; r += 2) {
-            unsigned w[C::PM];
-            split_pair<C::PM>(c[r], c[r + 1], w);
-#pragma unroll
-            for (int p = 0; p < C::PM; ++p) {
-                *(unsigned short *)(imageA + p * kMatrix + image_at(r, tid >> 3) + (tid & 7) * 2) = (unsigned short)(w[p] & 0xffffu);
-                *(unsigned short *)(imageA + p * kMatrix + image_at(r + 1, tid >> 3) + (tid & 7) * 2) = (unsigned short)(w[p] >> 16);
-            }
-        }
+        for (int r = 0; r < 16; ++r) D[r * C::TROW + j] = c[r];
     }
     __syncthreads();
-    uint4 *to = (uint4 *)(a.images + at * (2 * C::PM * kMatrix));
-    for (int e = tid; e < 2 * C::PM * kMatrix / 16; e += 128) { HN_G(to + e, 16); to[e] = ((const uint4 *)sm)[e]; }
+    merge<16, 64, true>(Ts, C::TROW, tid >> 6 << 5, tid & 63);
+    merge<16, 64, false>(Ts, C::TROW, tid >> 6 << 5, tid & 63);
+    merge<32, 128, true>(Ts, C::TROW, 0, tid);
+    merge<32, 128, false>(Ts, C::TROW, 0, tid);
+#pragma unroll 1
+    for (int e = tid; e < kTok * 8; e += 128) {
+        const int r = e >> 3, c = e & 7;
+        const float4 u = *(const float4 *)(Ts + r * C::TROW + 8 * c), v = *(const float4 *)(Ts + r * C::TROW + 8 * c + 4);
+        const float x[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+        uint4 w[C::PM];
+        planes8<C::PM>(w, x);
+#pragma unroll
+        for (int p = 0; p < C::PM; ++p) {
+            uint4 *o = (uint4 *)(to + p * kMatrix + image_at(r, c));
+            HN_G(o, 16);
+            *o = w[p];
+        }
+    }
+    if (tid == 96) tma_wait_all0();
 }
 
-#define WAIT(bar, parity) walk_wait(&ws, bar, parity, &hn_delta_status)
 // ---- walk -----------------------------------------------------------------------------------------------------------
+
+#define WAIT(bar, parity) walk_wait(&ws, bar, parity, &hn_delta_status)
 
 template <typename T, int KD> struct Walk {
     static constexpr int PI = Planes<T>::IN, PM = Planes<T>::MID, TILE = KD * 128, TENSOR = PI * TILE;
@@ -561,7 +618,7 @@ template <typename T> static int launch_prepare(DeltaArgs a, cudaStream_t st)
 {
     const long long blocks = (long long)a.B * a.H * a.chunks;
     DeltaMaps m{};
-    a.copies = delta_maps<T>(m, a, a.Dk <= 64 ? 64 : 128, a.v, nullptr);
+    a.copies = delta_maps<T>(m, a, a.Dk <= 64 ? 64 : 128, a.v, nullptr, nullptr);
     return a.Dk <= 64 ? launch_delta<delta_prepare_kernel<T, 64>>(a, blocks, 128, Prep<T, 64>::BYTES, st, m)
                       : launch_delta<delta_prepare_kernel<T, 128>>(a, blocks, 128, Prep<T, 128>::BYTES, st, m);
 }
@@ -578,7 +635,7 @@ int launch_delta_join(const DeltaArgs &a, const float *from, bool backward, cuda
 template <typename T, int KD> static int launch_walk(DeltaArgs a, cudaStream_t st)
 {
     DeltaMaps m{};
-    a.copies = delta_maps<T>(m, a, KD, a.v, a.y);
+    a.copies = delta_maps<T>(m, a, KD, a.v, a.y, nullptr);
     const long long blocks = (long long)a.B * a.H * a.segments;
     if (a.segments > 1) {
         if (const int e = launch_delta<delta_walk_kernel<T, KD, WALK_MAPS>>(a, 2 * blocks, kWalkThreads, Walk<T, KD>::BYTES, st, m)) return e;

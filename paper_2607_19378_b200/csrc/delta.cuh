@@ -61,6 +61,26 @@ __device__ __forceinline__ int live_tokens(const DeltaArgs &a, int b)
     return n < 0 ? 0 : n < a.L ? n : a.L;
 }
 
+// eight columns of this thread's lane
+__device__ __forceinline__ void tmem_ld8(float (&v)[8], unsigned at)
+{
+    unsigned u[8];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n"
+                 : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]) : "r"(at) : "memory");
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(u[i]);
+}
+__device__ __forceinline__ void tmem_st8(unsigned at, const float (&v)[8])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};\n"
+                 ::"r"(at), "r"(__float_as_uint(v[0])), "r"(__float_as_uint(v[1])), "r"(__float_as_uint(v[2])), "r"(__float_as_uint(v[3])), "r"(__float_as_uint(v[4])),
+                   "r"(__float_as_uint(v[5])), "r"(__float_as_uint(v[6])), "r"(__float_as_uint(v[7])) : "memory");
+}
+__device__ __forceinline__ void tmem_st4(unsigned at, const unsigned (&v)[4])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+}
+
 // a pair of numbers as PM planes of bf16 pairs, each the rest of the ones before, rounded to nearest (so that a rest has either sign
 // and what is left out of a product, rest times rest, averages out: cut off instead, states were off by 7e-6, now by 2e-6)
 template <int PM> __device__ __forceinline__ void split_pair(float x, float y, unsigned (&w)[PM])
@@ -98,6 +118,49 @@ template <int PM> __device__ __forceinline__ void planes_to_image(unsigned char 
         for (int i = 0; i < 4; ++i) split_pair<PM>(x[8 * c + 2 * i], x[8 * c + 2 * i + 1], u[i]);
 #pragma unroll
         for (int p = 0; p < PM; ++p) *(uint4 *)(image + p * pitch + image_at(row, half * 4 + c)) = make_uint4(u[0][p], u[1][p], u[2][p], u[3][p]);
+    }
+}
+// eight numbers as planes: into tensor memory (four columns each), into chunk `chunk` of row `row` of an image
+template <int PM> __device__ __forceinline__ void planes8_to_tmem(unsigned at, int pitch, const float (&x)[8])
+{
+    unsigned w[PM][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        unsigned u[PM];
+        split_pair<PM>(x[2 * i], x[2 * i + 1], u);
+#pragma unroll
+        for (int p = 0; p < PM; ++p) w[p][i] = u[p];
+    }
+#pragma unroll
+    for (int p = 0; p < PM; ++p) tmem_st4(at + p * pitch, w[p]);
+}
+template <int PM> __device__ __forceinline__ void planes8(uint4 (&w)[PM], const float (&x)[8])
+{
+    unsigned u[4][PM];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) split_pair<PM>(x[2 * i], x[2 * i + 1], u[i]);
+#pragma unroll
+    for (int p = 0; p < PM; ++p) w[p] = make_uint4(u[0][p], u[1][p], u[2][p], u[3][p]);
+}
+template <int PM> __device__ __forceinline__ void planes8_to_image(unsigned char *image, int pitch, int row, int chunk, const float (&x)[8])
+{
+    uint4 w[PM];
+    planes8<PM>(w, x);
+#pragma unroll
+    for (int p = 0; p < PM; ++p) *(uint4 *)(image + p * pitch + image_at(row, chunk)) = w[p];
+}
+template <int PI> __device__ __forceinline__ void image8(float (&x)[8], const unsigned char *image, int pitch, int row, int chunk)
+{
+#pragma unroll
+    for (int p = PI - 1; p >= 0; --p) {
+        const uint4 w = *(const uint4 *)(image + p * pitch + image_at(row, chunk));
+        const unsigned u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float lo = __uint_as_float(u[i] << 16), hi = __uint_as_float(u[i] & 0xffff0000u);
+            x[2 * i] = p == PI - 1 ? lo : x[2 * i] + lo;
+            x[2 * i + 1] = p == PI - 1 ? hi : x[2 * i + 1] + hi;
+        }
     }
 }
 // the numbers of a row of an image of a tensor: its planes' sum
@@ -260,6 +323,56 @@ template <> struct RowPart<float> {
     }
     __device__ __forceinline__ float get(int i) const { return x[i]; }
 };
+// eight tokens of one row from element `at`, zero from the nv-th on; and eight stored, the first `room` of them
+template <typename T> __device__ __forceinline__ void load8(float (&x)[8], const T *p, long long at, long long n, int L, int nv)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = 0.f;
+    if (nv <= 0) return;
+    if constexpr (sizeof(T) == 2) {
+        uint4 w;
+        if (L % 8 == 0) { HN_G(p + at, 16); w = __ldg((const uint4 *)(p + at)); }
+        else w = load_unaligned(p, at, n);
+        if (nv < 8) w = keep_first(w, nv);
+        const unsigned u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(u[i] << 16); x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < nv) x[i] = IO<T>::ld(p, at + i);
+    }
+}
+template <typename T> __device__ __forceinline__ void store8(T *p, long long at, int L, int room, int nv, const float (&x)[8])
+{
+    constexpr int V = 16 / sizeof(T);
+    if (L % V == 0) {
+#pragma unroll
+        for (int c = 0; c < 8 / V; ++c) {
+            if (c * V >= room) break;
+            uint4 w;
+            T *e = (T *)&w;
+#pragma unroll
+            for (int i = 0; i < V; ++i) e[i] = (T)(c * V + i < nv ? x[c * V + i] : 0.f);
+            HN_G(p + at + c * V, 16);
+            *(uint4 *)(p + at + c * V) = w;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < room) IO<T>::st(p, at + i, i < nv ? x[i] : 0.f);
+    }
+}
+__device__ __forceinline__ uint4 bf16_8(const float (&x)[8], int nv)
+{
+    unsigned u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 r = __floats2bfloat162_rn(2 * i < nv ? x[2 * i] : 0.f, 2 * i + 1 < nv ? x[2 * i + 1] : 0.f);
+        u[i] = *(const unsigned *)&r;
+    }
+    return make_uint4(u[0], u[1], u[2], u[3]);
+}
 // the first `room` of 32 tokens of one row; from token nv on they are zero
 template <typename T> __device__ __forceinline__ void store_row(T *p, long long at, int L, int room, int nv, const float (&x)[32])
 {
@@ -392,7 +505,7 @@ enum { B_ALL = 0, B_LOWER = 1, B_LOWER_T = 2 };
 
 // d (+)= sum of the products of planes p of A (tensor memory, `pa` columns apart) and q of B (images, `pb` bytes apart), p < NA, q < NB,
 // p + q < MAX, over the first `steps` of STEPS 16-steps; the smallest first (the sums are cut off, not rounded, at every instruction)
-template <int NA, int NB, int MAX, bool BCOLS, int STEPS, int PART = B_ALL>
+template <int NA, int NB, int MAX, bool BCOLS, int STEPS, int PART = B_ALL, int UNROLL = STEPS>
 __device__ __forceinline__ void issue_ts(unsigned d, unsigned a, int pa, unsigned b, int pb, int steps, int n, bool add, unsigned next = 1024)
 {
 #pragma unroll
@@ -400,7 +513,7 @@ __device__ __forceinline__ void issue_ts(unsigned d, unsigned a, int pa, unsigne
 #pragma unroll
         for (int p = 0; p <= sum; ++p)
             if (const int q = sum - p; p < NA && q < NB)
-#pragma unroll
+#pragma unroll UNROLL
                 for (int e = 0; e < STEPS; ++e) {
                     const int k = PART == B_LOWER_T ? STEPS - 1 - e : e, from = PART == B_LOWER ? 16 * k : 0, cols = PART == B_ALL ? n : PART == B_LOWER ? kTok - 16 * k : 16 * (k + 1);
                     if (k >= steps) continue;
@@ -409,7 +522,7 @@ __device__ __forceinline__ void issue_ts(unsigned d, unsigned a, int pa, unsigne
                 }
 }
 // the same with A in images; `next`: see umma_cols
-template <int NA, int NB, int MAX, bool ACOLS, bool BCOLS, int STEPS, int PART = B_ALL>
+template <int NA, int NB, int MAX, bool ACOLS, bool BCOLS, int STEPS, int PART = B_ALL, int UNROLL = STEPS>
 __device__ __forceinline__ void issue_ss(unsigned d, unsigned a, int pa, unsigned next, unsigned b, int pb, int steps, int n, bool add)
 {
 #pragma unroll
@@ -417,7 +530,7 @@ __device__ __forceinline__ void issue_ss(unsigned d, unsigned a, int pa, unsigne
 #pragma unroll
         for (int p = 0; p <= sum; ++p)
             if (const int q = sum - p; p < NA && q < NB)
-#pragma unroll
+#pragma unroll UNROLL
                 for (int e = 0; e < STEPS; ++e) {
                     const int k = PART == B_LOWER_T ? STEPS - 1 - e : e, from = PART == B_LOWER ? 16 * k : 0, cols = PART == B_ALL ? n : PART == B_LOWER ? kTok - 16 * k : 16 * (k + 1);
                     if (k >= steps) continue;
@@ -465,24 +578,24 @@ enum { WALK_RUN = 0, WALK_MAPS = 1 };
 
 // Tiles of bf16 tensors whose rows start on 16 bytes come as tensor copies: rows behind a head's channels and tokens behind L arrive as
 // zeros.  Others, and a chunk that ends before L, are fetched by threads (load_tile).
-struct DeltaMaps { CUtensorMap k, q, v, out; };            // v: values, or dy; out: y, or dv
+struct DeltaMaps { CUtensorMap k, q, v, more, out, outk; };        // v: values, or dy; more: values beside dy; out: y, dv or dq; outk: dk
 __device__ __forceinline__ bool by_copy(const DeltaArgs &a, int nv, int t0) { return a.copies && (nv == kTok || t0 + nv == a.L); }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
 
-template <typename T> static bool delta_maps(DeltaMaps &m, const DeltaArgs &a, int rows, const void *v, const void *out)
+// `v` as DeltaMaps has it; out, outk: results, of the keys' shape where there are two, of the values' where there is one (or none)
+template <typename T> static bool delta_maps(DeltaMaps &m, const DeltaArgs &a, int rows, const void *v, const void *out, const void *outk)
 {
     if (sizeof(T) != 2 || a.L % 8 || !tma_available()) return false;
-    auto one = [&](CUtensorMap *map, const void *p, int D, long long heads) {
-        const unsigned long long dims[3] = {(unsigned long long)a.L, (unsigned long long)D, (unsigned long long)heads},
+    auto one = [&](CUtensorMap *map, const void *p, bool keys) {
+        const int D = keys ? a.Dk : a.Dv;
+        const unsigned long long dims[3] = {(unsigned long long)a.L, (unsigned long long)D, (unsigned long long)a.B * (keys ? a.Hk : a.H)},
                                  strides[2] = {2ull * a.L, 2ull * a.L * D};
         const unsigned box[3] = {(unsigned)kTok, (unsigned)rows, 1};
-        return tma_encode_3d_cached(map, p, true, dims, strides, box, 128);
+        return !p || tma_encode_3d_cached(map, p, true, dims, strides, box, 128);
     };
-    const long long keys = (long long)a.B * a.Hk, values = (long long)a.B * a.H;
-    return one(&m.k, a.k, a.Dk, keys) && one(&m.q, a.q, a.Dk, keys) && one(&m.v, v, a.Dv, values) && (!out || one(&m.out, out, a.Dv, values));
+    return one(&m.k, a.k, true) && one(&m.q, a.q, true) && one(&m.v, v, false) && one(&m.more, a.v, false) && one(&m.out, out, outk != nullptr) && one(&m.outk, outk, true);
 }
-
 struct DeltaSizes { size_t images, gates, maps, starts, dstates, dz, all; };          // bytes of the parts of a workspace, in this order
 DeltaSizes delta_sizes(const DeltaArgs &a, int dtype, bool backward);
 int launch_delta_prepare(DeltaArgs a, int dtype, cudaStream_t st);

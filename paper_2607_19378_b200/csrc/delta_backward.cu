@@ -278,58 +278,62 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
 
 template <typename T, int KD> struct Grads {
     static constexpr int PI = Planes<T>::IN, PM = Planes<T>::MID, TILE = KD * 128;
-    // images: dY | K | Q | U | dZ (later E) | A (later F), and a state as it is kept.  With three planes there is no room for the last, and
-    // Q comes into dY's place once that is through.
+    // images: dY | K | Q | U (values before it, dQ and dK behind it) | dZ (later E) | A (later F), and a state as it is kept.  With three planes
+    // there is no room for the last, and Q comes into dY's place once that is through.
     static constexpr bool ROOM = PI == 1;
     static constexpr int DY = 0, K = PI * TILE, Q = ROOM ? 2 * PI * TILE : DY, U = (ROOM ? 3 : 2) * PI * TILE, DZ = U + PM * TILE, A = DZ + PM * TILE, STATE = A + PM * kMatrix,
                          BYTES = 1024 + STATE + (ROOM ? KD * KD * 4 : 0);
-    // tensor memory: a state as an operand | six sums of 64 columns, Z as an operand in the second and third
-    static constexpr int S0 = 0, SCOLS = PM * KD / 2, R0 = SCOLS;
-    static constexpr int SUMS = PI < PM ? 6 : 5;
-    static_assert(R0 + SUMS * kTok <= 512 && BYTES + 6144 <= 227 * 1024 && PM * kTok / 2 <= 2 * kTok && PM * TILE >= PM * kMatrix, "tensor and shared memory");
+    // tensor memory: a state as an operand | sums of 64 columns:
+    //     0: S0 k, U, S0 dY   1: Z (and 2), dY U^T and dZ U^T, F k   2: K K^T, E k and the erased part of dK   3: S0 dZ, F q and E k   4: dS1 u
+    // and, where a plane is left over, 5: the rest of dZ U^T
+    static constexpr int S0 = 0, SCOLS = PM * KD / 2, R0 = SCOLS, SUMS = PI < PM ? 6 : 5;
+    static_assert(R0 + SUMS * kTok <= 512 && BYTES + 7168 <= 227 * 1024 && PM * kTok / 2 <= 2 * kTok && PM * TILE >= PM * kMatrix, "tensor and shared memory");
 };
+constexpr int kGradThreads = 512;
 
-// x[c] summed over the warp's lanes; lane l is left with column l
-__device__ __forceinline__ float column_sum(float (&x)[32], int lane)
+// x[c] summed over the warp's lanes: lanes 4 c .. 4 c + 3 are left with column c
+__device__ __forceinline__ float column_sum8(float (&x)[8], int lane)
 {
 #pragma unroll
-    for (int m = 16; m; m >>= 1) {
-        const bool up = lane & m;
+    for (int m = 4; m; m >>= 1) {
+        const bool up = lane & (4 * m);
 #pragma unroll
         for (int c = 0; c < m; ++c) {
             const float give = up ? x[c] : x[c + m], keep = up ? x[c + m] : x[c];
-            x[c] = keep + __shfl_xor_sync(~0u, give, m);
+            x[c] = keep + __shfl_xor_sync(~0u, give, 4 * m);
         }
     }
-    return x[0];
+    x[0] += __shfl_xor_sync(~0u, x[0], 1);
+    return x[0] + __shfl_xor_sync(~0u, x[0], 2);
 }
 
-template <typename T, int KD> __global__ void __launch_bounds__(256, 1) delta_gradients_kernel(DeltaArgs a, const __grid_constant__ DeltaMaps maps)
+// 512 threads: a lane's columns in four quarters of 16 tokens (KD / 4 of a state), taken eight at a time: the loops stay rolled, as code that
+// runs once per CTA is bound by its fetching (unrolled over 32 columns, 256 threads: 1350 us on 6144 chunks of 128 channels).
+template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1) delta_gradients_kernel(DeltaArgs a, const __grid_constant__ DeltaMaps maps)
 {
     using C = Grads<T, KD>;
-    constexpr int PI = C::PI, PM = C::PM, HC = KD / 2;
+    constexpr int PI = C::PI, PM = C::PM, HC = KD / 4;
     extern __shared__ __align__(1024) unsigned char raw[];
     __shared__ WalkShared ws;                                // bar_a: products, full[0]: a head's inputs, full[1]: the gradient behind the chunk
     __shared__ __align__(16) float gates[kGates];
-    __shared__ float sums[3][4][kTok], erased[2][kTok], total[8];
+    __shared__ float sums[3][4][kTok], erased[4][kTok], total[16];
     const float *gamma = gates, *delta = gates + kTok, *beta = gates + 2 * kTok, *ghi = gates + 3 * kTok, *glo = gates + 4 * kTok;
     unsigned char *sm = align_images(raw);
-    const int tid = threadIdx.x, warp = uniform_warp(tid >> 5), lane = tid & 31, row = 32 * (warp & 3) + lane, half = warp >> 2, share = a.H / a.Hk;
+    const int tid = threadIdx.x, lane = tid & 31, warp = uniform_warp(tid >> 5), row = 32 * (warp & 3) + lane, quarter = warp >> 2, share = a.H / a.Hk;
     const long long bk = blockIdx.x / a.chunks;
-    const int chunk = (int)(blockIdx.x % a.chunks), b = (int)(bk / a.Hk), hk = (int)(bk % a.Hk), t0 = chunk * kTok, t = t0 + 32 * half;
+    const int chunk = (int)(blockIdx.x % a.chunks), b = (int)(bk / a.Hk), hk = (int)(bk % a.Hk), t0 = chunk * kTok, t = t0 + 16 * quarter;
     pdl_wait();
     const int n = live_tokens(a, b), nv = n - t0 < kTok ? n - t0 : kTok, room = a.L - t0 < kTok ? a.L - t0 : kTok, rows8 = kept_rows(a.Dv);
     const long long qrow = (bk * a.Dk + row) * a.L + t, qk = bk * a.Dk * a.L + t0, all = (long long)a.B * a.Hk * a.Dk * a.L, vall = (long long)a.B * a.H * a.Dv * a.L;
     const long long kept = kept_floats(a.Dv, a.Dk);
-    float dq[32], dk[32];
-#pragma unroll
-    for (int e = 0; e < 32; ++e) dq[e] = dk[e] = 0.f;
     if (nv <= 0) {                                           // nothing of this chunk counts
-        if (row < a.Dk && t < a.L) {
-            store_row<T>((T *)a.dq, qrow, a.L, a.L - t, 0, dq);
-            store_row<T>((T *)a.dk, qrow, a.L, a.L - t, 0, dk);
-        }
-        for (int i = tid; i < share * room; i += 256) {
+        const float none[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        for (int g = 0; g < 16; g += 8)
+            if (row < a.Dk && t + g < a.L) {
+                store8<T>((T *)a.dq, qrow + g, a.L, a.L - t - g, 0, none);
+                store8<T>((T *)a.dk, qrow + g, a.L, a.L - t - g, 0, none);
+            }
+        for (int i = tid; i < share * room; i += kGradThreads) {
             const long long at = (((long long)b * a.H + hk * share + i / room) * a.L) + t0 + i % room;
             HN_G(a.dbeta + at, 4);
             a.dbeta[at] = 0.f;
@@ -339,7 +343,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(256, 1) delta_gr
     }
     const bool copied = by_copy(a, nv, t0);
     if (tid == 0) {
-        mbar_init(&ws.bar_a, 1); mbar_init(&ws.full[0], 1); mbar_init(&ws.full[1], 1);
+        mbar_init(&ws.bar_a, 1); mbar_init(&ws.bar_b, 1); mbar_init(&ws.full[0], 1); mbar_init(&ws.full[1], 1);
         ws.gave_up = 0;
         fence_mbar_init();
     }
@@ -348,7 +352,11 @@ template <typename T, int KD> __global__ void __launch_bounds__(256, 1) delta_gr
     const int ksteps = (a.Dk + 15) / 16, vsteps = (a.Dv + 15) / 16;
     const unsigned images = smem_u32(sm), IK = images + C::K, IU = images + C::U, IZ = images + C::DZ, IA = images + C::A, IY = images + C::DY, IQ = images + C::Q;
     unsigned par = 0, tb = 0;
-    float x[32], y[32], erase[32];
+    float dq[2][8], dk[2][8];
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dq[g][e] = dk[g][e] = 0.f;
     auto go = [&] {                                          // what the threads wrote, for the products
         tmem_wait_st();
         fence_async_smem();
@@ -357,144 +365,159 @@ template <typename T, int KD> __global__ void __launch_bounds__(256, 1) delta_gr
         tmem_fence_after_sync();
     };
     auto done = [&] {
-        __syncwarp();
         WAIT(&ws.bar_a, par);
         par ^= 1;
         tmem_fence_after_sync();
     };
     for (int j = 0; j < share; ++j) {
-        const long long bh = (long long)b * a.H + hk * share + j, at = bh * a.chunks + chunk, grow = bh * a.L + t0;
+        const long long bh = (long long)b * a.H + hk * share + j, at = bh * a.chunks + chunk, grow = bh * a.L + t0, vrow = (bh * a.Dv + row) * a.L + t;
         const float *S = a.marks + at * kept, *D = a.dstates + at * kept;
         if (j) {                                             // the images and sums of the head before have been read
             fence_async_smem();
             __syncthreads();
         }
         if (tid == 0) {
-            mbar_expect_tx(&ws.full[0], PM * kMatrix + kGates * 4 + (C::ROOM ? (unsigned)(kept * 4) : 0) + (copied ? (j ? 1 : 3) * C::TILE : 0));
-            if (C::ROOM) bulk_load(sm + C::STATE, S, (unsigned)(kept * 4), &ws.full[0]);
+            mbar_expect_tx(&ws.full[0], PM * kMatrix + kGates * 4 + (C::ROOM ? (unsigned)(kept * 4) : 0) + (copied ? (j ? 2 : 4) * C::TILE : 0));
             if (copied) {
                 if (!j) tma_load_3d(sm + C::K, &maps.k, &ws.full[0], t0, 0, (int)bk);
+                tma_load_3d(sm + C::U, &maps.more, &ws.full[0], t0, 0, (int)bh);
                 tma_load_3d(sm + C::DY, &maps.v, &ws.full[0], t0, 0, (int)bh);
                 if (!j) tma_load_3d(sm + C::Q, &maps.q, &ws.full[0], t0, 0, (int)bk);
             }
+            if (C::ROOM) bulk_load(sm + C::STATE, S, (unsigned)(kept * 4), &ws.full[0]);
             bulk_load(gates, a.gates + at * kGates, kGates * 4, &ws.full[0]);
             bulk_load(sm + C::A, a.images + at * (2 * PM * kMatrix), PM * kMatrix, &ws.full[0]);
         }
         __syncwarp();
-        float dz[32];
-        {
-            const float4 *from = (const float4 *)a.dz + (at * 16 + 8 * half) * rows8 + row;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (row < rows8) { HN_G(from + e * rows8, 16); w = from[e * rows8]; }
-                dz[4 * e] = w.x; dz[4 * e + 1] = w.y; dz[4 * e + 2] = w.z; dz[4 * e + 3] = w.w;
-            }
-        }
-        RowPart<T> v;
-        v.load((const T *)a.v, (bh * a.Dv + row) * a.L + t, vall, a.L, row < a.Dv ? n - t : 0);
         if (!copied) {
-            load_tile<T>(sm + C::DY, C::TILE, (const T *)a.dy, bh * a.Dv * a.L + t0, vall, a.L, a.Dv, nv, tid, 256);
-            clear_rows(sm + C::DY, C::TILE, PI, a.Dv, KD, tid, 256);
+            load_tile<T>(sm + C::DY, C::TILE, (const T *)a.dy, bh * a.Dv * a.L + t0, vall, a.L, a.Dv, nv, tid, kGradThreads);
+            clear_rows(sm + C::DY, C::TILE, PI, a.Dv, KD, tid, kGradThreads);
             if (!j) {
-                load_tile<T>(sm + C::K, C::TILE, (const T *)a.k, qk, all, a.L, a.Dk, nv, tid, 256);
-                clear_rows(sm + C::K, C::TILE, PI, a.Dk, KD, tid, 256);
+                load_tile<T>(sm + C::K, C::TILE, (const T *)a.k, qk, all, a.L, a.Dk, nv, tid, kGradThreads);
+                clear_rows(sm + C::K, C::TILE, PI, a.Dk, KD, tid, kGradThreads);
                 if (C::ROOM) {
-                    load_tile<T>(sm + C::Q, C::TILE, (const T *)a.q, qk, all, a.L, a.Dk, nv, tid, 256);
-                    clear_rows(sm + C::Q, C::TILE, PI, a.Dk, KD, tid, 256);
+                    load_tile<T>(sm + C::Q, C::TILE, (const T *)a.q, qk, all, a.L, a.Dk, nv, tid, kGradThreads);
+                    clear_rows(sm + C::Q, C::TILE, PI, a.Dk, KD, tid, kGradThreads);
                 }
             }
+            load_tile<T>(sm + C::U, C::TILE, (const T *)a.v, bh * a.Dv * a.L + t0, vall, a.L, a.Dv, nv, tid, kGradThreads);
         }
-        if (row < KD) planes_to_image<PM>(sm + C::DZ, C::TILE, row, half, dz);
+        {   // dZ as an image
+            const float4 *from = (const float4 *)a.dz + (at * 16 + 4 * quarter) * rows8 + row;
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                float x[8];
+#pragma unroll
+                for (int e = 0; e < 8; e += 4) {
+                    float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (row < rows8) { HN_G(from + (2 * g + e / 4) * rows8, 16); w = from[(2 * g + e / 4) * rows8]; }
+                    x[e] = w.x; x[e + 1] = w.y; x[e + 2] = w.z; x[e + 3] = w.w;
+                }
+                if (row < KD) planes8_to_image<PM>(sm + C::DZ, C::TILE, row, 2 * quarter + g, x);
+            }
+        }
         tmem_fence_before_sync();
         __syncthreads();                                     // (tensor memory and its barrier are there)
         tmem_fence_after_sync();
         WAIT(&ws.full[0], j & 1);
         tb = ws.slot;
-        const unsigned lane_s = tmem_addr(tb, warp, C::S0 + half * (HC / 2)), lane_r = tmem_addr(tb, warp, C::R0 + half * 32);
+        const unsigned lane_s = tmem_addr(tb, warp, C::S0 + quarter * (HC / 2)), lane_r = tmem_addr(tb, warp, C::R0 + quarter * 16);
         const float4 *held = C::ROOM ? (const float4 *)(sm + C::STATE) : nullptr;
-        {   // the state before the chunk, its rows as lanes: S0 k
-            float s[HC];
+        // the state before the chunk, its rows as lanes: S0 k
+#pragma unroll 1
+        for (int e = 0; e < HC; e += 8) {
+            float s[8];
 #pragma unroll
-            for (int e = 0; e < HC; e += 4) {
-                const int c = half * HC + e;
+            for (int i = 0; i < 8; i += 4) {
+                const int c = quarter * HC + e + i;
                 float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
                 if (row < rows8 && c < a.Dk) {
-                    const int i = kept_at(row, c >> 2, rows8);
-                    if (C::ROOM) w = held[i];
-                    else { HN_G((const float4 *)S + i, 16); w = ((const float4 *)S)[i]; }
+                    const int k = kept_at(row, c >> 2, rows8);
+                    if (C::ROOM) w = held[k];
+                    else { HN_G((const float4 *)S + k, 16); w = ((const float4 *)S)[k]; }
                 }
-                s[e] = w.x; s[e + 1] = w.y; s[e + 2] = w.z; s[e + 3] = w.w;
+                s[i] = w.x; s[i + 1] = w.y; s[i + 2] = w.z; s[i + 3] = w.w;
             }
-            planes_to_tmem<PM, HC / 2>(lane_s, KD / 2, s);
+            planes8_to_tmem<PM>(lane_s + e / 2, KD / 2, s);
         }
         go();
         if (warp == 0) {
-            issue_ts<PM, PI, PM, true, KD / 16>(tb + C::R0, tb + C::S0, KD / 2, IK, C::TILE, ksteps, kTok, false);
+            issue_ts<PM, PI, PM, true, KD / 16, B_ALL, 1>(tb + C::R0, tb + C::S0, KD / 2, IK, C::TILE, ksteps, kTok, false);
             umma_commit(&ws.bar_a);
         }
         done();
-        TmemIO<32>::ld(x, lane_r);
-        tmem_wait_ld();
+#pragma unroll 1
+        for (int g = 0; g < 2; ++g) {                        // R, Z and what dZ R says about beta
+            const int c = 16 * quarter + 8 * g;
+            float x[8], v[8], z[8];
+            tmem_ld8(x, lane_r + 8 * g);
+            if (row < KD) {
+                image8<PI>(v, sm + C::U, C::TILE, row, c >> 3);
+                image8<PM>(z, sm + C::DZ, C::TILE, row, c >> 3);
+            }
+            tmem_wait_ld();
 #pragma unroll
-        for (int e = 0; e < 32; ++e) {
-            const int i = 32 * half + e;
-            x[e] = fmaf(-gamma[i], x[e], v.get(e));                         // R
-            y[e] = dz[e] * x[e];
-            x[e] *= beta[i];
+            for (int e = 0; e < 8; ++e) {
+                x[e] = row < a.Dv ? fmaf(-gamma[c + e], x[e], v[e]) : 0.f;
+                z[e] = row < a.Dv ? z[e] * x[e] : 0.f;
+                x[e] *= beta[c + e];
+            }
+            planes8_to_tmem<PM>(tmem_addr(tb, warp, C::R0 + kTok + quarter * 8 + 4 * g), kTok / 2, x);
+            const float sum = column_sum8(z, lane);
+            if (!(lane & 3)) sums[0][warp & 3][c + (lane >> 2)] = sum;
         }
-        planes_to_tmem<PM, 16>(tmem_addr(tb, warp, C::R0 + kTok + half * 16), kTok / 2, x);
         go();
         if (warp == 0) {
-            issue_ts<PM, PM, PM, false, kTok / 16, B_LOWER>(tb + C::R0, tb + C::R0 + kTok, kTok / 2, IA, kMatrix, kTok / 16, kTok, false);
+            issue_ts<PM, PM, PM, false, kTok / 16, B_LOWER, 1>(tb + C::R0, tb + C::R0 + kTok, kTok / 2, IA, kMatrix, kTok / 16, kTok, false);
             umma_commit(&ws.bar_a);
         }
-        sums[0][warp & 3][32 * half + lane] = column_sum(y, lane);
         // a state with its columns as lanes; `with`: the sum of its products with the one that is there
         auto columns = [&](const float *p, bool with) {
-            float s[32], inner = 0.f;
-            const int q7 = (row >> 2) & 7, mine = row < a.Dk ? (row >> 2) * rows8 * 4 + (row & 3) : 0;
+            float inner = 0.f;
+            const int q7 = (row >> 2) & 7;
+            const float *mine = (C::ROOM ? (const float *)held : p) + (row < a.Dk ? (row >> 2) * rows8 * 4 + (row & 3) : 0);
+#pragma unroll 1
+            for (int c = 0; c < HC; c += 8) {
+                const int r = quarter * HC + c;              // rows r .. r + 7, all kept or none
+                float s[8];
 #pragma unroll
-            for (int c = 0; c < HC; c += 32) {
-#pragma unroll
-                for (int g = 0; g < 32; g += 8) {
-                    const int r = half * HC + c + g;         // rows r .. r + 7, all kept or none
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) s[g + e] = 0.f;
-                    if (r >= rows8) continue;
-                    const float *from = (C::ROOM ? (const float *)held : p) + mine + r * 4;
+                for (int e = 0; e < 8; ++e) s[e] = 0.f;
+                if (r < rows8 && row < a.Dk) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        if (!C::ROOM) HN_G(from + (e ^ q7) * 4, 4);
-                        s[g + e] = from[(e ^ q7) * 4];
-                    }
-                    if (row >= a.Dk) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) s[g + e] = 0.f;
+                        if (!C::ROOM) HN_G(mine + r * 4 + (e ^ q7) * 4, 4);
+                        s[e] = mine[r * 4 + (e ^ q7) * 4];
                     }
                 }
+                __syncwarp();
                 if (with) {
-                    float o[16];
+                    unsigned o[PM][4];
 #pragma unroll
-                    for (int q = 0; q < PM; ++q) {
-                        TmemIO<16>::ld(o, lane_s + q * (KD / 2) + c / 2);
-                        tmem_wait_ld();
+                    for (int q = 0; q < PM; ++q)
+                        asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];\n"
+                                     : "=r"(o[q][0]), "=r"(o[q][1]), "=r"(o[q][2]), "=r"(o[q][3]) : "r"(lane_s + q * (KD / 2) + c / 2) : "memory");
+                    tmem_wait_ld();
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            inner = fmaf(__uint_as_float(__float_as_uint(o[e]) << 16), s[2 * e], inner);
-                            inner = fmaf(__uint_as_float(__float_as_uint(o[e]) & 0xffff0000u), s[2 * e + 1], inner);
+                    for (int q = 0; q < PM; ++q)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            inner = fmaf(__uint_as_float(o[q][e] << 16), s[2 * e], inner);
+                            inner = fmaf(__uint_as_float(o[q][e] & 0xffff0000u), s[2 * e + 1], inner);
                         }
-                    }
                 }
-                planes_to_tmem<PM, 16>(lane_s + c / 2, KD / 2, s);
+                planes8_to_tmem<PM>(lane_s + c / 2, KD / 2, s);
             }
             return inner;
         };
         columns(S, false);
         done();
-        TmemIO<32>::ld(x, lane_r);
-        tmem_wait_ld();
-        if (row < KD) planes_to_image<PM>(sm + C::U, C::TILE, row, half, x);
+#pragma unroll 1
+        for (int g = 0; g < 2; ++g) {
+            float x[8];
+            tmem_ld8(x, lane_r + 8 * g);
+            tmem_wait_ld();
+            if (row < KD) planes8_to_image<PM>(sm + C::U, C::TILE, row, 2 * quarter + g, x);
+        }
         go();
         if (warp == 0) {
             if (C::ROOM && lane == 0) {                      // the state has been read: the gradient behind the chunk into its place
@@ -503,115 +526,115 @@ template <typename T, int KD> __global__ void __launch_bounds__(256, 1) delta_gr
             }
             __syncwarp();
             // rows 0 .. 63: dY U^T, rows 64 ..: dZ U^T; where dY is one plane, dZ's second goes into a sum of its own
-            issue_ss<PI, PM, PM, true, true, KD / 16>(tb + C::R0 + kTok, IY, C::TILE, C::DZ - C::DY, IU, C::TILE, vsteps, kTok, false);
-            if (PI < PM) issue_ss<1, 1, PM, true, true, KD / 16>(tb + C::R0 + 5 * kTok, IY + C::TILE, C::TILE, C::DZ - C::DY, IU, C::TILE, vsteps, kTok, false);
+            issue_ss<PI, PM, PM, true, true, KD / 16, B_ALL, 1>(tb + C::R0 + kTok, IY, C::TILE, C::DZ - C::DY, IU, C::TILE, vsteps, kTok, false);
+            if (PI < PM) issue_ss<1, 1, 1, true, true, KD / 16, B_ALL, 1>(tb + C::R0 + 5 * kTok, IY + C::TILE, C::TILE, C::DZ - C::DY, IU, C::TILE, vsteps, kTok, false);
             // rows 64 ..: K K^T
-            issue_ss<PI, PI, PI, true, true, KD / 16>(tb + C::R0 + 2 * kTok, IY, C::TILE, C::K - C::DY, IK, C::TILE, ksteps, kTok, false);
-            issue_ts<PM, PI, PM, true, KD / 16>(tb + C::R0, tb + C::S0, KD / 2, IY, C::TILE, vsteps, kTok, false);
-            issue_ts<PM, PM, PM, true, KD / 16>(tb + C::R0 + 3 * kTok, tb + C::S0, KD / 2, IZ, C::TILE, vsteps, kTok, false);
+            issue_ss<PI, PI, PI, true, true, KD / 16, B_ALL, 1>(tb + C::R0 + 2 * kTok, IY, C::TILE, C::K - C::DY, IK, C::TILE, ksteps, kTok, false);
             umma_commit(&ws.bar_a);
+            issue_ts<PM, PI, PM, true, KD / 16, B_ALL, 1>(tb + C::R0, tb + C::S0, KD / 2, IY, C::TILE, vsteps, kTok, false);
+            issue_ts<PM, PM, PM, true, KD / 16, B_ALL, 1>(tb + C::R0 + 3 * kTok, tb + C::S0, KD / 2, IZ, C::TILE, vsteps, kTok, false);
+            umma_commit(&ws.bar_b);
         }
         done();
-        __syncthreads();                                     // every thread's wait is over: A and dZ may go
-        {
+        {   // F and E in the lower triangles, where their lanes' rows are tokens
             const int i = row & 63;
             const float Hi = ghi[i], Li = glo[i], bi = beta[i];
-            TmemIO<32>::ld(x, lane_r + kTok);
-            TmemIO<32>::ld(y, lane_r + 2 * kTok);
-            tmem_wait_ld();
-            if (PI < PM && row >= kTok) {
-                float z[32];
-                TmemIO<32>::ld(z, lane_r + 5 * kTok);
+            float own = 0.f;
+#pragma unroll 1
+            for (int g = 0; g < 2; ++g) {
+                const int c0 = 16 * quarter + 8 * g;
+                float x[8], y[8], z[8];
+                tmem_ld8(x, lane_r + kTok + 8 * g);
+                tmem_ld8(y, lane_r + 2 * kTok + 8 * g);
+                if (PI < PM) tmem_ld8(z, lane_r + 5 * kTok + 8 * g);
                 tmem_wait_ld();
 #pragma unroll
-                for (int e = 0; e < 32; ++e) x[e] += z[e];
-            }
-            float own = 0.f;
-#pragma unroll
-            for (int e = 0; e < 32; ++e) {
-                const int c = 32 * half + e;
-                const float r = ratio(Hi, Li, ghi[c], glo[c]);
-                if (row < kTok) x[e] = c <= i ? r * x[e] : 0.f;
-                else {
-                    own += c < i ? x[e] * r * y[e] : 0.f;
-                    x[e] = c < i ? -bi * r * x[e] : 0.f;
+                for (int e = 0; e < 8; ++e) {
+                    const int c = c0 + e;
+                    const float r = ratio(Hi, Li, ghi[c], glo[c]);
+                    if (warp & 2) {
+                        if (PI < PM) x[e] += z[e];
+                        own += c < i ? x[e] * r * y[e] : 0.f;
+                        x[e] = c < i ? -bi * r * x[e] : 0.f;
+                    } else x[e] = c <= i ? r * x[e] : 0.f;
                 }
+                // (dZ's image is in use until the products of the states are through)
+                if (g == 0 && (warp & 2)) WAIT(&ws.bar_b, j & 1);
+                planes8_to_image<PM>(sm + (warp & 2 ? C::DZ : C::A), kMatrix, i, c0 >> 3, x);
             }
-            if (row < kTok) planes_to_image<PM>(sm + C::A, kMatrix, i, half, x);                // F
-            else {
-                planes_to_image<PM>(sm + C::DZ, kMatrix, i, half, x);                           // E
-                erased[half][i] = own;
-            }
+            if (warp & 2) erased[quarter][i] = own;
         }
-        TmemIO<32>::ld(x, lane_r);
-        TmemIO<32>::ld(erase, lane_r + 3 * kTok);
-        tmem_wait_ld();
-#pragma unroll
-        for (int e = 0; e < 32; ++e) {
-            const float ga = gamma[32 * half + e];
-            x[e] *= ga;
-            erase[e] *= -ga * beta[32 * half + e];
-        }
+        WAIT(&ws.bar_b, j & 1);
         go();
         if (warp == 0) {
-            issue_ss<PI, PM, PM, false, false, kTok / 16, B_LOWER>(tb + C::R0 + kTok, IK, C::TILE, 0, IA, kMatrix, kTok / 16, kTok, false);         // F k
-            issue_ss<PI, PM, PM, false, false, kTok / 16, B_LOWER>(tb + C::R0 + 2 * kTok, IK, C::TILE, 0, IZ, kMatrix, kTok / 16, kTok, false);     // E k
+            issue_ss<PI, PM, PM, false, false, kTok / 16, B_LOWER, 1>(tb + C::R0 + kTok, IK, C::TILE, 0, IA, kMatrix, kTok / 16, kTok, false);         // F k
+            issue_ss<PI, PM, PM, false, false, kTok / 16, B_LOWER, 1>(tb + C::R0 + 2 * kTok, IK, C::TILE, 0, IZ, kMatrix, kTok / 16, kTok, false);     // E k
             umma_commit(&ws.bar_a);
         }
-        __syncwarp();
         if (C::ROOM) WAIT(&ws.full[1], j & 1);
         float inner = columns(D, true);
 #pragma unroll
         for (int m = 1; m < 32; m <<= 1) inner += __shfl_xor_sync(~0u, inner, m);
         if (lane == 0) total[warp] = inner;
         if (!C::ROOM) {                                      // queries take dY's place
-            load_tile<T>(sm + C::Q, C::TILE, (const T *)a.q, qk, all, a.L, a.Dk, nv, tid, 256);
-            clear_rows(sm + C::Q, C::TILE, PI, a.Dk, KD, tid, 256);
+            load_tile<T>(sm + C::Q, C::TILE, (const T *)a.q, qk, all, a.L, a.Dk, nv, tid, kGradThreads);
+            clear_rows(sm + C::Q, C::TILE, PI, a.Dk, KD, tid, kGradThreads);
         }
         done();
-        TmemIO<32>::ld(y, lane_r + kTok);
-        tmem_wait_ld();
-#pragma unroll
-        for (int e = 0; e < 32; ++e) {
-            x[e] += y[e];                                    // dQ of this head
-            dq[e] += x[e];
-        }
-        TmemIO<32>::ld(y, lane_r + 2 * kTok);
-        tmem_wait_ld();
-#pragma unroll
-        for (int e = 0; e < 32; ++e) erase[e] += y[e];
-        go();
-        if (warp == 0) {
-            issue_ts<PM, PM, PM, true, KD / 16>(tb + C::R0, tb + C::S0, KD / 2, IU, C::TILE, vsteps, kTok, false);                                  // dS1 u
-            issue_ss<PI, PM, PM, false, true, kTok / 16, B_LOWER_T>(tb + C::R0 + kTok, IQ, C::TILE, 0, IA, kMatrix, kTok / 16, kTok, false);        // F q
-            issue_ss<PI, PM, PM, false, true, kTok / 16, B_LOWER_T>(tb + C::R0 + kTok, IK, C::TILE, 0, IZ, kMatrix, kTok / 16, kTok, true);         // E k, the other way
-            umma_commit(&ws.bar_a);
-        }
-        __syncwarp();
-        float z[32];
-        {   // what queries say about the decays, meanwhile
-            if (row < KD) image_row<PI>(z, sm + C::Q, C::TILE, row, half);
-#pragma unroll
-            for (int e = 0; e < 32; ++e) x[e] = row < a.Dk ? x[e] * z[e] : 0.f;      // (a lane without a channel holds whatever lay behind an image)
-            if (row < KD) image_row<PI>(z, sm + C::K, C::TILE, row, half);
-        }
-        done();
-        {
-            float w[32];
-            TmemIO<32>::ld(y, lane_r);
-            TmemIO<32>::ld(w, lane_r + kTok);
+#pragma unroll 1
+        for (int g = 0; g < 2; ++g) {                        // the erased part of dK, so that the third sum is free
+            const int c = 16 * quarter + 8 * g;
+            float x[8], y[8];
+            tmem_ld8(x, lane_r + 2 * kTok + 8 * g);
+            tmem_ld8(y, lane_r + 3 * kTok + 8 * g);
             tmem_wait_ld();
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-                y[e] *= delta[32 * half + e];
-                w[e] += y[e];
-                dk[e] += erase[e] + w[e];
-                x[e] = row < a.Dk ? fmaf(z[e], erase[e] - w[e], x[e]) : 0.f;
-                y[e] = row < a.Dk ? y[e] * z[e] : 0.f;
+            for (int e = 0; e < 8; ++e) x[e] = fmaf(-gamma[c + e] * beta[c + e], y[e], x[e]);
+            tmem_st8(lane_r + 2 * kTok + 8 * g, x);
+        }
+        go();
+        if (warp == 0) {
+            issue_ss<PI, PM, PM, false, true, kTok / 16, B_LOWER_T, 1>(tb + C::R0 + 3 * kTok, IQ, C::TILE, 0, IA, kMatrix, kTok / 16, kTok, false);        // F q
+            issue_ss<PI, PM, PM, false, true, kTok / 16, B_LOWER_T, 1>(tb + C::R0 + 3 * kTok, IK, C::TILE, 0, IZ, kMatrix, kTok / 16, kTok, true);         // E k, the other way
+            issue_ts<PM, PM, PM, true, KD / 16, B_ALL, 1>(tb + C::R0 + 4 * kTok, tb + C::S0, KD / 2, IU, C::TILE, vsteps, kTok, false);                   // dS1 u
+            umma_commit(&ws.bar_a);
+        }
+        done();
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            const int c = 16 * quarter + 8 * g;
+            const bool in = row < a.Dk;                      // (a lane without a channel holds whatever lay behind an image)
+            float x[8], y[8], z[8], w[8];
+            tmem_ld8(x, lane_r + 8 * g);
+            tmem_ld8(y, lane_r + kTok + 8 * g);
+            if (row < KD) image8<PI>(z, sm + C::Q, C::TILE, row, c >> 3);
+            tmem_wait_ld();
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                x[e] = fmaf(gamma[c + e], x[e], y[e]);       // dQ of this head
+                dq[g][e] += x[e];
+                x[e] = in ? x[e] * z[e] : 0.f;
+            }
+            tmem_ld8(y, lane_r + 2 * kTok + 8 * g);
+            tmem_ld8(w, lane_r + 3 * kTok + 8 * g);
+            float u[8];
+            tmem_ld8(u, lane_r + 4 * kTok + 8 * g);
+            if (row < KD) image8<PI>(z, sm + C::K, C::TILE, row, c >> 3);
+            tmem_wait_ld();
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                u[e] *= delta[c + e];
+                w[e] += u[e];
+                dk[g][e] += y[e] + w[e];
+                x[e] = in ? fmaf(z[e], y[e] - w[e], x[e]) : 0.f;
+                u[e] = in ? u[e] * z[e] : 0.f;
+            }
+            const float s1 = column_sum8(x, lane), s2 = column_sum8(u, lane);
+            if (!(lane & 3)) {
+                sums[1][warp & 3][c + (lane >> 2)] = s1;
+                sums[2][warp & 3][c + (lane >> 2)] = s2;
             }
         }
-        sums[1][warp & 3][32 * half + lane] = column_sum(x, lane);
-        sums[2][warp & 3][32 * half + lane] = column_sum(y, lane);
         __syncthreads();
         if (warp < 2) {                                      // two tokens a lane of warp 0: sums from the chunk's end; warp 1: beta
             float s[2];
@@ -625,7 +648,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(256, 1) delta_gr
                 } else {
 #pragma unroll
                     for (int w = 0; w < 4; ++w) v += sums[0][w][i];
-                    v -= erased[0][i] + erased[1][i];
+                    v -= (erased[0][i] + erased[1][i]) + (erased[2][i] + erased[3][i]);
                 }
                 s[e] = v;
             }
@@ -636,7 +659,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(256, 1) delta_gr
 #pragma unroll
                 for (int m = 1; m < 32; m <<= 1) written += __shfl_xor_sync(~0u, written, m);
 #pragma unroll
-                for (int w = 0; w < 8; ++w) in += total[w];
+                for (int w = 0; w < 16; ++w) in += total[w];
                 double v = (double)s[0] + s[1];
                 double run = v;                              // (sums of many signs: in 64 bits)
 #pragma unroll
@@ -662,9 +685,29 @@ template <typename T, int KD> __global__ void __launch_bounds__(256, 1) delta_gr
             }
         }
     }
-    if (row < a.Dk && t < a.L) {
-        store_row<T>((T *)a.dq, qrow, a.L, a.L - t, n - t, dq);
-        store_row<T>((T *)a.dk, qrow, a.L, a.L - t, n - t, dk);
+    if (C::ROOM && a.copies) {                               // U is through: the results into its place, and away by copies
+        if (row < KD) {
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                *(uint4 *)(sm + C::U + image_at(row, 2 * quarter + g)) = bf16_8(dq[g], n - t - 8 * g);
+                *(uint4 *)(sm + C::U + C::TILE + image_at(row, 2 * quarter + g)) = bf16_8(dk[g], n - t - 8 * g);
+            }
+        }
+        fence_async_smem();
+        __syncthreads();
+        if (tid == 0) {
+            tma_store_3d(&maps.out, sm + C::U, t0, 0, (int)bk);
+            tma_store_3d(&maps.outk, sm + C::U + C::TILE, t0, 0, (int)bk);
+            tma_commit();
+            tma_wait_all0();
+        }
+    } else if (row < a.Dk) {
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+            if (t + 8 * g < a.L) {
+                store8<T>((T *)a.dq, qrow + 8 * g, a.L, a.L - t - 8 * g, n - t - 8 * g, dq[g]);
+                store8<T>((T *)a.dk, qrow + 8 * g, a.L, a.L - t - 8 * g, n - t - 8 * g, dk[g]);
+            }
     }
     tmem_fence_before_sync();
     __syncthreads();
@@ -682,14 +725,15 @@ int delta_backward_status()
 template <typename T, int KD> static int launch_back(DeltaArgs a, cudaStream_t st)
 {
     DeltaMaps m{};
-    a.copies = delta_maps<T>(m, a, KD, a.dy, a.dv);
+    a.copies = delta_maps<T>(m, a, KD, a.dy, a.dv, nullptr);
     const long long blocks = (long long)a.B * a.H * a.segments;
     if (a.segments > 1) {
         if (const int e = launch_delta<delta_walk_back_kernel<T, KD, WALK_MAPS>>(a, 2 * blocks, kWalkThreads, WalkBack<T, KD>::BYTES, st, m)) return e;
         if (const int e = launch_delta_join(a, a.ds_end, true, st)) return e;
     }
     if (const int e = launch_delta<delta_walk_back_kernel<T, KD, WALK_RUN>>(a, blocks, kWalkThreads, WalkBack<T, KD>::BYTES, st, m)) return e;
-    return launch_delta<delta_gradients_kernel<T, KD>>(a, (long long)a.B * a.Hk * a.chunks, 256, Grads<T, KD>::BYTES, st, m);
+    a.copies = delta_maps<T>(m, a, KD, a.dy, a.dq, a.dk);
+    return launch_delta<delta_gradients_kernel<T, KD>>(a, (long long)a.B * a.Hk * a.chunks, kGradThreads, Grads<T, KD>::BYTES, st, m);
 }
 int launch_delta_backward(const DeltaArgs &a, int dtype, cudaStream_t st)
 {
