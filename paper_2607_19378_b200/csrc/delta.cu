@@ -234,7 +234,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
     last = last < end ? last : end;
     if (warp == 0) tmem_alloc(smem_u32(&ws.slot), 512);
     if (tid == 0) {
-        for (int s = 0; s < C::STAGES; ++s) { mbar_init(&ws.full[s], kFetchers + 1); mbar_init(&ws.empty[s], 1); }
+        for (int s = 0; s < C::STAGES; ++s) { mbar_init(&ws.full[s], 2); mbar_init(&ws.empty[s], 1); }
         mbar_init(&ws.bar_a, 1); mbar_init(&ws.bar_b, 1); mbar_init(&ws.bar_c, 1); mbar_init(&ws.bar_y, 1); mbar_init(&ws.ready, 8);
         ws.gave_up = 0;
         fence_mbar_init();
@@ -255,9 +255,10 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
         const long long bk = (long long)b * a.Hk + h / (a.H / a.Hk), qk = bk * a.Dk * a.L, all = (long long)a.B * a.Hk * a.Dk * a.L;
         for (int c = first, i = 0; c < last; ++c, ++i) {
             const int s = i % C::STAGES, t0 = c * kTok, nv = n - t0 < kTok ? n - t0 : kTok;
-            if (i >= C::STAGES) WAIT(&ws.empty[s], (i / C::STAGES - 1) & 1);
             unsigned char *st = sm + s * C::STAGE;
             const bool copied = by_copy(a, nv, t0), values = C::VALUES && !phi;
+            if (copied && ft) continue;                      // (one thread's work)
+            if (i >= C::STAGES) WAIT(&ws.empty[s], (i / C::STAGES - 1) & 1);
             if (ft == 0) {
                 const long long at = bh * a.chunks + c;
                 const unsigned bytes = RUN ? C::IMAGES : C::IMAGES / 2, tiles = copied ? (RUN ? 2 : 1) * C::TENSOR + (values ? C::TILE : 0) : 0;
@@ -275,9 +276,10 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
                 if (RUN) load_tile<T>(st + C::Q, C::TILE, (const T *)a.q, qk + t0, all, a.L, a.Dk, nv, ft, kFetchers);
                 if constexpr (C::VALUES)
                     if (values) load_tile<T>(st + C::V, C::TILE, (const T *)a.v, vhead + t0, vall, a.L, a.Dv, nv, ft, kFetchers);
+                fence_async_smem();
+                fetchers_sync();
             }
-            fence_async_smem();
-            mbar_arrive(&ws.full[s]);
+            if (ft == 0) mbar_arrive(&ws.full[s]);
         }
     } else if (warp == 8) {
         // ---- the products

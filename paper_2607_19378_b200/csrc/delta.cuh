@@ -512,14 +512,16 @@ __device__ __forceinline__ void issue_ts(unsigned d, unsigned a, int pa, unsigne
     for (int sum = MAX - 1; sum >= 0; --sum)
 #pragma unroll
         for (int p = 0; p <= sum; ++p)
-            if (const int q = sum - p; p < NA && q < NB)
+            if (const int q = sum - p; p < NA && q < NB) {
+                const unsigned A = a + p * pa, B = BCOLS ? umma_cols(b + q * pb, next) : umma_rows(b + q * pb);
 #pragma unroll UNROLL
                 for (int e = 0; e < STEPS; ++e) {
                     const int k = PART == B_LOWER_T ? STEPS - 1 - e : e, from = PART == B_LOWER ? 16 * k : 0, cols = PART == B_ALL ? n : PART == B_LOWER ? kTok - 16 * k : 16 * (k + 1);
-                    if (k >= steps) continue;
-                    umma_ts(d + from, a + p * pa + k * 8, BCOLS ? umma_cols(b + q * pb, k, next) : umma_rows(b + q * pb, k, from), umma_kind(cols, false, BCOLS), add);
+                    if (PART == B_ALL && k >= steps) break;
+                    umma_ts(d + from, A + k * 8, B + k * (BCOLS ? kColStep : kRowStep) + from * (128 >> 4), umma_kind(cols, false, BCOLS), add);
                     add = true;
                 }
+            }
 }
 // the same with A in images; `next`: see umma_cols
 template <int NA, int NB, int MAX, bool ACOLS, bool BCOLS, int STEPS, int PART = B_ALL, int UNROLL = STEPS>
@@ -529,15 +531,16 @@ __device__ __forceinline__ void issue_ss(unsigned d, unsigned a, int pa, unsigne
     for (int sum = MAX - 1; sum >= 0; --sum)
 #pragma unroll
         for (int p = 0; p <= sum; ++p)
-            if (const int q = sum - p; p < NA && q < NB)
+            if (const int q = sum - p; p < NA && q < NB) {
+                const unsigned A = ACOLS ? umma_cols(a + p * pa, next) : umma_rows(a + p * pa), B = BCOLS ? umma_cols(b + q * pb) : umma_rows(b + q * pb);
 #pragma unroll UNROLL
                 for (int e = 0; e < STEPS; ++e) {
                     const int k = PART == B_LOWER_T ? STEPS - 1 - e : e, from = PART == B_LOWER ? 16 * k : 0, cols = PART == B_ALL ? n : PART == B_LOWER ? kTok - 16 * k : 16 * (k + 1);
-                    if (k >= steps) continue;
-                    umma_ss(d + from, ACOLS ? umma_cols(a + p * pa, k, next) : umma_rows(a + p * pa, k),
-                            BCOLS ? umma_cols(b + q * pb, k) : umma_rows(b + q * pb, k, from), umma_kind(cols, ACOLS, BCOLS), add);
+                    if (PART == B_ALL && k >= steps) break;
+                    umma_ss(d + from, A + k * (ACOLS ? kColStep : kRowStep), B + k * (BCOLS ? kColStep : kRowStep) + from * (128 >> 4), umma_kind(cols, ACOLS, BCOLS), add);
                     add = true;
                 }
+            }
 }
 
 // the warp's number, as a value that the compiler knows to be the same in all its lanes (see umma.cuh)
@@ -568,6 +571,7 @@ __device__ __forceinline__ void walk_ready(WalkShared *w, int lane)
     __syncwarp();
     if (lane == 0) mbar_arrive(&w->ready);
 }
+__device__ __forceinline__ void fetchers_sync() { asm volatile("bar.sync 3, %0;\n" ::"n"(kFetchers) : "memory"); }
 __device__ __forceinline__ void walkers_sync() { asm volatile("bar.sync 2, 256;\n" ::: "memory"); }
 
 __device__ __forceinline__ unsigned char *align_images(unsigned char *p) { return p + ((1024u - (smem_u32(p) & 1023u)) & 1023u); }

@@ -53,7 +53,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
     const int count = last > first ? last - first : 0;
     if (warp == 0) tmem_alloc(smem_u32(&ws.slot), 512);
     if (tid == 0) {
-        for (int s = 0; s < C::STAGES; ++s) { mbar_init(&ws.full[s], kFetchers + 1); mbar_init(&ws.empty[s], 1); }
+        for (int s = 0; s < C::STAGES; ++s) { mbar_init(&ws.full[s], 2); mbar_init(&ws.empty[s], 1); }
         mbar_init(&ws.bar_a, 1); mbar_init(&ws.bar_b, 1); mbar_init(&ws.bar_c, 1); mbar_init(&ws.ready, 8);
         ws.gave_up = 0;
         fence_mbar_init();
@@ -74,9 +74,10 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
         const long long bk = (long long)b * a.Hk + h / (a.H / a.Hk), qk = bk * a.Dk * a.L, all = (long long)a.B * a.Hk * a.Dk * a.L;
         for (int i = 0; i < count; ++i) {
             const int c = last - 1 - i, s = i % C::STAGES, t0 = c * kTok, nv = n - t0 < kTok ? n - t0 : kTok;
-            if (i >= C::STAGES) WAIT(&ws.empty[s], (i / C::STAGES - 1) & 1);
             unsigned char *st = sm + s * C::STAGE;
             const bool copied = by_copy(a, nv, t0);
+            if (copied && ft) continue;                      // (one thread's work)
+            if (i >= C::STAGES) WAIT(&ws.empty[s], (i / C::STAGES - 1) & 1);
             if (ft == 0) {
                 const long long at = bh * a.chunks + c;
                 mbar_expect_tx(&ws.full[s], C::IMAGES + kWalkGates + (copied ? (phi ? 2 : 3) * C::TENSOR : 0));
@@ -92,9 +93,10 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
                 load_tile<T>(st, C::TILE, (const T *)a.k, qk + t0, all, a.L, a.Dk, nv, ft, kFetchers);
                 load_tile<T>(st + C::Q, C::TILE, (const T *)a.q, qk + t0, all, a.L, a.Dk, nv, ft, kFetchers);
                 if (!phi) load_tile<T>(st + C::DY, C::TILE, (const T *)a.dy, vhead + t0, vall, a.L, a.Dv, nv, ft, kFetchers);
+                fence_async_smem();
+                fetchers_sync();
             }
-            fence_async_smem();
-            mbar_arrive(&ws.full[s]);
+            if (ft == 0) mbar_arrive(&ws.full[s]);
         }
     } else if (warp == 8) {
         // ---- the products
@@ -370,7 +372,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
         tmem_fence_after_sync();
     };
     for (int j = 0; j < share; ++j) {
-        const long long bh = (long long)b * a.H + hk * share + j, at = bh * a.chunks + chunk, grow = bh * a.L + t0, vrow = (bh * a.Dv + row) * a.L + t;
+        const long long bh = (long long)b * a.H + hk * share + j, at = bh * a.chunks + chunk, grow = bh * a.L + t0;
         const float *S = a.marks + at * kept, *D = a.dstates + at * kept;
         if (j) {                                             // the images and sums of the head before have been read
             fence_async_smem();
@@ -442,7 +444,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
         }
         go();
         if (warp == 0) {
-            issue_ts<PM, PI, PM, true, KD / 16, B_ALL, 1>(tb + C::R0, tb + C::S0, KD / 2, IK, C::TILE, ksteps, kTok, false);
+            issue_ts<PM, PI, PM, true, KD / 16, B_ALL, 4>(tb + C::R0, tb + C::S0, KD / 2, IK, C::TILE, ksteps, kTok, false);
             umma_commit(&ws.bar_a);
         }
         done();
@@ -468,7 +470,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
         }
         go();
         if (warp == 0) {
-            issue_ts<PM, PM, PM, false, kTok / 16, B_LOWER, 1>(tb + C::R0, tb + C::R0 + kTok, kTok / 2, IA, kMatrix, kTok / 16, kTok, false);
+            issue_ts<PM, PM, PM, false, kTok / 16, B_LOWER>(tb + C::R0, tb + C::R0 + kTok, kTok / 2, IA, kMatrix, kTok / 16, kTok, false);
             umma_commit(&ws.bar_a);
         }
         // a state with its columns as lanes; `with`: the sum of its products with the one that is there
@@ -526,13 +528,13 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
             }
             __syncwarp();
             // rows 0 .. 63: dY U^T, rows 64 ..: dZ U^T; where dY is one plane, dZ's second goes into a sum of its own
-            issue_ss<PI, PM, PM, true, true, KD / 16, B_ALL, 1>(tb + C::R0 + kTok, IY, C::TILE, C::DZ - C::DY, IU, C::TILE, vsteps, kTok, false);
-            if (PI < PM) issue_ss<1, 1, 1, true, true, KD / 16, B_ALL, 1>(tb + C::R0 + 5 * kTok, IY + C::TILE, C::TILE, C::DZ - C::DY, IU, C::TILE, vsteps, kTok, false);
+            issue_ss<PI, PM, PM, true, true, KD / 16, B_ALL, 4>(tb + C::R0 + kTok, IY, C::TILE, C::DZ - C::DY, IU, C::TILE, vsteps, kTok, false);
+            if (PI < PM) issue_ss<1, 1, 1, true, true, KD / 16, B_ALL, 4>(tb + C::R0 + 5 * kTok, IY + C::TILE, C::TILE, C::DZ - C::DY, IU, C::TILE, vsteps, kTok, false);
             // rows 64 ..: K K^T
-            issue_ss<PI, PI, PI, true, true, KD / 16, B_ALL, 1>(tb + C::R0 + 2 * kTok, IY, C::TILE, C::K - C::DY, IK, C::TILE, ksteps, kTok, false);
+            issue_ss<PI, PI, PI, true, true, KD / 16, B_ALL, 4>(tb + C::R0 + 2 * kTok, IY, C::TILE, C::K - C::DY, IK, C::TILE, ksteps, kTok, false);
             umma_commit(&ws.bar_a);
-            issue_ts<PM, PI, PM, true, KD / 16, B_ALL, 1>(tb + C::R0, tb + C::S0, KD / 2, IY, C::TILE, vsteps, kTok, false);
-            issue_ts<PM, PM, PM, true, KD / 16, B_ALL, 1>(tb + C::R0 + 3 * kTok, tb + C::S0, KD / 2, IZ, C::TILE, vsteps, kTok, false);
+            issue_ts<PM, PI, PM, true, KD / 16, B_ALL, 4>(tb + C::R0, tb + C::S0, KD / 2, IY, C::TILE, vsteps, kTok, false);
+            issue_ts<PM, PM, PM, true, KD / 16, B_ALL, 4>(tb + C::R0 + 3 * kTok, tb + C::S0, KD / 2, IZ, C::TILE, vsteps, kTok, false);
             umma_commit(&ws.bar_b);
         }
         done();
@@ -567,8 +569,8 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
         WAIT(&ws.bar_b, j & 1);
         go();
         if (warp == 0) {
-            issue_ss<PI, PM, PM, false, false, kTok / 16, B_LOWER, 1>(tb + C::R0 + kTok, IK, C::TILE, 0, IA, kMatrix, kTok / 16, kTok, false);         // F k
-            issue_ss<PI, PM, PM, false, false, kTok / 16, B_LOWER, 1>(tb + C::R0 + 2 * kTok, IK, C::TILE, 0, IZ, kMatrix, kTok / 16, kTok, false);     // E k
+            issue_ss<PI, PM, PM, false, false, kTok / 16, B_LOWER>(tb + C::R0 + kTok, IK, C::TILE, 0, IA, kMatrix, kTok / 16, kTok, false);         // F k
+            issue_ss<PI, PM, PM, false, false, kTok / 16, B_LOWER>(tb + C::R0 + 2 * kTok, IK, C::TILE, 0, IZ, kMatrix, kTok / 16, kTok, false);     // E k
             umma_commit(&ws.bar_a);
         }
         if (C::ROOM) WAIT(&ws.full[1], j & 1);
@@ -594,9 +596,9 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
         }
         go();
         if (warp == 0) {
-            issue_ss<PI, PM, PM, false, true, kTok / 16, B_LOWER_T, 1>(tb + C::R0 + 3 * kTok, IQ, C::TILE, 0, IA, kMatrix, kTok / 16, kTok, false);        // F q
-            issue_ss<PI, PM, PM, false, true, kTok / 16, B_LOWER_T, 1>(tb + C::R0 + 3 * kTok, IK, C::TILE, 0, IZ, kMatrix, kTok / 16, kTok, true);         // E k, the other way
-            issue_ts<PM, PM, PM, true, KD / 16, B_ALL, 1>(tb + C::R0 + 4 * kTok, tb + C::S0, KD / 2, IU, C::TILE, vsteps, kTok, false);                   // dS1 u
+            issue_ss<PI, PM, PM, false, true, kTok / 16, B_LOWER_T>(tb + C::R0 + 3 * kTok, IQ, C::TILE, 0, IA, kMatrix, kTok / 16, kTok, false);        // F q
+            issue_ss<PI, PM, PM, false, true, kTok / 16, B_LOWER_T>(tb + C::R0 + 3 * kTok, IK, C::TILE, 0, IZ, kMatrix, kTok / 16, kTok, true);         // E k, the other way
+            issue_ts<PM, PM, PM, true, KD / 16, B_ALL, 4>(tb + C::R0 + 4 * kTok, tb + C::S0, KD / 2, IU, C::TILE, vsteps, kTok, false);                   // dS1 u
             umma_commit(&ws.bar_a);
         }
         done();

@@ -10,18 +10,14 @@ namespace hn {
 
 __device__ __forceinline__ unsigned image_at(int row, int chunk) { return (unsigned)(row * 128 + ((chunk ^ (row & 7)) << 4)); }
 
-constexpr unsigned long long kUmmaBase = (1ull << 46) | (2ull << 61) | ((unsigned long long)(1024 >> 4) << 32);
-// rows of the image = rows of the operand, from row r0 (a multiple of 8); contraction steps 16 ks .. 16 ks + 15
-__device__ __forceinline__ unsigned long long umma_rows(unsigned image, int ks, int r0 = 0)
-{
-    return kUmmaBase | (1ull << 16) | (((image + (unsigned)(r0 * 128 + ks * 32)) & 0x3ffffu) >> 4);
-}
-// rows of the image = steps of the contraction, 16 ks .. 16 ks + 15; beyond 64 rows of the operand the next ones come from the image
-// `next` bytes behind
-__device__ __forceinline__ unsigned long long umma_cols(unsigned image, int ks, unsigned next = 1024)
-{
-    return kUmmaBase | ((unsigned long long)(next >> 4) << 16) | (((image + (unsigned)(ks * 2048)) & 0x3ffffu) >> 4);
-}
+// The low half of a descriptor (address, and for columns the distance to the next 64 rows of the operand); the high half is the same for
+// all: 1024 bytes from eight rows of an image to the next, 128-byte swizzle.
+// Rows of the image = rows of the operand, from row r0 (a multiple of 8); a 16-step of the contraction further on: kRowStep more
+constexpr unsigned kUmmaHigh = (1024u >> 4) | (1u << 14) | (2u << 29), kRowStep = 32 >> 4, kColStep = 2048 >> 4;
+__device__ __forceinline__ unsigned umma_rows(unsigned image, int r0 = 0) { return (1u << 16) | (((image + (unsigned)(r0 * 128)) & 0x3ffffu) >> 4); }
+// rows of the image = steps of the contraction; beyond 64 rows of the operand the next ones come from the image `next` bytes behind; a 16-step
+// further on: kColStep more
+__device__ __forceinline__ unsigned umma_cols(unsigned image, unsigned next = 1024) { return ((next >> 4) << 16) | ((image & 0x3ffffu) >> 4); }
 // bf16 operands, fp32 accumulator of 128 rows and n columns; a_cols / b_cols: the operand is an image taken by its columns
 __device__ __forceinline__ constexpr unsigned umma_kind(int n, bool a_cols, bool b_cols)
 {
@@ -30,16 +26,18 @@ __device__ __forceinline__ constexpr unsigned umma_kind(int n, bool a_cols, bool
 // The instructions are issued by one lane of a warp that comes here as a whole, in code that the compiler knows to be uniform: operands then
 // stay in uniform registers and an instruction costs what the product takes (34 cycles for 64 columns, 13 for 16); from a branch of
 // one thread each of them took 48 to 100.
-__device__ __forceinline__ void umma_ss(unsigned d, unsigned long long a, unsigned long long b, unsigned kind, bool add)
+__device__ __forceinline__ void umma_ss(unsigned d, unsigned a, unsigned b, unsigned kind, bool add)
 {
-    asm volatile("{\n .reg .pred p, one;\n elect.sync _|one, 0xffffffff;\n setp.ne.b32 p, %4, 0;\n @one tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n"
-                 ::"r"(d), "l"(a), "l"(b), "r"(kind), "r"((unsigned)add) : "memory");
+    asm volatile("{\n .reg .pred p, one;\n .reg .b64 a, b;\n mov.b64 a, {%1, %5};\n mov.b64 b, {%2, %5};\n elect.sync _|one, 0xffffffff;\n setp.ne.b32 p, %4, 0;\n"
+                 " @one tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n}\n"
+                 ::"r"(d), "r"(a), "r"(b), "r"(kind), "r"((unsigned)add), "r"(kUmmaHigh) : "memory");
 }
 // the A operand in tensor memory: row = lane, two values of the contraction to a column, 8 columns at `a`
-__device__ __forceinline__ void umma_ts(unsigned d, unsigned a, unsigned long long b, unsigned kind, bool add)
+__device__ __forceinline__ void umma_ts(unsigned d, unsigned a, unsigned b, unsigned kind, bool add)
 {
-    asm volatile("{\n .reg .pred p, one;\n elect.sync _|one, 0xffffffff;\n setp.ne.b32 p, %4, 0;\n @one tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n"
-                 ::"r"(d), "r"(a), "l"(b), "r"(kind), "r"((unsigned)add) : "memory");
+    asm volatile("{\n .reg .pred p, one;\n .reg .b64 b;\n mov.b64 b, {%2, %5};\n elect.sync _|one, 0xffffffff;\n setp.ne.b32 p, %4, 0;\n"
+                 " @one tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n}\n"
+                 ::"r"(d), "r"(a), "r"(b), "r"(kind), "r"((unsigned)add), "r"(kUmmaHigh) : "memory");
 }
 // everything this warp has issued so far arrives on bar when it is through (elect.sync names the same lane every time)
 __device__ __forceinline__ void umma_commit(uint64_t *bar)
