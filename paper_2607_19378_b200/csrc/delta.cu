@@ -108,9 +108,10 @@ template <typename T, int KD> __global__ void __launch_bounds__(128) delta_prepa
     }
     if (tid < kTok) {                                        // (the decays meanwhile)
         float *gates = a.gates + at * kGates;
-        const float x[5] = {ratio(hi[tid], lo[tid], 0.f, 0.f), ratio(hi[kTok - 1], lo[kTok - 1], hi[tid], lo[tid]), beta[tid], hi[tid], lo[tid]};
+        const float gamma = ratio(hi[tid], lo[tid], 0.f, 0.f);
+        const float x[6] = {gamma, ratio(hi[kTok - 1], lo[kTok - 1], hi[tid], lo[tid]), beta[tid], -beta[tid] * gamma, hi[tid], lo[tid]};
 #pragma unroll
-        for (int e = 0; e < 5; ++e) { HN_G(gates + e * kTok + tid, 4); gates[e * kTok + tid] = x[e]; }
+        for (int e = 0; e < 6; ++e) { HN_G(gates + e * kTok + tid, 4); gates[e * kTok + tid] = x[e]; }
     }
     ok = mbar_wait(&bar, 0) && ok;
     if (!ok) atomicExch(&hn_delta_status, 1);
@@ -206,12 +207,12 @@ template <typename T, int KD> struct Walk {
     static constexpr int OUT = VALUES ? 2 * TILE : 0;                         // two images of results
     static constexpr int STAGES = 3 * STAGE + OUT <= 220 * 1024 ? 3 : 2 * STAGE + OUT <= 220 * 1024 ? 2 : 1;
     static constexpr int BYTES = 1024 + STAGES * STAGE + OUT;
-    // tensor memory: S (later delta U) as an operand | Z, later U, as an operand | S k and S q, then U in the first's place | what S gains
+    // tensor memory: S as an operand | Z, later U, as an operand | S k, then U | S q, then y | what S gains | delta U as an operand
     static constexpr int SCOLS = PM * KD / 2, ZCOLS = PM * kTok / 2, S0 = 0, Z0 = SCOLS, X0 = Z0 + ZCOLS, Y0 = X0 + kTok;
-    // (with three planes of 128 columns its first half goes where U was)
-    static constexpr bool ROOM = Y0 + kTok + KD <= 512;
-    static constexpr int D0 = ROOM ? Y0 + kTok : X0, D1 = ROOM ? D0 + KD / 2 : Y0 + kTok;
-    static_assert(D1 + KD / 2 <= 512 && (ROOM || KD / 2 == kTok), "tensor memory");
+    // (with three planes of 128 columns delta U takes S's place, and the first half of the gain U's)
+    static constexpr bool ROOM = Y0 + kTok + KD + ZCOLS <= 512;
+    static constexpr int D0 = ROOM ? Y0 + kTok : X0, D1 = ROOM ? D0 + KD / 2 : Y0 + kTok, U0 = ROOM ? D0 + KD : S0;
+    static_assert(ROOM || (D1 + KD / 2 <= 512 && KD / 2 == kTok), "tensor memory");
 };
 
 template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkThreads, 1) delta_walk_kernel(DeltaArgs a, const __grid_constant__ DeltaMaps maps)
@@ -233,12 +234,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
     int last = (n + kTok - 1) / kTok;                        // chunks first .. last - 1 hold tokens
     last = last < end ? last : end;
     if (warp == 0) tmem_alloc(smem_u32(&ws.slot), 512);
-    if (tid == 0) {
-        for (int s = 0; s < C::STAGES; ++s) { mbar_init(&ws.full[s], 2); mbar_init(&ws.empty[s], 1); }
-        mbar_init(&ws.bar_a, 1); mbar_init(&ws.bar_b, 1); mbar_init(&ws.bar_c, 1); mbar_init(&ws.bar_y, 1); mbar_init(&ws.ready, 8);
-        ws.gave_up = 0;
-        fence_mbar_init();
-    }
+    if (tid == 0) walk_init(&ws, C::STAGES);
     for (int s = 0; s < C::STAGES; ++s) {
         clear_rows(sm + s * C::STAGE, C::TILE, 2 * PI, a.Dk, KD, tid, kWalkThreads);
         if (C::VALUES) clear_rows(sm + s * C::STAGE + C::V, C::TILE, 1, phi ? 0 : a.Dv, KD, tid, kWalkThreads);
@@ -284,28 +280,38 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
     } else if (warp == 8) {
         // ---- the products
         const int steps = (a.Dk + 15) / 16;
-        unsigned par = 0;
         for (int c = first, i = 0; c < last; ++c, ++i) {
             const int s = i % C::STAGES;
-            const unsigned k = smem_u32(sm) + s * C::STAGE, A = k + C::A, P = A + PM * kMatrix;
+            const unsigned par = i & 1, k = smem_u32(sm) + s * C::STAGE, A = k + C::A, P = A + PM * kMatrix;
             WAIT(&ws.full[s], (i / C::STAGES) & 1);
-            WAIT(&ws.ready, par); par ^= 1;                                     // S is there, and the results of the chunk before are taken
+            // S k, the first half of S's columns as soon as they are there
+            WAIT(&ws.state[0], par);
             tmem_fence_after_sync();
-            issue_ts<PM, PI, PM, true, KD / 16>(tb + C::X0, tb + C::S0, KD / 2, k, C::TILE, steps, RUN ? 2 * kTok : kTok, false, C::Q);
+            issue_ts<PM, PI, PM, true, KD / 32>(tb + C::X0, tb + C::S0, KD / 2, k, C::TILE, steps, kTok, false);
+            WAIT(&ws.state[1], par);
+            tmem_fence_after_sync();
+            if (a.Dk > KD / 2) issue_ts<PM, PI, PM, true, KD / 32>(tb + C::X0, tb + C::S0 + KD / 4, KD / 2, k + KD / 2 * 128, C::TILE, steps - KD / 32, kTok, true);
             umma_commit(&ws.bar_a);
-            WAIT(&ws.ready, par); par ^= 1;                                     // Z
+            if (RUN) {
+                if (i) WAIT(&ws.y_taken, par ^ 1);
+                tmem_fence_after_sync();
+                issue_ts<PM, PI, PM, true, KD / 16>(tb + C::Y0, tb + C::S0, KD / 2, k + C::Q, C::TILE, steps, kTok, false);
+                umma_commit(&ws.bar_q);
+            }
+            WAIT(&ws.z_ready, par);
             tmem_fence_after_sync();
             issue_ts<PM, PM, PM, false, kTok / 16, B_LOWER>(tb + C::X0, tb + C::Z0, kTok / 2, A, kMatrix, kTok / 16, kTok, false);
             umma_commit(&ws.bar_b);
-            WAIT(&ws.ready, par); par ^= 1;                                     // U, delta U
+            WAIT(&ws.u_ready, par);
             tmem_fence_after_sync();
-            if (C::ROOM) issue_ts<PM, PI, PM, false, kTok / 16>(tb + C::D0, tb + C::S0, kTok / 2, k, C::TILE, kTok / 16, KD, false);
-            else {
-                issue_ts<PM, PI, PM, false, kTok / 16>(tb + C::D0, tb + C::S0, kTok / 2, k, C::TILE, kTok / 16, KD / 2, false);
-                issue_ts<PM, PI, PM, false, kTok / 16>(tb + C::D1, tb + C::S0, kTok / 2, k + KD / 2 * 128, C::TILE, kTok / 16, KD / 2, false);
-            }
-            umma_commit(&ws.bar_c);
+            issue_ts<PM, PI, PM, false, kTok / 16>(tb + C::D0, tb + C::U0, kTok / 2, k, C::TILE, kTok / 16, KD / 2, false);
+            if (C::ROOM) umma_commit(&ws.bar_c[0]);
+            issue_ts<PM, PI, PM, false, kTok / 16>(tb + C::D1, tb + C::U0, kTok / 2, k + KD / 2 * 128, C::TILE, kTok / 16, KD / 2, false);
+            if (!C::ROOM) umma_commit(&ws.bar_c[0]);
+            umma_commit(&ws.bar_c[1]);
             if (RUN) {
+                WAIT(&ws.p_ready, par);
+                tmem_fence_after_sync();
                 issue_ts<PM, PM, PM, false, kTok / 16, B_LOWER>(tb + C::Y0, tb + C::Z0, kTok / 2, P, kMatrix, kTok / 16, kTok, true);
                 umma_commit(&ws.bar_y);
             }
@@ -314,25 +320,28 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
     } else {
         // ---- computing: lane of tensor memory = row of the state, `half` = which half of the columns
         const int row = 32 * (warp & 3) + lane, half = warp >> 2, rows = phi ? a.Dk : a.Dv;
-        const unsigned lane_s = tmem_addr(tb, warp, C::S0 + half * (HC / 2)), lane_z = tmem_addr(tb, warp, C::Z0 + half * 16),
+        const unsigned lane_s = tmem_addr(tb, warp, C::S0 + half * (HC / 2)), lane_z = tmem_addr(tb, warp, C::Z0 + half * 16), lane_u = tmem_addr(tb, warp, C::U0 + half * 16),
                        lane_x = tmem_addr(tb, warp, C::X0 + half * 32), lane_y = tmem_addr(tb, warp, C::Y0 + half * 32), lane_d = tmem_addr(tb, warp, half ? C::D1 : C::D0);
         const long long vrow = vhead + (long long)row * a.L;
         const bool real = row < a.Dv, stored = C::VALUES && a.copies;
         unsigned char *out = sm + C::STAGES * C::STAGE;
-        float S[HC], x[32], y[32];
+        f2 S[HC / 2], x[16], y[16];
+        {
+            float s[HC];
 #pragma unroll
-        for (int i = 0; i < HC; ++i) S[i] = 0.f;
-        if (!RUN) {
-            if (phi) {
-#pragma unroll
-                for (int i = 0; i < HC; ++i) S[i] = row == half * HC + i && row < a.Dk ? 1.f : 0.f;
-            }
-        } else {
+            for (int i = 0; i < HC; ++i) s[i] = phi && row == half * HC + i && row < a.Dk ? 1.f : 0.f;
             const float *from = a.segments > 1 ? a.starts + (bh * a.segments + segment) * states : a.s0 ? a.s0 + bh * states : nullptr;
-            if (from) load_state<HC>(S, from, row, a.Dv, half * HC, a.Dk);
+            if (RUN && from) load_state<HC>(s, from, row, a.Dv, half * HC, a.Dk);
+#pragma unroll
+            for (int i = 0; i < HC / 2; ++i) S[i] = make2(s[2 * i], s[2 * i + 1]);
         }
-        // results of chunk c, from y: as an image that a copy takes away, or by their threads
-        auto put_y = [&](int c) {
+        // the results of chunk c: as an image that a copy takes away, or by their threads
+        auto take_y = [&](int c, unsigned par) {
+            WAIT(&ws.bar_y, par);
+            tmem_fence_after_sync();
+            tmem_ld(y, lane_y);
+            tmem_wait_ld();
+            walk_ready(&ws.y_taken, lane);
             const int t = c * kTok + 32 * half;
             if (stored) {
                 unsigned char *image = out + (c & 1) * C::TILE;
@@ -352,101 +361,88 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             const unsigned par = i & 1;
             const unsigned char *st = sm + s * C::STAGE;
             const float *gates = (const float *)(st + C::GATES) + 32 * half;
+            float *mark = a.marks + (bh * a.chunks + c) * kept_floats(a.Dv, a.Dk);
+            const bool keep = RUN && a.marks;                // (in parts, where the threads wait anyhow)
             planes_to_tmem<PM, HC / 2>(lane_s, KD / 2, S);
-            if (RUN && i) {
-                WAIT(&ws.bar_y, par ^ 1);
-                tmem_fence_after_sync();
-                TmemIO<32>::ld(y, lane_y);
-                tmem_wait_ld();
-            }
-            tmem_wait_st();
-            tmem_fence_before_sync();
-            walk_ready(&ws, lane);
-            RowPart<T> v;
-            if constexpr (!C::VALUES) v.load((const T *)a.v, vrow + t, vall, a.L, real && !phi ? n - t : 0);
-            if (RUN && i) put_y(c - 1);
-            if (RUN && a.marks) keep_state<HC>(a.marks + (bh * a.chunks + c) * kept_floats(a.Dv, a.Dk), S, row, a.Dv, half * HC, a.Dk);
+            walk_ready(&ws.state[half], lane);
+            if (RUN && i) take_y(c - 1, par ^ 1);
+            if (keep) keep_state<0, HC / 16>(mark, S, row, a.Dv, half * HC, a.Dk);
+            f2 w[16];                                        // beta v
             WAIT(&ws.full[s], (i / C::STAGES) & 1);
-            float w[32];
-            if constexpr (C::VALUES) {
-                if (row < KD) image_row<1>(w, st + C::V, C::TILE, row, half);
-                else {
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) w[e] = 0.f;
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < 32; ++e) w[e] = v.get(e);
+            for (int e = 0; e < 16; ++e) w[e] = pair(0.f);
+            if (real && !phi) {
+                if constexpr (C::VALUES) image_row<1>(w, st + C::V, C::TILE, row, half);
+                else load_row(w, (const float *)a.v, vrow + t, a.L, n - t);
+                scale(w, gates + 2 * kTok);
             }
             WAIT(&ws.bar_a, par);
             tmem_fence_after_sync();
-            TmemIO<32>::ld(x, lane_x);
+            tmem_ld(x, lane_x);
             tmem_wait_ld();
 #pragma unroll
-            for (int e = 0; e < 32; e += 4) {
-                const float4 ga = *(const float4 *)(gates + e), be = *(const float4 *)(gates + 2 * kTok + e);
-                x[e] = be.x * fmaf(-ga.x, x[e], w[e]);
-                x[e + 1] = be.y * fmaf(-ga.y, x[e + 1], w[e + 1]);
-                x[e + 2] = be.z * fmaf(-ga.z, x[e + 2], w[e + 2]);
-                x[e + 3] = be.w * fmaf(-ga.w, x[e + 3], w[e + 3]);
+            for (int e = 0; e < 16; e += 2) {                // Z = beta v - beta gamma S k
+                const float4 bg = *(const float4 *)(gates + 3 * kTok + 2 * e);
+                x[e] = fma2(make2(bg.x, bg.y), x[e], w[e]);
+                x[e + 1] = fma2(make2(bg.z, bg.w), x[e + 1], w[e + 1]);
             }
             planes_to_tmem<PM, 16>(lane_z, kTok / 2, x);
-            tmem_wait_st();
-            tmem_fence_before_sync();
-            walk_ready(&ws, lane);
+            walk_ready(&ws.z_ready, lane);
             if (RUN) {                                       // y's first sum by gamma, while A Z is formed
-                TmemIO<32>::ld(y, lane_y);
+                WAIT(&ws.bar_q, par);
+                tmem_fence_after_sync();
+                tmem_ld(y, lane_y);
                 tmem_wait_ld();
-#pragma unroll
-                for (int e = 0; e < 32; e += 4) {
-                    const float4 ga = *(const float4 *)(gates + e);
-                    y[e] *= ga.x; y[e + 1] *= ga.y; y[e + 2] *= ga.z; y[e + 3] *= ga.w;
-                }
-                TmemIO<32>::st(lane_y, y);
+                scale(y, gates);
+                tmem_st(lane_y, y);
             }
+            if (keep) keep_state<HC / 16, HC / 8>(mark, S, row, a.Dv, half * HC, a.Dk);
             WAIT(&ws.bar_b, par);
             tmem_fence_after_sync();
-            TmemIO<32>::ld(x, lane_x);
+            tmem_ld(x, lane_x);
             tmem_wait_ld();
-            if (RUN) planes_to_tmem<PM, 16>(lane_z, kTok / 2, x);
 #pragma unroll
-            for (int e = 0; e < 32; e += 4) {
-                const float4 de = *(const float4 *)(gates + kTok + e);
-                x[e] *= de.x; x[e + 1] *= de.y; x[e + 2] *= de.z; x[e + 3] *= de.w;
+            for (int e = 0; e < 16; ++e) y[e] = x[e];
+            scale(x, gates + kTok);
+            planes_to_tmem<PM, 16>(lane_u, kTok / 2, x);
+            const f2 fade = pair(((const float *)(st + C::GATES))[kTok - 1]);
+            walk_ready(&ws.u_ready, lane);
+            if (RUN) {
+                planes_to_tmem<PM, 16>(lane_z, kTok / 2, y);
+                walk_ready(&ws.p_ready, lane);
             }
-            planes_to_tmem<PM, 16>(tmem_addr(tb, warp, C::S0 + half * 16), kTok / 2, x);
-            const float fade = ((const float *)(st + C::GATES))[kTok - 1];
-            tmem_wait_st();
-            tmem_fence_before_sync();
-            walk_ready(&ws, lane);
-            WAIT(&ws.bar_c, par);
+            if (keep) keep_state<HC / 8, HC / 4>(mark, S, row, a.Dv, half * HC, a.Dk);
+            WAIT(&ws.bar_c[half], par);
             tmem_fence_after_sync();
 #pragma unroll
-            for (int e = 0; e < HC; e += 32) {
-                TmemIO<32>::ld(x, lane_d + e);
+            for (int e = 0; e < HC / 2; e += 16) {
+                tmem_ld(x, lane_d + 2 * e);
                 tmem_wait_ld();
 #pragma unroll
-                for (int j = 0; j < 32; ++j) S[e + j] = fmaf(fade, S[e + j], x[j]);
+                for (int j = 0; j < 16; ++j) S[e + j] = fma2(fade, S[e + j], x[j]);
             }
         }
-        if (!RUN) {
-            float *to = a.maps + (bh * a.segments + segment) * (long long)(a.Dv + a.Dk) * a.Dk + (phi ? states : 0);
-            store_state<HC>(to, S, row, rows, half * HC, a.Dk);
-        } else {
-            if (first < last) {
-                WAIT(&ws.bar_y, (last - first - 1) & 1);
-                tmem_fence_after_sync();
-                TmemIO<32>::ld(y, lane_y);
-                tmem_wait_ld();
-                put_y(last - 1);
-            }
+        auto flat = [&](float (&s)[HC]) {
 #pragma unroll
-            for (int e = 0; e < 32; ++e) y[e] = 0.f;
+            for (int i = 0; i < HC / 2; ++i) split2(S[i], s[2 * i], s[2 * i + 1]);
+        };
+        if (!RUN) {
+            float *to = a.maps + (bh * a.segments + segment) * (long long)(a.Dv + a.Dk) * a.Dk + (phi ? states : 0), s[HC];
+            flat(s);
+            store_state<HC>(to, s, row, rows, half * HC, a.Dk);
+        } else {
+            if (first < last) take_y(last - 1, (last - first - 1) & 1);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) y[e] = pair(0.f);
             for (int c = first > last ? first : last; c < end; ++c) {
                 const int t = c * kTok + 32 * half;
                 if (real && t < a.L) store_row<T>((T *)a.y, vrow + t, a.L, a.L - t, 0, y);
             }
-            if (a.s_end && segment == a.segments - 1) store_state<HC>(a.s_end + bh * states, S, row, a.Dv, half * HC, a.Dk);
+            if (a.s_end && segment == a.segments - 1) {
+                float s[HC];
+                flat(s);
+                store_state<HC>(a.s_end + bh * states, s, row, a.Dv, half * HC, a.Dk);
+            }
             if (stored && tid == 0) tma_wait_all0();
         }
         tmem_fence_before_sync();

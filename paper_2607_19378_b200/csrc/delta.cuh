@@ -20,6 +20,8 @@
 // p and q is formed where p + q is below the number of planes.
 #pragma once
 #include "entry.cuh"
+#include "octet.cuh"
+#include "pair.cuh"
 #include "umma.cuh"
 
 namespace hn {
@@ -30,8 +32,8 @@ enum { DELTA_LOG = HYENAND_DECAY_LOG, DELTA_SIGMOID = HYENAND_DECAY_SIGMOID, DEL
 template <typename T> struct Planes { static constexpr int IN = 1, MID = 2; };
 template <> struct Planes<float> { static constexpr int IN = 3, MID = 3; };
 constexpr int kMatrix = kTok * 128;                       // bytes of one plane of a 64 x 64 matrix
-constexpr int kGates = 5 * kTok;                          // floats of a chunk: gamma, delta, beta, and G in two parts (see ratio)
-constexpr int kWalkGates = 3 * kTok * 4;                  // bytes of the first three
+constexpr int kGates = 6 * kTok;                          // floats of a chunk: gamma, delta, beta, -beta gamma, and G in two parts (see ratio)
+constexpr int kWalkGates = 4 * kTok * 4;                  // bytes of the first four
 
 struct DeltaArgs {
     const void *q, *k, *v;
@@ -46,7 +48,7 @@ struct DeltaArgs {
     float *dg, *dbeta, *ds0;
     // workspace
     unsigned char *images;                                // [B H][chunks]: planes of A, planes of P
-    float *gates;                                         // [B H][chunks][5][64]
+    float *gates;                                         // [B H][chunks][6][64]
     float *maps, *starts;                                 // [B H][segments][Dv + Dk][Dk], [B H][segments][Dv][Dk]
     float *dstates, *dz;                                  // [B H][chunks] states as kept, [B H][chunks][Dv][64]
     int B, H, Hk, L, Dk, Dv, decay, chunks, segments, per_segment;
@@ -83,16 +85,16 @@ __device__ __forceinline__ void tmem_st4(unsigned at, const unsigned (&v)[4])
 
 // a pair of numbers as PM planes of bf16 pairs, each the rest of the ones before, rounded to nearest (so that a rest has either sign
 // and what is left out of a product, rest times rest, averages out: cut off instead, states were off by 7e-6, now by 2e-6)
-template <int PM> __device__ __forceinline__ void split_pair(float x, float y, unsigned (&w)[PM])
+template <int PM> __device__ __forceinline__ void split_pair(f2 x, unsigned (&w)[PM])
 {
 #pragma unroll
     for (int p = 0; p < PM; ++p) {
-        const __nv_bfloat162 r = __floats2bfloat162_rn(x, y);
+        const __nv_bfloat162 r = __float22bfloat162_rn(x);
         w[p] = *(const unsigned *)&r;
-        x -= __uint_as_float(w[p] << 16);
-        y -= __uint_as_float(w[p] & 0xffff0000u);
+        if (p + 1 < PM) x = fma2(make2(__uint_as_float(w[p] << 16), __uint_as_float(w[p] & 0xffff0000u)), pair(-1.f), x);
     }
 }
+template <int PM> __device__ __forceinline__ void split_pair(float x, float y, unsigned (&w)[PM]) { split_pair<PM>(make2(x, y), w); }
 
 // 2 C numbers of this thread's row as the A operand in tensor memory: C columns per plane, planes `pitch` columns apart
 template <int PM, int C> __device__ __forceinline__ void planes_to_tmem(unsigned at, int pitch, const float (&x)[2 * C])
@@ -107,6 +109,44 @@ template <int PM, int C> __device__ __forceinline__ void planes_to_tmem(unsigned
     }
 #pragma unroll
     for (int p = 0; p < PM; ++p) TmemIO<C>::st(at + p * pitch, w[p]);
+}
+template <int PM, int C> __device__ __forceinline__ void planes_to_tmem(unsigned at, int pitch, const f2 (&x)[C])
+{
+    float w[PM][C];
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+        unsigned u[PM];
+        split_pair<PM>(x[i], u);
+#pragma unroll
+        for (int p = 0; p < PM; ++p) w[p][i] = __uint_as_float(u[p]);
+    }
+#pragma unroll
+    for (int p = 0; p < PM; ++p) TmemIO<C>::st(at + p * pitch, w[p]);
+}
+// 32 columns of this thread's lane, in pairs
+__device__ __forceinline__ void tmem_ld(f2 (&v)[16], unsigned at)
+{
+    float x[32];
+    TmemIO<32>::ld(x, at);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = make2(x[2 * i], x[2 * i + 1]);
+}
+__device__ __forceinline__ void tmem_st(unsigned at, const f2 (&v)[16])
+{
+    float x[32];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) split2(v[i], x[2 * i], x[2 * i + 1]);
+    TmemIO<32>::st(at, x);
+}
+// v[i] *= by[i], 32 numbers of shared memory
+__device__ __forceinline__ void scale(f2 (&v)[16], const float *by)
+{
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+        const float4 w = *(const float4 *)(by + 2 * i);
+        v[i] = mul2(v[i], make2(w.x, w.y));
+        v[i + 1] = mul2(v[i + 1], make2(w.z, w.w));
+    }
 }
 // 32 numbers, tokens 32 half .. of row `row` of an image
 template <int PM> __device__ __forceinline__ void planes_to_image(unsigned char *image, int pitch, int row, int half, const float (&x)[32])
@@ -164,22 +204,20 @@ template <int PI> __device__ __forceinline__ void image8(float (&x)[8], const un
     }
 }
 // the numbers of a row of an image of a tensor: its planes' sum
-template <int PI> __device__ __forceinline__ void image_row(float (&x)[32], const unsigned char *image, int pitch, int row, int half)
+template <int PI> __device__ __forceinline__ void image_row(f2 (&x)[16], const unsigned char *image, int pitch, int row, int half)
 {
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
+    for (int c = 0; c < 4; ++c)
 #pragma unroll
         for (int p = PI - 1; p >= 0; --p) {
             const uint4 w = *(const uint4 *)(image + p * pitch + image_at(row, half * 4 + c));
             const unsigned u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float lo = __uint_as_float(u[i] << 16), hi = __uint_as_float(u[i] & 0xffff0000u);
-                if (p == PI - 1) { x[8 * c + 2 * i] = lo; x[8 * c + 2 * i + 1] = hi; }
-                else { x[8 * c + 2 * i] += lo; x[8 * c + 2 * i + 1] += hi; }
+                const f2 v = make2(__uint_as_float(u[i] << 16), __uint_as_float(u[i] & 0xffff0000u));
+                x[4 * c + i] = p == PI - 1 ? v : add2(x[4 * c + i], v);
             }
         }
-    }
 }
 
 // ---- tensors in device memory ---------------------------------------------------------------------------------------
@@ -283,46 +321,23 @@ __device__ __forceinline__ void clear_rows(unsigned char *image, int pitch, int 
         for (int i = from * 8 + tid; i < to * 8; i += threads) *(uint4 *)(image + p * pitch + i * 16) = make_uint4(0, 0, 0, 0);
 }
 
-// 32 tokens of one row in registers, as they lie; zero behind the first nv
-template <typename T> struct RowPart;
-template <> struct RowPart<bf16> {
-    uint4 w[4];
-    __device__ __forceinline__ void load(const bf16 *p, long long at, long long n, int L, int nv)
-    {
+// 32 tokens of one row of fp32 values; zero behind the first nv
+__device__ __forceinline__ void load_row(f2 (&x)[16], const float *p, long long at, int L, int nv)
+{
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            w[c] = make_uint4(0, 0, 0, 0);
-            const int left = nv - 8 * c;
-            if (left <= 0) continue;
-            if (L % 8 == 0) { HN_G(p + at + 8 * c, 16); w[c] = __ldg((const uint4 *)(p + at + 8 * c)); }
-            else w[c] = load_unaligned(p, at + 8 * c, n);
-            if (left < 8) w[c] = keep_first(w[c], left);
+    for (int c = 0; c < 8; ++c) {
+        if (L % 4 == 0 && nv >= 4 * c + 4) {
+            HN_G(p + at + 4 * c, 16);
+            const float4 w = __ldg((const float4 *)(p + at) + c);
+            x[2 * c] = make2(w.x, w.y);
+            x[2 * c + 1] = make2(w.z, w.w);
+        } else {
+#pragma unroll
+            for (int i = 2 * c; i < 2 * c + 2; ++i)
+                x[i] = make2(2 * i < nv ? IO<float>::ld(p, at + 2 * i) : 0.f, 2 * i + 1 < nv ? IO<float>::ld(p, at + 2 * i + 1) : 0.f);
         }
     }
-    __device__ __forceinline__ float get(int i) const
-    {
-        const unsigned u = (i >> 1 & 3) == 0 ? w[i >> 3].x : (i >> 1 & 3) == 1 ? w[i >> 3].y : (i >> 1 & 3) == 2 ? w[i >> 3].z : w[i >> 3].w;
-        return __uint_as_float(i & 1 ? u & 0xffff0000u : u << 16);
-    }
-};
-template <> struct RowPart<float> {
-    float x[32];
-    __device__ __forceinline__ void load(const float *p, long long at, long long, int L, int nv)
-    {
-#pragma unroll
-        for (int c = 0; c < 8; ++c) {
-            if (L % 4 == 0 && nv >= 4 * c + 4) {
-                HN_G(p + at + 4 * c, 16);
-                const float4 w = __ldg((const float4 *)(p + at) + c);
-                x[4 * c] = w.x; x[4 * c + 1] = w.y; x[4 * c + 2] = w.z; x[4 * c + 3] = w.w;
-            } else {
-#pragma unroll
-                for (int i = 4 * c; i < 4 * c + 4; ++i) x[i] = i < nv ? IO<float>::ld(p, at + i) : 0.f;
-            }
-        }
-    }
-    __device__ __forceinline__ float get(int i) const { return x[i]; }
-};
+}
 // eight tokens of one row from element `at`, zero from the nv-th on; and eight stored, the first `room` of them
 template <typename T> __device__ __forceinline__ void load8(float (&x)[8], const T *p, long long at, long long n, int L, int nv)
 {
@@ -374,7 +389,7 @@ __device__ __forceinline__ uint4 bf16_8(const float (&x)[8], int nv)
     return make_uint4(u[0], u[1], u[2], u[3]);
 }
 // the first `room` of 32 tokens of one row; from token nv on they are zero
-template <typename T> __device__ __forceinline__ void store_row(T *p, long long at, int L, int room, int nv, const float (&x)[32])
+template <typename T> __device__ __forceinline__ void store_row(T *p, long long at, int L, int room, int nv, const f2 (&x)[16])
 {
     constexpr int V = 16 / sizeof(T);
     if (L % V == 0) {
@@ -384,14 +399,14 @@ template <typename T> __device__ __forceinline__ void store_row(T *p, long long 
             uint4 w;
             T *e = (T *)&w;
 #pragma unroll
-            for (int i = 0; i < V; ++i) e[i] = (T)(c * V + i < nv ? x[c * V + i] : 0.f);
+            for (int i = 0; i < V; ++i) e[i] = (T)(c * V + i < nv ? (i & 1 ? x[(c * V + i) / 2].y : x[(c * V + i) / 2].x) : 0.f);
             HN_G(p + at + c * V, 16);
             *(uint4 *)(p + at + c * V) = w;
         }
     } else {
 #pragma unroll
         for (int i = 0; i < 32; ++i)
-            if (i < room) IO<T>::st(p, at + i, i < nv ? x[i] : 0.f);
+            if (i < room) IO<T>::st(p, at + i, i < nv ? (i & 1 ? x[i / 2].y : x[i / 2].x) : 0.f);
     }
 }
 // A state that stays inside the library (marks, the gradient behind a chunk): column quartets [D / 4][rows], the rows of a group of eight
@@ -400,16 +415,17 @@ template <typename T> __device__ __forceinline__ void store_row(T *p, long long 
 __host__ __device__ __forceinline__ int kept_rows(int rows) { return (rows + 7) & ~7; }
 __host__ __device__ __forceinline__ long long kept_floats(int rows, int D) { return (long long)kept_rows(rows) * ((D + 3) & ~3); }
 __device__ __forceinline__ int kept_at(int row, int quartet, int rows8) { return quartet * rows8 + (row ^ (quartet & 7)); }
-template <int C> __device__ __forceinline__ void keep_state(float *p, const float (&s)[C], int row, int rows, int col, int D)
+// (quartets FROM .. TO - 1 of this thread's C columns from `col`)
+template <int FROM, int TO, int C> __device__ __forceinline__ void keep_state(float *p, const f2 (&s)[C], int row, int rows, int col, int D)
 {
     const int rows8 = kept_rows(rows);
     if (row >= rows8) return;
 #pragma unroll
-    for (int i = 0; i < C; i += 4)
+    for (int i = 4 * FROM; i < 4 * TO; i += 4)
         if (col + i < D) {
             float4 *to = (float4 *)p + kept_at(row, (col + i) >> 2, rows8);
             HN_G(to, 16);
-            *to = make_float4(s[i], s[i + 1], s[i + 2], s[i + 3]);
+            *to = make_float4(s[i / 2].x, s[i / 2].y, s[i / 2 + 1].x, s[i / 2 + 1].y);
         }
 }
 // this thread's C columns from `col` of row `row` of a state [rows][D], zero outside it
@@ -445,7 +461,7 @@ template <int C> __device__ __forceinline__ void store_state(float *p, const flo
 }
 
 // 32 tokens of a row as an image of a bf16 tensor's tile, zero from token nv on
-__device__ __forceinline__ void row_to_image(unsigned char *image, int row, int half, int nv, const float (&x)[32])
+__device__ __forceinline__ void row_to_image(unsigned char *image, int row, int half, int nv, const f2 (&x)[16])
 {
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
@@ -453,7 +469,7 @@ __device__ __forceinline__ void row_to_image(unsigned char *image, int row, int 
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int e = 8 * c + 2 * i;
-            const __nv_bfloat162 r = __floats2bfloat162_rn(e < nv ? x[e] : 0.f, e + 1 < nv ? x[e + 1] : 0.f);
+            const __nv_bfloat162 r = __floats2bfloat162_rn(e < nv ? x[e / 2].x : 0.f, e + 1 < nv ? x[e / 2].y : 0.f);
             u[i] = *(const unsigned *)&r;
         }
         *(uint4 *)(image + image_at(row, half * 4 + c)) = make_uint4(u[0], u[1], u[2], u[3]);
@@ -550,7 +566,8 @@ __device__ __forceinline__ int uniform_warp(int warp) { return __shfl_sync(~0u, 
 
 // What the warps of a walk share beside the stages.  A wait that gives up ends all later ones of the CTA.
 struct WalkShared {
-    uint64_t full[4], empty[4], bar_a, bar_b, bar_c, bar_y, ready;
+    uint64_t full[4], empty[4], bar_a, bar_b, bar_c[2], bar_q, bar_y;          // copies; products
+    uint64_t state[2], y_taken, z_ready, u_ready, p_ready;                    // the computing warps (of a half) to the one that issues
     unsigned slot;
     int gave_up;
 };
@@ -563,13 +580,24 @@ __device__ __forceinline__ void walk_wait(WalkShared *w, uint64_t *bar, unsigned
     if (!mbar_wait(bar, parity)) { *f = 1; atomicExch(status, 1); }
 }
 __device__ __forceinline__ void mbar_arrive(uint64_t *bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];\n" ::"r"(smem_u32(bar)) : "memory"); }
-// Warps 0 .. 7 compute, warp 8 issues the products, the others fetch.  What the eight wrote is handed to warp 8 by `ready`; what it gives
-// back they see by the products' barriers.
+// Warps 0 .. 7 compute, warp 8 issues the products, the others fetch.  What the eight wrote into tensor memory is handed to warp 8 by
+// barriers; what it gives back they see by the products' barriers.
 constexpr int kWalkThreads = 384, kFetchers = kWalkThreads - 288;
-__device__ __forceinline__ void walk_ready(WalkShared *w, int lane)
+__device__ __forceinline__ void walk_init(WalkShared *w, int stages)
 {
+    for (int s = 0; s < stages; ++s) { mbar_init(&w->full[s], 2); mbar_init(&w->empty[s], 1); }
+    mbar_init(&w->bar_a, 1); mbar_init(&w->bar_b, 1); mbar_init(&w->bar_c[0], 1); mbar_init(&w->bar_c[1], 1); mbar_init(&w->bar_q, 1); mbar_init(&w->bar_y, 1);
+    mbar_init(&w->state[0], 4); mbar_init(&w->state[1], 4);
+    mbar_init(&w->y_taken, 8); mbar_init(&w->z_ready, 8); mbar_init(&w->u_ready, 8); mbar_init(&w->p_ready, 8);
+    w->gave_up = 0;
+    fence_mbar_init();
+}
+__device__ __forceinline__ void walk_ready(uint64_t *bar, int lane)
+{
+    tmem_wait_st();
+    tmem_fence_before_sync();
     __syncwarp();
-    if (lane == 0) mbar_arrive(&w->ready);
+    if (lane == 0) mbar_arrive(bar);
 }
 __device__ __forceinline__ void fetchers_sync() { asm volatile("bar.sync 3, %0;\n" ::"n"(kFetchers) : "memory"); }
 __device__ __forceinline__ void walkers_sync() { asm volatile("bar.sync 2, 256;\n" ::: "memory"); }

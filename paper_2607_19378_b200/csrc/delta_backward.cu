@@ -24,12 +24,12 @@ template <typename T, int KD> struct WalkBack {
     // (the product of dY and P takes 128 rows of dY's image: with 64 it reads on into the images that follow, for rows nothing looks at)
     static constexpr int STAGES = 3 * STAGE + OUT <= 220 * 1024 ? 3 : 2 * STAGE + OUT <= 220 * 1024 ? 2 : 1;
     static constexpr int BYTES = 1024 + STAGES * STAGE + OUT;
-    // tensor memory: dS, later gamma dY, as operands | dU, later -gamma beta dZ | dS k, then dZ | P^T dY | what dS gains
+    // tensor memory: dS as an operand | dU, later -beta gamma dZ, as an operand | dS k, then dZ | P^T dY | what dS gains | gamma dY as an operand
     static constexpr int SCOLS = PM * KD / 2, ZCOLS = PM * kTok / 2, S0 = 0, Z0 = SCOLS, X0 = Z0 + ZCOLS, Y0 = X0 + kTok;
-    // (with three planes of 128 columns its first half goes where dZ was)
-    static constexpr bool ROOM = Y0 + kTok + KD <= 512;
-    static constexpr int D0 = ROOM ? Y0 + kTok : X0, D1 = ROOM ? D0 + KD / 2 : Y0 + kTok;
-    static_assert(D1 + KD / 2 <= 512 && (ROOM || KD / 2 == kTok) && BYTES + 1024 <= 227 * 1024, "tensor and shared memory");
+    // (with three planes of 128 columns gamma dY takes dS's place, and the first half of the gain dZ's)
+    static constexpr bool ROOM = Y0 + kTok + KD + ZCOLS <= 512;
+    static constexpr int D0 = ROOM ? Y0 + kTok : X0, D1 = ROOM ? D0 + KD / 2 : Y0 + kTok, G0 = ROOM ? D0 + KD : S0;
+    static_assert((ROOM || (D1 + KD / 2 <= 512 && KD / 2 == kTok)) && BYTES + 1024 <= 227 * 1024, "tensor and shared memory");
 };
 
 template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkThreads, 1) delta_walk_back_kernel(DeltaArgs a, const __grid_constant__ DeltaMaps maps)
@@ -52,12 +52,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
     last = last < end ? last : end;
     const int count = last > first ? last - first : 0;
     if (warp == 0) tmem_alloc(smem_u32(&ws.slot), 512);
-    if (tid == 0) {
-        for (int s = 0; s < C::STAGES; ++s) { mbar_init(&ws.full[s], 2); mbar_init(&ws.empty[s], 1); }
-        mbar_init(&ws.bar_a, 1); mbar_init(&ws.bar_b, 1); mbar_init(&ws.bar_c, 1); mbar_init(&ws.ready, 8);
-        ws.gave_up = 0;
-        fence_mbar_init();
-    }
+    if (tid == 0) walk_init(&ws, C::STAGES);
     for (int s = 0; s < C::STAGES; ++s) {
         clear_rows(sm + s * C::STAGE, C::TILE, 2 * PI, a.Dk, KD, tid, kWalkThreads);
         clear_rows(sm + s * C::STAGE + C::DY, C::TILE, PI, phi ? 0 : a.Dv, KD, tid, kWalkThreads);
@@ -101,135 +96,124 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
     } else if (warp == 8) {
         // ---- the products
         const int steps = (a.Dk + 15) / 16;
-        unsigned par = 0;
         for (int i = 0; i < count; ++i) {
             const int s = i % C::STAGES;
-            const unsigned k = smem_u32(sm) + s * C::STAGE, q = k + C::Q, A = k + C::A, P = A + PM * kMatrix;
-            // what dS gains from columns 0 .. of an operand in tensor memory and an image of Dk rows
-            auto gain = [&](unsigned from, unsigned image, bool add) {
-                if (C::ROOM) issue_ts<PM, PI, PM, false, kTok / 16>(tb + C::D0, from, kTok / 2, image, C::TILE, kTok / 16, KD, add);
-                else {
-                    issue_ts<PM, PI, PM, false, kTok / 16>(tb + C::D0, from, kTok / 2, image, C::TILE, kTok / 16, KD / 2, add);
-                    issue_ts<PM, PI, PM, false, kTok / 16>(tb + C::D1, from, kTok / 2, image + KD / 2 * 128, C::TILE, kTok / 16, KD / 2, add);
-                }
+            const unsigned par = i & 1, k = smem_u32(sm) + s * C::STAGE, q = k + C::Q, A = k + C::A, P = A + PM * kMatrix;
+            // what half h of dS's columns gains from an operand in tensor memory and an image of Dk rows
+            auto gain = [&](int h, unsigned from, unsigned image, bool add) {
+                issue_ts<PM, PI, PM, false, kTok / 16>(tb + (h ? C::D1 : C::D0), from, kTok / 2, image + h * (KD / 2) * 128, C::TILE, kTok / 16, KD / 2, add);
             };
             WAIT(&ws.full[s], (i / C::STAGES) & 1);
-            WAIT(&ws.ready, par); par ^= 1;                  // dS
-            tmem_fence_after_sync();
-            issue_ts<PM, PI, PM, true, KD / 16>(tb + C::X0, tb + C::S0, KD / 2, k, C::TILE, steps, kTok, false);
+            // (P^T dY of the chunk before has been read: its dU was there)
             issue_ss<PI, PM, PM, false, true, kTok / 16, B_LOWER_T>(tb + C::Y0, k + C::DY, C::TILE, 0, P, kMatrix, kTok / 16, kTok, false);
+            // dS k, the first half of dS's columns as soon as they are there
+            WAIT(&ws.state[0], par);
+            tmem_fence_after_sync();
+            issue_ts<PM, PI, PM, true, KD / 32>(tb + C::X0, tb + C::S0, KD / 2, k, C::TILE, steps, kTok, false);
+            WAIT(&ws.state[1], par);
+            tmem_fence_after_sync();
+            if (a.Dk > KD / 2) issue_ts<PM, PI, PM, true, KD / 32>(tb + C::X0, tb + C::S0 + KD / 4, KD / 2, k + KD / 2 * 128, C::TILE, steps - KD / 32, kTok, true);
             umma_commit(&ws.bar_a);
-            WAIT(&ws.ready, par); par ^= 1;                  // dU
+            if (C::ROOM) {                                   // gamma dY waits for nothing
+                WAIT(&ws.p_ready, par);
+                tmem_fence_after_sync();
+                gain(0, tb + C::G0, q, false);
+                gain(1, tb + C::G0, q, false);
+            }
+            WAIT(&ws.z_ready, par);                          // dU
             tmem_fence_after_sync();
             issue_ts<PM, PM, PM, true, kTok / 16, B_LOWER_T>(tb + C::X0, tb + C::Z0, kTok / 2, A, kMatrix, kTok / 16, kTok, false);
             umma_commit(&ws.bar_b);
-            if (C::ROOM) {
-                WAIT(&ws.ready, par); par ^= 1;              // gamma dY
-                tmem_fence_after_sync();
-                gain(tb + C::S0, q, false);
-            }
-            WAIT(&ws.ready, par); par ^= 1;                  // -gamma beta dZ
+            WAIT(&ws.u_ready, par);                          // -beta gamma dZ (without the room, gamma dY too)
             tmem_fence_after_sync();
-            if (!C::ROOM) gain(tb + C::S0, q, false);
-            gain(tb + C::Z0, k, true);
-            umma_commit(&ws.bar_c);
+            if (!C::ROOM) {
+                gain(0, tb + C::G0, q, false);
+                gain(1, tb + C::G0, q, false);
+            }
+            gain(0, tb + C::Z0, k, true);
+            if (C::ROOM) umma_commit(&ws.bar_c[0]);
+            gain(1, tb + C::Z0, k, true);
+            if (!C::ROOM) umma_commit(&ws.bar_c[0]);
+            umma_commit(&ws.bar_c[1]);
             umma_commit(&ws.empty[s]);
         }
     } else {
         // ---- computing
         const int row = 32 * (warp & 3) + lane, half = warp >> 2, rows = phi ? a.Dk : a.Dv, rows8 = kept_rows(a.Dv);
-        const unsigned lane_s = tmem_addr(tb, warp, C::S0 + half * (HC / 2)), lane_g = tmem_addr(tb, warp, C::S0 + half * 16),
+        const unsigned lane_s = tmem_addr(tb, warp, C::S0 + half * (HC / 2)), lane_g = tmem_addr(tb, warp, C::G0 + half * 16),
                        lane_z = tmem_addr(tb, warp, C::Z0 + half * 16), lane_x = tmem_addr(tb, warp, C::X0 + half * 32), lane_y = tmem_addr(tb, warp, C::Y0 + half * 32),
                        lane_d = tmem_addr(tb, warp, half ? C::D1 : C::D0);
         const long long vrow = vhead + (long long)row * a.L;
         const bool real = row < a.Dv, stored = C::VALUES && a.copies;
         unsigned char *out = sm + C::STAGES * C::STAGE;
-        float S[HC], x[32];
+        f2 S[HC / 2], x[16], y[16];
+        {
+            float s[HC];
 #pragma unroll
-        for (int i = 0; i < HC; ++i) S[i] = 0.f;
-        if (!RUN) {
-            if (phi) {
-#pragma unroll
-                for (int i = 0; i < HC; ++i) S[i] = row == half * HC + i && row < a.Dk ? 1.f : 0.f;
-            }
-        } else {
+            for (int i = 0; i < HC; ++i) s[i] = phi && row == half * HC + i && row < a.Dk ? 1.f : 0.f;
             const float *from = a.segments > 1 ? a.starts + (bh * a.segments + segment) * states : a.ds_end ? a.ds_end + bh * states : nullptr;
-            if (from) load_state<HC>(S, from, row, a.Dv, half * HC, a.Dk);
+            if (RUN && from) load_state<HC>(s, from, row, a.Dv, half * HC, a.Dk);
+#pragma unroll
+            for (int i = 0; i < HC / 2; ++i) S[i] = make2(s[2 * i], s[2 * i + 1]);
         }
         for (int i = 0; i < count; ++i) {
             const int c = last - 1 - i, s = i % C::STAGES, t = c * kTok + 32 * half;
             const unsigned par = i & 1;
             const unsigned char *st = sm + s * C::STAGE;
             const float *gates = (const float *)(st + C::GATES) + 32 * half;
+            float *kept = a.dstates + (bh * a.chunks + c) * kept_floats(a.Dv, a.Dk);
             planes_to_tmem<PM, HC / 2>(lane_s, KD / 2, S);
-            tmem_wait_st();
-            tmem_fence_before_sync();
-            walk_ready(&ws, lane);
-            if (RUN) keep_state<HC>(a.dstates + (bh * a.chunks + c) * kept_floats(a.Dv, a.Dk), S, row, a.Dv, half * HC, a.Dk);
+            walk_ready(&ws.state[half], lane);
             WAIT(&ws.full[s], (i / C::STAGES) & 1);
+            auto gamma_dy = [&] {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) x[e] = pair(0.f);
+                if (real && !phi) {
+                    image_row<PI>(x, st + C::DY, C::TILE, row, half);
+                    scale(x, gates);
+                }
+                planes_to_tmem<PM, 16>(lane_g, kTok / 2, x);
+            };
+            if (C::ROOM) {
+                gamma_dy();
+                walk_ready(&ws.p_ready, lane);
+            }
+            if (RUN) keep_state<0, HC / 16>(kept, S, row, a.Dv, half * HC, a.Dk);
             WAIT(&ws.bar_a, par);
             tmem_fence_after_sync();
-            {
-                float y[32];
-                TmemIO<32>::ld(x, lane_x);
-                TmemIO<32>::ld(y, lane_y);
-                tmem_wait_ld();
-#pragma unroll
-                for (int e = 0; e < 32; e += 4) {
-                    const float4 de = *(const float4 *)(gates + kTok + e);
-                    const float d[4] = {de.x, de.y, de.z, de.w};
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) x[e + j] = row < rows ? fmaf(d[j], x[e + j], phi ? 0.f : y[e + j]) : 0.f;
-                }
-            }
-            planes_to_tmem<PM, 16>(lane_z, kTok / 2, x);
-            tmem_wait_st();
-            tmem_fence_before_sync();
-            walk_ready(&ws, lane);
-            // gamma dY, in the state's place, while A^T dU is formed
-            if (row < KD) image_row<PI>(x, st + C::DY, C::TILE, row, half);
-            else {
-#pragma unroll
-                for (int e = 0; e < 32; ++e) x[e] = 0.f;
-            }
-#pragma unroll
-            for (int e = 0; e < 32; e += 4) {
-                const float4 ga = *(const float4 *)(gates + e);
-                x[e] *= ga.x; x[e + 1] *= ga.y; x[e + 2] *= ga.z; x[e + 3] *= ga.w;
-            }
-            planes_to_tmem<PM, 16>(lane_g, kTok / 2, x);
-            if (C::ROOM) {
-                tmem_wait_st();
-                tmem_fence_before_sync();
-                walk_ready(&ws, lane);
-            }
-            WAIT(&ws.bar_b, par);
-            tmem_fence_after_sync();
-            float dz[32];
-            TmemIO<32>::ld(dz, lane_x);
+            tmem_ld(x, lane_x);
+            tmem_ld(y, lane_y);
             tmem_wait_ld();
 #pragma unroll
-            for (int e = 0; e < 32; e += 4) {
-                const float4 ga = *(const float4 *)(gates + e), be = *(const float4 *)(gates + 2 * kTok + e);
-                x[e] = -ga.x * (dz[e] * be.x); x[e + 1] = -ga.y * (dz[e + 1] * be.y); x[e + 2] = -ga.z * (dz[e + 2] * be.z); x[e + 3] = -ga.w * (dz[e + 3] * be.w);
+            for (int e = 0; e < 16; e += 2) {                // dU = P^T dY + delta dS k
+                const float4 de = *(const float4 *)(gates + kTok + 2 * e);
+                x[e] = row < rows ? fma2(make2(de.x, de.y), x[e], phi ? pair(0.f) : y[e]) : pair(0.f);
+                x[e + 1] = row < rows ? fma2(make2(de.z, de.w), x[e + 1], phi ? pair(0.f) : y[e + 1]) : pair(0.f);
             }
             planes_to_tmem<PM, 16>(lane_z, kTok / 2, x);
-            const float fade = ((const float *)(st + C::GATES))[kTok - 1];
+            walk_ready(&ws.z_ready, lane);
+            if (!C::ROOM) gamma_dy();
+            if (RUN) keep_state<HC / 16, HC / 8>(kept, S, row, a.Dv, half * HC, a.Dk);
+            WAIT(&ws.bar_b, par);
+            tmem_fence_after_sync();
+            tmem_ld(y, lane_x);
+            tmem_wait_ld();
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[e] = y[e];
+            scale(x, gates + 3 * kTok);
+            planes_to_tmem<PM, 16>(lane_z, kTok / 2, x);
+            const f2 fade = pair(((const float *)(st + C::GATES))[kTok - 1]);
             if (RUN) {
 #pragma unroll
-                for (int e = 0; e < 32; e += 4) {
-                    const float4 be = *(const float4 *)(gates + 2 * kTok + e);
-                    x[e] = dz[e] * be.x; x[e + 1] = dz[e + 1] * be.y; x[e + 2] = dz[e + 2] * be.z; x[e + 3] = dz[e + 3] * be.w;
-                }
+                for (int e = 0; e < 16; ++e) x[e] = y[e];
+                scale(x, gates + 2 * kTok);                  // dV
             }
-            tmem_wait_st();
-            tmem_fence_before_sync();
-            walk_ready(&ws, lane);
+            walk_ready(&ws.u_ready, lane);
             if (RUN) {
                 if (row < rows8) {                           // dZ: [quartet of tokens][row]
                     float4 *to = (float4 *)a.dz + ((bh * a.chunks + c) * 16 + 8 * half) * rows8 + row;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) { HN_G(to + e * rows8, 16); to[e * rows8] = make_float4(dz[4 * e], dz[4 * e + 1], dz[4 * e + 2], dz[4 * e + 3]); }
+                    for (int e = 0; e < 8; ++e) { HN_G(to + e * rows8, 16); to[e * rows8] = make_float4(y[2 * e].x, y[2 * e].y, y[2 * e + 1].x, y[2 * e + 1].y); }
                 }
                 if (stored) {                                // dV as an image that a copy takes away
                     unsigned char *image = out + (i & 1) * C::TILE;
@@ -243,29 +227,38 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
                     }
                     __syncwarp();
                 } else if (real && t < a.L) store_row<T>((T *)a.dv, vrow + t, a.L, a.L - t, n - t, x);
+                keep_state<HC / 8, HC / 4>(kept, S, row, a.Dv, half * HC, a.Dk);
             }
-            WAIT(&ws.bar_c, par);
+            WAIT(&ws.bar_c[half], par);
             tmem_fence_after_sync();
 #pragma unroll
-            for (int e = 0; e < HC; e += 32) {
-                TmemIO<32>::ld(x, lane_d + e);
+            for (int e = 0; e < HC / 2; e += 16) {
+                tmem_ld(x, lane_d + 2 * e);
                 tmem_wait_ld();
 #pragma unroll
-                for (int j = 0; j < 32; ++j) S[e + j] = fmaf(fade, S[e + j], x[j]);
+                for (int j = 0; j < 16; ++j) S[e + j] = fma2(fade, S[e + j], x[j]);
             }
         }
-        if (!RUN) {
-            float *to = a.maps + (bh * a.segments + segment) * (long long)(a.Dv + a.Dk) * a.Dk + (phi ? states : 0);
-            store_state<HC>(to, S, row, rows, half * HC, a.Dk);
-        } else {
-            float none[32];
+        auto flat = [&](float (&s)[HC]) {
 #pragma unroll
-            for (int e = 0; e < 32; ++e) none[e] = 0.f;
+            for (int i = 0; i < HC / 2; ++i) split2(S[i], s[2 * i], s[2 * i + 1]);
+        };
+        if (!RUN) {
+            float *to = a.maps + (bh * a.segments + segment) * (long long)(a.Dv + a.Dk) * a.Dk + (phi ? states : 0), s[HC];
+            flat(s);
+            store_state<HC>(to, s, row, rows, half * HC, a.Dk);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) y[e] = pair(0.f);
             for (int c = first > last ? first : last; c < end; ++c) {
                 const int t = c * kTok + 32 * half;
-                if (real && t < a.L) store_row<T>((T *)a.dv, vrow + t, a.L, a.L - t, 0, none);
+                if (real && t < a.L) store_row<T>((T *)a.dv, vrow + t, a.L, a.L - t, 0, y);
             }
-            if (a.ds0 && segment == 0) store_state<HC>(a.ds0 + bh * states, S, row, a.Dv, half * HC, a.Dk);
+            if (a.ds0 && segment == 0) {
+                float s[HC];
+                flat(s);
+                store_state<HC>(a.ds0 + bh * states, s, row, a.Dv, half * HC, a.Dk);
+            }
             if (stored && tid == 0) tma_wait_all0();
         }
         tmem_fence_before_sync();
@@ -319,7 +312,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
     __shared__ WalkShared ws;                                // bar_a: products, full[0]: a head's inputs, full[1]: the gradient behind the chunk
     __shared__ __align__(16) float gates[kGates];
     __shared__ float sums[3][4][kTok], erased[4][kTok], total[16];
-    const float *gamma = gates, *delta = gates + kTok, *beta = gates + 2 * kTok, *ghi = gates + 3 * kTok, *glo = gates + 4 * kTok;
+    const float *gamma = gates, *delta = gates + kTok, *beta = gates + 2 * kTok, *ghi = gates + 4 * kTok, *glo = gates + 5 * kTok;
     unsigned char *sm = align_images(raw);
     const int tid = threadIdx.x, lane = tid & 31, warp = uniform_warp(tid >> 5), row = 32 * (warp & 3) + lane, quarter = warp >> 2, share = a.H / a.Hk;
     const long long bk = blockIdx.x / a.chunks;
