@@ -455,44 +455,41 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
 
 // ---- segments -------------------------------------------------------------------------------------------------------
 
-// States at the segments' starts from the maps S -> S Phi + N: eight rows to a CTA, four quarters of the sum over Phi's rows; the next
+// States at the segments' starts from the maps S -> S Phi + N: four rows to a CTA, four quarters of the sum over Phi's rows; the next
 // segment's Phi is on its way meanwhile.  `reverse`: from the last segment to the first (the gradient's states).
 __global__ void __launch_bounds__(512) delta_join_kernel(DeltaArgs a, const float *from, int reverse)
 {
-    constexpr int R = 8;
-    __shared__ float S[R][128], part[4][R][128];
+    constexpr int R = 4;
+    __shared__ __align__(16) float S[R][128];
+    __shared__ float part[4][R][128];
     const int j = threadIdx.x & 127, quarter = threadIdx.x >> 7, tiles = (a.Dv + R - 1) / R;
     const long long bh = blockIdx.x / tiles, states = (long long)a.Dv * a.Dk, map = states + (long long)a.Dk * a.Dk;
-    const int r0 = (int)(blockIdx.x % tiles) * R;
+    const int row = (int)(blockIdx.x % tiles) * R + quarter, n = a.segments, step = reverse ? -1 : 1;
+    const bool mine = row < a.Dv && j < a.Dk;                // (a quarter of the threads to a row)
     pdl_join();
-    for (int e = threadIdx.x; e < R * 128; e += 512) {
-        const int r = e >> 7, c = e & 127;
-        float v = 0.f;
-        if (from && r0 + r < a.Dv && c < a.Dk) { const float *p = from + bh * states + (long long)(r0 + r) * a.Dk + c; HN_G(p, 4); v = *p; }
-        S[r][c] = v;
-    }
-    float phi[32];
-    auto fetch = [&](int s) {
-        const float *p = a.maps + (bh * a.segments + s) * map + states;
+    float v = 0.f;
+    if (from && mine) { const float *p = from + bh * states + (long long)row * a.Dk + j; HN_G(p, 4); v = *p; }
+    float phi[2][32], add[2];
+    auto fetch = [&](int s, float (&to)[32], float &plus) {
+        const float *p = a.maps + (bh * n + s) * map;
+        plus = 0.f;
+        if (mine) { HN_G(p + (long long)row * a.Dk + j, 4); plus = p[(long long)row * a.Dk + j]; }
+        p += states + (long long)quarter * 32 * a.Dk + j;
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
-            const int k = quarter * 32 + i;
-            phi[i] = 0.f;
-            if (k < a.Dk && j < a.Dk) { HN_G(p + (long long)k * a.Dk + j, 4); phi[i] = p[(long long)k * a.Dk + j]; }
+            to[i] = 0.f;
+            if (quarter * 32 + i < a.Dk && j < a.Dk) { HN_G(p + i * a.Dk, 4); to[i] = p[i * a.Dk]; }
         }
     };
-    const int n = a.segments, step = reverse ? -1 : 1;
     int s = reverse ? n - 1 : 0;
-    fetch(s);
-    __syncthreads();
-    for (int i = 0; i < n; ++i, s += step) {
-        for (int r = quarter; r < R; r += 4)
-            if (r0 + r < a.Dv && j < a.Dk) {
-                float *p = a.starts + (bh * n + s) * states + (long long)(r0 + r) * a.Dk + j;
-                HN_G(p, 4);
-                *p = S[r][j];
-            }
-        if (i == n - 1) break;
+    auto advance = [&](const float (&with)[32], float plus) {
+        S[quarter][j] = v;
+        if (mine) {
+            float *p = a.starts + (bh * n + s) * states + (long long)row * a.Dk + j;
+            HN_G(p, 4);
+            *p = v;
+        }
+        __syncthreads();
         float acc[R];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -500,25 +497,23 @@ __global__ void __launch_bounds__(512) delta_join_kernel(DeltaArgs a, const floa
 #pragma unroll
             for (int k = 0; k < 32; k += 4) {
                 const float4 w = *(const float4 *)&S[r][quarter * 32 + k];
-                acc[r] = fmaf(w.x, phi[k], fmaf(w.y, phi[k + 1], fmaf(w.z, phi[k + 2], fmaf(w.w, phi[k + 3], acc[r]))));
+                acc[r] = fmaf(w.x, with[k], fmaf(w.y, with[k + 1], fmaf(w.z, with[k + 2], fmaf(w.w, with[k + 3], acc[r]))));
             }
         }
-        float add[2] = {0.f, 0.f};
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int r = quarter + 4 * e;
-            if (r0 + r < a.Dv && j < a.Dk) { const float *p = a.maps + (bh * n + s) * map + (long long)(r0 + r) * a.Dk + j; HN_G(p, 4); add[e] = *p; }
-        }
-        fetch(s + step);
 #pragma unroll
         for (int r = 0; r < R; ++r) part[quarter][r][j] = acc[r];
         __syncthreads();
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int r = quarter + 4 * e;
-            S[r][j] = ((part[0][r][j] + part[1][r][j]) + (part[2][r][j] + part[3][r][j])) + add[e];
-        }
-        __syncthreads();
+        v = ((part[0][quarter][j] + part[1][quarter][j]) + (part[2][quarter][j] + part[3][quarter][j])) + plus;
+    };
+    fetch(s, phi[0], add[0]);
+    for (int i = 0; i < n; i += 2) {
+        if (i + 1 < n) fetch(s + step, phi[1], add[1]);
+        advance(phi[0], add[0]);
+        s += step;
+        if (i + 1 >= n) break;
+        if (i + 2 < n) fetch(s + step, phi[0], add[0]);
+        advance(phi[1], add[1]);
+        s += step;
     }
 }
 
@@ -624,7 +619,7 @@ int launch_delta_prepare(DeltaArgs a, int dtype, cudaStream_t st) { return dtype
 
 int launch_delta_join(const DeltaArgs &a, const float *from, bool backward, cudaStream_t st)
 {
-    const long long blocks = (long long)a.B * a.H * ((a.Dv + 7) / 8);
+    const long long blocks = (long long)a.B * a.H * ((a.Dv + 3) / 4);
     if (blocks > 0x7fffffffll) return kTooLarge;
     launch_pdl(delta_join_kernel, dim3((unsigned)blocks), 512, 0, st, a, from, (int)backward);
     return 0;

@@ -279,10 +279,11 @@ template <typename T, int KD> struct Grads {
     static constexpr int DY = 0, K = PI * TILE, Q = ROOM ? 2 * PI * TILE : DY, U = (ROOM ? 3 : 2) * PI * TILE, DZ = U + PM * TILE, A = DZ + PM * TILE, STATE = A + PM * kMatrix,
                          BYTES = 1024 + STATE + (ROOM ? KD * KD * 4 : 0);
     // tensor memory: a state as an operand | sums of 64 columns:
-    //     0: S0 k, U, S0 dY   1: Z (and 2), dY U^T and dZ U^T, F k   2: K K^T, E k and the erased part of dK   3: S0 dZ, F q and E k   4: dS1 u
-    // and, where a plane is left over, 5: the rest of dZ U^T
-    static constexpr int S0 = 0, SCOLS = PM * KD / 2, R0 = SCOLS, SUMS = PI < PM ? 6 : 5;
-    static_assert(R0 + SUMS * kTok <= 512 && BYTES + 7168 <= 227 * 1024 && PM * kTok / 2 <= 2 * kTok && PM * TILE >= PM * kMatrix, "tensor and shared memory");
+    //     0: S0 k, U, the rest of dZ U^T   1: Z (and the next), dY U^T and dZ U^T   2: K K^T, the written part of dK but for dS1 u
+    //     3: S0 dZ, the erased part of dK   4: S0 dY, dQ   5 (0 where there is no rest): dS1 u
+    static constexpr bool REST = PI < PM;
+    static constexpr int S0 = 0, SCOLS = PM * KD / 2, R0 = SCOLS, R1 = R0 + kTok, R2 = R1 + kTok, R3 = R2 + kTok, R4 = R3 + kTok, R5 = REST ? R4 + kTok : R0;
+    static_assert(R4 + kTok <= 512 && R5 + kTok <= 512 && BYTES + 7168 <= 227 * 1024 && PM * kTok / 2 <= 2 * kTok && PM * TILE >= PM * kMatrix, "tensor and shared memory");
 };
 constexpr int kGradThreads = 512;
 
@@ -367,8 +368,9 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
     for (int j = 0; j < share; ++j) {
         const long long bh = (long long)b * a.H + hk * share + j, at = bh * a.chunks + chunk, grow = bh * a.L + t0;
         const float *S = a.marks + at * kept, *D = a.dstates + at * kept;
-        if (j) {                                             // the images and sums of the head before have been read
+        if (j) {                                             // the images, sums and tensor memory of the head before have been read
             fence_async_smem();
+            tmem_fence_before_sync();
             __syncthreads();
         }
         if (tid == 0) {
@@ -416,7 +418,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
         tmem_fence_after_sync();
         WAIT(&ws.full[0], j & 1);
         tb = ws.slot;
-        const unsigned lane_s = tmem_addr(tb, warp, C::S0 + quarter * (HC / 2)), lane_r = tmem_addr(tb, warp, C::R0 + quarter * 16);
+        const unsigned lane_s = tmem_addr(tb, warp, C::S0 + quarter * (HC / 2)), lane_r = tmem_addr(tb, warp, quarter * 16);
         const float4 *held = C::ROOM ? (const float4 *)(sm + C::STATE) : nullptr;
         // the state before the chunk, its rows as lanes: S0 k
 #pragma unroll 1
@@ -439,13 +441,15 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
         if (warp == 0) {
             issue_ts<PM, PI, PM, true, KD / 16, B_ALL, 4>(tb + C::R0, tb + C::S0, KD / 2, IK, C::TILE, ksteps, kTok, false);
             umma_commit(&ws.bar_a);
+            // rows 64 ..: K K^T
+            if (C::REST) issue_ss<PI, PI, PI, true, true, KD / 16, B_ALL, 4>(tb + C::R2, IY, C::TILE, C::K - C::DY, IK, C::TILE, ksteps, kTok, false);
         }
         done();
 #pragma unroll 1
         for (int g = 0; g < 2; ++g) {                        // R, Z and what dZ R says about beta
             const int c = 16 * quarter + 8 * g;
             float x[8], v[8], z[8];
-            tmem_ld8(x, lane_r + 8 * g);
+            tmem_ld8(x, lane_r + C::R0 + 8 * g);
             if (row < KD) {
                 image8<PI>(v, sm + C::U, C::TILE, row, c >> 3);
                 image8<PM>(z, sm + C::DZ, C::TILE, row, c >> 3);
@@ -457,13 +461,13 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
                 z[e] = row < a.Dv ? z[e] * x[e] : 0.f;
                 x[e] *= beta[c + e];
             }
-            planes8_to_tmem<PM>(tmem_addr(tb, warp, C::R0 + kTok + quarter * 8 + 4 * g), kTok / 2, x);
+            planes8_to_tmem<PM>(tmem_addr(tb, warp, C::R1 + quarter * 8 + 4 * g), kTok / 2, x);
             const float sum = column_sum8(z, lane);
             if (!(lane & 3)) sums[0][warp & 3][c + (lane >> 2)] = sum;
         }
         go();
         if (warp == 0) {
-            issue_ts<PM, PM, PM, false, kTok / 16, B_LOWER>(tb + C::R0, tb + C::R0 + kTok, kTok / 2, IA, kMatrix, kTok / 16, kTok, false);
+            issue_ts<PM, PM, PM, false, kTok / 16, B_LOWER>(tb + C::R0, tb + C::R1, kTok / 2, IA, kMatrix, kTok / 16, kTok, false);
             umma_commit(&ws.bar_a);
         }
         // a state with its columns as lanes; `with`: the sum of its products with the one that is there
@@ -505,14 +509,6 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
             return inner;
         };
         columns(S, false);
-        done();
-#pragma unroll 1
-        for (int g = 0; g < 2; ++g) {
-            float x[8];
-            tmem_ld8(x, lane_r + 8 * g);
-            tmem_wait_ld();
-            if (row < KD) planes8_to_image<PM>(sm + C::U, C::TILE, row, 2 * quarter + g, x);
-        }
         go();
         if (warp == 0) {
             if (C::ROOM && lane == 0) {                      // the state has been read: the gradient behind the chunk into its place
@@ -520,14 +516,37 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
                 bulk_load(sm + C::STATE, D, (unsigned)(kept * 4), &ws.full[1]);
             }
             __syncwarp();
+            issue_ts<PM, PI, PM, true, KD / 16, B_ALL, 4>(tb + C::R4, tb + C::S0, KD / 2, IY, C::TILE, vsteps, kTok, false);            // S0 dY
+            issue_ts<PM, PM, PM, true, KD / 16, B_ALL, 4>(tb + C::R3, tb + C::S0, KD / 2, IZ, C::TILE, vsteps, kTok, false);            // S0 dZ
+            umma_commit(&ws.bar_b);
+        }
+        done();
+#pragma unroll 1
+        for (int g = 0; g < 2; ++g) {
+            float x[8];
+            tmem_ld8(x, lane_r + C::R0 + 8 * g);
+            tmem_wait_ld();
+            if (row < KD) planes8_to_image<PM>(sm + C::U, C::TILE, row, 2 * quarter + g, x);
+        }
+        go();
+        if (warp == 0) {
             // rows 0 .. 63: dY U^T, rows 64 ..: dZ U^T; where dY is one plane, dZ's second goes into a sum of its own
-            issue_ss<PI, PM, PM, true, true, KD / 16, B_ALL, 4>(tb + C::R0 + kTok, IY, C::TILE, C::DZ - C::DY, IU, C::TILE, vsteps, kTok, false);
-            if (PI < PM) issue_ss<1, 1, 1, true, true, KD / 16, B_ALL, 4>(tb + C::R0 + 5 * kTok, IY + C::TILE, C::TILE, C::DZ - C::DY, IU, C::TILE, vsteps, kTok, false);
-            // rows 64 ..: K K^T
-            issue_ss<PI, PI, PI, true, true, KD / 16, B_ALL, 4>(tb + C::R0 + 2 * kTok, IY, C::TILE, C::K - C::DY, IK, C::TILE, ksteps, kTok, false);
+            issue_ss<PI, PM, PM, true, true, KD / 16, B_ALL, 4>(tb + C::R1, IY, C::TILE, C::DZ - C::DY, IU, C::TILE, vsteps, kTok, false);
+            if (C::REST) issue_ss<1, 1, 1, true, true, KD / 16, B_ALL, 4>(tb + C::R0, IY + C::TILE, C::TILE, C::DZ - C::DY, IU, C::TILE, vsteps, kTok, false);
+            else issue_ss<PI, PI, PI, true, true, KD / 16, B_ALL, 4>(tb + C::R2, IY, C::TILE, C::K - C::DY, IK, C::TILE, ksteps, kTok, false);
             umma_commit(&ws.bar_a);
-            issue_ts<PM, PI, PM, true, KD / 16, B_ALL, 4>(tb + C::R0, tb + C::S0, KD / 2, IY, C::TILE, vsteps, kTok, false);
-            issue_ts<PM, PM, PM, true, KD / 16, B_ALL, 4>(tb + C::R0 + 3 * kTok, tb + C::S0, KD / 2, IZ, C::TILE, vsteps, kTok, false);
+        }
+        // the gradient behind the chunk in the state's place, while those are formed
+        if (C::ROOM) WAIT(&ws.full[1], j & 1);
+        WAIT(&ws.bar_b, 0);                                  // (two phases a head)
+        tmem_fence_after_sync();
+        float inner = columns(D, true);
+#pragma unroll
+        for (int m = 1; m < 32; m <<= 1) inner += __shfl_xor_sync(~0u, inner, m);
+        if (lane == 0) total[warp] = inner;
+        go();
+        if (warp == 0) {
+            issue_ts<PM, PM, PM, true, KD / 16, B_ALL, 4>(tb + C::R5, tb + C::S0, KD / 2, IU, C::TILE, vsteps, kTok, false);            // dS1 u
             umma_commit(&ws.bar_b);
         }
         done();
@@ -539,59 +558,45 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
             for (int g = 0; g < 2; ++g) {
                 const int c0 = 16 * quarter + 8 * g;
                 float x[8], y[8], z[8];
-                tmem_ld8(x, lane_r + kTok + 8 * g);
-                tmem_ld8(y, lane_r + 2 * kTok + 8 * g);
-                if (PI < PM) tmem_ld8(z, lane_r + 5 * kTok + 8 * g);
+                tmem_ld8(x, lane_r + C::R1 + 8 * g);
+                tmem_ld8(y, lane_r + C::R2 + 8 * g);
+                if (C::REST) tmem_ld8(z, lane_r + C::R0 + 8 * g);
                 tmem_wait_ld();
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const int c = c0 + e;
                     const float r = ratio(Hi, Li, ghi[c], glo[c]);
                     if (warp & 2) {
-                        if (PI < PM) x[e] += z[e];
+                        if (C::REST) x[e] += z[e];
                         own += c < i ? x[e] * r * y[e] : 0.f;
                         x[e] = c < i ? -bi * r * x[e] : 0.f;
                     } else x[e] = c <= i ? r * x[e] : 0.f;
                 }
-                // (dZ's image is in use until the products of the states are through)
-                if (g == 0 && (warp & 2)) WAIT(&ws.bar_b, j & 1);
                 planes8_to_image<PM>(sm + (warp & 2 ? C::DZ : C::A), kMatrix, i, c0 >> 3, x);
+                // dQ and the erased part of dK, as far as they come from the state: F k and E k are added to them
+                tmem_ld8(x, lane_r + C::R4 + 8 * g);
+                tmem_ld8(y, lane_r + C::R3 + 8 * g);
+                tmem_wait_ld();
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    x[e] *= gamma[c0 + e];
+                    y[e] *= -gamma[c0 + e] * beta[c0 + e];
+                }
+                tmem_st8(lane_r + C::R4 + 8 * g, x);
+                tmem_st8(lane_r + C::R3 + 8 * g, y);
             }
             if (warp & 2) erased[quarter][i] = own;
         }
-        WAIT(&ws.bar_b, j & 1);
-        go();
-        if (warp == 0) {
-            issue_ss<PI, PM, PM, false, false, kTok / 16, B_LOWER>(tb + C::R0 + kTok, IK, C::TILE, 0, IA, kMatrix, kTok / 16, kTok, false);         // F k
-            issue_ss<PI, PM, PM, false, false, kTok / 16, B_LOWER>(tb + C::R0 + 2 * kTok, IK, C::TILE, 0, IZ, kMatrix, kTok / 16, kTok, false);     // E k
-            umma_commit(&ws.bar_a);
-        }
-        if (C::ROOM) WAIT(&ws.full[1], j & 1);
-        float inner = columns(D, true);
-#pragma unroll
-        for (int m = 1; m < 32; m <<= 1) inner += __shfl_xor_sync(~0u, inner, m);
-        if (lane == 0) total[warp] = inner;
         if (!C::ROOM) {                                      // queries take dY's place
             load_tile<T>(sm + C::Q, C::TILE, (const T *)a.q, qk, all, a.L, a.Dk, nv, tid, kGradThreads);
             clear_rows(sm + C::Q, C::TILE, PI, a.Dk, KD, tid, kGradThreads);
         }
-        done();
-#pragma unroll 1
-        for (int g = 0; g < 2; ++g) {                        // the erased part of dK, so that the third sum is free
-            const int c = 16 * quarter + 8 * g;
-            float x[8], y[8];
-            tmem_ld8(x, lane_r + 2 * kTok + 8 * g);
-            tmem_ld8(y, lane_r + 3 * kTok + 8 * g);
-            tmem_wait_ld();
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = fmaf(-gamma[c + e] * beta[c + e], y[e], x[e]);
-            tmem_st8(lane_r + 2 * kTok + 8 * g, x);
-        }
         go();
         if (warp == 0) {
-            issue_ss<PI, PM, PM, false, true, kTok / 16, B_LOWER_T>(tb + C::R0 + 3 * kTok, IQ, C::TILE, 0, IA, kMatrix, kTok / 16, kTok, false);        // F q
-            issue_ss<PI, PM, PM, false, true, kTok / 16, B_LOWER_T>(tb + C::R0 + 3 * kTok, IK, C::TILE, 0, IZ, kMatrix, kTok / 16, kTok, true);         // E k, the other way
-            issue_ts<PM, PM, PM, true, KD / 16, B_ALL, 4>(tb + C::R0 + 4 * kTok, tb + C::S0, KD / 2, IU, C::TILE, vsteps, kTok, false);                   // dS1 u
+            issue_ss<PI, PM, PM, false, false, kTok / 16, B_LOWER>(tb + C::R4, IK, C::TILE, 0, IA, kMatrix, kTok / 16, kTok, true);             // F k
+            issue_ss<PI, PM, PM, false, false, kTok / 16, B_LOWER>(tb + C::R3, IK, C::TILE, 0, IZ, kMatrix, kTok / 16, kTok, true);             // E k
+            issue_ss<PI, PM, PM, false, true, kTok / 16, B_LOWER_T>(tb + C::R2, IQ, C::TILE, 0, IA, kMatrix, kTok / 16, kTok, false);           // F q
+            issue_ss<PI, PM, PM, false, true, kTok / 16, B_LOWER_T>(tb + C::R2, IK, C::TILE, 0, IZ, kMatrix, kTok / 16, kTok, true);            // E k, the other way
             umma_commit(&ws.bar_a);
         }
         done();
@@ -599,23 +604,19 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
         for (int g = 0; g < 2; ++g) {
             const int c = 16 * quarter + 8 * g;
             const bool in = row < a.Dk;                      // (a lane without a channel holds whatever lay behind an image)
-            float x[8], y[8], z[8], w[8];
-            tmem_ld8(x, lane_r + 8 * g);
-            tmem_ld8(y, lane_r + kTok + 8 * g);
+            float x[8], y[8], z[8], w[8], u[8];
+            tmem_ld8(x, lane_r + C::R4 + 8 * g);             // dQ of this head
+            tmem_ld8(y, lane_r + C::R3 + 8 * g);
+            tmem_ld8(w, lane_r + C::R2 + 8 * g);
+            tmem_ld8(u, lane_r + C::R5 + 8 * g);
             if (row < KD) image8<PI>(z, sm + C::Q, C::TILE, row, c >> 3);
             tmem_wait_ld();
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                x[e] = fmaf(gamma[c + e], x[e], y[e]);       // dQ of this head
                 dq[g][e] += x[e];
                 x[e] = in ? x[e] * z[e] : 0.f;
             }
-            tmem_ld8(y, lane_r + 2 * kTok + 8 * g);
-            tmem_ld8(w, lane_r + 3 * kTok + 8 * g);
-            float u[8];
-            tmem_ld8(u, lane_r + 4 * kTok + 8 * g);
             if (row < KD) image8<PI>(z, sm + C::K, C::TILE, row, c >> 3);
-            tmem_wait_ld();
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 u[e] *= delta[c + e];
