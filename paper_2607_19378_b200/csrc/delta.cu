@@ -198,7 +198,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(128) delta_prepa
 
 // ---- walk -----------------------------------------------------------------------------------------------------------
 
-#define WAIT(bar, parity) walk_wait(&ws, bar, parity, &hn_delta_status)
+#define WAIT(bar, parity) walk_wait(&ws, bar, parity)
 
 template <typename T, int KD> struct Walk {
     static constexpr int PI = Planes<T>::IN, PM = Planes<T>::MID, TILE = KD * 128, TENSOR = PI * TILE;
@@ -245,7 +245,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
     tmem_fence_after_sync();
     const unsigned tb = ws.slot;
     const long long states = (long long)a.Dv * a.Dk, vhead = bh * a.Dv * a.L, vall = (long long)a.B * a.H * a.Dv * a.L;
-    if (warp > 8) {
+    if (warp > 8 && warp < 12) {
         // ---- fetching
         const int ft = tid - 288;
         const long long bk = (long long)b * a.Hk + h / (a.H / a.Hk), qk = bk * a.Dk * a.L, all = (long long)a.B * a.Hk * a.Dk * a.L;
@@ -293,7 +293,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             if (a.Dk > KD / 2) issue_ts<PM, PI, PM, true, KD / 32>(tb + C::X0, tb + C::S0 + KD / 4, KD / 2, k + KD / 2 * 128, C::TILE, steps - KD / 32, kTok, true);
             umma_commit(&ws.bar_a);
             if (RUN) {
-                if (i) WAIT(&ws.y_taken, par ^ 1);
+                if (i) WAIT(&ws.o_taken, par ^ 1);           // (y of the chunk before)
                 tmem_fence_after_sync();
                 issue_ts<PM, PI, PM, true, KD / 16>(tb + C::Y0, tb + C::S0, KD / 2, k + C::Q, C::TILE, steps, kTok, false);
                 umma_commit(&ws.bar_q);
@@ -303,6 +303,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             issue_ts<PM, PM, PM, false, kTok / 16, B_LOWER>(tb + C::X0, tb + C::Z0, kTok / 2, A, kMatrix, kTok / 16, kTok, false);
             umma_commit(&ws.bar_b);
             WAIT(&ws.u_ready, par);
+            if (RUN && !C::ROOM) WAIT(&ws.p_ready, par);     // (the gain comes where U is)
             tmem_fence_after_sync();
             issue_ts<PM, PI, PM, false, kTok / 16>(tb + C::D0, tb + C::U0, kTok / 2, k, C::TILE, kTok / 16, KD / 2, false);
             if (C::ROOM) umma_commit(&ws.bar_c[0]);
@@ -310,22 +311,76 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             if (!C::ROOM) umma_commit(&ws.bar_c[0]);
             umma_commit(&ws.bar_c[1]);
             if (RUN) {
-                WAIT(&ws.p_ready, par);
+                if (C::ROOM) WAIT(&ws.p_ready, par);
+                WAIT(&ws.o_ready, par);                      // (y's first sum times gamma)
                 tmem_fence_after_sync();
                 issue_ts<PM, PM, PM, false, kTok / 16, B_LOWER>(tb + C::Y0, tb + C::Z0, kTok / 2, P, kMatrix, kTok / 16, kTok, true);
                 umma_commit(&ws.bar_y);
             }
             umma_commit(&ws.empty[s]);
         }
+    } else if (warp >= 12) {
+        // ---- results: y's first sum times gamma, then y as an image that a copy takes away, or by these threads
+        const int row = 32 * (warp & 3) + lane;
+        const unsigned lane_y = tmem_addr(tb, warp, C::Y0);
+        const long long vrow = vhead + (long long)row * a.L;
+        const bool real = row < a.Dv, stored = C::VALUES && a.copies;
+        for (int c = first, i = 0; RUN && c < last; ++c, ++i) {
+            const int s = i % C::STAGES, t = c * kTok;
+            const float *gates = (const float *)(sm + s * C::STAGE + C::GATES);
+            WAIT(&ws.full[s], (i / C::STAGES) & 1);
+            WAIT(&ws.bar_q, i & 1);
+            tmem_fence_after_sync();
+#pragma unroll 2
+            for (int e = 0; e < kTok; e += 8) {
+                f2 y[4], ga[4];
+                tmem_ld8(y, lane_y + e);
+                shared8(ga, gates + e);
+                tmem_wait_ld();
+#pragma unroll
+                for (int j = 0; j < 4; ++j) y[j] = mul2(y[j], ga[j]);
+                tmem_st8(lane_y + e, y);
+            }
+            walk_ready(&ws.o_ready, lane);
+            unsigned char *image = sm + C::STAGES * C::STAGE + (i & 1) * C::TILE;
+            WAIT(&ws.bar_y, i & 1);
+            tmem_fence_after_sync();
+#pragma unroll 2
+            for (int e = 0; e < kTok; e += 8) {
+                float y[8];
+                tmem_ld8(y, lane_y + e);
+                tmem_wait_ld();
+                if (C::VALUES && stored) {
+                    if (row < KD) *(uint4 *)(image + image_at(row, e >> 3)) = bf16_8(y, n - t - e);
+                } else if (real && t + e < a.L) store8<T>((T *)a.y, vrow + t + e, a.L, a.L - t - e, n - t - e, y);
+            }
+            walk_ready(&ws.o_taken, lane);
+            if (stored) {
+                fence_async_smem();
+                takers_sync();
+                if (tid == 384) {
+                    tma_store_3d(&maps.out, image, t, 0, (int)bh);
+                    tma_commit();
+                    tma_wait_read1();                        // the other image is free again
+                }
+                takers_sync();
+            }
+        }
+        if (RUN) {
+            const float none[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+            for (int t = kTok * (first > last ? first : last); t < kTok * end; t += 8)
+                if (real && t < a.L) store8<T>((T *)a.y, vrow + t, a.L, a.L - t, 0, none);
+            if (stored && tid == 384) tma_wait_all0();
+        }
+        tmem_fence_before_sync();
     } else {
         // ---- computing: lane of tensor memory = row of the state, `half` = which half of the columns
         const int row = 32 * (warp & 3) + lane, half = warp >> 2, rows = phi ? a.Dk : a.Dv;
         const unsigned lane_s = tmem_addr(tb, warp, C::S0 + half * (HC / 2)), lane_z = tmem_addr(tb, warp, C::Z0 + half * 16), lane_u = tmem_addr(tb, warp, C::U0 + half * 16),
-                       lane_x = tmem_addr(tb, warp, C::X0 + half * 32), lane_y = tmem_addr(tb, warp, C::Y0 + half * 32), lane_d = tmem_addr(tb, warp, half ? C::D1 : C::D0);
-        const long long vrow = vhead + (long long)row * a.L;
-        const bool real = row < a.Dv, stored = C::VALUES && a.copies;
-        unsigned char *out = sm + C::STAGES * C::STAGE;
-        f2 S[HC / 2], x[16], y[16];
+                       lane_x = tmem_addr(tb, warp, C::X0 + half * 32), lane_d = tmem_addr(tb, warp, half ? C::D1 : C::D0);
+        const bool values = row < a.Dv && !phi;
+        f2 S[HC / 2];
         {
             float s[HC];
 #pragma unroll
@@ -335,87 +390,73 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
 #pragma unroll
             for (int i = 0; i < HC / 2; ++i) S[i] = make2(s[2 * i], s[2 * i + 1]);
         }
-        // the results of chunk c: as an image that a copy takes away, or by their threads
-        auto take_y = [&](int c, unsigned par) {
-            WAIT(&ws.bar_y, par);
-            tmem_fence_after_sync();
-            tmem_ld(y, lane_y);
-            tmem_wait_ld();
-            walk_ready(&ws.y_taken, lane);
-            const int t = c * kTok + 32 * half;
-            if (stored) {
-                unsigned char *image = out + (c & 1) * C::TILE;
-                if (row < KD) row_to_image(image, row, half, n - t, y);
-                fence_async_smem();
-                walkers_sync();
-                if (tid == 0) {
-                    tma_store_3d(&maps.out, image, c * kTok, 0, (int)bh);
-                    tma_commit();
-                    tma_wait_read1();                        // the other image is free again once thread 0 has been here
-                }
-                __syncwarp();
-            } else if (real && t < a.L) store_row<T>((T *)a.y, vrow + t, a.L, a.L - t, n - t, y);
-        };
         for (int c = first, i = 0; c < last; ++c, ++i) {
             const int s = i % C::STAGES, t = c * kTok + 32 * half;
             const unsigned par = i & 1;
             const unsigned char *st = sm + s * C::STAGE;
             const float *gates = (const float *)(st + C::GATES) + 32 * half;
-            float *mark = a.marks + (bh * a.chunks + c) * kept_floats(a.Dv, a.Dk);
-            const bool keep = RUN && a.marks;                // (in parts, where the threads wait anyhow)
             planes_to_tmem<PM, HC / 2>(lane_s, KD / 2, S);
             walk_ready(&ws.state[half], lane);
-            if (RUN && i) take_y(c - 1, par ^ 1);
-            if (keep) keep_state<0, HC / 16>(mark, S, row, a.Dv, half * HC, a.Dk);
-            f2 w[16];                                        // beta v
+            f2 held[C::VALUES ? 1 : 16];                     // (fp32 values come from device memory: ahead of their use)
+            if constexpr (!C::VALUES) load_row(held, (const float *)a.v, vhead + (long long)row * a.L + t, a.L, values ? n - t : 0);
+            if (RUN && a.marks) keep_state(a.marks + (bh * a.chunks + c) * kept_floats(a.Dv, a.Dk), S, row, a.Dv, half * HC, a.Dk);
             WAIT(&ws.full[s], (i / C::STAGES) & 1);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) w[e] = pair(0.f);
-            if (real && !phi) {
-                if constexpr (C::VALUES) image_row<1>(w, st + C::V, C::TILE, row, half);
-                else load_row(w, (const float *)a.v, vrow + t, a.L, n - t);
-                scale(w, gates + 2 * kTok);
-            }
             WAIT(&ws.bar_a, par);
             tmem_fence_after_sync();
-            tmem_ld(x, lane_x);
-            tmem_wait_ld();
 #pragma unroll
-            for (int e = 0; e < 16; e += 2) {                // Z = beta v - beta gamma S k
-                const float4 bg = *(const float4 *)(gates + 3 * kTok + 2 * e);
-                x[e] = fma2(make2(bg.x, bg.y), x[e], w[e]);
-                x[e + 1] = fma2(make2(bg.z, bg.w), x[e + 1], w[e + 1]);
-            }
-            planes_to_tmem<PM, 16>(lane_z, kTok / 2, x);
-            walk_ready(&ws.z_ready, lane);
-            if (RUN) {                                       // y's first sum by gamma, while A Z is formed
-                WAIT(&ws.bar_q, par);
-                tmem_fence_after_sync();
-                tmem_ld(y, lane_y);
+            for (int g = 0; g < 4; ++g) {                    // Z = beta v - beta gamma S k
+                f2 x[4], v[4], be[4], bg[4];
+                tmem_ld8(x, lane_x + 8 * g);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = pair(0.f);
+                if constexpr (C::VALUES) {
+                    if (values) {
+                        const uint4 w = *(const uint4 *)(st + C::V + image_at(row, 4 * half + g));
+                        v[0] = widen2(w.x); v[1] = widen2(w.y); v[2] = widen2(w.z); v[3] = widen2(w.w);
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = held[4 * g + e];
+                }
+                shared8(be, gates + 2 * kTok + 8 * g);
+                shared8(bg, gates + 3 * kTok + 8 * g);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = mul2(be[e], v[e]);
                 tmem_wait_ld();
-                scale(y, gates);
-                tmem_st(lane_y, y);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = fma2(bg[e], x[e], v[e]);
+                planes8_to_tmem<PM>(lane_z + 4 * g, kTok / 2, x);
             }
-            if (keep) keep_state<HC / 16, HC / 8>(mark, S, row, a.Dv, half * HC, a.Dk);
+            walk_ready(&ws.z_ready, lane);
+            const f2 fade = pair(((const float *)(st + C::GATES))[kTok - 1]);
             WAIT(&ws.bar_b, par);
             tmem_fence_after_sync();
-            tmem_ld(x, lane_x);
-            tmem_wait_ld();
 #pragma unroll
-            for (int e = 0; e < 16; ++e) y[e] = x[e];
-            scale(x, gates + kTok);
-            planes_to_tmem<PM, 16>(lane_u, kTok / 2, x);
-            const f2 fade = pair(((const float *)(st + C::GATES))[kTok - 1]);
+            for (int g = 0; g < 4; ++g) {
+                f2 x[4], de[4];
+                tmem_ld8(x, lane_x + 8 * g);
+                shared8(de, gates + kTok + 8 * g);
+                tmem_wait_ld();
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = mul2(x[e], de[e]);
+                planes8_to_tmem<PM>(lane_u + 4 * g, kTok / 2, x);
+            }
             walk_ready(&ws.u_ready, lane);
             if (RUN) {
-                planes_to_tmem<PM, 16>(lane_z, kTok / 2, y);
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    f2 x[4];
+                    tmem_ld8(x, lane_x + 8 * g);
+                    tmem_wait_ld();
+                    planes8_to_tmem<PM>(lane_z + 4 * g, kTok / 2, x);
+                }
                 walk_ready(&ws.p_ready, lane);
             }
-            if (keep) keep_state<HC / 8, HC / 4>(mark, S, row, a.Dv, half * HC, a.Dk);
             WAIT(&ws.bar_c[half], par);
             tmem_fence_after_sync();
 #pragma unroll
             for (int e = 0; e < HC / 2; e += 16) {
+                f2 x[16];
                 tmem_ld(x, lane_d + 2 * e);
                 tmem_wait_ld();
 #pragma unroll
@@ -431,25 +472,19 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             flat(s);
             store_state<HC>(to, s, row, rows, half * HC, a.Dk);
         } else {
-            if (first < last) take_y(last - 1, (last - first - 1) & 1);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) y[e] = pair(0.f);
-            for (int c = first > last ? first : last; c < end; ++c) {
-                const int t = c * kTok + 32 * half;
-                if (real && t < a.L) store_row<T>((T *)a.y, vrow + t, a.L, a.L - t, 0, y);
-            }
             if (a.s_end && segment == a.segments - 1) {
                 float s[HC];
                 flat(s);
                 store_state<HC>(a.s_end + bh * states, s, row, a.Dv, half * HC, a.Dk);
             }
-            if (stored && tid == 0) tma_wait_all0();
         }
         tmem_fence_before_sync();
     }
     __syncthreads();
-    if (ws.gave_up && tid == 0)                              // copies on their way end before the memory they go to is another CTA's
+    if (ws.gave_up && tid == 0) {                            // copies on their way end before the memory they go to is another CTA's
+        atomicExch(&hn_delta_status, 1);
         for (int s = 0; s < C::STAGES; ++s) mbar_wait(&ws.full[s], 0);
+    }
     if (warp == 0) tmem_dealloc(tb, 512);
 }
 

@@ -148,6 +148,40 @@ __device__ __forceinline__ void scale(f2 (&v)[16], const float *by)
         v[i + 1] = mul2(v[i + 1], make2(w.z, w.w));
     }
 }
+// the same eight columns at a time
+__device__ __forceinline__ void tmem_ld8(f2 (&v)[4], unsigned at)
+{
+    float x[8];
+    tmem_ld8(x, at);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = make2(x[2 * i], x[2 * i + 1]);
+}
+__device__ __forceinline__ void tmem_st8(unsigned at, const f2 (&v)[4])
+{
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) split2(v[i], x[2 * i], x[2 * i + 1]);
+    tmem_st8(at, x);
+}
+template <int PM> __device__ __forceinline__ void planes8_to_tmem(unsigned at, int pitch, const f2 (&x)[4])
+{
+    unsigned w[PM][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        unsigned u[PM];
+        split_pair<PM>(x[i], u);
+#pragma unroll
+        for (int p = 0; p < PM; ++p) w[p][i] = u[p];
+    }
+#pragma unroll
+    for (int p = 0; p < PM; ++p) tmem_st4(at + p * pitch, w[p]);
+}
+// eight numbers of shared memory
+__device__ __forceinline__ void shared8(f2 (&v)[4], const float *p)
+{
+    const float4 a = *(const float4 *)p, b = *(const float4 *)(p + 4);
+    v[0] = make2(a.x, a.y); v[1] = make2(a.z, a.w); v[2] = make2(b.x, b.y); v[3] = make2(b.z, b.w);
+}
 // 32 numbers, tokens 32 half .. of row `row` of an image
 template <int PM> __device__ __forceinline__ void planes_to_image(unsigned char *image, int pitch, int row, int half, const float (&x)[32])
 {
@@ -415,18 +449,19 @@ template <typename T> __device__ __forceinline__ void store_row(T *p, long long 
 __host__ __device__ __forceinline__ int kept_rows(int rows) { return (rows + 7) & ~7; }
 __host__ __device__ __forceinline__ long long kept_floats(int rows, int D) { return (long long)kept_rows(rows) * ((D + 3) & ~3); }
 __device__ __forceinline__ int kept_at(int row, int quartet, int rows8) { return quartet * rows8 + (row ^ (quartet & 7)); }
-// (quartets FROM .. TO - 1 of this thread's C columns from `col`)
-template <int FROM, int TO, int C> __device__ __forceinline__ void keep_state(float *p, const f2 (&s)[C], int row, int rows, int col, int D)
+// (this thread's 2 C columns from `col`, a multiple of 32)
+template <int C> __device__ __forceinline__ void keep_state(float *p, const f2 (&s)[C], int row, int rows, int col, int D)
 {
     const int rows8 = kept_rows(rows);
     if (row >= rows8) return;
+    float4 *to = (float4 *)p + (col >> 2) * rows8;
 #pragma unroll
-    for (int i = 4 * FROM; i < 4 * TO; i += 4)
-        if (col + i < D) {
-            float4 *to = (float4 *)p + kept_at(row, (col + i) >> 2, rows8);
-            HN_G(to, 16);
-            *to = make_float4(s[i / 2].x, s[i / 2].y, s[i / 2 + 1].x, s[i / 2 + 1].y);
-        }
+    for (int i = 0; i < C / 2; ++i) {
+        if (col + 4 * i >= D) break;
+        HN_G(to + (row ^ (i & 7)), 16);
+        to[row ^ (i & 7)] = make_float4(s[2 * i].x, s[2 * i].y, s[2 * i + 1].x, s[2 * i + 1].y);
+        to += rows8;
+    }
 }
 // this thread's C columns from `col` of row `row` of a state [rows][D], zero outside it
 template <int C> __device__ __forceinline__ void load_state(float (&s)[C], const float *p, int row, int rows, int col, int D)
@@ -567,28 +602,32 @@ __device__ __forceinline__ int uniform_warp(int warp) { return __shfl_sync(~0u, 
 // What the warps of a walk share beside the stages.  A wait that gives up ends all later ones of the CTA.
 struct WalkShared {
     uint64_t full[4], empty[4], bar_a, bar_b, bar_c[2], bar_q, bar_y;          // copies; products
-    uint64_t state[2], y_taken, z_ready, u_ready, p_ready;                    // the computing warps (of a half) to the one that issues
+    uint64_t state[2], z_ready, u_ready, p_ready;             // the computing warps (of a half) to the one that issues
+    uint64_t o_ready, o_taken;                                // the warps with the results to the one that issues
     unsigned slot;
     int gave_up;
 };
-__device__ __forceinline__ void walk_wait(WalkShared *w, uint64_t *bar, unsigned parity, int *status)
+// Bounded by its polls, which sleep up to some microseconds each.  As few instructions as can be, for there are twenty of these waits in a
+// walk's loop (see below); who gives up leaves a mark, and what it means is said at the kernel's end.
+constexpr unsigned kWalkPolls = 1u << 20;
+__device__ __forceinline__ void walk_wait(WalkShared *w, uint64_t *bar, unsigned parity)
 {
-    for (int i = 0; i < 64; ++i)                             // (before the clock is read, which takes longer than most waits)
-        if (mbar_try_wait(bar, parity)) return;
-    volatile int *f = &w->gave_up;
-    if (*f) return;
-    if (!mbar_wait(bar, parity)) { *f = 1; atomicExch(status, 1); }
+    asm volatile("{\n .reg .pred p;\n .reg .u32 i, f;\n mov.u32 i, 0;\n"
+                 "WALK_POLL_%=:\n mbarrier.try_wait.parity.shared::cta.b64 p, [%0], %1;\n @p bra WALK_DONE_%=;\n"
+                 " ld.volatile.shared.u32 f, [%2];\n add.u32 i, i, 1;\n setp.lt.u32 p, i, %3;\n setp.eq.and.u32 p, f, 0, p;\n @p bra WALK_POLL_%=;\n"
+                 " st.volatile.shared.u32 [%2], 1;\n"
+                 "WALK_DONE_%=:\n}\n" ::"r"(smem_u32(bar)), "r"(parity), "r"(smem_u32(&w->gave_up)), "n"(kWalkPolls) : "memory");
 }
 __device__ __forceinline__ void mbar_arrive(uint64_t *bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];\n" ::"r"(smem_u32(bar)) : "memory"); }
-// Warps 0 .. 7 compute, warp 8 issues the products, the others fetch.  What the eight wrote into tensor memory is handed to warp 8 by
-// barriers; what it gives back they see by the products' barriers.
-constexpr int kWalkThreads = 384, kFetchers = kWalkThreads - 288;
+// Warps 0 .. 7 compute, warp 8 issues the products, warps 9 .. 11 fetch, warps 12 .. 15 take results away.  What is written into tensor
+// memory is handed to warp 8 by barriers; what it gives back is seen by the products' barriers.
+constexpr int kWalkThreads = 512, kFetchers = 96;
 __device__ __forceinline__ void walk_init(WalkShared *w, int stages)
 {
     for (int s = 0; s < stages; ++s) { mbar_init(&w->full[s], 2); mbar_init(&w->empty[s], 1); }
     mbar_init(&w->bar_a, 1); mbar_init(&w->bar_b, 1); mbar_init(&w->bar_c[0], 1); mbar_init(&w->bar_c[1], 1); mbar_init(&w->bar_q, 1); mbar_init(&w->bar_y, 1);
     mbar_init(&w->state[0], 4); mbar_init(&w->state[1], 4);
-    mbar_init(&w->y_taken, 8); mbar_init(&w->z_ready, 8); mbar_init(&w->u_ready, 8); mbar_init(&w->p_ready, 8);
+    mbar_init(&w->z_ready, 8); mbar_init(&w->u_ready, 8); mbar_init(&w->p_ready, 8); mbar_init(&w->o_ready, 4); mbar_init(&w->o_taken, 4);
     w->gave_up = 0;
     fence_mbar_init();
 }
@@ -600,7 +639,7 @@ __device__ __forceinline__ void walk_ready(uint64_t *bar, int lane)
     if (lane == 0) mbar_arrive(bar);
 }
 __device__ __forceinline__ void fetchers_sync() { asm volatile("bar.sync 3, %0;\n" ::"n"(kFetchers) : "memory"); }
-__device__ __forceinline__ void walkers_sync() { asm volatile("bar.sync 2, 256;\n" ::: "memory"); }
+__device__ __forceinline__ void takers_sync() { asm volatile("bar.sync 2, 128;\n" ::: "memory"); }
 
 __device__ __forceinline__ unsigned char *align_images(unsigned char *p) { return p + ((1024u - (smem_u32(p) & 1023u)) & 1023u); }
 

@@ -12,7 +12,7 @@
 namespace hn {
 
 static __device__ int hn_delta_backward_status;
-#define WAIT(bar, parity) walk_wait(&ws, bar, parity, &hn_delta_backward_status)
+#define WAIT(bar, parity) walk_wait(&ws, bar, parity)
 
 // ---- walk -----------------------------------------------------------------------------------------------------------
 
@@ -63,7 +63,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
     tmem_fence_after_sync();
     const unsigned tb = ws.slot;
     const long long states = (long long)a.Dv * a.Dk, vhead = bh * a.Dv * a.L, vall = (long long)a.B * a.H * a.Dv * a.L;
-    if (warp > 8) {
+    if (warp > 8 && warp < 12) {
         // ---- fetching
         const int ft = tid - 288;
         const long long bk = (long long)b * a.Hk + h / (a.H / a.Hk), qk = bk * a.Dk * a.L, all = (long long)a.B * a.Hk * a.Dk * a.L;
@@ -104,7 +104,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
                 issue_ts<PM, PI, PM, false, kTok / 16>(tb + (h ? C::D1 : C::D0), from, kTok / 2, image + h * (KD / 2) * 128, C::TILE, kTok / 16, KD / 2, add);
             };
             WAIT(&ws.full[s], (i / C::STAGES) & 1);
-            // (P^T dY of the chunk before has been read: its dU was there)
+            // (P^T dY of the chunk before has been read: its dU was there; so has dZ)
             issue_ss<PI, PM, PM, false, true, kTok / 16, B_LOWER_T>(tb + C::Y0, k + C::DY, C::TILE, 0, P, kMatrix, kTok / 16, kTok, false);
             // dS k, the first half of dS's columns as soon as they are there
             WAIT(&ws.state[0], par);
@@ -115,7 +115,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             if (a.Dk > KD / 2) issue_ts<PM, PI, PM, true, KD / 32>(tb + C::X0, tb + C::S0 + KD / 4, KD / 2, k + KD / 2 * 128, C::TILE, steps - KD / 32, kTok, true);
             umma_commit(&ws.bar_a);
             if (C::ROOM) {                                   // gamma dY waits for nothing
-                WAIT(&ws.p_ready, par);
+                WAIT(&ws.o_ready, par);
                 tmem_fence_after_sync();
                 gain(0, tb + C::G0, q, false);
                 gain(1, tb + C::G0, q, false);
@@ -127,6 +127,9 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             WAIT(&ws.u_ready, par);                          // -beta gamma dZ (without the room, gamma dY too)
             tmem_fence_after_sync();
             if (!C::ROOM) {
+                WAIT(&ws.o_ready, par);
+                if (RUN) WAIT(&ws.o_taken, par);             // (the gain comes where dZ is)
+                tmem_fence_after_sync();
                 gain(0, tb + C::G0, q, false);
                 gain(1, tb + C::G0, q, false);
             }
@@ -135,18 +138,90 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             gain(1, tb + C::Z0, k, true);
             if (!C::ROOM) umma_commit(&ws.bar_c[0]);
             umma_commit(&ws.bar_c[1]);
+            if (RUN && C::ROOM) WAIT(&ws.o_taken, par);      // (the gates are read there too)
             umma_commit(&ws.empty[s]);
         }
-    } else {
-        // ---- computing
-        const int row = 32 * (warp & 3) + lane, half = warp >> 2, rows = phi ? a.Dk : a.Dv, rows8 = kept_rows(a.Dv);
-        const unsigned lane_s = tmem_addr(tb, warp, C::S0 + half * (HC / 2)), lane_g = tmem_addr(tb, warp, C::G0 + half * 16),
-                       lane_z = tmem_addr(tb, warp, C::Z0 + half * 16), lane_x = tmem_addr(tb, warp, C::X0 + half * 32), lane_y = tmem_addr(tb, warp, C::Y0 + half * 32),
-                       lane_d = tmem_addr(tb, warp, half ? C::D1 : C::D0);
+    } else if (warp >= 12) {
+        // ---- gamma dY as an operand; dZ and dV on their way out
+        const int row = 32 * (warp & 3) + lane, rows8 = kept_rows(a.Dv);
+        const unsigned lane_g = tmem_addr(tb, warp, C::G0), lane_x = tmem_addr(tb, warp, C::X0);
         const long long vrow = vhead + (long long)row * a.L;
         const bool real = row < a.Dv, stored = C::VALUES && a.copies;
-        unsigned char *out = sm + C::STAGES * C::STAGE;
-        f2 S[HC / 2], x[16], y[16];
+        for (int i = 0; i < count; ++i) {
+            const int c = last - 1 - i, s = i % C::STAGES, t = c * kTok;
+            const unsigned char *st = sm + s * C::STAGE;
+            const float *gates = (const float *)(st + C::GATES);
+            WAIT(&ws.full[s], (i / C::STAGES) & 1);
+            WAIT(C::ROOM ? &ws.state[0] : &ws.bar_a, i & 1);          // its place is free: the gain before has been formed; or dS k has
+            tmem_fence_after_sync();
+#pragma unroll 2
+            for (int e = 0; e < kTok; e += 8) {
+                f2 x[4], ga[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[j] = pair(0.f);
+                if (real && !phi) {
+                    float y[8];
+                    image8<PI>(y, st + C::DY, C::TILE, row, e >> 3);
+                    shared8(ga, gates + e);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[j] = mul2(make2(y[2 * j], y[2 * j + 1]), ga[j]);
+                }
+                __syncwarp();
+                planes8_to_tmem<PM>(lane_g + e / 2, kTok / 2, x);
+            }
+            walk_ready(&ws.o_ready, lane);
+            if (!RUN) continue;
+            unsigned char *image = sm + C::STAGES * C::STAGE + (i & 1) * C::TILE;
+            WAIT(&ws.bar_b, i & 1);
+            tmem_fence_after_sync();
+            float4 *to = (float4 *)a.dz + (bh * a.chunks + c) * 16 * rows8 + row;          // dZ: [quartet of tokens][row]
+#pragma unroll 2
+            for (int e = 0; e < kTok; e += 8) {
+                f2 z[4], be[4];
+                tmem_ld8(z, lane_x + e);
+                shared8(be, gates + 2 * kTok + e);
+                tmem_wait_ld();
+                if (row < rows8) {
+                    HN_G(to, 16); HN_G(to + rows8, 16);
+                    to[0] = make_float4(z[0].x, z[0].y, z[1].x, z[1].y);
+                    to[rows8] = make_float4(z[2].x, z[2].y, z[3].x, z[3].y);
+                }
+                to += 2 * rows8;
+                float y[8];                                  // dV: as an image that a copy takes away, or by these threads
+#pragma unroll
+                for (int j = 0; j < 4; ++j) split2(mul2(z[j], be[j]), y[2 * j], y[2 * j + 1]);
+                if (C::VALUES && stored) {
+                    if (row < KD) *(uint4 *)(image + image_at(row, e >> 3)) = bf16_8(y, n - t - e);
+                } else if (real && t + e < a.L) store8<T>((T *)a.dv, vrow + t + e, a.L, a.L - t - e, n - t - e, y);
+                __syncwarp();
+            }
+            walk_ready(&ws.o_taken, lane);                   // (the gates have been read as well)
+            if (stored) {
+                fence_async_smem();
+                takers_sync();
+                if (tid == 384) {
+                    tma_store_3d(&maps.out, image, t, 0, (int)bh);
+                    tma_commit();
+                    tma_wait_read1();                        // the other image is free again
+                }
+                takers_sync();
+            }
+        }
+        if (RUN) {
+            const float none[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+            for (int t = kTok * (first > last ? first : last); t < kTok * end; t += 8)
+                if (real && t < a.L) store8<T>((T *)a.dv, vrow + t, a.L, a.L - t, 0, none);
+            if (stored && tid == 384) tma_wait_all0();
+        }
+        tmem_fence_before_sync();
+    } else {
+        // ---- computing
+        const int row = 32 * (warp & 3) + lane, half = warp >> 2, rows = phi ? a.Dk : a.Dv;
+        const unsigned lane_s = tmem_addr(tb, warp, C::S0 + half * (HC / 2)),
+                       lane_z = tmem_addr(tb, warp, C::Z0 + half * 16), lane_x = tmem_addr(tb, warp, C::X0 + half * 32), lane_y = tmem_addr(tb, warp, C::Y0 + half * 32),
+                       lane_d = tmem_addr(tb, warp, half ? C::D1 : C::D0);
+        f2 S[HC / 2];
         {
             float s[HC];
 #pragma unroll
@@ -157,82 +232,46 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             for (int i = 0; i < HC / 2; ++i) S[i] = make2(s[2 * i], s[2 * i + 1]);
         }
         for (int i = 0; i < count; ++i) {
-            const int c = last - 1 - i, s = i % C::STAGES, t = c * kTok + 32 * half;
+            const int c = last - 1 - i, s = i % C::STAGES;
             const unsigned par = i & 1;
-            const unsigned char *st = sm + s * C::STAGE;
-            const float *gates = (const float *)(st + C::GATES) + 32 * half;
-            float *kept = a.dstates + (bh * a.chunks + c) * kept_floats(a.Dv, a.Dk);
+            const float *gates = (const float *)(sm + s * C::STAGE + C::GATES) + 32 * half;
             planes_to_tmem<PM, HC / 2>(lane_s, KD / 2, S);
             walk_ready(&ws.state[half], lane);
+            if (RUN) keep_state(a.dstates + (bh * a.chunks + c) * kept_floats(a.Dv, a.Dk), S, row, a.Dv, half * HC, a.Dk);
             WAIT(&ws.full[s], (i / C::STAGES) & 1);
-            auto gamma_dy = [&] {
-#pragma unroll
-                for (int e = 0; e < 16; ++e) x[e] = pair(0.f);
-                if (real && !phi) {
-                    image_row<PI>(x, st + C::DY, C::TILE, row, half);
-                    scale(x, gates);
-                }
-                planes_to_tmem<PM, 16>(lane_g, kTok / 2, x);
-            };
-            if (C::ROOM) {
-                gamma_dy();
-                walk_ready(&ws.p_ready, lane);
-            }
-            if (RUN) keep_state<0, HC / 16>(kept, S, row, a.Dv, half * HC, a.Dk);
             WAIT(&ws.bar_a, par);
             tmem_fence_after_sync();
-            tmem_ld(x, lane_x);
-            tmem_ld(y, lane_y);
-            tmem_wait_ld();
 #pragma unroll
-            for (int e = 0; e < 16; e += 2) {                // dU = P^T dY + delta dS k
-                const float4 de = *(const float4 *)(gates + kTok + 2 * e);
-                x[e] = row < rows ? fma2(make2(de.x, de.y), x[e], phi ? pair(0.f) : y[e]) : pair(0.f);
-                x[e + 1] = row < rows ? fma2(make2(de.z, de.w), x[e + 1], phi ? pair(0.f) : y[e + 1]) : pair(0.f);
+            for (int g = 0; g < 4; ++g) {                    // dU = P^T dY + delta dS k
+                f2 x[4], y[4], de[4];
+                tmem_ld8(x, lane_x + 8 * g);
+                tmem_ld8(y, lane_y + 8 * g);
+                shared8(de, gates + kTok + 8 * g);
+                tmem_wait_ld();
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = row < rows ? fma2(de[e], x[e], phi ? pair(0.f) : y[e]) : pair(0.f);
+                planes8_to_tmem<PM>(lane_z + 4 * g, kTok / 2, x);
             }
-            planes_to_tmem<PM, 16>(lane_z, kTok / 2, x);
             walk_ready(&ws.z_ready, lane);
-            if (!C::ROOM) gamma_dy();
-            if (RUN) keep_state<HC / 16, HC / 8>(kept, S, row, a.Dv, half * HC, a.Dk);
+            const f2 fade = pair(((const float *)(sm + s * C::STAGE + C::GATES))[kTok - 1]);
             WAIT(&ws.bar_b, par);
             tmem_fence_after_sync();
-            tmem_ld(y, lane_x);
-            tmem_wait_ld();
 #pragma unroll
-            for (int e = 0; e < 16; ++e) x[e] = y[e];
-            scale(x, gates + 3 * kTok);
-            planes_to_tmem<PM, 16>(lane_z, kTok / 2, x);
-            const f2 fade = pair(((const float *)(st + C::GATES))[kTok - 1]);
-            if (RUN) {
+            for (int g = 0; g < 4; ++g) {
+                f2 x[4], bg[4];
+                tmem_ld8(x, lane_x + 8 * g);
+                shared8(bg, gates + 3 * kTok + 8 * g);
+                tmem_wait_ld();
 #pragma unroll
-                for (int e = 0; e < 16; ++e) x[e] = y[e];
-                scale(x, gates + 2 * kTok);                  // dV
+                for (int e = 0; e < 4; ++e) x[e] = mul2(x[e], bg[e]);
+                planes8_to_tmem<PM>(lane_z + 4 * g, kTok / 2, x);
             }
             walk_ready(&ws.u_ready, lane);
-            if (RUN) {
-                if (row < rows8) {                           // dZ: [quartet of tokens][row]
-                    float4 *to = (float4 *)a.dz + ((bh * a.chunks + c) * 16 + 8 * half) * rows8 + row;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) { HN_G(to + e * rows8, 16); to[e * rows8] = make_float4(y[2 * e].x, y[2 * e].y, y[2 * e + 1].x, y[2 * e + 1].y); }
-                }
-                if (stored) {                                // dV as an image that a copy takes away
-                    unsigned char *image = out + (i & 1) * C::TILE;
-                    if (row < KD) row_to_image(image, row, half, n - t, x);
-                    fence_async_smem();
-                    walkers_sync();
-                    if (tid == 0) {
-                        tma_store_3d(&maps.out, image, c * kTok, 0, (int)bh);
-                        tma_commit();
-                        tma_wait_read1();                    // the other image is free again once thread 0 has been here
-                    }
-                    __syncwarp();
-                } else if (real && t < a.L) store_row<T>((T *)a.dv, vrow + t, a.L, a.L - t, n - t, x);
-                keep_state<HC / 8, HC / 4>(kept, S, row, a.Dv, half * HC, a.Dk);
-            }
             WAIT(&ws.bar_c[half], par);
             tmem_fence_after_sync();
 #pragma unroll
             for (int e = 0; e < HC / 2; e += 16) {
+                f2 x[16];
                 tmem_ld(x, lane_d + 2 * e);
                 tmem_wait_ld();
 #pragma unroll
@@ -248,24 +287,19 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             flat(s);
             store_state<HC>(to, s, row, rows, half * HC, a.Dk);
         } else {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) y[e] = pair(0.f);
-            for (int c = first > last ? first : last; c < end; ++c) {
-                const int t = c * kTok + 32 * half;
-                if (real && t < a.L) store_row<T>((T *)a.dv, vrow + t, a.L, a.L - t, 0, y);
-            }
             if (a.ds0 && segment == 0) {
                 float s[HC];
                 flat(s);
                 store_state<HC>(a.ds0 + bh * states, s, row, a.Dv, half * HC, a.Dk);
             }
-            if (stored && tid == 0) tma_wait_all0();
         }
         tmem_fence_before_sync();
     }
     __syncthreads();
-    if (ws.gave_up && tid == 0)                              // copies on their way end before the memory they go to is another CTA's
+    if (ws.gave_up && tid == 0) {                            // copies on their way end before the memory they go to is another CTA's
+        atomicExch(&hn_delta_backward_status, 1);
         for (int s = 0; s < C::STAGES; ++s) mbar_wait(&ws.full[s], 0);
+    }
     if (warp == 0) tmem_dealloc(tb, 512);
 }
 
@@ -707,6 +741,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
     }
     tmem_fence_before_sync();
     __syncthreads();
+    if (ws.gave_up && tid == 0) atomicExch(&hn_delta_backward_status, 1);
     if (warp == 0) tmem_dealloc(tb, 512);
 }
 
