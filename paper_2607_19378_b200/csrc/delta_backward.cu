@@ -344,49 +344,61 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
     using C = Grads<T, KD>;
     constexpr int PI = C::PI, PM = C::PM, HC = KD / 4;
     extern __shared__ __align__(1024) unsigned char raw[];
-    __shared__ WalkShared ws;                                // bar_a: products, full[0]: a head's inputs, full[1]: the gradient behind the chunk
-    __shared__ __align__(16) float gates[kGates];
-    __shared__ float sums[3][4][kTok], erased[4][kTok], total[16];
-    const float *gamma = gates, *delta = gates + kTok, *beta = gates + 2 * kTok, *ghi = gates + 4 * kTok, *glo = gates + 5 * kTok;
+    // bar_a, bar_b: products; full[0]: a unit's k, q, v, A, gates; full[1]: the gradient behind the chunk; full[2]: dY, the state before it
+    __shared__ WalkShared ws;
+    __shared__ __align__(16) float gates2[2][kGates];
+    __shared__ float sums[2][4][kTok], erased[4][kTok], total[16], writes[16];
     unsigned char *sm = align_images(raw);
-    const int tid = threadIdx.x, lane = tid & 31, warp = uniform_warp(tid >> 5), row = 32 * (warp & 3) + lane, quarter = warp >> 2, share = a.H / a.Hk;
-    const long long bk = blockIdx.x / a.chunks;
-    const int chunk = (int)(blockIdx.x % a.chunks), b = (int)(bk / a.Hk), hk = (int)(bk % a.Hk), t0 = chunk * kTok, t = t0 + 16 * quarter;
-    pdl_wait();
-    const int n = live_tokens(a, b), nv = n - t0 < kTok ? n - t0 : kTok, room = a.L - t0 < kTok ? a.L - t0 : kTok, rows8 = kept_rows(a.Dv);
-    const long long qrow = (bk * a.Dk + row) * a.L + t, qk = bk * a.Dk * a.L + t0, all = (long long)a.B * a.Hk * a.Dk * a.L, vall = (long long)a.B * a.H * a.Dv * a.L;
-    const long long kept = kept_floats(a.Dv, a.Dk);
-    if (nv <= 0) {                                           // nothing of this chunk counts
-        const float none[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        for (int g = 0; g < 16; g += 8)
-            if (row < a.Dk && t + g < a.L) {
-                store8<T>((T *)a.dq, qrow + g, a.L, a.L - t - g, 0, none);
-                store8<T>((T *)a.dk, qrow + g, a.L, a.L - t - g, 0, none);
-            }
-        for (int i = tid; i < share * room; i += kGradThreads) {
-            const long long at = (((long long)b * a.H + hk * share + i / room) * a.L) + t0 + i % room;
-            HN_G(a.dbeta + at, 4);
-            a.dbeta[at] = 0.f;
-            if (a.dg) { HN_G(a.dg + at, 4); a.dg[at] = 0.f; }
+    const int tid = threadIdx.x, lane = tid & 31, warp = uniform_warp(tid >> 5), row = 32 * (warp & 3) + lane, quarter = warp >> 2, share = a.H / a.Hk, c0 = 16 * quarter;
+    const int rows8 = kept_rows(a.Dv), ksteps = (a.Dk + 15) / 16, vsteps = (a.Dv + 15) / 16;
+    const long long all = (long long)a.B * a.Hk * a.Dk * a.L, vall = (long long)a.B * a.H * a.Dv * a.L, kept = kept_floats(a.Dv, a.Dk);
+    const unsigned images = smem_u32(sm), IK = images + C::K, IU = images + C::U, IZ = images + C::DZ, IA = images + C::A, IY = images + C::DY, IQ = images + C::Q;
+    // a unit: a chunk of a head of queries and keys, and one of the value heads that share it
+    struct Unit { long long bk; int chunk, b, j, n, nv; };
+    const long long items = (long long)a.B * a.Hk * a.chunks;
+    auto unit = [&](long long item, int j) {
+        Unit u;
+        u.bk = item / a.chunks; u.chunk = (int)(item % a.chunks); u.b = (int)(u.bk / a.Hk); u.j = j;
+        u.n = live_tokens(a, u.b);
+        u.nv = u.n - u.chunk * kTok < kTok ? u.n - u.chunk * kTok : kTok;
+        return u;
+    };
+    auto head = [&](const Unit &u) { return (long long)u.b * a.H + (u.bk % a.Hk) * share + u.j; };
+    // the copies of a unit, in two parts: what can come while the unit before is still at its products, and the rest
+    auto copy_early = [&](const Unit &u) {
+        const long long bh = head(u), at = bh * a.chunks + u.chunk;
+        const bool copied = by_copy(a, u.nv, u.chunk * kTok);
+        mbar_expect_tx(&ws.full[2], (C::ROOM ? (unsigned)(kept * 4) : 0) + (copied ? C::TILE : 0));
+        if (copied) tma_load_3d(sm + C::DY, &maps.v, &ws.full[2], u.chunk * kTok, 0, (int)bh);
+        if (C::ROOM) bulk_load(sm + C::STATE, a.marks + at * kept, (unsigned)(kept * 4), &ws.full[2]);
+    };
+    auto copy_rest = [&](const Unit &u, int which) {
+        const long long bh = head(u), at = bh * a.chunks + u.chunk;
+        const bool copied = by_copy(a, u.nv, u.chunk * kTok);
+        mbar_expect_tx(&ws.full[0], PM * kMatrix + kGates * 4 + (copied ? (u.j ? 1 : 3) * C::TILE : 0));
+        if (copied) {
+            if (!u.j) tma_load_3d(sm + C::K, &maps.k, &ws.full[0], u.chunk * kTok, 0, (int)u.bk);
+            tma_load_3d(sm + C::U, &maps.more, &ws.full[0], u.chunk * kTok, 0, (int)bh);
+            if (!u.j) tma_load_3d(sm + C::Q, &maps.q, &ws.full[0], u.chunk * kTok, 0, (int)u.bk);
         }
-        return;
-    }
-    const bool copied = by_copy(a, nv, t0);
+        bulk_load(gates2[which], a.gates + at * kGates, kGates * 4, &ws.full[0]);
+        bulk_load(sm + C::A, a.images + at * (2 * PM * kMatrix), PM * kMatrix, &ws.full[0]);
+    };
+    pdl_wait();
     if (tid == 0) {
-        mbar_init(&ws.bar_a, 1); mbar_init(&ws.bar_b, 1); mbar_init(&ws.full[0], 1); mbar_init(&ws.full[1], 1);
+        mbar_init(&ws.bar_a, 1); mbar_init(&ws.bar_b, 1); mbar_init(&ws.full[0], 1); mbar_init(&ws.full[1], 1); mbar_init(&ws.full[2], 1);
         ws.gave_up = 0;
         fence_mbar_init();
     }
     __syncwarp();
     if (warp == 0) tmem_alloc(smem_u32(&ws.slot), 512);
-    const int ksteps = (a.Dk + 15) / 16, vsteps = (a.Dv + 15) / 16;
-    const unsigned images = smem_u32(sm), IK = images + C::K, IU = images + C::U, IZ = images + C::DZ, IA = images + C::A, IY = images + C::DY, IQ = images + C::Q;
-    unsigned par = 0, tb = 0;
+    tmem_fence_before_sync();
+    __syncthreads();
+    tmem_fence_after_sync();
+    const unsigned tb = ws.slot;
+    const unsigned lane_s = tmem_addr(tb, warp, C::S0 + quarter * (HC / 2)), lane_r = tmem_addr(tb, warp, c0);
+    unsigned par = 0;
     float dq[2][8], dk[2][8];
-#pragma unroll
-    for (int g = 0; g < 2; ++g)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) dq[g][e] = dk[g][e] = 0.f;
     auto go = [&] {                                          // what the threads wrote, for the products
         tmem_wait_st();
         fence_async_smem();
@@ -399,31 +411,59 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
         par ^= 1;
         tmem_fence_after_sync();
     };
-    for (int j = 0; j < share; ++j) {
-        const long long bh = (long long)b * a.H + hk * share + j, at = bh * a.chunks + chunk, grow = bh * a.L + t0;
-        const float *S = a.marks + at * kept, *D = a.dstates + at * kept;
-        if (j) {                                             // the images, sums and tensor memory of the head before have been read
-            fence_async_smem();
-            tmem_fence_before_sync();
-            __syncthreads();
-        }
-        if (tid == 0) {
-            mbar_expect_tx(&ws.full[0], PM * kMatrix + kGates * 4 + (C::ROOM ? (unsigned)(kept * 4) : 0) + (copied ? (j ? 2 : 4) * C::TILE : 0));
-            if (copied) {
-                if (!j) tma_load_3d(sm + C::K, &maps.k, &ws.full[0], t0, 0, (int)bk);
-                tma_load_3d(sm + C::U, &maps.more, &ws.full[0], t0, 0, (int)bh);
-                tma_load_3d(sm + C::DY, &maps.v, &ws.full[0], t0, 0, (int)bh);
-                if (!j) tma_load_3d(sm + C::Q, &maps.q, &ws.full[0], t0, 0, (int)bk);
+    // the units of this CTA that hold tokens, one after the other; chunks without any are zeroed as they come
+    long long item = (long long)blockIdx.x - gridDim.x;
+    int j = share - 1;
+    auto next = [&](Unit &u) {
+        for (;;) {
+            if (++j >= share) {
+                j = 0;
+                item += gridDim.x;
+                if (item >= items) return false;
             }
-            if (C::ROOM) bulk_load(sm + C::STATE, S, (unsigned)(kept * 4), &ws.full[0]);
-            bulk_load(gates, a.gates + at * kGates, kGates * 4, &ws.full[0]);
-            bulk_load(sm + C::A, a.images + at * (2 * PM * kMatrix), PM * kMatrix, &ws.full[0]);
+            u = unit(item, j);
+            if (u.nv > 0) return true;
+            const int t = u.chunk * kTok, room = a.L - t < kTok ? a.L - t : kTok;
+            const long long qrow = (u.bk * a.Dk + row) * a.L + t + c0;
+            const float none[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+            for (int g = 0; g < 16; g += 8)
+                if (row < a.Dk && c0 + g < room) {
+                    store8<T>((T *)a.dq, qrow + g, a.L, room - c0 - g, 0, none);
+                    store8<T>((T *)a.dk, qrow + g, a.L, room - c0 - g, 0, none);
+                }
+            for (int i = tid; i < share * room; i += kGradThreads) {
+                const long long at = (((long long)u.b * a.H + (u.bk % a.Hk) * share + i / room) * a.L) + t + i % room;
+                HN_G(a.dbeta + at, 4);
+                a.dbeta[at] = 0.f;
+                if (a.dg) { HN_G(a.dg + at, 4); a.dg[at] = 0.f; }
+            }
+            j = share - 1;                                   // (the other heads of the chunk are done with)
         }
-        __syncwarp();
+    };
+    Unit now, then;
+    bool more = next(now);
+    if (more && tid == 0) { copy_early(now); copy_rest(now, 0); }
+    __syncwarp();
+    for (unsigned step = 0; more; ++step, now = then) {
+        const unsigned phase = step & 1;
+        const int t0 = now.chunk * kTok, nv = now.nv, room = a.L - t0 < kTok ? a.L - t0 : kTok, t = t0 + c0;
+        const long long bh = head(now), at = bh * a.chunks + now.chunk, grow = bh * a.L + t0, qk = now.bk * a.Dk * a.L + t0;
+        const float *S = a.marks + at * kept, *D = a.dstates + at * kept;
+        const float *gates = gates2[phase], *gamma = gates, *delta = gates + kTok, *beta = gates + 2 * kTok, *ghi = gates + 4 * kTok, *glo = gates + 5 * kTok;
+        const bool copied = by_copy(a, nv, t0), first = now.j == 0, last = now.j == share - 1;
+        more = next(then);
+        if (first) {
+#pragma unroll
+            for (int g = 0; g < 2; ++g)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) dq[g][e] = dk[g][e] = 0.f;
+        }
         if (!copied) {
+            __syncthreads();                                 // (the results of the unit before have left U's place: their thread has waited)
             load_tile<T>(sm + C::DY, C::TILE, (const T *)a.dy, bh * a.Dv * a.L + t0, vall, a.L, a.Dv, nv, tid, kGradThreads);
             clear_rows(sm + C::DY, C::TILE, PI, a.Dv, KD, tid, kGradThreads);
-            if (!j) {
+            if (first) {
                 load_tile<T>(sm + C::K, C::TILE, (const T *)a.k, qk, all, a.L, a.Dk, nv, tid, kGradThreads);
                 clear_rows(sm + C::K, C::TILE, PI, a.Dk, KD, tid, kGradThreads);
                 if (C::ROOM) {
@@ -435,24 +475,20 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
         }
         {   // dZ as an image
             const float4 *from = (const float4 *)a.dz + (at * 16 + 4 * quarter) * rows8 + row;
+            float4 w[4];
 #pragma unroll
-            for (int g = 0; g < 2; ++g) {
-                float x[8];
-#pragma unroll
-                for (int e = 0; e < 8; e += 4) {
-                    float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
-                    if (row < rows8) { HN_G(from + (2 * g + e / 4) * rows8, 16); w = from[(2 * g + e / 4) * rows8]; }
-                    x[e] = w.x; x[e + 1] = w.y; x[e + 2] = w.z; x[e + 3] = w.w;
-                }
-                if (row < KD) planes8_to_image<PM>(sm + C::DZ, C::TILE, row, 2 * quarter + g, x);
+            for (int e = 0; e < 4; ++e) {
+                w[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (row < rows8) { HN_G(from + e * rows8, 16); w[e] = from[e * rows8]; }
             }
+            if (row < KD)
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                    const float x[8] = {w[2 * g].x, w[2 * g].y, w[2 * g].z, w[2 * g].w, w[2 * g + 1].x, w[2 * g + 1].y, w[2 * g + 1].z, w[2 * g + 1].w};
+                    planes8_to_image<PM>(sm + C::DZ, C::TILE, row, 2 * quarter + g, x);
+                }
         }
-        tmem_fence_before_sync();
-        __syncthreads();                                     // (tensor memory and its barrier are there)
-        tmem_fence_after_sync();
-        WAIT(&ws.full[0], j & 1);
-        tb = ws.slot;
-        const unsigned lane_s = tmem_addr(tb, warp, C::S0 + quarter * (HC / 2)), lane_r = tmem_addr(tb, warp, quarter * 16);
+        WAIT(&ws.full[2], phase);
         const float4 *held = C::ROOM ? (const float4 *)(sm + C::STATE) : nullptr;
         // the state before the chunk, its rows as lanes: S0 k
 #pragma unroll 1
@@ -471,6 +507,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
             }
             planes8_to_tmem<PM>(lane_s + e / 2, KD / 2, s);
         }
+        WAIT(&ws.full[0], phase);
         go();
         if (warp == 0) {
             issue_ts<PM, PI, PM, true, KD / 16, B_ALL, 4>(tb + C::R0, tb + C::S0, KD / 2, IK, C::TILE, ksteps, kTok, false);
@@ -481,19 +518,24 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
         done();
 #pragma unroll 1
         for (int g = 0; g < 2; ++g) {                        // R, Z and what dZ R says about beta
-            const int c = 16 * quarter + 8 * g;
-            float x[8], v[8], z[8];
+            const int c = c0 + 8 * g;
+            f2 x[4], ga[4], be[4];
+            float v[8], z[8];
             tmem_ld8(x, lane_r + C::R0 + 8 * g);
+            shared8(ga, gamma + c);
+            shared8(be, beta + c);
             if (row < KD) {
                 image8<PI>(v, sm + C::U, C::TILE, row, c >> 3);
                 image8<PM>(z, sm + C::DZ, C::TILE, row, c >> 3);
             }
             tmem_wait_ld();
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                x[e] = row < a.Dv ? fmaf(-gamma[c + e], x[e], v[e]) : 0.f;
-                z[e] = row < a.Dv ? z[e] * x[e] : 0.f;
-                x[e] *= beta[c + e];
+            for (int e = 0; e < 4; ++e) {
+                x[e] = row < a.Dv ? fma2(mul2(ga[e], pair(-1.f)), x[e], make2(v[2 * e], v[2 * e + 1])) : pair(0.f);
+                const f2 zr = mul2(make2(z[2 * e], z[2 * e + 1]), x[e]);
+                z[2 * e] = row < a.Dv ? zr.x : 0.f;
+                z[2 * e + 1] = row < a.Dv ? zr.y : 0.f;
+                x[e] = mul2(x[e], be[e]);
             }
             planes8_to_tmem<PM>(tmem_addr(tb, warp, C::R1 + quarter * 8 + 4 * g), kTok / 2, x);
             const float sum = column_sum8(z, lane);
@@ -571,8 +613,8 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
             umma_commit(&ws.bar_a);
         }
         // the gradient behind the chunk in the state's place, while those are formed
-        if (C::ROOM) WAIT(&ws.full[1], j & 1);
-        WAIT(&ws.bar_b, 0);                                  // (two phases a head)
+        if (C::ROOM) WAIT(&ws.full[1], phase);
+        WAIT(&ws.bar_b, 0);                                  // (two phases a unit)
         tmem_fence_after_sync();
         float inner = columns(D, true);
 #pragma unroll
@@ -584,40 +626,48 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
             umma_commit(&ws.bar_b);
         }
         done();
+        if (C::ROOM && more && tid == 0) copy_early(then);   // (dY and the state's place are free: their products are through, every thread has read)
+        __syncwarp();
         {   // F and E in the lower triangles, where their lanes' rows are tokens
             const int i = row & 63;
-            const float Hi = ghi[i], Li = glo[i], bi = beta[i];
+            const float Hi = ghi[i], Li = glo[i], bi = -beta[i];
             float own = 0.f;
 #pragma unroll 1
             for (int g = 0; g < 2; ++g) {
-                const int c0 = 16 * quarter + 8 * g;
+                const int c = c0 + 8 * g;
                 float x[8], y[8], z[8];
+                f2 hj[4], lj[4], ga[4], be[4];
                 tmem_ld8(x, lane_r + C::R1 + 8 * g);
                 tmem_ld8(y, lane_r + C::R2 + 8 * g);
                 if (C::REST) tmem_ld8(z, lane_r + C::R0 + 8 * g);
+                shared8(hj, ghi + c);
+                shared8(lj, glo + c);
                 tmem_wait_ld();
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const int c = c0 + e;
-                    const float r = ratio(Hi, Li, ghi[c], glo[c]);
+                    const float r = ratio(Hi, Li, e & 1 ? hj[e / 2].y : hj[e / 2].x, e & 1 ? lj[e / 2].y : lj[e / 2].x);
                     if (warp & 2) {
                         if (C::REST) x[e] += z[e];
-                        own += c < i ? x[e] * r * y[e] : 0.f;
-                        x[e] = c < i ? -bi * r * x[e] : 0.f;
-                    } else x[e] = c <= i ? r * x[e] : 0.f;
+                        x[e] = c + e < i ? r * x[e] : 0.f;
+                        own = c + e < i ? fmaf(x[e], y[e], own) : own;
+                        x[e] *= bi;
+                    } else x[e] = c + e <= i ? r * x[e] : 0.f;
                 }
-                planes8_to_image<PM>(sm + (warp & 2 ? C::DZ : C::A), kMatrix, i, c0 >> 3, x);
+                planes8_to_image<PM>(sm + (warp & 2 ? C::DZ : C::A), kMatrix, i, c >> 3, x);
                 // dQ and the erased part of dK, as far as they come from the state: F k and E k are added to them
-                tmem_ld8(x, lane_r + C::R4 + 8 * g);
-                tmem_ld8(y, lane_r + C::R3 + 8 * g);
+                f2 p[4], q[4];
+                tmem_ld8(p, lane_r + C::R4 + 8 * g);
+                tmem_ld8(q, lane_r + C::R3 + 8 * g);
+                shared8(ga, gamma + c);
+                shared8(be, gates + 3 * kTok + c);
                 tmem_wait_ld();
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    x[e] *= gamma[c0 + e];
-                    y[e] *= -gamma[c0 + e] * beta[c0 + e];
+                for (int e = 0; e < 4; ++e) {
+                    p[e] = mul2(p[e], ga[e]);
+                    q[e] = mul2(q[e], be[e]);
                 }
-                tmem_st8(lane_r + C::R4 + 8 * g, x);
-                tmem_st8(lane_r + C::R3 + 8 * g, y);
+                tmem_st8(lane_r + C::R4 + 8 * g, p);
+                tmem_st8(lane_r + C::R3 + 8 * g, q);
             }
             if (warp & 2) erased[quarter][i] = own;
         }
@@ -634,15 +684,18 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
             umma_commit(&ws.bar_a);
         }
         done();
+        float written = 0.f;
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
-            const int c = 16 * quarter + 8 * g;
+            const int c = c0 + 8 * g;
             const bool in = row < a.Dk;                      // (a lane without a channel holds whatever lay behind an image)
             float x[8], y[8], z[8], w[8], u[8];
+            f2 de[4];
             tmem_ld8(x, lane_r + C::R4 + 8 * g);             // dQ of this head
             tmem_ld8(y, lane_r + C::R3 + 8 * g);
             tmem_ld8(w, lane_r + C::R2 + 8 * g);
             tmem_ld8(u, lane_r + C::R5 + 8 * g);
+            shared8(de, delta + c);
             if (row < KD) image8<PI>(z, sm + C::Q, C::TILE, row, c >> 3);
             tmem_wait_ld();
 #pragma unroll
@@ -653,51 +706,68 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
             if (row < KD) image8<PI>(z, sm + C::K, C::TILE, row, c >> 3);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                u[e] *= delta[c + e];
+                u[e] *= e & 1 ? de[e / 2].y : de[e / 2].x;
                 w[e] += u[e];
                 dk[g][e] += y[e] + w[e];
                 x[e] = in ? fmaf(z[e], y[e] - w[e], x[e]) : 0.f;
-                u[e] = in ? u[e] * z[e] : 0.f;
+                written = in ? fmaf(u[e], z[e], written) : 0.f;
             }
-            const float s1 = column_sum8(x, lane), s2 = column_sum8(u, lane);
-            if (!(lane & 3)) {
-                sums[1][warp & 3][c + (lane >> 2)] = s1;
-                sums[2][warp & 3][c + (lane >> 2)] = s2;
+            const float sum = column_sum8(x, lane);
+            if (!(lane & 3)) sums[1][warp & 3][c + (lane >> 2)] = sum;
+            if (last) {                                      // U is through: the results into its place
+                if (C::ROOM && a.copies) {
+                    if (row < KD) {
+                        *(uint4 *)(sm + C::U + image_at(row, 2 * quarter + g)) = bf16_8(dq[g], now.n - t - 8 * g);
+                        *(uint4 *)(sm + C::U + C::TILE + image_at(row, 2 * quarter + g)) = bf16_8(dk[g], now.n - t - 8 * g);
+                    }
+                } else if (in && t + 8 * g < a.L) {
+                    const long long to = (now.bk * a.Dk + row) * a.L + t + 8 * g;
+                    store8<T>((T *)a.dq, to, a.L, a.L - t - 8 * g, now.n - t - 8 * g, dq[g]);
+                    store8<T>((T *)a.dk, to, a.L, a.L - t - 8 * g, now.n - t - 8 * g, dk[g]);
+                }
             }
         }
-        __syncthreads();
+#pragma unroll
+        for (int m = 1; m < 32; m <<= 1) written += __shfl_xor_sync(~0u, written, m);
+        if (lane == 0) writes[warp] = written;
+        fence_async_smem();
+        tmem_fence_before_sync();
+        __syncthreads();                                     // images, sums and tensor memory have been read, results written
+        tmem_fence_after_sync();
+        if (tid == 128) {
+            if (last && C::ROOM && a.copies) {
+                tma_store_3d(&maps.out, sm + C::U, t0, 0, (int)now.bk);
+                tma_store_3d(&maps.outk, sm + C::U + C::TILE, t0, 0, (int)now.bk);
+                tma_commit();
+                tma_wait_read0();
+            }
+            if (more) {
+                if (!C::ROOM) copy_early(then);
+                copy_rest(then, phase ^ 1);
+            }
+        }
+        __syncwarp();
         if (warp < 2) {                                      // two tokens a lane of warp 0: sums from the chunk's end; warp 1: beta
             float s[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int i = 2 * lane + e;
-                float v = 0.f;
-                if (warp == 0) {
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) v += sums[1][w][i];
-                } else {
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) v += sums[0][w][i];
-                    v -= (erased[0][i] + erased[1][i]) + (erased[2][i] + erased[3][i]);
-                }
-                s[e] = v;
+                s[e] = (sums[1 - warp][0][i] + sums[1 - warp][1][i]) + (sums[1 - warp][2][i] + sums[1 - warp][3][i]);
+                if (warp) s[e] -= (erased[0][i] + erased[1][i]) + (erased[2][i] + erased[3][i]);
             }
             if (warp == 0) {
-                float written = 0.f, in = 0.f;
+                float w = lane < 16 ? fmaf(gamma[kTok - 1], total[lane], writes[lane]) : 0.f;
 #pragma unroll
-                for (int w = 0; w < 4; ++w) written += sums[2][w][2 * lane] + sums[2][w][2 * lane + 1];
-#pragma unroll
-                for (int m = 1; m < 32; m <<= 1) written += __shfl_xor_sync(~0u, written, m);
-#pragma unroll
-                for (int w = 0; w < 16; ++w) in += total[w];
-                double v = (double)s[0] + s[1];
+                for (int m = 1; m < 16; m <<= 1) w += __shfl_xor_sync(~0u, w, m);
+                w = __shfl_sync(~0u, w, 0);
+                const double v = (double)s[0] + s[1];
                 double run = v;                              // (sums of many signs: in 64 bits)
 #pragma unroll
                 for (int m = 1; m < 32; m <<= 1) {
                     const double o = __shfl_down_sync(~0u, run, m);
                     if (lane + m < 32) run += o;
                 }
-                run += (double)gamma[kTok - 1] * in + written;
+                run += w;
                 s[0] = (float)run;
                 s[1] = (float)(run - (v - s[1]));
             }
@@ -715,33 +785,12 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
             }
         }
     }
-    if (C::ROOM && a.copies) {                               // U is through: the results into its place, and away by copies
-        if (row < KD) {
-#pragma unroll
-            for (int g = 0; g < 2; ++g) {
-                *(uint4 *)(sm + C::U + image_at(row, 2 * quarter + g)) = bf16_8(dq[g], n - t - 8 * g);
-                *(uint4 *)(sm + C::U + C::TILE + image_at(row, 2 * quarter + g)) = bf16_8(dk[g], n - t - 8 * g);
-            }
-        }
-        fence_async_smem();
-        __syncthreads();
-        if (tid == 0) {
-            tma_store_3d(&maps.out, sm + C::U, t0, 0, (int)bk);
-            tma_store_3d(&maps.outk, sm + C::U + C::TILE, t0, 0, (int)bk);
-            tma_commit();
-            tma_wait_all0();
-        }
-    } else if (row < a.Dk) {
-#pragma unroll
-        for (int g = 0; g < 2; ++g)
-            if (t + 8 * g < a.L) {
-                store8<T>((T *)a.dq, qrow + 8 * g, a.L, a.L - t - 8 * g, n - t - 8 * g, dq[g]);
-                store8<T>((T *)a.dk, qrow + 8 * g, a.L, a.L - t - 8 * g, n - t - 8 * g, dk[g]);
-            }
-    }
     tmem_fence_before_sync();
     __syncthreads();
-    if (ws.gave_up && tid == 0) atomicExch(&hn_delta_backward_status, 1);
+    if (ws.gave_up && tid == 0) {                            // copies on their way end before the memory they go to is another CTA's
+        atomicExch(&hn_delta_backward_status, 1);
+        for (int s = 0; s < 3; ++s) mbar_wait(&ws.full[s], 0);
+    }
     if (warp == 0) tmem_dealloc(tb, 512);
 }
 
@@ -764,7 +813,8 @@ template <typename T, int KD> static int launch_back(DeltaArgs a, cudaStream_t s
     }
     if (const int e = launch_delta<delta_walk_back_kernel<T, KD, WALK_RUN>>(a, blocks, kWalkThreads, WalkBack<T, KD>::BYTES, st, m)) return e;
     a.copies = delta_maps<T>(m, a, KD, a.dy, a.dq, a.dk);
-    return launch_delta<delta_gradients_kernel<T, KD>>(a, (long long)a.B * a.Hk * a.chunks, kGradThreads, Grads<T, KD>::BYTES, st, m);
+    const long long items = (long long)a.B * a.Hk * a.chunks;
+    return launch_delta<delta_gradients_kernel<T, KD>>(a, items < kSms ? items : kSms, kGradThreads, Grads<T, KD>::BYTES, st, m);
 }
 int launch_delta_backward(const DeltaArgs &a, int dtype, cudaStream_t st)
 {
