@@ -6,15 +6,18 @@
 // t = p_a base^(-j / s_a) for the j-th of the s_a pairs of axis a, p_a the token's place on it.  Gradient: dn is dy turned back,
 //     dg = sum dn x^,   dx = rho (e - x^ (e . x^) / D)  (rms; l2: without the division; none: e),   e = dn g.
 //
-// Each tensor is read and written once: bandwidth is the bound.  Tokens are the contiguous axis, so a CTA takes a tile of 128 bytes of
-// tokens and walks the heads and batch entries on it; a head's channels are spread over R groups of eight lanes (a lane holds 16 bytes of
-// tokens of both channels of a pair), its sums go by shuffles and, beyond a warp, through shared memory.  The tile's sines and cosines
-// are formed once for all heads: angles as turns in 64 bits (in 32 a position of 100000 keeps two digits), reduced to half a
-// turn and rounded, so that an error stays below 2e-7 at any position.  A grid of fewer than eight tokens (generation) goes to a warp
-// per token and head.
+// Each tensor is read and written once: bandwidth is the bound, instructions the next one.  Tokens are the contiguous axis, so a CTA takes a
+// tile of 128 bytes of tokens and walks the heads and batch entries on it; a head's channels are spread over R groups of eight lanes (a
+// lane holds 16 bytes of tokens of both channels of a pair), its sums go by shuffles and, beyond a warp, through shared memory.
+// The tile's sines and cosines are formed once for all heads: angles as turns in 64 bits (in 32 a position of 100000 keeps two digits),
+// reduced to half a turn and rounded.  On the grid's own positions few of them are: along the last axis a tile's first position
+// turned on by those of 0, 1, 2 .. (kept for all tiles), along the others one for each row of the grid in the tile.  An error stays
+// below 2e-7 at any position.  A grid of fewer than eight tokens (generation) goes to a warp per token and head.
 #include <math.h>
 
 #include "entry.cuh"
+#include "octet.cuh"
+#include "pair.cuh"
 
 namespace hn {
 
@@ -26,9 +29,9 @@ struct HeadsArgs {
     void *out[2];
     const float *g[2];
     const int *positions;                    // [B][N][T], or the grid's
-    float *part;                             // [blocks of q, then of k][D]: sums of the weights' gradients
+    float *part;                             // [blocks][2][D]: sums of the weights' gradients
     float *dg[2];
-    int H[2], splits[2];
+    int H[2], splits;
     int B, D, T, ndim, dims[kMaxAxes], axes[kMaxAxes], turned;
     int tiles, norm;
     float eps, per_mean;                     // 1/D, or 1: what a sum over channels counts
@@ -67,231 +70,321 @@ template <typename T> struct Tile {
     static constexpr int V = 16 / sizeof(T), TOKENS = 8 * V;
 };
 
-// The V tokens of a lane in one row: side by side as one vector, or (rows that do not start on 16 bytes) every eighth token, so that
-// the eight lanes of a row share a sector
-template <typename T, bool VEC> __device__ __forceinline__ void load_tokens(float (&v)[Tile<T>::V], const T *row, int t0, int vc, int T_)
+// The V tokens of a lane in one row, in pairs: side by side as one vector, or (rows that do not start on 16 bytes) every eighth token, so
+// that the eight lanes of a row share a sector
+template <typename T, bool VEC> __device__ __forceinline__ void load_tokens(f2 (&v)[Tile<T>::V / 2], const T *row, int t0, int vc, int T_)
 {
     constexpr int V = Tile<T>::V;
     if constexpr (VEC) {
         uint4 w = make_uint4(0, 0, 0, 0);
         const int t = t0 + vc * V;
         if (t < T_) { HN_G(row + t, 16); w = __ldg((const uint4 *)(row + t)); }
-        const T *e = (const T *)&w;
+        const unsigned u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = (float)e[i];
+        for (int i = 0; i < V / 2; ++i) v[i] = sizeof(T) == 2 ? widen2(u[i]) : make2(__uint_as_float(u[2 * i & 3]), __uint_as_float(u[(2 * i + 1) & 3]));
     } else {
+        float x[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = t0 + i * 8 + vc < T_ ? IO<T>::ld(row, t0 + i * 8 + vc) : 0.f;
+        for (int i = 0; i < V; ++i) x[i] = t0 + i * 8 + vc < T_ ? IO<T>::ld(row, t0 + i * 8 + vc) : 0.f;
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) v[i] = make2(x[2 * i], x[2 * i + 1]);
     }
 }
-template <typename T, bool VEC> __device__ __forceinline__ void store_tokens(T *row, const float (&v)[Tile<T>::V], int t0, int vc, int T_)
+template <typename T, bool VEC> __device__ __forceinline__ void store_tokens(T *row, const f2 (&v)[Tile<T>::V / 2], int t0, int vc, int T_)
 {
     constexpr int V = Tile<T>::V;
     if constexpr (VEC) {
         const int t = t0 + vc * V;
         uint4 w;
-        T *e = (T *)&w;
-#pragma unroll
-        for (int i = 0; i < V; ++i) e[i] = (T)v[i];
+        if constexpr (sizeof(T) == 2) w = make_uint4(narrow2(v[0]), narrow2(v[1]), narrow2(v[V / 2 - 2]), narrow2(v[V / 2 - 1]));
+        else w = make_uint4(__float_as_uint(v[0].x), __float_as_uint(v[0].y), __float_as_uint(v[1].x), __float_as_uint(v[1].y));
         if (t < T_) { HN_G(row + t, 16); *(uint4 *)(row + t) = w; }
     } else {
 #pragma unroll
         for (int i = 0; i < V; ++i)
-            if (t0 + i * 8 + vc < T_) IO<T>::st(row, t0 + i * 8 + vc, v[i]);
+            if (t0 + i * 8 + vc < T_) IO<T>::st(row, t0 + i * 8 + vc, i & 1 ? v[i / 2].y : v[i / 2].x);
+    }
+}
+
+// where a lane's token e of a table's row lies: vectors of four, lane after lane
+__device__ __forceinline__ int table_at(int lane, int element) { return (element / 4 * 8 + lane) * 4 + element % 4; }
+template <typename T, bool VEC> __device__ __forceinline__ int token_at(int e) { return VEC ? table_at(e / Tile<T>::V, e % Tile<T>::V) : table_at(e % 8, e / 8); }
+
+// The tile's table: cosines and sines [pair][token_at].  `steps`: the same of the positions 0 .. TOKENS - 1 for the pairs of the last axis,
+// formed before; `rows`: room for rows_of_tile() rotors a pair.
+__host__ __device__ __forceinline__ int rows_of_tile(int tokens, int last) { return last >= tokens ? 2 : (tokens - 1) / last + 2; }
+template <typename T, bool VEC> __device__ __forceinline__ void fill_table(const HeadsArgs &a, int b, int t0, float *cs, float *sn, const float *step_c, const float *step_s, float2 *rows, const double *freq, const int *axis_of, int tid)
+{
+    constexpr int V = Tile<T>::V, TOKENS = Tile<T>::TOKENS;
+    if (a.positions) {
+        for (int i = tid; i < a.turned * TOKENS; i += 256) {
+            const int pr = i / TOKENS, e = i % TOKENS;
+            const float2 c = t0 + e < a.T ? rotor(place(a, b, axis_of[pr], t0 + e), freq[pr]) : make_float2(1.f, 0.f);
+            cs[pr * TOKENS + token_at<T, VEC>(e)] = c.x;
+            sn[pr * TOKENS + token_at<T, VEC>(e)] = c.y;
+        }
+        return;
+    }
+    // rotors of the rows of the grid that the tile touches (of the last axis: of its first position, the other rows start at 0)
+    const int Ln = a.dims[a.ndim - 1], pitch = rows_of_tile(TOKENS, Ln), row0 = t0 / Ln, first = t0 - row0 * Ln, n = (t0 + TOKENS - 1) / Ln - row0 + 1;
+    for (int i = tid; i < a.turned * n; i += 256) {
+        const int pr = n == 1 ? i : i / n, k = n == 1 ? 0 : i % n, axis = axis_of[pr];
+        float2 c = make_float2(1.f, 0.f);
+        if (axis == a.ndim - 1) { if (k == 0) c = rotor(first, freq[pr]); }
+        else {
+            int r = row0 + k;
+            for (int m = a.ndim - 2; m > axis; --m) r /= a.dims[m];
+            c = rotor(axis ? r % a.dims[axis] : r, freq[pr]);
+        }
+        rows[pr * pitch + k] = c;
+    }
+    __syncthreads();
+    if (n == 1) {                                                  // a lane's V tokens at a time
+        for (int i = tid; i < a.turned * 8; i += 256) {
+            const int pr = i >> 3;
+            const float2 c = rows[pr * pitch];
+#pragma unroll
+            for (int e = 0; e < V; e += 4) {
+                const int at = pr * TOKENS + table_at(i & 7, e);
+                f2 x[2] = {pair(c.x), pair(c.x)}, y[2] = {pair(c.y), pair(c.y)};
+                if (axis_of[pr] == a.ndim - 1) {
+                    const float4 p = *(const float4 *)(step_c + at), q = *(const float4 *)(step_s + at);
+                    const f2 u[2] = {make2(p.x, p.y), make2(p.z, p.w)}, w[2] = {make2(q.x, q.y), make2(q.z, q.w)};
+#pragma unroll
+                    for (int m = 0; m < 2; ++m) {
+                        x[m] = fma2(pair(c.x), u[m], mul2(pair(-c.y), w[m]));
+                        y[m] = fma2(pair(c.x), w[m], mul2(pair(c.y), u[m]));
+                    }
+                }
+                *(float4 *)(cs + at) = make_float4(x[0].x, x[0].y, x[1].x, x[1].y);
+                *(float4 *)(sn + at) = make_float4(y[0].x, y[0].y, y[1].x, y[1].y);
+            }
+        }
+        return;
+    }
+    for (int i = tid; i < a.turned * TOKENS; i += 256) {
+        const int pr = i / TOKENS, e = i % TOKENS, at = pr * TOKENS + token_at<T, VEC>(e), k = (first + e) / Ln;
+        float2 c = rows[pr * pitch + k];
+        if (axis_of[pr] == a.ndim - 1) {
+            const int from = pr * TOKENS + token_at<T, VEC>(k ? first + e - k * Ln : e);
+            c = make_float2(c.x * step_c[from] - c.y * step_s[from], c.x * step_s[from] + c.y * step_c[from]);
+        }
+        cs[at] = c.x;
+        sn[at] = c.y;
     }
 }
 
 // R groups of eight lanes to a head, P pairs of channels to a lane; 32 / R heads at a time
-template <typename T, int R, int P, bool BWD, bool VEC> __global__ void __launch_bounds__(256) heads_kernel(HeadsArgs a)
+template <typename T, int R, int P, bool BWD, bool VEC> __global__ void __launch_bounds__(256, P > 2 ? 1 : BWD ? 2 : 3) heads_kernel(HeadsArgs a)
 {
-    constexpr int V = Tile<T>::V, TOKENS = Tile<T>::TOKENS, HEADS = 32 / R, WARPS = R / 4, SUMS = BWD ? 2 : 1;
+    constexpr int V = Tile<T>::V, TOKENS = Tile<T>::TOKENS, HEADS = 32 / R, WARPS = R / 4, SUMS = BWD ? 2 : 1, N = V / 2;
     extern __shared__ __align__(16) float sm[];
     __shared__ double freq[kMaxD / 2];
     __shared__ int axis_of[kMaxD / 2];
-    __shared__ float meet[2][SUMS][8][TOKENS];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, vc = lane & 7, group = warp / WARPS, r = (warp % WARPS) * 4 + (lane >> 3);
-    const int half = a.D / 2, kind = (int)blockIdx.y >= a.splits[0] ? 1 : 0, split = (int)blockIdx.y - (kind ? a.splits[0] : 0), H = a.H[kind];
-    float *cs = sm, *sn = sm + (size_t)a.turned * TOKENS;          // [pair][quarter of V][lane][4]: vectors of four without bank conflicts
+    __shared__ float weights[2][kMaxD];
+    __shared__ __align__(16) float meet[2][SUMS][8][TOKENS];       // [warp][lane of eight][V]
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, vc = lane & 7, group = warp / WARPS, r = (warp % WARPS) * 4 + (lane >> 3), half = a.D / 2;
+    float *cs = sm, *sn = cs + a.turned * TOKENS;
+    float *step_c = sn + a.turned * TOKENS, *step_s = step_c + a.turned * TOKENS;
+    float2 *rows = (float2 *)(step_s + a.turned * TOKENS);
     pdl_join();
     for (int i = tid; i < a.turned; i += 256) freq[i] = pair_frequency(a, i, &axis_of[i]);
-    float w[P][2], acc[P][2];
+    for (int i = tid; i < 2 * a.D; i += 256) {
+        const int kind = i >= a.D, c = kind ? i - a.D : i;
+        weights[kind][c] = 1.f;
+        if (a.g[kind]) { HN_G(a.g[kind] + c, 4); weights[kind][c] = __ldg(a.g[kind] + c); }
+    }
+    __syncthreads();
+    if (!a.positions)
+        for (int i = tid; i < a.turned * TOKENS; i += 256)
+            if (axis_of[i / TOKENS] == a.ndim - 1) {
+                const float2 c = rotor(i % TOKENS, freq[i / TOKENS]);
+                const int at = i / TOKENS * TOKENS + token_at<T, VEC>(i % TOKENS);
+                step_c[at] = c.x;
+                step_s[at] = c.y;
+            }
+    float acc[BWD ? 2 : 1][P][2];
 #pragma unroll
-    for (int p = 0; p < P; ++p)
+    for (int k = 0; k < (BWD ? 2 : 1); ++k)
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const int i = r + R * p;
-            w[p][s] = 1.f;
-            acc[p][s] = 0.f;
-            if (a.g[kind] && i < half) { HN_G(a.g[kind] + i + s * half, 4); w[p][s] = __ldg(a.g[kind] + i + s * half); }
-        }
-    const long long units = (long long)a.B * H, per = (units + a.splits[kind] - 1) / a.splits[kind], first = split * per, last = first + per < units ? first + per : units;
+        for (int p = 0; p < P; ++p) acc[k][p][0] = acc[k][p][1] = 0.f;
+    // units: the heads of q and k of one batch entry after the other; a split of them to a CTA
+    const int HT = a.H[0] + a.H[1];
+    const long long units = (long long)a.B * HT, per = (units + a.splits - 1) / a.splits, from = blockIdx.y * per, to = from + per < units ? from + per : units;
     int turn = 0;
     for (int tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
         const int t0 = tile * TOKENS;
-        for (long long u = first; u < last;) {
-            const long long b0 = u / H, end = a.positions && (b0 + 1) * H < last ? (b0 + 1) * H : last;
-            __syncthreads();                                       // (the table's readers are through, the frequencies are there)
-            for (int i = tid; i < a.turned * TOKENS; i += 256) {
-                const int pr = i / TOKENS, e = i % TOKENS, t = t0 + e;
-                const int ln = VEC ? e / V : e % 8, el = VEC ? e % V : e / 8, at = pr * TOKENS + (el / 4 * 8 + ln) * 4 + el % 4;
-                const float2 c = t < a.T ? rotor(place(a, (int)b0, axis_of[pr], t), freq[pr]) : make_float2(1.f, 0.f);
-                cs[at] = c.x;
-                sn[at] = c.y;
-            }
+        for (long long u = from; u < to;) {
+            const long long b0 = u / HT, end = a.positions && (b0 + 1) * HT < to ? (b0 + 1) * HT : to;
+            __syncthreads();                                       // (the table's readers are through; the steps are there)
+            fill_table<T, VEC>(a, (int)b0, t0, cs, sn, step_c, step_s, rows, freq, axis_of, tid);
             __syncthreads();
+#pragma unroll 1
             for (; u < end; u += HEADS) {
                 const long long unit = u + group;
                 const bool on = unit < end;
-                const long long at = on ? unit * a.D * (long long)a.T : 0;       // (unit = b H + h: its channels lie side by side)
-                float x[P][2][V], d[BWD ? P : 1][2][V], s1[V], s2[V];
+                const int b = (int)(unit / HT), h = (int)(unit - (long long)b * HT), kind = h >= a.H[0];
+                const long long at = on ? ((long long)b * a.H[kind] + h - (kind ? a.H[0] : 0)) * a.D * (long long)a.T : 0;
+                const T *in = (const T *)a.x[kind], *gradient = (const T *)a.dy[kind];
+                T *out = (T *)a.out[kind];
+                const float *weight = weights[kind];
+                float w[P][2];
 #pragma unroll
-                for (int e = 0; e < V; ++e) s1[e] = s2[e] = 0.f;
+                for (int p = 0; p < P; ++p)
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) w[p][s] = r + R * p < half ? weight[r + R * p + s * half] : 0.f;
+                f2 x[P][2][N], d[BWD ? P : 1][2][N], s1[N], s2[BWD ? N : 1];
+#pragma unroll
+                for (int e = 0; e < N; ++e) s1[e] = pair(0.f);
+                if constexpr (BWD)
+#pragma unroll
+                    for (int e = 0; e < N; ++e) s2[e] = pair(0.f);
 #pragma unroll
                 for (int p = 0; p < P; ++p)
 #pragma unroll
                     for (int s = 0; s < 2; ++s) {
-                        const int i = r + R * p, c = i + s * half;
-                        const int live = on && i < half ? a.T : 0;
-                        load_tokens<T, VEC>(x[p][s], (const T *)a.x[kind] + at + (long long)c * a.T, t0, vc, live);
-                        if constexpr (BWD) load_tokens<T, VEC>(d[p][s], (const T *)a.dy[kind] + at + (long long)c * a.T, t0, vc, live);
+                        const int i = r + R * p, c = i + s * half, live = on && i < half ? a.T : 0;
+                        load_tokens<T, VEC>(x[p][s], in + at + (long long)c * a.T, t0, vc, live);
+                        if constexpr (BWD) load_tokens<T, VEC>(d[p][s], gradient + at + (long long)c * a.T, t0, vc, live);
                     }
+                auto turned = [&](f2 (&lo)[N], f2 (&hi)[N], int i, float way) {
 #pragma unroll
-                for (int p = 0; p < P; ++p) {
-                    const int i = r + R * p;
-                    if constexpr (BWD) {
-                        if (i < a.turned) {
+                    for (int e = 0; e < N; e += 2) {
+                        const int at4 = i * TOKENS + (e / 2 * 8 + vc) * 4;
+                        const float4 c4 = *(const float4 *)&cs[at4], n4 = *(const float4 *)&sn[at4];
+                        const f2 c[2] = {make2(c4.x, c4.y), make2(c4.z, c4.w)}, n[2] = {make2(n4.x, n4.y), make2(n4.z, n4.w)};
 #pragma unroll
-                            for (int e4 = 0; e4 < V; e4 += 4) {
-                                const float4 c4 = *(const float4 *)&cs[i * TOKENS + (e4 / 4 * 8 + vc) * 4], n4 = *(const float4 *)&sn[i * TOKENS + (e4 / 4 * 8 + vc) * 4];
-                                const float cc[4] = {c4.x, c4.y, c4.z, c4.w}, nn[4] = {n4.x, n4.y, n4.z, n4.w};
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) {
-                                    const float lo = d[p][0][e4 + e], hi = d[p][1][e4 + e];
-                                    d[p][0][e4 + e] = lo * cc[e] + hi * nn[e];
-                                    d[p][1][e4 + e] = hi * cc[e] - lo * nn[e];
-                                }
-                            }
+                        for (int m = 0; m < 2; ++m) {
+                            const f2 l = lo[e + m], h = hi[e + m], sine = mul2(n[m], pair(way));
+                            lo[e + m] = fma2(l, c[m], mul2(mul2(h, sine), pair(-1.f)));
+                            hi[e + m] = fma2(h, c[m], mul2(l, sine));
                         }
                     }
+                };
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    if constexpr (BWD)
+                        if (r + R * p < a.turned) turned(d[p][0], d[p][1], r + R * p, -1.f);
 #pragma unroll
                     for (int s = 0; s < 2; ++s)
 #pragma unroll
-                        for (int e = 0; e < V; ++e) {
-                            s1[e] = fmaf(x[p][s][e], x[p][s][e], s1[e]);
-                            if constexpr (BWD) s2[e] = fmaf(d[p][s][e] * w[p][s], x[p][s][e], s2[e]);
+                        for (int e = 0; e < N; ++e) {
+                            s1[e] = fma2(x[p][s][e], x[p][s][e], s1[e]);
+                            if constexpr (BWD) s2[e] = fma2(mul2(d[p][s][e], pair(w[p][s])), x[p][s][e], s2[e]);
                         }
                 }
-                float rho[V];
+                f2 rho[N];
                 if (a.norm == NORM_NONE) {
 #pragma unroll
-                    for (int e = 0; e < V; ++e) { rho[e] = 1.f; s2[e] = 0.f; }
+                    for (int e = 0; e < N; ++e) rho[e] = pair(1.f);
                 } else {
+                    auto lanes = [&](f2 (&v)[N]) {
 #pragma unroll
-                    for (int e = 0; e < V; ++e)
+                        for (int e = 0; e < N; ++e)
 #pragma unroll
-                        for (int m = 8; m < 32; m <<= 1) {
-                            s1[e] += __shfl_xor_sync(~0u, s1[e], m);
-                            if constexpr (BWD) s2[e] += __shfl_xor_sync(~0u, s2[e], m);
-                        }
+                            for (int m = 8; m < 32; m <<= 1) v[e] = add2(v[e], make2(__shfl_xor_sync(~0u, v[e].x, m), __shfl_xor_sync(~0u, v[e].y, m)));
+                    };
+                    lanes(s1);
+                    if constexpr (BWD) lanes(s2);
                     if constexpr (WARPS > 1) {
-                        if (lane < 8) {
+                        auto put = [&](float *m, const f2 (&v)[N]) {
 #pragma unroll
-                            for (int e = 0; e < V; ++e) {
-                                meet[turn][0][warp][e * 8 + vc] = s1[e];
-                                if constexpr (BWD) meet[turn][SUMS - 1][warp][e * 8 + vc] = s2[e];
+                            for (int e = 0; e < N; e += 2) *(float4 *)(m + vc * V + 2 * e) = make_float4(v[e].x, v[e].y, v[e + 1].x, v[e + 1].y);
+                        };
+                        auto get = [&](const float (*m)[TOKENS], f2 (&v)[N]) {
+#pragma unroll
+                            for (int e = 0; e < N; e += 2) {
+                                v[e] = v[e + 1] = pair(0.f);
+#pragma unroll
+                                for (int k = 0; k < WARPS; ++k) {
+                                    const float4 q = *(const float4 *)&m[group * WARPS + k][vc * V + 2 * e];
+                                    v[e] = add2(v[e], make2(q.x, q.y));
+                                    v[e + 1] = add2(v[e + 1], make2(q.z, q.w));
+                                }
                             }
+                        };
+                        if (lane < 8) {
+                            put(meet[turn][0][warp], s1);
+                            if constexpr (BWD) put(meet[turn][SUMS - 1][warp], s2);
                         }
                         __syncthreads();
-#pragma unroll
-                        for (int e = 0; e < V; ++e) {
-                            s1[e] = s2[e] = 0.f;
-#pragma unroll
-                            for (int j = 0; j < WARPS; ++j) {
-                                s1[e] += meet[turn][0][group * WARPS + j][e * 8 + vc];
-                                if constexpr (BWD) s2[e] += meet[turn][SUMS - 1][group * WARPS + j][e * 8 + vc];
-                            }
-                        }
+                        get(meet[turn][0], s1);
+                        if constexpr (BWD) get(meet[turn][SUMS - 1], s2);
                         turn ^= 1;
                     }
 #pragma unroll
-                    for (int e = 0; e < V; ++e) rho[e] = 1.f / sqrtf(fmaf(s1[e], a.per_mean, a.eps));
+                    for (int e = 0; e < N; ++e) rho[e] = make2(1.f / sqrtf(fmaf(s1[e].x, a.per_mean, a.eps)), 1.f / sqrtf(fmaf(s1[e].y, a.per_mean, a.eps)));
                 }
 #pragma unroll
                 for (int p = 0; p < P; ++p) {
                     const int i = r + R * p;
                     if constexpr (BWD) {
 #pragma unroll
-                        for (int s = 0; s < 2; ++s)
+                        for (int s = 0; s < 2; ++s) {
+                            f2 sum = pair(0.f);
 #pragma unroll
-                            for (int e = 0; e < V; ++e) {
-                                const float hat = x[p][s][e] * rho[e];
-                                acc[p][s] = fmaf(d[p][s][e], hat, acc[p][s]);
-                                const float e0 = d[p][s][e] * w[p][s];
-                                x[p][s][e] = a.norm == NORM_NONE ? e0 : rho[e] * (e0 - hat * (rho[e] * s2[e] * a.per_mean));
+                            for (int e = 0; e < N; ++e) {
+                                const f2 hat = mul2(x[p][s][e], rho[e]), own = mul2(d[p][s][e], pair(w[p][s]));
+                                sum = fma2(d[p][s][e], hat, sum);
+                                x[p][s][e] = a.norm == NORM_NONE ? own : mul2(rho[e], fma2(hat, mul2(mul2(rho[e], s2[e]), pair(-a.per_mean)), own));
                             }
+                            if (kind) acc[BWD][p][s] += sum2(sum);
+                            else acc[0][p][s] += sum2(sum);
+                        }
                     } else {
 #pragma unroll
                         for (int s = 0; s < 2; ++s)
 #pragma unroll
-                            for (int e = 0; e < V; ++e) x[p][s][e] *= rho[e] * w[p][s];
-                        if (i < a.turned) {
-#pragma unroll
-                            for (int e4 = 0; e4 < V; e4 += 4) {
-                                const float4 c4 = *(const float4 *)&cs[i * TOKENS + (e4 / 4 * 8 + vc) * 4], n4 = *(const float4 *)&sn[i * TOKENS + (e4 / 4 * 8 + vc) * 4];
-                                const float cc[4] = {c4.x, c4.y, c4.z, c4.w}, nn[4] = {n4.x, n4.y, n4.z, n4.w};
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) {
-                                    const float lo = x[p][0][e4 + e], hi = x[p][1][e4 + e];
-                                    x[p][0][e4 + e] = lo * cc[e] - hi * nn[e];
-                                    x[p][1][e4 + e] = lo * nn[e] + hi * cc[e];
-                                }
-                            }
-                        }
+                            for (int e = 0; e < N; ++e) x[p][s][e] = mul2(x[p][s][e], mul2(rho[e], pair(w[p][s])));
+                        if (i < a.turned) turned(x[p][0], x[p][1], i, 1.f);
                     }
 #pragma unroll
-                    for (int s = 0; s < 2; ++s)
-                        store_tokens<T, VEC>((T *)a.out[kind] + at + (long long)(i + s * half) * a.T, x[p][s], t0, vc, on && i < half ? a.T : 0);
+                    for (int s = 0; s < 2; ++s) store_tokens<T, VEC>(out + at + (long long)(i + s * half) * a.T, x[p][s], t0, vc, on && i < half ? a.T : 0);
                 }
             }
             u = end;
         }
     }
     if constexpr (BWD) {
-        if (!a.dg[kind]) return;
+        if (!a.dg[0] && !a.dg[1]) return;
         float *sum = &meet[0][0][0][0];                            // [HEADS][D]: at most 512 of its numbers
-        __syncthreads();
 #pragma unroll
-        for (int p = 0; p < P; ++p)
+        for (int kind = 0; kind < 2; ++kind) {
+            __syncthreads();
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                float v = acc[p][s];
+            for (int p = 0; p < P; ++p)
 #pragma unroll
-                for (int m = 1; m < 8; m <<= 1) v += __shfl_xor_sync(~0u, v, m);
-                if (vc == 0 && r + R * p < half) sum[group * a.D + r + R * p + s * half] = v;
+                for (int s = 0; s < 2; ++s) {
+                    float v = acc[kind][p][s];
+#pragma unroll
+                    for (int m = 1; m < 8; m <<= 1) v += __shfl_xor_sync(~0u, v, m);
+                    if (vc == 0 && r + R * p < half) sum[group * a.D + r + R * p + s * half] = v;
+                }
+            __syncthreads();
+            float *part = a.part + (((long long)blockIdx.y * gridDim.x + blockIdx.x) * 2 + kind) * a.D;
+            for (int c = tid; c < a.D; c += 256) {
+                float v = 0.f;
+                for (int j = 0; j < HEADS; ++j) v += sum[j * a.D + c];
+                HN_G(part + c, 4);
+                part[c] = v;
             }
-        __syncthreads();
-        float *to = a.part + ((long long)blockIdx.y * gridDim.x + blockIdx.x) * a.D;
-        for (int c = tid; c < a.D; c += 256) {
-            float v = 0.f;
-            for (int j = 0; j < HEADS; ++j) v += sum[j * a.D + c];
-            HN_G(to + c, 4);
-            to[c] = v;
         }
     }
 }
 
 // the blocks' sums of the weights' gradients, always in the same order: 8 channels and 32 spans of blocks to a CTA
-__global__ void __launch_bounds__(256) heads_sum_kernel(HeadsArgs a, int blocks_x)
+__global__ void __launch_bounds__(256) heads_sum_kernel(HeadsArgs a, int n)
 {
     __shared__ double s[32][8];
     const int kind = blockIdx.y, c = blockIdx.x * 8 + (threadIdx.x & 7), span = threadIdx.x >> 3;
     pdl_join();
     if (!a.dg[kind]) return;
-    const float *part = a.part + (kind ? (long long)a.splits[0] * blocks_x * a.D : 0);
-    const int n = a.splits[kind] * blocks_x;
+    const float *part = a.part + (long long)kind * a.D + c;
     double v = 0.;
-    if (c < a.D)
-        for (int i = span; i < n; i += 32) { HN_G(part + (long long)i * a.D + c, 4); v += part[(long long)i * a.D + c]; }
+    if (c < a.D) {
+#pragma unroll 4
+        for (int i = span; i < n; i += 32) { HN_G(part + (long long)i * 2 * a.D, 4); v += part[(long long)i * 2 * a.D]; }
+    }
     s[span][threadIdx.x & 7] = v;
     __syncthreads();
     if (span || c >= a.D) return;
@@ -345,27 +438,26 @@ template <typename T> __global__ void __launch_bounds__(256) heads_token_kernel(
     }
 }
 
-// CTAs along the tiles, and splits of the heads of q and of k: four CTAs an SM in all where there is work for them
+// CTAs along the tiles, and splits of the heads of q and k: two rounds of what the SMs hold where there is work for them
 static int plan(HeadsArgs &a, int dtype, int heads_at_once)
 {
-    const int tokens = dtype == HYENAND_F32 ? 32 : 64, want = 2 * kSms;
+    const int tokens = dtype == HYENAND_F32 ? 32 : 64, want = 6 * kSms;
     a.tiles = (int)(((long long)a.T + tokens - 1) / tokens);
-    for (int n = 0; n < 2; ++n) {
-        const long long most = ((long long)a.B * a.H[n] + heads_at_once - 1) / heads_at_once;
-        const long long s = a.tiles >= want ? 1 : want / a.tiles;
-        a.splits[n] = (int)(s < most ? s : most);
-    }
+    const long long most = ((long long)a.B * (a.H[0] + a.H[1]) + heads_at_once - 1) / heads_at_once, s = a.tiles >= want ? 1 : want / a.tiles;
+    a.splits = (int)(s < most ? s : most);
     return a.tiles < want ? a.tiles : want;
 }
 static int rows_of(int D) { return D <= 16 ? 4 : D <= 32 ? 8 : D <= 64 ? 16 : 32; }
 
+// cosines and sines of a tile; of the steps of one; of its rows
+static size_t table_bytes(int turned, int tokens, int last) { return (size_t)turned * (16 * tokens + 8 * rows_of_tile(tokens, last)); }
 template <auto FN, typename T> static int launch_tiles(const HeadsArgs &a, int grid_x, cudaStream_t st)
 {
-    const size_t bytes = (size_t)a.turned * Tile<T>::TOKENS * 8;
+    const size_t bytes = table_bytes(a.turned, Tile<T>::TOKENS, a.dims[a.ndim - 1]);
     static PerDevice ready;
-    if (bytes > 24 * 1024 && !ready.once([] { return cudaFuncSetAttribute(FN, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxD / 2 * Tile<T>::TOKENS * 8) == cudaSuccess ? 1 : -1; }))
+    if (bytes > 24 * 1024 && !ready.once([] { return cudaFuncSetAttribute(FN, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)table_bytes(kMaxD / 2, Tile<T>::TOKENS, 1)) == cudaSuccess ? 1 : -1; }))
         return kNoLaunch;
-    launch_pdl(FN, dim3(grid_x, a.splits[0] + a.splits[1]), 256, bytes, st, a);
+    launch_pdl(FN, dim3(grid_x, a.splits), 256, bytes, st, a);
     return 0;
 }
 template <typename T, bool BWD> static int launch_heads(HeadsArgs &a, int dtype, cudaStream_t st)
@@ -387,7 +479,7 @@ template <typename T, bool BWD> static int launch_heads(HeadsArgs &a, int dtype,
     else HN_HEADS(32, 4);
 #undef HN_HEADS
     if (e || !BWD || (!a.dg[0] && !a.dg[1])) return e;
-    launch_pdl(heads_sum_kernel, dim3((a.D + 7) / 8, 2), 256, 0, st, a, gx);
+    launch_pdl(heads_sum_kernel, dim3((a.D + 7) / 8, 2), 256, 0, st, a, gx * a.splits);
     return 0;
 }
 
@@ -425,7 +517,7 @@ static int fill(HeadsArgs &a, int ndim, const int *dims, int B, int Hq, int Hk, 
 static size_t part_bytes(HeadsArgs a, int dtype)
 {
     const long long gx = plan(a, dtype, 32 / rows_of(a.D));
-    return (size_t)(gx * (a.splits[0] + a.splits[1]) * a.D * (long long)sizeof(float));
+    return (size_t)(gx * a.splits * 2 * a.D * (long long)sizeof(float));
 }
 
 }  // namespace hn
