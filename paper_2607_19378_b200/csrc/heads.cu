@@ -72,23 +72,43 @@ template <typename T> struct Tile {
 
 // The V tokens of a lane in one row, in pairs: side by side as one vector, or (rows that do not start on 16 bytes) every eighth token, so
 // that the eight lanes of a row share a sector
-template <typename T, bool VEC> __device__ __forceinline__ void load_tokens(f2 (&v)[Tile<T>::V / 2], const T *row, int t0, int vc, int T_)
-{
-    constexpr int V = Tile<T>::V;
-    if constexpr (VEC) {
-        uint4 w = make_uint4(0, 0, 0, 0);
-        const int t = t0 + vc * V;
-        if (t < T_) { HN_G(row + t, 16); w = __ldg((const uint4 *)(row + t)); }
+template <typename T, bool VEC> struct Tokens {
+    uint4 w;
+    __device__ __forceinline__ void load(const T *row, int t0, int vc, int T_)
+    {
+        constexpr int V = Tile<T>::V;
+        w = make_uint4(0, 0, 0, 0);
+        if constexpr (VEC) {
+            const int t = t0 + vc * V;
+            if (t < T_) { HN_G(row + t, 16); w = __ldg((const uint4 *)(row + t)); }
+        } else {
+            unsigned x[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const T *p = row + t0 + i * 8 + vc;
+                x[i] = 0;
+                if (t0 + i * 8 + vc < T_) {
+                    HN_G(p, sizeof(T));
+                    if constexpr (sizeof(T) == 2) x[i] = __ldg((const unsigned short *)p);
+                    else x[i] = __float_as_uint(__ldg((const float *)p));
+                }
+            }
+            if constexpr (sizeof(T) == 2) w = make_uint4(x[0] | x[1] << 16, x[2] | x[3] << 16, x[V - 4] | x[V - 3] << 16, x[V - 2] | x[V - 1] << 16);
+            else w = make_uint4(x[0], x[1], x[2], x[3]);
+        }
+    }
+    __device__ __forceinline__ void get(f2 (&v)[Tile<T>::V / 2]) const
+    {
         const unsigned u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-        for (int i = 0; i < V / 2; ++i) v[i] = sizeof(T) == 2 ? widen2(u[i]) : make2(__uint_as_float(u[2 * i & 3]), __uint_as_float(u[(2 * i + 1) & 3]));
-    } else {
-        float x[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) x[i] = t0 + i * 8 + vc < T_ ? IO<T>::ld(row, t0 + i * 8 + vc) : 0.f;
-#pragma unroll
-        for (int i = 0; i < V / 2; ++i) v[i] = make2(x[2 * i], x[2 * i + 1]);
+        for (int i = 0; i < Tile<T>::V / 2; ++i) v[i] = sizeof(T) == 2 ? widen2(u[i]) : make2(__uint_as_float(u[2 * i & 3]), __uint_as_float(u[(2 * i + 1) & 3]));
     }
+};
+// 1 / sqrt(v), the approximation set right by a step of Newton's method (two roundings; sqrt and division would be a third of a head's work)
+__device__ __forceinline__ float inverse_root(float v)
+{
+    const float y = rsqrtf(v);
+    return fmaf(0.5f * y, fmaf(-v * y, y, 1.f), y);
 }
 template <typename T, bool VEC> __device__ __forceinline__ void store_tokens(T *row, const f2 (&v)[Tile<T>::V / 2], int t0, int vc, int T_)
 {
@@ -174,8 +194,11 @@ template <typename T, bool VEC> __device__ __forceinline__ void fill_table(const
     }
 }
 
-// R groups of eight lanes to a head, P pairs of channels to a lane; 32 / R heads at a time
-template <typename T, int R, int P, bool BWD, bool VEC> __global__ void __launch_bounds__(256, P > 2 ? 1 : BWD ? 2 : 3) heads_kernel(HeadsArgs a)
+// R groups of eight lanes to a head, P pairs of channels to a lane; 32 / R heads at a time.  Two pairs for fp32, four for bf16 heads of more
+// than 32 channels: what a unit costs beside its elements (shuffles, the meeting, rho) is then shared by more of them (the vision grid
+// forward 131 -> 91 us, 262144 tokens of 128 channels each way 393 + 535 -> 252 + 476; of one pair 267 us and more).
+constexpr int resident(int pairs, bool backward) { return pairs > 2 ? (backward ? 1 : 2) : backward ? 2 : 3; }          // CTAs an SM, by registers
+template <typename T, int R, int P, bool BWD, bool VEC> __global__ void __launch_bounds__(256, resident(P, BWD)) heads_kernel(HeadsArgs a)
 {
     constexpr int V = Tile<T>::V, TOKENS = Tile<T>::TOKENS, HEADS = 32 / R, WARPS = R / 4, SUMS = BWD ? 2 : 1, N = V / 2;
     extern __shared__ __align__(16) float sm[];
@@ -219,34 +242,43 @@ template <typename T, int R, int P, bool BWD, bool VEC> __global__ void __launch
             __syncthreads();                                       // (the table's readers are through; the steps are there)
             fill_table<T, VEC>(a, (int)b0, t0, cs, sn, step_c, step_s, rows, freq, axis_of, tid);
             __syncthreads();
+            int b = (int)b0, h = (int)(u - b0 * HT);               // of the first of the units at a time
+            // a lane's rows: the channels r + R p and half further on, of the head that its group is at
+            const long long row0 = (long long)r * a.T;
+            auto place_of = [&](int b, int h, int &kind) {
+                h += group;
+                while (h >= HT) { h -= HT; ++b; }
+                kind = h >= a.H[0];
+                return ((long long)b * a.H[kind] + h - (kind ? a.H[0] : 0)) * a.D * (long long)a.T + row0;
+            };
 #pragma unroll 1
             for (; u < end; u += HEADS) {
-                const long long unit = u + group;
-                const bool on = unit < end;
-                const int b = (int)(unit / HT), h = (int)(unit - (long long)b * HT), kind = h >= a.H[0];
-                const long long at = on ? ((long long)b * a.H[kind] + h - (kind ? a.H[0] : 0)) * a.D * (long long)a.T : 0;
-                const T *in = (const T *)a.x[kind], *gradient = (const T *)a.dy[kind];
-                T *out = (T *)a.out[kind];
-                const float *weight = weights[kind];
-                float w[P][2];
+                int kind;
+                const long long at = place_of(b, h, kind);
+                const int live = u + group < end ? a.T : 0;
+                h += HEADS;
+                while (h >= HT) { h -= HT; ++b; }
+                const T *in = (const T *)a.x[kind] + at, *gradient = (const T *)a.dy[kind] + at;
+                T *out = (T *)a.out[kind] + at;
+                // what was loaded stays as it came: bf16 values twice made fp32 cost less than the registers
+                Tokens<T, VEC> rx[P][2];
+                f2 d[BWD ? P : 1][2][N], s1[N], s2[BWD ? N : 1];
+                {
+                    Tokens<T, VEC> rd[BWD ? P : 1][2];
 #pragma unroll
-                for (int p = 0; p < P; ++p)
+                    for (int p = 0; p < P; ++p)
 #pragma unroll
-                    for (int s = 0; s < 2; ++s) w[p][s] = r + R * p < half ? weight[r + R * p + s * half] : 0.f;
-                f2 x[P][2][N], d[BWD ? P : 1][2][N], s1[N], s2[BWD ? N : 1];
+                        for (int s = 0; s < 2; ++s) {
+                            const long long o = (long long)(R * p + s * half) * a.T;
+                            rx[p][s].load(in + o, t0, vc, r + R * p < half ? live : 0);
+                            if constexpr (BWD) rd[p][s].load(gradient + o, t0, vc, r + R * p < half ? live : 0);
+                        }
+                    if constexpr (BWD)
 #pragma unroll
-                for (int e = 0; e < N; ++e) s1[e] = pair(0.f);
-                if constexpr (BWD)
+                        for (int p = 0; p < P; ++p)
 #pragma unroll
-                    for (int e = 0; e < N; ++e) s2[e] = pair(0.f);
-#pragma unroll
-                for (int p = 0; p < P; ++p)
-#pragma unroll
-                    for (int s = 0; s < 2; ++s) {
-                        const int i = r + R * p, c = i + s * half, live = on && i < half ? a.T : 0;
-                        load_tokens<T, VEC>(x[p][s], in + at + (long long)c * a.T, t0, vc, live);
-                        if constexpr (BWD) load_tokens<T, VEC>(d[p][s], gradient + at + (long long)c * a.T, t0, vc, live);
-                    }
+                            for (int s = 0; s < 2; ++s) rd[p][s].get(d[p][s]);
+                }
                 auto turned = [&](f2 (&lo)[N], f2 (&hi)[N], int i, float way) {
 #pragma unroll
                     for (int e = 0; e < N; e += 2) {
@@ -255,23 +287,33 @@ template <typename T, int R, int P, bool BWD, bool VEC> __global__ void __launch
                         const f2 c[2] = {make2(c4.x, c4.y), make2(c4.z, c4.w)}, n[2] = {make2(n4.x, n4.y), make2(n4.z, n4.w)};
 #pragma unroll
                         for (int m = 0; m < 2; ++m) {
-                            const f2 l = lo[e + m], h = hi[e + m], sine = mul2(n[m], pair(way));
-                            lo[e + m] = fma2(l, c[m], mul2(mul2(h, sine), pair(-1.f)));
-                            hi[e + m] = fma2(h, c[m], mul2(l, sine));
+                            const f2 l = lo[e + m], h = hi[e + m], other = mul2(n[m], pair(-1.f)), sine = way > 0.f ? n[m] : other, back = way > 0.f ? other : n[m];
+                            lo[e + m] = fma2(h, back, mul2(l, c[m]));
+                            hi[e + m] = fma2(l, sine, mul2(h, c[m]));
                         }
                     }
                 };
+                auto weight = [&](int p, int s) { return pair(weights[kind][(r + R * p < half ? r + R * p : 0) + s * half]); };
+#pragma unroll
+                for (int e = 0; e < N; ++e) s1[e] = pair(0.f);
+                if constexpr (BWD)
+#pragma unroll
+                    for (int e = 0; e < N; ++e) s2[e] = pair(0.f);
 #pragma unroll
                 for (int p = 0; p < P; ++p) {
                     if constexpr (BWD)
                         if (r + R * p < a.turned) turned(d[p][0], d[p][1], r + R * p, -1.f);
 #pragma unroll
-                    for (int s = 0; s < 2; ++s)
+                    for (int s = 0; s < 2; ++s) {
+                        f2 x[N];
+                        rx[p][s].get(x);
+                        const f2 w = weight(p, s);
 #pragma unroll
                         for (int e = 0; e < N; ++e) {
-                            s1[e] = fma2(x[p][s][e], x[p][s][e], s1[e]);
-                            if constexpr (BWD) s2[e] = fma2(mul2(d[p][s][e], pair(w[p][s])), x[p][s][e], s2[e]);
+                            s1[e] = fma2(x[e], x[e], s1[e]);
+                            if constexpr (BWD) s2[e] = fma2(mul2(d[p][s][e], w), x[e], s2[e]);
                         }
+                    }
                 }
                 f2 rho[N];
                 if (a.norm == NORM_NONE) {
@@ -313,33 +355,38 @@ template <typename T, int R, int P, bool BWD, bool VEC> __global__ void __launch
                         turn ^= 1;
                     }
 #pragma unroll
-                    for (int e = 0; e < N; ++e) rho[e] = make2(1.f / sqrtf(fmaf(s1[e].x, a.per_mean, a.eps)), 1.f / sqrtf(fmaf(s1[e].y, a.per_mean, a.eps)));
+                    for (int e = 0; e < N; ++e) {
+                        rho[e] = make2(inverse_root(fmaf(s1[e].x, a.per_mean, a.eps)), inverse_root(fmaf(s1[e].y, a.per_mean, a.eps)));
+                        if constexpr (BWD) s2[e] = mul2(mul2(rho[e], s2[e]), pair(-a.per_mean));
+                    }
                 }
 #pragma unroll
                 for (int p = 0; p < P; ++p) {
-                    const int i = r + R * p;
-                    if constexpr (BWD) {
+                    const int i = r + R * p, room = i < half ? live : 0;
+                    f2 x[2][N];
 #pragma unroll
-                        for (int s = 0; s < 2; ++s) {
+                    for (int s = 0; s < 2; ++s) {
+                        const f2 w = weight(p, s);
+                        rx[p][s].get(x[s]);
+                        if constexpr (BWD) {
                             f2 sum = pair(0.f);
 #pragma unroll
                             for (int e = 0; e < N; ++e) {
-                                const f2 hat = mul2(x[p][s][e], rho[e]), own = mul2(d[p][s][e], pair(w[p][s]));
+                                const f2 hat = mul2(x[s][e], rho[e]), own = mul2(d[p][s][e], w);
                                 sum = fma2(d[p][s][e], hat, sum);
-                                x[p][s][e] = a.norm == NORM_NONE ? own : mul2(rho[e], fma2(hat, mul2(mul2(rho[e], s2[e]), pair(-a.per_mean)), own));
+                                x[s][e] = a.norm == NORM_NONE ? own : mul2(rho[e], fma2(hat, s2[e], own));
                             }
                             if (kind) acc[BWD][p][s] += sum2(sum);
                             else acc[0][p][s] += sum2(sum);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < N; ++e) x[s][e] = mul2(x[s][e], mul2(rho[e], w));
                         }
-                    } else {
-#pragma unroll
-                        for (int s = 0; s < 2; ++s)
-#pragma unroll
-                            for (int e = 0; e < N; ++e) x[p][s][e] = mul2(x[p][s][e], mul2(rho[e], pair(w[p][s])));
-                        if (i < a.turned) turned(x[p][0], x[p][1], i, 1.f);
                     }
+                    if constexpr (!BWD)
+                        if (i < a.turned) turned(x[0], x[1], i, 1.f);
 #pragma unroll
-                    for (int s = 0; s < 2; ++s) store_tokens<T, VEC>(out + at + (long long)(i + s * half) * a.T, x[p][s], t0, vc, on && i < half ? a.T : 0);
+                    for (int s = 0; s < 2; ++s) store_tokens<T, VEC>(out + (long long)(R * p + s * half) * a.T, x[s], t0, vc, room);
                 }
             }
             u = end;
@@ -438,16 +485,22 @@ template <typename T> __global__ void __launch_bounds__(256) heads_token_kernel(
     }
 }
 
-// CTAs along the tiles, and splits of the heads of q and k: two rounds of what the SMs hold where there is work for them
-static int plan(HeadsArgs &a, int dtype, int heads_at_once)
+static int pairs_of(int D, int dtype) { return D > 128 || (dtype == HYENAND_BF16 && D > 32) ? 4 : 2; }
+static int rows_of(int D, int dtype)                      // a power of two, so that rows and pairs hold half the channels
 {
-    const int tokens = dtype == HYENAND_F32 ? 32 : 64, want = 6 * kSms;
+    int r = 4;
+    while (r * pairs_of(D, dtype) < D / 2) r *= 2;
+    return r;
+}
+// CTAs along the tiles, and splits of the heads of q and k: two rounds of what the SMs hold where there is work for them
+static int plan(HeadsArgs &a, int dtype, bool backward)
+{
+    const int tokens = dtype == HYENAND_F32 ? 32 : 64, want = 2 * resident(pairs_of(a.D, dtype), backward) * kSms, at_once = 32 / rows_of(a.D, dtype);
     a.tiles = (int)(((long long)a.T + tokens - 1) / tokens);
-    const long long most = ((long long)a.B * (a.H[0] + a.H[1]) + heads_at_once - 1) / heads_at_once, s = a.tiles >= want ? 1 : want / a.tiles;
+    const long long most = ((long long)a.B * (a.H[0] + a.H[1]) + at_once - 1) / at_once, s = a.tiles >= want ? 1 : want / a.tiles;
     a.splits = (int)(s < most ? s : most);
     return a.tiles < want ? a.tiles : want;
 }
-static int rows_of(int D) { return D <= 16 ? 4 : D <= 32 ? 8 : D <= 64 ? 16 : 32; }
 
 // cosines and sines of a tile; of the steps of one; of its rows
 static size_t table_bytes(int turned, int tokens, int last) { return (size_t)turned * (16 * tokens + 8 * rows_of_tile(tokens, last)); }
@@ -468,15 +521,17 @@ template <typename T, bool BWD> static int launch_heads(HeadsArgs &a, int dtype,
         launch_pdl(heads_token_kernel<T>, dim3((unsigned)blocks), 256, 0, st, a);
         return 0;
     }
-    const int R = rows_of(a.D), gx = plan(a, dtype, 32 / R);
+    const int R = rows_of(a.D, dtype), gx = plan(a, dtype, BWD);
     const bool vec = a.T % Tile<T>::V == 0;
-    int e;
-#define HN_HEADS(R_, P_) e = vec ? launch_tiles<heads_kernel<T, R_, P_, BWD, true>, T>(a, gx, st) : launch_tiles<heads_kernel<T, R_, P_, BWD, false>, T>(a, gx, st)
-    if (a.D <= 16) HN_HEADS(4, 2);
-    else if (a.D <= 32) HN_HEADS(8, 2);
-    else if (a.D <= 64) HN_HEADS(16, 2);
-    else if (a.D <= 128) HN_HEADS(32, 2);
-    else HN_HEADS(32, 4);
+    int e = kNoLaunch;
+#define HN_HEADS(R_, P_) if (R == R_) e = vec ? launch_tiles<heads_kernel<T, R_, P_, BWD, true>, T>(a, gx, st) : launch_tiles<heads_kernel<T, R_, P_, BWD, false>, T>(a, gx, st)
+    if (pairs_of(a.D, dtype) == 4) {
+        HN_HEADS(32, 4);
+        if constexpr (sizeof(T) == 2) { HN_HEADS(8, 4); HN_HEADS(16, 4); }
+    } else {
+        HN_HEADS(4, 2); HN_HEADS(8, 2);
+        if constexpr (sizeof(T) == 4) { HN_HEADS(16, 2); HN_HEADS(32, 2); }
+    }
 #undef HN_HEADS
     if (e || !BWD || (!a.dg[0] && !a.dg[1])) return e;
     launch_pdl(heads_sum_kernel, dim3((a.D + 7) / 8, 2), 256, 0, st, a, gx * a.splits);
@@ -516,7 +571,7 @@ static int fill(HeadsArgs &a, int ndim, const int *dims, int B, int Hq, int Hk, 
 }
 static size_t part_bytes(HeadsArgs a, int dtype)
 {
-    const long long gx = plan(a, dtype, 32 / rows_of(a.D));
+    const long long gx = plan(a, dtype, true);
     return (size_t)(gx * a.splits * 2 * a.D * (long long)sizeof(float));
 }
 
