@@ -780,11 +780,11 @@ extern "C" int hyenand_delta_backward(int B, int H, int Hk, int L, int Dk, int D
     if (int e = fill(a, B, H, Hk, L, Dk, Dv, decay, dtype)) return e;
     if (!marks || !dy || !dq || !dk || !dv || !dbeta || !workspace)
         return fail(HYENAND_ERR_INVALID_ARG, "marks, dy, dq, dk, dv, dbeta, workspace must be non-NULL");
-    if (decay == DELTA_NONE && dg) return fail(HYENAND_ERR_INVALID_ARG, "dg of a rule without a decay");
     a.q = q; a.k = k; a.v = v; a.g = g; a.beta = beta; a.lengths = lengths; a.marks = (float *)marks; a.dy = dy; a.ds_end = ds_end;
     a.dq = dq; a.dk = dk; a.dv = dv; a.dg = dg; a.dbeta = dbeta; a.ds0 = ds0;
     CallTensors c;
     if (int e = inputs(c, a, L, dtype)) return e;
+    if (decay == DELTA_NONE && dg) return fail(HYENAND_ERR_INVALID_ARG, "dg of a rule without a decay");
     const DeltaSizes s = delta_sizes(a, dtype, true);
     place_workspace(a, s, workspace);
     const size_t es = elsize(dtype) * (size_t)L * B, gb = (size_t)B * H * L * sizeof(float);
