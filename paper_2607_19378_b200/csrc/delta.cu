@@ -303,7 +303,6 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             issue_ts<PM, PM, PM, false, kTok / 16, B_LOWER>(tb + C::X0, tb + C::Z0, kTok / 2, A, kMatrix, kTok / 16, kTok, false);
             umma_commit(&ws.bar_b);
             WAIT(&ws.u_ready, par);
-            if (RUN && !C::ROOM) WAIT(&ws.p_ready, par);     // (the gain comes where U is)
             tmem_fence_after_sync();
             issue_ts<PM, PI, PM, false, kTok / 16>(tb + C::D0, tb + C::U0, kTok / 2, k, C::TILE, kTok / 16, KD / 2, false);
             if (C::ROOM) umma_commit(&ws.bar_c[0]);
@@ -311,7 +310,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             if (!C::ROOM) umma_commit(&ws.bar_c[0]);
             umma_commit(&ws.bar_c[1]);
             if (RUN) {
-                if (C::ROOM) WAIT(&ws.p_ready, par);
+                WAIT(&ws.p_ready, par);
                 WAIT(&ws.o_ready, par);                      // (y's first sum times gamma)
                 tmem_fence_after_sync();
                 issue_ts<PM, PM, PM, false, kTok / 16, B_LOWER>(tb + C::Y0, tb + C::Z0, kTok / 2, P, kMatrix, kTok / 16, kTok, true);
@@ -390,12 +389,12 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
 #pragma unroll
             for (int i = 0; i < HC / 2; ++i) S[i] = make2(s[2 * i], s[2 * i + 1]);
         }
+        planes_to_tmem<PM, HC / 2>(lane_s, KD / 2, S);
         for (int c = first, i = 0; c < last; ++c, ++i) {
             const int s = i % C::STAGES, t = c * kTok + 32 * half;
             const unsigned par = i & 1;
             const unsigned char *st = sm + s * C::STAGE;
             const float *gates = (const float *)(st + C::GATES) + 32 * half;
-            planes_to_tmem<PM, HC / 2>(lane_s, KD / 2, S);
             walk_ready(&ws.state[half], lane);
             f2 held[C::VALUES ? 1 : 16];                     // (fp32 values come from device memory: ahead of their use)
             if constexpr (!C::VALUES) load_row(held, (const float *)a.v, vhead + (long long)row * a.L + t, a.L, values ? n - t : 0);
@@ -403,74 +402,62 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             WAIT(&ws.full[s], (i / C::STAGES) & 1);
             WAIT(&ws.bar_a, par);
             tmem_fence_after_sync();
+            f2 x[16];
+            tmem_ld(x, lane_x);
+            tmem_wait_ld();
 #pragma unroll
             for (int g = 0; g < 4; ++g) {                    // Z = beta v - beta gamma S k
-                f2 x[4], v[4], be[4], bg[4];
-                tmem_ld8(x, lane_x + 8 * g);
+                f2 z[4], be[4], bg[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = pair(0.f);
+                for (int e = 0; e < 4; ++e) z[e] = pair(0.f);
                 if constexpr (C::VALUES) {
                     if (values) {
                         const uint4 w = *(const uint4 *)(st + C::V + image_at(row, 4 * half + g));
-                        v[0] = widen2(w.x); v[1] = widen2(w.y); v[2] = widen2(w.z); v[3] = widen2(w.w);
+                        z[0] = widen2(w.x); z[1] = widen2(w.y); z[2] = widen2(w.z); z[3] = widen2(w.w);
                     }
                 } else {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = held[4 * g + e];
+                    for (int e = 0; e < 4; ++e) z[e] = held[4 * g + e];
                 }
                 shared8(be, gates + 2 * kTok + 8 * g);
                 shared8(bg, gates + 3 * kTok + 8 * g);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = mul2(be[e], v[e]);
-                tmem_wait_ld();
-#pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = fma2(bg[e], x[e], v[e]);
-                planes8_to_tmem<PM>(lane_z + 4 * g, kTok / 2, x);
+                for (int e = 0; e < 4; ++e) z[e] = fma2(bg[e], x[4 * g + e], mul2(be[e], z[e]));
+                planes8_to_tmem<PM>(lane_z + 4 * g, kTok / 2, z);
             }
             walk_ready(&ws.z_ready, lane);
             const f2 fade = pair(((const float *)(st + C::GATES))[kTok - 1]);
             WAIT(&ws.bar_b, par);
             tmem_fence_after_sync();
+            tmem_ld(x, lane_x);
+            tmem_wait_ld();
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                f2 x[4], de[4];
-                tmem_ld8(x, lane_x + 8 * g);
+                f2 u[4], de[4];
                 shared8(de, gates + kTok + 8 * g);
-                tmem_wait_ld();
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = mul2(x[e], de[e]);
-                planes8_to_tmem<PM>(lane_u + 4 * g, kTok / 2, x);
+                for (int e = 0; e < 4; ++e) u[e] = mul2(x[4 * g + e], de[e]);
+                planes8_to_tmem<PM>(lane_u + 4 * g, kTok / 2, u);
             }
             walk_ready(&ws.u_ready, lane);
             if (RUN) {
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    f2 x[4];
-                    tmem_ld8(x, lane_x + 8 * g);
-                    tmem_wait_ld();
-                    planes8_to_tmem<PM>(lane_z + 4 * g, kTok / 2, x);
-                }
+                planes_to_tmem<PM, 16>(lane_z, kTok / 2, x);
                 walk_ready(&ws.p_ready, lane);
             }
             WAIT(&ws.bar_c[half], par);
             tmem_fence_after_sync();
-#pragma unroll
-            for (int e = 0; e < HC / 2; e += 16) {
-                f2 x[16];
-                tmem_ld(x, lane_d + 2 * e);
-                tmem_wait_ld();
-#pragma unroll
-                for (int j = 0; j < 16; ++j) S[e + j] = fma2(fade, S[e + j], x[j]);
-            }
+            state_onwards<PM>(S, fade, lane_d, lane_s, KD / 2);
         }
+        tmem_wait_st();
         auto flat = [&](float (&s)[HC]) {
 #pragma unroll
             for (int i = 0; i < HC / 2; ++i) split2(S[i], s[2 * i], s[2 * i + 1]);
         };
         if (!RUN) {
-            float *to = a.maps + (bh * a.segments + segment) * (long long)(a.Dv + a.Dk) * a.Dk + (phi ? states : 0), s[HC];
+            const int pitch = map_pitch(a.Dk);
+            float *to = a.maps + ((bh * a.segments + segment) * (a.Dv + a.Dk) + (phi ? a.Dv : 0)) * (long long)pitch, s[HC];
             flat(s);
-            store_state<HC>(to, s, row, rows, half * HC, a.Dk);
+            store_state<HC>(to, s, row, rows, half * HC, pitch);
         } else {
             if (a.s_end && segment == a.segments - 1) {
                 float s[HC];
@@ -490,66 +477,89 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
 
 // ---- segments -------------------------------------------------------------------------------------------------------
 
-// States at the segments' starts from the maps S -> S Phi + N: four rows to a CTA, four quarters of the sum over Phi's rows; the next
-// segment's Phi is on its way meanwhile.  `reverse`: from the last segment to the first (the gradient's states).
-__global__ void __launch_bounds__(512) delta_join_kernel(DeltaArgs a, const float *from, int reverse)
+// States at the segments' starts from the maps S -> S Phi + N: eight rows to a CTA, Phi by bulk copies, the next one under way; a thread
+// sums four columns of all rows over an eighth of Phi's rows.  `reverse`: from the last segment to the first (the gradient's states).
+constexpr int kJoinRows = 8, kJoinBytes = 2 * 128 * 128 * 4;
+__global__ void __launch_bounds__(256) delta_join_kernel(DeltaArgs a, const float *from, int reverse)
 {
-    constexpr int R = 4;
-    __shared__ __align__(16) float S[R][128];
-    __shared__ float part[4][R][128];
-    const int j = threadIdx.x & 127, quarter = threadIdx.x >> 7, tiles = (a.Dv + R - 1) / R;
-    const long long bh = blockIdx.x / tiles, states = (long long)a.Dv * a.Dk, map = states + (long long)a.Dk * a.Dk;
-    const int row = (int)(blockIdx.x % tiles) * R + quarter, n = a.segments, step = reverse ? -1 : 1;
-    const bool mine = row < a.Dv && j < a.Dk;                // (a quarter of the threads to a row)
-    pdl_join();
-    float v = 0.f;
-    if (from && mine) { const float *p = from + bh * states + (long long)row * a.Dk + j; HN_G(p, 4); v = *p; }
-    float phi[2][32], add[2];
-    auto fetch = [&](int s, float (&to)[32], float &plus) {
-        const float *p = a.maps + (bh * n + s) * map;
-        plus = 0.f;
-        if (mine) { HN_G(p + (long long)row * a.Dk + j, 4); plus = p[(long long)row * a.Dk + j]; }
-        p += states + (long long)quarter * 32 * a.Dk + j;
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            to[i] = 0.f;
-            if (quarter * 32 + i < a.Dk && j < a.Dk) { HN_G(p + i * a.Dk, 4); to[i] = p[i * a.Dk]; }
-        }
-    };
-    int s = reverse ? n - 1 : 0;
-    auto advance = [&](const float (&with)[32], float plus) {
-        S[quarter][j] = v;
-        if (mine) {
-            float *p = a.starts + (bh * n + s) * states + (long long)row * a.Dk + j;
-            HN_G(p, 4);
-            *p = v;
-        }
-        __syncthreads();
-        float acc[R];
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            acc[r] = 0.f;
-#pragma unroll
-            for (int k = 0; k < 32; k += 4) {
-                const float4 w = *(const float4 *)&S[r][quarter * 32 + k];
-                acc[r] = fmaf(w.x, with[k], fmaf(w.y, with[k + 1], fmaf(w.z, with[k + 2], fmaf(w.w, with[k + 3], acc[r]))));
-            }
-        }
-#pragma unroll
-        for (int r = 0; r < R; ++r) part[quarter][r][j] = acc[r];
-        __syncthreads();
-        v = ((part[0][quarter][j] + part[1][quarter][j]) + (part[2][quarter][j] + part[3][quarter][j])) + plus;
-    };
-    fetch(s, phi[0], add[0]);
-    for (int i = 0; i < n; i += 2) {
-        if (i + 1 < n) fetch(s + step, phi[1], add[1]);
-        advance(phi[0], add[0]);
-        s += step;
-        if (i + 1 >= n) break;
-        if (i + 2 < n) fetch(s + step, phi[0], add[0]);
-        advance(phi[1], add[1]);
-        s += step;
+    constexpr int R = kJoinRows;
+    extern __shared__ __align__(16) float phi[];             // two of [Dk][pitch]
+    __shared__ __align__(16) float S[R][128], part[8][R][128];
+    __shared__ WalkShared ws;
+    const int tid = threadIdx.x, quad = tid & 31, eighth = tid >> 5, tiles = (a.Dv + R - 1) / R, pitch = map_pitch(a.Dk), n = a.segments, step = reverse ? -1 : 1;
+    const long long bh = blockIdx.x / tiles, states = (long long)a.Dv * a.Dk, map = (long long)(a.Dv + a.Dk) * pitch;
+    const int row = (int)(blockIdx.x % tiles) * R + eighth, each = (a.Dk + 31) / 32 * 4;          // (a thread's row of S; Phi's rows of an eighth)
+    const unsigned bytes = (unsigned)(a.Dk * pitch * 4);
+    for (int e = tid; e < 2 * 128 * 128 / 4; e += 256) ((float4 *)phi)[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (tid == 0) {
+        mbar_init(&ws.full[0], 1); mbar_init(&ws.full[1], 1);
+        ws.gave_up = 0;
+        fence_mbar_init();
     }
+    fence_async_smem();
+    pdl_join();
+    __syncthreads();
+    auto fetch = [&](int i) {                                // (one thread) the i-th segment's
+        const int s = reverse ? n - 1 - i : i;
+        mbar_expect_tx(&ws.full[i & 1], bytes);
+        bulk_load(phi + (i & 1) * 128 * 128, a.maps + (bh * n + s) * map + (long long)a.Dv * pitch, bytes, &ws.full[i & 1]);
+    };
+    if (tid == 0 && n > 1) fetch(0);
+    if (tid == 0 && n > 2) fetch(1);
+    // a warp holds a row: four columns a lane
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    float *const mine = (float *)&v;
+    if (from && row < a.Dv)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (4 * quad + e < a.Dk) { const float *p = from + bh * states + (long long)row * a.Dk + 4 * quad + e; HN_G(p, 4); mine[e] = *p; }
+    for (int i = 0, s = reverse ? n - 1 : 0; i < n; ++i, s += step) {
+        *(float4 *)&S[eighth][4 * quad] = v;
+        if (row < a.Dv)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (4 * quad + e < a.Dk) {
+                    float *p = a.starts + (bh * n + s) * states + (long long)row * a.Dk + 4 * quad + e;
+                    HN_G(p, 4);
+                    *p = mine[e];
+                }
+        if (i == n - 1) break;
+        float4 add = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (row < a.Dv && 4 * quad < pitch) { const float4 *p = (const float4 *)(a.maps + (bh * n + s) * map + (long long)row * pitch) + quad; HN_G(p, 16); add = *p; }
+        __syncthreads();
+        WAIT(&ws.full[i & 1], (i >> 1) & 1);
+        f2 acc[R][2];
+#pragma unroll
+        for (int r = 0; r < R; ++r) acc[r][0] = acc[r][1] = pair(0.f);
+        const float *w = phi + (i & 1) * 128 * 128 + eighth * each * pitch + 4 * quad;
+        if (4 * quad < pitch)
+            for (int k = 0; k < each; k += 4) {
+                float4 p[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) p[e] = *(const float4 *)(w + (k + e) * pitch);
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const float4 q = *(const float4 *)&S[r][eighth * each + k];
+                    const float qk[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        acc[r][0] = fma2(pair(qk[e]), make2(p[e].x, p[e].y), acc[r][0]);
+                        acc[r][1] = fma2(pair(qk[e]), make2(p[e].z, p[e].w), acc[r][1]);
+                    }
+                }
+            }
+#pragma unroll
+        for (int r = 0; r < R; ++r) *(float4 *)&part[eighth][r][4 * quad] = make_float4(acc[r][0].x, acc[r][0].y, acc[r][1].x, acc[r][1].y);
+        __syncthreads();
+        if (tid == 0 && i + 2 < n - 1) fetch(i + 2);          // (every thread has read this one)
+        v = add;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float4 p = *(const float4 *)&part[e][eighth][4 * quad];
+            v.x += p.x; v.y += p.y; v.z += p.z; v.w += p.w;
+        }
+    }
+    if (ws.gave_up && tid == 0) atomicExch(&hn_delta_status, 1);
 }
 
 // ---- one token ------------------------------------------------------------------------------------------------------
@@ -621,7 +631,7 @@ DeltaSizes delta_sizes(const DeltaArgs &a, int dtype, bool backward)
     s.images = chunks * 2 * planes * kMatrix;
     s.gates = up(chunks * kGates * 4);
     if (a.segments > 1) {
-        s.maps = up(bh * a.segments * ((size_t)a.Dv + a.Dk) * a.Dk * 4);
+        s.maps = up(bh * a.segments * ((size_t)a.Dv + a.Dk) * map_pitch(a.Dk) * 4);
         s.starts = up(bh * a.segments * (size_t)a.Dv * a.Dk * 4);
     }
     if (backward) {
@@ -654,10 +664,7 @@ int launch_delta_prepare(DeltaArgs a, int dtype, cudaStream_t st) { return dtype
 
 int launch_delta_join(const DeltaArgs &a, const float *from, bool backward, cudaStream_t st)
 {
-    const long long blocks = (long long)a.B * a.H * ((a.Dv + 3) / 4);
-    if (blocks > 0x7fffffffll) return kTooLarge;
-    launch_pdl(delta_join_kernel, dim3((unsigned)blocks), 512, 0, st, a, from, (int)backward);
-    return 0;
+    return launch_delta<delta_join_kernel>(a, (long long)a.B * a.H * ((a.Dv + kJoinRows - 1) / kJoinRows), 256, kJoinBytes, st, from, (int)backward);
 }
 
 template <typename T, int KD> static int launch_walk(DeltaArgs a, cudaStream_t st)

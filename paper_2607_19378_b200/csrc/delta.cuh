@@ -49,11 +49,13 @@ struct DeltaArgs {
     // workspace
     unsigned char *images;                                // [B H][chunks]: planes of A, planes of P
     float *gates;                                         // [B H][chunks][6][64]
-    float *maps, *starts;                                 // [B H][segments][Dv + Dk][Dk], [B H][segments][Dv][Dk]
+    float *maps, *starts;                                 // [B H][segments][Dv + Dk][map_pitch], [B H][segments][Dv][Dk]
     float *dstates, *dz;                                  // [B H][chunks] states as kept, [B H][chunks][Dv][64]
     int B, H, Hk, L, Dk, Dv, decay, chunks, segments, per_segment;
     int copies;                                           // 1: tiles come as tensor copies
 };
+
+__host__ __device__ __forceinline__ int map_pitch(int Dk) { return (Dk + 3) & ~3; }
 
 __device__ __forceinline__ int live_tokens(const DeltaArgs &a, int b)
 {
@@ -175,6 +177,31 @@ template <int PM> __device__ __forceinline__ void planes8_to_tmem(unsigned at, i
     }
 #pragma unroll
     for (int p = 0; p < PM; ++p) tmem_st4(at + p * pitch, w[p]);
+}
+// 16 columns of this thread's lane, on their way until the next wait for loads
+struct Sixteen {
+    float x[16];
+    __device__ __forceinline__ void load(unsigned at) { TmemIO<16>::ld(x, at); }
+    __device__ __forceinline__ f2 get(int i) const { return make2(x[2 * i], x[2 * i + 1]); }
+};
+// S = fade S + gain (this thread's columns of both, eight pairs at a time, the next loads under way), and S as an operand again
+template <int PM, int C> __device__ __forceinline__ void state_onwards(f2 (&S)[C], f2 fade, unsigned gain, unsigned planes, int pitch)
+{
+    Sixteen g[2];
+    g[0].load(gain);
+#pragma unroll
+    for (int b = 0; b < C / 8; ++b) {
+        tmem_wait_ld();
+        if (b + 1 < C / 8) g[(b + 1) & 1].load(gain + 16 * (b + 1));
+        f2 x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = S[8 * b + j] = fma2(fade, S[8 * b + j], g[b & 1].get(j));
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const f2 y[4] = {x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]};
+            planes8_to_tmem<PM>(planes + 8 * b + 4 * j, pitch, y);
+        }
+    }
 }
 // eight numbers of shared memory
 __device__ __forceinline__ void shared8(f2 (&v)[4], const float *p)

@@ -231,61 +231,62 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
 #pragma unroll
             for (int i = 0; i < HC / 2; ++i) S[i] = make2(s[2 * i], s[2 * i + 1]);
         }
+        planes_to_tmem<PM, HC / 2>(lane_s, KD / 2, S);
         for (int i = 0; i < count; ++i) {
             const int c = last - 1 - i, s = i % C::STAGES;
             const unsigned par = i & 1;
             const float *gates = (const float *)(sm + s * C::STAGE + C::GATES) + 32 * half;
-            planes_to_tmem<PM, HC / 2>(lane_s, KD / 2, S);
             walk_ready(&ws.state[half], lane);
             if (RUN) keep_state(a.dstates + (bh * a.chunks + c) * kept_floats(a.Dv, a.Dk), S, row, a.Dv, half * HC, a.Dk);
             WAIT(&ws.full[s], (i / C::STAGES) & 1);
             WAIT(&ws.bar_a, par);
             tmem_fence_after_sync();
+            f2 x[16];
+            tmem_ld(x, lane_x);
+            Sixteen y[2];
+            y[0].load(lane_y);
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {                    // dU = P^T dY + delta dS k
-                f2 x[4], y[4], de[4];
-                tmem_ld8(x, lane_x + 8 * g);
-                tmem_ld8(y, lane_y + 8 * g);
-                shared8(de, gates + kTok + 8 * g);
+            for (int b = 0; b < 2; ++b) {                    // dU = P^T dY + delta dS k
                 tmem_wait_ld();
+                if (b == 0) y[1].load(lane_y + 16);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = row < rows ? fma2(de[e], x[e], phi ? pair(0.f) : y[e]) : pair(0.f);
-                planes8_to_tmem<PM>(lane_z + 4 * g, kTok / 2, x);
+                for (int g = 0; g < 2; ++g) {
+                    f2 u[4], de[4];
+                    shared8(de, gates + kTok + 16 * b + 8 * g);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) u[e] = row < rows ? fma2(de[e], x[8 * b + 4 * g + e], phi ? pair(0.f) : y[b].get(4 * g + e)) : pair(0.f);
+                    planes8_to_tmem<PM>(lane_z + 8 * b + 4 * g, kTok / 2, u);
+                }
             }
             walk_ready(&ws.z_ready, lane);
             const f2 fade = pair(((const float *)(sm + s * C::STAGE + C::GATES))[kTok - 1]);
             WAIT(&ws.bar_b, par);
             tmem_fence_after_sync();
+            tmem_ld(x, lane_x);
+            tmem_wait_ld();
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                f2 x[4], bg[4];
-                tmem_ld8(x, lane_x + 8 * g);
+                f2 z[4], bg[4];
                 shared8(bg, gates + 3 * kTok + 8 * g);
-                tmem_wait_ld();
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = mul2(x[e], bg[e]);
-                planes8_to_tmem<PM>(lane_z + 4 * g, kTok / 2, x);
+                for (int e = 0; e < 4; ++e) z[e] = mul2(x[4 * g + e], bg[e]);
+                planes8_to_tmem<PM>(lane_z + 4 * g, kTok / 2, z);
             }
             walk_ready(&ws.u_ready, lane);
             WAIT(&ws.bar_c[half], par);
             tmem_fence_after_sync();
-#pragma unroll
-            for (int e = 0; e < HC / 2; e += 16) {
-                f2 x[16];
-                tmem_ld(x, lane_d + 2 * e);
-                tmem_wait_ld();
-#pragma unroll
-                for (int j = 0; j < 16; ++j) S[e + j] = fma2(fade, S[e + j], x[j]);
-            }
+            state_onwards<PM>(S, fade, lane_d, lane_s, KD / 2);
         }
+        tmem_wait_st();
         auto flat = [&](float (&s)[HC]) {
 #pragma unroll
             for (int i = 0; i < HC / 2; ++i) split2(S[i], s[2 * i], s[2 * i + 1]);
         };
         if (!RUN) {
-            float *to = a.maps + (bh * a.segments + segment) * (long long)(a.Dv + a.Dk) * a.Dk + (phi ? states : 0), s[HC];
+            const int pitch = map_pitch(a.Dk);
+            float *to = a.maps + ((bh * a.segments + segment) * (a.Dv + a.Dk) + (phi ? a.Dv : 0)) * (long long)pitch, s[HC];
             flat(s);
-            store_state<HC>(to, s, row, rows, half * HC, a.Dk);
+            store_state<HC>(to, s, row, rows, half * HC, pitch);
         } else {
             if (a.ds0 && segment == 0) {
                 float s[HC];
