@@ -28,9 +28,9 @@ template <int N, int THREADS, bool FIRST> __device__ __forceinline__ void merge(
 {
     constexpr int EACH = N * N / THREADS;                    // 4 or 8
     const int r = r0 + N + t / (N / EACH), c = r0 + t % (N / EACH) * EACH;
-    float acc[EACH];
+    f2 acc[EACH / 2];
 #pragma unroll
-    for (int e = 0; e < EACH; ++e) acc[e] = 0.f;
+    for (int e = 0; e < EACH / 2; ++e) acc[e] = pair(0.f);
     // first: sum over m of T[r][r0 + m] B[r0 + m][c]; then: of inverse[r][r0 + N + m] C[r0 + N + m][c]
     const float *left = T + r * row + (FIRST ? r0 : r0 + N), *right = T + (FIRST ? r0 : r0 + N) * row + c;
 #pragma unroll 2
@@ -42,14 +42,16 @@ template <int N, int THREADS, bool FIRST> __device__ __forceinline__ void merge(
 #pragma unroll
             for (int e = 0; e < EACH; e += 4) {
                 const float4 w = *(const float4 *)(right + (m + i) * row + e);
-                acc[e] = fmaf(lm[i], w.x, acc[e]); acc[e + 1] = fmaf(lm[i], w.y, acc[e + 1]);
-                acc[e + 2] = fmaf(lm[i], w.z, acc[e + 2]); acc[e + 3] = fmaf(lm[i], w.w, acc[e + 3]);
+                acc[e / 2] = fma2(pair(lm[i]), make2(w.x, w.y), acc[e / 2]);
+                acc[e / 2 + 1] = fma2(pair(lm[i]), make2(w.z, w.w), acc[e / 2 + 1]);
             }
     }
     __syncthreads();
 #pragma unroll
-    for (int e = 0; e < EACH; e += 4)
-        *(float4 *)(T + r * row + c + e) = FIRST ? make_float4(acc[e], acc[e + 1], acc[e + 2], acc[e + 3]) : make_float4(-acc[e], -acc[e + 1], -acc[e + 2], -acc[e + 3]);
+    for (int e = 0; e < EACH / 2; e += 2) {
+        const f2 p = FIRST ? acc[e] : mul2(acc[e], pair(-1.f)), q = FIRST ? acc[e + 1] : mul2(acc[e + 1], pair(-1.f));
+        *(float4 *)(T + r * row + c + 2 * e) = make_float4(p.x, p.y, q.x, q.y);
+    }
     __syncthreads();
 }
 
@@ -125,16 +127,21 @@ template <typename T, int KD> __global__ void __launch_bounds__(128) delta_prepa
 #pragma unroll 2
         for (int g = 0; g < 8; ++g) {
             float x[8];
-            tmem_ld8(x, at_row + 8 * g);
-            tmem_wait_ld();
-            const float4 h0 = *(const float4 *)(hi + 8 * g), h1 = *(const float4 *)(hi + 8 * g + 4), l0 = *(const float4 *)(lo + 8 * g), l1 = *(const float4 *)(lo + 8 * g + 4);
-            const float hj[8] = {h0.x, h0.y, h0.z, h0.w, h1.x, h1.y, h1.z, h1.w}, lj[8] = {l0.x, l0.y, l0.z, l0.w, l1.x, l1.y, l1.z, l1.w};
-            // (a later token's ratio is of no use and may be no number)
+            if (g >= 4 && !(warp & 1)) {                      // rows 0 .. 31 have nothing there
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int j = 8 * g + e;
-                const float r = ratio(Hi, Li, hj[e], lj[e]);
-                x[e] = warp < 2 ? (j < i ? bi * r * x[e] : 0.f) : (j <= i ? r * x[e] : 0.f);
+                for (int e = 0; e < 8; ++e) x[e] = 0.f;
+            } else {
+                tmem_ld8(x, at_row + 8 * g);
+                tmem_wait_ld();
+                const float4 h0 = *(const float4 *)(hi + 8 * g), h1 = *(const float4 *)(hi + 8 * g + 4), l0 = *(const float4 *)(lo + 8 * g), l1 = *(const float4 *)(lo + 8 * g + 4);
+                const float hj[8] = {h0.x, h0.y, h0.z, h0.w, h1.x, h1.y, h1.z, h1.w}, lj[8] = {l0.x, l0.y, l0.z, l0.w, l1.x, l1.y, l1.z, l1.w};
+                // (a later token's ratio is of no use and may be no number)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int j = 8 * g + e;
+                    x[e] *= ratio(Hi, Li, hj[e], lj[e]);
+                    x[e] = warp < 2 ? (j < i ? bi * x[e] : 0.f) : (j <= i ? x[e] : 0.f);
+                }
             }
             if (warp < 2) {
                 *(float4 *)(Ts + i * C::TROW + 8 * g) = make_float4(x[0], x[1], x[2], x[3]);
@@ -384,8 +391,8 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             float s[HC];
 #pragma unroll
             for (int i = 0; i < HC; ++i) s[i] = phi && row == half * HC + i && row < a.Dk ? 1.f : 0.f;
-            const float *from = a.segments > 1 ? a.starts + (bh * a.segments + segment) * states : a.s0 ? a.s0 + bh * states : nullptr;
-            if (RUN && from) load_state<HC>(s, from, row, a.Dv, half * HC, a.Dk);
+            if (RUN && a.segments > 1) load_kept<HC>(s, a.starts + (bh * a.segments + segment) * kept_floats(a.Dv, a.Dk), row, a.Dv, half * HC, a.Dk);
+            else if (RUN && a.s0) load_state<HC>(s, a.s0 + bh * states, row, a.Dv, half * HC, a.Dk);
 #pragma unroll
             for (int i = 0; i < HC / 2; ++i) S[i] = make2(s[2 * i], s[2 * i + 1]);
         }
@@ -515,14 +522,11 @@ __global__ void __launch_bounds__(256) delta_join_kernel(DeltaArgs a, const floa
             if (4 * quad + e < a.Dk) { const float *p = from + bh * states + (long long)row * a.Dk + 4 * quad + e; HN_G(p, 4); mine[e] = *p; }
     for (int i = 0, s = reverse ? n - 1 : 0; i < n; ++i, s += step) {
         *(float4 *)&S[eighth][4 * quad] = v;
-        if (row < a.Dv)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (4 * quad + e < a.Dk) {
-                    float *p = a.starts + (bh * n + s) * states + (long long)row * a.Dk + 4 * quad + e;
-                    HN_G(p, 4);
-                    *p = mine[e];
-                }
+        if (row < kept_rows(a.Dv) && 4 * quad < a.Dk) {
+            float4 *p = (float4 *)(a.starts + (bh * n + s) * kept_floats(a.Dv, a.Dk)) + kept_at(row, quad, kept_rows(a.Dv));
+            HN_G(p, 16);
+            *p = v;
+        }
         if (i == n - 1) break;
         float4 add = make_float4(0.f, 0.f, 0.f, 0.f);
         if (row < a.Dv && 4 * quad < pitch) { const float4 *p = (const float4 *)(a.maps + (bh * n + s) * map + (long long)row * pitch) + quad; HN_G(p, 16); add = *p; }
@@ -632,7 +636,7 @@ DeltaSizes delta_sizes(const DeltaArgs &a, int dtype, bool backward)
     s.gates = up(chunks * kGates * 4);
     if (a.segments > 1) {
         s.maps = up(bh * a.segments * ((size_t)a.Dv + a.Dk) * map_pitch(a.Dk) * 4);
-        s.starts = up(bh * a.segments * (size_t)a.Dv * a.Dk * 4);
+        s.starts = up(bh * a.segments * (size_t)kept_floats(a.Dv, a.Dk) * 4);
     }
     if (backward) {
         s.dstates = up(chunks * (size_t)kept_floats(a.Dv, a.Dk) * 4);

@@ -49,7 +49,7 @@ struct DeltaArgs {
     // workspace
     unsigned char *images;                                // [B H][chunks]: planes of A, planes of P
     float *gates;                                         // [B H][chunks][6][64]
-    float *maps, *starts;                                 // [B H][segments][Dv + Dk][map_pitch], [B H][segments][Dv][Dk]
+    float *maps, *starts;                                 // [B H][segments][Dv + Dk][map_pitch], [B H][segments] states as kept
     float *dstates, *dz;                                  // [B H][chunks] states as kept, [B H][chunks][Dv][64]
     int B, H, Hk, L, Dk, Dv, decay, chunks, segments, per_segment;
     int copies;                                           // 1: tiles come as tensor copies
@@ -490,6 +490,20 @@ template <int C> __device__ __forceinline__ void keep_state(float *p, const f2 (
         to += rows8;
     }
 }
+template <int C> __device__ __forceinline__ void load_kept(float (&s)[C], const float *p, int row, int rows, int col, int D)
+{
+    const int rows8 = kept_rows(rows);
+#pragma unroll
+    for (int i = 0; i < C; i += 4) {
+        float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (row < rows8 && col + i < D) {
+            const float4 *from = (const float4 *)p + kept_at(row, (col + i) >> 2, rows8);
+            HN_G(from, 16);
+            w = *from;
+        }
+        s[i] = w.x; s[i + 1] = w.y; s[i + 2] = w.z; s[i + 3] = w.w;
+    }
+}
 // this thread's C columns from `col` of row `row` of a state [rows][D], zero outside it
 template <int C> __device__ __forceinline__ void load_state(float (&s)[C], const float *p, int row, int rows, int col, int D)
 {
@@ -573,7 +587,7 @@ __device__ __forceinline__ void chunk_sums(float *hi, float *lo, const float *g,
     }
 }
 // exp(G_i - G_j)
-__device__ __forceinline__ float ratio(float hi, float lo, float hj, float lj) { return exp2f((hi - hj) + (lo - lj)); }
+__device__ __forceinline__ float ratio(float hi, float lo, float hj, float lj) { return ex2((hi - hj) + (lo - lj)); }
 
 // ---- products ------------------------------------------------------------------------------------------------------------
 

@@ -226,8 +226,8 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             float s[HC];
 #pragma unroll
             for (int i = 0; i < HC; ++i) s[i] = phi && row == half * HC + i && row < a.Dk ? 1.f : 0.f;
-            const float *from = a.segments > 1 ? a.starts + (bh * a.segments + segment) * states : a.ds_end ? a.ds_end + bh * states : nullptr;
-            if (RUN && from) load_state<HC>(s, from, row, a.Dv, half * HC, a.Dk);
+            if (RUN && a.segments > 1) load_kept<HC>(s, a.starts + (bh * a.segments + segment) * kept_floats(a.Dv, a.Dk), row, a.Dv, half * HC, a.Dk);
+            else if (RUN && a.ds_end) load_state<HC>(s, a.ds_end + bh * states, row, a.Dv, half * HC, a.Dk);
 #pragma unroll
             for (int i = 0; i < HC / 2; ++i) S[i] = make2(s[2 * i], s[2 * i + 1]);
         }
