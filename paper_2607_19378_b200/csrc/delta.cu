@@ -405,7 +405,8 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             walk_ready(&ws.state[half], lane);
             f2 held[C::VALUES ? 1 : 16];                     // (fp32 values come from device memory: ahead of their use)
             if constexpr (!C::VALUES) load_row(held, (const float *)a.v, vhead + (long long)row * a.L + t, a.L, values ? n - t : 0);
-            if (RUN && a.marks) keep_state(a.marks + (bh * a.chunks + c) * kept_floats(a.Dv, a.Dk), S, row, a.Dv, half * HC, a.Dk);
+            float *mark = RUN && a.marks ? a.marks + (bh * a.chunks + c) * kept_floats(a.Dv, a.Dk) : nullptr;
+            if (mark) keep_state<0, HC / 16>(mark, S, row, a.Dv, half * HC, a.Dk);
             WAIT(&ws.full[s], (i / C::STAGES) & 1);
             WAIT(&ws.bar_a, par);
             tmem_fence_after_sync();
@@ -433,6 +434,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
                 planes8_to_tmem<PM>(lane_z + 4 * g, kTok / 2, z);
             }
             walk_ready(&ws.z_ready, lane);
+            if (mark) keep_state<HC / 16, HC / 8>(mark, S, row, a.Dv, half * HC, a.Dk);
             const f2 fade = pair(((const float *)(st + C::GATES))[kTok - 1]);
             WAIT(&ws.bar_b, par);
             tmem_fence_after_sync();
@@ -451,6 +453,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
                 planes_to_tmem<PM, 16>(lane_z, kTok / 2, x);
                 walk_ready(&ws.p_ready, lane);
             }
+            if (mark) keep_state<HC / 8, HC / 4>(mark, S, row, a.Dv, half * HC, a.Dk);
             WAIT(&ws.bar_c[half], par);
             tmem_fence_after_sync();
             state_onwards<PM>(S, fade, lane_d, lane_s, KD / 2);

@@ -476,14 +476,14 @@ template <typename T> __device__ __forceinline__ void store_row(T *p, long long 
 __host__ __device__ __forceinline__ int kept_rows(int rows) { return (rows + 7) & ~7; }
 __host__ __device__ __forceinline__ long long kept_floats(int rows, int D) { return (long long)kept_rows(rows) * ((D + 3) & ~3); }
 __device__ __forceinline__ int kept_at(int row, int quartet, int rows8) { return quartet * rows8 + (row ^ (quartet & 7)); }
-// (this thread's 2 C columns from `col`, a multiple of 32)
-template <int C> __device__ __forceinline__ void keep_state(float *p, const f2 (&s)[C], int row, int rows, int col, int D)
+// (columns 4 FROM .. 4 TO - 1 of this thread's 2 C from `col`, a multiple of 32)
+template <int FROM, int TO, int C> __device__ __forceinline__ void keep_state(float *p, const f2 (&s)[C], int row, int rows, int col, int D)
 {
     const int rows8 = kept_rows(rows);
     if (row >= rows8) return;
-    float4 *to = (float4 *)p + (col >> 2) * rows8;
+    float4 *to = (float4 *)p + ((col >> 2) + FROM) * rows8;
 #pragma unroll
-    for (int i = 0; i < C / 2; ++i) {
+    for (int i = FROM; i < TO; ++i) {
         if (col + 4 * i >= D) break;
         HN_G(to + (row ^ (i & 7)), 16);
         to[row ^ (i & 7)] = make_float4(s[2 * i].x, s[2 * i].y, s[2 * i + 1].x, s[2 * i + 1].y);

@@ -237,7 +237,8 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             const unsigned par = i & 1;
             const float *gates = (const float *)(sm + s * C::STAGE + C::GATES) + 32 * half;
             walk_ready(&ws.state[half], lane);
-            if (RUN) keep_state(a.dstates + (bh * a.chunks + c) * kept_floats(a.Dv, a.Dk), S, row, a.Dv, half * HC, a.Dk);
+            float *keep = RUN ? a.dstates + (bh * a.chunks + c) * kept_floats(a.Dv, a.Dk) : nullptr;
+            if (RUN) keep_state<0, HC / 16>(keep, S, row, a.Dv, half * HC, a.Dk);
             WAIT(&ws.full[s], (i / C::STAGES) & 1);
             WAIT(&ws.bar_a, par);
             tmem_fence_after_sync();
@@ -259,6 +260,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
                 }
             }
             walk_ready(&ws.z_ready, lane);
+            if (RUN) keep_state<HC / 16, HC / 8>(keep, S, row, a.Dv, half * HC, a.Dk);
             const f2 fade = pair(((const float *)(sm + s * C::STAGE + C::GATES))[kTok - 1]);
             WAIT(&ws.bar_b, par);
             tmem_fence_after_sync();
@@ -273,6 +275,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
                 planes8_to_tmem<PM>(lane_z + 4 * g, kTok / 2, z);
             }
             walk_ready(&ws.u_ready, lane);
+            if (RUN) keep_state<HC / 8, HC / 4>(keep, S, row, a.Dv, half * HC, a.Dk);
             WAIT(&ws.bar_c[half], par);
             tmem_fence_after_sync();
             state_onwards<PM>(S, fade, lane_d, lane_s, KD / 2);
