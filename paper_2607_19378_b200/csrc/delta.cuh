@@ -264,6 +264,12 @@ template <int PI> __device__ __forceinline__ void image8(float (&x)[8], const un
         }
     }
 }
+__device__ __forceinline__ void bf16_widen8(float (&x)[8], uint4 w)
+{
+    const unsigned u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(u[i] << 16); x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
+}
 // the numbers of a row of an image of a tensor: its planes' sum
 template <int PI> __device__ __forceinline__ void image_row(f2 (&x)[16], const unsigned char *image, int pitch, int row, int half)
 {

@@ -18,9 +18,9 @@ static __device__ int hn_delta_backward_status;
 
 template <typename T, int KD> struct WalkBack {
     static constexpr int PI = Planes<T>::IN, PM = Planes<T>::MID, TILE = KD * 128, TENSOR = PI * TILE;
-    static constexpr bool VALUES = PI == 1;                                   // dV travels as an image
+    static constexpr bool VALUES = PI == 1;                                   // dV and dZ's two planes travel as images
     static constexpr int IMAGES = 2 * PM * kMatrix, K = 0, Q = TENSOR, DY = 2 * TENSOR, A = 3 * TENSOR, GATES = A + IMAGES, STAGE = GATES + 1024;
-    static constexpr int OUT = VALUES ? 2 * TILE : 0;
+    static constexpr int OUT = VALUES ? 3 * TILE : 0;
     // (the product of dY and P takes 128 rows of dY's image: with 64 it reads on into the images that follow, for rows nothing looks at)
     static constexpr int STAGES = 3 * STAGE + OUT <= 220 * 1024 ? 3 : 2 * STAGE + OUT <= 220 * 1024 ? 2 : 1;
     static constexpr int BYTES = 1024 + STAGES * STAGE + OUT;
@@ -171,22 +171,32 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             }
             walk_ready(&ws.o_ready, lane);
             if (!RUN) continue;
-            unsigned char *image = sm + C::STAGES * C::STAGE + (i & 1) * C::TILE;
+            unsigned char *image = sm + C::STAGES * C::STAGE;
+            if (C::VALUES) {
+                if (tid == 384) tma_wait_read0();            // the images of the chunk before have been read
+                __syncwarp();
+                takers_sync();
+            }
             WAIT(&ws.bar_b, i & 1);
             tmem_fence_after_sync();
-            float4 *to = (float4 *)a.dz + (bh * a.chunks + c) * 16 * rows8 + row;          // dZ: [quartet of tokens][row]
+            float4 *to = (float4 *)a.dz + (bh * a.chunks + c) * 16 * rows8;     // dZ: two planes as images, or [quartet of tokens][row]
 #pragma unroll 2
             for (int e = 0; e < kTok; e += 8) {
                 f2 z[4], be[4];
                 tmem_ld8(z, lane_x + e);
                 shared8(be, gates + 2 * kTok + e);
                 tmem_wait_ld();
-                if (row < rows8) {
-                    HN_G(to, 16); HN_G(to + rows8, 16);
-                    to[0] = make_float4(z[0].x, z[0].y, z[1].x, z[1].y);
-                    to[rows8] = make_float4(z[2].x, z[2].y, z[3].x, z[3].y);
+                if constexpr (C::VALUES) {
+                    float x[8];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) split2(z[j], x[2 * j], x[2 * j + 1]);
+                    if (row < KD) planes8_to_image<PM>(image + C::TILE, C::TILE, row, e >> 3, x);
+                } else if (row < rows8) {
+                    float4 *at = to + (e >> 2) * rows8 + row;
+                    HN_G(at, 16); HN_G(at + rows8, 16);
+                    at[0] = make_float4(z[0].x, z[0].y, z[1].x, z[1].y);
+                    at[rows8] = make_float4(z[2].x, z[2].y, z[3].x, z[3].y);
                 }
-                to += 2 * rows8;
                 float y[8];                                  // dV: as an image that a copy takes away, or by these threads
 #pragma unroll
                 for (int j = 0; j < 4; ++j) split2(mul2(z[j], be[j]), y[2 * j], y[2 * j + 1]);
@@ -196,15 +206,18 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
                 __syncwarp();
             }
             walk_ready(&ws.o_taken, lane);                   // (the gates have been read as well)
-            if (stored) {
+            if (C::VALUES) {
                 fence_async_smem();
                 takers_sync();
                 if (tid == 384) {
-                    tma_store_3d(&maps.out, image, t, 0, (int)bh);
+                    if (stored) tma_store_3d(&maps.out, image, t, 0, (int)bh);
+                    for (int p = 0; p < 2; ++p) {
+                        HN_G((unsigned char *)to + p * rows8 * 128, rows8 * 128);
+                        bulk_store((unsigned char *)to + p * rows8 * 128, image + (p + 1) * C::TILE, rows8 * 128);
+                    }
                     tma_commit();
-                    tma_wait_read1();                        // the other image is free again
                 }
-                takers_sync();
+                __syncwarp();
             }
         }
         if (RUN) {
@@ -212,7 +225,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
 #pragma unroll 1
             for (int t = kTok * (first > last ? first : last); t < kTok * end; t += 8)
                 if (real && t < a.L) store8<T>((T *)a.dv, vrow + t, a.L, a.L - t, 0, none);
-            if (stored && tid == 384) tma_wait_all0();
+            if (C::VALUES && tid == 384) tma_wait_all0();
         }
         tmem_fence_before_sync();
     } else {
@@ -311,11 +324,11 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
 
 template <typename T, int KD> struct Grads {
     static constexpr int PI = Planes<T>::IN, PM = Planes<T>::MID, TILE = KD * 128;
-    // images: dY | K | Q | U (values before it, dQ and dK behind it) | dZ (later E) | A (later F), and a state as it is kept.  With three planes
-    // there is no room for the last, and Q comes into dY's place once that is through.
+    // images: dY | K | Q | U (values before it, dK in its second half behind it) | dZ (later E) | A (later F) | dQ, and a state as it is kept.
+    // With three planes there is no room for the last two, and Q comes into dY's place once that is through.
     static constexpr bool ROOM = PI == 1;
-    static constexpr int DY = 0, K = PI * TILE, Q = ROOM ? 2 * PI * TILE : DY, U = (ROOM ? 3 : 2) * PI * TILE, DZ = U + PM * TILE, A = DZ + PM * TILE, STATE = A + PM * kMatrix,
-                         BYTES = 1024 + STATE + (ROOM ? KD * KD * 4 : 0);
+    static constexpr int DY = 0, K = PI * TILE, Q = ROOM ? 2 * PI * TILE : DY, U = (ROOM ? 3 : 2) * PI * TILE, DZ = U + PM * TILE, A = DZ + PM * TILE, OUT = A + PM * kMatrix,
+                         STATE = OUT + (ROOM ? TILE : 0), BYTES = 1024 + STATE + (ROOM ? KD * KD * 4 : 0);
     // tensor memory: a state as an operand | sums of 64 columns:
     //     0: S0 k, U, the rest of dZ U^T   1: Z (and the next), dY U^T and dZ U^T   2: K K^T, the written part of dK but for dS1 u
     //     3: S0 dZ, the erased part of dK   4: S0 dY, dQ   5 (0 where there is no rest): dS1 u
@@ -379,7 +392,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
     auto copy_rest = [&](const Unit &u, int which) {
         const long long bh = head(u), at = bh * a.chunks + u.chunk;
         const bool copied = by_copy(a, u.nv, u.chunk * kTok);
-        mbar_expect_tx(&ws.full[0], PM * kMatrix + kGates * 4 + (copied ? (u.j ? 1 : 3) * C::TILE : 0));
+        mbar_expect_tx(&ws.full[0], PM * kMatrix + kGates * 4 + (C::ROOM ? rows8 * 256 : 0) + (copied ? (u.j ? 1 : 3) * C::TILE : 0));
         if (copied) {
             if (!u.j) tma_load_3d(sm + C::K, &maps.k, &ws.full[0], u.chunk * kTok, 0, (int)u.bk);
             tma_load_3d(sm + C::U, &maps.more, &ws.full[0], u.chunk * kTok, 0, (int)bh);
@@ -387,6 +400,8 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
         }
         bulk_load(gates2[which], a.gates + at * kGates, kGates * 4, &ws.full[0]);
         bulk_load(sm + C::A, a.images + at * (2 * PM * kMatrix), PM * kMatrix, &ws.full[0]);
+        if (C::ROOM)
+            for (int p = 0; p < 2; ++p) bulk_load(sm + C::DZ + p * C::TILE, (const unsigned char *)a.dz + (at * 2 + p) * rows8 * 128, rows8 * 128, &ws.full[0]);
     };
     pdl_wait();
     if (tid == 0) {
@@ -477,7 +492,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
             }
             load_tile<T>(sm + C::U, C::TILE, (const T *)a.v, bh * a.Dv * a.L + t0, vall, a.L, a.Dv, nv, tid, kGradThreads);
         }
-        {   // dZ as an image
+        if (!C::ROOM) {                                      // dZ as an image
             const float4 *from = (const float4 *)a.dz + (at * 16 + 4 * quarter) * rows8 + row;
             float4 w[4];
 #pragma unroll
@@ -512,6 +527,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
             planes8_to_tmem<PM>(lane_s + e / 2, KD / 2, s);
         }
         WAIT(&ws.full[0], phase);
+        if (C::ROOM) clear_rows(sm + C::DZ, C::TILE, PM, rows8, KD, tid, kGradThreads);
         go();
         if (warp == 0) {
             issue_ts<PM, PI, PM, true, KD / 16, B_ALL, 4>(tb + C::R0, tb + C::S0, KD / 2, IK, C::TILE, ksteps, kTok, false);
@@ -679,6 +695,13 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
             load_tile<T>(sm + C::Q, C::TILE, (const T *)a.q, qk, all, a.L, a.Dk, nv, tid, kGradThreads);
             clear_rows(sm + C::Q, C::TILE, PI, a.Dk, KD, tid, kGradThreads);
         }
+        uint4 qs[2], ks[2];
+        if (C::ROOM && row < KD)
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                qs[g] = *(const uint4 *)(sm + C::Q + image_at(row, 2 * quarter + g));
+                ks[g] = *(const uint4 *)(sm + C::K + image_at(row, 2 * quarter + g));
+            }
         go();
         if (warp == 0) {
             issue_ss<PI, PM, PM, false, false, kTok / 16, B_LOWER>(tb + C::R4, IK, C::TILE, 0, IA, kMatrix, kTok / 16, kTok, true);             // F k
@@ -688,6 +711,8 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
             umma_commit(&ws.bar_a);
         }
         done();
+        if (C::ROOM && more && tid == 0) copy_rest(then, phase ^ 1);     // (every product is through, and what the threads read they have)
+        __syncwarp();
         float written = 0.f;
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
@@ -700,14 +725,16 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
             tmem_ld8(w, lane_r + C::R2 + 8 * g);
             tmem_ld8(u, lane_r + C::R5 + 8 * g);
             shared8(de, delta + c);
-            if (row < KD) image8<PI>(z, sm + C::Q, C::TILE, row, c >> 3);
+            if (C::ROOM) bf16_widen8(z, qs[g]);
+            else if (row < KD) image8<PI>(z, sm + C::Q, C::TILE, row, c >> 3);
             tmem_wait_ld();
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 dq[g][e] += x[e];
                 x[e] = in ? x[e] * z[e] : 0.f;
             }
-            if (row < KD) image8<PI>(z, sm + C::K, C::TILE, row, c >> 3);
+            if (C::ROOM) bf16_widen8(z, ks[g]);
+            else if (row < KD) image8<PI>(z, sm + C::K, C::TILE, row, c >> 3);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 u[e] *= e & 1 ? de[e / 2].y : de[e / 2].x;
@@ -718,10 +745,10 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
             }
             const float sum = column_sum8(x, lane);
             if (!(lane & 3)) sums[1][warp & 3][c + (lane >> 2)] = sum;
-            if (last) {                                      // U is through: the results into its place
+            if (last) {                                      // U is through: dK into half of its place
                 if (C::ROOM && a.copies) {
                     if (row < KD) {
-                        *(uint4 *)(sm + C::U + image_at(row, 2 * quarter + g)) = bf16_8(dq[g], now.n - t - 8 * g);
+                        *(uint4 *)(sm + C::OUT + image_at(row, 2 * quarter + g)) = bf16_8(dq[g], now.n - t - 8 * g);
                         *(uint4 *)(sm + C::U + C::TILE + image_at(row, 2 * quarter + g)) = bf16_8(dk[g], now.n - t - 8 * g);
                     }
                 } else if (in && t + 8 * g < a.L) {
@@ -740,13 +767,13 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
         tmem_fence_after_sync();
         if (tid == 128) {
             if (last && C::ROOM && a.copies) {
-                tma_store_3d(&maps.out, sm + C::U, t0, 0, (int)now.bk);
+                tma_store_3d(&maps.out, sm + C::OUT, t0, 0, (int)now.bk);
                 tma_store_3d(&maps.outk, sm + C::U + C::TILE, t0, 0, (int)now.bk);
                 tma_commit();
-                tma_wait_read0();
+                tma_wait_read0();                            // (U is formed anew behind the next barriers)
             }
-            if (more) {
-                if (!C::ROOM) copy_early(then);
+            if (!C::ROOM && more) {
+                copy_early(then);
                 copy_rest(then, phase ^ 1);
             }
         }
