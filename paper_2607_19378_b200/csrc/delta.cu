@@ -408,6 +408,10 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             float *mark = RUN && a.marks ? a.marks + (bh * a.chunks + c) * kept_floats(a.Dv, a.Dk) : nullptr;
             if (mark) keep_state<0, HC / 16>(mark, S, row, a.Dv, half * HC, a.Dk);
             WAIT(&ws.full[s], (i / C::STAGES) & 1);
+            uint4 packed[C::VALUES ? 4 : 1];
+            if constexpr (C::VALUES)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) packed[g] = values ? *(const uint4 *)(st + C::V + image_at(row, 4 * half + g)) : make_uint4(0, 0, 0, 0);
             WAIT(&ws.bar_a, par);
             tmem_fence_after_sync();
             f2 x[16];
@@ -416,13 +420,8 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
 #pragma unroll
             for (int g = 0; g < 4; ++g) {                    // Z = beta v - beta gamma S k
                 f2 z[4], be[4], bg[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) z[e] = pair(0.f);
                 if constexpr (C::VALUES) {
-                    if (values) {
-                        const uint4 w = *(const uint4 *)(st + C::V + image_at(row, 4 * half + g));
-                        z[0] = widen2(w.x); z[1] = widen2(w.y); z[2] = widen2(w.z); z[3] = widen2(w.w);
-                    }
+                    z[0] = widen2(packed[g].x); z[1] = widen2(packed[g].y); z[2] = widen2(packed[g].z); z[3] = widen2(packed[g].w);
                 } else {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) z[e] = held[4 * g + e];

@@ -80,9 +80,10 @@ __device__ __forceinline__ void tmem_st8(unsigned at, const float (&v)[8])
                  ::"r"(at), "r"(__float_as_uint(v[0])), "r"(__float_as_uint(v[1])), "r"(__float_as_uint(v[2])), "r"(__float_as_uint(v[3])), "r"(__float_as_uint(v[4])),
                    "r"(__float_as_uint(v[5])), "r"(__float_as_uint(v[6])), "r"(__float_as_uint(v[7])) : "memory");
 }
+// (not "memory": loads of shared memory behind it may go ahead; the wait for stores is)
 __device__ __forceinline__ void tmem_st4(unsigned at, const unsigned (&v)[4])
 {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]));
 }
 
 // a pair of numbers as PM planes of bf16 pairs, each the rest of the ones before, rounded to nearest (so that a rest has either sign
