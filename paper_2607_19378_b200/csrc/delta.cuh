@@ -100,19 +100,6 @@ template <int PM> __device__ __forceinline__ void split_pair(f2 x, unsigned (&w)
 template <int PM> __device__ __forceinline__ void split_pair(float x, float y, unsigned (&w)[PM]) { split_pair<PM>(make2(x, y), w); }
 
 // 2 C numbers of this thread's row as the A operand in tensor memory: C columns per plane, planes `pitch` columns apart
-template <int PM, int C> __device__ __forceinline__ void planes_to_tmem(unsigned at, int pitch, const float (&x)[2 * C])
-{
-    float w[PM][C];
-#pragma unroll
-    for (int i = 0; i < C; ++i) {
-        unsigned u[PM];
-        split_pair<PM>(x[2 * i], x[2 * i + 1], u);
-#pragma unroll
-        for (int p = 0; p < PM; ++p) w[p][i] = __uint_as_float(u[p]);
-    }
-#pragma unroll
-    for (int p = 0; p < PM; ++p) TmemIO<C>::st(at + p * pitch, w[p]);
-}
 template <int PM, int C> __device__ __forceinline__ void planes_to_tmem(unsigned at, int pitch, const f2 (&x)[C])
 {
     float w[PM][C];
@@ -133,23 +120,6 @@ __device__ __forceinline__ void tmem_ld(f2 (&v)[16], unsigned at)
     TmemIO<32>::ld(x, at);
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = make2(x[2 * i], x[2 * i + 1]);
-}
-__device__ __forceinline__ void tmem_st(unsigned at, const f2 (&v)[16])
-{
-    float x[32];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) split2(v[i], x[2 * i], x[2 * i + 1]);
-    TmemIO<32>::st(at, x);
-}
-// v[i] *= by[i], 32 numbers of shared memory
-__device__ __forceinline__ void scale(f2 (&v)[16], const float *by)
-{
-#pragma unroll
-    for (int i = 0; i < 16; i += 2) {
-        const float4 w = *(const float4 *)(by + 2 * i);
-        v[i] = mul2(v[i], make2(w.x, w.y));
-        v[i + 1] = mul2(v[i + 1], make2(w.z, w.w));
-    }
 }
 // the same eight columns at a time
 __device__ __forceinline__ void tmem_ld8(f2 (&v)[4], unsigned at)
@@ -210,18 +180,6 @@ __device__ __forceinline__ void shared8(f2 (&v)[4], const float *p)
     const float4 a = *(const float4 *)p, b = *(const float4 *)(p + 4);
     v[0] = make2(a.x, a.y); v[1] = make2(a.z, a.w); v[2] = make2(b.x, b.y); v[3] = make2(b.z, b.w);
 }
-// 32 numbers, tokens 32 half .. of row `row` of an image
-template <int PM> __device__ __forceinline__ void planes_to_image(unsigned char *image, int pitch, int row, int half, const float (&x)[32])
-{
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-        unsigned u[4][PM];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) split_pair<PM>(x[8 * c + 2 * i], x[8 * c + 2 * i + 1], u[i]);
-#pragma unroll
-        for (int p = 0; p < PM; ++p) *(uint4 *)(image + p * pitch + image_at(row, half * 4 + c)) = make_uint4(u[0][p], u[1][p], u[2][p], u[3][p]);
-    }
-}
 // eight numbers as planes: into tensor memory (four columns each), into chunk `chunk` of row `row` of an image
 template <int PM> __device__ __forceinline__ void planes8_to_tmem(unsigned at, int pitch, const float (&x)[8])
 {
@@ -270,22 +228,6 @@ __device__ __forceinline__ void bf16_widen8(float (&x)[8], uint4 w)
     const unsigned u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(u[i] << 16); x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
-}
-// the numbers of a row of an image of a tensor: its planes' sum
-template <int PI> __device__ __forceinline__ void image_row(f2 (&x)[16], const unsigned char *image, int pitch, int row, int half)
-{
-#pragma unroll
-    for (int c = 0; c < 4; ++c)
-#pragma unroll
-        for (int p = PI - 1; p >= 0; --p) {
-            const uint4 w = *(const uint4 *)(image + p * pitch + image_at(row, half * 4 + c));
-            const unsigned u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const f2 v = make2(__uint_as_float(u[i] << 16), __uint_as_float(u[i] & 0xffff0000u));
-                x[4 * c + i] = p == PI - 1 ? v : add2(x[4 * c + i], v);
-            }
-        }
 }
 
 // ---- tensors in device memory ---------------------------------------------------------------------------------------
@@ -406,26 +348,7 @@ __device__ __forceinline__ void load_row(f2 (&x)[16], const float *p, long long 
         }
     }
 }
-// eight tokens of one row from element `at`, zero from the nv-th on; and eight stored, the first `room` of them
-template <typename T> __device__ __forceinline__ void load8(float (&x)[8], const T *p, long long at, long long n, int L, int nv)
-{
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = 0.f;
-    if (nv <= 0) return;
-    if constexpr (sizeof(T) == 2) {
-        uint4 w;
-        if (L % 8 == 0) { HN_G(p + at, 16); w = __ldg((const uint4 *)(p + at)); }
-        else w = load_unaligned(p, at, n);
-        if (nv < 8) w = keep_first(w, nv);
-        const unsigned u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(u[i] << 16); x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < nv) x[i] = IO<T>::ld(p, at + i);
-    }
-}
+// eight tokens of one row, the first `room` of them; from the nv-th on they are zero
 template <typename T> __device__ __forceinline__ void store8(T *p, long long at, int L, int room, int nv, const float (&x)[8])
 {
     constexpr int V = 16 / sizeof(T);
@@ -455,27 +378,6 @@ __device__ __forceinline__ uint4 bf16_8(const float (&x)[8], int nv)
         u[i] = *(const unsigned *)&r;
     }
     return make_uint4(u[0], u[1], u[2], u[3]);
-}
-// the first `room` of 32 tokens of one row; from token nv on they are zero
-template <typename T> __device__ __forceinline__ void store_row(T *p, long long at, int L, int room, int nv, const f2 (&x)[16])
-{
-    constexpr int V = 16 / sizeof(T);
-    if (L % V == 0) {
-#pragma unroll
-        for (int c = 0; c < 32 / V; ++c) {
-            if (c * V >= room) break;
-            uint4 w;
-            T *e = (T *)&w;
-#pragma unroll
-            for (int i = 0; i < V; ++i) e[i] = (T)(c * V + i < nv ? (i & 1 ? x[(c * V + i) / 2].y : x[(c * V + i) / 2].x) : 0.f);
-            HN_G(p + at + c * V, 16);
-            *(uint4 *)(p + at + c * V) = w;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 32; ++i)
-            if (i < room) IO<T>::st(p, at + i, i < nv ? (i & 1 ? x[i / 2].y : x[i / 2].x) : 0.f);
-    }
 }
 // A state that stays inside the library (marks, the gradient behind a chunk): column quartets [D / 4][rows], the rows of a group of eight
 // exchanged by the quartet.  Threads that hold rows write and read it in whole lines; from shared memory both rows and columns come
@@ -543,21 +445,6 @@ template <int C> __device__ __forceinline__ void store_state(float *p, const flo
     }
 }
 
-// 32 tokens of a row as an image of a bf16 tensor's tile, zero from token nv on
-__device__ __forceinline__ void row_to_image(unsigned char *image, int row, int half, int nv, const f2 (&x)[16])
-{
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-        unsigned u[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int e = 8 * c + 2 * i;
-            const __nv_bfloat162 r = __floats2bfloat162_rn(e < nv ? x[e / 2].x : 0.f, e + 1 < nv ? x[e / 2].y : 0.f);
-            u[i] = *(const unsigned *)&r;
-        }
-        *(uint4 *)(image + image_at(row, half * 4 + c)) = make_uint4(u[0], u[1], u[2], u[3]);
-    }
-}
 
 // ---- a chunk's decays ---------------------------------------------------------------------------------------------------
 
