@@ -194,9 +194,13 @@ template <typename T, bool VEC> __device__ __forceinline__ void fill_table(const
     }
 }
 
+__device__ __forceinline__ void prefetch_line(const void *p) { asm volatile("prefetch.global.L2 [%0];\n" ::"l"(p)); }
+
 // R groups of eight lanes to a head, P pairs of channels to a lane; 32 / R heads at a time.  Two pairs for fp32, four for bf16 heads of more
 // than 32 channels: what a unit costs beside its elements (shuffles, the meeting, rho) is then shared by more of them (the vision grid
-// forward 131 -> 91 us, 262144 tokens of 128 channels each way 393 + 535 -> 252 + 476; of one pair 267 us and more).
+// forward 131 -> 91 us, 262144 tokens of 128 channels each way 393 + 535 -> 252 + 476; of one pair 267 us and more).  With four pairs
+// there are one or two CTAs to an SM, too few loads on their way: the next unit's rows are fetched into L2 meanwhile (91 -> 79 us,
+// 252 + 464 -> 220 + 406; with two pairs, where there are enough, it costs: 250 + 356 -> 275 + 463 us).
 constexpr int resident(int pairs, bool backward) { return pairs > 2 ? (backward ? 1 : 2) : backward ? 2 : 3; }          // CTAs an SM, by registers
 template <typename T, int R, int P, bool BWD, bool VEC> __global__ void __launch_bounds__(256, resident(P, BWD)) heads_kernel(HeadsArgs a)
 {
@@ -273,6 +277,23 @@ template <typename T, int R, int P, bool BWD, bool VEC> __global__ void __launch
                             rx[p][s].load(in + o, t0, vc, r + R * p < half ? live : 0);
                             if constexpr (BWD) rd[p][s].load(gradient + o, t0, vc, r + R * p < half ? live : 0);
                         }
+                    if constexpr (P > 2 && VEC) {                  // the rows of the unit after, of the next tile behind the last, into L2
+                        const bool same = u + HEADS + group < end;
+                        const long long begin = end < to ? end : from;           // where the loop over units goes on
+                        const int bn = same ? b : (int)(begin / HT), hn = same ? h : (int)(begin - bn * (long long)HT), tn = same || end < to ? t0 : t0 + (int)gridDim.x * TOKENS;
+                        int k;
+                        const long long next = place_of(bn, hn, k);
+                        if (vc == 0 && (same || (tn < a.T && begin + group < to)))
+#pragma unroll
+                            for (int p = 0; p < P; ++p)
+#pragma unroll
+                                for (int s = 0; s < 2; ++s)
+                                    if (r + R * p < half) {
+                                        const long long o = next + (long long)(R * p + s * half) * a.T + tn;
+                                        prefetch_line((const T *)a.x[k] + o);
+                                        if constexpr (BWD) prefetch_line((const T *)a.dy[k] + o);
+                                    }
+                    }
                     if constexpr (BWD)
 #pragma unroll
                         for (int p = 0; p < P; ++p)
