@@ -1,10 +1,11 @@
 // The gated delta rule: forward pass, in chunks (formulas and number formats in delta.cuh).
 //
-// prepare: a CTA per chunk and head, all at once: k k^T and q k^T as one product of 128 rows, decays, A by forward substitution
-//     (a thread per column; fp32), A and P as planes into the workspace.
+// prepare: a CTA per chunk and head, all at once: k k^T and q k^T as one product of 128 rows, decays, A in fp32 (blocks of 16 by
+//     substitution, then merged in pairs), A and P as planes into the workspace.
 // walk: a CTA per head walks its chunks.  The state's rows are the lanes of tensor memory (Dv of 128), so that S^T products chain without a
 //     transposition: S k, then A Z, then the new state each take the result of the one before as their A operand in tensor memory, through
-//     registers (256 threads: a lane's columns in two halves).  The fp32 state stays in registers.  Four warps fetch the next chunks.
+//     registers (256 threads: a lane's columns in two halves).  The fp32 state stays in registers.  One warp issues the products, three
+//     fetch the next chunks, four take the results.
 // Few heads and many chunks: the walk is serial, so a head is cut into segments.  Where a segment starts from nothing it gives N, where it
 //     starts from the identity without values it gives Phi, and from any state S it ends at S Phi + N: both walks run for all
 //     segments at once, a small kernel joins them, and the walk proper starts every segment at once.
@@ -55,6 +56,9 @@ template <int N, int THREADS, bool FIRST> __device__ __forceinline__ void merge(
     __syncthreads();
 }
 
+// Read: a chunk's k and q; written: 16 KB of planes for each of A and P (bf16).  6144 chunks of 128 channels: 112 us, 0.3 GB, 2.7 TB/s.  It is
+// bound by the latency of its steps one after the other (copy, product, inverse, stores), which the few CTAs that an SM holds only partly
+// cover.  The inverse by blocks in place of 64 dependent steps took a batch of prompts, 192 heads of 64, from 319 to 230 us in all.
 template <typename T, int KD> __global__ void __launch_bounds__(128) delta_prepare_kernel(DeltaArgs a, const __grid_constant__ DeltaMaps maps)
 {
     using C = Prep<T, KD>;
@@ -222,6 +226,11 @@ template <typename T, int KD> struct Walk {
     static_assert(ROOM || (D1 + KD / 2 <= 512 && KD / 2 == kTok), "tensor memory");
 };
 
+// Bound by the chain of a chunk: S k, Z, A Z, the new state, each a product (some 300 to 700 cycles with its issue and its end's way back)
+// and a passage through registers (350 to 1300).  3.6 us a chunk of 128 channels with all SMs at work (96 heads of 4096 tokens: 232 us), whatever
+// the bytes: 0.5 GB, 2.3 TB/s.  What shortened it: y, its scaling and its stores on other warps (off the chain), the fp32 state in registers,
+// the columns of S in two halves so that S k begins with the first, kept states stored in thirds while products run (265 -> 242), values read
+// before the product they meet (242 -> 232).  Prefetches into L2 and more stages made it slower, as did anything that grew the code.
 template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkThreads, 1) delta_walk_kernel(DeltaArgs a, const __grid_constant__ DeltaMaps maps)
 {
     using C = Walk<T, KD>;
@@ -488,6 +497,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
 
 // States at the segments' starts from the maps S -> S Phi + N: eight rows to a CTA, Phi by bulk copies, the next one under way; a thread
 // sums four columns of all rows over an eighth of Phi's rows.  `reverse`: from the last segment to the first (the gradient's states).
+// Serial over the segments: 37 of 128 channels take 53 us, 1.4 us each, for 64 KB that every CTA reads from L2 and 128 x 128 x 8 fp32 products.
 constexpr int kJoinRows = 8, kJoinBytes = 2 * 128 * 128 * 4;
 __global__ void __launch_bounds__(256) delta_join_kernel(DeltaArgs a, const float *from, int reverse)
 {
@@ -571,7 +581,7 @@ __global__ void __launch_bounds__(256) delta_join_kernel(DeltaArgs a, const floa
 // ---- one token ------------------------------------------------------------------------------------------------------
 
 // W lanes to a row of the state, four columns each; the products with k and q are formed in one reading, the new state is written in
-// the same: bandwidth is the bound.  A decay next to 1 is applied as a - 1, so that thousands of tokens one by one cost a rounding each.
+// the same: bandwidth is the bound (64 sequences of 6 heads of 128 channels: 50 MB of states, 6.7 us where L2 holds them).  A decay next to 1 is applied as a - 1, so that thousands of tokens one by one cost a rounding each.
 template <typename T, int W> __global__ void __launch_bounds__(256) delta_step_kernel(DeltaArgs a)
 {
     constexpr int ROWS = 256 / W, EACH = 4;                  // rows at a time, and times

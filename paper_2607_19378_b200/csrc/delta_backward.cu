@@ -3,8 +3,8 @@
 // prepare: as in the forward pass.
 // walk: from the last chunk to the first, a CTA per head: the gradient of the state.  As in the forward walk its rows are the lanes of
 //     tensor memory and every product takes the one before as its operand there: dS k, then A^T dU, then the new dS.  It writes dV, dZ
-//     and the gradient behind every chunk.  Few heads and many chunks go in segments as there (dS0 = dS1 Phi + N).
-// gradients: a CTA per chunk and head of queries and keys, all at once: from the state before the chunk (the forward's mark) and the gradient
+//     (as images, for bf16) and the gradient behind every chunk.  Few heads and many chunks go in segments as there (dS0 = dS1 Phi + N).
+// gradients: a CTA an SM takes the chunks of the heads of queries and keys one after the other: from the state before the chunk (the forward's mark) and the gradient
 //     behind it, U again, then dQ, dK, and the sums over tokens for beta and the decay.  Value heads that share queries and keys follow
 //     one another in the CTA, so their sum has one order and needs no atomics.
 #include "delta.cuh"
@@ -32,6 +32,9 @@ template <typename T, int KD> struct WalkBack {
     static_assert((ROOM || (D1 + KD / 2 <= 512 && KD / 2 == kTok)) && BYTES + 1024 <= 227 * 1024, "tensor and shared memory");
 };
 
+// As the forward walk, bound by its chain: 252 us for 96 heads of 4096 tokens of 128 channels, 3.9 us a chunk.  dZ leaves as the two planes that
+// the gradients take, by copies out of shared memory (stored from registers in that order, 16 bytes a line, 281 us; in fp32 252 us, but
+// the gradients then paid 45 us for turning it).
 template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkThreads, 1) delta_walk_back_kernel(DeltaArgs a, const __grid_constant__ DeltaMaps maps)
 {
     using C = WalkBack<T, KD>;
@@ -356,6 +359,10 @@ __device__ __forceinline__ float column_sum8(float (&x)[8], int lane)
 
 // 512 threads: a lane's columns in four quarters of 16 tokens (KD / 4 of a state), taken eight at a time: the loops stay rolled, as code that
 // runs once per CTA is bound by its fetching (unrolled over 32 columns, 256 threads: 1350 us on 6144 chunks of 128 channels).
+// 525 us on those, 12.6 us a chunk: 1.7 GB, of which the kept states and gradients in fp32 are 0.8, so 3.2 TB/s, and some 150 products of 34
+// cycles, a fifth of the time.  What is left is the order of its six steps, each a write, a barrier, products, a reading.  The next chunk's
+// copies go out as soon as their places are free (588 -> 525).  A warp of its own for the products made it slower (645 us: 17 warps leave a
+// thread 96 registers, and the others run apart, through more code at a time).
 template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1) delta_gradients_kernel(DeltaArgs a, const __grid_constant__ DeltaMaps maps)
 {
     using C = Grads<T, KD>;
