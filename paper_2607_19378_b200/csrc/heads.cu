@@ -194,24 +194,36 @@ template <typename T, bool VEC> __device__ __forceinline__ void fill_table(const
     }
 }
 
-__device__ __forceinline__ void prefetch_line(const void *p) { asm volatile("prefetch.global.L2 [%0];\n" ::"l"(p)); }
 
 // R groups of eight lanes to a head, P pairs of channels to a lane; 32 / R heads at a time.  Two pairs for fp32, four for bf16 heads of more
 // than 32 channels: what a unit costs beside its elements (shuffles, the meeting, rho) is then shared by more of them (the vision grid
 // forward 131 -> 91 us, 262144 tokens of 128 channels each way 393 + 535 -> 252 + 476; of one pair 267 us and more).  With four pairs
-// there are one or two CTAs to an SM, too few loads on their way: the next unit's rows are fetched into L2 meanwhile (91 -> 79 us,
-// 252 + 464 -> 220 + 406; with two pairs, where there are enough, it costs: 250 + 356 -> 275 + 463 us).
+// there are one or two CTAs to an SM, too few loads on their way: the next unit's rows come by asynchronous copies meanwhile, each thread's
+// into places of its own (91 -> 75 us, 5.4 TB/s; 252 + 464 -> 210 + 375 us, 5.1 and 4.3 TB/s; fetched into L2 alone 79, 220 + 403).  With two
+// pairs there are enough loads as it is (fetches into L2: 250 + 356 -> 275 + 460 us); heads of more than 128 channels have no room beside
+// the table.
 constexpr int resident(int pairs, bool backward) { return pairs > 2 ? (backward ? 1 : 2) : backward ? 2 : 3; }          // CTAs an SM, by registers
+template <int R, int P, bool BWD, bool VEC> struct Staging {
+    static constexpr bool ON = VEC && P > 2 && R <= 16;
+    static constexpr int BYTES = ON ? 256 * 16 * 2 * P * (BWD ? 2 : 1) : 0;
+};
+__device__ __forceinline__ void copy16(void *to, const void *from, bool real)          // or zeros
+{
+    if (real) HN_G(from, 16);
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"((unsigned)__cvta_generic_to_shared(to)), "l"(from), "r"(real ? 16 : 0) : "memory");
+}
 template <typename T, int R, int P, bool BWD, bool VEC> __global__ void __launch_bounds__(256, resident(P, BWD)) heads_kernel(HeadsArgs a)
 {
     constexpr int V = Tile<T>::V, TOKENS = Tile<T>::TOKENS, HEADS = 32 / R, WARPS = R / 4, SUMS = BWD ? 2 : 1, N = V / 2;
+    constexpr bool STAGED = Staging<R, P, BWD, VEC>::ON;
     extern __shared__ __align__(16) float sm[];
     __shared__ double freq[kMaxD / 2];
     __shared__ int axis_of[kMaxD / 2];
     __shared__ float weights[2][kMaxD];
     __shared__ __align__(16) float meet[2][SUMS][8][TOKENS];       // [warp][lane of eight][V]
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, vc = lane & 7, group = warp / WARPS, r = (warp % WARPS) * 4 + (lane >> 3), half = a.D / 2;
-    float *cs = sm, *sn = cs + a.turned * TOKENS;
+    uint4 *const slot = (uint4 *)sm + tid;                         // one of every 256
+    float *cs = sm + Staging<R, P, BWD, VEC>::BYTES / 4, *sn = cs + a.turned * TOKENS;
     float *step_c = sn + a.turned * TOKENS, *step_s = step_c + a.turned * TOKENS;
     float2 *rows = (float2 *)(step_s + a.turned * TOKENS);
     pdl_join();
@@ -238,23 +250,42 @@ template <typename T, int R, int P, bool BWD, bool VEC> __global__ void __launch
     // units: the heads of q and k of one batch entry after the other; a split of them to a CTA
     const int HT = a.H[0] + a.H[1];
     const long long units = (long long)a.B * HT, per = (units + a.splits - 1) / a.splits, from = blockIdx.y * per, to = from + per < units ? from + per : units;
+    // a lane's rows: the channels r + R p and half further on, of the head that its group is at
+    const long long row0 = (long long)r * a.T;
+    auto place_of = [&](int b, int h, int &kind) {
+        h += group;
+        while (h >= HT) { h -= HT; ++b; }
+        kind = h >= a.H[0];
+        return ((long long)b * a.H[kind] + h - (kind ? a.H[0] : 0)) * a.D * (long long)a.T + row0;
+    };
+    auto end_of = [&](long long b0) { return a.positions && (b0 + 1) * HT < to ? (b0 + 1) * HT : to; };          // (positions are a batch entry's)
+    auto fetch = [&](int tile, long long u) {                      // this thread's part of the units from u on, into its own places
+        const long long b0 = u / HT;
+        int kind;
+        const long long at = place_of((int)b0, (int)(u - b0 * HT), kind);
+        const int t = tile * TOKENS + vc * V;
+        const bool in = u + group < end_of(b0) && t < a.T;
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const bool real = in && r + R * p < half;
+                const long long o = real ? at + (long long)(R * p + s * half) * a.T + t : 0;
+                copy16(slot + (2 * p + s) * 256, (const T *)a.x[kind] + o, real);
+                if constexpr (BWD) copy16(slot + (2 * P + 2 * p + s) * 256, (const T *)a.dy[kind] + o, real);
+            }
+    };
+    if constexpr (STAGED)
+        if (from < to && blockIdx.x < a.tiles) fetch(blockIdx.x, from);
     int turn = 0;
     for (int tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
         const int t0 = tile * TOKENS;
         for (long long u = from; u < to;) {
-            const long long b0 = u / HT, end = a.positions && (b0 + 1) * HT < to ? (b0 + 1) * HT : to;
+            const long long b0 = u / HT, end = end_of(b0);
             __syncthreads();                                       // (the table's readers are through; the steps are there)
             fill_table<T, VEC>(a, (int)b0, t0, cs, sn, step_c, step_s, rows, freq, axis_of, tid);
             __syncthreads();
             int b = (int)b0, h = (int)(u - b0 * HT);               // of the first of the units at a time
-            // a lane's rows: the channels r + R p and half further on, of the head that its group is at
-            const long long row0 = (long long)r * a.T;
-            auto place_of = [&](int b, int h, int &kind) {
-                h += group;
-                while (h >= HT) { h -= HT; ++b; }
-                kind = h >= a.H[0];
-                return ((long long)b * a.H[kind] + h - (kind ? a.H[0] : 0)) * a.D * (long long)a.T + row0;
-            };
 #pragma unroll 1
             for (; u < end; u += HEADS) {
                 int kind;
@@ -264,6 +295,7 @@ template <typename T, int R, int P, bool BWD, bool VEC> __global__ void __launch
                 while (h >= HT) { h -= HT; ++b; }
                 const T *in = (const T *)a.x[kind] + at, *gradient = (const T *)a.dy[kind] + at;
                 T *out = (T *)a.out[kind] + at;
+                if constexpr (STAGED) asm volatile("cp.async.wait_all;\n" ::: "memory");
                 // what was loaded stays as it came: bf16 values twice made fp32 cost less than the registers
                 Tokens<T, VEC> rx[P][2];
                 f2 d[BWD ? P : 1][2][N], s1[N], s2[BWD ? N : 1];
@@ -274,26 +306,14 @@ template <typename T, int R, int P, bool BWD, bool VEC> __global__ void __launch
 #pragma unroll
                         for (int s = 0; s < 2; ++s) {
                             const long long o = (long long)(R * p + s * half) * a.T;
-                            rx[p][s].load(in + o, t0, vc, r + R * p < half ? live : 0);
-                            if constexpr (BWD) rd[p][s].load(gradient + o, t0, vc, r + R * p < half ? live : 0);
+                            if constexpr (STAGED) {
+                                rx[p][s].w = slot[(2 * p + s) * 256];
+                                if constexpr (BWD) rd[p][s].w = slot[(2 * P + 2 * p + s) * 256];
+                            } else {
+                                rx[p][s].load(in + o, t0, vc, r + R * p < half ? live : 0);
+                                if constexpr (BWD) rd[p][s].load(gradient + o, t0, vc, r + R * p < half ? live : 0);
+                            }
                         }
-                    if constexpr (P > 2 && VEC) {                  // the rows of the unit after, of the next tile behind the last, into L2
-                        const bool same = u + HEADS + group < end;
-                        const long long begin = end < to ? end : from;           // where the loop over units goes on
-                        const int bn = same ? b : (int)(begin / HT), hn = same ? h : (int)(begin - bn * (long long)HT), tn = same || end < to ? t0 : t0 + (int)gridDim.x * TOKENS;
-                        int k;
-                        const long long next = place_of(bn, hn, k);
-                        if (vc == 0 && (same || (tn < a.T && begin + group < to)))
-#pragma unroll
-                            for (int p = 0; p < P; ++p)
-#pragma unroll
-                                for (int s = 0; s < 2; ++s)
-                                    if (r + R * p < half) {
-                                        const long long o = next + (long long)(R * p + s * half) * a.T + tn;
-                                        prefetch_line((const T *)a.x[k] + o);
-                                        if constexpr (BWD) prefetch_line((const T *)a.dy[k] + o);
-                                    }
-                    }
                     if constexpr (BWD)
 #pragma unroll
                         for (int p = 0; p < P; ++p)
@@ -335,6 +355,12 @@ template <typename T, int R, int P, bool BWD, bool VEC> __global__ void __launch
                             if constexpr (BWD) s2[e] = fma2(mul2(d[p][s][e], w), x[e], s2[e]);
                         }
                     }
+                }
+                if constexpr (STAGED) {                            // the copies have been read: the next unit's, of the next tile behind the last
+                    long long un = u + HEADS < end ? u + HEADS : end;
+                    int next = tile;
+                    if (un >= to) { un = from; next += gridDim.x; }
+                    if (next < a.tiles) fetch(next, un);
                 }
                 f2 rho[N];
                 if (a.norm == NORM_NONE) {
@@ -525,11 +551,11 @@ static int plan(HeadsArgs &a, int dtype, bool backward)
 
 // cosines and sines of a tile; of the steps of one; of its rows
 static size_t table_bytes(int turned, int tokens, int last) { return (size_t)turned * (16 * tokens + 8 * rows_of_tile(tokens, last)); }
-template <auto FN, typename T> static int launch_tiles(const HeadsArgs &a, int grid_x, cudaStream_t st)
+template <auto FN, typename T> static int launch_tiles(const HeadsArgs &a, int grid_x, int staging, cudaStream_t st)
 {
-    const size_t bytes = table_bytes(a.turned, Tile<T>::TOKENS, a.dims[a.ndim - 1]);
+    const size_t bytes = staging + table_bytes(a.turned, Tile<T>::TOKENS, a.dims[a.ndim - 1]);
     static PerDevice ready;
-    if (bytes > 24 * 1024 && !ready.once([] { return cudaFuncSetAttribute(FN, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)table_bytes(kMaxD / 2, Tile<T>::TOKENS, 1)) == cudaSuccess ? 1 : -1; }))
+    if (bytes > 24 * 1024 && !ready.once([&] { return cudaFuncSetAttribute(FN, cudaFuncAttributeMaxDynamicSharedMemorySize, staging + (int)table_bytes(staging ? 64 : kMaxD / 2, Tile<T>::TOKENS, 1)) == cudaSuccess ? 1 : -1; }))
         return kNoLaunch;
     launch_pdl(FN, dim3(grid_x, a.splits), 256, bytes, st, a);
     return 0;
@@ -545,7 +571,8 @@ template <typename T, bool BWD> static int launch_heads(HeadsArgs &a, int dtype,
     const int R = rows_of(a.D, dtype), gx = plan(a, dtype, BWD);
     const bool vec = a.T % Tile<T>::V == 0;
     int e = kNoLaunch;
-#define HN_HEADS(R_, P_) if (R == R_) e = vec ? launch_tiles<heads_kernel<T, R_, P_, BWD, true>, T>(a, gx, st) : launch_tiles<heads_kernel<T, R_, P_, BWD, false>, T>(a, gx, st)
+#define HN_HEADS(R_, P_) if (R == R_) e = vec ? launch_tiles<heads_kernel<T, R_, P_, BWD, true>, T>(a, gx, Staging<R_, P_, BWD, true>::BYTES, st) \
+                                 : launch_tiles<heads_kernel<T, R_, P_, BWD, false>, T>(a, gx, 0, st)
     if (pairs_of(a.D, dtype) == 4) {
         HN_HEADS(32, 4);
         if constexpr (sizeof(T) == 2) { HN_HEADS(8, 4); HN_HEADS(16, 4); }
