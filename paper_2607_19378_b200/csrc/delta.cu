@@ -270,7 +270,9 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             unsigned char *st = sm + s * C::STAGE;
             const bool copied = by_copy(a, nv, t0), values = C::VALUES && !phi;
             if (copied && ft) continue;                      // (one thread's work)
-            if (i >= C::STAGES) WAIT(&ws.empty[s], (i / C::STAGES - 1) & 1);
+            // one thread waits, for every chunk in turn: the others have passed over copied ones, and a barrier's parity tells them nothing
+            if (i >= C::STAGES && ft == 0) WAIT(&ws.empty[s], (i / C::STAGES - 1) & 1);
+            if (!copied) fetchers_sync();
             if (ft == 0) {
                 const long long at = bh * a.chunks + c;
                 const unsigned bytes = RUN ? C::IMAGES : C::IMAGES / 2, tiles = copied ? (RUN ? 2 : 1) * C::TENSOR + (values ? C::TILE : 0) : 0;

@@ -573,7 +573,7 @@ __device__ __forceinline__ void walk_ready(uint64_t *bar, int lane)
     __syncwarp();
     if (lane == 0) mbar_arrive(bar);
 }
-__device__ __forceinline__ void fetchers_sync() { asm volatile("bar.sync 3, %0;\n" ::"n"(kFetchers) : "memory"); }
+__device__ __forceinline__ void fetchers_sync() { __syncwarp(); asm volatile("bar.sync 3, %0;\n" ::"n"(kFetchers) : "memory"); }
 __device__ __forceinline__ void takers_sync() { asm volatile("bar.sync 2, 128;\n" ::: "memory"); }
 
 __device__ __forceinline__ unsigned char *align_images(unsigned char *p) { return p + ((1024u - (smem_u32(p) & 1023u)) & 1023u); }

@@ -75,7 +75,9 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             unsigned char *st = sm + s * C::STAGE;
             const bool copied = by_copy(a, nv, t0);
             if (copied && ft) continue;                      // (one thread's work)
-            if (i >= C::STAGES) WAIT(&ws.empty[s], (i / C::STAGES - 1) & 1);
+            // one thread waits, for every chunk in turn: the others have passed over copied ones, and a barrier's parity tells them nothing
+            if (i >= C::STAGES && ft == 0) WAIT(&ws.empty[s], (i / C::STAGES - 1) & 1);
+            if (!copied) fetchers_sync();
             if (ft == 0) {
                 const long long at = bh * a.chunks + c;
                 mbar_expect_tx(&ws.full[s], C::IMAGES + kWalkGates + (copied ? (phi ? 2 : 3) * C::TENSOR : 0));

@@ -116,6 +116,17 @@ def test_segments(shape, dtype, decay, ragged):
     check(shape, dtype, decay, 4, ragged)
 
 
+# rows that tensor copies read but for the last chunk, which ends inside: its threads have passed over the chunks before (every stage, early and late)
+@pytest.mark.parametrize("D", [64, 128])
+def test_ragged_rows_of_many_chunks(D):
+    shape = B, H, Hk, Dk, Dv, L = 10, 2, 1, D, D, 960
+    t = inputs(*shape, torch.bfloat16, "log", 12)
+    t["lengths"] = torch.tensor([900, 540, 300, 700, 959, 385, 449, 520, 960, 600], dtype=torch.int32)
+    got = run(t, shape, torch.bfloat16, "log")
+    ref = od.delta(t["q"], t["k"], t["v"], t["g"], t["beta"], "log", H, Hk, t["s0"], t["lengths"], t["dy"], t["ds"])
+    compare(got, ref, t, H, Hk, torch.bfloat16, [n for n in NAMES if n in got])
+
+
 # more heads than SMs, and a batch entry without tokens among them
 def test_many_heads():
     check((40, 4, 4, 16, 16, 130), "bf16", "log", 5, True)
