@@ -120,7 +120,10 @@ template <typename T, int KD> __global__ void __launch_bounds__(128) delta_prepa
         for (int e = 0; e < 6; ++e) { HN_G(gates + e * kTok + tid, 4); gates[e * kTok + tid] = x[e]; }
     }
     ok = mbar_wait(&bar, 0) && ok;
-    if (!ok) atomicExch(&hn_delta_status, 1);
+    if (!ok) {
+        atomicExch(&hn_delta_status, 1);
+        if (copied) mbar_wait(&there, 0);                     // (copies under way end before the CTA does)
+    }
     tmem_fence_after_sync();
     __syncthreads();                                          // (every thread has waited: the tiles' place is free)
     // lanes 0 .. 63: rows of k k^T, lanes 64 .. 127: rows of q k^T
@@ -273,7 +276,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             // one thread waits, for every chunk in turn: the others have passed over copied ones, and a barrier's parity tells them nothing
             if (i >= C::STAGES && ft == 0) WAIT(&ws.empty[s], (i / C::STAGES - 1) & 1);
             if (!copied) fetchers_sync();
-            if (ft == 0) {
+            if (ft == 0 && !walk_given_up(&ws)) {
                 const long long at = bh * a.chunks + c;
                 const unsigned bytes = RUN ? C::IMAGES : C::IMAGES / 2, tiles = copied ? (RUN ? 2 : 1) * C::TENSOR + (values ? C::TILE : 0) : 0;
                 mbar_expect_tx(&ws.full[s], bytes + kWalkGates + tiles);
@@ -488,9 +491,9 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
         tmem_fence_before_sync();
     }
     __syncthreads();
-    if (ws.gave_up && tid == 0) {                            // copies on their way end before the memory they go to is another CTA's
+    if (ws.gave_up && tid == 0) {
         atomicExch(&hn_delta_status, 1);
-        for (int s = 0; s < C::STAGES; ++s) mbar_wait(&ws.full[s], 0);
+        walk_drain(&ws, C::STAGES);
     }
     if (warp == 0) tmem_dealloc(tb, 512);
 }
@@ -569,7 +572,7 @@ __global__ void __launch_bounds__(256) delta_join_kernel(DeltaArgs a, const floa
 #pragma unroll
         for (int r = 0; r < R; ++r) *(float4 *)&part[eighth][r][4 * quad] = make_float4(acc[r][0].x, acc[r][0].y, acc[r][1].x, acc[r][1].y);
         __syncthreads();
-        if (tid == 0 && i + 2 < n - 1) fetch(i + 2);          // (every thread has read this one)
+        if (tid == 0 && i + 2 < n - 1 && !walk_given_up(&ws)) fetch(i + 2);          // (every thread has read this one)
         v = add;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -577,13 +580,18 @@ __global__ void __launch_bounds__(256) delta_join_kernel(DeltaArgs a, const floa
             v.x += p.x; v.y += p.y; v.z += p.z; v.w += p.w;
         }
     }
-    if (ws.gave_up && tid == 0) atomicExch(&hn_delta_status, 1);
+    __syncthreads();
+    if (ws.gave_up && tid == 0) {
+        atomicExch(&hn_delta_status, 1);
+        walk_drain(&ws, 2);
+    }
 }
 
 // ---- one token ------------------------------------------------------------------------------------------------------
 
 // W lanes to a row of the state, four columns each; the products with k and q are formed in one reading, the new state is written in
-// the same: bandwidth is the bound (64 sequences of 6 heads of 128 channels: 50 MB of states, 6.7 us where L2 holds them).  A decay next to 1 is applied as a - 1, so that thousands of tokens one by one cost a rounding each.
+// the same: bandwidth is the bound (32 sequences of 6 heads of 128 channels: 25 MB of states in and out, 6.6 us; 3.9 at the rate of a
+// copy).  A decay next to 1 is applied as a - 1, so that thousands of tokens one by one cost a rounding each.
 template <typename T, int W> __global__ void __launch_bounds__(256) delta_step_kernel(DeltaArgs a)
 {
     constexpr int ROWS = 256 / W, EACH = 4;                  // rows at a time, and times

@@ -566,6 +566,16 @@ __device__ __forceinline__ void walk_init(WalkShared *w, int stages)
     w->gave_up = 0;
     fence_mbar_init();
 }
+// A wait has given up: no more copies are begun, and whoever leaves last waits (bounded) for those under way, in whichever phase their barriers
+// are, so that they end before the memory they go to is another CTA's
+__device__ __forceinline__ bool walk_given_up(const WalkShared *w) { return *(const volatile int *)&w->gave_up; }
+__device__ __forceinline__ void walk_drain(WalkShared *w, int stages)
+{
+    for (int s = 0; s < stages; ++s) {
+        mbar_wait(&w->full[s], 0);
+        mbar_wait(&w->full[s], 1);
+    }
+}
 __device__ __forceinline__ void walk_ready(uint64_t *bar, int lane)
 {
     tmem_wait_st();

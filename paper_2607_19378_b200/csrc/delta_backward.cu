@@ -78,7 +78,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             // one thread waits, for every chunk in turn: the others have passed over copied ones, and a barrier's parity tells them nothing
             if (i >= C::STAGES && ft == 0) WAIT(&ws.empty[s], (i / C::STAGES - 1) & 1);
             if (!copied) fetchers_sync();
-            if (ft == 0) {
+            if (ft == 0 && !walk_given_up(&ws)) {
                 const long long at = bh * a.chunks + c;
                 mbar_expect_tx(&ws.full[s], C::IMAGES + kWalkGates + (copied ? (phi ? 2 : 3) * C::TENSOR : 0));
                 if (copied) {
@@ -318,9 +318,9 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
         tmem_fence_before_sync();
     }
     __syncthreads();
-    if (ws.gave_up && tid == 0) {                            // copies on their way end before the memory they go to is another CTA's
+    if (ws.gave_up && tid == 0) {
         atomicExch(&hn_delta_backward_status, 1);
-        for (int s = 0; s < C::STAGES; ++s) mbar_wait(&ws.full[s], 0);
+        walk_drain(&ws, C::STAGES);
     }
     if (warp == 0) tmem_dealloc(tb, 512);
 }
@@ -616,7 +616,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
         columns(S, false);
         go();
         if (warp == 0) {
-            if (C::ROOM && lane == 0) {                      // the state has been read: the gradient behind the chunk into its place
+            if (C::ROOM && lane == 0 && !walk_given_up(&ws)) {          // the state has been read: the gradient behind the chunk into its place
                 mbar_expect_tx(&ws.full[1], (unsigned)(kept * 4));
                 bulk_load(sm + C::STATE, D, (unsigned)(kept * 4), &ws.full[1]);
             }
@@ -655,7 +655,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
             umma_commit(&ws.bar_b);
         }
         done();
-        if (C::ROOM && more && tid == 0) copy_early(then);   // (dY and the state's place are free: their products are through, every thread has read)
+        if (C::ROOM && more && tid == 0 && !walk_given_up(&ws)) copy_early(then);   // (dY and the state's place are free: their products are through, every thread has read)
         __syncwarp();
         {   // F and E in the lower triangles, where their lanes' rows are tokens
             const int i = row & 63;
@@ -720,7 +720,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
             umma_commit(&ws.bar_a);
         }
         done();
-        if (C::ROOM && more && tid == 0) copy_rest(then, phase ^ 1);     // (every product is through, and what the threads read they have)
+        if (C::ROOM && more && tid == 0 && !walk_given_up(&ws)) copy_rest(then, phase ^ 1);     // (every product is through, and what the threads read they have)
         __syncwarp();
         float written = 0.f;
 #pragma unroll
@@ -781,7 +781,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
                 tma_commit();
                 tma_wait_read0();                            // (U is formed anew behind the next barriers)
             }
-            if (!C::ROOM && more) {
+            if (!C::ROOM && more && !walk_given_up(&ws)) {
                 copy_early(then);
                 copy_rest(then, phase ^ 1);
             }
@@ -827,9 +827,9 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
     }
     tmem_fence_before_sync();
     __syncthreads();
-    if (ws.gave_up && tid == 0) {                            // copies on their way end before the memory they go to is another CTA's
+    if (ws.gave_up && tid == 0) {
         atomicExch(&hn_delta_backward_status, 1);
-        for (int s = 0; s < 3; ++s) mbar_wait(&ws.full[s], 0);
+        walk_drain(&ws, 3);
     }
     if (warp == 0) tmem_dealloc(tb, 512);
 }

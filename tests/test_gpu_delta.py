@@ -127,6 +127,26 @@ def test_ragged_rows_of_many_chunks(D):
     compare(got, ref, t, H, Hk, torch.bfloat16, [n for n in NAMES if n in got])
 
 
+# what one entry and one head hold reaches no other, though they share CTAs, shared and tensor memory one after the other
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("Dk,Dv,L", [(50, 41, 136), (40, 97, 130)])
+def test_a_nan_stays_with_its_head(Dk, Dv, L, dtype):
+    shape = B, H, Hk, Dk, Dv, L = 12, 12, 12, Dk, Dv, L
+    t = inputs(*shape, DTYPES[dtype], "log", 13)
+    sick = torch.zeros(B, H, dtype=torch.bool)
+    sick[::3, ::2] = True
+    clean = {k: None if v is None else v.clone() for k, v in t.items()}
+    for name in ("q", "k", "v", "dy"):
+        rows = t[name].view(B, H, -1, L)
+        rows[sick] = float("nan") if name in ("q", "v") else float("inf")
+    t["s0"][sick] = float("nan")
+    got = run(t, shape, DTYPES[dtype], "log")
+    ref = od.delta(clean["q"], clean["k"], clean["v"], clean["g"], clean["beta"], "log", H, Hk, clean["s0"], None, clean["dy"], clean["ds"])
+    for n in NAMES:
+        a, b = got[n].reshape(B * H, -1)[~sick.flatten()], torch.from_numpy(np.ascontiguousarray(ref[n])).reshape(B * H, -1)[~sick.flatten()]
+        compare({n: a[None].reshape(1, len(a), -1)}, {n: b.numpy()[None]}, dict(clean, lengths=None), len(a), len(a), DTYPES[dtype], [n])
+
+
 # more heads than SMs, and a batch entry without tokens among them
 def test_many_heads():
     check((40, 4, 4, 16, 16, 130), "bf16", "log", 5, True)
