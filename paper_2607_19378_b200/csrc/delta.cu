@@ -106,6 +106,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(128) delta_prepa
     tmem_fence_before_sync();
     __syncthreads();
     tmem_fence_after_sync();
+    pdl_trigger();
     const unsigned tb = slot, images = smem_u32(sm);
     bool ok = !copied || mbar_wait(&there, 0);
     if (warp == 0) {
@@ -262,6 +263,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
     tmem_fence_before_sync();
     __syncthreads();
     tmem_fence_after_sync();
+    pdl_trigger();
     const unsigned tb = ws.slot;
     const long long states = (long long)a.Dv * a.Dk, vhead = bh * a.Dv * a.L, vall = (long long)a.B * a.H * a.Dv * a.L;
     if (warp > 8 && warp < 12) {
