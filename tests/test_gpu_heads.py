@@ -68,6 +68,13 @@ def test_given_positions(dims, D, dtype):
     check(dims, axes, 3, 2, 1, D, dtype, "l2", positions=True)
 
 
+# more tiles than CTAs, whose next rows are fetched a tile ahead, with positions of each batch entry's own; the largest table of a tile
+@pytest.mark.parametrize("dims,axes,B,Hq,Hk,D,positions", [((44840,), (20,), 2, 1, 1, 40, True), ((44800,), (30,), 3, 2, 1, 62, False), ((24, 1), (32, 32), 5, 3, 2, 128, False),
+                                                           ((24, 1), (32, 32), 5, 3, 2, 128, True)], ids=str)
+def test_tiles_in_turn(dims, axes, B, Hq, Hk, D, positions):
+    check(dims, axes, B, Hq, Hk, D, "bf16", "l2", positions=positions)
+
+
 def test_no_weights_no_axes():
     check((50,), (0,), 2, 2, 1, 20, "f32", "rms", weights=False)
 
