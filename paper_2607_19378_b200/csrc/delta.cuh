@@ -608,7 +608,7 @@ template <typename T> static bool delta_maps(DeltaMaps &m, const DeltaArgs &a, i
         const unsigned long long dims[3] = {(unsigned long long)a.L, (unsigned long long)D, (unsigned long long)a.B * (keys ? a.Hk : a.H)},
                                  strides[2] = {2ull * a.L, 2ull * a.L * D};
         const unsigned box[3] = {(unsigned)kTok, (unsigned)rows, 1};
-        return !p || tma_encode_3d_cached(map, p, true, dims, strides, box, 128);
+        return !p || tma_encode_3d(map, p, true, dims, strides, box, 128);
     };
     return one(&m.k, a.k, true) && one(&m.q, a.q, true) && one(&m.v, v, false) && one(&m.more, a.v, false) && one(&m.out, out, outk != nullptr) && one(&m.outk, outk, true);
 }

@@ -329,7 +329,7 @@ def test_elements_past_two_to_the_31():
     from paper_2607_19378_b200 import hyenand as hn
     import os
     if os.environ.get("HYENAND_LIB") == "debug":
-        pytest.skip("minutes under the checker, and no kernel that smaller ones leave out")
+        pytest.skip("minutes with range checks, and no kernel that smaller ones leave out")
     H, D, L = 17, 128, 1 << 20
     gen = torch.Generator(device="cuda").manual_seed(15)
     n = lambda *s: torch.randn(s, generator=gen, device="cuda", dtype=torch.bfloat16)
