@@ -106,7 +106,6 @@ template <typename T, int KD> __global__ void __launch_bounds__(128) delta_prepa
     tmem_fence_before_sync();
     __syncthreads();
     tmem_fence_after_sync();
-    pdl_trigger();
     const unsigned tb = slot, images = smem_u32(sm);
     bool ok = !copied || mbar_wait(&there, 0);
     if (warp == 0) {
@@ -166,6 +165,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(128) delta_prepa
         tma_commit();
     }
     if (warp == 0) tmem_dealloc(tb, 64);
+    pdl_trigger();                                           // (late: see delta.cuh)
     // A = (I + T)^{-1} in T's place: blocks of 16 by forward substitution, a thread a column; then pairs of blocks,
     //     (D1 0; T21 D2)^{-1} = (D1^{-1} 0; -D2^{-1} T21 D1^{-1} D2^{-1}), to 32 and to 64
     if (tid < kTok) {
@@ -263,7 +263,6 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
     tmem_fence_before_sync();
     __syncthreads();
     tmem_fence_after_sync();
-    pdl_trigger();
     const unsigned tb = ws.slot;
     const long long states = (long long)a.Dv * a.Dk, vhead = bh * a.Dv * a.L, vall = (long long)a.B * a.H * a.Dv * a.L;
     if (warp > 8 && warp < 12) {
@@ -498,6 +497,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
         walk_drain(&ws, C::STAGES);
     }
     if (warp == 0) tmem_dealloc(tb, 512);
+    pdl_trigger();                                           // (late: see delta.cuh)
 }
 
 // ---- segments -------------------------------------------------------------------------------------------------------

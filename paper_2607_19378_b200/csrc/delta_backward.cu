@@ -64,7 +64,6 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
     tmem_fence_before_sync();
     __syncthreads();
     tmem_fence_after_sync();
-    pdl_trigger();
     const unsigned tb = ws.slot;
     const long long states = (long long)a.Dv * a.Dk, vhead = bh * a.Dv * a.L, vall = (long long)a.B * a.H * a.Dv * a.L;
     if (warp > 8 && warp < 12) {
@@ -324,6 +323,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
         walk_drain(&ws, C::STAGES);
     }
     if (warp == 0) tmem_dealloc(tb, 512);
+    pdl_trigger();                                           // (late: see delta.cuh)
 }
 
 // ---- gradients ------------------------------------------------------------------------------------------------------
@@ -424,7 +424,6 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
     tmem_fence_before_sync();
     __syncthreads();
     tmem_fence_after_sync();
-    pdl_trigger();
     const unsigned tb = ws.slot;
     const unsigned lane_s = tmem_addr(tb, warp, C::S0 + quarter * (HC / 2)), lane_r = tmem_addr(tb, warp, c0);
     unsigned par = 0;
@@ -834,6 +833,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
         walk_drain(&ws, 3);
     }
     if (warp == 0) tmem_dealloc(tb, 512);
+    pdl_trigger();                                           // (late: see delta.cuh)
 }
 
 // ---- host -----------------------------------------------------------------------------------------------------------
