@@ -367,7 +367,7 @@ int hyenand_delta_device_status(void);
  * The first axes[0] pairs i turn with the position p on axis 0, the next axes[1] with that on axis 1, and so on; j counts the pairs of an
  * axis, and pairs behind them all stay as they are (axes may be NULL: no rotation).  Positions are the token's place on the grid, or
  * positions, int32 [B][ndim][T] on the device.  g_q, g_k: D fp32 weights or NULL (1).  Sums are fp32, angles 64 bits wide; every result
- * is rounded once.  q_out may be the buffer q, k_out the buffer k.
+ * is rounded once.  q_out may be the buffer q, k_out the buffer k; not where q and k are one buffer.
  * Limits: ndim <= 3, D even and <= 256, T <= 2^30, B (Hq + Hk) <= 2^28, 2^40 elements; eps > 0.  Errors and stream as
  * hyenand_forward_ex; no call allocates, synchronises or keeps anything.
  */
@@ -375,7 +375,7 @@ enum { HYENAND_NORM_NONE = 0, HYENAND_NORM_RMS = 1, HYENAND_NORM_L2 = 2 };
 int hyenand_heads_forward(int ndim, const int *dims, int B, int Hq, int Hk, int D, int dtype, int norm, const int *axes, double base, float eps,
                           const void *q, const void *k, const float *g_q, const float *g_k, const int *positions, void *q_out, void *k_out,
                           void *cuda_stream);
-/* The gradient: dq_out, dk_out in, dq, dk (dq may be the buffer dq_out, dk the buffer dk_out) and the sums over all tokens dg_q, dg_k (D fp32
+/* The gradient: dq_out, dk_out in, dq, dk (dq may be the buffer dq_out, dk the buffer dk_out, where those are two) and the sums over all tokens dg_q, dg_k (D fp32
  * each, or NULL) out; the forward's inputs are read again.  workspace: hyenand_heads_workspace_bytes() bytes on the device, 16-byte
  * aligned, where dg_q or dg_k is given; calls that may overlap need one each.  The order of the sums does not depend on timing. */
 int hyenand_heads_backward(int ndim, const int *dims, int B, int Hq, int Hk, int D, int dtype, int norm, const int *axes, double base, float eps,

@@ -798,7 +798,7 @@ extern "C" int hyenand_delta_forward(int B, int H, int Hk, int L, int Dk, int Dv
     const DeltaSizes s = delta_sizes(a, dtype, false);
     place_workspace(a, s, workspace);
     c.in("s0", s0, state_bytes(a));
-    c.out("y", y, (size_t)B * H * Dv * L * elsize(dtype)); c.out("s_end", s_end, state_bytes(a), 16, s0);
+    c.out("y", y, (size_t)B * H * Dv * L * elsize(dtype)); c.out("s_end", s_end, state_bytes(a), 16, "s0");
     c.out("marks", marks, mark_bytes(a)); c.out("workspace", workspace, s.all);
     if (int e = c.check()) return e;
     c.register_ranges();
@@ -825,7 +825,7 @@ extern "C" int hyenand_delta_backward(int B, int H, int Hk, int L, int Dk, int D
     const size_t es = elsize(dtype) * (size_t)L * B, gb = (size_t)B * H * L * sizeof(float);
     c.in("marks", marks, mark_bytes(a)); c.in("dy", dy, es * H * Dv); c.in("ds_end", ds_end, state_bytes(a));
     c.out("dq", dq, es * Hk * Dk); c.out("dk", dk, es * Hk * Dk); c.out("dv", dv, es * H * Dv); c.out("dg", dg, gb, 4); c.out("dbeta", dbeta, gb, 4);
-    c.out("ds0", ds0, state_bytes(a), 16, ds_end); c.out("workspace", workspace, s.all);
+    c.out("ds0", ds0, state_bytes(a), 16, "ds_end"); c.out("workspace", workspace, s.all);
     if (int e = c.check()) return e;
     c.register_ranges();
     return finish(launch_delta_backward(a, dtype, (cudaStream_t)cuda_stream));
@@ -842,7 +842,7 @@ extern "C" int hyenand_delta_step(int B, int H, int Hk, int Dk, int Dv, int deca
     CallTensors c;
     if (int e = inputs(c, a, 1, dtype)) return e;
     c.in("state", state, state_bytes(a));
-    c.out("y", y, (size_t)B * H * Dv * elsize(dtype)); c.out("new_state", new_state, state_bytes(a), 16, state);
+    c.out("y", y, (size_t)B * H * Dv * elsize(dtype)); c.out("new_state", new_state, state_bytes(a), 16, "state");
     if (int e = c.check()) return e;
     c.register_ranges();
     const cudaStream_t st = (cudaStream_t)cuda_stream;

@@ -71,7 +71,7 @@ extern "C" int hyenand_dropout(long long n, int dtype, const void *x, float p, c
     CallTensors c;
     c.in("x", x, (size_t)n * elsize(dtype));
     c.in("rng", rng, 2 * sizeof(long long));
-    c.out("y", y, (size_t)n * elsize(dtype), 16, x);
+    c.out("y", y, (size_t)n * elsize(dtype), 16, "x");
     if (int e = c.check()) return e;
     c.register_ranges();
     const long long octets = (n + 7) / 8, each = kDropThreads * (8 / (long long)elsize(dtype)), blocks = (octets + each - 1) / each;

@@ -2,6 +2,7 @@
 // overlapping arguments (internal).
 #pragma once
 #include <stdint.h>
+#include <string.h>
 
 #include <mutex>
 
@@ -68,14 +69,15 @@ struct DbgScope {
 #endif
 };
 
-// The tensors of one call.  Inputs may overlap one another, an output may overlap nothing else (`with`: the one input it may be
-// the same buffer as, where every element is read before the thread that replaces it does so).
+// The tensors of one call.  Inputs may overlap one another, an output may overlap nothing else (`with`: the name of the one input it may be
+// the same buffer as, where every element is read before the thread that replaces it does so; another input in that buffer is still
+// one that the call reads).
 struct CallTensors {
-    struct One { const void *ptr; size_t bytes; const char *name; int align; bool out; const void *with; };
+    struct One { const void *ptr; size_t bytes; const char *name; int align; bool out; const char *with; };
     One t[24];
     int n = 0;
     void in(const char *name, const void *ptr, size_t bytes, int align = 16) { if (ptr && bytes) t[n++] = {ptr, bytes, name, align, false, nullptr}; }
-    void out(const char *name, const void *ptr, size_t bytes, int align = 16, const void *with = nullptr)
+    void out(const char *name, const void *ptr, size_t bytes, int align = 16, const char *with = nullptr)
     {
         if (ptr && bytes) t[n++] = {ptr, bytes, name, align, true, with};
     }
@@ -86,7 +88,7 @@ struct CallTensors {
         for (int i = 0; i < n; ++i)
             for (int j = 0; j < n; ++j) {
                 if (i == j || !t[i].out) continue;
-                if (!t[j].out && t[i].with == t[i].ptr && t[j].ptr == t[i].ptr && t[j].bytes == t[i].bytes) continue;
+                if (!t[j].out && t[i].with && !strcmp(t[i].with, t[j].name) && t[j].ptr == t[i].ptr && t[j].bytes == t[i].bytes) continue;
                 const char *a = (const char *)t[i].ptr, *b = (const char *)t[j].ptr;
                 if (a < b + t[j].bytes && b < a + t[i].bytes) return fail(HYENAND_ERR_INVALID_ARG, "%s overlaps %s", t[i].name, t[j].name);
             }

@@ -648,7 +648,7 @@ extern "C" int hyenand_heads_forward(int ndim, const int *dims, int B, int Hq, i
     const size_t one = (size_t)B * D * a.T * elsize(dtype);
     c.in("q", q, one * Hq); c.in("k", k, one * Hk); c.in("g_q", g_q, (size_t)D * 4, 4); c.in("g_k", g_k, (size_t)D * 4, 4);
     c.in("positions", positions, (size_t)B * ndim * a.T * sizeof(int), 4);
-    c.out("q_out", q_out, one * Hq, 16, q); c.out("k_out", k_out, one * Hk, 16, k);
+    c.out("q_out", q_out, one * Hq, 16, "q"); c.out("k_out", k_out, one * Hk, 16, "k");
     if (int e = c.check()) return e;
     c.register_ranges();
     const cudaStream_t st = (cudaStream_t)cuda_stream;
@@ -672,7 +672,7 @@ extern "C" int hyenand_heads_backward(int ndim, const int *dims, int B, int Hq, 
     c.in("q", q, one * Hq); c.in("k", k, one * Hk); c.in("g_q", g_q, (size_t)D * 4, 4); c.in("g_k", g_k, (size_t)D * 4, 4);
     c.in("positions", positions, (size_t)B * ndim * a.T * sizeof(int), 4);
     c.in("dq_out", dq_out, one * Hq); c.in("dk_out", dk_out, one * Hk);
-    c.out("dq", dq, one * Hq, 16, dq_out); c.out("dk", dk, one * Hk, 16, dk_out);
+    c.out("dq", dq, one * Hq, 16, "dq_out"); c.out("dk", dk, one * Hk, 16, "dk_out");
     c.out("dg_q", dg_q, (size_t)D * 4, 4); c.out("dg_k", dg_k, (size_t)D * 4, 4);
     if (dg_q || dg_k) c.out("workspace", workspace, part_bytes(a, dtype));
     if (int e = c.check()) return e;
