@@ -367,7 +367,8 @@ int hyenand_delta_device_status(void);
  * The first axes[0] pairs i turn with the position p on axis 0, the next axes[1] with that on axis 1, and so on; j counts the pairs of an
  * axis, and pairs behind them all stay as they are (axes may be NULL: no rotation).  Positions are the token's place on the grid, or
  * positions, int32 [B][ndim][T] on the device.  g_q, g_k: D fp32 weights or NULL (1).  Sums are fp32, angles 64 bits wide; every result
- * is rounded once.  q_out may be the buffer q, k_out the buffer k; not where q and k are one buffer.
+ * is rounded once.  Finite channels whose squares pass fp32 are normalised as any others; beside an infinite one, which becomes NaN, the
+ * rest of a head is 0 under a norm.  q_out may be the buffer q, k_out the buffer k; not where q and k are one buffer.
  * Limits: ndim <= 3, D even and <= 256, T <= 2^30, B (Hq + Hk) <= 2^28, 2^40 elements; eps > 0.  Errors and stream as
  * hyenand_forward_ex; no call allocates, synchronises or keeps anything.
  */

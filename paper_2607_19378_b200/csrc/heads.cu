@@ -70,6 +70,10 @@ template <typename T> struct Tile {
     static constexpr int V = 16 / sizeof(T), TOKENS = 8 * V;
 };
 
+// A token whose mean square is beyond fp32 though its channels are not is taken at this scale: then 256 squares of the largest number fit,
+// and one that brought the mean there is still 2^-10.
+constexpr float kShrink = 0x1p-70f, kLargest = 3.402823466e38f;
+
 // The V tokens of a lane in one row, in pairs: side by side as one vector, or (rows that do not start on 16 bytes) every eighth token, so
 // that the eight lanes of a row share a sector
 template <typename T, bool VEC> struct Tokens {
@@ -212,6 +216,103 @@ __device__ __forceinline__ void copy16(void *to, const void *from, bool real)   
     if (real) HN_G(from, 16);
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"((unsigned)__cvta_generic_to_shared(to)), "l"(from), "r"(real ? 16 : 0) : "memory");
 }
+// A unit in which a mean square was not finite, once more from the tensors, by the warps of its head: the tokens of `large` at kShrink, the
+// others as before, to the bit.  Returns this lane's sums for the weights' gradients.  A call: in line, as a second round of the same loop,
+// it cost the common path more (heads of 50 channels on 31 x 33 each way 42 -> 46 us, of 256 on 16384 tokens 536 -> 558; with the call 42
+// and 533; 262144 tokens of 128 channels each way 585 -> 595 and with the call 603).
+template <int P> struct LaneSums { float v[P][2]; };
+template <typename T, int R, int P, bool BWD, bool VEC>
+__device__ __noinline__ LaneSums<P> heads_again(const T *in, const T *gradient, T *out, const float *w, const float *cs, const float *sn, float *meet, int live, int t0, int half,
+                                                int turned, int T_, float per_mean, float eps, unsigned large, int r, int group)
+{
+    constexpr int V = Tile<T>::V, TOKENS = Tile<T>::TOKENS, WARPS = R / 4, SUMS = BWD ? 2 : 1;
+    const int lane = threadIdx.x & 31, vc = lane & 7;
+    LaneSums<P> dg;
+#pragma unroll
+    for (int p = 0; p < P; ++p) dg.v[p][0] = dg.v[p][1] = 0.f;
+    auto token = [&](int e) { return t0 + (VEC ? vc * V + e : e * 8 + vc); };
+    // the channels of a pair and its gradient before the rotation
+    auto pair_of = [&](int e, int p, float (&x)[2], float (&d)[2]) {
+        const int t = token(e), i = r + R * p;
+        const bool real = t < live && i < half;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const long long at = (long long)(R * p + s * half) * T_ + t;
+            x[s] = real ? IO<T>::ld(in, at) * (large >> e & 1 ? kShrink : 1.f) : 0.f;
+            d[s] = BWD && real ? IO<T>::ld(gradient, at) : 0.f;
+        }
+        if (BWD && i < turned) {
+            const int at = i * TOKENS + table_at(vc, e);
+            const float c = cs[at], n = sn[at], l = d[0], h = d[1];
+            d[0] = fmaf(h, n, l * c);
+            d[1] = fmaf(l, -n, h * c);
+        }
+    };
+    auto weight = [&](int p, int s) { return w[(r + R * p < half ? r + R * p : 0) + s * half]; };
+    float s1[V], s2[V];
+#pragma unroll 1
+    for (int e = 0; e < V; ++e) {
+        float a = 0.f, b = 0.f;
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            float x[2], d[2];
+            pair_of(e, p, x, d);
+#pragma unroll
+            for (int s = 0; s < 2; ++s) { a = fmaf(x[s], x[s], a); b = fmaf(d[s] * weight(p, s), x[s], b); }
+        }
+#pragma unroll
+        for (int m = 8; m < 32; m <<= 1) { a += __shfl_xor_sync(~0u, a, m); b += __shfl_xor_sync(~0u, b, m); }
+        s1[e] = a;
+        s2[e] = b;
+        if (WARPS > 1 && lane < 8) {
+            meet[(threadIdx.x >> 5) * TOKENS + vc * V + e] = a;
+            if (BWD) meet[((SUMS - 1) * 8 + (threadIdx.x >> 5)) * TOKENS + vc * V + e] = b;
+        }
+    }
+    if (WARPS > 1) {
+        __syncwarp();
+        asm volatile("bar.sync %0, %1;\n" ::"r"(1 + group), "n"(32 * WARPS) : "memory");
+    }
+#pragma unroll 1
+    for (int e = 0; e < V; ++e) {
+        const float shrink = large >> e & 1 ? kShrink : 1.f;
+        float a = s1[e], b = s2[e];
+        if (WARPS > 1) {
+            a = b = 0.f;
+            for (int k = 0; k < WARPS; ++k) {
+                a += meet[(group * WARPS + k) * TOKENS + vc * V + e];
+                if (BWD) b += meet[((SUMS - 1) * 8 + group * WARPS + k) * TOKENS + vc * V + e];
+            }
+        }
+        const float v = fmaf(a, per_mean, eps * shrink * shrink), rho = v > kLargest ? 0.f : inverse_root(v);      // (0: a channel is infinite)
+        b = rho * b * -per_mean;
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            float x[2], d[2];
+            pair_of(e, p, x, d);
+            const int i = r + R * p;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                if (BWD) {
+                    const float hat = x[s] * rho, own = d[s] * weight(p, s);
+                    dg.v[p][s] = fmaf(d[s], hat, dg.v[p][s]);
+                    x[s] = rho * fmaf(hat, b, own) * shrink;
+                } else x[s] *= rho * weight(p, s);
+            }
+            if (!BWD && i < turned) {
+                const int at = i * TOKENS + table_at(vc, e);
+                const float c = cs[at], n = sn[at], l = x[0], h = x[1];
+                x[0] = fmaf(h, -n, l * c);
+                x[1] = fmaf(l, n, h * c);
+            }
+            if (token(e) < live && i < half)
+#pragma unroll
+                for (int s = 0; s < 2; ++s) IO<T>::st(out, (long long)(R * p + s * half) * T_ + token(e), x[s]);
+        }
+    }
+    return dg;
+}
+
 template <typename T, int R, int P, bool BWD, bool VEC> __global__ void __launch_bounds__(256, resident(P, BWD)) heads_kernel(HeadsArgs a)
 {
     constexpr int V = Tile<T>::V, TOKENS = Tile<T>::TOKENS, HEADS = 32 / R, WARPS = R / 4, SUMS = BWD ? 2 : 1, N = V / 2;
@@ -401,9 +502,32 @@ template <typename T, int R, int P, bool BWD, bool VEC> __global__ void __launch
                         if constexpr (BWD) get(meet[turn][SUMS - 1], s2);
                         turn ^= 1;
                     }
+                    f2 all = pair(0.f);                            // finite where all are
 #pragma unroll
                     for (int e = 0; e < N; ++e) {
-                        rho[e] = make2(inverse_root(fmaf(s1[e].x, a.per_mean, a.eps)), inverse_root(fmaf(s1[e].y, a.per_mean, a.eps)));
+                        s1[e] = fma2(s1[e], pair(a.per_mean), pair(a.eps));
+                        all = fma2(s1[e], pair(0x1p-8f), all);
+                    }
+                    if (__any_sync(~0u, !(sum2(all) <= kLargest))) {      // (in all warps of the head: they hold the same sums)
+                        unsigned large = 0;
+#pragma unroll
+                        for (int e = 0; e < N; ++e) large |= (!(s1[e].x <= kLargest) ? 1u : 0u) << (2 * e) | (!(s1[e].y <= kLargest) ? 2u : 0u) << (2 * e);
+                        const LaneSums<P> more = heads_again<T, R, P, BWD, VEC>(in, gradient, out, weights[kind], cs, sn, &meet[turn][0][0][0], live, t0, half, a.turned, a.T, a.per_mean,
+                                                                                a.eps, large, r, group);
+                        turn ^= 1;
+                        if constexpr (BWD)
+#pragma unroll
+                            for (int p = 0; p < P; ++p)
+#pragma unroll
+                                for (int s = 0; s < 2; ++s) {
+                                    if (kind) acc[1][p][s] += more.v[p][s];
+                                    else acc[0][p][s] += more.v[p][s];
+                                }
+                        continue;
+                    }
+#pragma unroll
+                    for (int e = 0; e < N; ++e) {
+                        rho[e] = make2(inverse_root(s1[e].x), inverse_root(s1[e].y));
                         if constexpr (BWD) s2[e] = mul2(mul2(rho[e], s2[e]), pair(-a.per_mean));
                     }
                 }
@@ -497,18 +621,31 @@ template <typename T> __global__ void __launch_bounds__(256) heads_token_kernel(
     const int t = (int)(i % a.T), b = (int)(i / a.T / HT), hh = (int)(i / a.T % HT), kind = hh >= a.H[0], h = kind ? hh - a.H[0] : hh;
     const long long at = ((long long)b * a.H[kind] + h) * a.D * a.T + t;
     constexpr int P = kMaxD / 64;
-    float x[P][2], sum = 0.f;
+    float x[P][2], rho = 1.f;
 #pragma unroll
     for (int p = 0; p < P; ++p)
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             const int c = lane + 32 * p;
             x[p][s] = c < half ? IO<T>::ld((const T *)a.x[kind], at + (long long)(c + s * half) * a.T) : 0.f;
-            sum = fmaf(x[p][s], x[p][s], sum);
         }
+    if (a.norm != NORM_NONE) {
+        auto mean_square = [&](float eps) {
+            float sum = 0.f;
 #pragma unroll
-    for (int m = 1; m < 32; m <<= 1) sum += __shfl_xor_sync(~0u, sum, m);
-    const float rho = a.norm == NORM_NONE ? 1.f : 1.f / sqrtf(fmaf(sum, a.per_mean, a.eps));
+            for (int p = 0; p < P; ++p) sum = fmaf(x[p][1], x[p][1], fmaf(x[p][0], x[p][0], sum));
+#pragma unroll
+            for (int m = 1; m < 32; m <<= 1) sum += __shfl_xor_sync(~0u, sum, m);
+            return fmaf(sum, a.per_mean, eps);
+        };
+        float v = mean_square(a.eps);
+        if (!(v <= kLargest)) {                              // (the same in all lanes; see heads_again)
+#pragma unroll
+            for (int p = 0; p < P; ++p) { x[p][0] *= kShrink; x[p][1] *= kShrink; }
+            v = mean_square(a.eps * kShrink * kShrink);
+        }
+        rho = 1.f / sqrtf(v);
+    }
 #pragma unroll
     for (int p = 0; p < P; ++p) {
         const int c = lane + 32 * p;
