@@ -117,7 +117,16 @@ template <typename T, int KD> __global__ void __launch_bounds__(128) delta_prepa
         const float gamma = ratio(hi[tid], lo[tid], 0.f, 0.f);
         const float x[6] = {gamma, ratio(hi[kTok - 1], lo[kTok - 1], hi[tid], lo[tid]), beta[tid], -beta[tid] * gamma, hi[tid], lo[tid]};
 #pragma unroll
-        for (int e = 0; e < 6; ++e) { HN_G(gates + e * kTok + tid, 4); gates[e * kTok + tid] = x[e]; }
+        for (int e = 0; e < 6; ++e) {
+            float *to = gates + (e < 4 ? 0 : kSums - kCarry) + e * kTok + tid;
+            HN_G(to, 4);
+            *to = x[e];
+        }
+        if (tid == kTok - 1) {                               // (its gamma is the chunk's)
+            const float less = expm1f((hi[tid] + lo[tid]) * 0.6931471805599453f);
+            HN_G(gates + kCarry, 16);
+            *(float4 *)(gates + kCarry) = less > -0.5f ? make_float4(1.f, less, 0.f, 0.f) : make_float4(0.f, gamma, 0.f, 0.f);
+        }
     }
     ok = mbar_wait(&bar, 0) && ok;
     if (!ok) {
@@ -218,7 +227,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(128) delta_prepa
 template <typename T, int KD> struct Walk {
     static constexpr int PI = Planes<T>::IN, PM = Planes<T>::MID, TILE = KD * 128, TENSOR = PI * TILE;
     static constexpr bool VALUES = PI == 1;                                   // values and results travel as images
-    static constexpr int IMAGES = 2 * PM * kMatrix, K = 0, Q = TENSOR, A = 2 * TENSOR, V = A + IMAGES, GATES = V + (VALUES ? TILE : 0), STAGE = GATES + 1024;
+    static constexpr int IMAGES = 2 * PM * kMatrix, K = 0, Q = TENSOR, A = 2 * TENSOR, V = A + IMAGES, GATES = V + (VALUES ? TILE : 0), STAGE = GATES + 2048;
     static constexpr int OUT = VALUES ? 2 * TILE : 0;                         // two images of results
     static constexpr int STAGES = 3 * STAGE + OUT <= 220 * 1024 ? 3 : 2 * STAGE + OUT <= 220 * 1024 ? 2 : 1;
     static constexpr int BYTES = 1024 + STAGES * STAGE + OUT;
@@ -449,7 +458,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             }
             walk_ready(&ws.z_ready, lane);
             if (mark) keep_state<HC / 16, HC / 8>(mark, S, row, a.Dv, half * HC, a.Dk);
-            const f2 fade = pair(((const float *)(st + C::GATES))[kTok - 1]);
+            const Carry carry((const float *)(st + C::GATES));
             WAIT(&ws.bar_b, par);
             tmem_fence_after_sync();
             tmem_ld(x, lane_x);
@@ -470,7 +479,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             if (mark) keep_state<HC / 8, HC / 4>(mark, S, row, a.Dv, half * HC, a.Dk);
             WAIT(&ws.bar_c[half], par);
             tmem_fence_after_sync();
-            state_onwards<PM>(S, fade, lane_d, lane_s, KD / 2);
+            state_onwards<PM>(S, carry, lane_d, lane_s, KD / 2);
         }
         tmem_wait_st();
         auto flat = [&](float (&s)[HC]) {

@@ -32,8 +32,9 @@ enum { DELTA_LOG = HYENAND_DECAY_LOG, DELTA_SIGMOID = HYENAND_DECAY_SIGMOID, DEL
 template <typename T> struct Planes { static constexpr int IN = 1, MID = 2; };
 template <> struct Planes<float> { static constexpr int IN = 3, MID = 3; };
 constexpr int kMatrix = kTok * 128;                       // bytes of one plane of a 64 x 64 matrix
-constexpr int kGates = 6 * kTok;                          // floats of a chunk: gamma, delta, beta, -beta gamma, and G in two parts (see ratio)
-constexpr int kWalkGates = 4 * kTok * 4;                  // bytes of the first four
+// floats of a chunk: gamma, delta, beta, -beta gamma, what carries the state (see Carry), and G in two parts (see ratio)
+constexpr int kGates = 6 * kTok + 4, kCarry = 4 * kTok, kSums = kCarry + 4;
+constexpr int kWalkGates = kSums * 4;                     // bytes in front of the sums
 
 struct DeltaArgs {
     const void *q, *k, *v;
@@ -48,7 +49,7 @@ struct DeltaArgs {
     float *dg, *dbeta, *ds0;
     // workspace
     unsigned char *images;                                // [B H][chunks]: planes of A, planes of P
-    float *gates;                                         // [B H][chunks][6][64]
+    float *gates;                                         // [B H][chunks][kGates]
     float *maps, *starts;                                 // [B H][segments][Dv + Dk][map_pitch], [B H][segments] states as kept
     float *dstates, *dz;                                  // [B H][chunks] states as kept, [B H][chunks][Dv][64]
     int B, H, Hk, L, Dk, Dv, decay, chunks, segments, per_segment;
@@ -155,8 +156,15 @@ struct Sixteen {
     __device__ __forceinline__ void load(unsigned at) { TmemIO<16>::ld(x, at); }
     __device__ __forceinline__ f2 get(int i) const { return make2(x[2 * i], x[2 * i + 1]); }
 };
-// S = fade S + gain (this thread's columns of both, eight pairs at a time, the next loads under way), and S as an operand again
-template <int PM, int C> __device__ __forceinline__ void state_onwards(f2 (&S)[C], f2 fade, unsigned gain, unsigned planes, int pitch)
+// What a chunk leaves of a state, gamma_64 S = keep S + by S: a decay next to 1 as S + (gamma_64 - 1) S, where only the sum rounds the
+// state, with either sign.  As a factor, it is off by up to half a step in every chunk alike: at g = -1e-6 a state of 262144 tokens was off by
+// 7e-5.  Below a half there is nothing to lose: 0 S + gamma_64 S.
+struct Carry {
+    f2 keep, by;
+    __device__ __forceinline__ explicit Carry(const float *gates) { const float2 c = *(const float2 *)(gates + kCarry); keep = pair(c.x); by = pair(c.y); }
+};
+// S = gamma_64 S + gain (this thread's columns of both, eight pairs at a time, the next loads under way), and S as an operand again
+template <int PM, int C> __device__ __forceinline__ void state_onwards(f2 (&S)[C], const Carry &carry, unsigned gain, unsigned planes, int pitch)
 {
     Sixteen g[2];
     g[0].load(gain);
@@ -166,7 +174,7 @@ template <int PM, int C> __device__ __forceinline__ void state_onwards(f2 (&S)[C
         if (b + 1 < C / 8) g[(b + 1) & 1].load(gain + 16 * (b + 1));
         f2 x[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = S[8 * b + j] = fma2(fade, S[8 * b + j], g[b & 1].get(j));
+        for (int j = 0; j < 8; ++j) x[j] = S[8 * b + j] = fma2(carry.keep, S[8 * b + j], fma2(carry.by, S[8 * b + j], g[b & 1].get(j)));
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const f2 y[4] = {x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]};

@@ -19,7 +19,7 @@ static __device__ int hn_delta_backward_status;
 template <typename T, int KD> struct WalkBack {
     static constexpr int PI = Planes<T>::IN, PM = Planes<T>::MID, TILE = KD * 128, TENSOR = PI * TILE;
     static constexpr bool VALUES = PI == 1;                                   // dV and dZ's two planes travel as images
-    static constexpr int IMAGES = 2 * PM * kMatrix, K = 0, Q = TENSOR, DY = 2 * TENSOR, A = 3 * TENSOR, GATES = A + IMAGES, STAGE = GATES + 1024;
+    static constexpr int IMAGES = 2 * PM * kMatrix, K = 0, Q = TENSOR, DY = 2 * TENSOR, A = 3 * TENSOR, GATES = A + IMAGES, STAGE = GATES + 2048;
     static constexpr int OUT = VALUES ? 3 * TILE : 0;
     // (the product of dY and P takes 128 rows of dY's image: with 64 it reads on into the images that follow, for rows nothing looks at)
     static constexpr int STAGES = 3 * STAGE + OUT <= 220 * 1024 ? 3 : 2 * STAGE + OUT <= 220 * 1024 ? 2 : 1;
@@ -279,7 +279,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             }
             walk_ready(&ws.z_ready, lane);
             if (RUN) keep_state<HC / 16, HC / 8>(keep, S, row, a.Dv, half * HC, a.Dk);
-            const f2 fade = pair(((const float *)(sm + s * C::STAGE + C::GATES))[kTok - 1]);
+            const Carry carry((const float *)(sm + s * C::STAGE + C::GATES));
             WAIT(&ws.bar_b, par);
             tmem_fence_after_sync();
             tmem_ld(x, lane_x);
@@ -296,7 +296,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             if (RUN) keep_state<HC / 8, HC / 4>(keep, S, row, a.Dv, half * HC, a.Dk);
             WAIT(&ws.bar_c[half], par);
             tmem_fence_after_sync();
-            state_onwards<PM>(S, fade, lane_d, lane_s, KD / 2);
+            state_onwards<PM>(S, carry, lane_d, lane_s, KD / 2);
         }
         tmem_wait_st();
         auto flat = [&](float (&s)[HC]) {
@@ -479,7 +479,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
         const int t0 = now.chunk * kTok, nv = now.nv, room = a.L - t0 < kTok ? a.L - t0 : kTok, t = t0 + c0;
         const long long bh = head(now), at = bh * a.chunks + now.chunk, grow = bh * a.L + t0, qk = now.bk * a.Dk * a.L + t0;
         const float *S = a.marks + at * kept, *D = a.dstates + at * kept;
-        const float *gates = gates2[phase], *gamma = gates, *delta = gates + kTok, *beta = gates + 2 * kTok, *ghi = gates + 4 * kTok, *glo = gates + 5 * kTok;
+        const float *gates = gates2[phase], *gamma = gates, *delta = gates + kTok, *beta = gates + 2 * kTok, *ghi = gates + kSums, *glo = ghi + kTok;
         const bool copied = by_copy(a, nv, t0), first = now.j == 0, last = now.j == share - 1;
         more = next(then);
         if (first) {
