@@ -11,8 +11,10 @@
 //     dQ_i = gamma_i S0^T dY_i + sum_j F_ij k_j,
 //     dK_i = [sum_j E_ij k_j - gamma_i beta_i S0^T dZ_i]  +  [sum_j (F_ji q_j + E_ji k_j) + delta_i dS1^T u_i]      (erased, written),
 //     dbeta_i = dZ_i . R_i - sum_{j<i} (dZ_i . u_j) r_ij (k_i . k_j),
-//     dG_i = q_i . dQ_i + k_i . dK_i^erased - k_i . dK_i^written,   dG_64 += <S1, dS1>,   d log a_t = sum_{i >= t} dG_i.
-// (A token's decay scales its query and what it erases, and divides what it writes: hence dG.)
+//     d log a_t = sum_{i >= t > j} [F_ij (q_i . k_j) + E_ij (k_i . k_j)]  +  sum_{i >= t} gamma_i [q_i . S0^T dY_i - beta_i k_i . S0^T dZ_i]
+//                 +  sum_{j < t} delta_j k_j . dS1^T u_j  +  gamma_64 <S0, dS1>.
+// (What crosses token t carries a_t and nothing else does.  The same as a running sum of q dQ + k dK, erased less written, is a difference of
+// numbers of order 1: right to 1e-3 of itself at log a = -8, to nothing at -16.)
 //
 // The products run on the tensor cores in bf16 with fp32 sums.  A number that is no bf16 value goes in as a sum of bf16 values ("planes"):
 // two for bf16 tensors (16 bits, errors of 2^-17: states and sums are fp32 and a result is rounded once, so these errors stay far

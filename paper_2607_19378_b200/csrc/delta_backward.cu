@@ -5,7 +5,7 @@
 //     tensor memory and every product takes the one before as its operand there: dS k, then A^T dU, then the new dS.  It writes dV, dZ
 //     (as images, for bf16) and the gradient behind every chunk.  Few heads and many chunks go in segments as there (dS0 = dS1 Phi + N).
 // gradients: a CTA an SM takes the chunks of the heads of queries and keys one after the other: from the state before the chunk (the forward's mark) and the gradient
-//     behind it, U again, then dQ, dK, and the sums over tokens for beta and the decay.  Value heads that share queries and keys follow
+//     behind it, U again, then dQ, dK, and the sums for beta and, over what crosses each token, for the decay.  Value heads that share queries and keys follow
 //     one another in the CTA, so their sum has one order and needs no atomics.
 #include "delta.cuh"
 
@@ -330,17 +330,17 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
 
 template <typename T, int KD> struct Grads {
     static constexpr int PI = Planes<T>::IN, PM = Planes<T>::MID, TILE = KD * 128;
-    // images: dY | K | Q | U (values before it, dK in its second half behind it) | dZ (later E) | A (later F) | dQ, and a state as it is kept.
+    // images: dY | Q | K | U (values before it, dK in its second half behind it) | dZ (later E) | A (later F) | dQ, and a state as it is kept.
     // With three planes there is no room for the last two, and Q comes into dY's place once that is through.
     static constexpr bool ROOM = PI == 1;
-    static constexpr int DY = 0, K = PI * TILE, Q = ROOM ? 2 * PI * TILE : DY, U = (ROOM ? 3 : 2) * PI * TILE, DZ = U + PM * TILE, A = DZ + PM * TILE, OUT = A + PM * kMatrix,
+    static constexpr int DY = 0, K = (ROOM ? 2 : 1) * PI * TILE, Q = ROOM ? PI * TILE : DY, U = (ROOM ? 3 : 2) * PI * TILE, DZ = U + PM * TILE, A = DZ + PM * TILE, OUT = A + PM * kMatrix,
                          STATE = OUT + (ROOM ? TILE : 0), BYTES = 1024 + STATE + (ROOM ? KD * KD * 4 : 0);
     // tensor memory: a state as an operand | sums of 64 columns:
-    //     0: S0 k, U, the rest of dZ U^T   1: Z (and the next), dY U^T and dZ U^T   2: K K^T, the written part of dK but for dS1 u
+    //     0: S0 k, U, the rest of dZ U^T   1: Z (and the next), dY U^T and dZ U^T   2: Q K^T and K K^T, the written part of dK but for dS1 u
     //     3: S0 dZ, the erased part of dK   4: S0 dY, dQ   5 (0 where there is no rest): dS1 u
     static constexpr bool REST = PI < PM;
     static constexpr int S0 = 0, SCOLS = PM * KD / 2, R0 = SCOLS, R1 = R0 + kTok, R2 = R1 + kTok, R3 = R2 + kTok, R4 = R3 + kTok, R5 = REST ? R4 + kTok : R0;
-    static_assert(R4 + kTok <= 512 && R5 + kTok <= 512 && BYTES + 7168 <= 227 * 1024 && PM * kTok / 2 <= 2 * kTok && PM * TILE >= PM * kMatrix, "tensor and shared memory");
+    static_assert(R4 + kTok <= 512 && R5 + kTok <= 512 && BYTES + 9728 <= 227 * 1024 && PM * kTok / 2 <= 2 * kTok && PM * TILE >= PM * kMatrix, "tensor and shared memory");
 };
 constexpr int kGradThreads = 512;
 
@@ -374,7 +374,9 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
     // bar_a, bar_b: products; full[0]: a unit's k, q, v, A, gates; full[1]: the gradient behind the chunk; full[2]: dY, the state before it
     __shared__ WalkShared ws;
     __shared__ __align__(16) float gates2[2][kGates];
-    __shared__ float sums[2][4][kTok], erased[4][kTok], total[16], writes[16];
+    // sums over lanes, by the four warps of a quarter: dZ R | S0's part of a token's query and key | delta (dS1 u) k | a column's pairs in front
+    // of it; a row's pairs in a quarter (rows 0 .. 63 of F, 64 .. of E without beta)
+    __shared__ float sums[4][4][kTok], pairs[4][2 * kTok], total[16];
     unsigned char *sm = align_images(raw);
     const int tid = threadIdx.x, lane = tid & 31, warp = uniform_warp(tid >> 5), row = 32 * (warp & 3) + lane, quarter = warp >> 2, share = a.H / a.Hk, c0 = 16 * quarter;
     const int rows8 = kept_rows(a.Dv), ksteps = (a.Dk + 15) / 16, vsteps = (a.Dv + 15) / 16;
@@ -542,8 +544,8 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
         if (warp == 0) {
             issue_ts<PM, PI, PM, true, KD / 16, B_ALL, 4>(tb + C::R0, tb + C::S0, KD / 2, IK, C::TILE, ksteps, kTok, false);
             umma_commit(&ws.bar_a);
-            // rows 64 ..: K K^T
-            if (C::REST) issue_ss<PI, PI, PI, true, true, KD / 16, B_ALL, 4>(tb + C::R2, IY, C::TILE, C::K - C::DY, IK, C::TILE, ksteps, kTok, false);
+            // rows 0 .. 63: Q K^T, rows 64 ..: K K^T
+            if (C::ROOM) issue_ss<PI, PI, PI, true, true, KD / 16, B_ALL, 4>(tb + C::R2, IQ, C::TILE, C::K - C::Q, IK, C::TILE, ksteps, kTok, false);
         }
         done();
 #pragma unroll 1
@@ -639,7 +641,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
             // rows 0 .. 63: dY U^T, rows 64 ..: dZ U^T; where dY is one plane, dZ's second goes into a sum of its own
             issue_ss<PI, PM, PM, true, true, KD / 16, B_ALL, 4>(tb + C::R1, IY, C::TILE, C::DZ - C::DY, IU, C::TILE, vsteps, kTok, false);
             if (C::REST) issue_ss<1, 1, 1, true, true, KD / 16, B_ALL, 4>(tb + C::R0, IY + C::TILE, C::TILE, C::DZ - C::DY, IU, C::TILE, vsteps, kTok, false);
-            else issue_ss<PI, PI, PI, true, true, KD / 16, B_ALL, 4>(tb + C::R2, IY, C::TILE, C::K - C::DY, IK, C::TILE, ksteps, kTok, false);
+            if (!C::ROOM) issue_ss<PI, PI, PI, true, true, KD / 16, B_ALL, 4>(tb + C::R2, IY, C::TILE, C::K - C::DY, IK, C::TILE, ksteps, kTok, false);    // rows 64 ..: K K^T
             umma_commit(&ws.bar_a);
         }
         // the gradient behind the chunk in the state's place, while those are formed
@@ -658,10 +660,15 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
         done();
         if (C::ROOM && more && tid == 0 && !walk_given_up(&ws)) copy_early(then);   // (dY and the state's place are free: their products are through, every thread has read)
         __syncwarp();
-        {   // F and E in the lower triangles, where their lanes' rows are tokens
+        if (!C::ROOM) {                                      // queries take dY's place
+            load_tile<T>(sm + C::Q, C::TILE, (const T *)a.q, qk, all, a.L, a.Dk, nv, tid, kGradThreads);
+            clear_rows(sm + C::Q, C::TILE, PI, a.Dk, KD, tid, kGradThreads);
+            __syncthreads();
+        }
+        {   // F and E in the lower triangles, where their lanes' rows are tokens, and what they say about the decays
             const int i = row & 63;
-            const float Hi = ghi[i], Li = glo[i], bi = -beta[i];
-            float own = 0.f;
+            const float Hi = ghi[i], Li = glo[i], bi = -beta[i], scale = warp & 2 ? bi : 1.f;
+            float own = 0.f;                                 // of this row's pairs in the quarter, up to a column
 #pragma unroll 1
             for (int g = 0; g < 2; ++g) {
                 const int c = c0 + 8 * g;
@@ -673,45 +680,55 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
                 shared8(hj, ghi + c);
                 shared8(lj, glo + c);
                 tmem_wait_ld();
+                if (!C::ROOM && !(warp & 2)) {               // Q K^T with its ratios: P
+                    const unsigned char *P = a.images + at * (2 * PM * kMatrix) + PM * kMatrix;
+                    for (int q = 0; q < PM; ++q) HN_G(P + q * kMatrix + image_at(i, c >> 3), 16);
+                    image8<PM>(y, P, kMatrix, i, c >> 3);
+                }
+                __syncwarp();
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const float r = ratio(Hi, Li, e & 1 ? hj[e / 2].y : hj[e / 2].x, e & 1 ? lj[e / 2].y : lj[e / 2].x);
-                    if (warp & 2) {
-                        if (C::REST) x[e] += z[e];
-                        x[e] = c + e < i ? r * x[e] : 0.f;
-                        own = c + e < i ? fmaf(x[e], y[e], own) : own;
-                        x[e] *= bi;
-                    } else x[e] = c + e <= i ? r * x[e] : 0.f;
+                    if (C::REST && (warp & 2)) x[e] += z[e];
+                    const float plain = x[e];
+                    x[e] = c + e < i || (c + e == i && !(warp & 2)) ? r * x[e] : 0.f;
+                    z[e] = c + e <= i ? own * scale : 0.f;
+                    own = c + e < i ? fmaf(C::ROOM || (warp & 2) ? x[e] : plain, y[e], own) : own;
+                    x[e] *= scale;
                 }
                 planes8_to_image<PM>(sm + (warp & 2 ? C::DZ : C::A), kMatrix, i, c >> 3, x);
+                const float before = column_sum8(z, lane);
+                if (!(lane & 3)) sums[3][warp & 3][c + (lane >> 2)] = before;
                 // dQ and the erased part of dK, as far as they come from the state: F k and E k are added to them
                 f2 p[4], q[4];
                 tmem_ld8(p, lane_r + C::R4 + 8 * g);
                 tmem_ld8(q, lane_r + C::R3 + 8 * g);
                 shared8(ga, gamma + c);
                 shared8(be, gates + 3 * kTok + c);
+                if (row < KD) {
+                    image8<PI>(x, sm + C::Q, C::TILE, row, c >> 3);
+                    image8<PI>(y, sm + C::K, C::TILE, row, c >> 3);
+                }
                 tmem_wait_ld();
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     p[e] = mul2(p[e], ga[e]);
                     q[e] = mul2(q[e], be[e]);
+                    const f2 both = fma2(q[e], make2(y[2 * e], y[2 * e + 1]), mul2(p[e], make2(x[2 * e], x[2 * e + 1])));
+                    z[2 * e] = row < a.Dk ? both.x : 0.f;    // (a lane without a channel holds whatever lay behind an image)
+                    z[2 * e + 1] = row < a.Dk ? both.y : 0.f;
                 }
                 tmem_st8(lane_r + C::R4 + 8 * g, p);
                 tmem_st8(lane_r + C::R3 + 8 * g, q);
+                const float state = column_sum8(z, lane);
+                if (!(lane & 3)) sums[1][warp & 3][c + (lane >> 2)] = state;
             }
-            if (warp & 2) erased[quarter][i] = own;
+            pairs[quarter][row] = own;
         }
-        if (!C::ROOM) {                                      // queries take dY's place
-            load_tile<T>(sm + C::Q, C::TILE, (const T *)a.q, qk, all, a.L, a.Dk, nv, tid, kGradThreads);
-            clear_rows(sm + C::Q, C::TILE, PI, a.Dk, KD, tid, kGradThreads);
-        }
-        uint4 qs[2], ks[2];
+        uint4 ks[2];
         if (C::ROOM && row < KD)
 #pragma unroll
-            for (int g = 0; g < 2; ++g) {
-                qs[g] = *(const uint4 *)(sm + C::Q + image_at(row, 2 * quarter + g));
-                ks[g] = *(const uint4 *)(sm + C::K + image_at(row, 2 * quarter + g));
-            }
+            for (int g = 0; g < 2; ++g) ks[g] = *(const uint4 *)(sm + C::K + image_at(row, 2 * quarter + g));
         go();
         if (warp == 0) {
             issue_ss<PI, PM, PM, false, false, kTok / 16, B_LOWER>(tb + C::R4, IK, C::TILE, 0, IA, kMatrix, kTok / 16, kTok, true);             // F k
@@ -723,11 +740,10 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
         done();
         if (C::ROOM && more && tid == 0 && !walk_given_up(&ws)) copy_rest(then, phase ^ 1);     // (every product is through, and what the threads read they have)
         __syncwarp();
-        float written = 0.f;
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
             const int c = c0 + 8 * g;
-            const bool in = row < a.Dk;                      // (a lane without a channel holds whatever lay behind an image)
+            const bool in = row < a.Dk;
             float x[8], y[8], z[8], w[8], u[8];
             f2 de[4];
             tmem_ld8(x, lane_r + C::R4 + 8 * g);             // dQ of this head
@@ -735,26 +751,18 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
             tmem_ld8(w, lane_r + C::R2 + 8 * g);
             tmem_ld8(u, lane_r + C::R5 + 8 * g);
             shared8(de, delta + c);
-            if (C::ROOM) bf16_widen8(z, qs[g]);
-            else if (row < KD) image8<PI>(z, sm + C::Q, C::TILE, row, c >> 3);
+            if (C::ROOM) bf16_widen8(z, ks[g]);
+            else if (row < KD) image8<PI>(z, sm + C::K, C::TILE, row, c >> 3);
             tmem_wait_ld();
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                dq[g][e] += x[e];
-                x[e] = in ? x[e] * z[e] : 0.f;
-            }
-            if (C::ROOM) bf16_widen8(z, ks[g]);
-            else if (row < KD) image8<PI>(z, sm + C::K, C::TILE, row, c >> 3);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
                 u[e] *= e & 1 ? de[e / 2].y : de[e / 2].x;
-                w[e] += u[e];
-                dk[g][e] += y[e] + w[e];
-                x[e] = in ? fmaf(z[e], y[e] - w[e], x[e]) : 0.f;
-                written = in ? fmaf(u[e], z[e], written) : 0.f;
+                dq[g][e] += x[e];
+                dk[g][e] += y[e] + (w[e] + u[e]);
+                x[e] = in ? u[e] * z[e] : 0.f;
             }
             const float sum = column_sum8(x, lane);
-            if (!(lane & 3)) sums[1][warp & 3][c + (lane >> 2)] = sum;
+            if (!(lane & 3)) sums[2][warp & 3][c + (lane >> 2)] = sum;
             if (last) {                                      // U is through: dK into half of its place
                 if (C::ROOM && a.copies) {
                     if (row < KD) {
@@ -768,9 +776,6 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
                 }
             }
         }
-#pragma unroll
-        for (int m = 1; m < 32; m <<= 1) written += __shfl_xor_sync(~0u, written, m);
-        if (lane == 0) writes[warp] = written;
         fence_async_smem();
         tmem_fence_before_sync();
         __syncthreads();                                     // images, sums and tensor memory have been read, results written
@@ -788,30 +793,64 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
             }
         }
         __syncwarp();
-        if (warp < 2) {                                      // two tokens a lane of warp 0: sums from the chunk's end; warp 1: beta
+        if (warp < 2) {                                      // two tokens a lane; warp 0: the decays, warp 1: beta
             float s[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int i = 2 * lane + e;
-                s[e] = (sums[1 - warp][0][i] + sums[1 - warp][1][i]) + (sums[1 - warp][2][i] + sums[1 - warp][3][i]);
-                if (warp) s[e] -= (erased[0][i] + erased[1][i]) + (erased[2][i] + erased[3][i]);
-            }
+            auto token = [&](int what, int i) { return (sums[what][0][i] + sums[what][1][i]) + (sums[what][2][i] + sums[what][3][i]); };
             if (warp == 0) {
-                float w = lane < 16 ? fmaf(gamma[kTok - 1], total[lane], writes[lane]) : 0.f;
+                // what crosses a token: pairs of a query or an erasure from it on and a value before it (in the quarter of the earlier token's
+                // column: summed above; in the quarters before), the state before the chunk and tokens from it on, the gradient behind the
+                // chunk and tokens before it, the state before the chunk and the gradient behind it.  Every sum runs towards its larger terms
+                float c[2], d[2], in[3][2], rest[4], front;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int i = 2 * lane + e;
+                    c[e] = token(1, i);
+                    d[e] = token(2, i);
+                    s[e] = token(3, i);
+                    float up = 0.f;                          // row i's pairs in the quarters 0 .. q
+#pragma unroll
+                    for (int q = 0; q < 3; ++q) in[q][e] = up += fmaf(-beta[i], pairs[q][kTok + i], pairs[q][i]);
+                }
+                rest[0] = c[0] + c[1];
+#pragma unroll
+                for (int q = 0; q < 3; ++q) rest[q + 1] = in[q][0] + in[q][1];
+                front = d[0] + d[1];
+#pragma unroll
+                for (int m = 1; m < 32; m <<= 1) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const float o = __shfl_down_sync(~0u, rest[q], m);
+                        if (lane + m < 32) rest[q] += o;
+                    }
+                    const float o = __shfl_up_sync(~0u, front, m);
+                    if (lane >= m) front += o;
+                }
+#pragma unroll
+                for (int q = 0; q < 4; ++q) { const float o = __shfl_down_sync(~0u, rest[q], 1); rest[q] = lane < 31 ? o : 0.f; }
+                const float o = __shfl_up_sync(~0u, front, 1);
+                front = lane ? o : 0.f;
+                float w = lane < 16 ? gamma[kTok - 1] * total[lane] : 0.f;
 #pragma unroll
                 for (int m = 1; m < 16; m <<= 1) w += __shfl_xor_sync(~0u, w, m);
                 w = __shfl_sync(~0u, w, 0);
-                const double v = (double)s[0] + s[1];
-                double run = v;                              // (sums of many signs: in 64 bits)
+                const int quarter_of = lane >> 3;
 #pragma unroll
-                for (int m = 1; m < 32; m <<= 1) {
-                    const double o = __shfl_down_sync(~0u, run, m);
-                    if (lane + m < 32) run += o;
+                for (int e = 1; e >= 0; --e) {
+                    rest[0] += c[e];
+                    float before = 0.f;
+#pragma unroll
+                    for (int q = 0; q < 3; ++q) {
+                        rest[q + 1] += in[q][e];
+                        if (quarter_of == q + 1) before = rest[q + 1];
+                    }
+                    s[e] += before + rest[0] + (e ? front + d[0] : front) + w;
                 }
-                run += w;
-                s[0] = (float)run;
-                s[1] = (float)(run - (v - s[1]));
-            }
+            } else
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int i = 2 * lane + e;
+                    s[e] = token(0, i) - ((pairs[0][kTok + i] + pairs[1][kTok + i]) + (pairs[2][kTok + i] + pairs[3][kTok + i]));
+                }
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int i = 2 * lane + e;
