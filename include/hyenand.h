@@ -353,8 +353,13 @@ int hyenand_delta_backward(int B, int H, int Hk, int L, int Dk, int Dv, int deca
 int hyenand_delta_step(int B, int H, int Hk, int Dk, int Dv, int decay, int dtype, const void *q, const void *k, const void *v, const float *g,
                        const float *beta, const float *state, const int *active, void *y, float *new_state, void *cuda_stream);
 /* Every wait of the kernels (for copies, for the tensor cores) is bounded.  Returns 0, or 1 once one has given up since the library
- * was loaded (the call that met it left its results incomplete), -1 if the word cannot be read.  Synchronises the device. */
+ * was loaded, -1 if the word cannot be read.  In the call that met it, the chunk concerned and all that follows from it is NaN.
+ * Synchronises the device. */
 int hyenand_delta_device_status(void);
+/* For tests of the checked build: from now on the calls' kernel `kernel` (0 .. 6: chunk factors, walk, maps of segments, join, walk back, its
+ * maps, gradients) takes a wait of head 0 at chunk `chunk` (join: segment) to run out, though what it waits for comes: wait 0 for copies, 1 and 2
+ * for products; kernel < 0: none again.  Returns 0, -1 in the product library. */
+int hyenand_debug_delta_late(int kernel, int chunk, int wait);
 
 /*
  * Queries and keys as heads: the norm of each head and the rotation by its token's position on the native grid, in one pass, as a mixer

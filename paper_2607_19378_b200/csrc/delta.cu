@@ -9,6 +9,8 @@
 // Few heads and many chunks: the walk is serial, so a head is cut into segments.  Where a segment starts from nothing it gives N, where it
 //     starts from the identity without values it gives Phi, and from any state S it ends at S Phi + N: both walks run for all
 //     segments at once, a small kernel joins them, and the walk proper starts every segment at once.
+#include <atomic>
+
 #include "delta.cuh"
 
 namespace hn {
@@ -107,15 +109,15 @@ template <typename T, int KD> __global__ void __launch_bounds__(128) delta_prepa
     __syncthreads();
     tmem_fence_after_sync();
     const unsigned tb = slot, images = smem_u32(sm);
-    bool ok = !copied || mbar_wait(&there, 0);
+    bool ok = (!copied || mbar_wait(&there, 0)) && !is_late(a, LATE_PREPARE, bh, chunk, LATE_COPIES);
     if (warp == 0) {
         issue_ss<C::PI, C::PI, C::PI, true, true, KD / 16>(tb, images, C::PITCH, C::TILE, images, C::PITCH, steps, kTok, false);
         umma_commit(&bar);
     }
-    if (tid < kTok) {                                        // (the decays meanwhile)
+    auto store_gates = [&](float sick) {                     // (of a token each; sick: 0, or NaN)
         float *gates = a.gates + at * kGates;
-        const float gamma = ratio(hi[tid], lo[tid], 0.f, 0.f);
-        const float x[6] = {gamma, ratio(hi[kTok - 1], lo[kTok - 1], hi[tid], lo[tid]), beta[tid], -beta[tid] * gamma, hi[tid], lo[tid]};
+        const float gamma = ratio(hi[tid], lo[tid], 0.f, 0.f) + sick;
+        const float x[6] = {gamma, ratio(hi[kTok - 1], lo[kTok - 1], hi[tid], lo[tid]) + sick, beta[tid] + sick, -beta[tid] * gamma, hi[tid] + sick, lo[tid] + sick};
 #pragma unroll
         for (int e = 0; e < 6; ++e) {
             float *to = gates + (e < 4 ? 0 : kSums - kCarry) + e * kTok + tid;
@@ -123,18 +125,21 @@ template <typename T, int KD> __global__ void __launch_bounds__(128) delta_prepa
             *to = x[e];
         }
         if (tid == kTok - 1) {                               // (its gamma is the chunk's)
-            const float less = expm1f((hi[tid] + lo[tid]) * 0.6931471805599453f);
+            const float less = expm1f((hi[tid] + lo[tid]) * 0.6931471805599453f) + sick;
             HN_G(gates + kCarry, 16);
             *(float4 *)(gates + kCarry) = less > -0.5f ? make_float4(1.f, less, 0.f, 0.f) : make_float4(0.f, gamma, 0.f, 0.f);
         }
-    }
-    ok = mbar_wait(&bar, 0) && ok;
-    if (!ok) {
-        atomicExch(&hn_delta_status, 1);
-        if (copied) mbar_wait(&there, 0);                     // (copies under way end before the CTA does)
-    }
+    };
+    if (tid < kTok) store_gates(0.f);                        // (the decays meanwhile)
+    ok = mbar_wait(&bar, 0) && ok && !is_late(a, LATE_PREPARE, bh, chunk, LATE_PRODUCT);
     tmem_fence_after_sync();
-    __syncthreads();                                          // (every thread has waited: the tiles' place is free)
+    if (__syncthreads_or(!ok)) {                             // (every thread has waited: the tiles' place is free)
+        // the chunk's factors are NaN, and with them all that comes of it; copies and products under way end before the CTA does
+        if (!ok) atomicExch(&hn_delta_status, 1);
+        if (copied) mbar_wait(&there, 0);
+        mbar_wait(&bar, 0);
+        if (tid < kTok) store_gates(kLost);
+    }
     // lanes 0 .. 63: rows of k k^T, lanes 64 .. 127: rows of q k^T
     const int i = tid & 63;
     {
@@ -249,6 +254,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
     using C = Walk<T, KD>;
     constexpr int PI = C::PI, PM = C::PM, HC = KD / 2;
     constexpr bool RUN = MODE == WALK_RUN;
+    constexpr int KERNEL = RUN ? LATE_WALK : LATE_MAPS;
     extern __shared__ __align__(1024) unsigned char raw[];
     __shared__ WalkShared ws;
     unsigned char *sm = align_images(raw);
@@ -286,8 +292,10 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             // one thread waits, for every chunk in turn: the others have passed over copied ones, and a barrier's parity tells them nothing
             if (i >= C::STAGES && ft == 0) WAIT(&ws.empty[s], (i / C::STAGES - 1) & 1);
             if (!copied) fetchers_sync();
-            if (ft == 0 && !walk_given_up(&ws)) {
+            const bool begun = ft == 0 && !walk_given_up(&ws);
+            if (begun) {
                 const long long at = bh * a.chunks + c;
+                ++ws.begun[s];
                 const unsigned bytes = RUN ? C::IMAGES : C::IMAGES / 2, tiles = copied ? (RUN ? 2 : 1) * C::TENSOR + (values ? C::TILE : 0) : 0;
                 mbar_expect_tx(&ws.full[s], bytes + kWalkGates + tiles);
                 if (copied) {
@@ -306,7 +314,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
                 fence_async_smem();
                 fetchers_sync();
             }
-            if (ft == 0) mbar_arrive(&ws.full[s]);
+            if (begun) mbar_arrive(&ws.full[s]);
         }
     } else if (warp == 8) {
         // ---- the products
@@ -314,6 +322,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
         for (int c = first, i = 0; c < last; ++c, ++i) {
             const int s = i % C::STAGES;
             const unsigned par = i & 1, k = smem_u32(sm) + s * C::STAGE, A = k + C::A, P = A + PM * kMatrix;
+            walk_late(&ws, is_late(a, KERNEL, bh, c, LATE_COPIES));
             WAIT(&ws.full[s], (i / C::STAGES) & 1);
             // S k, the first half of S's columns as soon as they are there
             WAIT(&ws.state[0], par);
@@ -349,6 +358,8 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             }
             umma_commit(&ws.empty[s]);
         }
+        // (the last arrival on a barrier that nobody waits for comes before the CTA ends)
+        if (last > first) WAIT(&ws.empty[(last - first - 1) % C::STAGES], ((last - first - 1) / C::STAGES) & 1);
     } else if (warp >= 12) {
         // ---- results: y's first sum times gamma, then y as an image that a copy takes away, or by these threads
         const int row = 32 * (warp & 3) + lane;
@@ -373,18 +384,28 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             }
             walk_ready(&ws.o_ready, lane);
             unsigned char *image = sm + C::STAGES * C::STAGE + (i & 1) * C::TILE;
+            walk_late(&ws, is_late(a, KERNEL, bh, c, LATE_RESULT));
             WAIT(&ws.bar_y, i & 1);
             tmem_fence_after_sync();
+            auto put = [&](int e, const float (&y)[8]) {
+                if (C::VALUES && stored) {
+                    if (row < KD) *(uint4 *)(image + image_at(row, e >> 3)) = bf16_8(y, n - t - e);
+                } else if (real && t + e < a.L) store8<T>((T *)a.y, vrow + t + e, a.L, a.L - t - e, n - t - e, y);
+            };
 #pragma unroll 2
             for (int e = 0; e < kTok; e += 8) {
                 float y[8];
                 tmem_ld8(y, lane_y + e);
                 tmem_wait_ld();
-                if (C::VALUES && stored) {
-                    if (row < KD) *(uint4 *)(image + image_at(row, e >> 3)) = bf16_8(y, n - t - e);
-                } else if (real && t + e < a.L) store8<T>((T *)a.y, vrow + t + e, a.L, a.L - t - e, n - t - e, y);
+                put(e, y);
             }
             walk_ready(&ws.o_taken, lane);
+            if (walk_given_up(&ws)) {
+                const float y[8] = {kLost, kLost, kLost, kLost, kLost, kLost, kLost, kLost};
+#pragma unroll 1
+                for (int e = 0; e < kTok; e += 8) put(e, y);
+                __syncwarp();
+            }
             if (stored) {
                 fence_async_smem();
                 takers_sync();
@@ -459,6 +480,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             walk_ready(&ws.z_ready, lane);
             if (mark) keep_state<HC / 16, HC / 8>(mark, S, row, a.Dv, half * HC, a.Dk);
             const Carry carry((const float *)(st + C::GATES));
+            walk_late(&ws, is_late(a, KERNEL, bh, c, LATE_PRODUCT));
             WAIT(&ws.bar_b, par);
             tmem_fence_after_sync();
             tmem_ld(x, lane_x);
@@ -480,6 +502,9 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             WAIT(&ws.bar_c[half], par);
             tmem_fence_after_sync();
             state_onwards<PM>(S, carry, lane_d, lane_s, KD / 2);
+            if (walk_given_up(&ws))
+#pragma unroll
+                for (int j = 0; j < HC / 2; ++j) S[j] = pair(kLost);
         }
         tmem_wait_st();
         auto flat = [&](float (&s)[HC]) {
@@ -500,11 +525,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
         }
         tmem_fence_before_sync();
     }
-    __syncthreads();
-    if (ws.gave_up && tid == 0) {
-        atomicExch(&hn_delta_status, 1);
-        walk_drain(&ws, C::STAGES);
-    }
+    walk_end(&ws, C::STAGES, &hn_delta_status, warp, 8);
     if (warp == 0) tmem_dealloc(tb, 512);
     pdl_trigger();                                           // (late: see delta.cuh)
 }
@@ -528,14 +549,14 @@ __global__ void __launch_bounds__(256) delta_join_kernel(DeltaArgs a, const floa
     for (int e = tid; e < 2 * 128 * 128 / 4; e += 256) ((float4 *)phi)[e] = make_float4(0.f, 0.f, 0.f, 0.f);
     if (tid == 0) {
         mbar_init(&ws.full[0], 1); mbar_init(&ws.full[1], 1);
-        ws.gave_up = 0;
-        fence_mbar_init();
+        walk_marks_init(&ws);
     }
     fence_async_smem();
     pdl_join();
     __syncthreads();
     auto fetch = [&](int i) {                                // (one thread) the i-th segment's
         const int s = reverse ? n - 1 - i : i;
+        ++ws.begun[i & 1];
         mbar_expect_tx(&ws.full[i & 1], bytes);
         bulk_load(phi + (i & 1) * 128 * 128, a.maps + (bh * n + s) * map + (long long)a.Dv * pitch, bytes, &ws.full[i & 1]);
     };
@@ -559,6 +580,7 @@ __global__ void __launch_bounds__(256) delta_join_kernel(DeltaArgs a, const floa
         float4 add = make_float4(0.f, 0.f, 0.f, 0.f);
         if (row < a.Dv && 4 * quad < pitch) { const float4 *p = (const float4 *)(a.maps + (bh * n + s) * map + (long long)row * pitch) + quad; HN_G(p, 16); add = *p; }
         __syncthreads();
+        walk_late(&ws, is_late(a, LATE_JOIN, bh, s, LATE_COPIES));
         WAIT(&ws.full[i & 1], (i >> 1) & 1);
         f2 acc[R][2];
 #pragma unroll
@@ -590,12 +612,9 @@ __global__ void __launch_bounds__(256) delta_join_kernel(DeltaArgs a, const floa
             const float4 p = *(const float4 *)&part[e][eighth][4 * quad];
             v.x += p.x; v.y += p.y; v.z += p.z; v.w += p.w;
         }
+        if (walk_given_up(&ws)) v = make_float4(kLost, kLost, kLost, kLost);
     }
-    __syncthreads();
-    if (ws.gave_up && tid == 0) {
-        atomicExch(&hn_delta_status, 1);
-        walk_drain(&ws, 2);
-    }
+    walk_end(&ws, 2, &hn_delta_status, 0, -1);
 }
 
 // ---- one token ------------------------------------------------------------------------------------------------------
@@ -738,6 +757,10 @@ static int segments_of(long long heads, int chunks)
     return (int)((chunks + most - 1) / most);
 }
 
+#ifdef HYENAND_DEBUG
+static std::atomic<int> late_kernel{-1}, late_chunk{-1}, late_wait{-1};
+#endif
+
 static int fill(DeltaArgs &a, int B, int H, int Hk, int L, int Dk, int Dv, int decay, int dtype)
 {
     if (B < 1 || H < 1 || Hk < 1 || L < 1 || Dk < 1 || Dv < 1) return fail(HYENAND_ERR_INVALID_ARG, "B, H, Hk, L, Dk and Dv must be >= 1");
@@ -747,6 +770,9 @@ static int fill(DeltaArgs &a, int B, int H, int Hk, int L, int Dk, int Dv, int d
     if (Dk > 128 || Dv > 128) return fail(HYENAND_ERR_UNSUPPORTED, "heads of up to 128 channels (Dk = %d, Dv = %d)", Dk, Dv);
     if (L > (1 << 30)) return fail(HYENAND_ERR_UNSUPPORTED, "L = %d is above 2^30", L);
     if ((long long)B * H > (1 << 24)) return fail(HYENAND_ERR_UNSUPPORTED, "B * H is above 2^24");
+#ifdef HYENAND_DEBUG
+    a.late_kernel = late_kernel; a.late_chunk = late_chunk; a.late_wait = late_wait;
+#endif
     a.B = B; a.H = H; a.Hk = Hk; a.L = L; a.Dk = Dk; a.Dv = Dv; a.decay = decay;
     a.chunks = (L + kTok - 1) / kTok;
     if ((long long)B * H * a.chunks > 0x3fffffffll) return fail(HYENAND_ERR_UNSUPPORTED, "B * H * L is above 2^36");
@@ -783,6 +809,17 @@ extern "C" long long hyenand_delta_workspace_bytes(int B, int H, int Hk, int L, 
     DeltaArgs a{};
     if (fill(a, B, H, Hk, L, Dk, Dv, DELTA_NONE, dtype)) return 0;
     return (long long)delta_sizes(a, dtype, backward != 0).all;
+}
+
+extern "C" int hyenand_debug_delta_late(int kernel, int chunk, int wait)
+{
+#ifdef HYENAND_DEBUG
+    late_kernel = kernel; late_chunk = chunk; late_wait = wait;
+    return 0;
+#else
+    (void)kernel; (void)chunk; (void)wait;
+    return -1;
+#endif
 }
 
 extern "C" int hyenand_delta_device_status(void)

@@ -56,7 +56,22 @@ struct DeltaArgs {
     float *dstates, *dz;                                  // [B H][chunks] states as kept, [B H][chunks][Dv][64]
     int B, H, Hk, L, Dk, Dv, decay, chunks, segments, per_segment;
     int copies;                                           // 1: tiles come as tensor copies
+#ifdef HYENAND_DEBUG
+    int late_kernel, late_chunk, late_wait;               // the wait of head 0 that is taken to run out (late_kernel < 0: none)
+#endif
 };
+// The kernels whose waits the checked build can take to run out, and which wait of a chunk (of a segment, in the join): for copies; for a
+// product, by the threads that go on from it; for a product, by those that store it
+enum { LATE_PREPARE, LATE_WALK, LATE_MAPS, LATE_JOIN, LATE_BACK, LATE_BACK_MAPS, LATE_GRADIENTS };
+enum { LATE_COPIES, LATE_PRODUCT, LATE_RESULT };
+#ifdef HYENAND_DEBUG
+__device__ __forceinline__ bool is_late(const DeltaArgs &a, int kernel, long long head, int chunk, int wait)
+{
+    return a.late_kernel == kernel && head == 0 && a.late_chunk == chunk && a.late_wait == wait;
+}
+#else
+__device__ __forceinline__ bool is_late(const DeltaArgs &, int, long long, int, int) { return false; }
+#endif
 
 __host__ __device__ __forceinline__ int map_pitch(int Dk) { return (Dk + 3) & ~3; }
 
@@ -544,16 +559,18 @@ __device__ __forceinline__ int uniform_warp(int warp) { return __shfl_sync(~0u, 
 
 // ---- walks -----------------------------------------------------------------------------------------------------------
 
-// What the warps of a walk share beside the stages.  A wait that gives up ends all later ones of the CTA.
+// What the warps of a walk share beside the stages.  A wait that gives up ends all later ones of the CTA, and what is computed and stored
+// from there on is NaN: whoever went on without what it waited for, and whose place it then took, finds the mark behind what it has read.
 struct WalkShared {
-    uint64_t full[4], empty[4], bar_a, bar_b, bar_c[2], bar_q, bar_y;          // copies; products
+    uint64_t full[4], empty[4], bar_a, bar_b, bar_c[2], bar_q, bar_y, bar_end; // copies; products; all of them
     uint64_t state[2], z_ready, u_ready, p_ready;             // the computing warps (of a half) to the one that issues
     uint64_t o_ready, o_taken;                                // the warps with the results to the one that issues
     unsigned slot;
-    int gave_up;
+    int gave_up, begun[4];                                    // begun: how often copies to a stage were begun
 };
+constexpr float kLost = __builtin_nanf("");
 // Bounded by its polls, which sleep up to some microseconds each.  As few instructions as can be, for there are twenty of these waits in a
-// walk's loop (see below); who gives up leaves a mark, and what it means is said at the kernel's end.
+// walk's loop; who gives up leaves a mark, and the status is set at the kernel's end (see walk_end).
 constexpr unsigned kWalkPolls = 1u << 20;
 __device__ __forceinline__ void walk_wait(WalkShared *w, uint64_t *bar, unsigned parity)
 {
@@ -562,6 +579,38 @@ __device__ __forceinline__ void walk_wait(WalkShared *w, uint64_t *bar, unsigned
                  " ld.volatile.shared.u32 f, [%2];\n add.u32 i, i, 1;\n setp.lt.u32 p, i, %3;\n setp.eq.and.u32 p, f, 0, p;\n @p bra WALK_POLL_%=;\n"
                  " st.volatile.shared.u32 [%2], 1;\n"
                  "WALK_DONE_%=:\n}\n" ::"r"(smem_u32(bar)), "r"(parity), "r"(smem_u32(&w->gave_up)), "n"(kWalkPolls) : "memory");
+}
+__device__ __forceinline__ bool walk_given_up(const WalkShared *w) { return __builtin_expect(*(const volatile int *)&w->gave_up, 0); }
+__device__ __forceinline__ void walk_late(WalkShared *w, bool late) { if (late) *(volatile int *)&w->gave_up = 1; }
+__device__ __forceinline__ void walk_marks_init(WalkShared *w)
+{
+    mbar_init(&w->bar_end, 1);
+    w->gave_up = w->begun[0] = w->begun[1] = w->begun[2] = w->begun[3] = 0;
+    fence_mbar_init();
+}
+__device__ __forceinline__ void walk_last_wait(uint64_t *bar, unsigned parity)
+{
+#pragma unroll 1
+    for (unsigned i = 0; i < kWalkPolls && !mbar_try_wait(bar, parity); ++i) { }
+}
+// The end of a CTA, by all its threads, `issuer` the warp that issued its products (-1: there are none).  Where a wait has given up no more
+// copies were begun, and the CTA waits (bounded) for those under way and for its products, so that they end before the memory they
+// work on is another CTA's.
+__device__ __forceinline__ void walk_end(WalkShared *w, int stages, int *status, int warp, int issuer)
+{
+    __syncthreads();
+    if (!w->gave_up) return;
+    if (warp == issuer) {
+        umma_commit(&w->bar_end);
+        walk_last_wait(&w->bar_end, 0);
+    }
+    if (threadIdx.x == 0) {
+        atomicExch(status, 1);
+#pragma unroll 1
+        for (int s = 0; s < stages; ++s)
+            if (w->begun[s]) walk_last_wait(&w->full[s], (w->begun[s] - 1) & 1);
+    }
+    __syncthreads();
 }
 __device__ __forceinline__ void mbar_arrive(uint64_t *bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];\n" ::"r"(smem_u32(bar)) : "memory"); }
 // Warps 0 .. 7 compute, warp 8 issues the products, warps 9 .. 11 fetch, warps 12 .. 15 take results away.  What is written into tensor
@@ -573,18 +622,7 @@ __device__ __forceinline__ void walk_init(WalkShared *w, int stages)
     mbar_init(&w->bar_a, 1); mbar_init(&w->bar_b, 1); mbar_init(&w->bar_c[0], 1); mbar_init(&w->bar_c[1], 1); mbar_init(&w->bar_q, 1); mbar_init(&w->bar_y, 1);
     mbar_init(&w->state[0], 4); mbar_init(&w->state[1], 4);
     mbar_init(&w->z_ready, 8); mbar_init(&w->u_ready, 8); mbar_init(&w->p_ready, 8); mbar_init(&w->o_ready, 4); mbar_init(&w->o_taken, 4);
-    w->gave_up = 0;
-    fence_mbar_init();
-}
-// A wait has given up: no more copies are begun, and whoever leaves last waits (bounded) for those under way, in whichever phase their barriers
-// are, so that they end before the memory they go to is another CTA's
-__device__ __forceinline__ bool walk_given_up(const WalkShared *w) { return *(const volatile int *)&w->gave_up; }
-__device__ __forceinline__ void walk_drain(WalkShared *w, int stages)
-{
-    for (int s = 0; s < stages; ++s) {
-        mbar_wait(&w->full[s], 0);
-        mbar_wait(&w->full[s], 1);
-    }
+    walk_marks_init(w);
 }
 __device__ __forceinline__ void walk_ready(uint64_t *bar, int lane)
 {

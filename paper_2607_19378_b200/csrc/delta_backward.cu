@@ -40,6 +40,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
     using C = WalkBack<T, KD>;
     constexpr int PI = C::PI, PM = C::PM, HC = KD / 2;
     constexpr bool RUN = MODE == WALK_RUN;
+    constexpr int KERNEL = RUN ? LATE_BACK : LATE_BACK_MAPS;
     extern __shared__ __align__(1024) unsigned char raw[];
     __shared__ WalkShared ws;
     unsigned char *sm = align_images(raw);
@@ -78,8 +79,10 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             // one thread waits, for every chunk in turn: the others have passed over copied ones, and a barrier's parity tells them nothing
             if (i >= C::STAGES && ft == 0) WAIT(&ws.empty[s], (i / C::STAGES - 1) & 1);
             if (!copied) fetchers_sync();
-            if (ft == 0 && !walk_given_up(&ws)) {
+            const bool begun = ft == 0 && !walk_given_up(&ws);
+            if (begun) {
                 const long long at = bh * a.chunks + c;
+                ++ws.begun[s];
                 mbar_expect_tx(&ws.full[s], C::IMAGES + kWalkGates + (copied ? (phi ? 2 : 3) * C::TENSOR : 0));
                 if (copied) {
                     tma_load_3d(st, &maps.k, &ws.full[s], t0, 0, (int)bk);
@@ -96,7 +99,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
                 fence_async_smem();
                 fetchers_sync();
             }
-            if (ft == 0) mbar_arrive(&ws.full[s]);
+            if (begun) mbar_arrive(&ws.full[s]);
         }
     } else if (warp == 8) {
         // ---- the products
@@ -108,6 +111,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             auto gain = [&](int h, unsigned from, unsigned image, bool add) {
                 issue_ts<PM, PI, PM, false, kTok / 16>(tb + (h ? C::D1 : C::D0), from, kTok / 2, image + h * (KD / 2) * 128, C::TILE, kTok / 16, KD / 2, add);
             };
+            walk_late(&ws, is_late(a, KERNEL, bh, last - 1 - i, LATE_COPIES));
             WAIT(&ws.full[s], (i / C::STAGES) & 1);
             // (P^T dY of the chunk before has been read: its dU was there; so has dZ)
             issue_ss<PI, PM, PM, false, true, kTok / 16, B_LOWER_T>(tb + C::Y0, k + C::DY, C::TILE, 0, P, kMatrix, kTok / 16, kTok, false);
@@ -146,6 +150,8 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             if (RUN && C::ROOM) WAIT(&ws.o_taken, par);      // (the gates are read there too)
             umma_commit(&ws.empty[s]);
         }
+        // (the last arrival on a barrier that nobody waits for comes before the CTA ends)
+        if (count) WAIT(&ws.empty[(count - 1) % C::STAGES], ((count - 1) / C::STAGES) & 1);
     } else if (warp >= 12) {
         // ---- gamma dY as an operand; dZ and dV on their way out
         const int row = 32 * (warp & 3) + lane, rows8 = kept_rows(a.Dv);
@@ -182,15 +188,11 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
                 __syncwarp();
                 takers_sync();
             }
+            walk_late(&ws, is_late(a, KERNEL, bh, c, LATE_RESULT));
             WAIT(&ws.bar_b, i & 1);
             tmem_fence_after_sync();
             float4 *to = (float4 *)a.dz + (bh * a.chunks + c) * 16 * rows8;     // dZ: two planes as images, or [quartet of tokens][row]
-#pragma unroll 2
-            for (int e = 0; e < kTok; e += 8) {
-                f2 z[4], be[4];
-                tmem_ld8(z, lane_x + e);
-                shared8(be, gates + 2 * kTok + e);
-                tmem_wait_ld();
+            auto put = [&](int e, const f2 (&z)[4], const f2 (&be)[4]) {
                 if constexpr (C::VALUES) {
                     float x[8];
 #pragma unroll
@@ -209,8 +211,21 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
                     if (row < KD) *(uint4 *)(image + image_at(row, e >> 3)) = bf16_8(y, n - t - e);
                 } else if (real && t + e < a.L) store8<T>((T *)a.dv, vrow + t + e, a.L, a.L - t - e, n - t - e, y);
                 __syncwarp();
+            };
+#pragma unroll 2
+            for (int e = 0; e < kTok; e += 8) {
+                f2 z[4], be[4];
+                tmem_ld8(z, lane_x + e);
+                shared8(be, gates + 2 * kTok + e);
+                tmem_wait_ld();
+                put(e, z, be);
             }
             walk_ready(&ws.o_taken, lane);                   // (the gates have been read as well)
+            if (walk_given_up(&ws)) {
+                const f2 z[4] = {pair(kLost), pair(kLost), pair(kLost), pair(kLost)};
+#pragma unroll 1
+                for (int e = 0; e < kTok; e += 8) put(e, z, z);
+            }
             if (C::VALUES) {
                 fence_async_smem();
                 takers_sync();
@@ -280,6 +295,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             walk_ready(&ws.z_ready, lane);
             if (RUN) keep_state<HC / 16, HC / 8>(keep, S, row, a.Dv, half * HC, a.Dk);
             const Carry carry((const float *)(sm + s * C::STAGE + C::GATES));
+            walk_late(&ws, is_late(a, KERNEL, bh, c, LATE_PRODUCT));
             WAIT(&ws.bar_b, par);
             tmem_fence_after_sync();
             tmem_ld(x, lane_x);
@@ -297,6 +313,9 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             WAIT(&ws.bar_c[half], par);
             tmem_fence_after_sync();
             state_onwards<PM>(S, carry, lane_d, lane_s, KD / 2);
+            if (walk_given_up(&ws))
+#pragma unroll
+                for (int j = 0; j < HC / 2; ++j) S[j] = pair(kLost);
         }
         tmem_wait_st();
         auto flat = [&](float (&s)[HC]) {
@@ -317,11 +336,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
         }
         tmem_fence_before_sync();
     }
-    __syncthreads();
-    if (ws.gave_up && tid == 0) {
-        atomicExch(&hn_delta_backward_status, 1);
-        walk_drain(&ws, C::STAGES);
-    }
+    walk_end(&ws, C::STAGES, &hn_delta_backward_status, warp, 8);
     if (warp == 0) tmem_dealloc(tb, 512);
     pdl_trigger();                                           // (late: see delta.cuh)
 }
@@ -397,6 +412,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
     auto copy_early = [&](const Unit &u) {
         const long long bh = head(u), at = bh * a.chunks + u.chunk;
         const bool copied = by_copy(a, u.nv, u.chunk * kTok);
+        ++ws.begun[2];
         mbar_expect_tx(&ws.full[2], (C::ROOM ? (unsigned)(kept * 4) : 0) + (copied ? C::TILE : 0));
         if (copied) tma_load_3d(sm + C::DY, &maps.v, &ws.full[2], u.chunk * kTok, 0, (int)bh);
         if (C::ROOM) bulk_load(sm + C::STATE, a.marks + at * kept, (unsigned)(kept * 4), &ws.full[2]);
@@ -404,6 +420,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
     auto copy_rest = [&](const Unit &u, int which) {
         const long long bh = head(u), at = bh * a.chunks + u.chunk;
         const bool copied = by_copy(a, u.nv, u.chunk * kTok);
+        ++ws.begun[0];
         mbar_expect_tx(&ws.full[0], PM * kMatrix + kGates * 4 + (C::ROOM ? rows8 * 256 : 0) + (copied ? (u.j ? 1 : 3) * C::TILE : 0));
         if (copied) {
             if (!u.j) tma_load_3d(sm + C::K, &maps.k, &ws.full[0], u.chunk * kTok, 0, (int)u.bk);
@@ -418,8 +435,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
     pdl_wait();
     if (tid == 0) {
         mbar_init(&ws.bar_a, 1); mbar_init(&ws.bar_b, 1); mbar_init(&ws.full[0], 1); mbar_init(&ws.full[1], 1); mbar_init(&ws.full[2], 1);
-        ws.gave_up = 0;
-        fence_mbar_init();
+        walk_marks_init(&ws);
     }
     __syncwarp();
     if (warp == 0) tmem_alloc(smem_u32(&ws.slot), 512);
@@ -538,6 +554,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
             }
             planes8_to_tmem<PM>(lane_s + e / 2, KD / 2, s);
         }
+        walk_late(&ws, is_late(a, LATE_GRADIENTS, bh, now.chunk, LATE_COPIES));
         WAIT(&ws.full[0], phase);
         if (C::ROOM) clear_rows(sm + C::DZ, C::TILE, PM, rows8, KD, tid, kGradThreads);
         go();
@@ -620,6 +637,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
         go();
         if (warp == 0) {
             if (C::ROOM && lane == 0 && !walk_given_up(&ws)) {          // the state has been read: the gradient behind the chunk into its place
+                ++ws.begun[1];
                 mbar_expect_tx(&ws.full[1], (unsigned)(kept * 4));
                 bulk_load(sm + C::STATE, D, (unsigned)(kept * 4), &ws.full[1]);
             }
@@ -646,6 +664,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
         }
         // the gradient behind the chunk in the state's place, while those are formed
         if (C::ROOM) WAIT(&ws.full[1], phase);
+        walk_late(&ws, is_late(a, LATE_GRADIENTS, bh, now.chunk, LATE_PRODUCT));
         WAIT(&ws.bar_b, 0);                                  // (two phases a unit)
         tmem_fence_after_sync();
         float inner = columns(D, true);
@@ -737,6 +756,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
             issue_ss<PI, PM, PM, false, true, kTok / 16, B_LOWER_T>(tb + C::R2, IK, C::TILE, 0, IZ, kMatrix, kTok / 16, kTok, true);            // E k, the other way
             umma_commit(&ws.bar_a);
         }
+        WAIT(&ws.bar_b, 1);                                  // (dS1 u: in front of the next unit's wait for it)
         done();
         if (C::ROOM && more && tid == 0 && !walk_given_up(&ws)) copy_rest(then, phase ^ 1);     // (every product is through, and what the threads read they have)
         __syncwarp();
@@ -754,6 +774,9 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
             if (C::ROOM) bf16_widen8(z, ks[g]);
             else if (row < KD) image8<PI>(z, sm + C::K, C::TILE, row, c >> 3);
             tmem_wait_ld();
+            if (walk_given_up(&ws))
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = y[e] = kLost;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 u[e] *= e & 1 ? de[e / 2].y : de[e / 2].x;
@@ -854,6 +877,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int i = 2 * lane + e;
+                if (walk_given_up(&ws)) s[e] = kLost;
                 if (i >= room) continue;
                 if (warp == 1) { HN_G(a.dbeta + grow + i, 4); a.dbeta[grow + i] = i < nv ? s[e] : 0.f; }
                 else if (a.dg) {
@@ -866,11 +890,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
         }
     }
     tmem_fence_before_sync();
-    __syncthreads();
-    if (ws.gave_up && tid == 0) {
-        atomicExch(&hn_delta_backward_status, 1);
-        walk_drain(&ws, 3);
-    }
+    walk_end(&ws, 3, &hn_delta_backward_status, warp, 0);
     if (warp == 0) tmem_dealloc(tb, 512);
     pdl_trigger();                                           // (late: see delta.cuh)
 }

@@ -410,6 +410,10 @@ def hyenand_delta_device_status() -> int:
     return int(lib().hyenand_delta_device_status())
 
 
+def hyenand_debug_delta_late(kernel: int, chunk: int = 0, wait: int = 0) -> int:
+    return int(lib().hyenand_debug_delta_late(int(kernel), int(chunk), int(wait)))
+
+
 def hyenand_delta_forward(B: int, H: int, Hk: int, L: int, Dk: int, Dv: int, decay: int, dtype: int, q, k, v, g, beta, s0, lengths, y, s_end, marks,
                           workspace, stream=None) -> None:
     _check(lib().hyenand_delta_forward(*_ints((B, H, Hk, L, Dk, Dv, decay, dtype)), q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(g), beta.data_ptr(),
