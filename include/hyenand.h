@@ -326,8 +326,9 @@ int hyenand_debug_recurrence_late(int tile, int warp);
  * aligned, that the backward pass of the same inputs needs.
  * Keys are meant to have a norm of about 1 at most and beta to lie in 0 .. 2 (else the rule itself grows without bound), decays to be at
  * most 1; a decay below exp(-110) is taken as exp(-110), which fp32 cannot hold.  Tokens are taken 64 at a time on the tensor cores;
- * states, sums and decays are fp32, and what enters a product is a sum of bf16 values: exact to 2^-17 for bf16 tensors, to
- * 2^-24 for fp32 ones.  y is rounded once, at its store.  A NaN spreads to its chunk of 64 tokens and everything behind it, an infinity
+ * states, sums and decays are fp32, a state is rounded once for every 64 tokens, and what enters a product is a sum of bf16 values: exact to
+ * 2^-17 for bf16 tensors, to 2^-24 for fp32 ones and for the inverse of a chunk's elimination, which cancels where keys repeat.  y is rounded
+ * once, at its store.  A NaN spreads to its chunk of 64 tokens and everything behind it, an infinity
  * does as NaN.  Results do not depend on timing.
  * workspace: hyenand_delta_workspace_bytes() bytes on the device, 16-byte aligned, whose contents mean nothing before and after; calls
  * that may overlap need one each.

@@ -20,7 +20,7 @@ static __device__ int hn_delta_status;
 // ---- prepare --------------------------------------------------------------------------------------------------------
 
 template <typename T, int KD> struct Prep {
-    static constexpr int PI = Planes<T>::IN, PM = Planes<T>::MID, TILE = KD * 128, PITCH = 2 * TILE, TROW = 68;
+    static constexpr int PI = Planes<T>::IN, PM = Planes<T>::MID, PA = Planes<T>::INVERSE, TILE = KD * 128, PITCH = 2 * TILE, TROW = 68;
     // the tiles of k and q; T and the planes of P take their place
     static constexpr int P = kTok * TROW * 4 + 1024 - kTok * TROW * 4 % 1024, AFTER = P + PM * kMatrix, IMAGES = PI * PITCH > AFTER ? PI * PITCH : AFTER, BYTES = 1024 + IMAGES;
 };
@@ -173,9 +173,9 @@ template <typename T, int KD> __global__ void __launch_bounds__(128) delta_prepa
     fence_async_smem();
     tmem_fence_before_sync();
     __syncthreads();
-    unsigned char *to = a.images + at * (2 * C::PM * kMatrix);
+    unsigned char *to = a.images + at * ((C::PA + C::PM) * kMatrix);
     if (tid == 96) {
-        bulk_store(to + C::PM * kMatrix, sm + C::P, C::PM * kMatrix);
+        bulk_store(to + C::PA * kMatrix, sm + C::P, C::PM * kMatrix);
         tma_commit();
     }
     if (warp == 0) tmem_dealloc(tb, 64);
@@ -213,10 +213,10 @@ template <typename T, int KD> __global__ void __launch_bounds__(128) delta_prepa
         const int r = e >> 3, c = e & 7;
         const float4 u = *(const float4 *)(Ts + r * C::TROW + 8 * c), v = *(const float4 *)(Ts + r * C::TROW + 8 * c + 4);
         const float x[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
-        uint4 w[C::PM];
-        planes8<C::PM>(w, x);
+        uint4 w[C::PA];
+        planes8<C::PA>(w, x);
 #pragma unroll
-        for (int p = 0; p < C::PM; ++p) {
+        for (int p = 0; p < C::PA; ++p) {
             uint4 *o = (uint4 *)(to + p * kMatrix + image_at(r, c));
             HN_G(o, 16);
             *o = w[p];
@@ -230,18 +230,18 @@ template <typename T, int KD> __global__ void __launch_bounds__(128) delta_prepa
 #define WAIT(bar, parity) walk_wait(&ws, bar, parity)
 
 template <typename T, int KD> struct Walk {
-    static constexpr int PI = Planes<T>::IN, PM = Planes<T>::MID, TILE = KD * 128, TENSOR = PI * TILE;
+    static constexpr int PI = Planes<T>::IN, PM = Planes<T>::MID, PA = Planes<T>::INVERSE, TILE = KD * 128, TENSOR = PI * TILE;
     static constexpr bool VALUES = PI == 1;                                   // values and results travel as images
-    static constexpr int IMAGES = 2 * PM * kMatrix, K = 0, Q = TENSOR, A = 2 * TENSOR, V = A + IMAGES, GATES = V + (VALUES ? TILE : 0), STAGE = GATES + 2048;
+    static constexpr int IMAGES = (PA + PM) * kMatrix, K = 0, Q = TENSOR, A = 2 * TENSOR, V = A + IMAGES, GATES = V + (VALUES ? TILE : 0), STAGE = GATES + kWalkGates;
     static constexpr int OUT = VALUES ? 2 * TILE : 0;                         // two images of results
-    static constexpr int STAGES = 3 * STAGE + OUT <= 220 * 1024 ? 3 : 2 * STAGE + OUT <= 220 * 1024 ? 2 : 1;
-    static constexpr int BYTES = 1024 + STAGES * STAGE + OUT;
+    static constexpr int STAGES = 3 * STAGE + OUT <= kWalkBytes ? 3 : 2 * STAGE + OUT <= kWalkBytes ? 2 : 1;
+    static constexpr int BYTES = STAGES * STAGE + OUT;
     // tensor memory: S as an operand | Z, later U, as an operand | S k, then U | S q, then y | what S gains | delta U as an operand
     static constexpr int SCOLS = PM * KD / 2, ZCOLS = PM * kTok / 2, S0 = 0, Z0 = SCOLS, X0 = Z0 + ZCOLS, Y0 = X0 + kTok;
     // (with three planes of 128 columns delta U takes S's place, and the first half of the gain U's)
     static constexpr bool ROOM = Y0 + kTok + KD + ZCOLS <= 512;
     static constexpr int D0 = ROOM ? Y0 + kTok : X0, D1 = ROOM ? D0 + KD / 2 : Y0 + kTok, U0 = ROOM ? D0 + KD : S0;
-    static_assert(ROOM || (D1 + KD / 2 <= 512 && KD / 2 == kTok), "tensor memory");
+    static_assert((ROOM || (D1 + KD / 2 <= 512 && KD / 2 == kTok)) && BYTES <= kWalkBytes, "tensor and shared memory");
 };
 
 // Bound by the chain of a chunk: S k, Z, A Z, the new state, each a product (some 300 to 700 cycles with its issue and its end's way back)
@@ -257,7 +257,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
     constexpr int KERNEL = RUN ? LATE_WALK : LATE_MAPS;
     extern __shared__ __align__(1024) unsigned char raw[];
     __shared__ WalkShared ws;
-    unsigned char *sm = align_images(raw);
+    unsigned char *const sm = raw;
     const int tid = threadIdx.x, lane = tid & 31, warp = uniform_warp(tid >> 5);
     long long id = blockIdx.x;
     const bool phi = !RUN && (id & 1);                       // from the identity, without values
@@ -296,8 +296,8 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             if (begun) {
                 const long long at = bh * a.chunks + c;
                 ++ws.begun[s];
-                const unsigned bytes = RUN ? C::IMAGES : C::IMAGES / 2, tiles = copied ? (RUN ? 2 : 1) * C::TENSOR + (values ? C::TILE : 0) : 0;
-                mbar_expect_tx(&ws.full[s], bytes + kWalkGates + tiles);
+                const unsigned bytes = RUN ? C::IMAGES : C::PA * kMatrix, tiles = copied ? (RUN ? 2 : 1) * C::TENSOR + (values ? C::TILE : 0) : 0;
+                mbar_expect_tx(&ws.full[s], bytes + kWalkGates + 16 + tiles);
                 if (copied) {
                     tma_load_3d(st, &maps.k, &ws.full[s], t0, 0, (int)bk);
                     if (RUN) tma_load_3d(st + C::Q, &maps.q, &ws.full[s], t0, 0, (int)bk);
@@ -305,6 +305,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
                 }
                 bulk_load(st + C::A, a.images + at * C::IMAGES, bytes, &ws.full[s]);
                 bulk_load(st + C::GATES, a.gates + at * kGates, kWalkGates, &ws.full[s]);
+                bulk_load(&ws.carry[s], a.gates + at * kGates + kCarry, 16, &ws.full[s]);
             }
             if (!copied) {
                 load_tile<T>(st, C::TILE, (const T *)a.k, qk + t0, all, a.L, a.Dk, nv, ft, kFetchers);
@@ -321,7 +322,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
         const int steps = (a.Dk + 15) / 16;
         for (int c = first, i = 0; c < last; ++c, ++i) {
             const int s = i % C::STAGES;
-            const unsigned par = i & 1, k = smem_u32(sm) + s * C::STAGE, A = k + C::A, P = A + PM * kMatrix;
+            const unsigned par = i & 1, k = smem_u32(sm) + s * C::STAGE, A = k + C::A, P = A + C::PA * kMatrix;
             walk_late(&ws, is_late(a, KERNEL, bh, c, LATE_COPIES));
             WAIT(&ws.full[s], (i / C::STAGES) & 1);
             // S k, the first half of S's columns as soon as they are there
@@ -340,7 +341,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             }
             WAIT(&ws.z_ready, par);
             tmem_fence_after_sync();
-            issue_ts<PM, PM, PM, false, kTok / 16, B_LOWER>(tb + C::X0, tb + C::Z0, kTok / 2, A, kMatrix, kTok / 16, kTok, false);
+            issue_ts<PM, C::PA, C::PA, false, kTok / 16, B_LOWER>(tb + C::X0, tb + C::Z0, kTok / 2, A, kMatrix, kTok / 16, kTok, false);
             umma_commit(&ws.bar_b);
             WAIT(&ws.u_ready, par);
             tmem_fence_after_sync();
@@ -479,7 +480,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             }
             walk_ready(&ws.z_ready, lane);
             if (mark) keep_state<HC / 16, HC / 8>(mark, S, row, a.Dv, half * HC, a.Dk);
-            const Carry carry((const float *)(st + C::GATES));
+            const Carry carry(&ws.carry[s].x);
             walk_late(&ws, is_late(a, KERNEL, bh, c, LATE_PRODUCT));
             WAIT(&ws.bar_b, par);
             tmem_fence_after_sync();
@@ -684,7 +685,7 @@ DeltaSizes delta_sizes(const DeltaArgs &a, int dtype, bool backward)
 {
     const size_t bh = (size_t)a.B * a.H, chunks = bh * a.chunks, planes = dtype == HYENAND_F32 ? Planes<float>::MID : Planes<bf16>::MID;
     DeltaSizes s{};
-    s.images = chunks * 2 * planes * kMatrix;
+    s.images = chunks * (Planes<bf16>::INVERSE + planes) * kMatrix;
     s.gates = up(chunks * kGates * 4);
     if (a.segments > 1) {
         s.maps = up(bh * a.segments * ((size_t)a.Dv + a.Dk) * map_pitch(a.Dk) * 4);

@@ -19,7 +19,10 @@
 // The products run on the tensor cores in bf16 with fp32 sums.  A number that is no bf16 value goes in as a sum of bf16 values ("planes"):
 // two for bf16 tensors (16 bits, errors of 2^-17: states and sums are fp32 and a result is rounded once, so these errors stay far
 // below a bf16 result's own), three for fp32 tensors (24 bits).  Tensors of bf16 are one plane as they are.  A product of planes
-// p and q is formed where p + q is below the number of planes.
+// p and q is formed where p + q is below the number of planes.  A has three planes always: with keys that repeat its entries are as large
+// as beta and the same along its diagonals, their roundings too, and what is summed of A Z over a chunk cancels (512 tokens with one key at
+// beta = 2: with two planes a state was off by 1.8e-2, with three by 1.8e-4, 7e-5 from fp32 tensors.  Two products more on the chain:
+// a walk of 64 chunks 236 -> 241 us, back 255 -> 263).
 #pragma once
 #include "entry.cuh"
 #include "octet.cuh"
@@ -31,12 +34,12 @@ namespace hn {
 constexpr int kTok = 64;                                  // tokens of a chunk
 enum { DELTA_LOG = HYENAND_DECAY_LOG, DELTA_SIGMOID = HYENAND_DECAY_SIGMOID, DELTA_NONE = HYENAND_DECAY_NONE };
 
-template <typename T> struct Planes { static constexpr int IN = 1, MID = 2; };
-template <> struct Planes<float> { static constexpr int IN = 3, MID = 3; };
+template <typename T> struct Planes { static constexpr int IN = 1, MID = 2, INVERSE = 3; };
+template <> struct Planes<float> { static constexpr int IN = 3, MID = 3, INVERSE = 3; };
 constexpr int kMatrix = kTok * 128;                       // bytes of one plane of a 64 x 64 matrix
 // floats of a chunk: gamma, delta, beta, -beta gamma, what carries the state (see Carry), and G in two parts (see ratio)
 constexpr int kGates = 6 * kTok + 4, kCarry = 4 * kTok, kSums = kCarry + 4;
-constexpr int kWalkGates = kSums * 4;                     // bytes in front of the sums
+constexpr int kWalkGates = kCarry * 4;                    // bytes of the first four
 
 struct DeltaArgs {
     const void *q, *k, *v;
@@ -178,7 +181,7 @@ struct Sixteen {
 // 7e-5.  Below a half there is nothing to lose: 0 S + gamma_64 S.
 struct Carry {
     f2 keep, by;
-    __device__ __forceinline__ explicit Carry(const float *gates) { const float2 c = *(const float2 *)(gates + kCarry); keep = pair(c.x); by = pair(c.y); }
+    __device__ __forceinline__ explicit Carry(const float *two) { const float2 c = *(const float2 *)two; keep = pair(c.x); by = pair(c.y); }
 };
 // S = gamma_64 S + gain (this thread's columns of both, eight pairs at a time, the next loads under way), and S as an operand again
 template <int PM, int C> __device__ __forceinline__ void state_onwards(f2 (&S)[C], const Carry &carry, unsigned gain, unsigned planes, int pitch)
@@ -565,6 +568,7 @@ struct WalkShared {
     uint64_t full[4], empty[4], bar_a, bar_b, bar_c[2], bar_q, bar_y, bar_end; // copies; products; all of them
     uint64_t state[2], z_ready, u_ready, p_ready;             // the computing warps (of a half) to the one that issues
     uint64_t o_ready, o_taken;                                // the warps with the results to the one that issues
+    float4 carry[4];                                          // of a stage's chunk (see Carry)
     unsigned slot;
     int gave_up, begun[4];                                    // begun: how often copies to a stage were begun
 };
@@ -637,6 +641,10 @@ __device__ __forceinline__ void takers_sync() { asm volatile("bar.sync 2, 128;\n
 __device__ __forceinline__ unsigned char *align_images(unsigned char *p) { return p + ((1024u - (smem_u32(p) & 1023u)) & 1023u); }
 
 enum { WALK_RUN = 0, WALK_MAPS = 1 };
+// A walk takes up to all the shared memory that a CTA can have, its images from the first byte of the dynamic part on, which starts on 1024
+// bytes: it is declared so, and the static part, below that, is padded to it.
+constexpr int kWalkStatic = 1024, kWalkBytes = 227 * 1024 - kWalkStatic;
+static_assert(sizeof(WalkShared) <= kWalkStatic, "shared memory");
 
 // ---- tensor copies -----------------------------------------------------------------------------------------------------
 

@@ -17,19 +17,19 @@ static __device__ int hn_delta_backward_status;
 // ---- walk -----------------------------------------------------------------------------------------------------------
 
 template <typename T, int KD> struct WalkBack {
-    static constexpr int PI = Planes<T>::IN, PM = Planes<T>::MID, TILE = KD * 128, TENSOR = PI * TILE;
+    static constexpr int PI = Planes<T>::IN, PM = Planes<T>::MID, PA = Planes<T>::INVERSE, TILE = KD * 128, TENSOR = PI * TILE;
     static constexpr bool VALUES = PI == 1;                                   // dV and dZ's two planes travel as images
-    static constexpr int IMAGES = 2 * PM * kMatrix, K = 0, Q = TENSOR, DY = 2 * TENSOR, A = 3 * TENSOR, GATES = A + IMAGES, STAGE = GATES + 2048;
+    static constexpr int IMAGES = (PA + PM) * kMatrix, K = 0, Q = TENSOR, DY = 2 * TENSOR, A = 3 * TENSOR, GATES = A + IMAGES, STAGE = GATES + kWalkGates;
     static constexpr int OUT = VALUES ? 3 * TILE : 0;
     // (the product of dY and P takes 128 rows of dY's image: with 64 it reads on into the images that follow, for rows nothing looks at)
-    static constexpr int STAGES = 3 * STAGE + OUT <= 220 * 1024 ? 3 : 2 * STAGE + OUT <= 220 * 1024 ? 2 : 1;
-    static constexpr int BYTES = 1024 + STAGES * STAGE + OUT;
+    static constexpr int STAGES = 3 * STAGE + OUT <= kWalkBytes ? 3 : 2 * STAGE + OUT <= kWalkBytes ? 2 : 1;
+    static constexpr int BYTES = STAGES * STAGE + OUT;
     // tensor memory: dS as an operand | dU, later -beta gamma dZ, as an operand | dS k, then dZ | P^T dY | what dS gains | gamma dY as an operand
     static constexpr int SCOLS = PM * KD / 2, ZCOLS = PM * kTok / 2, S0 = 0, Z0 = SCOLS, X0 = Z0 + ZCOLS, Y0 = X0 + kTok;
     // (with three planes of 128 columns gamma dY takes dS's place, and the first half of the gain dZ's)
     static constexpr bool ROOM = Y0 + kTok + KD + ZCOLS <= 512;
     static constexpr int D0 = ROOM ? Y0 + kTok : X0, D1 = ROOM ? D0 + KD / 2 : Y0 + kTok, G0 = ROOM ? D0 + KD : S0;
-    static_assert((ROOM || (D1 + KD / 2 <= 512 && KD / 2 == kTok)) && BYTES + 1024 <= 227 * 1024, "tensor and shared memory");
+    static_assert((ROOM || (D1 + KD / 2 <= 512 && KD / 2 == kTok)) && BYTES <= kWalkBytes, "tensor and shared memory");
 };
 
 // As the forward walk, bound by its chain: 252 us for 96 heads of 4096 tokens of 128 channels, 3.9 us a chunk.  dZ leaves as the two planes that
@@ -43,7 +43,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
     constexpr int KERNEL = RUN ? LATE_BACK : LATE_BACK_MAPS;
     extern __shared__ __align__(1024) unsigned char raw[];
     __shared__ WalkShared ws;
-    unsigned char *sm = align_images(raw);
+    unsigned char *const sm = raw;
     const int tid = threadIdx.x, lane = tid & 31, warp = uniform_warp(tid >> 5);
     long long id = blockIdx.x;
     const bool phi = !RUN && (id & 1);                       // from the identity, without dY
@@ -83,7 +83,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             if (begun) {
                 const long long at = bh * a.chunks + c;
                 ++ws.begun[s];
-                mbar_expect_tx(&ws.full[s], C::IMAGES + kWalkGates + (copied ? (phi ? 2 : 3) * C::TENSOR : 0));
+                mbar_expect_tx(&ws.full[s], C::IMAGES + kWalkGates + 16 + (copied ? (phi ? 2 : 3) * C::TENSOR : 0));
                 if (copied) {
                     tma_load_3d(st, &maps.k, &ws.full[s], t0, 0, (int)bk);
                     tma_load_3d(st + C::Q, &maps.q, &ws.full[s], t0, 0, (int)bk);
@@ -91,6 +91,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
                 }
                 bulk_load(st + C::A, a.images + at * C::IMAGES, C::IMAGES, &ws.full[s]);
                 bulk_load(st + C::GATES, a.gates + at * kGates, kWalkGates, &ws.full[s]);
+                bulk_load(&ws.carry[s], a.gates + at * kGates + kCarry, 16, &ws.full[s]);
             }
             if (!copied) {
                 load_tile<T>(st, C::TILE, (const T *)a.k, qk + t0, all, a.L, a.Dk, nv, ft, kFetchers);
@@ -106,7 +107,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
         const int steps = (a.Dk + 15) / 16;
         for (int i = 0; i < count; ++i) {
             const int s = i % C::STAGES;
-            const unsigned par = i & 1, k = smem_u32(sm) + s * C::STAGE, q = k + C::Q, A = k + C::A, P = A + PM * kMatrix;
+            const unsigned par = i & 1, k = smem_u32(sm) + s * C::STAGE, q = k + C::Q, A = k + C::A, P = A + C::PA * kMatrix;
             // what half h of dS's columns gains from an operand in tensor memory and an image of Dk rows
             auto gain = [&](int h, unsigned from, unsigned image, bool add) {
                 issue_ts<PM, PI, PM, false, kTok / 16>(tb + (h ? C::D1 : C::D0), from, kTok / 2, image + h * (KD / 2) * 128, C::TILE, kTok / 16, KD / 2, add);
@@ -131,7 +132,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             }
             WAIT(&ws.z_ready, par);                          // dU
             tmem_fence_after_sync();
-            issue_ts<PM, PM, PM, true, kTok / 16, B_LOWER_T>(tb + C::X0, tb + C::Z0, kTok / 2, A, kMatrix, kTok / 16, kTok, false);
+            issue_ts<PM, C::PA, C::PA, true, kTok / 16, B_LOWER_T>(tb + C::X0, tb + C::Z0, kTok / 2, A, kMatrix, kTok / 16, kTok, false);
             umma_commit(&ws.bar_b);
             WAIT(&ws.u_ready, par);                          // -beta gamma dZ (without the room, gamma dY too)
             tmem_fence_after_sync();
@@ -294,7 +295,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
             }
             walk_ready(&ws.z_ready, lane);
             if (RUN) keep_state<HC / 16, HC / 8>(keep, S, row, a.Dv, half * HC, a.Dk);
-            const Carry carry((const float *)(sm + s * C::STAGE + C::GATES));
+            const Carry carry(&ws.carry[s].x);
             walk_late(&ws, is_late(a, KERNEL, bh, c, LATE_PRODUCT));
             WAIT(&ws.bar_b, par);
             tmem_fence_after_sync();
@@ -344,11 +345,11 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
 // ---- gradients ------------------------------------------------------------------------------------------------------
 
 template <typename T, int KD> struct Grads {
-    static constexpr int PI = Planes<T>::IN, PM = Planes<T>::MID, TILE = KD * 128;
+    static constexpr int PI = Planes<T>::IN, PM = Planes<T>::MID, PA = Planes<T>::INVERSE, TILE = KD * 128;
     // images: dY | Q | K | U (values before it, dK in its second half behind it) | dZ (later E) | A (later F) | dQ, and a state as it is kept.
     // With three planes there is no room for the last two, and Q comes into dY's place once that is through.
     static constexpr bool ROOM = PI == 1;
-    static constexpr int DY = 0, K = (ROOM ? 2 : 1) * PI * TILE, Q = ROOM ? PI * TILE : DY, U = (ROOM ? 3 : 2) * PI * TILE, DZ = U + PM * TILE, A = DZ + PM * TILE, OUT = A + PM * kMatrix,
+    static constexpr int DY = 0, K = (ROOM ? 2 : 1) * PI * TILE, Q = ROOM ? PI * TILE : DY, U = (ROOM ? 3 : 2) * PI * TILE, DZ = U + PM * TILE, A = DZ + PM * TILE, OUT = A + PA * kMatrix,
                          STATE = OUT + (ROOM ? TILE : 0), BYTES = 1024 + STATE + (ROOM ? KD * KD * 4 : 0);
     // tensor memory: a state as an operand | sums of 64 columns:
     //     0: S0 k, U, the rest of dZ U^T   1: Z (and the next), dY U^T and dZ U^T   2: Q K^T and K K^T, the written part of dK but for dS1 u
@@ -421,14 +422,14 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
         const long long bh = head(u), at = bh * a.chunks + u.chunk;
         const bool copied = by_copy(a, u.nv, u.chunk * kTok);
         ++ws.begun[0];
-        mbar_expect_tx(&ws.full[0], PM * kMatrix + kGates * 4 + (C::ROOM ? rows8 * 256 : 0) + (copied ? (u.j ? 1 : 3) * C::TILE : 0));
+        mbar_expect_tx(&ws.full[0], C::PA * kMatrix + kGates * 4 + (C::ROOM ? rows8 * 256 : 0) + (copied ? (u.j ? 1 : 3) * C::TILE : 0));
         if (copied) {
             if (!u.j) tma_load_3d(sm + C::K, &maps.k, &ws.full[0], u.chunk * kTok, 0, (int)u.bk);
             tma_load_3d(sm + C::U, &maps.more, &ws.full[0], u.chunk * kTok, 0, (int)bh);
             if (!u.j) tma_load_3d(sm + C::Q, &maps.q, &ws.full[0], u.chunk * kTok, 0, (int)u.bk);
         }
         bulk_load(gates2[which], a.gates + at * kGates, kGates * 4, &ws.full[0]);
-        bulk_load(sm + C::A, a.images + at * (2 * PM * kMatrix), PM * kMatrix, &ws.full[0]);
+        bulk_load(sm + C::A, a.images + at * ((C::PA + PM) * kMatrix), C::PA * kMatrix, &ws.full[0]);
         if (C::ROOM)
             for (int p = 0; p < 2; ++p) bulk_load(sm + C::DZ + p * C::TILE, (const unsigned char *)a.dz + (at * 2 + p) * rows8 * 128, rows8 * 128, &ws.full[0]);
     };
@@ -592,7 +593,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
         }
         go();
         if (warp == 0) {
-            issue_ts<PM, PM, PM, false, kTok / 16, B_LOWER>(tb + C::R0, tb + C::R1, kTok / 2, IA, kMatrix, kTok / 16, kTok, false);
+            issue_ts<PM, C::PA, C::PA, false, kTok / 16, B_LOWER>(tb + C::R0, tb + C::R1, kTok / 2, IA, kMatrix, kTok / 16, kTok, false);
             umma_commit(&ws.bar_a);
         }
         // a state with its columns as lanes; `with`: the sum of its products with the one that is there
@@ -700,7 +701,7 @@ template <typename T, int KD> __global__ void __launch_bounds__(kGradThreads, 1)
                 shared8(lj, glo + c);
                 tmem_wait_ld();
                 if (!C::ROOM && !(warp & 2)) {               // Q K^T with its ratios: P
-                    const unsigned char *P = a.images + at * (2 * PM * kMatrix) + PM * kMatrix;
+                    const unsigned char *P = a.images + at * ((C::PA + PM) * kMatrix) + C::PA * kMatrix;
                     for (int q = 0; q < PM; ++q) HN_G(P + q * kMatrix + image_at(i, c >> 3), 16);
                     image8<PM>(y, P, kMatrix, i, c >> 3);
                 }
