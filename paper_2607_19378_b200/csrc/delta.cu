@@ -58,7 +58,7 @@ template <int N, int THREADS, bool FIRST> __device__ __forceinline__ void merge(
     __syncthreads();
 }
 
-// Read: a chunk's k and q; written: 16 KB of planes for each of A and P (bf16).  6144 chunks of 128 channels: 112 us, 0.3 GB, 2.7 TB/s.  It is
+// Read: a chunk's k and q; written: 24 KB of planes of A and 16 of P (bf16).  6144 chunks of 128 channels: 117 us, 0.41 GB, 3.5 TB/s.  It is
 // bound by the latency of its steps one after the other (copy, product, inverse, stores), which the few CTAs that an SM holds only partly
 // cover.  The inverse by blocks in place of 64 dependent steps took a batch of prompts, 192 heads of 64, from 319 to 230 us in all.
 template <typename T, int KD> __global__ void __launch_bounds__(128) delta_prepare_kernel(DeltaArgs a, const __grid_constant__ DeltaMaps maps)
@@ -245,9 +245,9 @@ template <typename T, int KD> struct Walk {
 };
 
 // Bound by the chain of a chunk: S k, Z, A Z, the new state, each a product (some 300 to 700 cycles with its issue and its end's way back)
-// and a passage through registers (350 to 1300).  3.6 us a chunk of 128 channels with all SMs at work (96 heads of 4096 tokens: 232 us), whatever
+// and a passage through registers (350 to 1300).  3.8 us a chunk of 128 channels (96 heads of 4096 tokens: 241 us), whatever
 // the bytes: 0.5 GB, 2.3 TB/s.  What shortened it: y, its scaling and its stores on other warps (off the chain), the fp32 state in registers,
-// the columns of S in two halves so that S k begins with the first, kept states stored in thirds while products run (265 -> 242), values read
+// the columns of S in two halves so that S k begins with the first, kept states stored in three parts (a quarter, a quarter, a half) while products run (265 -> 242), values read
 // before the product they meet (242 -> 232).  Prefetches into L2 and more stages made it slower, as did anything that grew the code.
 template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkThreads, 1) delta_walk_kernel(DeltaArgs a, const __grid_constant__ DeltaMaps maps)
 {
@@ -535,7 +535,7 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
 
 // States at the segments' starts from the maps S -> S Phi + N: eight rows to a CTA, Phi by bulk copies, the next one under way; a thread
 // sums four columns of all rows over an eighth of Phi's rows.  `reverse`: from the last segment to the first (the gradient's states).
-// Serial over the segments: 37 of 128 channels take 53 us, 1.4 us each, for 64 KB that every CTA reads from L2 and 128 x 128 x 8 fp32 products.
+// Serial over the segments: 37 of 128 channels take 56 us, 1.5 us each, for 64 KB that every CTA reads from L2 and 128 x 128 x 8 fp32 products.
 constexpr int kJoinRows = 8, kJoinBytes = 2 * 128 * 128 * 4;
 __global__ void __launch_bounds__(256) delta_join_kernel(DeltaArgs a, const float *from, int reverse)
 {
@@ -749,7 +749,10 @@ template <typename T> static int launch_step(const DeltaArgs &a, cudaStream_t st
 }
 
 // Segments of a head.  They cost three walks in place of one (two CTAs for the maps), so they pay where each SM would otherwise have a
-// quarter of a head or less.
+// quarter of a head or less, and from some length on.  Scans with one walk and with segments, us: 37 heads of 128 channels (four segments)
+// of 128 chunks 441 and 397, of 64 channels 408 and 324, fp32 2373 and 1472; 48 heads (three) 462 and 499, 434 and 412, 2448 and 1937; 60 (two)
+// 497 and 647, 445 and 535, 2533 and 2731; 8 heads of 16 chunks 70 and 61, 55 and 45, 212 and 120, of 8 chunks 49 and 57, 38 and 42, 122 and 111.
+// The worst of the rule: 37 heads of 16 chunks 78 and 110, 67 and 75, 300 and 233.  Training steps have the same borders.
 static int segments_of(long long heads, int chunks)
 {
     const long long n = kSms / heads;

@@ -675,8 +675,9 @@ int launch_delta_join(const DeltaArgs &a, const float *from, bool backward, cuda
 int launch_delta_backward(const DeltaArgs &a, int dtype, cudaStream_t st);
 int delta_backward_status();
 
-// The kernels that hold tensor memory let the next one in at their end.  Right behind the allocation, CTAs of the next came to the SMs that a walk
-// of 96 heads leaves free and to no others (a training step on 6144 chunks 1312 us, so 1260).
+// The walks and the gradients let the next kernel in at their end, prepare once its tensor memory is free, in front of the inverse.  Right
+// behind the allocation, CTAs of the next came to the SMs that a walk of 96 heads leaves free and to no others (a training step on 6144 chunks
+// 1312 us, so 1260).
 template <auto FN, typename... M> static int launch_delta(const DeltaArgs &a, long long blocks, unsigned threads, int bytes, cudaStream_t st, const M &...maps)
 {
     if (blocks > 0x7fffffffll) return kTooLarge;

@@ -32,8 +32,8 @@ template <typename T, int KD> struct WalkBack {
     static_assert((ROOM || (D1 + KD / 2 <= 512 && KD / 2 == kTok)) && BYTES <= kWalkBytes, "tensor and shared memory");
 };
 
-// As the forward walk, bound by its chain: 252 us for 96 heads of 4096 tokens of 128 channels, 3.9 us a chunk.  dZ leaves as the two planes that
-// the gradients take, by copies out of shared memory (stored from registers in that order, 16 bytes a line, 281 us; in fp32 252 us, but
+// As the forward walk, bound by its chain: 262 us for 96 heads of 4096 tokens of 128 channels, 4.1 us a chunk.  dZ leaves as the two planes that
+// the gradients take, by copies out of shared memory (where that took 252 us, stored from registers in that order, 16 bytes a line, 281; in fp32 252, but
 // the gradients then paid 45 us for turning it).
 template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkThreads, 1) delta_walk_back_kernel(DeltaArgs a, const __grid_constant__ DeltaMaps maps)
 {
@@ -378,7 +378,7 @@ __device__ __forceinline__ float column_sum8(float (&x)[8], int lane)
 
 // 512 threads: a lane's columns in four quarters of 16 tokens (KD / 4 of a state), taken eight at a time: the loops stay rolled, as code that
 // runs once per CTA is bound by its fetching (unrolled over 32 columns, 256 threads: 1350 us on 6144 chunks of 128 channels).
-// 525 us on those, 12.6 us a chunk: 1.7 GB, of which the kept states and gradients in fp32 are 0.8, so 3.2 TB/s, and some 150 products of 34
+// 563 us on those, 13.6 us a chunk: 1.76 GB, of which the kept states and gradients in fp32 are 0.8, so 3.1 TB/s, and some 160 products of 34
 // cycles, a fifth of the time.  What is left is the order of its six steps, each a write, a barrier, products, a reading.  The next chunk's
 // copies go out as soon as their places are free (588 -> 525).  A warp of its own for the products made it slower (645 us: 17 warps leave a
 // thread 96 registers, and the others run apart, through more code at a time).

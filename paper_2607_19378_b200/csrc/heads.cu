@@ -203,7 +203,8 @@ template <typename T, bool VEC> __device__ __forceinline__ void fill_table(const
 // than 32 channels: what a unit costs beside its elements (shuffles, the meeting, rho) is then shared by more of them (the vision grid
 // forward 131 -> 91 us, 262144 tokens of 128 channels each way 393 + 535 -> 252 + 476; of one pair 267 us and more).  With four pairs
 // there are one or two CTAs to an SM, too few loads on their way: the next unit's rows come by asynchronous copies meanwhile, each thread's
-// into places of its own (91 -> 75 us, 5.4 TB/s; 252 + 464 -> 210 + 375 us, 5.1 and 4.3 TB/s; fetched into L2 alone 79, 220 + 403).  With two
+// into places of its own (91 -> 75 us, 5.4 TB/s; 252 + 464 -> 210 + 375 us; fetched into L2 alone 79, 220 + 403; since sums beyond fp32 are looked
+// for 208 + 388, 5.2 and 4.1 TB/s).  With two
 // pairs there are enough loads as it is (fetches into L2: 250 + 356 -> 275 + 460 us); heads of more than 128 channels have no room beside
 // the table.
 constexpr int resident(int pairs, bool backward) { return pairs > 2 ? (backward ? 1 : 2) : backward ? 2 : 3; }          // CTAs an SM, by registers
