@@ -69,9 +69,9 @@ struct DbgScope {
 #endif
 };
 
-// The tensors of one call.  Inputs may overlap one another, an output may overlap nothing else (`with`: the name of the one input it may be
-// the same buffer as, where every element is read before the thread that replaces it does so; another input in that buffer is still
-// one that the call reads).
+// The tensors of one call.  Inputs may overlap one another, an output may overlap nothing else (`with`: the input it may be the same buffer as,
+// because every element is read before the thread that replaces it does so, and behind it, after blanks, other inputs of that size of
+// which the same is true; any other input in that buffer is still one that the call reads).
 struct CallTensors {
     struct One { const void *ptr; size_t bytes; const char *name; int align; bool out; const char *with; };
     One t[24];
@@ -81,6 +81,21 @@ struct CallTensors {
     {
         if (ptr && bytes) t[n++] = {ptr, bytes, name, align, true, with};
     }
+    // whether `o` is an output in place of its first input, and input j one of those in that buffer
+    bool in_place(const One &o, const One &j) const
+    {
+        if (!o.with || j.out || j.ptr != o.ptr || j.bytes != o.bytes) return false;
+        const size_t first = strcspn(o.with, " ");
+        bool over = false, named = false;
+        for (int i = 0; i < n; ++i)
+            over = over || (!t[i].out && t[i].ptr == o.ptr && t[i].bytes == o.bytes && strlen(t[i].name) == first && !strncmp(t[i].name, o.with, first));
+        for (const char *p = o.with; *p; p += strspn(p, " ")) {
+            const size_t len = strcspn(p, " ");
+            named = named || (strlen(j.name) == len && !strncmp(j.name, p, len));
+            p += len;
+        }
+        return over && named;
+    }
     int check() const
     {
         for (int i = 0; i < n; ++i)
@@ -88,9 +103,8 @@ struct CallTensors {
         for (int i = 0; i < n; ++i)
             for (int j = 0; j < n; ++j) {
                 if (i == j || !t[i].out) continue;
-                if (!t[j].out && t[i].with && !strcmp(t[i].with, t[j].name) && t[j].ptr == t[i].ptr && t[j].bytes == t[i].bytes) continue;
                 const char *a = (const char *)t[i].ptr, *b = (const char *)t[j].ptr;
-                if (a < b + t[j].bytes && b < a + t[i].bytes) return fail(HYENAND_ERR_INVALID_ARG, "%s overlaps %s", t[i].name, t[j].name);
+                if (a < b + t[j].bytes && b < a + t[i].bytes && !in_place(t[i], t[j])) return fail(HYENAND_ERR_INVALID_ARG, "%s overlaps %s", t[i].name, t[j].name);
             }
         return HYENAND_OK;
     }

@@ -873,7 +873,7 @@ extern "C" int hyenand_recurrence_forward(int B, int C, int L, int decay, int dt
     const size_t nb = (size_t)a.n * elsize(dtype), rb = (size_t)a.rows * sizeof(float);
     c.in("q", q, nb); c.in("k", k, nb); c.in("v", v, nb); c.in("g", g, nb);
     c.in("s0", s0, rb, 4); c.in("lengths", lengths, (size_t)B * sizeof(int), 4);
-    c.out("y", y, nb); c.out("s_end", s_end, rb, 4, "s0"); c.out("marks", marks, rb * a.marks_row, 4);
+    c.out("y", y, nb); c.out("s_end", s_end, rb, 4, "s0 q k v g"); c.out("marks", marks, rb * a.marks_row, 4);
     if (a.segments > 1) c.out("workspace", workspace, (size_t)a.rows * a.segments * sizeof(float4));
     if (int e = c.check()) return e;
     c.register_ranges();
@@ -898,7 +898,7 @@ extern "C" int hyenand_recurrence_backward(int B, int C, int L, int decay, int d
     const size_t nb = (size_t)a.n * elsize(dtype), rb = (size_t)a.rows * sizeof(float);
     c.in("q", q, nb); c.in("k", k, nb); c.in("v", v, nb); c.in("g", g, nb); c.in("dy", dy, nb);
     c.in("lengths", lengths, (size_t)B * sizeof(int), 4); c.in("marks", marks, rb * a.marks_row, 4); c.in("ds_end", ds_end, rb, 4);
-    c.out("dq", dq, nb); c.out("dk", dk, nb); c.out("dv", dv, nb); c.out("dg", dg, nb); c.out("ds0", ds0, rb, 4, "ds_end");
+    c.out("dq", dq, nb); c.out("dk", dk, nb); c.out("dv", dv, nb); c.out("dg", dg, nb); c.out("ds0", ds0, rb, 4, "ds_end q k v g dy marks");
     if (a.segments > 1) c.out("workspace", workspace, (size_t)a.rows * a.segments * sizeof(float4));
     if (int e = c.check()) return e;
     c.register_ranges();
@@ -919,7 +919,7 @@ extern "C" int hyenand_recurrence_step(int B, int C, int decay, int dtype, const
     const size_t nb = (size_t)a.n * elsize(dtype), rb = (size_t)a.rows * sizeof(float);
     c.in("q", q, nb); c.in("k", k, nb); c.in("v", v, nb); c.in("g", g, nb);
     c.in("state", state, rb, 4); c.in("active", active, (size_t)B * sizeof(int), 4);
-    c.out("y", y, nb); c.out("new_state", new_state, rb, 4, "state");
+    c.out("y", y, nb); c.out("new_state", new_state, rb, 4, "state q k v g");          // (an element a thread)
     if (int e = c.check()) return e;
     c.register_ranges();
     return finish(launch_step(a, decay, dtype, (cudaStream_t)cuda_stream));

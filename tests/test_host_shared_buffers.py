@@ -45,4 +45,9 @@ def test_states(hn):
     # keys of 16 tokens of one entry, fp32, as a state of 16 x 16
     refused(hn, L.hyenand_delta_forward(2, 1, 1, 16, 16, 16, 1, 0, A[0], A[5], *A[2:5], A[5], None, A[7], A[5], None, A[9], None), "s_end overlaps k")
     refused(hn, L.hyenand_delta_step(2, 1, 1, 16, 1, 1, 0, A[0], A[5], *A[2:5], A[5], None, A[7], A[5], None), "new_state overlaps k")
-    refused(hn, L.hyenand_recurrence_step(2, 3, 1, 0, *A[:3], A[5], A[5], None, A[7], A[5], None), "new_state overlaps g")
+    # a recurrence's states in place of another input than the states (of one token; over states and other inputs in one buffer, element by
+    # element, test_gpu_operators_memory.py has it)
+    refused(hn, L.hyenand_recurrence_step(2, 3, 1, 0, A[0], A[5], *A[2:5], None, A[7], A[5], None), "new_state overlaps k")
+    refused(hn, L.hyenand_recurrence_forward(2, 3, 1, 1, 0, A[5], *A[1:4], None, None, A[7], A[5], None, None, None), "s_end overlaps q")
+    # dropout's key of 16 bytes as its four numbers
+    refused(hn, L.hyenand_dropout(4, 0, A[0], 0.5, A[0], 0, A[0], None), "y overlaps rng")
