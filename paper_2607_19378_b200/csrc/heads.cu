@@ -502,7 +502,7 @@ template <typename T, int R, int P, bool BWD, bool VEC> __global__ void __launch
                         get(meet[turn][0], s1);
                         if constexpr (BWD) get(meet[turn][SUMS - 1], s2);
                         turn ^= 1;
-                    }
+                    } else asm volatile("" ::: "memory");          // (nothing further down is begun above: a quarter of the spills)
                     f2 all = pair(0.f);                            // finite where all are
 #pragma unroll
                     for (int e = 0; e < N; ++e) {
