@@ -269,7 +269,10 @@ template <typename T, int KD, int MODE> __global__ void __launch_bounds__(kWalkT
     int last = (n + kTok - 1) / kTok;                        // chunks first .. last - 1 hold tokens
     last = last < end ? last : end;
     if (warp == 0) tmem_alloc(smem_u32(&ws.slot), 512);
-    if (tid == 0) walk_init(&ws, C::STAGES);
+    if (tid == 0) {
+        walk_init(&ws, C::STAGES);
+        walk_late(&ws, smem_u32(raw) & 1023u);               // (images that start elsewhere would be read wrongly: see kWalkBytes)
+    }
     for (int s = 0; s < C::STAGES; ++s) {
         clear_rows(sm + s * C::STAGE, C::TILE, 2 * PI, a.Dk, KD, tid, kWalkThreads);
         if (C::VALUES) clear_rows(sm + s * C::STAGE + C::V, C::TILE, 1, phi ? 0 : a.Dv, KD, tid, kWalkThreads);
