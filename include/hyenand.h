@@ -383,7 +383,8 @@ int hyenand_heads_forward(int ndim, const int *dims, int B, int Hq, int Hk, int 
                           const void *q, const void *k, const float *g_q, const float *g_k, const int *positions, void *q_out, void *k_out,
                           void *cuda_stream);
 /* The gradient: dq_out, dk_out in, dq, dk (dq may be the buffer dq_out, dk the buffer dk_out, where those are two) and the sums over all tokens dg_q, dg_k (D fp32
- * each, or NULL) out; the forward's inputs are read again.  workspace: hyenand_heads_workspace_bytes() bytes on the device, 16-byte
+ * each, or NULL) out; the forward's inputs are read again.  Products of dq_out and q, dk_out and k are formed in fp32 and
+ * have to fit there.  workspace: hyenand_heads_workspace_bytes() bytes on the device, 16-byte
  * aligned, where dg_q or dg_k is given; calls that may overlap need one each.  The order of the sums does not depend on timing. */
 int hyenand_heads_backward(int ndim, const int *dims, int B, int Hq, int Hk, int D, int dtype, int norm, const int *axes, double base, float eps,
                            const void *q, const void *k, const float *g_q, const float *g_k, const int *positions, const void *dq_out,
